@@ -307,6 +307,117 @@ vcs_status vcs_attn_fwd_reuse(const void* q, const void* k, const void* v, const
                               size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Rotary positions with several axes.  The paper's path applies none; these
+ * calls give a policy that uses them its positions and rotates the rows on
+ * their way between trajectory and segment layout.  Positions start over in
+ * every stream, so a trajectory token has other positions in every segment
+ * that copies it.
+ *
+ * vcs_stream_positions: three positions (time, height, width) of every
+ * segment token.  Along a segment a position p starts at 0; a text token has
+ * (p, p, p) and moves p by 1; a screenshot of a grid of T x H x W tokens
+ * (frames, rows, columns) gives its token k the positions
+ * (p + k / (H W), p + k / W mod H, p + k mod W) and moves p by max(T, H, W).
+ *   cu_seqlens, tok_src_step  from vcs_build_segments (device); within a
+ *               segment a step's tokens are consecutive: all of them, or its
+ *               response alone
+ *   step_img, step_txt  int32 [num_steps] device, as for vcs_build_segments
+ *   step_grid   int32 [num_steps, 3] device: T, H, W of each step's
+ *               screenshot, T H W = step_img (not read for steps whose
+ *               screenshot no segment holds)
+ *   pos         int32 [3, num_tokens] device (written)
+ *   dev_status  int32 device-visible word, zeroed by the caller, or NULL:
+ *               VCS_ERR_DEVICE_CHECK for inconsistent cu_seqlens (that
+ *               segment is skipped), a source step outside [0, num_steps) or
+ *               out of order (skipped), a run of tokens that is neither all of
+ *               its step nor its response, or a grid that does not hold the
+ *               screenshot (its tokens are counted like text)
+ * Returns VCS_ERR_INVALID_ARG for negative counts or null pointers,
+ * VCS_ERR_OVERFLOW for counts above INT32_MAX.
+ *
+ * vcs_rope: how a row is rotated.  Pair i < rot_dim / 2 of a head is turned by
+ * the angle inv_freq[i] * (position on axis pair_axis[i]); it consists of the
+ * dims i and i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved.  Dims from
+ * rot_dim on are copied.  vcs_rope_init fills it: axis a takes the next
+ * sections[a] pairs, inv_freq[i] = theta^(-2 i / rot_dim).  The caller may
+ * change inv_freq and pair_axis afterwards (scaled frequencies, axes by turns).
+ * Returns VCS_ERR_INVALID_ARG for a null pointer, a rot_dim that is not a
+ * multiple of 16 from 16 to 256, num_axes outside 1 .. VCS_ROPE_MAX_AXES,
+ * negative sections or sections that do not sum to rot_dim / 2, or a theta
+ * that is not a positive finite number.
+ *
+ * vcs_gather_rope: vcs_gather with Q and K rotated:
+ *   q[n] = R(pos[., n]) q_traj[tok_gather[n]], k alike, v[n] = v_traj[tok_gather[n]].
+ *   tok_gather  as for vcs_gather, or NULL: row n is token n (then traj_tokens
+ *               equals num_tokens)
+ *   pos         int32 [rope->num_axes, num_tokens] device; any int32
+ *   rope        host pointer, read during the call
+ *   q, k, v     must not overlap the inputs
+ * The angle is exact to 2^-32 of a turn for every position; products and sums
+ * are fp32, rounded once to bf16.  The v rows are copied bit for bit.
+ *
+ * vcs_gather_inverse: the gather map the other way, for vcs_gather_rope_bwd:
+ * inv_tok[inv_off[t] .. inv_off[t+1]) are the segment tokens n with
+ * tok_gather[n] = t, in increasing order.
+ *   inv_off     int32 [traj_tokens + 1] device (written)
+ *   inv_tok     int32 [num_tokens] device (written)
+ *   dev_status  as above: VCS_ERR_DEVICE_CHECK for an index outside
+ *               [0, traj_tokens) (that token is in no list; inv_tok's entries
+ *               from inv_off[traj_tokens] on are such tokens)
+ *   ws          device workspace of vcs_gather_inverse_workspace_size() bytes,
+ *               256-byte aligned
+ *
+ * vcs_gather_rope_bwd: the gradient of vcs_gather_rope: over the copies n of
+ * trajectory token t, dq_traj[t] = sum R(-pos[., n]) dq[n], dk_traj alike,
+ * dv_traj[t] = sum dv[n] (0 for tokens no segment reads).  Sums in fp32, in
+ * increasing n, rounded once: the same inputs give the same bits.
+ *   inv_off, inv_tok  from vcs_gather_inverse, or both NULL: token n is row n
+ *   dev_status  VCS_ERR_DEVICE_CHECK for a list outside [0, num_tokens] (read
+ *               as empty) or a token outside [0, num_tokens) (left out)
+ * One warp takes a trajectory token's copies in turn: a token with very many
+ * copies takes time in proportion.
+ * Both return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
+ * bytes) pointers, a rope that vcs_rope_init would refuse, a pair_axis outside
+ * [0, num_axes) or an inv_freq that is not finite; VCS_ERR_UNSUPPORTED for a
+ * d that is not a multiple of 8 from rot_dim to 256 or more than 65,535 heads;
+ * VCS_ERR_OVERFLOW for counts above INT32_MAX.
+ * ------------------------------------------------------------------------ */
+#define VCS_ROPE_MAX_PAIRS 128
+#define VCS_ROPE_MAX_AXES 4
+
+typedef struct vcs_rope {
+  int32_t rot_dim;
+  int32_t num_axes;
+  int32_t interleaved;
+  int32_t reserved;                       /* 0 */
+  double inv_freq[VCS_ROPE_MAX_PAIRS];    /* radians per position */
+  int32_t pair_axis[VCS_ROPE_MAX_PAIRS];
+} vcs_rope;
+
+vcs_status vcs_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
+                                const int32_t* tok_src_step, const int32_t* step_img, const int32_t* step_txt,
+                                const int32_t* step_grid, int64_t num_steps, int32_t* pos, int32_t* dev_status,
+                                void* stream);
+
+vcs_status vcs_rope_init(vcs_rope* rope, int32_t rot_dim, int32_t num_axes, const int32_t* sections, double theta,
+                         int32_t interleaved);
+
+vcs_status vcs_gather_rope(const void* q_traj, const void* k_traj, const void* v_traj, int64_t traj_tokens,
+                           const int32_t* tok_gather, const int32_t* pos, int64_t num_tokens, int32_t hq, int32_t hkv,
+                           int32_t d, const vcs_rope* rope, void* q, void* k, void* v, int32_t* dev_status,
+                           void* stream);
+
+size_t vcs_gather_inverse_workspace_size(int64_t num_tokens);
+
+vcs_status vcs_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
+                              int32_t* inv_tok, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream);
+
+vcs_status vcs_gather_rope_bwd(const void* dq, const void* dk, const void* dv, int64_t num_tokens, const int32_t* pos,
+                               const int32_t* inv_off, const int32_t* inv_tok, int64_t traj_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, const vcs_rope* rope, void* dq_traj, void* dk_traj,
+                               void* dv_traj, int32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------------
  * Token-ID stream fields (App. C.1, Algorithm 1's (ids, mask, logp) stream).
  * Response tokens enter a segment's stream as trainable tokens with their
  * rollout log-probabilities; observation tokens and the re-tokenised history

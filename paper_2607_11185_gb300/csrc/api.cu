@@ -237,6 +237,121 @@ size_t vcs_attn_bwd_workspace_size(int32_t num_segments, int64_t num_tokens, int
   return attn_bwd_ws_bytes(a);
 }
 
+// ---------------------------------------------------------------- rotary positions
+vcs_status vcs_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
+                                const int32_t* tok_src_step, const int32_t* step_img, const int32_t* step_txt,
+                                const int32_t* step_grid, int64_t num_steps, int32_t* pos, int32_t* dev_status,
+                                void* stream) {
+  vcs::ApiRange nvtx_range("vcs_stream_positions");
+  if (num_segments < 0 || num_tokens < 0 || num_steps < 0) return VCS_ERR_INVALID_ARG;
+  if (num_tokens > INT32_MAX || num_steps > INT32_MAX) return VCS_ERR_OVERFLOW;
+  if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
+  if (num_tokens > 0 && (num_segments == 0 || num_steps == 0 || tok_src_step == nullptr || step_img == nullptr ||
+                         step_txt == nullptr || step_grid == nullptr || pos == nullptr))
+    return VCS_ERR_INVALID_ARG;
+  if (launch_stream_positions(cu_seqlens, num_segments, (int32_t)num_tokens, tok_src_step, step_img, step_txt,
+                              step_grid, (int32_t)num_steps, pos, dev_status, as_stream(stream)) != cudaSuccess)
+    return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+static bool rot_dim_ok(int32_t rot_dim) { return rot_dim >= 16 && rot_dim <= 2 * VCS_ROPE_MAX_PAIRS && rot_dim % 16 == 0; }
+
+vcs_status vcs_rope_init(vcs_rope* rope, int32_t rot_dim, int32_t num_axes, const int32_t* sections, double theta,
+                         int32_t interleaved) {
+  if (rope == nullptr || sections == nullptr || !rot_dim_ok(rot_dim)) return VCS_ERR_INVALID_ARG;
+  if (num_axes < 1 || num_axes > VCS_ROPE_MAX_AXES || !(theta > 0.0) || !std::isfinite(theta))
+    return VCS_ERR_INVALID_ARG;
+  int64_t sum = 0;
+  for (int32_t a = 0; a < num_axes; ++a) {
+    if (sections[a] < 0) return VCS_ERR_INVALID_ARG;
+    sum += sections[a];
+  }
+  if (sum != rot_dim / 2) return VCS_ERR_INVALID_ARG;
+  std::memset(rope, 0, sizeof(*rope));
+  rope->rot_dim = rot_dim;
+  rope->num_axes = num_axes;
+  rope->interleaved = interleaved != 0;
+  int32_t i = 0;
+  for (int32_t a = 0; a < num_axes; ++a)
+    for (int32_t j = 0; j < sections[a]; ++j, ++i) {
+      rope->inv_freq[i] = std::pow(theta, -2.0 * i / rot_dim);
+      rope->pair_axis[i] = a;
+    }
+  return VCS_OK;
+}
+
+// The checks both directions share: seg_rows segment tokens, traj_rows trajectory tokens.
+static vcs_status check_rope(const void* const (&in)[3], void* const (&out)[3], int64_t rows_in, int64_t rows_out,
+                             int64_t num_tokens, const int32_t* pos, int32_t hq, int32_t hkv, int32_t d,
+                             const vcs_rope* rope) {
+  if (rows_in < 0 || rows_out < 0 || hq <= 0 || hkv <= 0 || d <= 0 || rope == nullptr) return VCS_ERR_INVALID_ARG;
+  if (rows_in > INT32_MAX || rows_out > INT32_MAX) return VCS_ERR_OVERFLOW;
+  if (!rot_dim_ok(rope->rot_dim) || rope->num_axes < 1 || rope->num_axes > VCS_ROPE_MAX_AXES)
+    return VCS_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
+    if (rope->pair_axis[i] < 0 || rope->pair_axis[i] >= rope->num_axes || !std::isfinite(rope->inv_freq[i]))
+      return VCS_ERR_INVALID_ARG;
+  if (d % 8 != 0 || d < rope->rot_dim || d > 256 || hq > 65535 || hkv > 65535) return VCS_ERR_UNSUPPORTED;
+  for (int i = 0; i < 3; ++i) {
+    if ((rows_in > 0 && in[i] == nullptr) || (rows_out > 0 && out[i] == nullptr)) return VCS_ERR_INVALID_ARG;
+    if (!aligned16(in[i]) || !aligned16(out[i])) return VCS_ERR_INVALID_ARG;
+  }
+  if (num_tokens > 0 && pos == nullptr) return VCS_ERR_INVALID_ARG;
+  return VCS_OK;
+}
+
+vcs_status vcs_gather_rope(const void* q_traj, const void* k_traj, const void* v_traj, int64_t traj_tokens,
+                           const int32_t* tok_gather, const int32_t* pos, int64_t num_tokens, int32_t hq, int32_t hkv,
+                           int32_t d, const vcs_rope* rope, void* q, void* k, void* v, int32_t* dev_status,
+                           void* stream) {
+  vcs::ApiRange nvtx_range("vcs_gather_rope");
+  const void* const in[3] = {q_traj, k_traj, v_traj};
+  void* const out[3] = {q, k, v};
+  const vcs_status s = check_rope(in, out, traj_tokens, num_tokens, num_tokens, pos, hq, hkv, d, rope);
+  if (s != VCS_OK) return s;
+  if (tok_gather == nullptr && num_tokens != traj_tokens) return VCS_ERR_INVALID_ARG;
+  if (launch_gather_rope(q_traj, k_traj, v_traj, traj_tokens, num_tokens, pos, num_tokens, tok_gather, nullptr, false,
+                         hq, hkv, d, *rope, q, k, v, dev_status, as_stream(stream)) != cudaSuccess)
+    return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+size_t vcs_gather_inverse_workspace_size(int64_t num_tokens) {
+  return gather_inverse_ws_bytes(num_tokens < 0 ? 0 : num_tokens);
+}
+
+vcs_status vcs_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
+                              int32_t* inv_tok, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_gather_inverse");
+  if (num_tokens < 0 || traj_tokens < 0 || inv_off == nullptr) return VCS_ERR_INVALID_ARG;
+  if (num_tokens > INT32_MAX || traj_tokens > INT32_MAX - 1) return VCS_ERR_OVERFLOW;
+  if (num_tokens > 0 && (tok_gather == nullptr || inv_tok == nullptr)) return VCS_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < gather_inverse_ws_bytes(num_tokens) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  if (launch_gather_inverse(tok_gather, num_tokens, traj_tokens, inv_off, inv_tok, ws, dev_status,
+                            as_stream(stream)) != cudaSuccess)
+    return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+vcs_status vcs_gather_rope_bwd(const void* dq, const void* dk, const void* dv, int64_t num_tokens, const int32_t* pos,
+                               const int32_t* inv_off, const int32_t* inv_tok, int64_t traj_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, const vcs_rope* rope, void* dq_traj, void* dk_traj,
+                               void* dv_traj, int32_t* dev_status, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_gather_rope_bwd");
+  const void* const in[3] = {dq, dk, dv};
+  void* const out[3] = {dq_traj, dk_traj, dv_traj};
+  const vcs_status s = check_rope(in, out, num_tokens, traj_tokens, num_tokens, pos, hq, hkv, d, rope);
+  if (s != VCS_OK) return s;
+  if (inv_off == nullptr ? inv_tok != nullptr || num_tokens != traj_tokens : num_tokens > 0 && inv_tok == nullptr)
+    return VCS_ERR_INVALID_ARG;
+  if (launch_gather_rope(dq, dk, dv, num_tokens, traj_tokens, pos, num_tokens, inv_tok, inv_off, true, hq, hkv, d,
+                         *rope, dq_traj, dk_traj, dv_traj, dev_status, as_stream(stream)) != cudaSuccess)
+    return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
 vcs_status vcs_stream_fields(const int32_t* traj_ids, const float* traj_logp, int64_t traj_tokens,
                              const int32_t* tok_gather, const uint8_t* tok_loss_mask, int64_t num_tokens,
                              int32_t* ids, float* logp, int32_t* dev_status, void* stream) {

@@ -103,6 +103,21 @@ cudaError_t launch_shared_prefix(const int32_t* cu_seqlens, const int32_t* seg_t
                                  int32_t num_segments, int32_t num_tokens, int32_t* seg_shared, int32_t* status,
                                  cudaStream_t st);
 
+// ---- rotary positions over segments (rope.cu) ----
+cudaError_t launch_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int32_t num_tokens,
+                                    const int32_t* src_step, const int32_t* step_img, const int32_t* step_txt,
+                                    const int32_t* step_grid, int32_t num_steps, int32_t* pos, int32_t* status,
+                                    cudaStream_t st);
+size_t gather_inverse_ws_bytes(int64_t num_tokens);
+cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
+                                  int32_t* inv_tok, void* ws, int32_t* status, cudaStream_t st);
+// forward: map = tok_gather, rows_out segment tokens; backward: off, map = the inverse, rows_out trajectory
+// tokens; map (and off) nullptr: row n is token n
+cudaError_t launch_gather_rope(const void* q_in, const void* k_in, const void* v_in, int64_t rows_in, int64_t rows_out,
+                               const int32_t* pos, int64_t pos_stride, const int32_t* map, const int32_t* off,
+                               bool backward, int32_t hq, int32_t hkv, int32_t d, const vcs_rope& rope, void* q_out,
+                               void* k_out, void* v_out, int32_t* status, cudaStream_t st);
+
 // TMA descriptor encoding through the driver entry point (no libcuda link).
 bool encode_tma_3d_bf16(void* map /*CUtensorMap*/, const void* base, uint64_t d, uint64_t heads, uint64_t tokens,
                         uint32_t box_d, uint32_t box_rows);

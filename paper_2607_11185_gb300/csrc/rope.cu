@@ -1,0 +1,739 @@
+// rope.cu - rotary positions with several axes over training segments, sm_103a.
+//
+// A fresh stream (App. C.1) starts its positions over, so a trajectory token stands at other
+// positions in every segment that copies it, and the rotation belongs on the way from the trajectory
+// rows to the segment rows:
+//   stream_positions   pos[a][n], a = time, height, width, of every segment token
+//   gather_rope        q[n] = R(pos[., n]) q_traj[tok_gather[n]], k alike, v copied
+//   gather_rope_bwd    dq_traj[t] = sum over the copies n of t of R(-pos[., n]) dq[n], dk alike, dv summed
+// R turns pair i, dims (a, b), by the angle x = inv_freq[i] * pos[axis[i]]:
+//   (a, b) -> (a cos x - b sin x, b cos x + a sin x).
+//
+// The angle is reduced exactly: inv_freq / 2 pi is a 64-bit fraction of a turn, its product with the
+// position modulo 2^64 is the fraction of a turn the angle ends at, and the upper 32 bits of that go to
+// sincospi.  A position of 2^31 is as exact as a position of 1 (a product in fp32 would be off by
+// 4e-3 radians at 67,000).
+//
+// All three are bound by HBM.  The rotation reads and writes each row once; a pass of its own over
+// the gathered rows would double that.
+#include <cmath>
+#include <cstdint>
+
+#include "internal.h"
+#include "sm100.cuh"
+
+namespace vcs {
+namespace {
+
+using dev::set_status;
+
+// ------------------------------------------------------------------ positions
+constexpr int kPosThreads = 256;
+constexpr int kPosChunk = 8192;  // tokens of a segment a block writes
+
+// One block: tokens [chunk * kPosChunk, + kPosChunk) of segment blockIdx.x.  The segment's steps in
+// tiles of a step a thread: a step's run of tokens starts at the lower bound of its index in
+// tok_src_step (non-decreasing within a segment), how far it moves the position follows from the run's
+// length (text only, or screenshot and text), and a block scan gives each run's first position.  Every
+// chunk of a segment repeats the scan of the steps before it: the searches' latency, a few us, against
+// a launch and a workspace.
+__global__ void __launch_bounds__(kPosThreads)
+    stream_positions_kernel(const int32_t* __restrict__ cu_seqlens, int32_t num_segments, int32_t num_tokens,
+                            const int32_t* __restrict__ src_step, const int32_t* __restrict__ step_img,
+                            const int32_t* __restrict__ step_txt, const int32_t* __restrict__ step_grid,
+                            int32_t num_steps, int32_t* __restrict__ pos, int32_t* status) {
+  __shared__ int32_t run_at[kPosThreads + 1];   // first token of the step's run
+  __shared__ int32_t run_pos[kPosThreads];      // its first position
+  __shared__ int32_t run_img[kPosThreads];      // screenshot tokens of the run, 0 if it is text only
+  __shared__ int32_t run_skip[kPosThreads];     // positions the screenshot takes
+  __shared__ int32_t run_h[kPosThreads], run_w[kPosThreads];
+  __shared__ int32_t wsum[kPosThreads / 32];
+  __shared__ int32_t carry_s;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const size_t N = (size_t)num_tokens;
+  for (int seg = blockIdx.x; seg < num_segments; seg += gridDim.x) {
+    const int start = cu_seqlens[seg], end = cu_seqlens[seg + 1];
+    if (start < 0 || end < start || end > num_tokens || (seg == 0 && start != 0) ||
+        (seg == num_segments - 1 && end != num_tokens)) {
+      if (tid == 0 && blockIdx.y == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
+      continue;
+    }
+    for (int64_t c0 = start + (int64_t)blockIdx.y * kPosChunk; c0 < end; c0 += (int64_t)gridDim.y * kPosChunk) {
+      const int lo_tok = (int)c0, hi_tok = (int)(c0 + kPosChunk < end ? c0 + kPosChunk : end);
+      const int first = src_step[start], last = src_step[end - 1];
+      if (first < 0 || last < first || last >= num_steps) {
+        if (tid == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
+        continue;
+      }
+      int carry = 0;  // position at the tile's first run
+      for (int64_t s0 = first; s0 <= last; s0 += kPosThreads) {
+        const int64_t s = s0 + tid;
+        int lo = end;
+        if (s <= last) {  // lower bound of s in src_step[start, end)
+          int a = start, b = end;
+          while (a < b) {
+            const int mid = a + ((b - a) >> 1);
+            if (src_step[mid] < s) a = mid + 1;
+            else b = mid;
+          }
+          lo = a;
+        }
+        run_at[tid] = lo;
+        if (tid == kPosThreads - 1) {
+          int a = lo, b = end;
+          while (a < b) {
+            const int mid = a + ((b - a) >> 1);
+            if (src_step[mid] < s + 1) a = mid + 1;
+            else b = mid;
+          }
+          run_at[kPosThreads] = a;
+        }
+        __syncthreads();
+        const int len = run_at[tid + 1] - lo;
+        int adv = 0;
+        if (s <= last) {
+          const int img = step_img[s], txt = step_txt[s];
+          int im = 0, skip = 0, h = 1, w = 1;
+          bool ok = len == 0 || len == txt || (int64_t)len == (int64_t)img + txt;
+          if (len > 0 && img > 0 && (int64_t)len == (int64_t)img + txt) {
+            const int t = step_grid[3 * s];
+            h = step_grid[3 * s + 1];
+            w = step_grid[3 * s + 2];
+            // the grid holds the screenshot's tokens: then every product below is at most img
+            ok = t > 0 && h > 0 && w > 0 && t <= img && h <= img && w <= img && (int64_t)h * w <= img &&
+                 (int64_t)t * (h * w) == img;
+            if (ok) {
+              im = img;
+              skip = max(t, max(h, w));
+            } else {
+              h = w = 1;
+            }
+          }
+          if (!ok) set_status(status, VCS_ERR_DEVICE_CHECK);  // its tokens are counted like text
+          adv = len - im + skip;
+          run_img[tid] = im;
+          run_skip[tid] = skip;
+          run_h[tid] = h;
+          run_w[tid] = w;
+        }
+        int x = adv;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        if (lane == 31) wsum[wid] = x;
+        __syncthreads();
+        int before = carry;
+        for (int i = 0; i < wid; ++i) before += wsum[i];
+        run_pos[tid] = before + x - adv;
+        if (tid == kPosThreads - 1) carry_s = before + x;
+        __syncthreads();
+        carry = carry_s;
+        const int n0 = max(lo_tok, run_at[0]), n1 = min(hi_tok, run_at[kPosThreads]);
+        for (int n = n0 + tid; n < n1; n += kPosThreads) {
+          const int64_t r = (int64_t)src_step[n] - s0;
+          if (r < 0 || r >= kPosThreads || s0 + r > last || n < run_at[r] || n >= run_at[r + 1]) {
+            set_status(status, VCS_ERR_DEVICE_CHECK);  // tok_src_step decreases within the segment
+            continue;
+          }
+          const int k = n - run_at[r], im = run_img[r];
+          int p0 = run_pos[r], p1, p2;
+          if (k < im) {
+            const int h = run_h[r], w = run_w[r];
+            const int line = k / w, frame = line / h;
+            p1 = p0 + line - frame * h;
+            p2 = p0 + k - line * w;
+            p0 += frame;
+          } else {
+            p0 += run_skip[r] + k - im;
+            p1 = p2 = p0;
+          }
+          pos[n] = p0;
+          pos[N + n] = p1;
+          pos[2 * N + n] = p2;
+        }
+        const int tile_end = run_at[kPosThreads];
+        __syncthreads();
+        if (tile_end >= hi_tok) break;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ inverse map
+// Stable radix sort of (tok_gather[n], n) by 8-bit digits: the n of equal keys stay in order, whatever
+// the map, and no atomic decides an order.  A pass is three launches: digit counts of tiles of kTile
+// keys, per digit the scan of its tiles' counts, and the scatter.  Keys outside [0, T) become T, behind
+// all others.
+constexpr int kSortThreads = 256;
+constexpr int kPerThread = 16;
+constexpr int kTile = kSortThreads * kPerThread;
+
+__device__ __forceinline__ uint32_t load_key(const int32_t* __restrict__ keys, int64_t i, uint32_t T, bool first,
+                                             int32_t* status) {
+  const uint32_t k = (uint32_t)__ldg(&keys[i]);
+  if (first && k >= T) {
+    set_status(status, VCS_ERR_DEVICE_CHECK);
+    return T;
+  }
+  return k;
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_count(const int32_t* __restrict__ keys, int64_t n, uint32_t T, int shift, int32_t* __restrict__ counts,
+                  int tiles, bool first, int32_t* status) {
+  __shared__ int32_t c[256];
+  c[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * kTile;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int64_t i = base + u * kSortThreads + threadIdx.x;
+    if (i < n) atomicAdd(&c[(load_key(keys, i, T, first, status) >> shift) & 255u], 1);
+  }
+  __syncthreads();
+  counts[(size_t)threadIdx.x * tiles + blockIdx.x] = c[threadIdx.x];
+}
+
+// Block b: the exclusive scan of digit b's counts over the tiles, and their sum.
+__global__ void __launch_bounds__(1024)
+    inverse_scan(int32_t* __restrict__ counts, int tiles, int32_t* __restrict__ totals) {
+  __shared__ int32_t wsum[32];
+  int32_t* c = counts + (size_t)blockIdx.x * tiles;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  int carry = 0;
+  for (int base = 0; base < tiles; base += 1024) {
+    const int i = base + (int)threadIdx.x;
+    const int v = i < tiles ? c[i] : 0;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[wid] = x;
+    __syncthreads();
+    int w = wsum[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += y;
+    }
+    const int before = wid > 0 ? __shfl_sync(0xffffffffu, w, wid - 1) : 0;
+    if (i < tiles) c[i] = carry + before + x - v;
+    carry += __shfl_sync(0xffffffffu, w, 31);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+}
+
+// Warp w of a tile takes its keys [512 w, + 512) in order, 32 at a time: a key's rank among the warp's
+// equal digits is the count of them before it, by a vote among the 32 and a running count.
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ vals, int64_t n, uint32_t T,
+                    int shift, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, int tiles,
+                    bool first, int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
+  constexpr int W = kSortThreads / 32;
+  __shared__ int32_t seen[W][256];
+  __shared__ int32_t wsum[W];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+#pragma unroll
+  for (int w = 0; w < W; ++w) seen[w][tid] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * kTile + wid * (32 * kPerThread) + lane;
+  uint32_t key[kPerThread];
+  int rank[kPerThread];
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u)
+    key[u] = base + 32 * u < n ? load_key(keys, base + 32 * u, T, first, nullptr) : 0xffffffffu;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const bool live = base + 32 * u < n;
+    const uint32_t dg = (key[u] >> shift) & 255u;
+    const unsigned same = __match_any_sync(0xffffffffu, live ? dg : 256u);
+    const int below = __popc(same & ((1u << lane) - 1u));
+    int before = 0;
+    if (live) before = seen[wid][dg];
+    __syncwarp();
+    if (live && below == 0) seen[wid][dg] = before + __popc(same);
+    __syncwarp();
+    rank[u] = before + below;
+  }
+  __syncthreads();
+  {  // thread = digit: where the digit starts in the output, then in each warp's part of this tile
+    const int tot = totals[tid];
+    int x = tot;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[wid] = x;
+    __syncthreads();
+    int at = x - tot + counts[(size_t)tid * tiles + blockIdx.x];
+    for (int i = 0; i < wid; ++i) at += wsum[i];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int c = seen[w][tid];
+      seen[w][tid] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int64_t i = base + 32 * u;
+    if (i >= n) continue;
+    const int to = seen[wid][(key[u] >> shift) & 255u] + rank[u];
+    keys_out[to] = (int32_t)key[u];
+    vals_out[to] = first ? (int32_t)i : vals[i];
+  }
+}
+
+// off[t] = first place of a key >= t in the sorted keys, for t in a block's 1,024: two searches bound
+// the block's keys, counts of them in shared memory and a scan give the rest.
+constexpr int kOffTile = 1024;
+__global__ void __launch_bounds__(256) inverse_offsets(const int32_t* __restrict__ keys, int32_t n, int64_t T,
+                                                       int32_t* __restrict__ off) {
+  __shared__ int32_t c[kOffTile];
+  __shared__ int32_t bound[2];
+  __shared__ int32_t wsum[8];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int64_t t0 = (int64_t)blockIdx.x * kOffTile;
+#pragma unroll
+  for (int u = 0; u < kOffTile / 256; ++u) c[u * 256 + tid] = 0;
+  if (tid < 2) {
+    const int64_t t = t0 + tid * (int64_t)kOffTile;
+    int a = 0, b = n;
+    while (a < b) {
+      const int mid = a + ((b - a) >> 1);
+      if (keys[mid] < t) a = mid + 1;
+      else b = mid;
+    }
+    bound[tid] = a;
+  }
+  __syncthreads();
+  const int lo = bound[0], hi = bound[1];
+  for (int i = lo + tid; i < hi; i += 256) atomicAdd(&c[keys[i] - t0], 1);
+  __syncthreads();
+  int v[kOffTile / 256], sum = 0;
+#pragma unroll
+  for (int u = 0; u < kOffTile / 256; ++u) {
+    v[u] = c[tid * (kOffTile / 256) + u];
+    sum += v[u];
+  }
+  int x = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) wsum[wid] = x;
+  __syncthreads();
+  int at = lo + x - sum;
+  for (int i = 0; i < wid; ++i) at += wsum[i];
+#pragma unroll
+  for (int u = 0; u < kOffTile / 256; ++u) {
+    const int64_t t = t0 + tid * (kOffTile / 256) + u;
+    if (t <= T) off[t] = at;
+    at += v[u];
+  }
+}
+
+// ------------------------------------------------------------------ rotation
+constexpr int kRopeThreads = 256;
+constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kBatch = 8;  // copies of a trajectory row whose angles a warp holds (backward)
+constexpr int kMaxPairs = VCS_ROPE_MAX_PAIRS;
+
+struct RopeArgs {
+  const int4 *q_in, *k_in, *v_in;
+  int4 *q_out, *k_out, *v_out;
+  int64_t rows_in, rows_out;     // tokens of the inputs and of the outputs
+  const int32_t* pos;            // [axes][segment tokens]
+  int64_t pos_stride;
+  const int32_t* map;            // forward: tok_gather; backward: inv_tok (nullptr: token n is row n)
+  const int32_t* off;            // backward: inv_off
+  int32_t hq, hkv;
+  int32_t chunks;                // 16-byte chunks of a row
+  int32_t turned;                // items of a row that are rotated (pairs of chunks, or chunks if interleaved)
+  int32_t plain;                 // and its chunks that are not
+  uint32_t turned_magic, plain_magic;  // of div_by
+  int32_t* status;
+  uint64_t turn[kMaxPairs];      // inv_freq / 2 pi in 2^-64 turns
+  uint8_t axis[kMaxPairs];
+};
+
+__device__ __forceinline__ int4 ld_stream(const int4* p) {
+  int4 r;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.s32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p));
+  return r;
+}
+__device__ __forceinline__ void st_stream(int4* p, int4 v) {
+  asm volatile("st.global.cs.v4.s32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+               : "memory");
+}
+
+// the two bf16 of a word, exactly
+__device__ __forceinline__ float lo_f(int w) { return __uint_as_float((uint32_t)w << 16); }
+__device__ __forceinline__ float hi_f(int w) { return __uint_as_float((uint32_t)w & 0xffff0000u); }
+__device__ __forceinline__ void unpack8(int4 x, float (&f)[8]) {
+  f[0] = lo_f(x.x), f[1] = hi_f(x.x), f[2] = lo_f(x.y), f[3] = hi_f(x.y);
+  f[4] = lo_f(x.z), f[5] = hi_f(x.z), f[6] = lo_f(x.w), f[7] = hi_f(x.w);
+}
+__device__ __forceinline__ int4 pack8(const float* f) {
+  return make_int4((int)dev::pack_bf16(f[0], f[1]), (int)dev::pack_bf16(f[2], f[3]), (int)dev::pack_bf16(f[4], f[5]),
+                   (int)dev::pack_bf16(f[6], f[7]));
+}
+
+// i / c by the magic 2^32 / c + 1, exactly for i < 2^32 / c; c = 1 has none
+__device__ __forceinline__ int div_by(int i, int c, uint32_t magic) {
+  return c == 1 ? i : (int)__umulhi((uint32_t)i, magic);
+}
+
+// One warp per output token.  Lane l computes the angles of pairs l, l + 32, ... of the token's copies into
+// the warp's table, then the lanes take the row's items in turn.  An item is, with pairs (i, i + rot/2), the
+// chunks of eight dims c and c + rot/16, which hold eight whole pairs; with neighbouring pairs, one chunk
+// of four.  The table holds two pairs (cos, sin, cos, sin) in 16 bytes, at [pair of the item / 2][item of
+// the row], so that lanes on neighbouring items read neighbouring 16 bytes.
+template <int NP, bool INTER, bool BWD>
+__global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant__ RopeArgs a) {
+  constexpr int B = BWD ? kBatch : 1;
+  constexpr int IP = INTER ? 4 : 8;        // pairs of an item
+  constexpr int IC = INTER ? 1 : 2;        // chunks of an item
+  constexpr int U = INTER ? 4 : 2;         // items a lane has in flight
+  extern __shared__ float4 table[];        // [warp][copy][NP * 16]
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  float4* tab = table + (size_t)wid * B * NP * 16;
+  uint64_t turn[NP];
+  int axis[NP];
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    turn[p] = a.turn[lane + 32 * p];
+    axis[p] = a.axis[lane + 32 * p];
+  }
+  const int heads = a.hq + a.hkv;
+  const int turned = heads * a.turned, plain = heads * a.plain;
+  const int64_t warps = (int64_t)gridDim.x * kRopeWarps;
+  for (int64_t r = blockIdx.x * (int64_t)kRopeWarps + wid; r < a.rows_out; r += warps) {
+    // the row's copies: list[0 .. m), or row `only` alone
+    int64_t m = 1, only = r;
+    const int32_t* list = nullptr;
+    if constexpr (BWD) {
+      if (a.off != nullptr) {
+        const int32_t lo = __ldg(&a.off[r]), hi = __ldg(&a.off[r + 1]);
+        const bool ok = lo >= 0 && hi >= lo && hi <= a.rows_in;
+        if (!ok && lane == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
+        m = ok ? hi - lo : 0;
+        list = a.map + lo;
+      }
+    } else if (a.map != nullptr) {
+      only = __ldg(&a.map[r]);
+      if (only < 0 || only >= a.rows_in) {
+        if (lane == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
+        continue;
+      }
+    }
+    // copy j of the batch at b0: its row, on every lane; -1 outside the rows
+    int64_t held = -1;
+    auto hold = [&](int64_t b0) {
+      if constexpr (BWD) {
+        held = only;
+        if (list != nullptr) {
+          held = b0 + lane < m && lane < B ? __ldg(&list[b0 + lane]) : -1;
+          if (held < -1 || held >= a.rows_in || (held < 0 && b0 + lane < m && lane < B)) {
+            set_status(a.status, VCS_ERR_DEVICE_CHECK);
+            held = -1;
+          }
+        }
+      }
+    };
+    auto copy = [&](int j) -> int64_t {
+      if constexpr (BWD) return __shfl_sync(0xffffffffu, held, list != nullptr ? j : 0);
+      else return only;
+    };
+    auto angles = [&](int count) {
+      __syncwarp();
+      for (int j = 0; j < count; ++j) {
+        const int64_t n = BWD ? copy(j) : r;
+        if (n < 0) continue;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const int pair = lane + 32 * p;
+          if (pair >= a.turned * IP) continue;
+          const int32_t x = __ldg(&a.pos[axis[p] * a.pos_stride + n]);
+          const uint64_t ph = (uint64_t)(int64_t)x * turn[p];
+          float s, c;
+          sincospif((float)(int32_t)(ph >> 32) * 0x1p-31f, &s, &c);
+          const int item = pair / IP, k = pair % IP;
+          reinterpret_cast<float2*>(tab + (size_t)j * NP * 16)[2 * ((k >> 1) * a.turned + item) + (k & 1)] =
+              make_float2(c, BWD ? -s : s);
+        }
+      }
+      __syncwarp();
+    };
+    bool ready = false;
+    for (int i0 = 0; i0 < turned; i0 += 32 * U) {
+      float acc[U][8 * IC];
+      int at[U];        // chunk of the item in its row of q or k
+      int row[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + 32 * u + lane;
+        row[u] = div_by(i, a.turned, a.turned_magic);
+        at[u] = i - row[u] * a.turned;
+#pragma unroll
+        for (int e = 0; e < 8 * IC; ++e) acc[u][e] = 0.f;
+        if (i >= turned) row[u] = -1;
+      }
+      for (int64_t b0 = 0; b0 < m; b0 += B) {
+        const int cnt = (int)(m - b0 < B ? m - b0 : B);
+        if (!ready || m > B) {
+          hold(b0);
+          angles(cnt);
+          ready = true;
+        }
+        for (int j = 0; j < cnt; ++j) {
+          const int64_t n = copy(j);
+          if (n < 0) continue;
+          int4 x[U][IC];
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (row[u] >= 0) {
+              const int4* src = row[u] < a.hq ? a.q_in + (n * a.hq + row[u]) * a.chunks
+                                              : a.k_in + (n * a.hkv + (row[u] - a.hq)) * a.chunks;
+#pragma unroll
+              for (int e = 0; e < IC; ++e) x[u][e] = ld_stream(src + at[u] + e * a.turned);
+            }
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (row[u] >= 0) {
+              float f[8 * IC], g[8 * IC];
+#pragma unroll
+              for (int e = 0; e < IC; ++e) unpack8(x[u][e], *reinterpret_cast<float(*)[8]>(&f[8 * e]));
+              const float4* t = tab + (size_t)j * NP * 16 + at[u];
+#pragma unroll
+              for (int k = 0; k < IP; k += 2) {
+                const float4 cs = t[(k >> 1) * a.turned];
+                const int i0p = INTER ? 2 * k : k, i1p = INTER ? 2 * k + 2 : k + 1;   // first dims of the pairs
+                const int o = INTER ? 1 : 8;                                          // to their second dims
+                g[i0p] = f[i0p] * cs.x - f[i0p + o] * cs.y;
+                g[i0p + o] = f[i0p + o] * cs.x + f[i0p] * cs.y;
+                g[i1p] = f[i1p] * cs.z - f[i1p + o] * cs.w;
+                g[i1p + o] = f[i1p + o] * cs.z + f[i1p] * cs.w;
+              }
+#pragma unroll
+              for (int e = 0; e < 8 * IC; ++e) acc[u][e] = BWD ? acc[u][e] + g[e] : g[e];
+            }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (row[u] >= 0) {
+          int4* dst = row[u] < a.hq ? a.q_out + (r * a.hq + row[u]) * a.chunks
+                                    : a.k_out + (r * a.hkv + (row[u] - a.hq)) * a.chunks;
+#pragma unroll
+          for (int e = 0; e < IC; ++e) st_stream(dst + at[u] + e * a.turned, pack8(&acc[u][8 * e]));
+        }
+    }
+    // chunks that are not rotated: the ends of the rows of q and k, and v
+    const int rest = plain + a.hkv * a.chunks;
+    for (int i0 = 0; i0 < rest; i0 += 64) {
+      const int4* src[2];
+      int4* dst[2];
+      int64_t stride[2];
+      bool live[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int i = i0 + 32 * u + lane;
+        live[u] = i < rest;
+        if (i < plain) {
+          const int h = div_by(i, a.plain, a.plain_magic);
+          const int c = h * a.chunks + IC * a.turned + i - h * a.plain;
+          const bool is_q = h < a.hq;
+          stride[u] = (int64_t)(is_q ? a.hq : a.hkv) * a.chunks;
+          src[u] = is_q ? a.q_in + c : a.k_in + c - a.hq * a.chunks;
+          dst[u] = is_q ? a.q_out + c : a.k_out + c - a.hq * a.chunks;
+        } else {
+          stride[u] = (int64_t)a.hkv * a.chunks;
+          src[u] = a.v_in + (i - plain);
+          dst[u] = a.v_out + (i - plain);
+        }
+      }
+      if constexpr (!BWD) {
+        int4 x[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (live[u]) x[u] = ld_stream(src[u] + only * stride[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (live[u]) st_stream(dst[u] + r * stride[u], x[u]);
+      } else {
+        float acc[2][8];
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[u][e] = 0.f;
+        for (int64_t b0 = 0; b0 < m; b0 += B) {
+          const int cnt = (int)(m - b0 < B ? m - b0 : B);
+          if (!ready || m > B) {
+            hold(b0);
+            ready = true;
+          }
+          for (int j = 0; j < cnt; ++j) {
+            const int64_t n = copy(j);
+            if (n < 0) continue;
+            int4 x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (live[u]) x[u] = ld_stream(src[u] + n * stride[u]);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              if (live[u]) {
+                float f[8];
+                unpack8(x[u], f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[u][e] = any ? acc[u][e] + f[e] : f[e];  // one copy: its bits
+              }
+            any = true;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          if (live[u]) st_stream(dst[u] + r * stride[u], pack8(acc[u]));
+      }
+    }
+  }
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+int key_passes(int64_t traj_tokens) {  // 8-bit digits of the keys 0 .. traj_tokens
+  int p = 1;
+  while (p < 4 && (traj_tokens >> (8 * p)) != 0) ++p;
+  return p;
+}
+
+template <bool INTER, bool BWD>
+cudaError_t launch_rope(const RopeArgs& a, int pairs, cudaStream_t st) {
+  const int np = (pairs + 31) / 32;
+  int64_t blocks = (a.rows_out + kRopeWarps - 1) / kRopeWarps;
+  if (blocks > 152 * 8) blocks = 152 * 8;
+  const size_t smem = (size_t)kRopeWarps * (BWD ? kBatch : 1) * np * 16 * sizeof(float4);
+  auto go = [&](auto kernel) {
+    if (smem > 48 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e != cudaSuccess) return e;
+    }
+    kernel<<<(unsigned)blocks, kRopeThreads, smem, st>>>(a);
+    return cudaGetLastError();
+  };
+  if (np == 1) return go(rope_rows<1, INTER, BWD>);
+  if (np == 2) return go(rope_rows<2, INTER, BWD>);
+  return go(rope_rows<4, INTER, BWD>);
+}
+
+}  // namespace
+
+cudaError_t launch_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int32_t num_tokens,
+                                    const int32_t* src_step, const int32_t* step_img, const int32_t* step_txt,
+                                    const int32_t* step_grid, int32_t num_steps, int32_t* pos, int32_t* status,
+                                    cudaStream_t st) {
+  if (num_segments == 0 || num_tokens == 0) return cudaSuccess;
+  // A block per segment and chunk: all the chunks that one segment can have while that is a few blocks an
+  // SM, else those of the average segment; a longer one's are taken in turn.
+  const int64_t all = ((int64_t)num_tokens + kPosChunk - 1) / kPosChunk, few = 152 * 64 / num_segments;
+  int64_t chunks = num_tokens / num_segments / kPosChunk + 1;
+  if (chunks < few) chunks = few;
+  if (chunks > all) chunks = all;
+  if (chunks > 65535) chunks = 65535;
+  dim3 grid((unsigned)num_segments, (unsigned)chunks);
+  stream_positions_kernel<<<grid, kPosThreads, 0, st>>>(cu_seqlens, num_segments, num_tokens, src_step, step_img,
+                                                        step_txt, step_grid, num_steps, pos, status);
+  return cudaGetLastError();
+}
+
+// Workspace: digit counts of the tiles and their totals, then keys twice and tokens once.
+size_t gather_inverse_ws_bytes(int64_t num_tokens) {
+  const int64_t tiles = (num_tokens + kTile - 1) / kTile;
+  return align256((size_t)tiles * 256 * 4) + align256(256 * 4) + 3 * align256((size_t)num_tokens * 4) + 256;
+}
+
+cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
+                                  int32_t* inv_tok, void* ws, int32_t* status, cudaStream_t st) {
+  if (num_tokens == 0) {
+    return cudaMemsetAsync(inv_off, 0, ((size_t)traj_tokens + 1) * 4, st);
+  }
+  const int tiles = (int)((num_tokens + kTile - 1) / kTile);
+  char* w = static_cast<char*>(ws);
+  int32_t* counts = reinterpret_cast<int32_t*>(w);
+  w += align256((size_t)tiles * 256 * 4);
+  int32_t* totals = reinterpret_cast<int32_t*>(w);
+  w += align256(256 * 4);
+  const size_t nb = align256((size_t)num_tokens * 4);
+  int32_t* keys[2] = {reinterpret_cast<int32_t*>(w), reinterpret_cast<int32_t*>(w + nb)};
+  int32_t* spare = reinterpret_cast<int32_t*>(w + 2 * nb);
+  const int passes = key_passes(traj_tokens);
+  const int32_t* kin = tok_gather;
+  const int32_t* vin = nullptr;
+  for (int p = 0; p < passes; ++p) {
+    // the last pass writes inv_tok, the others alternate so that none writes what it reads
+    int32_t* vout = (passes - 1 - p) % 2 == 0 ? inv_tok : spare;
+    inverse_count<<<tiles, kSortThreads, 0, st>>>(kin, num_tokens, (uint32_t)traj_tokens, 8 * p, counts, tiles, p == 0,
+                                                  status);
+    inverse_scan<<<256, 1024, 0, st>>>(counts, tiles, totals);
+    inverse_scatter<<<tiles, kSortThreads, 0, st>>>(kin, vin, num_tokens, (uint32_t)traj_tokens, 8 * p, counts, totals,
+                                                    tiles, p == 0, keys[p & 1], vout);
+    kin = keys[p & 1];
+    vin = vout;
+  }
+  inverse_offsets<<<(unsigned)((traj_tokens + kOffTile) / kOffTile), 256, 0, st>>>(kin, (int32_t)num_tokens,
+                                                                                  traj_tokens, inv_off);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_gather_rope(const void* q_in, const void* k_in, const void* v_in, int64_t rows_in, int64_t rows_out,
+                               const int32_t* pos, int64_t pos_stride, const int32_t* map, const int32_t* off,
+                               bool backward, int32_t hq, int32_t hkv, int32_t d, const vcs_rope& rope, void* q_out,
+                               void* k_out, void* v_out, int32_t* status, cudaStream_t st) {
+  if (rows_out == 0) return cudaSuccess;
+  RopeArgs a;
+  a.q_in = static_cast<const int4*>(q_in);
+  a.k_in = static_cast<const int4*>(k_in);
+  a.v_in = static_cast<const int4*>(v_in);
+  a.q_out = static_cast<int4*>(q_out);
+  a.k_out = static_cast<int4*>(k_out);
+  a.v_out = static_cast<int4*>(v_out);
+  a.rows_in = rows_in;
+  a.rows_out = rows_out;
+  a.pos = pos;
+  a.pos_stride = pos_stride;
+  a.map = map;
+  a.off = off;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.chunks = d / 8;
+  a.turned = rope.interleaved ? rope.rot_dim / 8 : rope.rot_dim / 16;
+  a.plain = (d - rope.rot_dim) / 8;
+  auto magic = [](int32_t c) { return c > 1 ? (uint32_t)((1ull << 32) / (uint32_t)c + 1) : 0u; };
+  a.turned_magic = magic(a.turned);
+  a.plain_magic = magic(a.plain);
+  a.status = status;
+  const int pairs = rope.rot_dim / 2;
+  for (int i = 0; i < kMaxPairs; ++i) {
+    const double turns = i < pairs ? rope.inv_freq[i] * 0.15915494309189533577 : 0.0;
+    double f = turns - std::floor(turns);
+    if (!(f < 1.0)) f = 0.0;  // a tiny negative's fraction rounds to 1
+    a.turn[i] = (uint64_t)std::ldexp(f, 64);
+    a.axis[i] = (uint8_t)(i < pairs ? rope.pair_axis[i] : 0);
+  }
+  if (backward)
+    return rope.interleaved ? launch_rope<true, true>(a, pairs, st) : launch_rope<false, true>(a, pairs, st);
+  return rope.interleaved ? launch_rope<true, false>(a, pairs, st) : launch_rope<false, false>(a, pairs, st);
+}
+
+}  // namespace vcs

@@ -77,6 +77,22 @@ _lib_adv = _sig("vcs_group_advantage", _i32, [_p, _i64, _i32, _f32, _p, _p])
 _lib_fields = _sig("vcs_stream_fields", _i32, [_p, _p, _i64, _p, _p, _i64, _p, _p, _p, _p])
 _lib_compact_ws = _sig("vcs_compact_workspace_size", _sz, [_i64])
 _lib_compact = _sig("vcs_compact_trainable", _i32, [_p, _i64, _p, _i64, _p, _p, _sz, _p])
+
+
+class VcsRope(ctypes.Structure):
+    """How a row is rotated (vcs_rope in include/vcs.h); made by rope_plan."""
+    _fields_ = [("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("inv_freq", ctypes.c_double * 128), ("pair_axis", ctypes.c_int32 * 128)]
+
+
+_lib_positions = _sig("vcs_stream_positions", _i32, [_p, _i32, _i64, _p, _p, _p, _p, _i64, _p, _p, _p])
+_lib_rope_init = _sig("vcs_rope_init", _i32, [_p, _i32, _i32, _p, _f64, _i32])
+_lib_gather_rope = _sig("vcs_gather_rope", _i32,
+                        [_p, _p, _p, _i64, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p])
+_lib_inverse_ws = _sig("vcs_gather_inverse_workspace_size", _sz, [_i64])
+_lib_inverse = _sig("vcs_gather_inverse", _i32, [_p, _i64, _i64, _p, _p, _p, _p, _sz, _p])
+_lib_gather_rope_bwd = _sig("vcs_gather_rope_bwd", _i32,
+                            [_p, _p, _p, _i64, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p])
 _lib_selftest_wait = _sig("vcs_selftest_bounded_wait", _i32, [_p, _i64, _p])
 
 EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "vcs_plan_segments",
@@ -84,7 +100,9 @@ EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "
             "vcs_attn_bwd_workspace_size", "vcs_attn_bwd", "vcs_attn_bwd_noalloc", "vcs_grpo_loss_workspace_size",
             "vcs_grpo_loss", "vcs_group_advantage", "vcs_stream_fields", "vcs_compact_workspace_size",
             "vcs_compact_trainable", "vcs_attn_fwd_gathered", "vcs_attn_bwd_gathered_workspace_size",
-            "vcs_attn_bwd_gathered", "vcs_shared_prefix", "vcs_attn_fwd_reuse", "vcs_selftest_bounded_wait"]
+            "vcs_attn_bwd_gathered", "vcs_shared_prefix", "vcs_attn_fwd_reuse", "vcs_stream_positions", "vcs_rope_init",
+            "vcs_gather_rope", "vcs_gather_inverse_workspace_size", "vcs_gather_inverse", "vcs_gather_rope_bwd",
+            "vcs_selftest_bounded_wait"]
 
 LIB_PATH = _LIB_PATH
 
@@ -247,6 +265,41 @@ def vcs_compact_trainable(tok_loss_mask, num_tokens, idx, idx_capacity, count, w
                         _stream(stream))
 
 
+def vcs_stream_positions(cu_seqlens, num_segments, num_tokens, tok_src_step, step_img, step_txt, step_grid, num_steps,
+                         pos, dev_status, stream=None) -> int:
+    return _lib_positions(_ptr(cu_seqlens), num_segments, num_tokens, _ptr(tok_src_step), _ptr(step_img),
+                          _ptr(step_txt), _ptr(step_grid), num_steps, _ptr(pos), _ptr(dev_status), _stream(stream))
+
+
+def vcs_rope_init(rope, rot_dim, num_axes, sections, theta, interleaved) -> int:
+    arr = (ctypes.c_int32 * len(sections))(*sections) if sections is not None else None
+    return _lib_rope_init(_ptr(rope), rot_dim, num_axes, arr, theta, interleaved)
+
+
+def vcs_gather_rope(q_traj, k_traj, v_traj, traj_tokens, tok_gather, pos, num_tokens, hq, hkv, d, rope, q, k, v,
+                    dev_status, stream=None) -> int:
+    return _lib_gather_rope(_ptr(q_traj), _ptr(k_traj), _ptr(v_traj), traj_tokens, _ptr(tok_gather), _ptr(pos),
+                            num_tokens, hq, hkv, d, _ptr(rope), _ptr(q), _ptr(k), _ptr(v), _ptr(dev_status),
+                            _stream(stream))
+
+
+def vcs_gather_inverse_workspace_size(num_tokens: int) -> int:
+    return int(_lib_inverse_ws(num_tokens))
+
+
+def vcs_gather_inverse(tok_gather, num_tokens, traj_tokens, inv_off, inv_tok, dev_status, ws, ws_bytes,
+                       stream=None) -> int:
+    return _lib_inverse(_ptr(tok_gather), num_tokens, traj_tokens, _ptr(inv_off), _ptr(inv_tok), _ptr(dev_status),
+                        _ptr(ws), ws_bytes, _stream(stream))
+
+
+def vcs_gather_rope_bwd(dq, dk, dv, num_tokens, pos, inv_off, inv_tok, traj_tokens, hq, hkv, d, rope, dq_traj, dk_traj,
+                        dv_traj, dev_status, stream=None) -> int:
+    return _lib_gather_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), num_tokens, _ptr(pos), _ptr(inv_off), _ptr(inv_tok),
+                                traj_tokens, hq, hkv, d, _ptr(rope), _ptr(dq_traj), _ptr(dk_traj), _ptr(dv_traj),
+                                _ptr(dev_status), _stream(stream))
+
+
 def vcs_selftest_bounded_wait(dev_status, limit_cycles, stream=None) -> int:
     return _lib_selftest_wait(_ptr(dev_status), int(limit_cycles), _stream(stream))
 
@@ -406,6 +459,122 @@ def attn_bwd(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, softmax_scale: 
     if check:
         _check(int(ws[0].item()), "vcs_attn_bwd (device)")
     return dq, dk, dv
+
+
+def _expect(where: str, **tensors):
+    """Refuses tensors the kernels would misread: name=(tensor, dtype, shape), None in a shape matching any size.
+    They lie on the current device, contiguous."""
+    dev = None
+    for name, (t, dtype, shape) in tensors.items():
+        if not t.is_cuda:
+            raise ValueError(f"{where}: {name} is on {t.device}, not a CUDA device")
+        dev = torch.cuda.current_device() if dev is None else dev
+        if t.device.index != dev:
+            raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{dev}")
+        if t.dtype != dtype:
+            raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
+        if t.dim() != len(shape) or any(b is not None and a != b for a, b in zip(t.shape, shape)):
+            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+        if not t.is_contiguous():
+            raise ValueError(f"{where}: {name} is not contiguous")
+
+
+def _word(check: bool):
+    """The status word of a call that is checked, None for one that is not."""
+    return _host_words(1, torch.int32) if check else None
+
+
+def _checked(status: int, word, where: str):
+    """The call's status, and what its kernels left in `word` if there is one (synchronises)."""
+    if word is None:
+        return _check(status, where)
+    _done(status, where)
+    _check(word.tolist()[0], where + " (device)")
+
+
+def stream_positions(cu_seqlens, tok_src_step, step_img, step_txt, step_grid, stream=None, check=True):
+    """int32 [3, num_tokens]: the time, height and width positions of every segment token.  step_grid is
+    int32 [num_steps, 3], the frames, rows and columns of each step's screenshot."""
+    if stream is not None:
+        return _on_stream(stream, stream_positions, cu_seqlens, tok_src_step, step_img, step_txt, step_grid,
+                          check=check)
+    ns, nt = cu_seqlens.numel() - 1, tok_src_step.numel()
+    i32 = torch.int32
+    _expect("stream_positions", cu_seqlens=(cu_seqlens, i32, (None,)), tok_src_step=(tok_src_step, i32, (None,)),
+            step_img=(step_img, i32, (None,)), step_txt=(step_txt, i32, (step_img.numel(),)),
+            step_grid=(step_grid, i32, (step_img.numel(), 3)))
+    pos = torch.empty((3, nt), dtype=torch.int32, device=tok_src_step.device)
+    word = _word(check)
+    _checked(vcs_stream_positions(cu_seqlens, ns, nt, tok_src_step, step_img, step_txt, step_grid, step_img.numel(),
+                                  pos, word), word, "vcs_stream_positions")
+    return pos
+
+
+def rope_plan(d: int, sections=None, theta: float = 10000.0, rot_dim: Optional[int] = None,
+              interleaved: bool = False) -> VcsRope:
+    """The rotation of the first rot_dim (default: all d) dims of a head: axis a turns the next sections[a]
+    pairs (default: one axis), pair i by theta^(-2i / rot_dim) radians a position."""
+    rot = d if rot_dim is None else rot_dim
+    rope = VcsRope()
+    sections = (rot // 2,) if sections is None else tuple(sections)
+    _check(vcs_rope_init(rope, rot, len(sections), sections, theta, int(interleaved)), "vcs_rope_init")
+    return rope
+
+
+def gather_rope(q_traj, k_traj, v_traj, tok_gather, pos, rope: VcsRope, stream=None, check=True):
+    """gather with Q and K rotated by pos [axes, num_tokens]; tok_gather None: the rows are the segments'."""
+    if stream is not None:
+        return _on_stream(stream, gather_rope, q_traj, k_traj, v_traj, tok_gather, pos, rope, check=check)
+    nt = q_traj.shape[0] if tok_gather is None else tok_gather.numel()
+    bf16, i32 = torch.bfloat16, torch.int32
+    _expect("gather_rope", q_traj=(q_traj, bf16, (None, None, None)))
+    tt, hq, d = q_traj.shape
+    _expect("gather_rope", k_traj=(k_traj, bf16, (tt, None, d)), v_traj=(v_traj, bf16, tuple(k_traj.shape)),
+            pos=(pos, i32, (rope.num_axes, nt)), **({} if tok_gather is None else dict(tok_gather=(tok_gather, i32, (nt,)))))
+    hkv = k_traj.shape[1]
+    q = torch.empty((nt, hq, d), dtype=q_traj.dtype, device=q_traj.device)
+    k = torch.empty((nt, hkv, d), dtype=k_traj.dtype, device=q_traj.device)
+    v = torch.empty((nt, hkv, d), dtype=v_traj.dtype, device=q_traj.device)
+    word = _word(check)
+    _checked(vcs_gather_rope(q_traj, k_traj, v_traj, tt, tok_gather, pos, nt, hq, hkv, d, rope, q, k, v, word), word,
+             "vcs_gather_rope")
+    return q, k, v
+
+
+def gather_inverse(tok_gather, traj_tokens: int, stream=None, check=True):
+    """(inv_off [traj_tokens + 1], inv_tok [num_tokens]) int32: the segment tokens of every trajectory token."""
+    if stream is not None:
+        return _on_stream(stream, gather_inverse, tok_gather, traj_tokens, check=check)
+    _expect("gather_inverse", tok_gather=(tok_gather, torch.int32, (None,)))
+    nt, dev = tok_gather.numel(), tok_gather.device
+    off = torch.empty(traj_tokens + 1, dtype=torch.int32, device=dev)
+    tok = torch.empty(nt, dtype=torch.int32, device=dev)
+    nb = vcs_gather_inverse_workspace_size(nt)
+    word = _word(check)
+    _checked(vcs_gather_inverse(tok_gather, nt, traj_tokens, off, tok, word, _ws(nb, dev), nb), word,
+             "vcs_gather_inverse")
+    return off, tok
+
+
+def gather_rope_bwd(dq, dk, dv, pos, inv_off, inv_tok, rope: VcsRope, stream=None, check=True):
+    """Gradients of gather_rope's inputs from those of its outputs: rotated back and summed over each trajectory
+    token's copies (gather_inverse's lists; both None: the rows are the segments')."""
+    if stream is not None:
+        return _on_stream(stream, gather_rope_bwd, dq, dk, dv, pos, inv_off, inv_tok, rope, check=check)
+    bf16, i32 = torch.bfloat16, torch.int32
+    _expect("gather_rope_bwd", dq=(dq, bf16, (None, None, None)))
+    nt, hq, d = dq.shape
+    _expect("gather_rope_bwd", dk=(dk, bf16, (nt, None, d)), dv=(dv, bf16, tuple(dk.shape)),
+            pos=(pos, i32, (rope.num_axes, nt)))
+    if inv_off is not None:
+        _expect("gather_rope_bwd", inv_off=(inv_off, i32, (None,)), inv_tok=(inv_tok, i32, (nt,)))
+    hkv = dk.shape[1]
+    tt = nt if inv_off is None else inv_off.numel() - 1
+    out = [torch.empty((tt, h, d), dtype=dq.dtype, device=dq.device) for h in (hq, hkv, hkv)]
+    word = _word(check)
+    _checked(vcs_gather_rope_bwd(dq, dk, dv, nt, pos, inv_off, inv_tok, tt, hq, hkv, d, rope, *out, word), word,
+             "vcs_gather_rope_bwd")
+    return tuple(out)
 
 
 def shared_prefix(cu_seqlens, seg_traj, tok_gather, stream=None):

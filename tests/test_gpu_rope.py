@@ -1,0 +1,312 @@
+"""GPU parity of the rotary calls: positions and inverse exactly, rotated rows and gradients against fp64.
+
+Tolerances: a result is rounded once to bf16 (half a step, 2^-8 of it).  Before that a rotated pair
+(a, b) is off by at most 1e-6 (|a| + |b|): sincospi within 2 ulp of a value below 1 (2.4e-7), its
+argument's rounding to 24 bits and to 2^-32 of a turn (1e-7 radians), two roundings of fp32 (1.2e-7).  The
+frequency in turns is rounded to 2^-52 of itself, 2^-51 radians a position with the oracle's own angle.
+A sum of m copies adds at most m 2^-24 of the terms' sizes.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rope as orope
+from oracle import segments as oseg
+from paper_2607_11185_gb300 import workloads
+from tests.gpu_cases import random_steps
+
+pytestmark = pytest.mark.gpu
+HALF = 2.0 ** -8
+
+
+def _vcs():
+    from paper_2607_11185_gb300 import vcs
+    return vcs
+
+
+def dev(*xs):
+    return [torch.from_numpy(np.ascontiguousarray(x, np.int32)).cuda() for x in xs]
+
+
+def grids(img, rng, frames=2):
+    """A T x H x W for every screenshot size."""
+    out = np.zeros((len(img), 3), np.int32)
+    for i, n in enumerate(img):
+        if n == 0:
+            continue
+        t = int(rng.choice([x for x in range(1, frames + 1) if n % x == 0]))
+        h = int(rng.choice([x for x in range(1, n // t + 1) if (n // t) % x == 0]))
+        out[i] = t, h, n // t // h
+    return out
+
+
+# ------------------------------------------------------------------ positions
+def check_positions(lay, img, txt, grid):
+    vcs = _vcs()
+    pos = vcs.stream_positions(*dev(lay["cu_seqlens"], lay["tok_src_step"], img, txt, grid))
+    want = orope.positions(lay["cu_seqlens"], lay["tok_src_step"], img, txt, grid)
+    assert pos.shape == (3, len(lay["tok_src_step"])) and np.array_equal(pos.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_positions_random(seed):
+    cu, img, txt = random_steps(seed, max_traj=6, max_T=30)
+    lay = oseg.build(cu, img, txt, seed % 4 + 1, seed % 3)
+    check_positions(lay, img, txt, grids(img, np.random.default_rng(seed)))
+
+
+@pytest.mark.parametrize("name,window,keep", [("tiny", 2, 0), ("traj8_w3", 3, 0), ("traj8_w3", 1, 1)])
+def test_positions_workloads(name, window, keep):
+    cu, img, txt = workloads.draw_steps(workloads.WORKLOADS[name])
+    check_positions(oseg.build(cu, img, txt, window, keep), img, txt, grids(img, np.random.default_rng(3)))
+
+
+def test_positions_many_steps_and_chunks():
+    # one segment of 700 steps (three tiles of steps) and 30,000 tokens (four chunks), one of 5 tokens
+    rng = np.random.default_rng(5)
+    img = rng.integers(0, 60, size=705).astype(np.int32)
+    txt = rng.integers(0, 30, size=705).astype(np.int32)
+    cu = np.array([0, 700, 705], np.int32)
+    check_positions(oseg.build(cu, img, txt, 1000, 0), img, txt, grids(img, rng))
+
+
+def test_positions_device_checks():
+    vcs = _vcs()
+    img, txt, grid = [6, 4], [2, 1], [[1, 2, 3], [1, 1, 4]]
+    cu, src = [0, 13], [0] * 8 + [1] * 5
+    vcs.stream_positions(*dev(cu, src, img, txt, grid))
+    for bad in (dict(grid=[[1, 2, 4], [1, 1, 4]]), dict(grid=[[-1, -2, 3], [1, 1, 4]]),
+                dict(grid=[[1, 65536, 65536], [1, 1, 4]]), dict(src=[0] * 7 + [1] * 6), dict(src=[2] * 13),
+                dict(src=[-1] * 13), dict(src=[1] * 5 + [0] * 8), dict(src=[0, 1, 0, 1, 0, 1, 0, 1, 0, 1, 0, 1, 1]),
+                dict(cu=[0, 12]), dict(cu=[1, 13]), dict(cu=[0, 14])):
+        x = dict(cu=cu, src=src, img=img, txt=txt, grid=grid) | bad
+        with pytest.raises(vcs.VcsError) as e:
+            vcs.stream_positions(*dev(x["cu"], x["src"], x["img"], x["txt"], x["grid"]))
+        assert e.value.status == 6, bad
+
+
+def test_positions_empty():
+    vcs = _vcs()
+    i = torch.zeros(0, dtype=torch.int32, device="cuda")
+    pos = vcs.stream_positions(torch.zeros(1, dtype=torch.int32, device="cuda"), i, i, i, i.view(0, 3))
+    assert pos.shape == (3, 0)
+
+
+# ------------------------------------------------------------------ inverse map
+@pytest.mark.parametrize("n,t", [(0, 0), (0, 7), (1, 1), (1, 5000), (31, 3), (4096, 1), (4097, 255), (9000, 256),
+                                 (50_000, 70_000), (300_000, 65_535), (20_000, 17_000_000)])
+def test_inverse(n, t):
+    vcs = _vcs()
+    rng = np.random.default_rng(n + t)
+    gat = rng.integers(0, max(t, 1), size=n)
+    off, tok = vcs.gather_inverse(*dev(gat), t)
+    order = np.argsort(gat, kind="stable")
+    assert np.array_equal(tok.cpu().numpy(), order)
+    assert np.array_equal(off.cpu().numpy(), np.searchsorted(gat[order], np.arange(t + 1)))
+
+
+def test_inverse_of_a_layout_and_bad_entries():
+    vcs = _vcs()
+    cu, img, txt = random_steps(3)
+    lay = oseg.build(cu, img, txt, 2, 1)
+    t = int(img.sum() + txt.sum())
+    off, tok = vcs.gather_inverse(*dev(lay["tok_gather"]), t)
+    want = orope.inverse(lay["tok_gather"], t)
+    assert np.array_equal(off.cpu().numpy(), want[0]) and np.array_equal(tok.cpu().numpy(), want[1])
+    bad = np.array([2, -1, 0, 7, 2, 5, -2 ** 31])
+    with pytest.raises(vcs.VcsError) as e:
+        vcs.gather_inverse(*dev(bad), 5)
+    assert e.value.status == 6
+    off, tok = vcs.gather_inverse(*dev(bad), 5, check=False)
+    assert off.tolist() == [0, 1, 1, 3, 3, 3] and tok.tolist() == [2, 0, 4, 1, 3, 5, 6]
+
+
+# ------------------------------------------------------------------ rotation
+def bound(ref, size, pos, copies=1):
+    far = np.abs(np.asarray(pos, np.float64)).max() if np.size(pos) else 0.0
+    slip = (1e-6 + far * 2.0 ** -51 + copies * 2.0 ** -24) * size
+    return HALF * (np.abs(ref) + slip) + slip
+
+
+def pair_size(x, rot, interleaved):
+    """|a| + |b| of the pair each dim is in, and the dim's own size where it is not turned."""
+    y = np.abs(x).copy()
+    a, b = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    y[..., a] = y[..., b] = np.abs(x[..., a]) + np.abs(x[..., b])
+    return y
+
+
+def rows(seed, n, h, d):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn((n, h, d), generator=g, device="cuda").bfloat16()
+
+
+CASES = [  # hq, hkv, d, rot, sections, interleaved
+    (2, 1, 64, 64, (8, 12, 12), False), (2, 1, 64, 64, (8, 12, 12), True), (28, 4, 128, 128, (16, 24, 24), False),
+    (5, 5, 128, 96, (16, 16, 16), False), (3, 3, 128, 48, (24,), True), (1, 1, 16, 16, (4, 4), False),
+    (1, 1, 24, 16, (8,), True), (7, 1, 256, 256, (32, 32, 32, 32), False), (2, 2, 256, 240, (60, 60), True),
+    (3, 1, 72, 64, (0, 32), False)]
+
+
+@pytest.mark.parametrize("hq,hkv,d,rot,sections,inter", CASES)
+@pytest.mark.parametrize("n,t", [(1, 1), (37, 20), (700, 90)])
+def test_gather_rope_and_backward(hq, hkv, d, rot, sections, inter, n, t):
+    vcs = _vcs()
+    rng = np.random.default_rng(n + d)
+    gat = rng.integers(0, t, size=n)
+    pos = rng.integers(0, 70_000, size=(len(sections), n))
+    rope = vcs.rope_plan(d, sections, 1e6, rot_dim=rot, interleaved=inter)
+    inv, axis = orope.frequencies(rot, sections, 1e6)
+    q, k, v = rows(1, t, hq, d), rows(2, t, hkv, d), rows(3, t, hkv, d)
+    got = vcs.gather_rope(q, k, v, *dev(gat, pos), rope)
+    assert torch.equal(got[2], v[torch.from_numpy(gat).cuda()])
+    for x, y in ((q, got[0]), (k, got[1])):
+        src = x.double().cpu().numpy()[gat]
+        ref = orope.rotate(src, pos, inv, axis, inter)
+        assert (np.abs(y.double().cpu().numpy() - ref) <= bound(ref, pair_size(src, rot, inter), pos)).all()
+    dq, dk, dv = rows(4, n, hq, d), rows(5, n, hkv, d), rows(6, n, hkv, d)
+    off, tok = vcs.gather_inverse(*dev(gat), t)
+    back = vcs.gather_rope_bwd(dq, dk, dv, *dev(pos), off, tok, rope)
+    copies = int(np.bincount(gat).max())
+    for x, y, turn in ((dq, back[0], True), (dk, back[1], True), (dv, back[2], False)):
+        src = x.double().cpu().numpy()
+        ref = orope.rotate(src, pos, inv, axis, inter, back=True) if turn else src
+        size = pair_size(src, rot, inter) if turn else np.abs(src)
+        ref, size = orope.scatter(ref, gat, t), orope.scatter(size, gat, t)
+        assert (np.abs(y.double().cpu().numpy() - ref) <= bound(ref, size, pos, copies)).all()
+    again = vcs.gather_rope_bwd(dq, dk, dv, *dev(pos), off, tok, rope)
+    assert all(torch.equal(a, b) for a, b in zip(back, again))
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_identity_map_any_position(inter):
+    # no map: row n is token n; positions of any int32, exact angles far out and negative ones
+    vcs = _vcs()
+    pos = np.array([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 123_456_789, 1000, -77, 5, 6, 7]])
+    n = pos.shape[1]
+    rope = vcs.rope_plan(64, (32,), 1e4, interleaved=inter)
+    inv, axis = orope.frequencies(64, (32,), 1e4)
+    q, k, v = rows(1, n, 4, 64), rows(2, n, 2, 64), rows(3, n, 2, 64)
+    got = vcs.gather_rope(q, k, v, None, *dev(pos), rope)
+    back = vcs.gather_rope_bwd(q, k, v, *dev(pos), None, None, rope)
+    assert torch.equal(got[2], v) and torch.equal(back[2], v) and torch.equal(got[0][0], q[0])
+    for x, y, z in ((q, got[0], back[0]), (k, got[1], back[1])):
+        src = x.double().cpu().numpy()
+        for res, b in ((y, False), (z, True)):
+            ref = orope.rotate(src, pos, inv, axis, inter, back=b)
+            assert (np.abs(res.double().cpu().numpy() - ref) <= bound(ref, pair_size(src, 64, inter), pos)).all()
+
+
+def test_changed_frequencies_and_axes():
+    # axes by turns, a frequency of 0, a negative one and one of many turns a position
+    vcs = _vcs()
+    rng = np.random.default_rng(8)
+    rope = vcs.rope_plan(32, (6, 5, 5), 100.0)
+    inv, axis = orope.frequencies(32, (6, 5, 5), 100.0)
+    axis = np.arange(16) % 3
+    inv[3], inv[5], inv[7], inv[9] = 0.0, -0.25, 40.0, -1e-300
+    for i in range(16):
+        rope.inv_freq[i], rope.pair_axis[i] = inv[i], int(axis[i])
+    pos = rng.integers(0, 430, size=(3, 50))
+    x = rows(1, 50, 2, 32)
+    got = vcs.gather_rope(x, x, x, None, *dev(pos), rope)
+    src = x.double().cpu().numpy()
+    ref = orope.rotate(src, pos, inv, axis)
+    assert (np.abs(got[0].double().cpu().numpy() - ref) <= bound(ref, pair_size(src, 32, False), 40 * pos)).all()
+
+
+def test_many_copies_and_none():
+    # a token of 1,000 copies, some of 7 to 9 (around a warp's batch of angles), some of none
+    vcs = _vcs()
+    gat = np.concatenate([np.full(1000, 3), np.repeat([1, 5, 6], [7, 8, 9]), [9]])
+    n, t = len(gat), 12
+    gat = np.random.default_rng(0).permutation(gat)
+    pos = np.random.default_rng(1).integers(0, 5000, size=(3, n))
+    rope = vcs.rope_plan(64, (8, 12, 12), 1e6)
+    inv, axis = orope.frequencies(64, (8, 12, 12), 1e6)
+    dq, dk, dv = rows(4, n, 3, 64), rows(5, n, 1, 64), rows(6, n, 1, 64)
+    back = vcs.gather_rope_bwd(dq, dk, dv, *dev(pos), *vcs.gather_inverse(*dev(gat), t), rope)
+    for x, y, turn in ((dq, back[0], True), (dk, back[1], True), (dv, back[2], False)):
+        src = x.double().cpu().numpy()
+        ref = orope.scatter(orope.rotate(src, pos, inv, axis, back=True) if turn else src, gat, t)
+        size = orope.scatter(pair_size(src, 64, False), gat, t)
+        assert (np.abs(y.double().cpu().numpy() - ref) <= bound(ref, size, pos, 1000)).all()
+        assert not y[[0, 2, 4, 7, 8, 10, 11]].any()
+    assert torch.equal(back[2][9], dv[int(np.nonzero(gat == 9)[0][0])])
+
+
+def test_one_copy_keeps_the_bits_of_v():
+    vcs = _vcs()
+    v = torch.tensor([0.0, -0.0, float("inf"), -float("inf"), 1e-40, -1e-40, 3.0, -5.0] * 2).bfloat16().cuda().view(1, 1, 16)
+    pos = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    rope = vcs.rope_plan(16)
+    x = torch.ones_like(v)
+    for got in (vcs.gather_rope(x, x, v, pos[0], pos, rope)[2],
+                vcs.gather_rope_bwd(x, x, v, pos, one, pos[0], rope)[2]):
+        assert torch.equal(got.view(torch.int16), v.view(torch.int16))
+
+
+def test_device_checks_leave_rows_out():
+    vcs = _vcs()
+    x = rows(1, 6, 2, 64)
+    rope = vcs.rope_plan(64)
+    gat, pos = dev([0, 6, 2, -1, 5], np.zeros((1, 5)))
+    with pytest.raises(vcs.VcsError) as e:
+        vcs.gather_rope(x, x, x, gat, pos, rope)
+    assert e.value.status == 6
+    out = [torch.full((5, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+    assert vcs.vcs_gather_rope(x, x, x, 6, gat, pos, 5, 2, 2, 64, rope, *out, None) == 0
+    for o in out:
+        assert torch.equal(o[[0, 2, 4]], x[[0, 2, 5]]) and (o[[1, 3]] == 7).all()
+    y, pos6 = rows(2, 6, 2, 64), torch.zeros((1, 6), dtype=torch.int32, device="cuda")
+    for off, tok in (([0, 2, 7, 7], [0, 1, 2, 3, 4, 5]), ([0, 2, 1, 6], [0, 1, 2, 3, 4, 5]), ([-1, 2, 3, 6], [0, 1, 2, 3, 4, 5]),
+                     ([0, 2, 3, 6], [0, 6, 2, 3, 4, 5]), ([0, 2, 3, 6], [0, -1, 2, 3, 4, 5])):
+        with pytest.raises(vcs.VcsError) as e:
+            vcs.gather_rope_bwd(y, y, y, pos6, *dev(off, tok), rope)
+        assert e.value.status == 6, (off, tok)
+    got = vcs.gather_rope_bwd(y, y, y, pos6, *dev([0, 2, 3, 6], [0, -1, 2, 3, 4, 9]), rope, check=False)
+    assert torch.equal(got[2][0], y[0]) and torch.equal(got[2][1], y[2])
+    assert torch.equal(got[2][2], (y[3].float() + y[4].float()).bfloat16())
+
+
+def test_wrappers_refuse_other_layouts():
+    vcs = _vcs()
+    rope = vcs.rope_plan(64)
+    x, pos = rows(1, 6, 2, 64), torch.zeros((1, 6), dtype=torch.int32, device="cuda")
+    gat = torch.zeros(6, dtype=torch.int32, device="cuda")
+    for bad in ((x.float(), x, x, gat, pos), (x, x[:5], x, gat, pos), (x, x, x[:, :1], gat, pos),
+                (x, x, x, gat.long(), pos), (x, x, x, gat, pos[:, :5]), (x, x, x, gat, pos.repeat(3, 1)),
+                (rows(1, 12, 2, 64)[::2], x, x, gat, pos), (x, x.cpu(), x, gat, pos), (x, x, x, gat, pos.view(6, 1))):
+        with pytest.raises(ValueError):
+            vcs.gather_rope(*bad, rope)
+
+
+def test_on_a_stream_and_in_a_graph():
+    vcs = _vcs()
+    rng = np.random.default_rng(4)
+    n, t = 900, 300
+    gat, pos = dev(rng.integers(0, t, size=n), rng.integers(0, 999, size=(3, n)))
+    rope = vcs.rope_plan(64, (8, 12, 12))
+    q, k, v = rows(1, t, 4, 64), rows(2, t, 2, 64), rows(3, t, 2, 64)
+    off, tok = vcs.gather_inverse(gat, t)
+    want = vcs.gather_rope(q, k, v, gat, pos, rope)
+    wantb = vcs.gather_rope_bwd(*want, pos, off, tok, rope)
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)
+    side.wait_stream(torch.cuda.current_stream())
+    o2 = vcs.gather_inverse(gat, t, stream=side)
+    got = vcs.gather_rope(q, k, v, gat, pos, rope, stream=side)
+    gotb = vcs.gather_rope_bwd(*got, pos, *o2, rope, stream=side.cuda_stream)
+    assert all(torch.equal(a, b) for a, b in zip((*got, *gotb, *o2), (*want, *wantb, off, tok)))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o3 = vcs.gather_inverse(gat, t, check=False)
+        got = vcs.gather_rope(q, k, v, gat, pos, rope, check=False)
+        gotb = vcs.gather_rope_bwd(*got, pos, *o3, rope, check=False)
+    q.copy_(rows(9, t, 4, 64))
+    gat.copy_(torch.flip(gat, (0,)))
+    g.replay()
+    want = vcs.gather_rope(q, k, v, gat, pos, rope)
+    wantb = vcs.gather_rope_bwd(*want, pos, *vcs.gather_inverse(gat, t), rope)
+    assert all(torch.equal(a, b) for a, b in zip((*got, *gotb), (*want, *wantb)))
