@@ -307,6 +307,38 @@ vcs_status vcs_attn_fwd_reuse(const void* q, const void* k, const void* v, const
                               size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Attention with a sliding window and sinks, forward and backward.  The paper
+ * attends to whole segments; these calls are vcs_attn_fwd / vcs_attn_bwd for
+ * policies with local layers: token i of a segment sees token j of it for
+ * j <= i and (i - j < window or j < sinks).  Every token sees itself; a window
+ * of the longest segment or more is causal attention.
+ *   window      >= 1: the tokens a query sees, up to and with its own
+ *   sinks       >= 0: first tokens of each segment that stay visible
+ * Other arguments, layouts, workspaces and errors as for vcs_attn_fwd /
+ * vcs_attn_bwd (the forward's workspace is vcs_attn_fwd_workspace_size), plus
+ * VCS_ERR_INVALID_ARG for a window or sinks outside their ranges.  The backward
+ * takes the forward's o and lse for the same window and sinks.
+ * The work grows with window + sinks, not with the segment.  Invisible scores
+ * never reach a result, but a NaN or infinity in a v (or, backward, q, k, v or
+ * dout) row may reach every row whose 128-row tile meets it: pass finite rows.
+ * dk and dv are summed in one order; dq by fp32 atomic additions, whose order,
+ * and with it dq's last bits, varies from run to run, as in vcs_attn_bwd.
+ * ------------------------------------------------------------------------ */
+vcs_status vcs_attn_fwd_window(const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                               int32_t num_segments, int64_t num_tokens, int32_t max_seqlen, int32_t hq, int32_t hkv,
+                               int32_t d, float softmax_scale, int32_t window, int32_t sinks, void* o, float* lse,
+                               void* ws, size_t ws_bytes, void* stream);
+
+size_t vcs_attn_bwd_window_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t max_seqlen, int32_t hq,
+                                          int32_t hkv, int32_t d, int32_t window, int32_t sinks);
+
+vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse,
+                               const void* dout, const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
+                               int32_t max_seqlen, int32_t hq, int32_t hkv, int32_t d, float softmax_scale,
+                               int32_t window, int32_t sinks, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/* ------------------------------------------------------------------------
  * Rotary positions with several axes.  The paper's path applies none; these
  * calls give a policy that uses them its positions and rotates the rows on
  * their way between trajectory and segment layout.  Positions start over in

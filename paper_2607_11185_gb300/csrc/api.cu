@@ -237,6 +237,61 @@ size_t vcs_attn_bwd_workspace_size(int32_t num_segments, int64_t num_tokens, int
   return attn_bwd_ws_bytes(a);
 }
 
+// ---------------------------------------------------------------- sliding window and sinks
+static vcs_status check_window(AttnArgs& a, int32_t window, int32_t sinks) {
+  if (window < 1 || sinks < 0) return VCS_ERR_INVALID_ARG;
+  a.window = window;
+  a.sinks = sinks;
+  return check_attn(a);
+}
+
+vcs_status vcs_attn_fwd_window(const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                               int32_t num_segments, int64_t num_tokens, int32_t max_seqlen, int32_t hq, int32_t hkv,
+                               int32_t d, float softmax_scale, int32_t window, int32_t sinks, void* o, float* lse,
+                               void* ws, size_t ws_bytes, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_attn_fwd_window");
+  AttnArgs a = make_args(q, k, v, cu_seqlens, num_segments, num_tokens, max_seqlen, hq, hkv, d, softmax_scale);
+  const vcs_status s = check_window(a, window, sinks);
+  if (s != VCS_OK) return s;
+  if (o == nullptr || lse == nullptr || !aligned16(o) || !aligned16(lse)) return VCS_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < attn_fwd_ws_bytes(a) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  a.status = static_cast<int32_t*>(ws);
+  cudaStream_t st = as_stream(stream);
+  if (num_tokens == 0 || num_segments == 0) return clear_header(ws, st);
+  if (launch_attn_fwd_window(a, o, lse, ws, st) != cudaSuccess) return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+size_t vcs_attn_bwd_window_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t max_seqlen, int32_t hq,
+                                          int32_t hkv, int32_t d, int32_t window, int32_t sinks) {
+  AttnArgs a = make_args(nullptr, nullptr, nullptr, nullptr, num_segments, num_tokens, max_seqlen, hq, hkv, d, 0.f);
+  a.window = window;
+  a.sinks = sinks;
+  return attn_bwd_ws_bytes(a);
+}
+
+vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, const void* o, const float* lse,
+                               const void* dout, const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
+                               int32_t max_seqlen, int32_t hq, int32_t hkv, int32_t d, float softmax_scale,
+                               int32_t window, int32_t sinks, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                               void* stream) {
+  vcs::ApiRange nvtx_range("vcs_attn_bwd_window");
+  AttnArgs a = make_args(q, k, v, cu_seqlens, num_segments, num_tokens, max_seqlen, hq, hkv, d, softmax_scale);
+  const vcs_status s = check_window(a, window, sinks);
+  if (s != VCS_OK) return s;
+  const void* outs[6] = {o, lse, dout, dq, dk, dv};
+  for (const void* p : outs)
+    if (p == nullptr || !aligned16(p)) return VCS_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < attn_bwd_ws_bytes(a) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  a.status = static_cast<int32_t*>(ws);
+  cudaStream_t st = as_stream(stream);
+  if (num_tokens == 0 || num_segments == 0) return clear_header(ws, st);
+  if (launch_attn_bwd(a, o, lse, dout, dq, dk, dv, ws, st) != cudaSuccess) return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
 // ---------------------------------------------------------------- rotary positions
 vcs_status vcs_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
                                 const int32_t* tok_src_step, const int32_t* step_img, const int32_t* step_txt,

@@ -282,13 +282,40 @@ __device__ __forceinline__ void drain_d64(const uint32_t (&v)[2][32], int lane, 
     }
 }
 
+// Sliding window and sinks: key j is visible to query i >= j if i - j < window or j < sinks.  A key tile past
+// the sinks meets the row tiles up to its last key's window; a tile that holds sinks meets all of them, and
+// would run long after the others of a long segment.  So its row tiles are dealt to up to `parts` CTAs, in
+// runs of `chunk`; each leaves its dK and dV in fp32 in a slot of `acc`, and bwd_sink_sum adds a tile's slots
+// in order (the sum does not depend on which CTA comes first).  chunk is at least 16 row tiles, twice a
+// window's and a quarter of what an SM has to do, so that a launch of many segments, or of short ones, splits
+// none and pays nothing.  One segment of 32,768, window 1,024, sinks 4, at 28/4/128: see launch_bwd_d.
+struct WinArgs {
+  int32_t window, sinks;   // at most max_seqlen (and the window at least 1)
+  int32_t tiles;           // key tiles that hold sinks
+  int32_t parts, chunk;    // CTAs a sink tile may take (1: it is not split), row tiles of each
+  float* acc;              // slots of [kv head][sink tile], each dK then dV, [128][D]
+};
+// A segment has split sink tiles only if it is longer than chunk row tiles.  Part p of it begins chunk * p row
+// tiles into it; at most one part that is no segment's first and one that is begin in any run of chunk * 128
+// tokens of the packed buffer, which gives each of them a slot.
+__host__ __device__ __forceinline__ int64_t sink_slots(int64_t num_tokens, int chunk) {
+  return 2 * (num_tokens / ((int64_t)chunk * 128) + 1);
+}
+__device__ __forceinline__ int64_t sink_slot(int start, int p, int chunk) {
+  return 2 * ((start + (int64_t)p * chunk * 128) / ((int64_t)chunk * 128)) + (p == 0 ? 1 : 0);
+}
+__device__ __forceinline__ int sink_parts(const WinArgs& w, int rows) {  // of a sink tile with `rows` row tiles
+  return w.parts > 1 ? (rows + w.chunk - 1) / w.chunk : 1;
+}
+
 // GATHER: Q, K and V are trajectory-layout tensors read through tok_gather, one warp per
 // tile (TMA gather4 with the 2-D maps tm_q/k/v, or tiled loads with the 3-D maps
 // tm_qr/kr/vr and tm_qs/ks/vs, 128- and 32-row boxes, where a tile or a 32-row group is one
 // run of consecutive trajectory rows), and dQ, dK, dV are added in fp32 to trajectory-layout
 // accumulators (dq_acc, dk_acc, dv_acc) at row tok_gather[token]; otherwise segment-layout tiled
 // loads, dq_acc in segment layout, bf16 dK, dV, and the other maps unused.
-template <int D, bool GATHER>
+// WIN: a sliding window and sinks (WinArgs below).
+template <int D, bool GATHER, bool WIN>
 __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     bwd_main(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
              const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do,
@@ -299,7 +326,7 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
              int32_t traj_tokens, float* __restrict__ dk_acc, float* __restrict__ dv_acc,
              const __grid_constant__ CUtensorMap tm_qr, const __grid_constant__ CUtensorMap tm_kr,
              const __grid_constant__ CUtensorMap tm_vr, const __grid_constant__ CUtensorMap tm_qs,
-             const __grid_constant__ CUtensorMap tm_ks, const __grid_constant__ CUtensorMap tm_vs) {
+             const __grid_constant__ CUtensorMap tm_ks, const __grid_constant__ CUtensorMap tm_vs, const WinArgs win) {
   using C = Bwd<D>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = smem_raw;
@@ -317,13 +344,23 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     n = (int)(t / tail_groups);
     sg = ngroups - tail_groups + (int)(t % tail_groups);
   }
+  int part = 0;
+  if constexpr (WIN) {  // the sink tiles' further parts come first
+    const int more = win.tiles * (win.parts - 1);
+    if (n < more) {
+      part = 1 + n / win.tiles;
+      n %= win.tiles;
+    } else {
+      n -= more;
+    }
+  }
   const int seg = sg / hkv;
   const int g = sg - seg * hkv;
   const int start = cu_seqlens[seg];
   const int end = cu_seqlens[seg + 1];
   if (start < 0 || end < start || end > num_tokens || end - start > max_seqlen ||
       (seg == 0 && start != 0) || (seg == num_segments - 1 && end != num_tokens)) {
-    if (threadIdx.x == 0 && n == 0 && g == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
+    if (threadIdx.x == 0 && n == 0 && g == 0 && part == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
     return;
   }
   const int L = end - start;
@@ -338,8 +375,21 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
   // CTAs that have a key tile)
   if (*reinterpret_cast<volatile int32_t*>(status) == VCS_ERR_DEVICE_TIMEOUT) return;
   const int G = hq / hkv;
-  const int nsub = (L - n * C::BM + C::BQ - 1) / C::BQ;  // 128-row query tiles at or after this key tile
-  const int U = G * nsub;
+  int nsub = (L - n * C::BM + C::BQ - 1) / C::BQ;  // 128-row query tiles at or after this key tile
+  int sub0 = 0, parts = 1;                         // WIN: the first of this CTA's, the CTAs of the tile
+  if constexpr (WIN) {
+    if (n * C::BM >= win.sinks) {
+      nsub = min(nsub, (win.window + C::BM - 2) / C::BQ + 1);
+    } else {
+      parts = sink_parts(win, nsub);
+      if (part >= parts) return;
+      if (parts > 1) {
+        sub0 = part * win.chunk;
+        nsub = min(nsub, sub0 + win.chunk);
+      }
+    }
+  }
+  const int U = G * (nsub - sub0);
   // Tile u covers query rows n*BM + sub*BQ ... +BQ-1 of one head.  d = 128: swept from the segment
   // end toward the key tile with the G heads of one row block in turn, so that the key tiles of one
   // (segment, kv head) running together meet the same Q/dO/dQ lines in L2.  d = 64: head by head
@@ -347,10 +397,11 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
   // tiles that run together are on different rows of dQ.
   struct Walk {  // tile u's row block and head, stepped without divisions
     int sub, head, first, count;  // first head and heads (d = 128); row blocks and last head + 1 (d = 64)
+    int low;                      // WIN: the first row block
     __device__ __forceinline__ void next() {
       if constexpr (D == 64) {
         if (++sub == first) {
-          sub = 0;
+          sub = WIN ? low : 0;
           ++head;
         }
       } else if (++head == first + count) {
@@ -358,9 +409,9 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
         --sub;
       }
     }
-    __device__ __forceinline__ bool live() const { return D == 64 ? head < count : sub >= 0; }
+    __device__ __forceinline__ bool live() const { return D == 64 ? head < count : sub >= (WIN ? low : 0); }
   };
-  const Walk walk0 = D == 64 ? Walk{0, g * G, nsub, g * G + G} : Walk{nsub - 1, g * G, g * G, G};
+  const Walk walk0 = D == 64 ? Walk{sub0, g * G, nsub, g * G + G, sub0} : Walk{nsub - 1, g * G, g * G, G, sub0};
   // lse and D of query i of w's tile, as loaded: scaled only where they are staged
   auto row_terms = [&](const Walk& w, int i, bool mine, float& l, float& dd) {
     l = __int_as_float(0x7f800000);  // +inf: query outside the segment -> P = 0
@@ -663,6 +714,11 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
       // the query rows are the key tile's own: mask keys after queries (column c of the
       // warpgroup's half hf is hidden from key row r when c < dlim - 64 hf)
       const int dlim = wc.sub == 0 ? r - 32 * k : 0;
+      // and keys behind the query's window, unless they are sinks (column c is hidden when c >= wlim - 64 hf)
+      int wlim = C::BQ;
+      if constexpr (WIN) {
+        if (n * C::BM + r >= win.sinks) wlim = win.window + r - wc.sub * C::BQ - 32 * k;
+      }
       wc.next();
       const uint32_t rt = rt_u32 + (u & 1) * 1024;
       if constexpr (!C::ROW_WARP) {
@@ -727,6 +783,14 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
 #pragma unroll
           for (int c = 0; c < 16; ++c)
             if (c < hide) x[x0 + c] = 0u;
+        }
+        if constexpr (WIN) {
+          const int from = wlim - 64 * (ch >> 1) - x0;
+          if (from < 16) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (c >= from) x[x0 + c] = 0u;
+          }
         }
         uint32_t pk[8];
 #pragma unroll
@@ -800,7 +864,21 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
       tc_fence_after();
       // warpgroup 1 writes dK, warpgroup 2 writes dV (key row r on the TMEM lane)
       const uint32_t col = k == 0 ? C::TM_DK : C::TM_DV;
-      if constexpr (GATHER) {  // fp32 add at the key's trajectory row
+      if (WIN && parts > 1) {  // this part's fp32 sums
+        float* slot = win.acc + ((((int64_t)g * win.tiles + n) * sink_slots(num_tokens, win.chunk) +
+                                  sink_slot(start, part, win.chunk)) * 2 + k) * (128 * D) + r * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v32[32];
+          tmem_ld_32x32b_x32(trow + col + c * 32, v32);
+          tmem_ld_wait();
+          reg_fence<32>(v32);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            reinterpret_cast<uint4*>(slot + c * 32)[q] =
+                make_uint4(v32[4 * q], v32[4 * q + 1], v32[4 * q + 2], v32[4 * q + 3]);
+        }
+      } else if constexpr (GATHER) {  // fp32 add at the key's trajectory row
         const int kpos = n * C::BM + r;
         float* accp = nullptr;
         if (kpos < L) {
@@ -996,9 +1074,68 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
   }
 }
 
+// dK and dV of the keys of split sink tiles: their parts' sums added in order, four dims a thread.
+template <int D>
+__global__ void __launch_bounds__(256) bwd_sink_sum(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
+                                                    int32_t num_tokens, int32_t max_seqlen, int32_t hkv,
+                                                    const WinArgs win, __nv_bfloat16* __restrict__ dk,
+                                                    __nv_bfloat16* __restrict__ dv) {
+  const int64_t slots = sink_slots(num_tokens, win.chunk), groups = (int64_t)num_segments * hkv * win.tiles;
+  for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
+    const int n = (int)(b % win.tiles), g = (int)(b / win.tiles % hkv), seg = (int)(b / win.tiles / hkv);
+    const int start = cu_seqlens[seg], end = cu_seqlens[seg + 1];
+    if (start < 0 || end < start || end > num_tokens || end - start > max_seqlen || (seg == 0 && start != 0) ||
+        (seg == num_segments - 1 && end != num_tokens))
+      continue;  // as bwd_main
+    const int L = end - start, rows = min(128, L - n * 128);
+    if (rows <= 0) continue;
+    const int parts = sink_parts(win, (L - n * 128 + 127) / 128);
+    if (parts <= 1) continue;
+    const float* base = win.acc + ((int64_t)g * win.tiles + n) * slots * 2 * (128 * D);
+    for (int i = threadIdx.x; i < 2 * rows * (D / 4); i += 256) {
+      const int which = i / (rows * (D / 4)), j = i % (rows * (D / 4));  // dK, dV; float4 of the tile
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int p = 0; p < parts; ++p) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(
+                                   base + (sink_slot(start, p, win.chunk) * 2 + which) * (128 * D)) + j);
+        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+      }
+      __nv_bfloat16* out = (which == 0 ? dk : dv) +
+                           ((size_t)(start + n * 128 + j / (D / 4)) * hkv + g) * D + j % (D / 4) * 4;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
+    }
+  }
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-template <int D, bool GATHER>
+// How a windowed launch splits its sink tiles (WinArgs).
+WinArgs plan_window(const AttnArgs& a) {
+  WinArgs w{};
+  const int32_t longest = a.max_seqlen > 1 ? a.max_seqlen : 1;
+  w.window = a.window < longest ? a.window : longest;
+  w.sinks = a.sinks < longest ? a.sinks : longest;
+  w.tiles = (int32_t)(((int64_t)w.sinks + 127) / 128);
+  w.parts = 1;
+  w.chunk = 1;
+  const int64_t rows = ((int64_t)longest + 127) / 128, wrows = ((int64_t)w.window + 126) / 128 + 1;
+  int64_t chunk = a.hkv * (a.num_tokens / 128) * wrows / 152 / 4;  // a quarter of an SM's row tiles
+  if (chunk < 2 * wrows) chunk = 2 * wrows;
+  if (chunk < 16) chunk = 16;
+  // many sinks are many tiles, which balance each other as the causal kernel's do
+  if (w.tiles > 0 && w.tiles <= 8 && chunk < rows) {
+    w.chunk = (int32_t)chunk;
+    w.parts = (int32_t)((rows + chunk - 1) / chunk);
+  }
+  return w;
+}
+size_t sink_bytes(const AttnArgs& a) {
+  const WinArgs w = plan_window(a);
+  if (w.parts <= 1) return 0;
+  return align256((size_t)a.hkv * w.tiles * sink_slots(a.num_tokens, w.chunk) * 2 * 128 * a.d * 4);
+}
+
+template <int D, bool GATHER, bool WIN>
 cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, const void* dout, void* dq, void* dk,
                          void* dv, void* ws, cudaStream_t st) {
   using C = Bwd<D>;
@@ -1043,6 +1180,11 @@ cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, con
   }
   if (!encode_tma_3d_bf16(&tdo, dout, D, a.hq, a.num_tokens, 64, 128)) return cudaErrorInvalidValue;
   const int ntiles = (a.max_seqlen + C::BM - 1) / C::BM;
+  WinArgs win{};
+  if (WIN) {
+    win = plan_window(a);
+    win.acc = dq_acc + align256((size_t)a.num_tokens * a.hq * D * 4) / 4;
+  }
   const int64_t gx = (int64_t)a.num_segments * a.hkv;
   if (gx > (int64_t)65535 * 65535) return cudaErrorInvalidConfiguration;
   dim3 grid((unsigned)ntiles, (unsigned)(gx < 65535 ? gx : 65535), (unsigned)((gx + 65534) / 65535));
@@ -1055,22 +1197,35 @@ cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, con
   double tail_groups = 152.0 * ntiles / (tavg < 1.0 ? 1.0 : tavg * tavg);
   if (tail_groups < 1.0) tail_groups = 1.0;
   if (tail_groups > (double)gx) tail_groups = (double)gx;
+  if (WIN) {  // its key tiles are alike: group by group
+    tail_groups = 0.0;
+    grid.x = (unsigned)(ntiles + win.tiles * (win.parts - 1));
+  }
   if (ntiles > 0) {
     static std::atomic<int> regs_cache{-1};
     bool regs_ok = false;
-    if (cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(bwd_main<D, GATHER>), C::REG_LAUNCH,
+    if (cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(bwd_main<D, GATHER, WIN>), C::REG_LAUNCH,
                                           &regs_cache, &regs_ok);
         e != cudaSuccess)
       return e;
     if (!regs_ok) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(bwd_main<D, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(bwd_main<D, GATHER, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     if (e != cudaSuccess) return e;
-    bwd_main<D, GATHER><<<grid, C::THREADS, C::SMEM, st>>>(
+    bwd_main<D, GATHER, WIN><<<grid, C::THREADS, C::SMEM, st>>>(
         tq, tk, tv, tdo, a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens, a.max_seqlen, a.hq, a.hkv,
         (int32_t)tail_groups, a.scale, a.scale * 1.4426950408889634f, lse, dvec, GATHER ? dq_t : dq_acc, static_cast<__nv_bfloat16*>(dk),
         static_cast<__nv_bfloat16*>(dv), a.status, a.tok_gather, (int32_t)a.traj_tokens, dk_t, dv_t,
         GATHER ? tqr : tq, GATHER ? tkr : tk, GATHER ? tvr : tv, GATHER ? tqs : tq, GATHER ? tks : tk,
-        GATHER ? tvs : tv);
+        GATHER ? tvs : tv, win);
+    if (WIN && win.parts > 1) {
+      e = cudaGetLastError();
+      if (e != cudaSuccess) return e;
+      int64_t blocks = gx * win.tiles;
+      if (blocks > 152 * 32) blocks = 152 * 32;
+      bwd_sink_sum<D><<<(unsigned)blocks, 256, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens,
+                                                        a.max_seqlen, a.hkv, win, static_cast<__nv_bfloat16*>(dk),
+                                                        static_cast<__nv_bfloat16*>(dv));
+    }
   }
   auto convert = [&](const float* acc, void* out, int64_t elems) {
     const int64_t n8 = elems / 8;
@@ -1097,17 +1252,22 @@ size_t attn_bwd_ws_bytes(const AttnArgs& a) {
   // these, stays: its segment-layout dQ term is unused space then.
   if (a.traj_tokens > 0)
     b += align256((size_t)a.traj_tokens * a.hq * a.d * 4) + 2 * align256((size_t)a.traj_tokens * a.hkv * a.d * 4);
+  if (a.window > 0) b += sink_bytes(a);
   return b;
 }
 
 cudaError_t launch_attn_bwd(const AttnArgs& a, const void* o, const float* lse, const void* dout, void* dq, void* dk,
                             void* dv, void* ws, cudaStream_t st) {
   if (a.tok_gather != nullptr) {
-    if (a.d == 64) return launch_bwd_d<64, true>(a, o, lse, dout, dq, dk, dv, ws, st);
-    return launch_bwd_d<128, true>(a, o, lse, dout, dq, dk, dv, ws, st);
+    if (a.d == 64) return launch_bwd_d<64, true, false>(a, o, lse, dout, dq, dk, dv, ws, st);
+    return launch_bwd_d<128, true, false>(a, o, lse, dout, dq, dk, dv, ws, st);
   }
-  if (a.d == 64) return launch_bwd_d<64, false>(a, o, lse, dout, dq, dk, dv, ws, st);
-  return launch_bwd_d<128, false>(a, o, lse, dout, dq, dk, dv, ws, st);
+  if (a.window > 0) {
+    if (a.d == 64) return launch_bwd_d<64, false, true>(a, o, lse, dout, dq, dk, dv, ws, st);
+    return launch_bwd_d<128, false, true>(a, o, lse, dout, dq, dk, dv, ws, st);
+  }
+  if (a.d == 64) return launch_bwd_d<64, false, false>(a, o, lse, dout, dq, dk, dv, ws, st);
+  return launch_bwd_d<128, false, false>(a, o, lse, dout, dq, dk, dv, ws, st);
 }
 
 }  // namespace vcs

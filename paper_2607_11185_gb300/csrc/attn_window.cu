@@ -1,0 +1,750 @@
+// attn_window.cu - causal grouped-query attention with a sliding window and sinks, forward, over packed
+// variable-length segments, for sm_103a (tcgen05 + TMEM + TMA).
+//
+// Token i of a segment sees token j of it for j <= i and (i - j < window or j < sinks):
+//   s_ij = scale <q_i, k_j>,  o_i = sum_j softmax_j(s_ij) v_j,  lse_i = ln sum_j exp(s_ij)
+// over the visible j.  Every row sees itself, so no row is empty.
+//
+// Work unit: two 128-row query tiles that stream the same key tiles.  Where a kv head serves two or more
+// query heads they are the same rows of two heads, whose key tiles are the same ones; of an odd group's
+// last head, or a single head, they are two consecutive row tiles (m, m + 1), which share all but one
+// tile at each end of the window.  A block of two row tiles of one kv head is G units either way.
+// A unit's key tiles: those of the sinks, then those from the window of its first row to the diagonal.
+// Masked element-wise: the diagonal tile, the tiles the window's edge crosses, and the sinks' tiles
+// outside the window.
+//
+// A long window's unit is bound by the tensor pipe like the causal kernel's (attn_fwd.cu, whose inner
+// loops these are); a short window's, of two to four steps, by what precedes and follows its steps.  So
+// a CTA stays on its SM and takes every grid-th unit: barriers and TMEM are set up once, the ring of K/V
+// tiles runs on across units, the next unit's Q is loaded once the last S of this one is complete, and
+// its first S is computed while the softmax warps write this unit's O.
+//
+// Warp roles (384 threads):
+//   warp 0      TMA producer: Q0/Q1 of a unit, K and V tiles into a ring (K runs one tile ahead of V)
+//   warp 1      TMEM allocator and tcgen05.mma issuer; at d = 64 of S only
+//   warp 2      d = 64: issuer of P V
+//   warps 4-7   softmax + epilogue of tile 0 (thread = query row);  warps 8-11 of tile 1
+// TMEM (512 columns): S0, S1 (128 each), O0 and O1 from 256 and 384 on.  d = 128: P_k goes over the first
+// 64 columns of S_k; d = 64: it has 64 columns of its own behind O_k.  P is read straight from TMEM.
+// The order of the MMAs on the pipe, and what each barrier then says, is as in the causal kernel:
+// d = 128, step j: for each tile O_k += P_k(j) V_j, then S_k(j+1); d = 64: S_k(j+1) as soon as S_k(j)
+// has been read, by one warp, and P V by another.
+#include <cfloat>
+#include <cstdint>
+
+#include "internal.h"
+#include "sm100.cuh"
+
+namespace vcs {
+namespace {
+
+using namespace dev;
+
+constexpr int kThreads = 384;
+// registers per thread after rebalancing, as in the causal kernel
+constexpr int kRegLaunch = 168, kRegCtrl = 80, kRegSoftmax = 208;
+static_assert(kRegCtrl + 2 * kRegSoftmax <= 3 * kRegLaunch, "setmaxnreg targets exceed the launch registers");
+constexpr float kRescaleThreshold = 8.0f;  // log2 units a row's maximum may grow before O is rescaled
+constexpr float kHidden = -INFINITY;
+
+template <int D>
+struct Win {
+  static constexpr int BM = 128;
+  static constexpr int BN = 128;
+  static constexpr int KB = D / 64;                 // 128-byte column blocks per row
+  static constexpr int TILE = BM * D * 2;           // bytes of a 128 x D bf16 tile
+  static constexpr int BLOCK = BM * 128;            // bytes of one 128 x 64 column block
+  static constexpr bool OWN_P = D == 64;            // P in TMEM columns of its own
+  static constexpr int NSLOT = OWN_P ? 8 : 4;
+  static constexpr int NGRP = 4;                    // ring-item group barriers
+  static constexpr int OFF_Q0 = 0;
+  static constexpr int OFF_Q1 = TILE;
+  static constexpr int OFF_KV = 2 * TILE;
+  static constexpr int OFF_OUT = OFF_KV + NSLOT * TILE;  // a column block of O of each tile, on its way out
+  static constexpr int OFF_BAR = OFF_OUT + 2 * BLOCK;
+  static constexpr int SMEM = OFF_BAR + 256 + 1024;
+  static constexpr int TM_S0 = 0, TM_S1 = 128, TM_O0 = 256, TM_O1 = 384;
+  static constexpr int TM_P0 = OWN_P ? TM_O0 + 64 : TM_S0, TM_P1 = OWN_P ? TM_O1 + 64 : TM_S1;
+  static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);   // Q (K-major) x K^T (K-major)
+  static constexpr uint32_t IDESC_PV = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
+};
+static_assert(Win<64>::SMEM <= 232448 && Win<128>::SMEM <= 232448, "shared memory budget");
+
+struct Bars {
+  uint64_t q_full;       // a unit's Q tiles landed
+  uint64_t q_free;       // its last S is complete
+  uint64_t kv_full[8];   // per ring slot (OWN_P)
+  uint64_t kv_empty[8];
+  uint64_t grp_full[4];  // per group of ring items consumed in one step (without OWN_P)
+  uint64_t s_full[2];
+  uint64_t s_read[2];    // OWN_P: S(j) is in the softmax warps' registers
+  uint64_t p_full[2];
+  uint64_t o_done[2];    // the unit's last P V is complete; OWN_P: every step's
+  uint32_t tmem_base;
+  int32_t abort;
+};
+static_assert(sizeof(Bars) <= 256, "barrier space");
+
+// workspace header: the number of listed work units sits after the status word
+constexpr size_t kWsItemTotal = 128;
+
+__device__ __forceinline__ void on_timeout(Bars* b, int32_t* status) {
+  set_status(status, VCS_ERR_DEVICE_TIMEOUT);
+  *reinterpret_cast<volatile int32_t*>(&b->abort) = 1;
+}
+__device__ __forceinline__ bool aborted(Bars* b) { return *reinterpret_cast<volatile int32_t*>(&b->abort) != 0; }
+
+// S = Q K^T; qd, kd are K-major descriptors of the Q tile and the K tile.
+template <int D>
+__device__ __forceinline__ void issue_s(uint32_t tmem_d, uint64_t qd, uint64_t kd) {
+  using C = Win<D>;
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    const uint32_t off = (kk >> 2) * C::BLOCK + (kk & 3) * 32;
+    tc_mma_ss(tmem_d, desc_at(qd, off), desc_at(kd, off), C::IDESC_S, kk > 0);
+  }
+}
+
+// O (+)= P V with P (128 x 128 keys, bf16) in TMEM; vd is the MN-major descriptor of the V tile.
+template <int D>
+__device__ __forceinline__ void issue_pv(uint32_t tmem_d, uint32_t p_tmem, uint64_t vd, bool accumulate) {
+  using C = Win<D>;
+  const uint32_t acc0 = accumulate ? 1u : 0u;
+#pragma unroll
+  for (int kk = 0; kk < C::BN / 16; ++kk)
+    tc_mma_ts(tmem_d, p_tmem + kk * 8, desc_at(vd, kk * 16 * 128), C::IDESC_PV, kk > 0 ? 1u : acc0);
+}
+
+// ------------------------------------------------------------------ work units
+// A unit as listed: {segment start, segment end, 2 * (row tile of tile 0) + (its tiles are two heads), head
+// of tile 0}.
+__device__ __forceinline__ long long seg_units(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
+                                         int32_t num_tokens, int32_t max_seqlen, int32_t G, int s, int32_t* status) {
+  const int start = cu_seqlens[s], end = cu_seqlens[s + 1];
+  if (start < 0 || end < start || end > num_tokens || end - start > max_seqlen || (s == 0 && start != 0) ||
+      (s == num_segments - 1 && end != num_tokens)) {
+    set_status(status, VCS_ERR_DEVICE_CHECK);
+    return 0;
+  }
+  const int tiles = (end - start + 127) / 128;
+  return (long long)(tiles >> 1) * G + (tiles & 1) * ((G + 1) >> 1);  // of one kv head
+}
+
+// off[s] = units of segments 0 .. s-1 (clipped to the capacity), *total = their sum, or 0 where it passes the
+// capacity: only segments that overlap, which inconsistent bounds describe, list so many, and no CTA then
+// reads a unit that was not written.  The call's first kernel: it clears the status word.  items != nullptr:
+// it writes the units too, a warp a segment.
+__device__ __forceinline__ void write_units(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
+                                            int32_t num_tokens, int32_t max_seqlen, int32_t hkv, int32_t G,
+                                            int32_t capacity, long long base, int4* __restrict__ items,
+                                            int32_t* status, int s, int tid, int n) {
+  const long long one = seg_units(cu_seqlens, num_segments, num_tokens, max_seqlen, G, s, status);
+  const long long units = hkv * one;
+  if (one == 0 || base + units > capacity) return;
+  const int per = (int)one;
+  const int start = cu_seqlens[s], end = cu_seqlens[s + 1];
+  const int tiles = (end - start + 127) / 128, pairs = G >> 1;
+  for (int i = tid; i < (int)units; i += n) {
+    const int g = i / per, u = i - g * per;
+    const int p = u / G, r = u - p * G;                 // block of two row tiles, unit of it
+    const bool half = 2 * p + 1 >= tiles;               // the last block may be one tile
+    const int pair = half ? r : r >> 1;                 // (an odd group's last head has r = 2 * pairs, or pairs)
+    const bool two = pair < pairs;
+    const int m = 2 * p + (two && !half ? r & 1 : 0);
+    items[base + i] = make_int4(start, end, 2 * m + (two ? 1 : 0), g * G + 2 * pair);
+  }
+}
+
+__global__ void __launch_bounds__(1024) window_unit_scan(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
+                                                         int32_t num_tokens, int32_t max_seqlen, int32_t hkv, int32_t G,
+                                                         int32_t capacity, int32_t* off, int32_t* __restrict__ total,
+                                                         int4* __restrict__ items, int32_t* status) {
+  __shared__ long long wsum[32];
+  __shared__ long long carry;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    carry = 0;
+    *reinterpret_cast<volatile int32_t*>(status) = VCS_OK;
+  }
+  __syncthreads();
+  for (int base = 0; base < num_segments; base += 1024) {
+    const int s = base + (int)threadIdx.x;
+    const long long cnt =
+        s < num_segments
+            ? hkv * seg_units(cu_seqlens, num_segments, num_tokens, max_seqlen, G, s, status)
+            : 0;
+    long long x = cnt;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[wid] = x;
+    __syncthreads();
+    if (wid == 0) {
+      long long w = wsum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+      }
+      wsum[lane] = w;
+    }
+    __syncthreads();
+    const long long incl = carry + (wid > 0 ? wsum[wid - 1] : 0) + x;
+    if (s < num_segments) off[s] = (int32_t)(incl - cnt < capacity ? incl - cnt : capacity);
+    __syncthreads();
+    if (threadIdx.x == 1023) carry = incl;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    const int32_t t = carry <= capacity ? (int32_t)carry : 0;
+    if (carry > capacity) set_status(status, VCS_ERR_DEVICE_CHECK);
+    off[num_segments] = t;
+    *total = t;
+  }
+  if (items == nullptr) return;
+  __syncthreads();
+  for (int s = wid; s < num_segments; s += 32)
+    write_units(cu_seqlens, num_segments, num_tokens, max_seqlen, hkv, G, capacity, off[s], items, status, s, lane, 32);
+}
+
+__global__ void __launch_bounds__(256) window_unit_fill(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
+                                                        int32_t num_tokens, int32_t max_seqlen, int32_t hkv, int32_t G,
+                                                        int32_t capacity, const int32_t* __restrict__ off,
+                                                        int4* __restrict__ items, int32_t* status) {
+  for (int s = blockIdx.x; s < num_segments; s += gridDim.x)
+    write_units(cu_seqlens, num_segments, num_tokens, max_seqlen, hkv, G, capacity, off[s], items, status, s,
+                threadIdx.x, blockDim.x);
+}
+
+// What every role derives from a listed unit.  Step j takes key tile kt(j): the sinks' first `ns` tiles, then
+// lo, lo + 1, ...  Tile 0 takes steps j < n0; tile 1 (if has1) all but `skip`, the window's first tile where
+// two row tiles share a unit and none of its keys is visible to the second.
+struct Unit {
+  int start, L, h[2], m[2], ns, lo, nkv, n0, skip;
+  bool has1;
+  __device__ __forceinline__ Unit(int4 e, int window, int sinks) {
+    start = e.x;
+    L = e.y - e.x;
+    const bool two = e.z & 1;
+    m[0] = e.z >> 1;
+    m[1] = two ? m[0] : m[0] + 1;
+    h[0] = e.w;
+    h[1] = two ? e.w + 1 : e.w;
+    has1 = two || m[1] * 128 < L;
+    const int last = has1 ? m[1] : m[0];
+    lo = max(0, m[0] * 128 - window + 1) >> 7;
+    ns = min((sinks >> 7) + ((sinks & 127) != 0), lo);
+    nkv = ns + last - lo + 1;
+    n0 = nkv - (last - m[0]);
+    skip = !two && has1 && (max(0, m[1] * 128 - window + 1) >> 7) > lo && lo * 128 >= sinks ? ns : -1;
+  }
+  __device__ __forceinline__ int kt(int j) const { return j < ns ? j : j - ns + lo; }
+  __device__ __forceinline__ bool active(int t, int j) const { return t == 0 ? j < n0 : has1 && j != skip; }
+  // ring items of the unit in load order: K0, K1, V0, K2, V1, ..., K_{n-1}, V_{n-2}, V_{n-1}
+  __device__ __forceinline__ int k_item(int j) const { return j == 0 ? 0 : 2 * j - 1; }
+  __device__ __forceinline__ int v_item(int j) const { return j == nkv - 1 ? 2 * nkv - 1 : 2 * j + 2; }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    attn_window_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                       const __grid_constant__ CUtensorMap tm_v, const int4* __restrict__ items,
+                       const int32_t* __restrict__ item_total, int32_t num_tokens, int32_t hq, int32_t hkv,
+                       int32_t window, int32_t sinks, float scale_log2, __nv_bfloat16* __restrict__ out,
+                       float* __restrict__ lse, int32_t* status) {
+  using C = Win<D>;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Bars* bars = reinterpret_cast<Bars*>(smem + C::OFF_BAR);
+
+  const int G = hq / hkv;
+  const int total = *item_total;
+  const int st = *reinterpret_cast<volatile int32_t*>(status);
+  if ((int)blockIdx.x >= total) return;  // the grid is bounded by an upper bound of the listed units
+  // once any CTA of this launch has given up on a wait, those not started stand down
+  if (st == VCS_ERR_DEVICE_TIMEOUT) return;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t sbase = smem_u32(smem);
+
+  if (threadIdx.x == 0) {
+    mbar_init(&bars->q_full, 1);
+    mbar_init(&bars->q_free, 1);
+    for (int i = 0; i < C::NSLOT; ++i) {
+      mbar_init(&bars->kv_full[i], 1);
+      mbar_init(&bars->kv_empty[i], 1);
+    }
+    for (int i = 0; i < C::NGRP; ++i) mbar_init(&bars->grp_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->s_read[i], 4);
+      mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->o_done[i], 1);
+    }
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+
+  // Every role walks the same units and counts what it has passed: ring items (`ib`) and groups (`gb`) before
+  // the unit, units (`un`), and per tile the steps taken.
+  if (warp < 4) {
+    setmaxnreg_dec<kRegCtrl>();
+    if (warp == 0 && lane == 0) {
+    // ------------------------------------------------------------ producer
+      tma_prefetch_desc(&tm_q);
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+      const uint64_t keep_l2 = l2_policy_evict_last();
+      uint32_t ib = 0, gb = 0, un = 0;
+      bool go = true;
+      int4 e = items[blockIdx.x];
+      for (int i = blockIdx.x; go && i < total; i += gridDim.x) {
+        const Unit u(e, window, sinks);
+        if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
+        for (int c = 0; c < 2 * u.nkv; ++c) {
+          const bool is_v = c == 2 * u.nkv - 1 || (c > 0 && (c & 1) == 0);
+          const int j = c == 2 * u.nkv - 1 ? u.nkv - 1 : (is_v ? (c - 2) >> 1 : (c + 1) >> 1);
+          const uint32_t it = ib + c, slot = it % C::NSLOT;
+          if ((it >= C::NSLOT && !mbar_wait(&bars->kv_empty[slot], (it / C::NSLOT - 1) & 1))) {
+            on_timeout(bars, status);
+            go = false;
+            break;
+          }
+          if (aborted(bars)) {
+            go = false;
+            break;
+          }
+          // Without OWN_P items 2m-1, 2m of the unit (K_m, V_{m-1}), which step m-1 consumes, complete one
+          // barrier, armed for both by the first; group 0 (K_0) and group nkv (V_{nkv-1}) hold one item
+          const int m = (c + 1) >> 1;
+          uint64_t* bar = C::OWN_P ? &bars->kv_full[slot] : &bars->grp_full[(gb + m) % C::NGRP];
+          if (C::OWN_P)
+            mbar_arrive_expect_tx(bar, C::TILE);
+          else if (c == 0 || (c & 1))
+            mbar_arrive_expect_tx(bar, (m == 0 || m == u.nkv ? 1 : 2) * C::TILE);
+          const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+#pragma unroll
+          for (int kb = 0; kb < C::KB; ++kb)
+            tma_load_3d_hint(smem + C::OFF_KV + slot * C::TILE + kb * C::BLOCK, tm, bar, kb * 64, u.h[0] / G,
+                             u.start + u.kt(j) * C::BN, keep_l2);
+          if (c == 0) {  // Q behind the first K, which needs no wait for the unit before
+            if (un > 0 && !mbar_wait(&bars->q_free, (un - 1) & 1)) {
+              on_timeout(bars, status);
+              go = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&bars->q_full, (u.has1 ? 2 : 1) * C::TILE);
+#pragma unroll
+            for (int kb = 0; kb < C::KB; ++kb) {
+              tma_load_3d(smem + C::OFF_Q0 + kb * C::BLOCK, &tm_q, &bars->q_full, kb * 64, u.h[0],
+                          u.start + u.m[0] * C::BM);
+              if (u.has1)
+                tma_load_3d(smem + C::OFF_Q1 + kb * C::BLOCK, &tm_q, &bars->q_full, kb * 64, u.h[1],
+                            u.start + u.m[1] * C::BM);
+            }
+          }
+        }
+        ib += 2 * u.nkv;
+        gb += u.nkv + 1;
+        ++un;
+      }
+    } else if (C::OWN_P && (warp == 1 || warp == 2)) {
+    // ---------------------------------------------------- MMA issuers (S; P V)
+      const uint64_t q0d = smem_desc(sbase + C::OFF_Q0, 16, 1024);
+      const uint64_t kv_kmaj = smem_desc(sbase + C::OFF_KV, 16, 1024);
+      const uint64_t kv_mnmaj = smem_desc(sbase + C::OFF_KV, C::BLOCK, 1024);
+      // A wait can run out between two lanes' reads, so no lane's answer decides where the warp goes:
+      // every lane runs every step, one that has given up waits no more, and the elected lane issues as
+      // long as its own waits were met.  A vote a unit ends the walk.
+      bool ok = true;
+      uint32_t ib = 0, un = 0, steps[2] = {0, 0};
+      int4 e = items[blockIdx.x];
+      for (int i = blockIdx.x; i < total; i += gridDim.x) {
+        const Unit u(e, window, sinks);
+        if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
+        if (warp == 1) ok = ok && mbar_wait(&bars->q_full, un & 1);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        for (int j = 0; j < u.nkv; ++j) {
+          const uint32_t it = ib + (warp == 1 ? u.k_item(j) : u.v_item(j)), slot = it % C::NSLOT;
+          ok = ok && mbar_wait(&bars->kv_full[slot], (it / C::NSLOT) & 1);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!u.active(t, j)) continue;
+            if (warp == 1) {
+              if (steps[t] > 0) ok = ok && mbar_wait(&bars->s_read[t], (steps[t] - 1) & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                issue_s<D>(tmem + (t ? C::TM_S1 : C::TM_S0), desc_at(q0d, t * C::TILE),
+                           desc_at(kv_kmaj, slot * C::TILE));
+                tc_commit(&bars->s_full[t]);
+              }
+            } else {
+              ok = ok && mbar_wait(&bars->p_full[t], steps[t] & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                issue_pv<D>(tmem + (t ? C::TM_O1 : C::TM_O0), tmem + (t ? C::TM_P1 : C::TM_P0),
+                            desc_at(kv_mnmaj, slot * C::TILE), j > (t == 1 && u.skip == 0 ? 1 : 0));
+                tc_commit(&bars->o_done[t]);
+              }
+            }
+            __syncwarp();
+            ++steps[t];
+          }
+        }
+        if (warp == 1) {
+          if (elect_one() && ok) tc_commit(&bars->q_free);
+          __syncwarp();
+        }
+        ib += 2 * u.nkv;
+        ++un;
+      }
+      if (!ok) on_timeout(bars, status);
+    } else if (!C::OWN_P && warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    // The whole warp runs the loop and one elected lane issues, so that descriptors and addresses stay in
+    // uniform registers.  As above, no lane's answer decides where the warp goes; here a vote a step does.
+      bool ok = true;
+      const uint64_t q0d = smem_desc(sbase + C::OFF_Q0, 16, 1024), q1d = desc_at(q0d, C::TILE);
+      const uint64_t kv_kmaj = smem_desc(sbase + C::OFF_KV, 16, 1024);
+      const uint64_t kv_mnmaj = smem_desc(sbase + C::OFF_KV, C::BLOCK, 1024);
+      uint32_t ib = 0, gb = 0, un = 0, p0 = 0, p1 = 0;
+      auto acquire_group = [&](uint32_t g) {
+        ok &= mbar_wait(&bars->grp_full[g % C::NGRP], (g / C::NGRP) & 1);
+        tc_fence_after();
+      };
+      int4 e = items[blockIdx.x];
+      for (int i = blockIdx.x; i < total; i += gridDim.x) {
+        const Unit u(e, window, sinks);
+        if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
+        auto slot_off = [&](int item) { return (uint32_t)(((ib + item) % C::NSLOT) * C::TILE); };
+        ok &= mbar_wait(&bars->q_full, un & 1);
+        acquire_group(gb);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        uint32_t kaddr = slot_off(0);
+        // S of the first step overwrites the P that the last P V of the unit before, issued before, reads
+        if (elect_one() && ok) {
+          issue_s<D>(tmem + C::TM_S0, q0d, desc_at(kv_kmaj, kaddr));
+          tc_commit(&bars->s_full[0]);
+          if (u.active(1, 0)) {
+            issue_s<D>(tmem + C::TM_S1, q1d, desc_at(kv_kmaj, kaddr));
+            tc_commit(&bars->s_full[1]);
+          }
+          if (u.nkv == 1) tc_commit(&bars->q_free);
+        }
+        __syncwarp();
+        for (int j = 0; j < u.nkv; ++j) {
+          const bool next = j + 1 < u.nkv;
+          acquire_group(gb + j + 1);
+          if (!__all_sync(0xffffffffu, ok)) break;
+          const uint32_t vaddr = slot_off(u.v_item(j));
+          if (next) kaddr = slot_off(u.k_item(j + 1));
+          if (j < u.n0) {  // tile 0: O0 += P0(j) V_j, then S0(j+1)
+            ok &= mbar_wait(&bars->p_full[0], p0++ & 1);
+            tc_fence_after();
+            if (elect_one() && ok) {
+              issue_pv<D>(tmem + C::TM_O0, tmem + C::TM_S0, desc_at(kv_mnmaj, vaddr), j > 0);
+              if (j + 1 < u.n0) {
+                issue_s<D>(tmem + C::TM_S0, q0d, desc_at(kv_kmaj, kaddr));
+                tc_commit(&bars->s_full[0]);
+              } else {
+                tc_commit(&bars->o_done[0]);
+              }
+            }
+            __syncwarp();
+          }
+          if (u.has1) {  // tile 1
+            if (j != u.skip) {
+              ok &= mbar_wait(&bars->p_full[1], p1++ & 1);
+              tc_fence_after();
+            }
+            if (elect_one() && ok) {
+              if (j != u.skip)
+                issue_pv<D>(tmem + C::TM_O1, tmem + C::TM_S1, desc_at(kv_mnmaj, vaddr), j > (u.skip == 0 ? 1 : 0));
+              if (next && j + 1 != u.skip) {
+                issue_s<D>(tmem + C::TM_S1, q1d, desc_at(kv_kmaj, kaddr));
+                tc_commit(&bars->s_full[1]);
+              } else if (!next) {
+                tc_commit(&bars->o_done[1]);
+              }
+            }
+            __syncwarp();
+          }
+          if (j == u.nkv - 2) {  // the unit's last S is issued
+            if (elect_one() && ok) tc_commit(&bars->q_free);
+            __syncwarp();
+          }
+        }
+        if (!__all_sync(0xffffffffu, ok)) break;
+        ib += 2 * u.nkv;
+        gb += u.nkv + 1;
+        ++un;
+      }
+      if (!ok) on_timeout(bars, status);
+    }
+  } else {
+    // ------------------------------------------------------------ softmax
+    setmaxnreg_inc<kRegSoftmax>();
+    const int wg = (warp - 4) >> 2;
+    const int quad = warp & 3;
+    const int r = quad * 32 + lane;  // query row within the tile
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t s_col = wg == 0 ? C::TM_S0 : C::TM_S1;
+    const uint32_t o_col = wg == 0 ? C::TM_O0 : C::TM_O1;
+    const uint32_t p_col = wg == 0 ? C::TM_P0 : C::TM_P1;
+    const uint64_t sc2 = f2pack(scale_log2, scale_log2);
+    const uint32_t stage = sbase + C::OFF_OUT + wg * C::BLOCK;
+    uint32_t ib = 0, steps = 0, outs = 0;  // outs: phases of o_done passed
+    bool ok = true;
+    int4 e = items[blockIdx.x];
+    for (int i = blockIdx.x; ok && i < total; i += gridDim.x) {
+      const Unit u(e, window, sinks);
+      if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
+      if (wg == 1 && !u.has1) {
+        ib += 2 * u.nkv;
+        continue;
+      }
+      const int mt = u.m[wg];
+      float m_run = kHidden, l = 0.f;
+      // The ring slots are handed back from here rather than by commits of the MMA thread (a commit holds it
+      // about as long as an MMA): once S(j) of the unit's last tile is complete, so are the MMAs issued
+      // before it, which are all that read K_0 .. K_j and, without OWN_P, V_0 .. V_{j-1} (with it, that
+      // tile's o_done says so of V); one thread of that tile frees their slots.
+      const bool releaser = wg == (u.has1 ? 1 : 0) && quad == 0 && lane == 0;
+      int kr = 0, vr = 0;  // K and V tiles handed back
+      auto release_k = [&](int upto) {
+        for (; kr <= upto; ++kr) mbar_arrive(&bars->kv_empty[(ib + u.k_item(kr)) % C::NSLOT]);
+      };
+      auto release_v = [&](int upto) {
+        for (; vr <= upto; ++vr) mbar_arrive(&bars->kv_empty[(ib + u.v_item(vr)) % C::NSLOT]);
+      };
+      bool first = true;
+      for (int j = 0; j < u.nkv; ++j) {
+        if (!u.active(wg, j)) continue;
+        // Without OWN_P, S(j) complete also means that the P before it was consumed and O is up to date.  The
+        // wait's outcome is the warp's: the TMEM loads and votes below are warp-collective.
+        if (!mbar_wait_warp(&bars->s_full[wg], steps & 1)) { ok = false; break; }
+        ++steps;
+        if (releaser) {
+          release_k(j);
+          if (!C::OWN_P) release_v(j - 1);
+        }
+        tc_fence_after();
+        uint32_t s[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          tmem_ld_32x32b_x32(trow + s_col + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+        tmem_ld_wait();
+        reg_fence<128>(s);
+        if constexpr (C::OWN_P) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->s_read[wg]);
+        }
+        const int kt = u.kt(j);
+        if (kt == mt) {  // diagonal tile: key c is visible to row r only if c <= r
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c > r) s[c] = __float_as_uint(kHidden);
+        }
+        // keys c <= r + ahead - window are behind the window, and hidden unless they are sinks
+        const int ahead = (mt - kt) * 128, keep = sinks - kt * 128;
+        if (ahead + 127 >= window && keep < 128) {
+          const int behind = r + ahead - window;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c <= behind && c >= keep) s[c] = __float_as_uint(kHidden);
+        }
+        // row maximum: 8 independent three-input chains
+        float pm[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) pm[x] = fmaxf(__uint_as_float(s[2 * x]), __uint_as_float(s[2 * x + 1]));
+#pragma unroll
+        for (int c = 16; c < 128; c += 16)
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            pm[x] = fmax3(pm[x], __uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1]));
+        const float mx = fmax3(fmax3(pm[0], pm[1], pm[2]), fmax3(pm[3], pm[4], pm[5]), fmaxf(pm[6], pm[7]));
+        const float mx2 = mx * scale_log2;
+        float alpha = 1.f;
+        bool rescale = false;
+        if (first) {
+          m_run = mx2;
+        } else if (mx2 > m_run + kRescaleThreshold) {
+          alpha = ex2(m_run - mx2);  // 0 where the tiles before were hidden from the row
+          m_run = mx2;
+          rescale = true;
+        }
+        // P = exp2(s*scale*log2e - m) as bf16 pairs; a row that has seen nothing yet subtracts 0 and gets zeros
+        const float shift = m_run == kHidden ? 0.f : -m_run;
+        const uint64_t nm2 = f2pack(shift, shift);
+        uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+        for (int c2 = 0; c2 < 64; ++c2) {
+          float x0, x1;
+          f2unpack(ffma2(f2pack(__uint_as_float(s[2 * c2]), __uint_as_float(s[2 * c2 + 1])), sc2, nm2), x0, x1);
+          const float p0 = ex2(x0), p1 = ex2(x1);
+          acc[c2 & 3] = fadd2(acc[c2 & 3], f2pack(p0, p1));
+          s[c2] = pack_bf16(p0, p1);
+        }
+        float a0, a1, b0, b1;
+        f2unpack(fadd2(acc[0], acc[1]), a0, a1);
+        f2unpack(fadd2(acc[2], acc[3]), b0, b1);
+        l = l * alpha + ((a0 + a1) + (b0 + b1));
+        if (C::OWN_P && !first) {  // the P V before is complete: P's columns are free and O is up to date
+          if (!mbar_wait_warp(&bars->o_done[wg], outs & 1)) { ok = false; break; }
+          ++outs;
+          if (releaser) release_v(j - 1 - (u.skip >= 0 && j == u.skip + 1 ? 1 : 0));
+          tc_fence_after();
+        }
+        tmem_st_32x32b_x32(trow + p_col, *reinterpret_cast<uint32_t(*)[32]>(&s[0]));
+        tmem_st_32x32b_x32(trow + p_col + 32, *reinterpret_cast<uint32_t(*)[32]>(&s[32]));
+        if (!first && __any_sync(0xffffffffu, rescale)) {
+          const uint64_t al2 = f2pack(alpha, alpha);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(trow + o_col + c * 32, o);
+            tmem_ld_wait();
+            reg_fence<32>(o);
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              float x0, x1;
+              f2unpack(fmul2(f2pack(__uint_as_float(o[x]), __uint_as_float(o[x + 1])), al2), x0, x1);
+              o[x] = __float_as_uint(x0);
+              o[x + 1] = __float_as_uint(x1);
+            }
+            tmem_st_32x32b_x32(trow + o_col + c * 32, o);
+          }
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&bars->p_full[wg]);
+        first = false;
+      }
+      if (ok) ok = mbar_wait_warp(&bars->o_done[wg], outs & 1);
+      ++outs;
+      // another role's giving up is looked for once a unit; the waits are bounded without it
+      if (ok && __any_sync(0xffffffffu, aborted(bars))) ok = false;
+      if (!ok) break;
+      if (releaser) release_v(u.nkv - 1);
+      ib += 2 * u.nkv;
+      if (mt * C::BM + quad * 32 < u.L) {  // the warp has rows in the segment
+        tc_fence_after();
+        const int row = mt * C::BM + r;
+        const float inv_l = 1.f / l;
+        const uint64_t il2 = f2pack(inv_l, inv_l);
+        // A column block of the warp's 32 rows passes through the warp's part of the staging buffer, so that 8
+        // lanes store a row's 128 bytes.
+        const int row0 = quad * 32 + (lane >> 3), chunk = lane & 7;
+        __nv_bfloat16* dst = out + ((size_t)(u.start + mt * C::BM + row0) * hq + u.h[wg]) * D + chunk * 8;
+#pragma unroll
+        for (int kb = 0; kb < C::KB; ++kb) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(trow + o_col + kb * 64 + c * 32, o);
+            tmem_ld_wait();
+            reg_fence<32>(o);
+            uint32_t pk[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              float x0, x1;
+              f2unpack(fmul2(f2pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), il2), x0, x1);
+              pk[x] = pack_bf16(x0, x1);
+            }
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+              st_shared_v4(stage + r * 128 + (uint32_t)(((c * 4 + v4) ^ (r & 7)) << 4), pk[4 * v4], pk[4 * v4 + 1],
+                           pk[4 * v4 + 2], pk[4 * v4 + 3]);
+          }
+          asm volatile("" ::: "memory");
+          __syncwarp();
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const int ri = row0 + 4 * x;
+            const uint4 v = ld_shared_v4(stage + ri * 128 + (uint32_t)((chunk ^ (ri & 7)) << 4));
+            if (mt * C::BM + ri < u.L) *reinterpret_cast<uint4*>(dst + (size_t)(4 * x) * hq * D + kb * 64) = v;
+          }
+          asm volatile("" ::: "memory");
+          __syncwarp();
+          asm volatile("" ::: "memory");
+        }
+        if (row < u.L)
+          lse[(size_t)u.h[wg] * num_tokens + u.start + row] = (m_run + lg2(l)) * 0.69314718055994531f;
+      }
+    }
+    if (!ok) on_timeout(bars, status);
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Upper bound of a launch's units: a segment of t row tiles lists hkv (G floor(t / 2) + (t odd) ceil(G / 2))
+// <= hq (L / 256 + 1), so they fit the causal forward's list of hq (T / 256 + S + 1).
+template <int D>
+cudaError_t launch_window_d(const AttnArgs& a, void* o, float* lse, void* ws, cudaStream_t st) {
+  using C = Win<D>;
+  alignas(64) CUtensorMap tq, tk, tv;
+  if (!encode_tma_3d_bf16(&tq, a.q, D, a.hq, a.num_tokens, 64, 128) ||
+      !encode_tma_3d_bf16(&tk, a.k, D, a.hkv, a.num_tokens, 64, 128) ||
+      !encode_tma_3d_bf16(&tv, a.v, D, a.hkv, a.num_tokens, 64, 128))
+    return cudaErrorInvalidValue;
+  static std::atomic<int> regs_cache{-1};
+  bool regs_ok = false;
+  if (cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(attn_window_kernel<D>), kRegLaunch, &regs_cache,
+                                        &regs_ok);
+      e != cudaSuccess)
+    return e;
+  if (!regs_ok) return cudaErrorInvalidConfiguration;
+  cudaError_t e = cudaFuncSetAttribute(attn_window_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  const int64_t max_items = (int64_t)a.hq * (a.num_tokens / 256 + (int64_t)a.num_segments + 1);
+  if (max_items > INT32_MAX) return cudaErrorInvalidConfiguration;
+  char* w = static_cast<char*>(ws);
+  int32_t* total = reinterpret_cast<int32_t*>(w + kWsItemTotal);
+  int32_t* off = reinterpret_cast<int32_t*>(w + kWsHeader);
+  int4* items = reinterpret_cast<int4*>(w + kWsHeader + align256(((size_t)a.num_segments + 1) * 4));
+  // small launches list their units in the scan's launch, as the causal forward does
+  const bool one = max_items <= 2048 && a.num_segments <= 64;
+  const int G = a.hq / a.hkv;
+  window_unit_scan<<<1, 1024, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens, a.max_seqlen, a.hkv, G,
+                                       (int32_t)max_items, off, total, one ? items : nullptr, a.status);
+  if (!one) {
+    const int fill_blocks = a.num_segments < 152 * 8 ? a.num_segments : 152 * 8;
+    window_unit_fill<<<fill_blocks, 256, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens, a.max_seqlen,
+                                                  a.hkv, G, (int32_t)max_items, off, items, a.status);
+  }
+  const unsigned grid = (unsigned)(max_items < 152 ? max_items : 152);
+  attn_window_kernel<D><<<grid, kThreads, C::SMEM, st>>>(
+      tq, tk, tv, items, total, (int32_t)a.num_tokens, a.hq, a.hkv, a.window, a.sinks, a.scale * 1.4426950408889634f,
+      static_cast<__nv_bfloat16*>(o), lse, a.status);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_attn_fwd_window(const AttnArgs& a, void* o, float* lse, void* ws, cudaStream_t st) {
+  if (a.d == 64) return launch_window_d<64>(a, o, lse, ws, st);
+  return launch_window_d<128>(a, o, lse, ws, st);
+}
+
+}  // namespace vcs

@@ -75,9 +75,14 @@ struct AttnArgs {
   // prefix reuse (forward): per segment, the length of its common prefix with the previous
   // segment of its trajectory (vcs_shared_prefix); nullptr computes every row
   const int32_t* seg_shared = nullptr;
+  // windowed variants: tokens a query sees up to its own, 0 for all; first tokens of a segment that stay visible
+  int32_t window = 0;
+  int32_t sinks = 0;
 };
 size_t attn_fwd_ws_bytes(const AttnArgs& a);
 cudaError_t launch_attn_fwd(const AttnArgs& a, void* o, float* lse, void* ws, cudaStream_t st);
+// windowed forward (attn_window.cu); its workspace is the forward's
+cudaError_t launch_attn_fwd_window(const AttnArgs& a, void* o, float* lse, void* ws, cudaStream_t st);
 size_t attn_bwd_ws_bytes(const AttnArgs& a);
 cudaError_t launch_attn_bwd(const AttnArgs& a, const void* o, const float* lse, const void* dout, void* dq, void* dk,
                             void* dv, void* ws, cudaStream_t st);

@@ -93,6 +93,12 @@ _lib_inverse_ws = _sig("vcs_gather_inverse_workspace_size", _sz, [_i64])
 _lib_inverse = _sig("vcs_gather_inverse", _i32, [_p, _i64, _i64, _p, _p, _p, _p, _sz, _p])
 _lib_gather_rope_bwd = _sig("vcs_gather_rope_bwd", _i32,
                             [_p, _p, _p, _i64, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p])
+_lib_fwd_w = _sig("vcs_attn_fwd_window", _i32,
+                  [_p, _p, _p, _p, _i32, _i64, _i32, _i32, _i32, _i32, _f32, _i32, _i32, _p, _p, _p, _sz, _p])
+_lib_bwd_w_ws = _sig("vcs_attn_bwd_window_workspace_size", _sz, [_i32, _i64, _i32, _i32, _i32, _i32, _i32, _i32])
+_lib_bwd_w = _sig("vcs_attn_bwd_window", _i32,
+                  [_p, _p, _p, _p, _p, _p, _p, _i32, _i64, _i32, _i32, _i32, _i32, _f32, _i32, _i32, _p, _p, _p, _p,
+                   _sz, _p])
 _lib_selftest_wait = _sig("vcs_selftest_bounded_wait", _i32, [_p, _i64, _p])
 
 EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "vcs_plan_segments",
@@ -102,6 +108,7 @@ EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "
             "vcs_compact_trainable", "vcs_attn_fwd_gathered", "vcs_attn_bwd_gathered_workspace_size",
             "vcs_attn_bwd_gathered", "vcs_shared_prefix", "vcs_attn_fwd_reuse", "vcs_stream_positions", "vcs_rope_init",
             "vcs_gather_rope", "vcs_gather_inverse_workspace_size", "vcs_gather_inverse", "vcs_gather_rope_bwd",
+            "vcs_attn_fwd_window", "vcs_attn_bwd_window_workspace_size", "vcs_attn_bwd_window",
             "vcs_selftest_bounded_wait"]
 
 LIB_PATH = _LIB_PATH
@@ -263,6 +270,23 @@ def vcs_compact_workspace_size(num_tokens: int) -> int:
 def vcs_compact_trainable(tok_loss_mask, num_tokens, idx, idx_capacity, count, ws, ws_bytes, stream=None) -> int:
     return _lib_compact(_ptr(tok_loss_mask), num_tokens, _ptr(idx), idx_capacity, _ptr(count), _ptr(ws), ws_bytes,
                         _stream(stream))
+
+
+def vcs_attn_fwd_window(q, k, v, cu_seqlens, num_segments, num_tokens, max_seqlen, hq, hkv, d, softmax_scale, window,
+                        sinks, o, lse, ws, ws_bytes, stream=None) -> int:
+    return _lib_fwd_w(_ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), num_segments, num_tokens, max_seqlen, hq, hkv, d,
+                      softmax_scale, window, sinks, _ptr(o), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def vcs_attn_bwd_window_workspace_size(num_segments, num_tokens, max_seqlen, hq, hkv, d, window, sinks) -> int:
+    return int(_lib_bwd_w_ws(num_segments, num_tokens, max_seqlen, hq, hkv, d, window, sinks))
+
+
+def vcs_attn_bwd_window(q, k, v, o, lse, dout, cu_seqlens, num_segments, num_tokens, max_seqlen, hq, hkv, d,
+                        softmax_scale, window, sinks, dq, dk, dv, ws, ws_bytes, stream=None) -> int:
+    return _lib_bwd_w(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dout), _ptr(cu_seqlens), num_segments,
+                      num_tokens, max_seqlen, hq, hkv, d, softmax_scale, window, sinks, _ptr(dq), _ptr(dk), _ptr(dv),
+                      _ptr(ws), ws_bytes, _stream(stream))
 
 
 def vcs_stream_positions(cu_seqlens, num_segments, num_tokens, tok_src_step, step_img, step_txt, step_grid, num_steps,
@@ -490,6 +514,58 @@ def _checked(status: int, word, where: str):
         return _check(status, where)
     _done(status, where)
     _check(word.tolist()[0], where + " (device)")
+
+
+def _expect_attn(where: str, q, k, v, cu_seqlens):
+    bf16 = torch.bfloat16
+    _expect(where, q=(q, bf16, (None, None, None)))
+    nt, _, d = q.shape
+    _expect(where, k=(k, bf16, (nt, None, d)), v=(v, bf16, tuple(k.shape)),
+            cu_seqlens=(cu_seqlens, torch.int32, (None,)))
+
+
+def attn_fwd_window(q, k, v, cu_seqlens, max_seqlen: int, window: int, sinks: int = 0, softmax_scale: float = 0.0,
+                    stream=None, check=True):
+    """attn_fwd in which a token sees the last `window` tokens, itself among them, and its segment's first
+    `sinks`; o [num_tokens, hq, d] and lse [hq, num_tokens]."""
+    if stream is not None:
+        return _on_stream(stream, attn_fwd_window, q, k, v, cu_seqlens, max_seqlen, window, sinks, softmax_scale,
+                          check=check)
+    _expect_attn("attn_fwd_window", q, k, v, cu_seqlens)
+    nt, hq, d = q.shape
+    hkv = k.shape[1]
+    ns = cu_seqlens.numel() - 1
+    o = torch.empty_like(q)
+    lse = torch.empty((hq, nt), dtype=torch.float32, device=q.device)
+    nb = vcs_attn_fwd_workspace_size(ns, nt, max_seqlen, hq, hkv, d)
+    ws = _ws(nb, q.device)
+    _check(vcs_attn_fwd_window(q, k, v, cu_seqlens, ns, nt, max_seqlen, hq, hkv, d, softmax_scale, window, sinks, o,
+                               lse, ws, nb), "vcs_attn_fwd_window")
+    if check:
+        _check(int(ws[0].item()), "vcs_attn_fwd_window (device)")
+    return o, lse
+
+
+def attn_bwd_window(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, window: int, sinks: int = 0,
+                    softmax_scale: float = 0.0, stream=None, check=True):
+    """dq, dk, dv of attn_fwd_window from its o and lse."""
+    if stream is not None:
+        return _on_stream(stream, attn_bwd_window, q, k, v, o, lse, dout, cu_seqlens, max_seqlen, window, sinks,
+                          softmax_scale, check=check)
+    _expect_attn("attn_bwd_window", q, k, v, cu_seqlens)
+    nt, hq, d = q.shape
+    _expect("attn_bwd_window", o=(o, q.dtype, tuple(q.shape)), lse=(lse, torch.float32, (hq, nt)),
+            dout=(dout, q.dtype, tuple(q.shape)))
+    hkv = k.shape[1]
+    ns = cu_seqlens.numel() - 1
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    nb = vcs_attn_bwd_window_workspace_size(ns, nt, max_seqlen, hq, hkv, d, window, sinks)
+    ws = _ws(nb, q.device)
+    _check(vcs_attn_bwd_window(q, k, v, o, lse, dout, cu_seqlens, ns, nt, max_seqlen, hq, hkv, d, softmax_scale,
+                               window, sinks, dq, dk, dv, ws, nb), "vcs_attn_bwd_window")
+    if check:
+        _check(int(ws[0].item()), "vcs_attn_bwd_window (device)")
+    return dq, dk, dv
 
 
 def stream_positions(cu_seqlens, tok_src_step, step_img, step_txt, step_grid, stream=None, check=True):
