@@ -17,13 +17,14 @@
 // loops these are); a short window's, of two to four steps, by what precedes and follows its steps.  So
 // a CTA stays on its SM and takes every grid-th unit: barriers and TMEM are set up once, the ring of K/V
 // tiles runs on across units, the next unit's Q is loaded once the last S of this one is complete, and
-// its first S is computed while the softmax warps write this unit's O.
+// warps of their own write its O while the softmax warps are at the next one's first tile.
 //
-// Warp roles (384 threads):
+// Warp roles (512 threads):
 //   warp 0      TMA producer: Q0/Q1 of a unit, K and V tiles into a ring (K runs one tile ahead of V)
 //   warp 1      TMEM allocator and tcgen05.mma issuer; at d = 64 of S only
 //   warp 2      d = 64: issuer of P V
-//   warps 4-7   softmax + epilogue of tile 0 (thread = query row);  warps 8-11 of tile 1
+//   warps 4-7   softmax of tile 0 (thread = query row);  warps 8-11 of tile 1
+//   warps 12-15 O of both tiles, out of TMEM, scaled, through shared memory, by a bulk copy a row
 // TMEM (512 columns): S0, S1 (128 each), O0 and O1 from 256 and 384 on.  d = 128: P_k goes over the first
 // 64 columns of S_k; d = 64: it has 64 columns of its own behind O_k.  P is read straight from TMEM.
 // The order of the MMAs on the pipe, and what each barrier then says, is as in the causal kernel:
@@ -40,10 +41,8 @@ namespace {
 
 using namespace dev;
 
-constexpr int kThreads = 384;
-// registers per thread after rebalancing, as in the causal kernel
-constexpr int kRegLaunch = 168, kRegCtrl = 80, kRegSoftmax = 208;
-static_assert(kRegCtrl + 2 * kRegSoftmax <= 3 * kRegLaunch, "setmaxnreg targets exceed the launch registers");
+constexpr int kThreads = 512;
+constexpr int kRegLaunch = 128;  // registers per thread of the block, which its warpgroups then trade
 constexpr float kRescaleThreshold = 8.0f;  // log2 units a row's maximum may grow before O is rescaled
 constexpr float kHidden = -INFINITY;
 
@@ -60,13 +59,20 @@ struct Win {
   static constexpr int OFF_Q0 = 0;
   static constexpr int OFF_Q1 = TILE;
   static constexpr int OFF_KV = 2 * TILE;
-  static constexpr int OFF_OUT = OFF_KV + NSLOT * TILE;  // a column block of O of each tile, on its way out
-  static constexpr int OFF_BAR = OFF_OUT + 2 * BLOCK;
-  static constexpr int SMEM = OFF_BAR + 256 + 1024;
+  // A tile's O on its way out.  Rows are 16 bytes apart, so that threads on neighbouring rows write to other
+  // banks; the 16 bytes hold the row's 1 / l of each tile.
+  static constexpr int OFF_OUT = OFF_KV + NSLOT * TILE;
+  static constexpr int OUT_ROW = D * 2 + 16;
+  static constexpr int OFF_BAR = OFF_OUT + BM * OUT_ROW;
+  static constexpr int SMEM = OFF_BAR + 512;
   static constexpr int TM_S0 = 0, TM_S1 = 128, TM_O0 = 256, TM_O1 = 384;
   static constexpr int TM_P0 = OWN_P ? TM_O0 + 64 : TM_S0, TM_P1 = OWN_P ? TM_O1 + 64 : TM_S1;
   static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);   // Q (K-major) x K^T (K-major)
   static constexpr uint32_t IDESC_PV = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
+  // the issuer of both products wants more than one of each; with 64 registers it spills and a step takes 10% longer
+  static constexpr int REG_CTRL = OWN_P ? 80 : 96, REG_OUT = 48, REG_SOFTMAX = OWN_P ? 192 : 184;
+  static_assert(REG_CTRL + REG_OUT + 2 * REG_SOFTMAX <= 4 * kRegLaunch,
+                "setmaxnreg targets exceed the launch registers");
 };
 static_assert(Win<64>::SMEM <= 232448 && Win<128>::SMEM <= 232448, "shared memory budget");
 
@@ -80,13 +86,24 @@ struct Bars {
   uint64_t s_read[2];    // OWN_P: S(j) is in the softmax warps' registers
   uint64_t p_full[2];
   uint64_t o_done[2];    // the unit's last P V is complete; OWN_P: every step's
+  uint64_t l_full[2];    // the unit's 1 / l are written (and, OWN_P, all but the last o_done have passed)
+  uint64_t o_free[2];    // the unit's O has been read out of TMEM
   uint32_t tmem_base;
   int32_t abort;
 };
-static_assert(sizeof(Bars) <= 256, "barrier space");
+static_assert(sizeof(Bars) <= 512, "barrier space");
 
 // workspace header: the number of listed work units sits after the status word
 constexpr size_t kWsItemTotal = 128;
+
+// Bulk copies of a thread's own: shared memory to global (16-byte aligned), and the wait until all that it
+// has committed have been read from shared memory.
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 
 __device__ __forceinline__ void on_timeout(Bars* b, int32_t* status) {
   set_status(status, VCS_ERR_DEVICE_TIMEOUT);
@@ -256,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                        float* __restrict__ lse, int32_t* status) {
   using C = Win<D>;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* smem = smem_raw;
   Bars* bars = reinterpret_cast<Bars*>(smem + C::OFF_BAR);
 
   const int G = hq / hkv;
@@ -265,6 +282,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if ((int)blockIdx.x >= total) return;  // the grid is bounded by an upper bound of the listed units
   // once any CTA of this launch has given up on a wait, those not started stand down
   if (st == VCS_ERR_DEVICE_TIMEOUT) return;
+  // The tiles' 128-byte swizzle wants 1,024-byte aligned blocks.  A kernel without static shared memory gets
+  // its dynamic shared memory so aligned; there is no room to align it here.
+  if (smem_u32(smem) & 1023u) {
+    if (threadIdx.x == 0) set_status(status, VCS_ERR_CUDA);
+    return;
+  }
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t sbase = smem_u32(smem);
@@ -282,6 +305,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars->s_read[i], 4);
       mbar_init(&bars->p_full[i], 128);
       mbar_init(&bars->o_done[i], 1);
+      mbar_init(&bars->l_full[i], 128);
+      mbar_init(&bars->o_free[i], 4);
     }
     bars->abort = 0;
     fence_mbar_init();
@@ -298,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // Every role walks the same units and counts what it has passed: ring items (`ib`) and groups (`gb`) before
   // the unit, units (`un`), and per tile the steps taken.
   if (warp < 4) {
-    setmaxnreg_dec<kRegCtrl>();
+    setmaxnreg_dec<C::REG_CTRL>();
     if (warp == 0 && lane == 0) {
     // ------------------------------------------------------------ producer
       tma_prefetch_desc(&tm_q);
@@ -367,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // every lane runs every step, one that has given up waits no more, and the elected lane issues as
       // long as its own waits were met.  A vote a unit ends the walk.
       bool ok = true;
-      uint32_t ib = 0, un = 0, steps[2] = {0, 0};
+      uint32_t ib = 0, un = 0, steps[2] = {0, 0}, outs[2] = {0, 0};
       int4 e = items[blockIdx.x];
       for (int i = blockIdx.x; i < total; i += gridDim.x) {
         const Unit u(e, window, sinks);
@@ -389,11 +414,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_commit(&bars->s_full[t]);
               }
             } else {
+              const bool more = j > (t == 1 && u.skip == 0 ? 1 : 0);
               ok = ok && mbar_wait(&bars->p_full[t], steps[t] & 1);
+              if (!more) {  // O of the unit before has been read
+                if (outs[t] > 0) ok = ok && mbar_wait(&bars->o_free[t], (outs[t] - 1) & 1);
+                ++outs[t];
+              }
               tc_fence_after();
               if (elect_one() && ok) {
                 issue_pv<D>(tmem + (t ? C::TM_O1 : C::TM_O0), tmem + (t ? C::TM_P1 : C::TM_P0),
-                            desc_at(kv_mnmaj, slot * C::TILE), j > (t == 1 && u.skip == 0 ? 1 : 0));
+                            desc_at(kv_mnmaj, slot * C::TILE), more);
                 tc_commit(&bars->o_done[t]);
               }
             }
@@ -417,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t q0d = smem_desc(sbase + C::OFF_Q0, 16, 1024), q1d = desc_at(q0d, C::TILE);
       const uint64_t kv_kmaj = smem_desc(sbase + C::OFF_KV, 16, 1024);
       const uint64_t kv_mnmaj = smem_desc(sbase + C::OFF_KV, C::BLOCK, 1024);
-      uint32_t ib = 0, gb = 0, un = 0, p0 = 0, p1 = 0;
+      uint32_t ib = 0, gb = 0, un = 0, p0 = 0, p1 = 0, un1 = 0;  // un1: units with a tile 1
       auto acquire_group = [&](uint32_t g) {
         ok &= mbar_wait(&bars->grp_full[g % C::NGRP], (g / C::NGRP) & 1);
         tc_fence_after();
@@ -450,6 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (next) kaddr = slot_off(u.k_item(j + 1));
           if (j < u.n0) {  // tile 0: O0 += P0(j) V_j, then S0(j+1)
             ok &= mbar_wait(&bars->p_full[0], p0++ & 1);
+            if (j == 0 && un > 0) ok &= mbar_wait(&bars->o_free[0], (un - 1) & 1);  // O of the unit before read
             tc_fence_after();
             if (elect_one() && ok) {
               issue_pv<D>(tmem + C::TM_O0, tmem + C::TM_S0, desc_at(kv_mnmaj, vaddr), j > 0);
@@ -463,13 +494,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
           }
           if (u.has1) {  // tile 1
+            const bool more = j > (u.skip == 0 ? 1 : 0);
             if (j != u.skip) {
               ok &= mbar_wait(&bars->p_full[1], p1++ & 1);
+              if (!more && un1 > 0) ok &= mbar_wait(&bars->o_free[1], (un1 - 1) & 1);
               tc_fence_after();
             }
             if (elect_one() && ok) {
-              if (j != u.skip)
-                issue_pv<D>(tmem + C::TM_O1, tmem + C::TM_S1, desc_at(kv_mnmaj, vaddr), j > (u.skip == 0 ? 1 : 0));
+              if (j != u.skip) issue_pv<D>(tmem + C::TM_O1, tmem + C::TM_S1, desc_at(kv_mnmaj, vaddr), more);
               if (next && j + 1 != u.skip) {
                 issue_s<D>(tmem + C::TM_S1, q1d, desc_at(kv_kmaj, kaddr));
                 tc_commit(&bars->s_full[1]);
@@ -488,12 +520,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         ib += 2 * u.nkv;
         gb += u.nkv + 1;
         ++un;
+        if (u.has1) ++un1;
       }
       if (!ok) on_timeout(bars, status);
     }
-  } else {
+  } else if (warp < 12) {
     // ------------------------------------------------------------ softmax
-    setmaxnreg_inc<kRegSoftmax>();
+    setmaxnreg_inc<C::REG_SOFTMAX>();
     const int wg = (warp - 4) >> 2;
     const int quad = warp & 3;
     const int r = quad * 32 + lane;  // query row within the tile
@@ -502,8 +535,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t o_col = wg == 0 ? C::TM_O0 : C::TM_O1;
     const uint32_t p_col = wg == 0 ? C::TM_P0 : C::TM_P1;
     const uint64_t sc2 = f2pack(scale_log2, scale_log2);
-    const uint32_t stage = sbase + C::OFF_OUT + wg * C::BLOCK;
-    uint32_t ib = 0, steps = 0, outs = 0;  // outs: phases of o_done passed
+    float* inv_s = reinterpret_cast<float*>(smem + C::OFF_OUT + r * C::OUT_ROW + D * 2) + wg;
+    uint32_t ib = 0, steps = 0, un = 0;
     bool ok = true;
     int4 e = items[blockIdx.x];
     for (int i = blockIdx.x; ok && i < total; i += gridDim.x) {
@@ -550,19 +583,24 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars->s_read[wg]);
         }
+        // Column c of key tile kt is ahead of row r if c > r + ahead, and behind its window if
+        // c <= r + ahead - window, unless it is a sink (c < keep).  A bit a column says what the row sees, so that a
+        // masked tile takes two instructions an element and shares the rest of the code with the others: code of
+        // its own for masked tiles, which leaves out the exponentials of hidden columns, made the warps wait for
+        // instructions (28/4/128, 32 segments of 4,096, window 256: 1.09 ms against 0.77).
         const int kt = u.kt(j);
-        if (kt == mt) {  // diagonal tile: key c is visible to row r only if c <= r
-#pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c > r) s[c] = __float_as_uint(kHidden);
-        }
-        // keys c <= r + ahead - window are behind the window, and hidden unless they are sinks
         const int ahead = (mt - kt) * 128, keep = sinks - kt * 128;
-        if (ahead + 127 >= window && keep < 128) {
-          const int behind = r + ahead - window;
+        if (ahead == 0 || (ahead + 127 >= window && keep < 128)) {
+          auto low = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+          const int last = r + ahead;
 #pragma unroll
-          for (int c = 0; c < 128; ++c)
-            if (c <= behind && c >= keep) s[c] = __float_as_uint(kHidden);
+          for (int ch = 0; ch < 4; ++ch) {
+            const int c0 = 32 * ch;
+            const uint32_t seen = low(last + 1 - c0) & (~low(last - window + 1 - c0) | low(keep - c0));
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if (!(seen >> c & 1)) s[c0 + c] = __float_as_uint(kHidden);
+          }
         }
         // row maximum: 8 independent three-input chains
         float pm[8];
@@ -600,10 +638,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         f2unpack(fadd2(acc[0], acc[1]), a0, a1);
         f2unpack(fadd2(acc[2], acc[3]), b0, b1);
         l = l * alpha + ((a0 + a1) + (b0 + b1));
-        if (C::OWN_P && !first) {  // the P V before is complete: P's columns are free and O is up to date
-          if (!mbar_wait_warp(&bars->o_done[wg], outs & 1)) { ok = false; break; }
-          ++outs;
-          if (releaser) release_v(j - 1 - (u.skip >= 0 && j == u.skip + 1 ? 1 : 0));
+        if (C::OWN_P && steps > 1) {  // the P V before is complete: P's columns are free and O is up to date
+          if (!mbar_wait_warp(&bars->o_done[wg], steps & 1)) { ok = false; break; }
+          if (releaser && !first) release_v(j - 1 - (u.skip >= 0 && j == u.skip + 1 ? 1 : 0));
           tc_fence_after();
         }
         tmem_st_32x32b_x32(trow + p_col, *reinterpret_cast<uint32_t(*)[32]>(&s[0]));
@@ -631,59 +668,86 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_arrive(&bars->p_full[wg]);
         first = false;
       }
-      if (ok) ok = mbar_wait_warp(&bars->o_done[wg], outs & 1);
-      ++outs;
       // another role's giving up is looked for once a unit; the waits are bounded without it
       if (ok && __any_sync(0xffffffffu, aborted(bars))) ok = false;
+      // 1 / l of the unit before has been read, and its l_full waited for
+      if (ok && un > 0) ok = mbar_wait_warp(&bars->o_free[wg], (un - 1) & 1);
       if (!ok) break;
-      if (releaser) release_v(u.nkv - 1);
       ib += 2 * u.nkv;
-      if (mt * C::BM + quad * 32 < u.L) {  // the warp has rows in the segment
-        tc_fence_after();
-        const int row = mt * C::BM + r;
-        const float inv_l = 1.f / l;
-        const uint64_t il2 = f2pack(inv_l, inv_l);
-        // A column block of the warp's 32 rows passes through the warp's part of the staging buffer, so that 8
-        // lanes store a row's 128 bytes.
-        const int row0 = quad * 32 + (lane >> 3), chunk = lane & 7;
-        __nv_bfloat16* dst = out + ((size_t)(u.start + mt * C::BM + row0) * hq + u.h[wg]) * D + chunk * 8;
-#pragma unroll
-        for (int kb = 0; kb < C::KB; ++kb) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t o[32];
-            tmem_ld_32x32b_x32(trow + o_col + kb * 64 + c * 32, o);
-            tmem_ld_wait();
-            reg_fence<32>(o);
-            uint32_t pk[16];
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              float x0, x1;
-              f2unpack(fmul2(f2pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), il2), x0, x1);
-              pk[x] = pack_bf16(x0, x1);
-            }
-#pragma unroll
-            for (int v4 = 0; v4 < 4; ++v4)
-              st_shared_v4(stage + r * 128 + (uint32_t)(((c * 4 + v4) ^ (r & 7)) << 4), pk[4 * v4], pk[4 * v4 + 1],
-                           pk[4 * v4 + 2], pk[4 * v4 + 3]);
-          }
-          asm volatile("" ::: "memory");
-          __syncwarp();
-          asm volatile("" ::: "memory");
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int ri = row0 + 4 * x;
-            const uint4 v = ld_shared_v4(stage + ri * 128 + (uint32_t)((chunk ^ (ri & 7)) << 4));
-            if (mt * C::BM + ri < u.L) *reinterpret_cast<uint4*>(dst + (size_t)(4 * x) * hq * D + kb * 64) = v;
-          }
-          asm volatile("" ::: "memory");
-          __syncwarp();
-          asm volatile("" ::: "memory");
-        }
-        if (row < u.L)
-          lse[(size_t)u.h[wg] * num_tokens + u.start + row] = (m_run + lg2(l)) * 0.69314718055994531f;
-      }
+      *inv_s = 1.f / l;
+      mbar_arrive(&bars->l_full[wg]);
+      ++un;
+      const int row = mt * C::BM + r;
+      if (row < u.L)
+        lse[(size_t)u.h[wg] * num_tokens + u.start + row] = (m_run + lg2(l)) * 0.69314718055994531f;
     }
+    if (!ok) on_timeout(bars, status);
+  } else {
+    // ------------------------------------------------------------ O
+    setmaxnreg_dec<C::REG_OUT>();
+    const int quad = warp & 3;
+    const int r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t stage = sbase + C::OFF_OUT + r * C::OUT_ROW;
+    uint32_t ib = 0, un[2] = {0, 0}, steps[2] = {0, 0};
+    bool ok = true;
+    int4 e = items[blockIdx.x];
+    for (int i = blockIdx.x; ok && i < total; i += gridDim.x) {
+      const Unit u(e, window, sinks);
+      if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (t == 1 && !u.has1) continue;
+        steps[t] += t == 0 ? u.n0 : u.nkv - (u.skip >= 0 ? 1 : 0);
+        // o_done of the unit's last step: behind l_full, all phases before it have passed
+        if (!mbar_wait_warp(&bars->l_full[t], un[t] & 1) ||
+            !mbar_wait_warp(&bars->o_done[t], (C::OWN_P ? steps[t] - 1 : un[t]) & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // every MMA of the unit is complete: its last V may be overwritten (OWN_P: and the one before it, if
+        // tile 1 skipped that step and so could not say when it was done)
+        if (t == (u.has1 ? 1 : 0) && quad == 0 && lane == 0) {
+          if (C::OWN_P && u.skip >= 0 && u.skip == u.nkv - 2)
+            mbar_arrive(&bars->kv_empty[(ib + u.v_item(u.nkv - 2)) % C::NSLOT]);
+          mbar_arrive(&bars->kv_empty[(ib + u.v_item(u.nkv - 1)) % C::NSLOT]);
+        }
+        const float inv_l = reinterpret_cast<const float*>(smem + C::OFF_OUT + r * C::OUT_ROW + D * 2)[t];
+        const uint64_t il2 = f2pack(inv_l, inv_l);
+        bulk_wait_read();  // the thread's row of the tile before has left the staging buffer
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld_32x32b_x32(trow + (t ? C::TM_O1 : C::TM_O0) + c * 32, o);
+          tmem_ld_wait();
+          reg_fence<32>(o);
+          if (c == D / 32 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->o_free[t]);
+          }
+          uint32_t pk[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            float x0, x1;
+            f2unpack(fmul2(f2pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), il2), x0, x1);
+            pk[x] = pack_bf16(x0, x1);
+          }
+#pragma unroll
+          for (int v4 = 0; v4 < 4; ++v4)
+            st_shared_v4(stage + c * 64 + v4 * 16, pk[4 * v4], pk[4 * v4 + 1], pk[4 * v4 + 2], pk[4 * v4 + 3]);
+        }
+        fence_proxy_async_smem();
+        const int row = u.m[t] * C::BM + r;
+        if (row < u.L)
+          bulk_store(out + ((size_t)(u.start + row) * hq + u.h[t]) * D, stage, D * 2);
+        bulk_commit();
+        ++un[t];
+      }
+      ib += 2 * u.nkv;
+    }
+    bulk_wait_read();  // shared memory outlives the copies that read it
     if (!ok) on_timeout(bars, status);
   }
 
