@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     int sub, head, first, count;  // first head and heads (d = 128); row blocks and last head + 1 (d = 64)
     int low;                      // WIN: the first row block
     __device__ __forceinline__ void next() {
-      if constexpr (D == 64) {
+      if constexpr (D == 64 || WIN) {
         if (++sub == first) {
           sub = WIN ? low : 0;
           ++head;
@@ -409,9 +409,9 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
         --sub;
       }
     }
-    __device__ __forceinline__ bool live() const { return D == 64 ? head < count : sub >= (WIN ? low : 0); }
+    __device__ __forceinline__ bool live() const { return D == 64 || WIN ? head < count : sub >= 0; }
   };
-  const Walk walk0 = D == 64 ? Walk{sub0, g * G, nsub, g * G + G, sub0} : Walk{nsub - 1, g * G, g * G, G, sub0};
+  const Walk walk0 = D == 64 || WIN ? Walk{sub0, g * G, nsub, g * G + G, sub0} : Walk{nsub - 1, g * G, g * G, G, sub0};
   // lse and D of query i of w's tile, as loaded: scaled only where they are staged
   auto row_terms = [&](const Walk& w, int i, bool mine, float& l, float& dd) {
     l = __int_as_float(0x7f800000);  // +inf: query outside the segment -> P = 0
@@ -779,18 +779,19 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
           x[x0 + c + 1] = __float_as_uint(ex2(b));
         }
         const int hide = dlim - 64 * (ch >> 1) - x0;
-        if (hide > 0) {
+        if constexpr (WIN) {
+          const int from = wlim - 64 * (ch >> 1) - x0;
+          if (hide > 0 || from < 16) {  // bit c: column c is seen
+            const uint32_t seen = (from >= 16 ? 0xffffu : from <= 0 ? 0u : (1u << from) - 1u) &
+                                  (hide >= 16 ? 0u : hide <= 0 ? 0xffffu : 0xffffu << hide);
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              if (!(seen >> c & 1)) x[x0 + c] = 0u;
+          }
+        } else if (hide > 0) {
 #pragma unroll
           for (int c = 0; c < 16; ++c)
             if (c < hide) x[x0 + c] = 0u;
-        }
-        if constexpr (WIN) {
-          const int from = wlim - 64 * (ch >> 1) - x0;
-          if (from < 16) {
-#pragma unroll
-            for (int c = 0; c < 16; ++c)
-              if (c >= from) x[x0 + c] = 0u;
-          }
         }
         uint32_t pk[8];
 #pragma unroll
@@ -1074,36 +1075,36 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
   }
 }
 
-// dK and dV of the keys of split sink tiles: their parts' sums added in order, four dims a thread.
+// dK and dV of the keys of split sink tiles: their parts' sums added in order, four dims a thread, and a block
+// 1,024 values of a tile.
 template <int D>
 __global__ void __launch_bounds__(256) bwd_sink_sum(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
                                                     int32_t num_tokens, int32_t max_seqlen, int32_t hkv,
                                                     const WinArgs win, __nv_bfloat16* __restrict__ dk,
                                                     __nv_bfloat16* __restrict__ dv) {
-  const int64_t slots = sink_slots(num_tokens, win.chunk), groups = (int64_t)num_segments * hkv * win.tiles;
-  for (int64_t b = blockIdx.x; b < groups; b += gridDim.x) {
-    const int n = (int)(b % win.tiles), g = (int)(b / win.tiles % hkv), seg = (int)(b / win.tiles / hkv);
+  constexpr int PER = 2 * 128 * D / 4 / 256;  // blocks of a tile: dK, then dV
+  const int64_t slots = sink_slots(num_tokens, win.chunk), blocks = (int64_t)num_segments * hkv * win.tiles * PER;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+    const int i = (int)(b % PER) * 256 + threadIdx.x;  // float4 of dK and dV
+    const int64_t t = b / PER;
+    const int n = (int)(t % win.tiles), g = (int)(t / win.tiles % hkv), seg = (int)(t / win.tiles / hkv);
     const int start = cu_seqlens[seg], end = cu_seqlens[seg + 1];
     if (start < 0 || end < start || end > num_tokens || end - start > max_seqlen || (seg == 0 && start != 0) ||
         (seg == num_segments - 1 && end != num_tokens))
       continue;  // as bwd_main
-    const int L = end - start, rows = min(128, L - n * 128);
-    if (rows <= 0) continue;
+    const int L = end - start, which = i / (32 * D), j = i % (32 * D), row = j / (D / 4);
+    if (n * 128 + row >= L) continue;
     const int parts = sink_parts(win, (L - n * 128 + 127) / 128);
     if (parts <= 1) continue;
-    const float* base = win.acc + ((int64_t)g * win.tiles + n) * slots * 2 * (128 * D);
-    for (int i = threadIdx.x; i < 2 * rows * (D / 4); i += 256) {
-      const int which = i / (rows * (D / 4)), j = i % (rows * (D / 4));  // dK, dV; float4 of the tile
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int p = 0; p < parts; ++p) {
-        const float4 x = __ldg(reinterpret_cast<const float4*>(
-                                   base + (sink_slot(start, p, win.chunk) * 2 + which) * (128 * D)) + j);
-        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
-      }
-      __nv_bfloat16* out = (which == 0 ? dk : dv) +
-                           ((size_t)(start + n * 128 + j / (D / 4)) * hkv + g) * D + j % (D / 4) * 4;
-      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
+    const float* base = win.acc + (((int64_t)g * win.tiles + n) * slots * 2 + which) * (128 * D);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) {
+      const float4 x = __ldg(reinterpret_cast<const float4*>(base + sink_slot(start, p, win.chunk) * 2 * (128 * D)) + j);
+      sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
     }
+    __nv_bfloat16* out = (which == 0 ? dk : dv) + ((size_t)(start + n * 128 + row) * hkv + g) * D + j % (D / 4) * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
   }
 }
 
@@ -1220,7 +1221,7 @@ cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, con
     if (WIN && win.parts > 1) {
       e = cudaGetLastError();
       if (e != cudaSuccess) return e;
-      int64_t blocks = gx * win.tiles;
+      int64_t blocks = gx * win.tiles * (2 * 128 * D / 4 / 256);
       if (blocks > 152 * 32) blocks = 152 * 32;
       bwd_sink_sum<D><<<(unsigned)blocks, 256, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens,
                                                         a.max_seqlen, a.hkv, win, static_cast<__nv_bfloat16*>(dk),
