@@ -342,9 +342,9 @@ __global__ void __launch_bounds__(256) inverse_offsets(const int32_t* __restrict
 }
 
 // ------------------------------------------------------------------ rotation
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 128;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kBatch = 8;  // copies of a trajectory row whose angles a warp holds (backward)
+constexpr int kBatch = 8;  // copies of rows whose angles a warp holds
 constexpr int kMaxPairs = VCS_ROPE_MAX_PAIRS;
 
 struct RopeArgs {
@@ -357,6 +357,7 @@ struct RopeArgs {
   const int32_t* off;            // backward: inv_off
   int32_t hq, hkv;
   int32_t chunks;                // 16-byte chunks of a row
+  int32_t per;                   // rows a warp takes together
   int32_t turned;                // items of a row that are rotated (pairs of chunks, or chunks if interleaved)
   int32_t plain;                 // and its chunks that are not
   uint32_t turned_magic, plain_magic;  // of div_by
@@ -380,13 +381,11 @@ __device__ __forceinline__ void st_stream(int4* p, int4 v) {
 // the two bf16 of a word, exactly
 __device__ __forceinline__ float lo_f(int w) { return __uint_as_float((uint32_t)w << 16); }
 __device__ __forceinline__ float hi_f(int w) { return __uint_as_float((uint32_t)w & 0xffff0000u); }
-__device__ __forceinline__ void unpack8(int4 x, float (&f)[8]) {
-  f[0] = lo_f(x.x), f[1] = hi_f(x.x), f[2] = lo_f(x.y), f[3] = hi_f(x.y);
-  f[4] = lo_f(x.z), f[5] = hi_f(x.z), f[6] = lo_f(x.w), f[7] = hi_f(x.w);
-}
-__device__ __forceinline__ int4 pack8(const float* f) {
-  return make_int4((int)dev::pack_bf16(f[0], f[1]), (int)dev::pack_bf16(f[2], f[3]), (int)dev::pack_bf16(f[4], f[5]),
-                   (int)dev::pack_bf16(f[6], f[7]));
+__device__ __forceinline__ int& word(int4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+__device__ __forceinline__ int pack2(uint64_t f) {
+  float a, b;
+  dev::f2unpack(f, a, b);
+  return (int)dev::pack_bf16(a, b);
 }
 
 // i / c by the magic 2^32 / c + 1, exactly for i < 2^32 / c; c = 1 has none
@@ -394,217 +393,243 @@ __device__ __forceinline__ int div_by(int i, int c, uint32_t magic) {
   return c == 1 ? i : (int)__umulhi((uint32_t)i, magic);
 }
 
-// One warp per output token.  Lane l computes the angles of pairs l, l + 32, ... of the token's copies into
-// the warp's table, then the lanes take the row's items in turn.  An item is, with pairs (i, i + rot/2), the
-// chunks of eight dims c and c + rot/16, which hold eight whole pairs; with neighbouring pairs, one chunk
-// of four.  The table holds two pairs (cos, sin, cos, sin) in 16 bytes, at [pair of the item / 2][item of
+// A warp takes `per` consecutive output tokens, one where a row is some 8 KB or more.  Lane l computes the
+// angles of pairs l, l + 32, ... of all their copies into the warp's table (forward: a token has one copy), then
+// the lanes take each row's items in turn.  An item is, with pairs (i, i + rot/2), the chunks of eight dims c and
+// c + rot/16, which hold eight whole pairs; with neighbouring pairs, one chunk of four.  The table holds two
+// pairs (cos, cos, sin, sin) in 16 bytes, the operands of packed fp32 arithmetic, at [pair of the item / 2][item of
 // the row], so that lanes on neighbouring items read neighbouring 16 bytes.
 template <int NP, bool INTER, bool BWD>
-__global__ void __launch_bounds__(kRopeThreads) rope_rows(const __grid_constant__ RopeArgs a) {
-  constexpr int B = BWD ? kBatch : 1;
-  constexpr int IP = INTER ? 4 : 8;        // pairs of an item
+__global__ void __launch_bounds__(kRopeThreads, 8) rope_rows(const __grid_constant__ RopeArgs a) {
+  constexpr int B = kBatch;
+  constexpr int H = INTER ? 2 : 4;         // two pairs each: an item's table entries
   constexpr int IC = INTER ? 1 : 2;        // chunks of an item
-  constexpr int U = INTER ? 4 : 2;         // items a lane has in flight
+  constexpr int U = INTER ? 2 : 1;         // items a lane has in flight
   extern __shared__ float4 table[];        // [warp][copy][NP * 16]
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  float4* tab = table + (size_t)wid * B * NP * 16;
+  float4* tab = table + (size_t)wid * (BWD ? B : a.per) * NP * 16;
   uint64_t turn[NP];
-  int axis[NP];
+  int axis[NP], slot[NP];                  // slot: of the pair's cosine in the table, as floats; -1: none
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
-    turn[p] = a.turn[lane + 32 * p];
-    axis[p] = a.axis[lane + 32 * p];
+    const int pair = lane + 32 * p, item = pair / (2 * H), k = pair % (2 * H);
+    turn[p] = a.turn[pair];
+    axis[p] = a.axis[pair];
+    slot[p] = pair < a.turned * 2 * H ? 4 * ((k >> 1) * a.turned + item) + (k & 1) : -1;
   }
   const int heads = a.hq + a.hkv;
   const int turned = heads * a.turned, plain = heads * a.plain;
-  const int64_t warps = (int64_t)gridDim.x * kRopeWarps;
-  for (int64_t r = blockIdx.x * (int64_t)kRopeWarps + wid; r < a.rows_out; r += warps) {
-    // the row's copies: list[0 .. m), or row `only` alone
-    int64_t m = 1, only = r;
-    const int32_t* list = nullptr;
-    if constexpr (BWD) {
-      if (a.off != nullptr) {
-        const int32_t lo = __ldg(&a.off[r]), hi = __ldg(&a.off[r + 1]);
-        const bool ok = lo >= 0 && hi >= lo && hi <= a.rows_in;
-        if (!ok && lane == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
-        m = ok ? hi - lo : 0;
-        list = a.map + lo;
-      }
-    } else if (a.map != nullptr) {
-      only = __ldg(&a.map[r]);
-      if (only < 0 || only >= a.rows_in) {
-        if (lane == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
-        continue;
-      }
-    }
-    // copy j of the batch at b0: its row, on every lane; -1 outside the rows
-    int64_t held = -1;
-    auto hold = [&](int64_t b0) {
-      if constexpr (BWD) {
-        held = only;
-        if (list != nullptr) {
-          held = b0 + lane < m && lane < B ? __ldg(&list[b0 + lane]) : -1;
-          if (held < -1 || held >= a.rows_in || (held < 0 && b0 + lane < m && lane < B)) {
-            set_status(a.status, VCS_ERR_DEVICE_CHECK);
-            held = -1;
+  const int q_row = a.hq * a.chunks, kv_row = a.hkv * a.chunks;  // chunks of a token
+  const int64_t stride = (int64_t)gridDim.x * kRopeWarps * a.per;
+  for (int64_t r0 = (blockIdx.x * (int64_t)kRopeWarps + wid) * a.per; r0 < a.rows_out; r0 += stride) {
+    const int rows = (int)(a.rows_out - r0 < a.per ? a.rows_out - r0 : a.per);
+    // held: on lane j, the input row of copy j of the batch, -1 for none
+    int held = -1;
+    // of `count` copies; their positions are those of tokens first + j (forward) or of the rows held
+    auto angles = [&](int count, int64_t first) {
+      __syncwarp();
+      for (int j = 0; j < count; ++j) {
+        const int64_t n = BWD ? __shfl_sync(0xffffffffu, held, j) : first + j;
+        if (n < 0) continue;
+        float* t = reinterpret_cast<float*>(tab + j * NP * 16);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          const uint64_t ph = (uint64_t)(int64_t)__ldg(&a.pos[axis[p] * a.pos_stride + n]) * turn[p];
+          float s, c;
+          sincospif((float)(int32_t)(ph >> 32) * 0x1p-31f, &s, &c);
+          if (slot[p] >= 0) {
+            t[slot[p]] = c;
+            t[slot[p] + 2] = BWD ? -s : s;
           }
         }
       }
-    };
-    auto copy = [&](int j) -> int64_t {
-      if constexpr (BWD) return __shfl_sync(0xffffffffu, held, list != nullptr ? j : 0);
-      else return only;
-    };
-    auto angles = [&](int count) {
-      __syncwarp();
-      for (int j = 0; j < count; ++j) {
-        const int64_t n = BWD ? copy(j) : r;
-        if (n < 0) continue;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int pair = lane + 32 * p;
-          if (pair >= a.turned * IP) continue;
-          const int32_t x = __ldg(&a.pos[axis[p] * a.pos_stride + n]);
-          const uint64_t ph = (uint64_t)(int64_t)x * turn[p];
-          float s, c;
-          sincospif((float)(int32_t)(ph >> 32) * 0x1p-31f, &s, &c);
-          const int item = pair / IP, k = pair % IP;
-          reinterpret_cast<float2*>(tab + (size_t)j * NP * 16)[2 * ((k >> 1) * a.turned + item) + (k & 1)] =
-              make_float2(c, BWD ? -s : s);
-        }
-      }
       __syncwarp();
     };
-    bool ready = false;
-    for (int i0 = 0; i0 < turned; i0 += 32 * U) {
-      float acc[U][8 * IC];
-      int at[U];        // chunk of the item in its row of q or k
-      int row[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + 32 * u + lane;
-        row[u] = div_by(i, a.turned, a.turned_magic);
-        at[u] = i - row[u] * a.turned;
-#pragma unroll
-        for (int e = 0; e < 8 * IC; ++e) acc[u][e] = 0.f;
-        if (i >= turned) row[u] = -1;
+    // a batch of copies: on lanes j < count, row j of the list (or, without one, rows r0 + j themselves)
+    auto hold = [&](const int32_t* list, int count) {
+      const bool mine = lane < count;
+      held = !mine ? -1 : list != nullptr ? __ldg(&list[lane]) : (int)r0 + lane;
+      if (mine && (held < 0 || held >= a.rows_in)) {
+        set_status(a.status, VCS_ERR_DEVICE_CHECK);
+        held = -1;
       }
-      for (int64_t b0 = 0; b0 < m; b0 += B) {
-        const int cnt = (int)(m - b0 < B ? m - b0 : B);
-        if (!ready || m > B) {
-          hold(b0);
-          angles(cnt);
-          ready = true;
-        }
-        for (int j = 0; j < cnt; ++j) {
-          const int64_t n = copy(j);
-          if (n < 0) continue;
-          int4 x[U][IC];
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (row[u] >= 0) {
-              const int4* src = row[u] < a.hq ? a.q_in + (n * a.hq + row[u]) * a.chunks
-                                              : a.k_in + (n * a.hkv + (row[u] - a.hq)) * a.chunks;
-#pragma unroll
-              for (int e = 0; e < IC; ++e) x[u][e] = ld_stream(src + at[u] + e * a.turned);
-            }
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (row[u] >= 0) {
-              float f[8 * IC], g[8 * IC];
-#pragma unroll
-              for (int e = 0; e < IC; ++e) unpack8(x[u][e], *reinterpret_cast<float(*)[8]>(&f[8 * e]));
-              const float4* t = tab + (size_t)j * NP * 16 + at[u];
-#pragma unroll
-              for (int k = 0; k < IP; k += 2) {
-                const float4 cs = t[(k >> 1) * a.turned];
-                const int i0p = INTER ? 2 * k : k, i1p = INTER ? 2 * k + 2 : k + 1;   // first dims of the pairs
-                const int o = INTER ? 1 : 8;                                          // to their second dims
-                g[i0p] = f[i0p] * cs.x - f[i0p + o] * cs.y;
-                g[i0p + o] = f[i0p + o] * cs.x + f[i0p] * cs.y;
-                g[i1p] = f[i1p] * cs.z - f[i1p + o] * cs.w;
-                g[i1p + o] = f[i1p + o] * cs.z + f[i1p] * cs.w;
-              }
-#pragma unroll
-              for (int e = 0; e < 8 * IC; ++e) acc[u][e] = BWD ? acc[u][e] + g[e] : g[e];
-            }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (row[u] >= 0) {
-          int4* dst = row[u] < a.hq ? a.q_out + (r * a.hq + row[u]) * a.chunks
-                                    : a.k_out + (r * a.hkv + (row[u] - a.hq)) * a.chunks;
-#pragma unroll
-          for (int e = 0; e < IC; ++e) st_stream(dst + at[u] + e * a.turned, pack8(&acc[u][8 * e]));
-        }
+    };
+    // backward: lane i <= rows holds where row i's copies start in the inverse's list; of an inconsistent
+    // list there are none
+    int start = lane;
+    if (BWD && a.off != nullptr) start = lane <= rows ? __ldg(&a.off[r0 + lane]) : 0;
+    const int64_t most = BWD && a.off != nullptr ? a.rows_in : B;
+    const int next = __shfl_down_sync(0xffffffffu, start, 1);
+    const bool bad = lane < rows && (start < 0 || next < start || next > most);
+    if (bad) set_status(a.status, VCS_ERR_DEVICE_CHECK);
+    // All the rows' copies as one batch if they are few, else a row's at a time.
+    const int begin = __shfl_sync(0xffffffffu, start, 0);
+    const int all = __shfl_sync(0xffffffffu, start, rows) - begin;
+    const bool together = !__any_sync(0xffffffffu, bad) && all <= B;
+    if (together) {
+      hold(BWD ? (a.off != nullptr ? a.map + begin : nullptr) : a.map != nullptr ? a.map + r0 : nullptr, all);
+      angles(all, r0);
     }
-    // chunks that are not rotated: the ends of the rows of q and k, and v
-    const int rest = plain + a.hkv * a.chunks;
-    for (int i0 = 0; i0 < rest; i0 += 64) {
-      const int4* src[2];
-      int4* dst[2];
-      int64_t stride[2];
-      bool live[2];
+    for (int i = 0; i < rows; ++i) {
+      const int64_t r = r0 + i;
+      // the row's copies [lo, lo + m) of the list; j of the batch at b0 is on lane at0 + j
+      const int lo = __shfl_sync(0xffffffffu, start, i), hi = __shfl_sync(0xffffffffu, start, i + 1);
+      const int m = lo >= 0 && hi >= lo && hi <= most ? hi - lo : 0;
+      const int at0 = together ? lo - begin : 0;
+      auto copy = [&](int j) { return __shfl_sync(0xffffffffu, held, at0 + j); };
+      if (!BWD && copy(0) < 0) continue;
+      bool ready = together;
+      for (int i0 = 0; i0 < turned; i0 += 32 * U) {
+        uint64_t acc[U][H][2];  // two pairs' first and second dims
+        int at[U];              // chunk of the item in its token's row of q or k
+        int entry[U];           // item of its head's row
+        bool live[U], is_q[U];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int i = i0 + 32 * u + lane;
-        live[u] = i < rest;
-        if (i < plain) {
-          const int h = div_by(i, a.plain, a.plain_magic);
-          const int c = h * a.chunks + IC * a.turned + i - h * a.plain;
-          const bool is_q = h < a.hq;
-          stride[u] = (int64_t)(is_q ? a.hq : a.hkv) * a.chunks;
-          src[u] = is_q ? a.q_in + c : a.k_in + c - a.hq * a.chunks;
-          dst[u] = is_q ? a.q_out + c : a.k_out + c - a.hq * a.chunks;
-        } else {
-          stride[u] = (int64_t)a.hkv * a.chunks;
-          src[u] = a.v_in + (i - plain);
-          dst[u] = a.v_out + (i - plain);
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * u + lane, h = div_by(i, a.turned, a.turned_magic);
+          live[u] = i < turned;
+          is_q[u] = h < a.hq;
+          entry[u] = i - h * a.turned;
+          at[u] = (is_q[u] ? h : h - a.hq) * a.chunks + entry[u];
+#pragma unroll
+          for (int k = 0; k < H; ++k) acc[u][k][0] = acc[u][k][1] = 0ull;
         }
-      }
-      if constexpr (!BWD) {
-        int4 x[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if (live[u]) x[u] = ld_stream(src[u] + only * stride[u]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if (live[u]) st_stream(dst[u] + r * stride[u], x[u]);
-      } else {
-        float acc[2][8];
-        bool any = false;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[u][e] = 0.f;
-        for (int64_t b0 = 0; b0 < m; b0 += B) {
-          const int cnt = (int)(m - b0 < B ? m - b0 : B);
+        for (int b0 = 0; b0 < m; b0 += B) {
+          const int cnt = m - b0 < B ? m - b0 : B;
           if (!ready || m > B) {
-            hold(b0);
+            hold(a.map + lo + b0, cnt);
+            angles(cnt, 0);
             ready = true;
           }
           for (int j = 0; j < cnt; ++j) {
-            const int64_t n = copy(j);
+            const int n = copy(j);
+            if (n < 0) continue;
+            const int4* qs = a.q_in + (int64_t)n * q_row;
+            const int4* ks = a.k_in + (int64_t)n * kv_row;
+            int4 x[U][IC];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (live[u]) {
+                const int4* src = (is_q[u] ? qs : ks) + at[u];
+#pragma unroll
+                for (int e = 0; e < IC; ++e) x[u][e] = ld_stream(src + e * a.turned);
+              }
+            const float4* t0 = tab + (at0 + j) * NP * 16;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (live[u]) {
+#pragma unroll
+                for (int k = 0; k < H; ++k) {
+                  const float4 cs = t0[k * a.turned + entry[u]];
+                  const uint64_t c = dev::f2pack(cs.x, cs.y), s = dev::f2pack(cs.z, cs.w);
+                  const uint64_t ns = s ^ 0x8000000080000000ull;
+                  uint64_t f, g;  // first and second dims of two pairs
+                  if constexpr (INTER) {
+                    const int w0 = word(x[u][0], 2 * k), w1 = word(x[u][0], 2 * k + 1);
+                    f = dev::f2pack(lo_f(w0), lo_f(w1));
+                    g = dev::f2pack(hi_f(w0), hi_f(w1));
+                  } else {
+                    const int w0 = word(x[u][0], k), w1 = word(x[u][IC - 1], k);
+                    f = dev::f2pack(lo_f(w0), hi_f(w0));
+                    g = dev::f2pack(lo_f(w1), hi_f(w1));
+                  }
+                  acc[u][k][0] = dev::ffma2(g, ns, BWD ? dev::ffma2(f, c, acc[u][k][0]) : dev::fmul2(f, c));
+                  acc[u][k][1] = dev::ffma2(f, s, BWD ? dev::ffma2(g, c, acc[u][k][1]) : dev::fmul2(g, c));
+                }
+              }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (live[u]) {
+            int4* dst = (is_q[u] ? a.q_out + r * q_row : a.k_out + r * kv_row) + at[u];
+            int4 y[IC];
+#pragma unroll
+            for (int k = 0; k < H; ++k) {
+              if constexpr (INTER) {
+                float f0, f1, g0, g1;
+                dev::f2unpack(acc[u][k][0], f0, f1);
+                dev::f2unpack(acc[u][k][1], g0, g1);
+                word(y[0], 2 * k) = (int)dev::pack_bf16(f0, g0);
+                word(y[0], 2 * k + 1) = (int)dev::pack_bf16(f1, g1);
+              } else {
+                word(y[0], k) = pack2(acc[u][k][0]);
+                word(y[IC - 1], k) = pack2(acc[u][k][1]);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < IC; ++e) st_stream(dst + e * a.turned, y[e]);
+          }
+      }
+      // chunks that are not rotated: the ends of the rows of q and k, and v
+      const int rest = plain + kv_row;
+      for (int i0 = 0; i0 < rest; i0 += 64) {
+        const int4* src[2];
+        int4* dst[2];
+        int stride[2];
+        bool live[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int i = i0 + 32 * u + lane;
+          live[u] = i < rest;
+          if (i < plain) {
+            const int h = div_by(i, a.plain, a.plain_magic);
+            const bool is_q = h < a.hq;
+            const int c = (is_q ? h : h - a.hq) * a.chunks + IC * a.turned + i - h * a.plain;
+            stride[u] = is_q ? q_row : kv_row;
+            src[u] = (is_q ? a.q_in : a.k_in) + c;
+            dst[u] = (is_q ? a.q_out : a.k_out) + c;
+          } else {
+            stride[u] = kv_row;
+            src[u] = a.v_in + (i - plain);
+            dst[u] = a.v_out + (i - plain);
+          }
+          dst[u] += r * stride[u];
+        }
+        if (!ready) {
+          hold(a.map + lo, min(m, B));
+          ready = true;
+        }
+        if (!BWD || m == 1) {  // a copy, bit for bit
+          const int n = copy(0);
+          int4 x[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            x[u] = make_int4(0, 0, 0, 0);
+            if (live[u] && n >= 0) x[u] = ld_stream(src[u] + (int64_t)n * stride[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            if (live[u]) st_stream(dst[u], x[u]);
+          continue;
+        }
+        uint64_t acc[2][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[u][e] = 0ull;
+        for (int b0 = 0; b0 < m; b0 += B) {
+          const int cnt = m - b0 < B ? m - b0 : B;
+          if (m > B) hold(a.map + lo + b0, cnt);
+          for (int j = 0; j < cnt; ++j) {
+            const int n = copy(j);
             if (n < 0) continue;
             int4 x[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              if (live[u]) x[u] = ld_stream(src[u] + n * stride[u]);
+              if (live[u]) x[u] = ld_stream(src[u] + (int64_t)n * stride[u]);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              if (live[u]) {
-                float f[8];
-                unpack8(x[u], f);
+              if (live[u])
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[u][e] = any ? acc[u][e] + f[e] : f[e];  // one copy: its bits
-              }
-            any = true;
+                for (int e = 0; e < 4; ++e)
+                  acc[u][e] = dev::fadd2(acc[u][e], dev::f2pack(lo_f(word(x[u], e)), hi_f(word(x[u], e))));
           }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-          if (live[u]) st_stream(dst[u] + r * stride[u], pack8(acc[u]));
+          if (live[u])
+            st_stream(dst[u], make_int4(pack2(acc[u][0]), pack2(acc[u][1]), pack2(acc[u][2]), pack2(acc[u][3])));
       }
     }
   }
@@ -619,11 +644,19 @@ int key_passes(int64_t traj_tokens) {  // 8-bit digits of the keys 0 .. traj_tok
 }
 
 template <bool INTER, bool BWD>
-cudaError_t launch_rope(const RopeArgs& a, int pairs, cudaStream_t st) {
+cudaError_t launch_rope(RopeArgs a, int pairs, cudaStream_t st) {
   const int np = (pairs + 31) / 32;
-  int64_t blocks = (a.rows_out + kRopeWarps - 1) / kRopeWarps;
-  if (blocks > 152 * 8) blocks = 152 * 8;
-  const size_t smem = (size_t)kRopeWarps * (BWD ? kBatch : 1) * np * 16 * sizeof(float4);
+  // Rows of some 8 KB are a warp's each; of smaller ones it takes up to eight together, so that the latencies of
+  // the map, the positions and the sines are met once for all, while enough warps for every SM remain.
+  const int64_t chunks = (int64_t)(a.hq + 2 * a.hkv) * a.chunks;
+  a.per = 1;
+  while (a.per < kBatch && 2 * a.per * chunks <= 512 && a.rows_out >= 2 * a.per * 152 * 32) a.per *= 2;
+  // Backward, a row takes as long as it has copies: a block for every few rows, which the SMs take as they get
+  // free.  One long rollout at 40/8/128, step by step at 14/2/64 (up to 50 copies), us: 1,042 and 613; with blocks
+  // that walk rows in a fixed stride, eight an SM, 1,324 and 925.
+  int64_t blocks = (a.rows_out + kRopeWarps * a.per - 1) / (kRopeWarps * a.per);
+  if (!BWD && blocks > 152 * 32) blocks = 152 * 32;
+  const size_t smem = (size_t)kRopeWarps * (BWD ? kBatch : a.per) * np * 16 * sizeof(float4);
   auto go = [&](auto kernel) {
     if (smem > 48 * 1024) {
       const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
