@@ -27,6 +27,11 @@ namespace {
 
 using dev::set_status;
 
+// i / c by the magic 2^32 / c + 1, exactly for i < 2^32 / c; c = 1 has none
+__device__ __forceinline__ int div_by(int i, int c, uint32_t magic) {
+  return c == 1 ? i : (int)__umulhi((uint32_t)i, magic);
+}
+
 // ------------------------------------------------------------------ positions
 constexpr int kPosThreads = 256;
 constexpr int kPosChunk = 8192;  // tokens of a segment a block writes
@@ -47,6 +52,7 @@ __global__ void __launch_bounds__(kPosThreads)
   __shared__ int32_t run_img[kPosThreads];      // screenshot tokens of the run, 0 if it is text only
   __shared__ int32_t run_skip[kPosThreads];     // positions the screenshot takes
   __shared__ int32_t run_h[kPosThreads], run_w[kPosThreads];
+  __shared__ uint32_t run_hm[kPosThreads], run_wm[kPosThreads];  // magics of div_by; 0: divide
   __shared__ int32_t wsum[kPosThreads / 32];
   __shared__ int32_t carry_s;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -115,6 +121,9 @@ __global__ void __launch_bounds__(kPosThreads)
           run_skip[tid] = skip;
           run_h[tid] = h;
           run_w[tid] = w;
+          // exact below 2^32 / c
+          run_hm[tid] = h > 1 && (int64_t)img * h < (1ll << 32) ? 0xffffffffu / (uint32_t)h + 1u : 0u;
+          run_wm[tid] = w > 1 && (int64_t)img * w < (1ll << 32) ? 0xffffffffu / (uint32_t)w + 1u : 0u;
         }
         int x = adv;
 #pragma unroll
@@ -131,27 +140,37 @@ __global__ void __launch_bounds__(kPosThreads)
         __syncthreads();
         carry = carry_s;
         const int n0 = max(lo_tok, run_at[0]), n1 = min(hi_tok, run_at[kPosThreads]);
-        for (int n = n0 + tid; n < n1; n += kPosThreads) {
-          const int64_t r = (int64_t)src_step[n] - s0;
-          if (r < 0 || r >= kPosThreads || s0 + r > last || n < run_at[r] || n >= run_at[r + 1]) {
-            set_status(status, VCS_ERR_DEVICE_CHECK);  // tok_src_step decreases within the segment
-            continue;
+        for (int m = n0 + tid; m < n1; m += 4 * kPosThreads) {
+          int step[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) step[v] = __ldg(&src_step[min(m + v * kPosThreads, n1 - 1)]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int n = m + v * kPosThreads;
+            if (n >= n1) break;
+            const int64_t r = (int64_t)step[v] - s0;
+            if (r < 0 || r >= kPosThreads || s0 + r > last || n < run_at[r] || n >= run_at[r + 1]) {
+              set_status(status, VCS_ERR_DEVICE_CHECK);  // tok_src_step decreases within the segment
+              continue;
+            }
+            const int k = n - run_at[r], im = run_img[r];
+            int p0 = run_pos[r], p1, p2;
+            if (k < im) {
+              const int h = run_h[r], w = run_w[r];
+              const uint32_t hm = run_hm[r], wm = run_wm[r];
+              const int line = wm != 0u ? div_by(k, w, wm) : k / w;
+              const int frame = hm != 0u ? div_by(line, h, hm) : line / h;
+              p1 = p0 + line - frame * h;
+              p2 = p0 + k - line * w;
+              p0 += frame;
+            } else {
+              p0 += run_skip[r] + k - im;
+              p1 = p2 = p0;
+            }
+            pos[n] = p0;
+            pos[N + n] = p1;
+            pos[2 * N + n] = p2;
           }
-          const int k = n - run_at[r], im = run_img[r];
-          int p0 = run_pos[r], p1, p2;
-          if (k < im) {
-            const int h = run_h[r], w = run_w[r];
-            const int line = k / w, frame = line / h;
-            p1 = p0 + line - frame * h;
-            p2 = p0 + k - line * w;
-            p0 += frame;
-          } else {
-            p0 += run_skip[r] + k - im;
-            p1 = p2 = p0;
-          }
-          pos[n] = p0;
-          pos[N + n] = p1;
-          pos[2 * N + n] = p2;
         }
         const int tile_end = run_at[kPosThreads];
         __syncthreads();
@@ -164,20 +183,30 @@ __global__ void __launch_bounds__(kPosThreads)
 // ------------------------------------------------------------------ inverse map
 // Stable radix sort of (tok_gather[n], n) by 8-bit digits: the n of equal keys stay in order, whatever
 // the map, and no atomic decides an order.  A pass is three launches: digit counts of tiles of kTile
-// keys, per digit the scan of its tiles' counts, and the scatter.  Keys outside [0, T) become T, behind
-// all others.
+// keys, per digit the scan of its tiles' counts, and the scatter; up to one tile of keys is sorted by one block
+// in shared memory.  Keys outside [0, T) become T, behind all others.
 constexpr int kSortThreads = 256;
 constexpr int kPerThread = 16;
 constexpr int kTile = kSortThreads * kPerThread;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int64_t kSmallOffsets = 8192;  // trajectory tokens whose searches take the one block about a launch's time
 
-__device__ __forceinline__ uint32_t load_key(const int32_t* __restrict__ keys, int64_t i, uint32_t T, bool first,
-                                             int32_t* status) {
-  const uint32_t k = (uint32_t)__ldg(&keys[i]);
-  if (first && k >= T) {
-    set_status(status, VCS_ERR_DEVICE_CHECK);
-    return T;
-  }
-  return k;
+// Keys at, at + step, ... before n.  All loads first (the check of a key, which may report, would hold up the next
+// one's load: a pass over 15.8 M keys took 140 us with it in between).
+template <int STEP>
+__device__ __forceinline__ void load_keys(const int32_t* __restrict__ keys, int64_t at, int64_t n, uint32_t T,
+                                          bool first, int32_t* status, uint32_t (&key)[kPerThread]) {
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) key[u] = (uint32_t)__ldg(&keys[at + u * STEP < n ? at + u * STEP : n - 1]);
+  if (!first) return;
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u)
+    if (key[u] >= T) {
+      key[u] = T;
+      bad = bad || at + u * STEP < n;
+    }
+  if (bad) set_status(status, VCS_ERR_DEVICE_CHECK);
 }
 
 __global__ void __launch_bounds__(kSortThreads)
@@ -186,12 +215,12 @@ __global__ void __launch_bounds__(kSortThreads)
   __shared__ int32_t c[256];
   c[threadIdx.x] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kTile;
+  const int64_t base = (int64_t)blockIdx.x * kTile + threadIdx.x;
+  uint32_t key[kPerThread];
+  load_keys<kSortThreads>(keys, base, n, T, first, status, key);
 #pragma unroll
-  for (int u = 0; u < kPerThread; ++u) {
-    const int64_t i = base + u * kSortThreads + threadIdx.x;
-    if (i < n) atomicAdd(&c[(load_key(keys, i, T, first, status) >> shift) & 255u], 1);
-  }
+  for (int u = 0; u < kPerThread; ++u)
+    if (base + u * kSortThreads < n) atomicAdd(&c[(key[u] >> shift) & 255u], 1);
   __syncthreads();
   counts[(size_t)threadIdx.x * tiles + blockIdx.x] = c[threadIdx.x];
 }
@@ -228,66 +257,165 @@ __global__ void __launch_bounds__(1024)
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
-// Warp w of a tile takes its keys [512 w, + 512) in order, 32 at a time: a key's rank among the warp's
-// equal digits is the count of them before it, by a vote among the 32 and a running count.
-__global__ void __launch_bounds__(kSortThreads)
+// Exclusive sum over the block's threads of v.
+__device__ __forceinline__ int block_before(int v, int32_t* wsum) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) wsum[wid] = x;
+  __syncthreads();
+  int at = x - v;
+  for (int i = 0; i < wid; ++i) at += wsum[i];
+  __syncthreads();
+  return at;
+}
+
+struct SortTile {
+  int32_t seen[kSortWarps][256];  // keys of each digit that a warp has passed; then where its next one goes
+  int32_t wsum[kSortWarps];
+  int32_t to[256];                // from a place in the tile to the digit's place in the output
+  uint32_t key[kTile];
+  int32_t val[kTile];
+};
+
+// Places of the tile's keys sorted by a digit.  Warp w has its keys [32 rounds w, + 32 rounds) in order, 32 at a
+// time (key u of a thread is there if 32 u < live, and u < rounds): a key's
+// rank among the warp's equal digits is the count of them before it, by votes on the digit's bits (a match
+// instruction takes several times as long) and a running count.
+// Returns the thread's digit's first place.
+__device__ __forceinline__ int place_tile(SortTile& s, const uint32_t (&key)[kPerThread], int live, int rounds,
+                                          int shift, int (&place)[kPerThread]) {
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) s.seen[w][tid] = 0;
+  __syncthreads();
+  uint32_t same[kPerThread];
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    if (u >= rounds) break;
+    const bool on = 32 * u < live;
+    const uint32_t dg = (key[u] >> shift) & 255u;
+    same[u] = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const bool bit = dg >> b & 1;
+      const uint32_t v = __ballot_sync(0xffffffffu, bit);
+      same[u] &= bit ? v : ~v;
+    }
+    // the first lane of each digit adds; a warp's additions to shared memory are done in order
+    place[u] = 0;
+    if (on && (same[u] & ((1u << lane) - 1u)) == 0) place[u] = atomicAdd(&s.seen[wid][dg], __popc(same[u]));
+  }
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    if (u >= rounds) break;
+    place[u] = __shfl_sync(0xffffffffu, place[u], (__ffs(same[u]) - 1) & 31) + __popc(same[u] & ((1u << lane) - 1u));
+  }
+  __syncthreads();
+  int sum = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) sum += s.seen[w][tid];
+  const int first = block_before(sum, s.wsum);
+  int at = first;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) {
+    const int c = s.seen[w][tid];
+    s.seen[w][tid] = at;
+    at += c;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u)
+    if (u < rounds) place[u] += s.seen[wid][(key[u] >> shift) & 255u];
+  return first;
+}
+
+// The tile is sorted in shared memory first, so that a digit's keys leave as one run: 4-byte stores to 256 places
+// took 265 us of a pass over 15.8 M keys.
+__global__ void __launch_bounds__(kSortThreads, 4)
     inverse_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ vals, int64_t n, uint32_t T,
                     int shift, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, int tiles,
                     bool first, int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
-  constexpr int W = kSortThreads / 32;
-  __shared__ int32_t seen[W][256];
-  __shared__ int32_t wsum[W];
+  __shared__ SortTile s;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-#pragma unroll
-  for (int w = 0; w < W; ++w) seen[w][tid] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kTile + wid * (32 * kPerThread) + lane;
+  const int64_t base = (int64_t)blockIdx.x * kTile;
+  const int here = (int)(n - base < kTile ? n - base : kTile);
+  const int off = wid * (32 * kPerThread) + lane, live = here - off;  // key u of the thread: off + 32 u < here
   uint32_t key[kPerThread];
-  int rank[kPerThread];
+  int val[kPerThread], place[kPerThread];
+  load_keys<32>(keys, base + off, n, T, first, nullptr, key);
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) val[u] = (int)(base + off) + 32 * u;
+  if (!first) {
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) val[u] = __ldg(&vals[val[u] < n ? val[u] : n - 1]);
+  }
+  const int digit = block_before(totals[tid], s.wsum) + counts[(size_t)tid * tiles + blockIdx.x];
+  s.to[tid] = digit - place_tile(s, key, live, kPerThread, shift, place);
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u)
-    key[u] = base + 32 * u < n ? load_key(keys, base + 32 * u, T, first, nullptr) : 0xffffffffu;
-#pragma unroll
-  for (int u = 0; u < kPerThread; ++u) {
-    const bool live = base + 32 * u < n;
-    const uint32_t dg = (key[u] >> shift) & 255u;
-    const unsigned same = __match_any_sync(0xffffffffu, live ? dg : 256u);
-    const int below = __popc(same & ((1u << lane) - 1u));
-    int before = 0;
-    if (live) before = seen[wid][dg];
-    __syncwarp();
-    if (live && below == 0) seen[wid][dg] = before + __popc(same);
-    __syncwarp();
-    rank[u] = before + below;
-  }
-  __syncthreads();
-  {  // thread = digit: where the digit starts in the output, then in each warp's part of this tile
-    const int tot = totals[tid];
-    int x = tot;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
+    if (32 * u < live) {
+      s.key[place[u]] = key[u];
+      s.val[place[u]] = val[u];
     }
-    if (lane == 31) wsum[wid] = x;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = tid; i < here; i += kSortThreads) {
+    const uint32_t k = s.key[i];
+    const int to = s.to[(k >> shift) & 255u] + i;
+    keys_out[to] = (int32_t)k;
+    vals_out[to] = s.val[i];
+  }
+}
+
+// Up to one tile of keys: all passes in shared memory, and the offsets of few trajectory tokens by searches there
+// (off not nullptr).
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_small(const int32_t* __restrict__ keys, int32_t n, uint32_t T, int passes, int32_t* __restrict__ keys_out,
+                  int32_t* __restrict__ vals_out, int32_t* __restrict__ off, int32_t* status) {
+  __shared__ SortTile s;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int rounds = (n + kSortThreads - 1) / kSortThreads;
+  const int at = wid * 32 * rounds + lane, live = n - at;
+  uint32_t key[kPerThread];
+  int val[kPerThread], place[kPerThread];
+  load_keys<32>(keys, at, n, T, true, status, key);
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) val[u] = at + 32 * u;
+  for (int p = 0; p < passes; ++p) {
+    place_tile(s, key, live, rounds, 8 * p, place);
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u)
+      if (u < rounds && 32 * u < live) {
+        s.key[place[u]] = key[u];
+        s.val[place[u]] = val[u];
+      }
     __syncthreads();
-    int at = x - tot + counts[(size_t)tid * tiles + blockIdx.x];
-    for (int i = 0; i < wid; ++i) at += wsum[i];
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const int c = seen[w][tid];
-      seen[w][tid] = at;
-      at += c;
-    }
+    for (int u = 0; u < kPerThread; ++u)
+      if (u < rounds && 32 * u < live) {
+        key[u] = s.key[at + 32 * u];
+        val[u] = s.val[at + 32 * u];
+      }
+    __syncthreads();
   }
-  __syncthreads();
-#pragma unroll
-  for (int u = 0; u < kPerThread; ++u) {
-    const int64_t i = base + 32 * u;
-    if (i >= n) continue;
-    const int to = seen[wid][(key[u] >> shift) & 255u] + rank[u];
-    keys_out[to] = (int32_t)key[u];
-    vals_out[to] = first ? (int32_t)i : vals[i];
+  for (int i = tid; i < n; i += kSortThreads) {
+    keys_out[i] = (int32_t)s.key[i];
+    vals_out[i] = s.val[i];
+  }
+  if (off == nullptr) return;
+  for (uint32_t t = tid; t <= T; t += kSortThreads) {
+    int a = 0, b = n;
+    while (a < b) {
+      const int mid = (a + b) >> 1;
+      if (s.key[mid] < t) a = mid + 1;
+      else b = mid;
+    }
+    off[t] = a;
   }
 }
 
@@ -303,15 +431,20 @@ __global__ void __launch_bounds__(256) inverse_offsets(const int32_t* __restrict
   const int64_t t0 = (int64_t)blockIdx.x * kOffTile;
 #pragma unroll
   for (int u = 0; u < kOffTile / 256; ++u) c[u * 256 + tid] = 0;
-  if (tid < 2) {
-    const int64_t t = t0 + tid * (int64_t)kOffTile;
-    int a = 0, b = n;
-    while (a < b) {
-      const int mid = a + ((b - a) >> 1);
-      if (keys[mid] < t) a = mid + 1;
-      else b = mid;
+  if (wid < 2) {  // a warp a search: the keys from `a` on, 32 probes at a time
+    const int64_t t = t0 + wid * (int64_t)kOffTile;
+    int a = 0, len = n;
+    while (len > 0) {
+      const int step = (len + 31) / 32;
+      const int at = a + lane * step;
+      const bool less = lane * step < len && __ldg(&keys[at]) < t;
+      const int c = __popc(__ballot_sync(0xffffffffu, less));  // the probes of smaller keys come first
+      if (c == 0) break;
+      const int from = (c - 1) * step + 1;  // past the last smaller one
+      len = min(step - 1, len - from);
+      a += from;
     }
-    bound[tid] = a;
+    if (lane == 0) bound[wid] = a;
   }
   __syncthreads();
   const int lo = bound[0], hi = bound[1];
@@ -386,11 +519,6 @@ __device__ __forceinline__ int pack2(uint64_t f) {
   float a, b;
   dev::f2unpack(f, a, b);
   return (int)dev::pack_bf16(a, b);
-}
-
-// i / c by the magic 2^32 / c + 1, exactly for i < 2^32 / c; c = 1 has none
-__device__ __forceinline__ int div_by(int i, int c, uint32_t magic) {
-  return c == 1 ? i : (int)__umulhi((uint32_t)i, magic);
 }
 
 // A warp takes `per` consecutive output tokens, one where a row is some 8 KB or more.  Lane l computes the
@@ -713,7 +841,14 @@ cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens,
   const int passes = key_passes(traj_tokens);
   const int32_t* kin = tok_gather;
   const int32_t* vin = nullptr;
-  for (int p = 0; p < passes; ++p) {
+  if (tiles == 1) {
+    const bool all = traj_tokens <= kSmallOffsets;
+    inverse_small<<<1, kSortThreads, 0, st>>>(tok_gather, (int32_t)num_tokens, (uint32_t)traj_tokens, passes, keys[0],
+                                              inv_tok, all ? inv_off : nullptr, status);
+    if (all) return cudaGetLastError();
+    kin = keys[0];
+  }
+  for (int p = 0; p < passes && tiles > 1; ++p) {
     // the last pass writes inv_tok, the others alternate so that none writes what it reads
     int32_t* vout = (passes - 1 - p) % 2 == 0 ? inv_tok : spare;
     inverse_count<<<tiles, kSortThreads, 0, st>>>(kin, num_tokens, (uint32_t)traj_tokens, 8 * p, counts, tiles, p == 0,
@@ -758,11 +893,14 @@ cudaError_t launch_gather_rope(const void* q_in, const void* k_in, const void* v
   a.status = status;
   const int pairs = rope.rot_dim / 2;
   for (int i = 0; i < kMaxPairs; ++i) {
-    const double turns = i < pairs ? rope.inv_freq[i] * 0.15915494309189533577 : 0.0;
+    a.turn[i] = 0;
+    a.axis[i] = 0;
+    if (i >= pairs) continue;
+    const double turns = rope.inv_freq[i] * 0.15915494309189533577;
     double f = turns - std::floor(turns);
     if (!(f < 1.0)) f = 0.0;  // a tiny negative's fraction rounds to 1
-    a.turn[i] = (uint64_t)std::ldexp(f, 64);
-    a.axis[i] = (uint8_t)(i < pairs ? rope.pair_axis[i] : 0);
+    a.turn[i] = (uint64_t)(f * 18446744073709551616.0);
+    a.axis[i] = (uint8_t)rope.pair_axis[i];
   }
   if (backward)
     return rope.interleaved ? launch_rope<true, true>(a, pairs, st) : launch_rope<false, true>(a, pairs, st);

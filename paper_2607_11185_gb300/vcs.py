@@ -488,17 +488,22 @@ def attn_bwd(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, softmax_scale: 
 def _expect(where: str, **tensors):
     """Refuses tensors the kernels would misread: name=(tensor, dtype, shape), None in a shape matching any size.
     They lie on the current device, contiguous."""
-    dev = None
+    dev = -1
     for name, (t, dtype, shape) in tensors.items():
-        if not t.is_cuda:
+        on, size = t.get_device(), t.shape
+        if dev < 0 <= on:
+            dev = torch.cuda.current_device()
+        if on < 0:
             raise ValueError(f"{where}: {name} is on {t.device}, not a CUDA device")
-        dev = torch.cuda.current_device() if dev is None else dev
-        if t.device.index != dev:
+        if on != dev:
             raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{dev}")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
-        if t.dim() != len(shape) or any(b is not None and a != b for a, b in zip(t.shape, shape)):
-            raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+        if len(size) != len(shape):
+            raise ValueError(f"{where}: {name} has shape {tuple(size)}, not {shape}")
+        for have, want in zip(size, shape):
+            if have != want and want is not None:
+                raise ValueError(f"{where}: {name} has shape {tuple(size)}, not {shape}")
         if not t.is_contiguous():
             raise ValueError(f"{where}: {name} is not contiguous")
 
