@@ -365,7 +365,8 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
  *               its step nor its response, or a grid that does not hold the
  *               screenshot (its tokens are counted like text)
  * Returns VCS_ERR_INVALID_ARG for negative counts or null pointers,
- * VCS_ERR_OVERFLOW for counts above INT32_MAX.
+ * VCS_ERR_OVERFLOW for counts above INT32_MAX - 4096 (as the other calls of
+ * this section).
  *
  * vcs_rope: how a row is rotated.  Pair i < rot_dim / 2 of a head is turned by
  * the angle inv_freq[i] * (position on axis pair_axis[i]); it consists of the
@@ -384,7 +385,8 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
  *               equals num_tokens)
  *   pos         int32 [rope->num_axes, num_tokens] device; any int32
  *   rope        host pointer, read during the call
- *   q, k, v     must not overlap the inputs
+ *   q, k, v     must not overlap the inputs (VCS_ERR_INVALID_ARG); likewise
+ *               the backward's outputs
  * The angle is exact to 2^-32 of a turn for every position; products and sums
  * are fp32, rounded once to bf16.  The v rows are copied bit for bit.
  *
@@ -411,8 +413,7 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
  * Both return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
  * bytes) pointers, a rope that vcs_rope_init would refuse, a pair_axis outside
  * [0, num_axes) or an inv_freq that is not finite; VCS_ERR_UNSUPPORTED for a
- * d that is not a multiple of 8 from rot_dim to 256 or more than 65,535 heads;
- * VCS_ERR_OVERFLOW for counts above INT32_MAX.
+ * d that is not a multiple of 8 from rot_dim to 256 or more than 65,535 heads.
  * ------------------------------------------------------------------------ */
 #define VCS_ROPE_MAX_PAIRS 128
 #define VCS_ROPE_MAX_AXES 4

@@ -293,13 +293,15 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
 }
 
 // ---------------------------------------------------------------- rotary positions
+constexpr int64_t kRopeMaxCount = INT32_MAX - 4096;  // the kernels' 32-bit indexes run up to a tile past the end
+
 vcs_status vcs_stream_positions(const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens,
                                 const int32_t* tok_src_step, const int32_t* step_img, const int32_t* step_txt,
                                 const int32_t* step_grid, int64_t num_steps, int32_t* pos, int32_t* dev_status,
                                 void* stream) {
   vcs::ApiRange nvtx_range("vcs_stream_positions");
   if (num_segments < 0 || num_tokens < 0 || num_steps < 0) return VCS_ERR_INVALID_ARG;
-  if (num_tokens > INT32_MAX || num_steps > INT32_MAX) return VCS_ERR_OVERFLOW;
+  if (num_tokens > kRopeMaxCount || num_steps > kRopeMaxCount) return VCS_ERR_OVERFLOW;
   if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
   if (num_tokens > 0 && (num_segments == 0 || num_steps == 0 || tok_src_step == nullptr || step_img == nullptr ||
                          step_txt == nullptr || step_grid == nullptr || pos == nullptr))
@@ -341,7 +343,7 @@ static vcs_status check_rope(const void* const (&in)[3], void* const (&out)[3], 
                              int64_t num_tokens, const int32_t* pos, int32_t hq, int32_t hkv, int32_t d,
                              const vcs_rope* rope) {
   if (rows_in < 0 || rows_out < 0 || hq <= 0 || hkv <= 0 || d <= 0 || rope == nullptr) return VCS_ERR_INVALID_ARG;
-  if (rows_in > INT32_MAX || rows_out > INT32_MAX) return VCS_ERR_OVERFLOW;
+  if (rows_in > kRopeMaxCount || rows_out > kRopeMaxCount) return VCS_ERR_OVERFLOW;
   if (!rot_dim_ok(rope->rot_dim) || rope->num_axes < 1 || rope->num_axes > VCS_ROPE_MAX_AXES)
     return VCS_ERR_INVALID_ARG;
   for (int32_t i = 0; i < rope->rot_dim / 2; ++i)
@@ -352,6 +354,13 @@ static vcs_status check_rope(const void* const (&in)[3], void* const (&out)[3], 
     if ((rows_in > 0 && in[i] == nullptr) || (rows_out > 0 && out[i] == nullptr)) return VCS_ERR_INVALID_ARG;
     if (!aligned16(in[i]) || !aligned16(out[i])) return VCS_ERR_INVALID_ARG;
   }
+  for (int i = 0; i < 3; ++i)    // no output overlaps an input
+    for (int j = 0; j < 3; ++j) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(in[i]), b = reinterpret_cast<uintptr_t>(out[j]);
+      const uintptr_t na = (uintptr_t)rows_in * (i == 0 ? hq : hkv) * d * 2;
+      const uintptr_t nb = (uintptr_t)rows_out * (j == 0 ? hq : hkv) * d * 2;
+      if (a < b + nb && b < a + na) return VCS_ERR_INVALID_ARG;
+    }
   if (num_tokens > 0 && pos == nullptr) return VCS_ERR_INVALID_ARG;
   return VCS_OK;
 }
@@ -380,7 +389,7 @@ vcs_status vcs_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int
                               int32_t* inv_tok, int32_t* dev_status, void* ws, size_t ws_bytes, void* stream) {
   vcs::ApiRange nvtx_range("vcs_gather_inverse");
   if (num_tokens < 0 || traj_tokens < 0 || inv_off == nullptr) return VCS_ERR_INVALID_ARG;
-  if (num_tokens > INT32_MAX || traj_tokens > INT32_MAX - 1) return VCS_ERR_OVERFLOW;
+  if (num_tokens > kRopeMaxCount || traj_tokens > kRopeMaxCount) return VCS_ERR_OVERFLOW;
   if (num_tokens > 0 && (tok_gather == nullptr || inv_tok == nullptr)) return VCS_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < gather_inverse_ws_bytes(num_tokens) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
     return VCS_ERR_WORKSPACE;

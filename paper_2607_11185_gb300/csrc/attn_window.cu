@@ -798,8 +798,10 @@ cudaError_t launch_window_d(const AttnArgs& a, void* o, float* lse, void* ws, cu
                                                   a.hkv, G, (int32_t)max_items, off, items, a.status);
   }
   const unsigned grid = (unsigned)(max_items < 152 ? max_items : 152);
+  const int32_t longest = a.max_seqlen > 1 ? a.max_seqlen : 1;  // as far as either reaches; the kernel's sums stay in range
+  const int32_t window = a.window < longest ? a.window : longest, sinks = a.sinks < longest ? a.sinks : longest;
   attn_window_kernel<D><<<grid, kThreads, C::SMEM, st>>>(
-      tq, tk, tv, items, total, (int32_t)a.num_tokens, a.hq, a.hkv, a.window, a.sinks, a.scale * 1.4426950408889634f,
+      tq, tk, tv, items, total, (int32_t)a.num_tokens, a.hq, a.hkv, window, sinks, a.scale * 1.4426950408889634f,
       static_cast<__nv_bfloat16*>(o), lse, a.status);
   return cudaGetLastError();
 }

@@ -57,6 +57,8 @@ __global__ void __launch_bounds__(kPosThreads)
   __shared__ int32_t carry_s;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const size_t N = (size_t)num_tokens;
+  const bool vec =
+      num_tokens % 4 == 0 && ((reinterpret_cast<uintptr_t>(src_step) | reinterpret_cast<uintptr_t>(pos)) & 15u) == 0;
   for (int seg = blockIdx.x; seg < num_segments; seg += gridDim.x) {
     const int start = cu_seqlens[seg], end = cu_seqlens[seg + 1];
     if (start < 0 || end < start || end > num_tokens || (seg == 0 && start != 0) ||
@@ -140,36 +142,63 @@ __global__ void __launch_bounds__(kPosThreads)
         __syncthreads();
         carry = carry_s;
         const int n0 = max(lo_tok, run_at[0]), n1 = min(hi_tok, run_at[kPosThreads]);
-        for (int m = n0 + tid; m < n1; m += 4 * kPosThreads) {
-          int step[4];
+        const int step0 = (int)s0;
+        // token k of run r: a screenshot's by its grid, or text
+        auto place = [&](int r, int k, int& frame, int& line, int& col) {
+          const int h = run_h[r], w = run_w[r];
+          const uint32_t hm = run_hm[r], wm = run_wm[r];
+          line = wm != 0u ? div_by(k, w, wm) : k / w;
+          col = k - line * w;
+          frame = hm != 0u ? div_by(line, h, hm) : line / h;
+          line -= frame * h;
+        };
+        for (int m = (n0 & ~3) + 4 * tid; m < n1; m += 4 * kPosThreads) {
+          // four tokens of one run, of its screenshot or of its text, in 16-byte accesses and with one division
+          if (vec && m >= n0 && m + 4 <= n1) {
+            const int4 step = __ldg(reinterpret_cast<const int4*>(src_step + m));
+            const int r = step.x - step0;
+            if (step.y == step.x && step.z == step.x && step.w == step.x && r >= 0 && r < kPosThreads &&
+                m >= run_at[r] && m + 3 < run_at[r + 1]) {
+              const int k = m - run_at[r], im = run_img[r], p = run_pos[r];
+              if (k >= im) {
+                const int t = p + run_skip[r] + k - im;
+                const int4 x = make_int4(t, t + 1, t + 2, t + 3);
+                *reinterpret_cast<int4*>(pos + m) = *reinterpret_cast<int4*>(pos + N + m) =
+                    *reinterpret_cast<int4*>(pos + 2 * N + m) = x;
+                continue;
+              }
+              if (k + 3 < im) {
+                int f[4], l[4], c[4];
+                place(r, k, f[0], l[0], c[0]);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) step[v] = __ldg(&src_step[min(m + v * kPosThreads, n1 - 1)]);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int n = m + v * kPosThreads;
-            if (n >= n1) break;
-            const int64_t r = (int64_t)step[v] - s0;
-            if (r < 0 || r >= kPosThreads || s0 + r > last || n < run_at[r] || n >= run_at[r + 1]) {
+                for (int v = 1; v < 4; ++v) {
+                  const bool wrap = c[v - 1] + 1 == run_w[r], next = wrap && l[v - 1] + 1 == run_h[r];
+                  c[v] = wrap ? 0 : c[v - 1] + 1;
+                  l[v] = next ? 0 : l[v - 1] + wrap;
+                  f[v] = f[v - 1] + next;
+                }
+                *reinterpret_cast<int4*>(pos + m) = make_int4(p + f[0], p + f[1], p + f[2], p + f[3]);
+                *reinterpret_cast<int4*>(pos + N + m) = make_int4(p + l[0], p + l[1], p + l[2], p + l[3]);
+                *reinterpret_cast<int4*>(pos + 2 * N + m) = make_int4(p + c[0], p + c[1], p + c[2], p + c[3]);
+                continue;
+              }
+            }
+          }
+          for (int n = max(m, n0); n < min(m + 4, n1); ++n) {
+            const int r = __ldg(&src_step[n]) - step0;
+            if (r < 0 || r >= kPosThreads || n < run_at[r] || n >= run_at[r + 1]) {
               set_status(status, VCS_ERR_DEVICE_CHECK);  // tok_src_step decreases within the segment
               continue;
             }
-            const int k = n - run_at[r], im = run_img[r];
-            int p0 = run_pos[r], p1, p2;
-            if (k < im) {
-              const int h = run_h[r], w = run_w[r];
-              const uint32_t hm = run_hm[r], wm = run_wm[r];
-              const int line = wm != 0u ? div_by(k, w, wm) : k / w;
-              const int frame = hm != 0u ? div_by(line, h, hm) : line / h;
-              p1 = p0 + line - frame * h;
-              p2 = p0 + k - line * w;
-              p0 += frame;
-            } else {
-              p0 += run_skip[r] + k - im;
-              p1 = p2 = p0;
-            }
-            pos[n] = p0;
-            pos[N + n] = p1;
-            pos[2 * N + n] = p2;
+            const int k = n - run_at[r], im = run_img[r], p = run_pos[r];
+            int f, l, c;
+            if (k < im)
+              place(r, k, f, l, c);
+            else
+              f = l = c = run_skip[r] + k - im;
+            pos[n] = p + f;
+            pos[N + n] = p + l;
+            pos[2 * N + n] = p + c;
           }
         }
         const int tile_end = run_at[kPosThreads];

@@ -113,6 +113,9 @@ EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "
 
 LIB_PATH = _LIB_PATH
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 
 class VcsError(RuntimeError):
     def __init__(self, status: int, where: str):
@@ -131,8 +134,8 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # the handle alone: a stream object takes 3 us to make
+        return _raw_stream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -611,7 +614,9 @@ def gather_rope(q_traj, k_traj, v_traj, tok_gather, pos, rope: VcsRope, stream=N
     _expect("gather_rope", q_traj=(q_traj, bf16, (None, None, None)))
     tt, hq, d = q_traj.shape
     _expect("gather_rope", k_traj=(k_traj, bf16, (tt, None, d)), v_traj=(v_traj, bf16, tuple(k_traj.shape)),
-            pos=(pos, i32, (rope.num_axes, nt)), **({} if tok_gather is None else dict(tok_gather=(tok_gather, i32, (nt,)))))
+            pos=(pos, i32, (rope.num_axes, nt)))
+    if tok_gather is not None:
+        _expect("gather_rope", tok_gather=(tok_gather, i32, (None,)))
     hkv = k_traj.shape[1]
     q = torch.empty((nt, hq, d), dtype=q_traj.dtype, device=q_traj.device)
     k = torch.empty((nt, hkv, d), dtype=k_traj.dtype, device=q_traj.device)
@@ -647,6 +652,8 @@ def gather_rope_bwd(dq, dk, dv, pos, inv_off, inv_tok, rope: VcsRope, stream=Non
     nt, hq, d = dq.shape
     _expect("gather_rope_bwd", dk=(dk, bf16, (nt, None, d)), dv=(dv, bf16, tuple(dk.shape)),
             pos=(pos, i32, (rope.num_axes, nt)))
+    if (inv_off is None) != (inv_tok is None):
+        raise ValueError("gather_rope_bwd: inv_off and inv_tok go together")
     if inv_off is not None:
         _expect("gather_rope_bwd", inv_off=(inv_off, i32, (None,)), inv_tok=(inv_tok, i32, (nt,)))
     hkv = dk.shape[1]

@@ -310,3 +310,30 @@ def test_on_a_stream_and_in_a_graph():
     want = vcs.gather_rope(q, k, v, gat, pos, rope)
     wantb = vcs.gather_rope_bwd(*want, pos, *vcs.gather_inverse(gat, t), rope)
     assert all(torch.equal(a, b) for a, b in zip((*got, *gotb), (*want, *wantb)))
+
+
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_positions_at_any_alignment(shift):
+    # token counts that are and are not multiples of four, buffers off the 16-byte alignment, grids of one row or
+    # column and many frames, runs that begin and end inside four tokens
+    vcs = _vcs()
+    rng = np.random.default_rng(shift)
+    grid = np.array([[1, 1, 37], [5, 1, 1], [3, 2, 1], [2, 7, 3], [1, 9, 9], [7, 1, 2], [1, 1, 1]], np.int32)
+    grid = grid[rng.integers(0, 7, size=40)]
+    img, txt = grid.prod(1).astype(np.int32), rng.integers(0, 7, size=40).astype(np.int32)
+    for extra in range(4):
+        txt[39] = 5
+        lay = oseg.build(np.array([0, 13, 40], np.int32), img, txt, 4, 1)
+        txt[39] += (extra - len(lay["tok_src_step"])) % 4
+        lay = oseg.build(np.array([0, 13, 40], np.int32), img, txt, 4, 1)
+        n = len(lay["tok_src_step"])
+        src = torch.zeros(n + 4, dtype=torch.int32, device="cuda")[shift:shift + n]
+        src.copy_(torch.from_numpy(lay["tok_src_step"]))
+        pos = torch.full((3 * n + 8,), -1, dtype=torch.int32, device="cuda")
+        cu, i, t, g = dev(lay["cu_seqlens"], img, txt, grid)
+        word = torch.zeros(1, dtype=torch.int32, device="cuda")
+        assert vcs.vcs_stream_positions(cu, cu.numel() - 1, n, src, i, t, g, 40, pos[shift:], word) == 0
+        want = orope.positions(lay["cu_seqlens"], lay["tok_src_step"], img, txt, grid)
+        assert n % 4 == extra and int(word) == 0
+        assert np.array_equal(pos[shift:shift + 3 * n].view(3, n).cpu().numpy(), want)
+        assert (pos[:shift] == -1).all() and (pos[shift + 3 * n:] == -1).all()

@@ -7,7 +7,7 @@ import torch
 
 from oracle import rope as orope
 
-A = 256  # an aligned address that no refused call reads
+A, B = 256, 1 << 40  # aligned addresses, of inputs and outputs, that no refused call reads
 
 
 @pytest.fixture(scope="module")
@@ -56,10 +56,10 @@ def test_rope_refusals(vcs):
                 setattr(r, k, v)
         return r
 
-    def fwd(q=A, k=A, v=A, tt=10, gat=A, pos=A, nt=12, hq=2, hkv=1, d=64, rope=good, oq=A, ok=A, ov=A):
+    def fwd(q=A, k=A, v=A, tt=10, gat=A, pos=A, nt=12, hq=2, hkv=1, d=64, rope=good, oq=B, ok=2 * B, ov=3 * B):
         return vcs.vcs_gather_rope(q, k, v, tt, gat, pos, nt, hq, hkv, d, rope, oq, ok, ov, None, 0)
 
-    def bwd(q=A, k=A, v=A, nt=12, pos=A, off=A, tok=A, tt=10, hq=2, hkv=1, d=64, rope=good, oq=A, ok=A, ov=A):
+    def bwd(q=A, k=A, v=A, nt=12, pos=A, off=A, tok=A, tt=10, hq=2, hkv=1, d=64, rope=good, oq=B, ok=2 * B, ov=3 * B):
         return vcs.vcs_gather_rope_bwd(q, k, v, nt, pos, off, tok, tt, hq, hkv, d, rope, oq, ok, ov, None, 0)
 
     ropes = [bad(rot_dim=24), bad(rot_dim=0), bad(rot_dim=512), bad(num_axes=0), bad(num_axes=5),
@@ -68,11 +68,15 @@ def test_rope_refusals(vcs):
     for f in (fwd, bwd):
         for kw in [dict(q=None), dict(k=None), dict(v=None), dict(pos=None), dict(oq=None), dict(ok=None),
                    dict(ov=None), dict(nt=-1), dict(tt=-1), dict(hq=0), dict(hkv=0), dict(d=0), dict(rope=None),
-                   dict(q=A + 8), dict(ov=A + 2), *(dict(rope=r) for r in ropes)]:
+                   dict(q=A + 8), dict(ov=B + 2), *(dict(rope=r) for r in ropes)]:
             assert f(**kw) == 1, kw
         for kw in (dict(d=60), dict(d=48), dict(d=264), dict(hq=65536), dict(hkv=65536)):
             assert f(**kw) == 2, kw
         assert f(nt=1 << 31) == 4 and f(tt=1 << 31) == 4
+    for f, rows, out in ((fwd, 10, 12), (bwd, 12, 10)):     # outputs that reach into an input, by a row or whole
+        for kw in (dict(oq=A), dict(ok=A), dict(ov=A), dict(q=B - 256, oq=B), dict(v=B + (out - 1) * 256, oq=B),
+                   dict(q=2 * B - rows * 256 + 128), dict(k=3 * B + out * 128 - 16)):
+            assert f(**kw) == 1, kw
     assert fwd(gat=None) == 1                       # no map: as many rows as tokens
     assert bwd(off=None) == 1 and bwd(tok=None) == 1 and bwd(off=None, tok=None) == 1
 
@@ -84,7 +88,7 @@ def test_inverse_refusals(vcs):
         return vcs.vcs_gather_inverse(gat, nt, tt, off, tok, None, ws, n, 0)
     for kw in (dict(gat=None), dict(nt=-1), dict(tt=-1), dict(off=None), dict(tok=None)):
         assert f(**kw) == 1, kw
-    assert f(tt=(1 << 31) - 1) == 4 and f(nt=1 << 31) == 4
+    assert f(tt=(1 << 31) - 1) == 4 and f(nt=1 << 31) == 4 and f(nt=(1 << 31) - 4096) == 4
     assert f(ws=None) == 8 and f(n=nb - 1) == 8 and f(ws=A + 16) == 8
     assert vcs.vcs_gather_inverse_workspace_size(-1) == vcs.vcs_gather_inverse_workspace_size(0)
 
