@@ -21,14 +21,15 @@
 //
 // Warp roles (512 threads):
 //   warp 0      TMA producer: Q0/Q1 of a unit, K and V tiles into a ring (K runs one tile ahead of V)
-//   warp 1      TMEM allocator and tcgen05.mma issuer; at d = 64 of S only
-//   warp 2      d = 64: issuer of P V
+//   warp 1      TMEM allocator and tcgen05.mma issuer of tile 0; at d = 64 of both tiles' S
+//   warp 2      issuer of tile 1; at d = 64 of both tiles' P V
 //   warps 4-7   softmax of tile 0 (thread = query row);  warps 8-11 of tile 1
 //   warps 12-15 O of both tiles, out of TMEM, scaled, through shared memory, by a bulk copy a row
 // TMEM (512 columns): S0, S1 (128 each), O0 and O1 from 256 and 384 on.  d = 128: P_k goes over the first
 // 64 columns of S_k; d = 64: it has 64 columns of its own behind O_k.  P is read straight from TMEM.
-// The order of the MMAs on the pipe, and what each barrier then says, is as in the causal kernel:
-// d = 128, step j: for each tile O_k += P_k(j) V_j, then S_k(j+1); d = 64: S_k(j+1) as soon as S_k(j)
+// d = 128, step j of a tile: O_k += P_k(j) V_j, then S_k(j+1), which overwrites P_k(j): the MMAs of one issuer
+// execute in order, as the causal kernel relies on too, so S_k(j+1) complete also says that P_k(j) has been
+// consumed, O_k is up to date and V_j no longer read by the tile.  d = 64: S_k(j+1) as soon as S_k(j)
 // has been read, by one warp, and P V by another.
 #include <cfloat>
 #include <cstdint>
@@ -69,8 +70,8 @@ struct Win {
   static constexpr int TM_P0 = OWN_P ? TM_O0 + 64 : TM_S0, TM_P1 = OWN_P ? TM_O1 + 64 : TM_S1;
   static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);   // Q (K-major) x K^T (K-major)
   static constexpr uint32_t IDESC_PV = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
-  // the issuer of both products wants more than one of each; with 64 registers it spills and a step takes 10% longer
-  static constexpr int REG_CTRL = OWN_P ? 80 : 96, REG_OUT = 48, REG_SOFTMAX = OWN_P ? 192 : 184;
+  // with 64 for the issuers a d = 128 step took 10% longer while one warp issued for both tiles
+  static constexpr int REG_CTRL = 80, REG_OUT = 48, REG_SOFTMAX = 192;
   static_assert(REG_CTRL + REG_OUT + 2 * REG_SOFTMAX <= 4 * kRegLaunch,
                 "setmaxnreg targets exceed the launch registers");
 };
@@ -259,6 +260,8 @@ struct Unit {
   }
   __device__ __forceinline__ int kt(int j) const { return j < ns ? j : j - ns + lo; }
   __device__ __forceinline__ bool active(int t, int j) const { return t == 0 ? j < n0 : has1 && j != skip; }
+  __device__ __forceinline__ int end(int t) const { return t == 0 ? n0 : nkv; }       // behind the tile's last step
+  __device__ __forceinline__ int after(int t, int j) const { return t == 1 && j + 1 == skip ? j + 2 : j + 1; }
   // ring items of the unit in load order: K0, K1, V0, K2, V1, ..., K_{n-1}, V_{n-2}, V_{n-1}
   __device__ __forceinline__ int k_item(int j) const { return j == 0 ? 0 : 2 * j - 1; }
   __device__ __forceinline__ int v_item(int j) const { return j == nkv - 1 ? 2 * nkv - 1 : 2 * j + 2; }
@@ -294,10 +297,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (threadIdx.x == 0) {
     mbar_init(&bars->q_full, 1);
-    mbar_init(&bars->q_free, 1);
+    mbar_init(&bars->q_free, C::OWN_P ? 1 : 2);
     for (int i = 0; i < C::NSLOT; ++i) {
       mbar_init(&bars->kv_full[i], 1);
-      mbar_init(&bars->kv_empty[i], 1);
+      mbar_init(&bars->kv_empty[i], 2);  // one for each tile
     }
     for (int i = 0; i < C::NGRP; ++i) mbar_init(&bars->grp_full[i], 1);
     for (int i = 0; i < 2; ++i) {
@@ -439,15 +442,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         ++un;
       }
       if (!ok) on_timeout(bars, status);
-    } else if (!C::OWN_P && warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
+    } else if (!C::OWN_P && (warp == 1 || warp == 2)) {
+    // ---------------------------------------------------- MMA issuers (tile 0; tile 1)
     // The whole warp runs the loop and one elected lane issues, so that descriptors and addresses stay in
     // uniform registers.  As above, no lane's answer decides where the warp goes; here a vote a step does.
+    // A warp a tile: a barrier wait takes its thread 200 to 300 cycles while the pipe streams from shared
+    // memory, and there are two or three a step, which the other tile's MMAs now cover.
+      const int t = warp - 1;
       bool ok = true;
-      const uint64_t q0d = smem_desc(sbase + C::OFF_Q0, 16, 1024), q1d = desc_at(q0d, C::TILE);
+      const uint64_t qd = desc_at(smem_desc(sbase + C::OFF_Q0, 16, 1024), t * C::TILE);
       const uint64_t kv_kmaj = smem_desc(sbase + C::OFF_KV, 16, 1024);
       const uint64_t kv_mnmaj = smem_desc(sbase + C::OFF_KV, C::BLOCK, 1024);
-      uint32_t ib = 0, gb = 0, un = 0, p0 = 0, p1 = 0, un1 = 0;  // un1: units with a tile 1
+      const uint32_t tm_s = tmem + (t ? C::TM_S1 : C::TM_S0), tm_o = tmem + (t ? C::TM_O1 : C::TM_O0);
+      uint32_t ib = 0, gb = 0, un = 0, steps = 0, outs = 0;  // outs: units that have this tile
       auto acquire_group = [&](uint32_t g) {
         ok &= mbar_wait(&bars->grp_full[g % C::NGRP], (g / C::NGRP) & 1);
         tc_fence_after();
@@ -458,69 +465,49 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (i + (int)gridDim.x < total) e = items[i + gridDim.x];
         auto slot_off = [&](int item) { return (uint32_t)(((ib + item) % C::NSLOT) * C::TILE); };
         ok &= mbar_wait(&bars->q_full, un & 1);
-        acquire_group(gb);
-        if (!__all_sync(0xffffffffu, ok)) break;
-        uint32_t kaddr = slot_off(0);
-        // S of the first step overwrites the P that the last P V of the unit before, issued before, reads
-        if (elect_one() && ok) {
-          issue_s<D>(tmem + C::TM_S0, q0d, desc_at(kv_kmaj, kaddr));
-          tc_commit(&bars->s_full[0]);
-          if (u.active(1, 0)) {
-            issue_s<D>(tmem + C::TM_S1, q1d, desc_at(kv_kmaj, kaddr));
-            tc_commit(&bars->s_full[1]);
-          }
-          if (u.nkv == 1) tc_commit(&bars->q_free);
-        }
-        __syncwarp();
-        for (int j = 0; j < u.nkv; ++j) {
-          const bool next = j + 1 < u.nkv;
-          acquire_group(gb + j + 1);
+        const int first = t == 1 && u.skip == 0 ? 1 : 0, end = u.end(t);
+        if (t == 0 || u.has1) {
+          acquire_group(gb + first);
           if (!__all_sync(0xffffffffu, ok)) break;
-          const uint32_t vaddr = slot_off(u.v_item(j));
-          if (next) kaddr = slot_off(u.k_item(j + 1));
-          if (j < u.n0) {  // tile 0: O0 += P0(j) V_j, then S0(j+1)
-            ok &= mbar_wait(&bars->p_full[0], p0++ & 1);
-            if (j == 0 && un > 0) ok &= mbar_wait(&bars->o_free[0], (un - 1) & 1);  // O of the unit before read
+          // S of the first step overwrites the P that the last P V of the unit before, issued before, reads
+          if (elect_one() && ok) {
+            issue_s<D>(tm_s, qd, desc_at(kv_kmaj, slot_off(u.k_item(first))));
+            tc_commit(&bars->s_full[t]);
+            if (u.after(t, first) >= end) tc_commit(&bars->q_free);
+          }
+          __syncwarp();
+          for (int j = first; j < end; j = u.after(t, j)) {
+            // O += P(j) V_j, then S of the tile's next step; K and V are in groups j + 1 and, of a step that was
+            // skipped to, next
+            const int next = u.after(t, j);
+            acquire_group(gb + j + 1);
+            if (next < end && next > j + 1) acquire_group(gb + next);
+            ok &= mbar_wait(&bars->p_full[t], steps++ & 1);
+            if (j == first && outs > 0) ok &= mbar_wait(&bars->o_free[t], (outs - 1) & 1);  // O of the unit before read
+            if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
+            const uint32_t vaddr = slot_off(u.v_item(j)), kaddr = next < end ? slot_off(u.k_item(next)) : 0u;
             if (elect_one() && ok) {
-              issue_pv<D>(tmem + C::TM_O0, tmem + C::TM_S0, desc_at(kv_mnmaj, vaddr), j > 0);
-              if (j + 1 < u.n0) {
-                issue_s<D>(tmem + C::TM_S0, q0d, desc_at(kv_kmaj, kaddr));
-                tc_commit(&bars->s_full[0]);
+              issue_pv<D>(tm_o, tm_s, desc_at(kv_mnmaj, vaddr), j > first);
+              if (next < end) {
+                issue_s<D>(tm_s, qd, desc_at(kv_kmaj, kaddr));
+                tc_commit(&bars->s_full[t]);
+                if (u.after(t, next) >= end) tc_commit(&bars->q_free);  // the unit's last S
               } else {
-                tc_commit(&bars->o_done[0]);
+                tc_commit(&bars->o_done[t]);
               }
             }
             __syncwarp();
           }
-          if (u.has1) {  // tile 1
-            const bool more = j > (u.skip == 0 ? 1 : 0);
-            if (j != u.skip) {
-              ok &= mbar_wait(&bars->p_full[1], p1++ & 1);
-              if (!more && un1 > 0) ok &= mbar_wait(&bars->o_free[1], (un1 - 1) & 1);
-              tc_fence_after();
-            }
-            if (elect_one() && ok) {
-              if (j != u.skip) issue_pv<D>(tmem + C::TM_O1, tmem + C::TM_S1, desc_at(kv_mnmaj, vaddr), more);
-              if (next && j + 1 != u.skip) {
-                issue_s<D>(tmem + C::TM_S1, q1d, desc_at(kv_kmaj, kaddr));
-                tc_commit(&bars->s_full[1]);
-              } else if (!next) {
-                tc_commit(&bars->o_done[1]);
-              }
-            }
-            __syncwarp();
-          }
-          if (j == u.nkv - 2) {  // the unit's last S is issued
-            if (elect_one() && ok) tc_commit(&bars->q_free);
-            __syncwarp();
-          }
+          ++outs;
+        } else {
+          if (elect_one() && ok) mbar_arrive(&bars->q_free);
+          __syncwarp();
         }
         if (!__all_sync(0xffffffffu, ok)) break;
         ib += 2 * u.nkv;
         gb += u.nkv + 1;
         ++un;
-        if (u.has1) ++un1;
       }
       if (!ok) on_timeout(bars, status);
     }
@@ -548,18 +535,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       const int mt = u.m[wg];
       float m_run = kHidden, l = 0.f;
-      // The ring slots are handed back from here rather than by commits of the MMA thread (a commit holds it
-      // about as long as an MMA): once S(j) of the unit's last tile is complete, so are the MMAs issued
-      // before it, which are all that read K_0 .. K_j and, without OWN_P, V_0 .. V_{j-1} (with it, that
-      // tile's o_done says so of V); one thread of that tile frees their slots.
-      const bool releaser = wg == (u.has1 ? 1 : 0) && quad == 0 && lane == 0;
-      int kr = 0, vr = 0;  // K and V tiles handed back
-      auto release_k = [&](int upto) {
-        for (; kr <= upto; ++kr) mbar_arrive(&bars->kv_empty[(ib + u.k_item(kr)) % C::NSLOT]);
+      // The ring slots are handed back from here rather than by commits of the MMA threads (a commit holds its thread
+      // about as long as an MMA): once S(j) of a tile is complete, so is what its issuer issued before, which with
+      // K_j is done, and without OWN_P with the V of the tile's step before (with it, o_done says so of V).  A slot
+      // is free when both tiles have given it back, each for the steps it takes, or twice if it takes one alone.
+      const bool releaser = quad == 0 && lane == 0;
+      auto release = [&](int item, int j) {
+        mbar_arrive(&bars->kv_empty[(ib + item) % C::NSLOT]);
+        if (!u.active(wg ^ 1, j)) mbar_arrive(&bars->kv_empty[(ib + item) % C::NSLOT]);
       };
-      auto release_v = [&](int upto) {
-        for (; vr <= upto; ++vr) mbar_arrive(&bars->kv_empty[(ib + u.v_item(vr)) % C::NSLOT]);
-      };
+      int prev = -1;  // the tile's step before
       bool first = true;
       for (int j = 0; j < u.nkv; ++j) {
         if (!u.active(wg, j)) continue;
@@ -568,8 +553,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!mbar_wait_warp(&bars->s_full[wg], steps & 1)) { ok = false; break; }
         ++steps;
         if (releaser) {
-          release_k(j);
-          if (!C::OWN_P) release_v(j - 1);
+          release(u.k_item(j), j);
+          if (!C::OWN_P && prev >= 0) release(u.v_item(prev), prev);
         }
         tc_fence_after();
         uint32_t s[128];
@@ -640,7 +625,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         l = l * alpha + ((a0 + a1) + (b0 + b1));
         if (C::OWN_P && steps > 1) {  // the P V before is complete: P's columns are free and O is up to date
           if (!mbar_wait_warp(&bars->o_done[wg], steps & 1)) { ok = false; break; }
-          if (releaser && !first) release_v(j - 1 - (u.skip >= 0 && j == u.skip + 1 ? 1 : 0));
+          if (releaser && prev >= 0) release(u.v_item(prev), prev);
           tc_fence_after();
         }
         tmem_st_32x32b_x32(trow + p_col, *reinterpret_cast<uint32_t(*)[32]>(&s[0]));
@@ -667,6 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         mbar_arrive(&bars->p_full[wg]);
         first = false;
+        prev = j;
       }
       // another role's giving up is looked for once a unit; the waits are bounded without it
       if (ok && __any_sync(0xffffffffu, aborted(bars))) ok = false;
@@ -706,12 +692,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         tc_fence_after();
-        // every MMA of the unit is complete: its last V may be overwritten (OWN_P: and the one before it, if
-        // tile 1 skipped that step and so could not say when it was done)
-        if (t == (u.has1 ? 1 : 0) && quad == 0 && lane == 0) {
-          if (C::OWN_P && u.skip >= 0 && u.skip == u.nkv - 2)
-            mbar_arrive(&bars->kv_empty[(ib + u.v_item(u.nkv - 2)) % C::NSLOT]);
-          mbar_arrive(&bars->kv_empty[(ib + u.v_item(u.nkv - 1)) % C::NSLOT]);
+        // the tile is done with its last V
+        if (quad == 0 && lane == 0) {
+          const int j = u.end(t) - 1;
+          mbar_arrive(&bars->kv_empty[(ib + u.v_item(j)) % C::NSLOT]);
+          if (!u.active(t ^ 1, j)) mbar_arrive(&bars->kv_empty[(ib + u.v_item(j)) % C::NSLOT]);
         }
         const float inv_l = reinterpret_cast<const float*>(smem + C::OFF_OUT + r * C::OUT_ROW + D * 2)[t];
         const uint64_t il2 = f2pack(inv_l, inv_l);
