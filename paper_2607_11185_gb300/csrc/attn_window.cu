@@ -13,11 +13,14 @@
 // Masked element-wise: the diagonal tile, the tiles the window's edge crosses, and the sinks' tiles
 // outside the window.
 //
-// A long window's unit is bound by the tensor pipe like the causal kernel's (attn_fwd.cu, whose inner
-// loops these are); a short window's, of two to four steps, by what precedes and follows its steps.  So
+// What bounds it is the chain of one tile, softmax, P V and next S, beside the other tile's: about 1.6 us a step
+// at 28/4/128 of 1.1 that the MMAs of both take, and 2.6 us a unit besides, for which a CTA of its own took longer
+// (512 segments of 256: 0.84 ms in the causal kernel, 0.46 here).  So
 // a CTA stays on its SM and takes every grid-th unit: barriers and TMEM are set up once, the ring of K/V
 // tiles runs on across units, the next unit's Q is loaded once the last S of this one is complete, and
 // warps of their own write its O while the softmax warps are at the next one's first tile.
+// 28/4/128, 32 segments of 4,096, window 128 / 1,024: 0.55 / 1.41 ms (0.78 / 1.66 with O written by the softmax
+// warps, masks compared column by column and one issuer).
 //
 // Warp roles (512 threads):
 //   warp 0      TMA producer: Q0/Q1 of a unit, K and V tiles into a ring (K runs one tile ahead of V)
@@ -148,10 +151,9 @@ __device__ __forceinline__ long long seg_units(const int32_t* __restrict__ cu_se
   return (long long)(tiles >> 1) * G + (tiles & 1) * ((G + 1) >> 1);  // of one kv head
 }
 
-// off[s] = units of segments 0 .. s-1 (clipped to the capacity), *total = their sum, or 0 where it passes the
-// capacity: only segments that overlap, which inconsistent bounds describe, list so many, and no CTA then
-// reads a unit that was not written.  The call's first kernel: it clears the status word.  items != nullptr:
-// it writes the units too, a warp a segment.
+// The units of segment s at items[base ..], by threads tid of n: kv head by kv head, blocks of two row tiles in order,
+// so that the units running together share their key tiles in L2.  A segment whose units would pass the capacity
+// writes none.
 __device__ __forceinline__ void write_units(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
                                             int32_t num_tokens, int32_t max_seqlen, int32_t hkv, int32_t G,
                                             int32_t capacity, long long base, int4* __restrict__ items,
@@ -173,6 +175,10 @@ __device__ __forceinline__ void write_units(const int32_t* __restrict__ cu_seqle
   }
 }
 
+// off[s] = units of segments 0 .. s-1 (clipped to the capacity), *total = their sum, or 0 where it passes the
+// capacity: only segments that overlap, which inconsistent bounds describe, list so many, and no CTA then
+// reads a unit that was not written.  The call's first kernel: it clears the status word.  items != nullptr:
+// it writes the units too, a warp a segment.
 __global__ void __launch_bounds__(1024) window_unit_scan(const int32_t* __restrict__ cu_seqlens, int32_t num_segments,
                                                          int32_t num_tokens, int32_t max_seqlen, int32_t hkv, int32_t G,
                                                          int32_t capacity, int32_t* off, int32_t* __restrict__ total,
