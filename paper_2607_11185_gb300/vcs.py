@@ -488,27 +488,27 @@ def attn_bwd(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, softmax_scale: 
     return dq, dk, dv
 
 
-def _expect(where: str, **tensors):
-    """Refuses tensors the kernels would misread: name=(tensor, dtype, shape), None in a shape matching any size.
-    They lie on the current device, contiguous."""
-    dev = -1
-    for name, (t, dtype, shape) in tensors.items():
-        on, size = t.get_device(), t.shape
-        if dev < 0 <= on:
-            dev = torch.cuda.current_device()
-        if on < 0:
-            raise ValueError(f"{where}: {name} is on {t.device}, not a CUDA device")
-        if on != dev:
-            raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{dev}")
-        if t.dtype is not dtype:
-            raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
-        if len(size) != len(shape):
-            raise ValueError(f"{where}: {name} has shape {tuple(size)}, not {shape}")
-        for have, want in zip(size, shape):
-            if have != want and want is not None:
-                raise ValueError(f"{where}: {name} has shape {tuple(size)}, not {shape}")
-        if not t.is_contiguous():
-            raise ValueError(f"{where}: {name} is not contiguous")
+def _expect(where: str, *tensors):
+    """Refuses tensors the kernels would misread: (name, tensor, dtype, shape), or a number of dims in the place of the
+    shape.  They lie on the current device, contiguous."""
+    dev = torch.cuda.current_device() if tensors[0][1].is_cuda else -1
+    for name, t, dtype, shape in tensors:
+        if not (t.get_device() == dev >= 0 and t.dtype is dtype and t.is_contiguous() and
+                (t.shape == shape or t.dim() == shape)):
+            _refuse(where, name, t, dtype, shape)
+
+
+def _refuse(where: str, name: str, t, dtype, shape):
+    if not t.is_cuda:
+        raise ValueError(f"{where}: {name} is on {t.device}, not a CUDA device")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{where}: {name} is {t.dtype}, not {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{where}: {name} is not contiguous")
+    want = f"{shape} dims" if isinstance(shape, int) else f"shape {tuple(shape)}"
+    raise ValueError(f"{where}: {name} has shape {tuple(t.shape)}, not {want}")
 
 
 def _word(check: bool):
@@ -526,10 +526,9 @@ def _checked(status: int, word, where: str):
 
 def _expect_attn(where: str, q, k, v, cu_seqlens):
     bf16 = torch.bfloat16
-    _expect(where, q=(q, bf16, (None, None, None)))
-    nt, _, d = q.shape
-    _expect(where, k=(k, bf16, (nt, None, d)), v=(v, bf16, tuple(k.shape)),
-            cu_seqlens=(cu_seqlens, torch.int32, (None,)))
+    _expect(where, ("q", q, bf16, 3), ("k", k, bf16, 3))
+    kv = (q.shape[0], k.shape[1], q.shape[2])
+    _expect(where, ("k", k, bf16, kv), ("v", v, bf16, kv), ("cu_seqlens", cu_seqlens, torch.int32, 1))
 
 
 def attn_fwd_window(q, k, v, cu_seqlens, max_seqlen: int, window: int, sinks: int = 0, softmax_scale: float = 0.0,
@@ -562,8 +561,8 @@ def attn_bwd_window(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, window: 
                           softmax_scale, check=check)
     _expect_attn("attn_bwd_window", q, k, v, cu_seqlens)
     nt, hq, d = q.shape
-    _expect("attn_bwd_window", o=(o, q.dtype, tuple(q.shape)), lse=(lse, torch.float32, (hq, nt)),
-            dout=(dout, q.dtype, tuple(q.shape)))
+    _expect("attn_bwd_window", ("o", o, q.dtype, q.shape), ("lse", lse, torch.float32, (hq, nt)),
+            ("dout", dout, q.dtype, q.shape))
     hkv = k.shape[1]
     ns = cu_seqlens.numel() - 1
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
@@ -584,9 +583,9 @@ def stream_positions(cu_seqlens, tok_src_step, step_img, step_txt, step_grid, st
                           check=check)
     ns, nt = cu_seqlens.numel() - 1, tok_src_step.numel()
     i32 = torch.int32
-    _expect("stream_positions", cu_seqlens=(cu_seqlens, i32, (None,)), tok_src_step=(tok_src_step, i32, (None,)),
-            step_img=(step_img, i32, (None,)), step_txt=(step_txt, i32, (step_img.numel(),)),
-            step_grid=(step_grid, i32, (step_img.numel(), 3)))
+    n = step_img.numel()
+    _expect("stream_positions", ("cu_seqlens", cu_seqlens, i32, 1), ("tok_src_step", tok_src_step, i32, 1),
+            ("step_img", step_img, i32, 1), ("step_txt", step_txt, i32, (n,)), ("step_grid", step_grid, i32, (n, 3)))
     pos = torch.empty((3, nt), dtype=torch.int32, device=tok_src_step.device)
     word = _word(check)
     _checked(vcs_stream_positions(cu_seqlens, ns, nt, tok_src_step, step_img, step_txt, step_grid, step_img.numel(),
@@ -611,13 +610,13 @@ def gather_rope(q_traj, k_traj, v_traj, tok_gather, pos, rope: VcsRope, stream=N
         return _on_stream(stream, gather_rope, q_traj, k_traj, v_traj, tok_gather, pos, rope, check=check)
     nt = q_traj.shape[0] if tok_gather is None else tok_gather.numel()
     bf16, i32 = torch.bfloat16, torch.int32
-    _expect("gather_rope", q_traj=(q_traj, bf16, (None, None, None)))
+    _expect("gather_rope", ("q_traj", q_traj, bf16, 3), ("k_traj", k_traj, bf16, 3))
     tt, hq, d = q_traj.shape
-    _expect("gather_rope", k_traj=(k_traj, bf16, (tt, None, d)), v_traj=(v_traj, bf16, tuple(k_traj.shape)),
-            pos=(pos, i32, (rope.num_axes, nt)))
-    if tok_gather is not None:
-        _expect("gather_rope", tok_gather=(tok_gather, i32, (None,)))
     hkv = k_traj.shape[1]
+    _expect("gather_rope", ("k_traj", k_traj, bf16, (tt, hkv, d)), ("v_traj", v_traj, bf16, (tt, hkv, d)),
+            ("pos", pos, i32, (rope.num_axes, nt)))
+    if tok_gather is not None:
+        _expect("gather_rope", ("tok_gather", tok_gather, i32, 1))
     q = torch.empty((nt, hq, d), dtype=q_traj.dtype, device=q_traj.device)
     k = torch.empty((nt, hkv, d), dtype=k_traj.dtype, device=q_traj.device)
     v = torch.empty((nt, hkv, d), dtype=v_traj.dtype, device=q_traj.device)
@@ -631,7 +630,7 @@ def gather_inverse(tok_gather, traj_tokens: int, stream=None, check=True):
     """(inv_off [traj_tokens + 1], inv_tok [num_tokens]) int32: the segment tokens of every trajectory token."""
     if stream is not None:
         return _on_stream(stream, gather_inverse, tok_gather, traj_tokens, check=check)
-    _expect("gather_inverse", tok_gather=(tok_gather, torch.int32, (None,)))
+    _expect("gather_inverse", ("tok_gather", tok_gather, torch.int32, 1))
     nt, dev = tok_gather.numel(), tok_gather.device
     off = torch.empty(traj_tokens + 1, dtype=torch.int32, device=dev)
     tok = torch.empty(nt, dtype=torch.int32, device=dev)
@@ -648,15 +647,15 @@ def gather_rope_bwd(dq, dk, dv, pos, inv_off, inv_tok, rope: VcsRope, stream=Non
     if stream is not None:
         return _on_stream(stream, gather_rope_bwd, dq, dk, dv, pos, inv_off, inv_tok, rope, check=check)
     bf16, i32 = torch.bfloat16, torch.int32
-    _expect("gather_rope_bwd", dq=(dq, bf16, (None, None, None)))
+    _expect("gather_rope_bwd", ("dq", dq, bf16, 3), ("dk", dk, bf16, 3))
     nt, hq, d = dq.shape
-    _expect("gather_rope_bwd", dk=(dk, bf16, (nt, None, d)), dv=(dv, bf16, tuple(dk.shape)),
-            pos=(pos, i32, (rope.num_axes, nt)))
+    hkv = dk.shape[1]
+    _expect("gather_rope_bwd", ("dk", dk, bf16, (nt, hkv, d)), ("dv", dv, bf16, (nt, hkv, d)),
+            ("pos", pos, i32, (rope.num_axes, nt)))
     if (inv_off is None) != (inv_tok is None):
         raise ValueError("gather_rope_bwd: inv_off and inv_tok go together")
     if inv_off is not None:
-        _expect("gather_rope_bwd", inv_off=(inv_off, i32, (None,)), inv_tok=(inv_tok, i32, (nt,)))
-    hkv = dk.shape[1]
+        _expect("gather_rope_bwd", ("inv_off", inv_off, i32, 1), ("inv_tok", inv_tok, i32, (nt,)))
     tt = nt if inv_off is None else inv_off.numel() - 1
     out = [torch.empty((tt, h, d), dtype=dq.dtype, device=dq.device) for h in (hq, hkv, hkv)]
     word = _word(check)
