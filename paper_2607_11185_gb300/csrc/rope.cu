@@ -225,8 +225,14 @@ constexpr int64_t kSmallOffsets = 8192;  // trajectory tokens whose searches tak
 template <int STEP>
 __device__ __forceinline__ void load_keys(const int32_t* __restrict__ keys, int64_t at, int64_t n, uint32_t T,
                                           bool first, int32_t* status, uint32_t (&key)[kPerThread]) {
+  if (at + (kPerThread - 1) * STEP < n) {  // a whole tile: one address
+    const int32_t* p = keys + at;
 #pragma unroll
-  for (int u = 0; u < kPerThread; ++u) key[u] = (uint32_t)__ldg(&keys[at + u * STEP < n ? at + u * STEP : n - 1]);
+    for (int u = 0; u < kPerThread; ++u) key[u] = (uint32_t)__ldg(p + u * STEP);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) key[u] = (uint32_t)__ldg(&keys[at + u * STEP < n ? at + u * STEP : n - 1]);
+  }
   if (!first) return;
   bool bad = false;
 #pragma unroll
@@ -307,9 +313,12 @@ struct SortTile {
   int32_t seen[kSortWarps][256];  // keys of each digit that a warp has passed; then where its next one goes
   int32_t wsum[kSortWarps];
   int32_t to[256];                // from a place in the tile to the digit's place in the output
-  uint32_t key[kTile];
-  int32_t val[kTile];
+  uint32_t key[kTile + kTile / 16];  // at skew(place)
+  int32_t val[kTile + kTile / 16];
 };
+// A tile has some 16 keys a digit, so that a warp's keys of consecutive digits go 16 places apart, all to two banks: a
+// word of space behind every 16 spreads them.
+__device__ __forceinline__ int skew(int i) { return i + (i >> 4); }
 
 // Places of the tile's keys sorted by a digit.  Warp w has its keys [32 rounds w, + 32 rounds) in order, 32 at a
 // time (key u of a thread is there if 32 u < live, and u < rounds): a key's
@@ -379,7 +388,11 @@ __global__ void __launch_bounds__(kSortThreads, 4)
   load_keys<32>(keys, base + off, n, T, first, nullptr, key);
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) val[u] = (int)(base + off) + 32 * u;
-  if (!first) {
+  if (!first && here == kTile) {
+    const int32_t* p = vals + base + off;
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) val[u] = __ldg(p + 32 * u);
+  } else if (!first) {
 #pragma unroll
     for (int u = 0; u < kPerThread; ++u) val[u] = __ldg(&vals[val[u] < n ? val[u] : n - 1]);
   }
@@ -388,16 +401,16 @@ __global__ void __launch_bounds__(kSortThreads, 4)
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u)
     if (32 * u < live) {
-      s.key[place[u]] = key[u];
-      s.val[place[u]] = val[u];
+      s.key[skew(place[u])] = key[u];
+      s.val[skew(place[u])] = val[u];
     }
   __syncthreads();
 #pragma unroll 4
   for (int i = tid; i < here; i += kSortThreads) {
-    const uint32_t k = s.key[i];
+    const uint32_t k = s.key[skew(i)];
     const int to = s.to[(k >> shift) & 255u] + i;
     keys_out[to] = (int32_t)k;
-    vals_out[to] = s.val[i];
+    vals_out[to] = s.val[skew(i)];
   }
 }
 
@@ -420,28 +433,28 @@ __global__ void __launch_bounds__(kSortThreads)
 #pragma unroll
     for (int u = 0; u < kPerThread; ++u)
       if (u < rounds && 32 * u < live) {
-        s.key[place[u]] = key[u];
-        s.val[place[u]] = val[u];
+        s.key[skew(place[u])] = key[u];
+        s.val[skew(place[u])] = val[u];
       }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < kPerThread; ++u)
       if (u < rounds && 32 * u < live) {
-        key[u] = s.key[at + 32 * u];
-        val[u] = s.val[at + 32 * u];
+        key[u] = s.key[skew(at + 32 * u)];
+        val[u] = s.val[skew(at + 32 * u)];
       }
     __syncthreads();
   }
   for (int i = tid; i < n; i += kSortThreads) {
-    keys_out[i] = (int32_t)s.key[i];
-    vals_out[i] = s.val[i];
+    keys_out[i] = (int32_t)s.key[skew(i)];
+    vals_out[i] = s.val[skew(i)];
   }
   if (off == nullptr) return;
   for (uint32_t t = tid; t <= T; t += kSortThreads) {
     int a = 0, b = n;
     while (a < b) {
       const int mid = (a + b) >> 1;
-      if (s.key[mid] < t) a = mid + 1;
+      if (s.key[skew(mid)] < t) a = mid + 1;
       else b = mid;
     }
     off[t] = a;
