@@ -210,21 +210,35 @@ __global__ void __launch_bounds__(kPosThreads)
 }
 
 // ------------------------------------------------------------------ inverse map
-// Stable radix sort of (tok_gather[n], n) by 8-bit digits: the n of equal keys stay in order, whatever
-// the map, and no atomic decides an order.  A pass is three launches: digit counts of tiles of kTile
-// keys, per digit the scan of its tiles' counts, and the scatter; up to one tile of keys is sorted by one block
-// in shared memory.  Keys outside [0, T) become T, behind all others.
+// For every trajectory token t the segment tokens that are copies of it, in order, whatever the map; no atomic
+// decides an order.  A layout's map is made of stretches of consecutive tokens, so what is sorted is not its keys but
+// runs: up to 512 neighbouring consecutive keys within one group of 2^shift trajectory tokens, as one word (group,
+// length - 1) and the place of the first.  inverse_runs finds them and counts every group's runs and keys; a
+// stable radix sort by 8-bit digits of the group brings a group's runs together, in order; then a warp takes a group:
+// the ends of its runs give the tokens' counts, their scan inv_off and where each token's next copy goes.  The map is
+// read once, and once more where runs begin.  15.8 M keys of long rollouts: 130 us (a sort of the keys themselves by
+// three digits and a search of the offsets took 400); random keys, which are runs of one, take 720 against 430.
+// Keys outside [0, T) become T, behind all others.
 constexpr int kSortThreads = 256;
 constexpr int kPerThread = 16;
 constexpr int kTile = kSortThreads * kPerThread;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int64_t kSmallOffsets = 8192;  // trajectory tokens whose searches take the one block about a launch's time
+constexpr int kRunBits = 9;              // a run is within a warp's 512 keys
+constexpr int kGroupKeys = 256;          // keys a group, on average: 15.8 M keys take 261, 220 and 216 us at 128, 256, 512
+constexpr int kGroups = 256;             // but one digit of groups at least
+constexpr int kMostGroups = 4096;        // and up to these where a group would pass kCounters tokens
+constexpr int kCounters = 512;           // trajectory tokens that a warp counts at a time
+constexpr int kGroupTile = 4096;         // groups scanned by a block
+constexpr int kLongRun = 8;              // keys of a run, on average of 32, from which runs are taken one by one
+constexpr int kAhead = 4;                // of a run's keys, loads before their stores
+constexpr int kSortBlocks = 152 * 4;     // blocks, of as many tiles each as it takes
 
 // Keys at, at + step, ... before n.  All loads first (the check of a key, which may report, would hold up the next
 // one's load: a pass over 15.8 M keys took 140 us with it in between).
 template <int STEP>
 __device__ __forceinline__ void load_keys(const int32_t* __restrict__ keys, int64_t at, int64_t n, uint32_t T,
-                                          bool first, int32_t* status, uint32_t (&key)[kPerThread]) {
+                                          int32_t* status, uint32_t (&key)[kPerThread]) {
   if (at + (kPerThread - 1) * STEP < n) {  // a whole tile: one address
     const int32_t* p = keys + at;
 #pragma unroll
@@ -233,7 +247,6 @@ __device__ __forceinline__ void load_keys(const int32_t* __restrict__ keys, int6
 #pragma unroll
     for (int u = 0; u < kPerThread; ++u) key[u] = (uint32_t)__ldg(&keys[at + u * STEP < n ? at + u * STEP : n - 1]);
   }
-  if (!first) return;
   bool bad = false;
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u)
@@ -242,54 +255,6 @@ __device__ __forceinline__ void load_keys(const int32_t* __restrict__ keys, int6
       bad = bad || at + u * STEP < n;
     }
   if (bad) set_status(status, VCS_ERR_DEVICE_CHECK);
-}
-
-__global__ void __launch_bounds__(kSortThreads)
-    inverse_count(const int32_t* __restrict__ keys, int64_t n, uint32_t T, int shift, int32_t* __restrict__ counts,
-                  int tiles, bool first, int32_t* status) {
-  __shared__ int32_t c[256];
-  c[threadIdx.x] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kTile + threadIdx.x;
-  uint32_t key[kPerThread];
-  load_keys<kSortThreads>(keys, base, n, T, first, status, key);
-#pragma unroll
-  for (int u = 0; u < kPerThread; ++u)
-    if (base + u * kSortThreads < n) atomicAdd(&c[(key[u] >> shift) & 255u], 1);
-  __syncthreads();
-  counts[(size_t)threadIdx.x * tiles + blockIdx.x] = c[threadIdx.x];
-}
-
-// Block b: the exclusive scan of digit b's counts over the tiles, and their sum.
-__global__ void __launch_bounds__(1024)
-    inverse_scan(int32_t* __restrict__ counts, int tiles, int32_t* __restrict__ totals) {
-  __shared__ int32_t wsum[32];
-  int32_t* c = counts + (size_t)blockIdx.x * tiles;
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  int carry = 0;
-  for (int base = 0; base < tiles; base += 1024) {
-    const int i = base + (int)threadIdx.x;
-    const int v = i < tiles ? c[i] : 0;
-    int x = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) wsum[wid] = x;
-    __syncthreads();
-    int w = wsum[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, w, o);
-      if (lane >= o) w += y;
-    }
-    const int before = wid > 0 ? __shfl_sync(0xffffffffu, w, wid - 1) : 0;
-    if (i < tiles) c[i] = carry + before + x - v;
-    carry += __shfl_sync(0xffffffffu, w, 31);
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
 // Exclusive sum over the block's threads of v.
@@ -309,6 +274,157 @@ __device__ __forceinline__ int block_before(int v, int32_t* wsum) {
   return at;
 }
 
+// The runs of a block's `each` tiles, packed at the block's own places of run_key and run_at; how many of each first
+// digit; and what they add to their groups (runs above 32 bits, keys below).
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_runs(const int32_t* __restrict__ keys, int64_t n, uint32_t T, int shift, int each,
+                 uint32_t* __restrict__ run_key, int32_t* __restrict__ run_at, int32_t* __restrict__ block_runs,
+                 int32_t* __restrict__ counts, unsigned long long* __restrict__ groups, int32_t* status) {
+  __shared__ int32_t c[256];
+  __shared__ int32_t wsum[2][kSortWarps];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  c[tid] = 0;
+  int64_t base = (int64_t)blockIdx.x * each * kTile;
+  run_key += base;
+  run_at += base;
+  int runs = 0;
+  for (int t = 0; t < each && base < n; ++t, base += kTile) {
+    const int off = wid * (32 * kPerThread), here = (int)(n - base < kTile ? n - base : kTile);
+    const int live = min(32 * kPerThread, here - off);  // keys of the warp, possibly less than none
+    uint32_t key[kPerThread], heads[kPerThread];
+    load_keys<32>(keys, base + off + lane, n, T, status, key);
+    int found = 0;
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u) {
+      uint32_t last = __shfl_up_sync(0xffffffffu, key[u], 1);
+      if (u > 0) {
+        const uint32_t end = __shfl_sync(0xffffffffu, key[u - 1], 31);
+        if (lane == 0) last = end;
+      }
+      const bool head = key[u] != last + 1 || (key[u] & ((1u << shift) - 1u)) == 0 || (u == 0 && lane == 0);
+      heads[u] = __ballot_sync(0xffffffffu, head && 32 * u + lane < live);
+      found += __popc(heads[u]);
+    }
+    if (lane == 0) wsum[t & 1][wid] = found;
+    __syncthreads();
+    int at = runs + found;  // behind the warp's runs
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+      if (w < wid) at += wsum[t & 1][w];
+      runs += wsum[t & 1][w];
+    }
+    int next = live;  // the first place behind the run
+#pragma unroll
+    for (int u = kPerThread - 1; u >= 0; --u) {
+      at -= __popc(heads[u]);
+      if (heads[u] >> lane & 1) {
+        const uint32_t later = heads[u] & ~((2u << lane) - 1u), group = key[u] >> shift;
+        const int len = (later != 0 ? 32 * u + __ffs(later) - 1 : next) - (32 * u + lane);
+        const int to = at + __popc(heads[u] & ((1u << lane) - 1u));
+        run_key[to] = group << kRunBits | (uint32_t)(len - 1);
+        run_at[to] = (int32_t)(base + off + 32 * u + lane);
+        atomicAdd(&c[group & 255u], 1);
+        atomicAdd(&groups[group], 1ull << 32 | (unsigned long long)len);
+      }
+      if (heads[u] != 0) next = 32 * u + __ffs(heads[u]) - 1;
+    }
+  }
+  __syncthreads();
+  counts[(size_t)tid * gridDim.x + blockIdx.x] = c[tid];
+  if (tid == 0) block_runs[blockIdx.x] = runs;
+}
+
+// Tiles of n packed runs that a block of so many takes.
+__device__ __forceinline__ int packed_each(int64_t n, int blocks) {
+  return (int)(((n + kTile - 1) / kTile + blocks - 1) / blocks);
+}
+
+// Digit counts of packed runs.
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_count(const uint32_t* __restrict__ run_key, const int32_t* __restrict__ num_runs, int shift,
+                  int32_t* __restrict__ counts) {
+  __shared__ int32_t c[256];
+  const int64_t n = *num_runs;
+  const int each = packed_each(n, gridDim.x);
+  const int64_t base = (int64_t)blockIdx.x * each * kTile;
+  if (base >= n) return;
+  c[threadIdx.x] = 0;
+  __syncthreads();
+  const int here = (int)min(n - base, (int64_t)each * kTile);
+  run_key += base;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < here; i += kSortThreads) atomicAdd(&c[run_key[i] >> shift & 255u], 1);
+  __syncthreads();
+  counts[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = c[threadIdx.x];
+}
+
+// Exclusive scan of v over the block's 1,024 threads; all is its sum.
+template <typename T>
+__device__ __forceinline__ T scan_1024(T v, T* wsum, T& all) {
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  T x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) wsum[wid] = x;
+  __syncthreads();
+  T w = wsum[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += y;
+  }
+  const T before = __shfl_sync(0xffffffffu, w, wid > 0 ? wid - 1 : 0);
+  all = __shfl_sync(0xffffffffu, w, 31);
+  __syncthreads();
+  return x - v + (wid > 0 ? before : T(0));
+}
+
+// Block b < 256: the exclusive scan of digit b's counts over the blocks that counted (with packed runs, as many as
+// num_runs fill), and their sum.
+// A block behind them: that of kGroupTile groups, and their sum.
+__global__ void __launch_bounds__(1024)
+    inverse_scan(int32_t* __restrict__ counts, int blocks, const int32_t* __restrict__ num_runs,
+                 int32_t* __restrict__ totals, unsigned long long* __restrict__ groups, int num_groups,
+                 unsigned long long* __restrict__ group_sums) {
+  if (blockIdx.x < 256) {
+    __shared__ int32_t wsum[32];
+    int32_t* c = counts + (size_t)blockIdx.x * blocks;
+    int live = blocks;
+    if (num_runs != nullptr) {
+      const int64_t n = *num_runs, part = (int64_t)packed_each(n, blocks) * kTile;
+      live = (int)((n + part - 1) / part);
+    }
+    int carry = 0, all;
+    for (int base = 0; base < live; base += 1024) {
+      const int i = base + (int)threadIdx.x;
+      const int x = scan_1024(i < live ? c[i] : 0, wsum, all);
+      if (i < live) c[i] = carry + x;
+      carry += all;
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = carry;
+  } else {
+    __shared__ unsigned long long wsum[32];
+    constexpr int kEach = kGroupTile / 1024;
+    const int at = ((int)blockIdx.x - 256) * kGroupTile + (int)threadIdx.x * kEach;
+    unsigned long long v[kEach], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      v[i] = at + i < num_groups ? groups[at + i] : 0ull;
+      sum += v[i];
+    }
+    unsigned long long x = scan_1024(sum, wsum, all);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (at + i < num_groups) groups[at + i] = x;
+      x += v[i];
+    }
+    if (threadIdx.x == 0) group_sums[blockIdx.x - 256] = all;
+  }
+}
+
 struct SortTile {
   int32_t seen[kSortWarps][256];  // keys of each digit that a warp has passed; then where its next one goes
   int32_t wsum[kSortWarps];
@@ -324,9 +440,9 @@ __device__ __forceinline__ int skew(int i) { return i + (i >> 4); }
 // time (key u of a thread is there if 32 u < live, and u < rounds): a key's
 // rank among the warp's equal digits is the count of them before it, by votes on the digit's bits (a match
 // instruction takes several times as long) and a running count.
-// Returns the thread's digit's first place.
+// Returns the first place of the thread's digit, and how many keys have it.
 __device__ __forceinline__ int place_tile(SortTile& s, const uint32_t (&key)[kPerThread], int live, int rounds,
-                                          int shift, int (&place)[kPerThread]) {
+                                          int shift, int (&place)[kPerThread], int& count) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
 #pragma unroll
   for (int w = 0; w < kSortWarps; ++w) s.seen[w][tid] = 0;
@@ -354,10 +470,10 @@ __device__ __forceinline__ int place_tile(SortTile& s, const uint32_t (&key)[kPe
     place[u] = __shfl_sync(0xffffffffu, place[u], (__ffs(same[u]) - 1) & 31) + __popc(same[u] & ((1u << lane) - 1u));
   }
   __syncthreads();
-  int sum = 0;
+  count = 0;
 #pragma unroll
-  for (int w = 0; w < kSortWarps; ++w) sum += s.seen[w][tid];
-  const int first = block_before(sum, s.wsum);
+  for (int w = 0; w < kSortWarps; ++w) count += s.seen[w][tid];
+  const int first = block_before(count, s.wsum);
   int at = first;
 #pragma unroll
   for (int w = 0; w < kSortWarps; ++w) {
@@ -372,64 +488,79 @@ __device__ __forceinline__ int place_tile(SortTile& s, const uint32_t (&key)[kPe
   return first;
 }
 
-// The tile is sorted in shared memory first, so that a digit's keys leave as one run: 4-byte stores to 256 places
-// took 265 us of a pass over 15.8 M keys.
+// A pass of the runs' sort.  The first one's blocks have block_runs runs each, and it says how many there are; later
+// ones' are packed.  A tile is sorted in shared memory first, so that a digit's runs leave together.
 __global__ void __launch_bounds__(kSortThreads, 4)
-    inverse_scatter(const int32_t* __restrict__ keys, const int32_t* __restrict__ vals, int64_t n, uint32_t T,
-                    int shift, const int32_t* __restrict__ counts, const int32_t* __restrict__ totals, int tiles,
-                    bool first, int32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
+    inverse_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ vals, int shift, int each,
+                    const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
+                    const int32_t* __restrict__ block_runs, int32_t* __restrict__ num_runs,
+                    uint32_t* __restrict__ keys_out, int32_t* __restrict__ vals_out) {
   __shared__ SortTile s;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int64_t base = (int64_t)blockIdx.x * kTile;
-  const int here = (int)(n - base < kTile ? n - base : kTile);
-  const int off = wid * (32 * kPerThread) + lane, live = here - off;  // key u of the thread: off + 32 u < here
-  uint32_t key[kPerThread];
-  int val[kPerThread], place[kPerThread];
-  load_keys<32>(keys, base + off, n, T, first, nullptr, key);
-#pragma unroll
-  for (int u = 0; u < kPerThread; ++u) val[u] = (int)(base + off) + 32 * u;
-  if (!first && here == kTile) {
-    const int32_t* p = vals + base + off;
-#pragma unroll
-    for (int u = 0; u < kPerThread; ++u) val[u] = __ldg(p + 32 * u);
-  } else if (!first) {
-#pragma unroll
-    for (int u = 0; u < kPerThread; ++u) val[u] = __ldg(&vals[val[u] < n ? val[u] : n - 1]);
+  int64_t base = (int64_t)blockIdx.x * each * kTile;
+  int all;
+  if (block_runs != nullptr) {
+    all = block_runs[blockIdx.x];
+  } else {
+    const int64_t n = *num_runs;
+    each = packed_each(n, gridDim.x);
+    base = (int64_t)blockIdx.x * each * kTile;
+    if (base >= n) return;
+    all = (int)min(n - base, (int64_t)each * kTile);
   }
-  const int digit = block_before(totals[tid], s.wsum) + counts[(size_t)tid * tiles + blockIdx.x];
-  s.to[tid] = digit - place_tile(s, key, live, kPerThread, shift, place);
+  keys += base;
+  vals += base;
+  int to = block_before(totals[tid], s.wsum);  // of the thread's digit
+  if (block_runs != nullptr && blockIdx.x == 0 && tid == kSortThreads - 1) *num_runs = to + totals[tid];
+  to += counts[(size_t)tid * gridDim.x + blockIdx.x];
+  for (int done = 0; done < all; done += kTile) {
+    const int here = min(all - done, kTile), rounds = (here + kSortThreads - 1) / kSortThreads;
+    const int off = wid * (32 * rounds) + lane, live = here - off;  // run u of the thread: off + 32 u < here
+    uint32_t key[kPerThread];
+    int val[kPerThread], place[kPerThread];
 #pragma unroll
-  for (int u = 0; u < kPerThread; ++u)
-    if (32 * u < live) {
-      s.key[skew(place[u])] = key[u];
-      s.val[skew(place[u])] = val[u];
+    for (int u = 0; u < kPerThread; ++u) {
+      const bool on = u < rounds && 32 * u < live;
+      key[u] = on ? __ldg(&keys[done + off + 32 * u]) : 0u;
+      val[u] = on ? __ldg(&vals[done + off + 32 * u]) : 0;
     }
-  __syncthreads();
-#pragma unroll 4
-  for (int i = tid; i < here; i += kSortThreads) {
-    const uint32_t k = s.key[skew(i)];
-    const int to = s.to[(k >> shift) & 255u] + i;
-    keys_out[to] = (int32_t)k;
-    vals_out[to] = s.val[skew(i)];
+    int count;
+    s.to[tid] = to - place_tile(s, key, live, rounds, shift, place, count);
+    to += count;
+#pragma unroll
+    for (int u = 0; u < kPerThread; ++u)
+      if (u < rounds && 32 * u < live) {
+        s.key[skew(place[u])] = key[u];
+        s.val[skew(place[u])] = val[u];
+      }
+    __syncthreads();
+    for (int i = tid; i < here; i += kSortThreads) {
+      const uint32_t k = s.key[skew(i)];
+      const int at = s.to[k >> shift & 255u] + i;
+      keys_out[at] = k;
+      vals_out[at] = s.val[skew(i)];
+    }
+    __syncthreads();
   }
 }
 
-// Up to one tile of keys: all passes in shared memory, and the offsets of few trajectory tokens by searches there
-// (off not nullptr).
+// Up to one tile of keys of few trajectory tokens: sorted by one block in shared memory, and the offsets by searches
+// there.
 __global__ void __launch_bounds__(kSortThreads)
-    inverse_small(const int32_t* __restrict__ keys, int32_t n, uint32_t T, int passes, int32_t* __restrict__ keys_out,
-                  int32_t* __restrict__ vals_out, int32_t* __restrict__ off, int32_t* status) {
+    inverse_small(const int32_t* __restrict__ keys, int32_t n, uint32_t T, int passes, int32_t* __restrict__ off,
+                  int32_t* __restrict__ vals_out, int32_t* status) {
   __shared__ SortTile s;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int rounds = (n + kSortThreads - 1) / kSortThreads;
   const int at = wid * 32 * rounds + lane, live = n - at;
   uint32_t key[kPerThread];
   int val[kPerThread], place[kPerThread];
-  load_keys<32>(keys, at, n, T, true, status, key);
+  load_keys<32>(keys, at, n, T, status, key);
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) val[u] = at + 32 * u;
   for (int p = 0; p < passes; ++p) {
-    place_tile(s, key, live, rounds, 8 * p, place);
+    int count;
+    place_tile(s, key, live, rounds, 8 * p, place, count);
 #pragma unroll
     for (int u = 0; u < kPerThread; ++u)
       if (u < rounds && 32 * u < live) {
@@ -445,11 +576,7 @@ __global__ void __launch_bounds__(kSortThreads)
       }
     __syncthreads();
   }
-  for (int i = tid; i < n; i += kSortThreads) {
-    keys_out[i] = (int32_t)s.key[skew(i)];
-    vals_out[i] = s.val[skew(i)];
-  }
-  if (off == nullptr) return;
+  for (int i = tid; i < n; i += kSortThreads) vals_out[i] = s.val[skew(i)];
   for (uint32_t t = tid; t <= T; t += kSortThreads) {
     int a = 0, b = n;
     while (a < b) {
@@ -461,58 +588,136 @@ __global__ void __launch_bounds__(kSortThreads)
   }
 }
 
-// off[t] = first place of a key >= t in the sorted keys, for t in a block's 1,024: two searches bound
-// the block's keys, counts of them in shared memory and a scan give the rest.
-constexpr int kOffTile = 1024;
-__global__ void __launch_bounds__(256) inverse_offsets(const int32_t* __restrict__ keys, int32_t n, int64_t T,
-                                                       int32_t* __restrict__ off) {
-  __shared__ int32_t c[kOffTile];
-  __shared__ int32_t bound[2];
-  __shared__ int32_t wsum[8];
-  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int64_t t0 = (int64_t)blockIdx.x * kOffTile;
+// A warp a group of trajectory tokens, kCounters at a time: the copies of each, from where runs begin and end; their
+// scan; and the copies in order to their places.  A run's tokens differ, so long runs are taken one by one; the keys
+// of short ones are taken 32 at a time, and those of one token told apart by votes on the bits.
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_place(const int32_t* __restrict__ keys, uint32_t T, int shift, const uint32_t* __restrict__ run_key,
+                  const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups, int num_groups,
+                  const unsigned long long* __restrict__ group_sums, int32_t* __restrict__ inv_off,
+                  int32_t* __restrict__ inv_tok) {
+  __shared__ int32_t counters[kSortWarps][kCounters];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int g = blockIdx.x * kSortWarps + wid;
+  if (g >= num_groups) return;
+  unsigned long long before = 0;
+  for (int i = lane; i < g / kGroupTile; i += 32) before += group_sums[i];
 #pragma unroll
-  for (int u = 0; u < kOffTile / 256; ++u) c[u * 256 + tid] = 0;
-  if (wid < 2) {  // a warp a search: the keys from `a` on, 32 probes at a time
-    const int64_t t = t0 + wid * (int64_t)kOffTile;
-    int a = 0, len = n;
-    while (len > 0) {
-      const int step = (len + 31) / 32;
-      const int at = a + lane * step;
-      const bool less = lane * step < len && __ldg(&keys[at]) < t;
-      const int c = __popc(__ballot_sync(0xffffffffu, less));  // the probes of smaller keys come first
-      if (c == 0) break;
-      const int from = (c - 1) * step + 1;  // past the last smaller one
-      len = min(step - 1, len - from);
-      a += from;
+  for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+  const unsigned long long in_tile = groups[g];
+  const unsigned long long end = (g + 1) % kGroupTile == 0 || g + 1 == num_groups ? group_sums[g / kGroupTile]
+                                                                                  : groups[g + 1];
+  const int runs = (int)((end >> 32) - (in_tile >> 32));
+  before += in_tile;
+  run_key += before >> 32;
+  run_at += before >> 32;
+  int next = (int)(uint32_t)before;  // the group's first place
+  int32_t* c = counters[wid];
+  const int64_t lo = (int64_t)g << shift, hi = min(lo + ((int64_t)1 << shift), (int64_t)T + 1);
+  const int bits = min(shift, 9);
+  for (int64_t t0 = lo; t0 < hi; t0 += kCounters) {
+    const int width = (int)min((int64_t)kCounters, hi - t0);
+    // run r's part of the counters [first, first + len), and its place in the map
+    auto load_run = [&](int r, int& first, int& len, int& at) {
+      first = len = at = 0;
+      if (r >= runs) return;
+      at = run_at[r];
+      const int64_t k = (int64_t)min((uint32_t)__ldg(&keys[at]), T) - t0;
+      const int64_t from = max(k, (int64_t)0), upto = min(k + (run_key[r] & ((1u << kRunBits) - 1u)) + 1, (int64_t)width);
+      if (from >= upto) return;
+      first = (int)from;
+      len = (int)(upto - from);
+      at += (int)(from - k);
+    };
+    for (int i = lane; i < width; i += 32) c[i] = 0;
+    __syncwarp();
+    for (int r = lane; r < runs; r += 32) {
+      int first, len, at;
+      load_run(r, first, len, at);
+      if (len > 0) {
+        atomicAdd(&c[first], 1);
+        if (first + len < width) atomicAdd(&c[first + len], -1);
+      }
     }
-    if (lane == 0) bound[wid] = a;
-  }
-  __syncthreads();
-  const int lo = bound[0], hi = bound[1];
-  for (int i = lo + tid; i < hi; i += 256) atomicAdd(&c[keys[i] - t0], 1);
-  __syncthreads();
-  int v[kOffTile / 256], sum = 0;
+    __syncwarp();
+    int copies = 0;  // of the token before
+    for (int i = lane; i - lane < width; i += 32) {
+      int x = i < width ? c[i] : 0;
 #pragma unroll
-  for (int u = 0; u < kOffTile / 256; ++u) {
-    v[u] = c[tid * (kOffTile / 256) + u];
-    sum += v[u];
-  }
-  int x = sum;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      x += copies;
+      copies = __shfl_sync(0xffffffffu, x, 31);
+      const int v = i < width ? x : 0;
+      x = v;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) wsum[wid] = x;
-  __syncthreads();
-  int at = lo + x - sum;
-  for (int i = 0; i < wid; ++i) at += wsum[i];
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (i < width) {
+        c[i] = next + x - v;
+        inv_off[t0 + i] = next + x - v;
+      }
+      next += __shfl_sync(0xffffffffu, x, 31);
+    }
+    __syncwarp();
+    for (int r = 0; r < runs; r += 32) {
+      int first, len, at;
+      load_run(r + lane, first, len, at);
+      int upto = len;  // keys of the runs up to this one
 #pragma unroll
-  for (int u = 0; u < kOffTile / 256; ++u) {
-    const int64_t t = t0 + tid * (kOffTile / 256) + u;
-    if (t <= T) off[t] = at;
-    at += v[u];
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const int all = __shfl_sync(0xffffffffu, upto, 31), here = min(runs - r, 32);
+      if (all >= here * kLongRun) {
+        for (int j = 0; j < here; ++j) {
+          const int f = __shfl_sync(0xffffffffu, first, j), l = __shfl_sync(0xffffffffu, len, j);
+          const int a = __shfl_sync(0xffffffffu, at, j);
+          for (int e = lane; e < l; e += 32 * kAhead) {
+            int to[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+              if (e + 32 * u < l) to[u] = c[f + e + 32 * u];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+              if (e + 32 * u < l) {
+                inv_tok[to[u]] = a + e + 32 * u;
+                c[f + e + 32 * u] = to[u] + 1;
+              }
+          }
+          __syncwarp();
+        }
+      } else {
+        for (int b = 0; b < all; b += 32) {
+          const int e = b + lane;
+          int j = 0;  // runs that end at or before key e
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1)
+            if (__shfl_sync(0xffffffffu, upto, j + o - 1) <= e) j += o;
+          const int in_run = e - __shfl_sync(0xffffffffu, upto - len, j);
+          const int i = __shfl_sync(0xffffffffu, first, j) + in_run, a = __shfl_sync(0xffffffffu, at, j) + in_run;
+          const bool on = e < all;
+          uint32_t same = __ballot_sync(0xffffffffu, on);
+          for (int k = 0; k < bits; ++k) {
+            const bool bit = i >> k & 1;
+            const uint32_t v = __ballot_sync(0xffffffffu, bit);
+            same &= bit ? v : ~v;
+          }
+          const int to = on ? c[i] + __popc(same & ((1u << lane) - 1u)) : 0;
+          __syncwarp();
+          if (on) {
+            inv_tok[to] = a;
+            if (same >> lane == 1u) c[i] = to + 1;  // the last of its token
+          }
+          __syncwarp();
+        }
+      }
+    }
   }
 }
 
@@ -860,10 +1065,35 @@ cudaError_t launch_stream_positions(const int32_t* cu_seqlens, int32_t num_segme
   return cudaGetLastError();
 }
 
-// Workspace: digit counts of the tiles and their totals, then keys twice and tokens once.
+// Groups that the workspace has room for.
+int64_t group_limit(int64_t num_tokens) {
+  return num_tokens / kGroupKeys > kMostGroups ? num_tokens / kGroupKeys : kMostGroups;
+}
+
+// A group's trajectory tokens as a power of two; T, the token of the keys that are out of range, is in the last one.
+int group_shift(int64_t num_tokens, int64_t T) {
+  const int64_t want = num_tokens / kGroupKeys > kGroups ? num_tokens / kGroupKeys : kGroups;
+  int shift = 0;
+  while ((T >> shift) + 1 > want) ++shift;
+  while (1 << shift > kCounters && (T >> (shift - 1)) + 1 <= group_limit(num_tokens)) --shift;
+  return shift;
+}
+
+struct SortGrid {
+  int each, blocks;  // tiles a block
+};
+SortGrid sort_grid(int64_t num_tokens) {
+  const int64_t tiles = (num_tokens + kTile - 1) / kTile, each = (tiles + kSortBlocks - 1) / kSortBlocks;
+  return {(int)each, each == 0 ? 0 : (int)((tiles + each - 1) / each)};
+}
+
+// Workspace: digit counts of the blocks, their totals and the blocks' runs; the groups' counts and their sums; the
+// runs twice, but for one array (inv_tok).
 size_t gather_inverse_ws_bytes(int64_t num_tokens) {
-  const int64_t tiles = (num_tokens + kTile - 1) / kTile;
-  return align256((size_t)tiles * 256 * 4) + align256(256 * 4) + 3 * align256((size_t)num_tokens * 4) + 256;
+  const int64_t blocks = sort_grid(num_tokens).blocks, groups = group_limit(num_tokens);
+  return align256((size_t)blocks * 256 * 4) + align256(257 * 4) + align256((size_t)blocks * 4) +
+         align256((size_t)groups * 8) + align256((size_t)(groups / kGroupTile + 1) * 8) +
+         3 * align256((size_t)num_tokens * 4) + 256;
 }
 
 cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
@@ -871,38 +1101,49 @@ cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens,
   if (num_tokens == 0) {
     return cudaMemsetAsync(inv_off, 0, ((size_t)traj_tokens + 1) * 4, st);
   }
-  const int tiles = (int)((num_tokens + kTile - 1) / kTile);
+  const SortGrid grid = sort_grid(num_tokens);
+  const uint32_t T = (uint32_t)traj_tokens;
+  const int64_t limit = group_limit(num_tokens);
+  const int shift = group_shift(num_tokens, traj_tokens);
   char* w = static_cast<char*>(ws);
-  int32_t* counts = reinterpret_cast<int32_t*>(w);
-  w += align256((size_t)tiles * 256 * 4);
-  int32_t* totals = reinterpret_cast<int32_t*>(w);
-  w += align256(256 * 4);
-  const size_t nb = align256((size_t)num_tokens * 4);
-  int32_t* keys[2] = {reinterpret_cast<int32_t*>(w), reinterpret_cast<int32_t*>(w + nb)};
-  int32_t* spare = reinterpret_cast<int32_t*>(w + 2 * nb);
-  const int passes = key_passes(traj_tokens);
-  const int32_t* kin = tok_gather;
-  const int32_t* vin = nullptr;
-  if (tiles == 1) {
-    const bool all = traj_tokens <= kSmallOffsets;
-    inverse_small<<<1, kSortThreads, 0, st>>>(tok_gather, (int32_t)num_tokens, (uint32_t)traj_tokens, passes, keys[0],
-                                              inv_tok, all ? inv_off : nullptr, status);
-    if (all) return cudaGetLastError();
-    kin = keys[0];
+  auto take = [&w](size_t bytes) {
+    char* at = w;
+    w += align256(bytes);
+    return at;
+  };
+  auto* counts = reinterpret_cast<int32_t*>(take((size_t)grid.blocks * 256 * 4));
+  auto* totals = reinterpret_cast<int32_t*>(take(257 * 4));
+  int32_t* num_runs = totals + 256;
+  auto* block_runs = reinterpret_cast<int32_t*>(take((size_t)grid.blocks * 4));
+  auto* groups = reinterpret_cast<unsigned long long*>(take((size_t)limit * 8));
+  auto* group_sums = reinterpret_cast<unsigned long long*>(take((size_t)(limit / kGroupTile + 1) * 8));
+  const size_t nb = (size_t)num_tokens * 4;
+  uint32_t* key[2] = {reinterpret_cast<uint32_t*>(take(nb)), reinterpret_cast<uint32_t*>(take(nb))};
+  auto* spare = reinterpret_cast<int32_t*>(take(nb));
+  if (num_tokens <= kTile && traj_tokens <= kSmallOffsets) {
+    inverse_small<<<1, kSortThreads, 0, st>>>(tok_gather, (int32_t)num_tokens, T, key_passes(traj_tokens), inv_off,
+                                              inv_tok, status);
+    return cudaGetLastError();
   }
-  for (int p = 0; p < passes && tiles > 1; ++p) {
-    // the last pass writes inv_tok, the others alternate so that none writes what it reads
-    int32_t* vout = (passes - 1 - p) % 2 == 0 ? inv_tok : spare;
-    inverse_count<<<tiles, kSortThreads, 0, st>>>(kin, num_tokens, (uint32_t)traj_tokens, 8 * p, counts, tiles, p == 0,
-                                                  status);
-    inverse_scan<<<256, 1024, 0, st>>>(counts, tiles, totals);
-    inverse_scatter<<<tiles, kSortThreads, 0, st>>>(kin, vin, num_tokens, (uint32_t)traj_tokens, 8 * p, counts, totals,
-                                                    tiles, p == 0, keys[p & 1], vout);
-    kin = keys[p & 1];
-    vin = vout;
+  const int num_groups = (int)((traj_tokens >> shift) + 1), group_tiles = (num_groups + kGroupTile - 1) / kGroupTile;
+  const int passes = key_passes(num_groups - 1);
+  // the runs that are sorted last must not be where inverse_place writes
+  int32_t* at[2] = {passes % 2 == 0 ? spare : inv_tok, passes % 2 == 0 ? inv_tok : spare};
+  cudaError_t err = cudaMemsetAsync(groups, 0, (size_t)num_groups * 8, st);
+  if (err != cudaSuccess) return err;
+  inverse_runs<<<grid.blocks, kSortThreads, 0, st>>>(tok_gather, num_tokens, T, shift, grid.each, key[0], at[0],
+                                                     block_runs, counts, groups, status);
+  for (int p = 0; p < passes; ++p) {
+    const int digit = kRunBits + 8 * p, in = p & 1;
+    if (p > 0) inverse_count<<<grid.blocks, kSortThreads, 0, st>>>(key[in], num_runs, digit, counts);
+    inverse_scan<<<256 + (p == 0 ? group_tiles : 0), 1024, 0, st>>>(counts, grid.blocks, p == 0 ? nullptr : num_runs,
+                                                                    totals, groups, num_groups, group_sums);
+    inverse_scatter<<<grid.blocks, kSortThreads, 0, st>>>(key[in], at[in], digit, grid.each, counts, totals,
+                                                          p == 0 ? block_runs : nullptr, num_runs, key[in ^ 1],
+                                                          at[in ^ 1]);
   }
-  inverse_offsets<<<(unsigned)((traj_tokens + kOffTile) / kOffTile), 256, 0, st>>>(kin, (int32_t)num_tokens,
-                                                                                  traj_tokens, inv_off);
+  inverse_place<<<(num_groups + kSortWarps - 1) / kSortWarps, kSortThreads, 0, st>>>(
+      tok_gather, T, shift, key[passes & 1], at[passes & 1], groups, num_groups, group_sums, inv_off, inv_tok);
   return cudaGetLastError();
 }
 

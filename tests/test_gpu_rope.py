@@ -105,6 +105,33 @@ def test_inverse(n, t):
     assert np.array_equal(off.cpu().numpy(), np.searchsorted(gat[order], np.arange(t + 1)))
 
 
+@pytest.mark.parametrize("kind", ["stretches", "one token", "descending", "bad", "pairs"])
+@pytest.mark.parametrize("n,t", [(4097, 9000), (100_003, 8191), (100_003, 3_000_001), (5_000_011, 1_200_000)])
+def test_inverse_of_runs(n, t, kind):
+    """Stretches of consecutive tokens (a layout's map), and maps whose runs are longest, shortest, or out of range."""
+    vcs = _vcs()
+    rng = np.random.default_rng(n + t)
+    i = np.arange(n)
+    if kind == "stretches":
+        cuts = np.unique(rng.integers(0, n, n // 300))
+        start = rng.integers(0, t, len(cuts) + 1)
+        part = np.searchsorted(cuts, i, side="right")
+        gat = (start[part] + i - np.concatenate([[0], cuts])[part]) % t
+    elif kind == "one token":
+        gat = np.full(n, t - 1)
+    elif kind == "descending":
+        gat = (n - 1 - i) % t
+    elif kind == "bad":
+        gat = np.where(i % 1000 < 300, i % t, np.where(i % 2 == 0, -1 - i, t + i))
+    else:
+        gat = i // 2 % t
+    off, tok = vcs.gather_inverse(*dev(gat), t, check=False)
+    key = np.where((gat < 0) | (gat >= t), t, gat)
+    order = np.argsort(key, kind="stable")
+    assert np.array_equal(tok.cpu().numpy(), order)
+    assert np.array_equal(off.cpu().numpy(), np.searchsorted(key[order], np.arange(t + 1)))
+
+
 def test_inverse_of_a_layout_and_bad_entries():
     vcs = _vcs()
     cu, img, txt = random_steps(3)
