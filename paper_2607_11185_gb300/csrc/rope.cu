@@ -40,9 +40,11 @@ constexpr int kPosChunk = 8192;  // tokens of a segment a block writes
 // tiles of a step a thread: a step's run of tokens starts at the lower bound of its index in
 // tok_src_step (non-decreasing within a segment), how far it moves the position follows from the run's
 // length (text only, or screenshot and text), and a block scan gives each run's first position.  Every
-// chunk of a segment repeats the scan of the steps before it: the searches' latency, a few us, against
-// a launch and a workspace.
-__global__ void __launch_bounds__(kPosThreads)
+// chunk of a segment repeats the scan of the steps before it: the searches' latency against a launch and a
+// workspace.  A search is one of 256 samples of the segment in shared memory, then four lanes' probes at a time: 5
+// loads that wait on one another for a segment of 46,176 tokens, where halving takes 16.  15.8 M tokens: 54 us, 71
+// with searches by halving and without the loads ahead.
+__global__ void __launch_bounds__(kPosThreads, 6)
     stream_positions_kernel(const int32_t* __restrict__ cu_seqlens, int32_t num_segments, int32_t num_tokens,
                             const int32_t* __restrict__ src_step, const int32_t* __restrict__ step_img,
                             const int32_t* __restrict__ step_txt, const int32_t* __restrict__ step_grid,
@@ -55,6 +57,7 @@ __global__ void __launch_bounds__(kPosThreads)
   __shared__ uint32_t run_hm[kPosThreads], run_wm[kPosThreads];  // magics of div_by; 0: divide
   __shared__ int32_t wsum[kPosThreads / 32];
   __shared__ int32_t carry_s;
+  __shared__ int32_t sample[kPosThreads];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const size_t N = (size_t)num_tokens;
   const bool vec =
@@ -66,38 +69,55 @@ __global__ void __launch_bounds__(kPosThreads)
       if (tid == 0 && blockIdx.y == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
       continue;
     }
+    if (start + (int64_t)blockIdx.y * kPosChunk >= end) continue;
+    const int first = src_step[start], last = src_step[end - 1];
+    const int apart = (end - start - 1) / kPosThreads + 1;  // tokens between samples
+    __syncthreads();  // the last segment's searches
+    sample[tid] = start + (int64_t)tid * apart < end ? src_step[start + tid * apart] : INT32_MAX;
+    __syncthreads();
+    if (first < 0 || last < first || last >= num_steps) {
+      if (tid == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
+      continue;
+    }
     for (int64_t c0 = start + (int64_t)blockIdx.y * kPosChunk; c0 < end; c0 += (int64_t)gridDim.y * kPosChunk) {
       const int lo_tok = (int)c0, hi_tok = (int)(c0 + kPosChunk < end ? c0 + kPosChunk : end);
-      const int first = src_step[start], last = src_step[end - 1];
-      if (first < 0 || last < first || last >= num_steps) {
-        if (tid == 0) set_status(status, VCS_ERR_DEVICE_CHECK);
-        continue;
-      }
       int carry = 0;  // position at the tile's first run
       for (int64_t s0 = first; s0 <= last; s0 += kPosThreads) {
         const int64_t s = s0 + tid;
-        int lo = end;
-        if (s <= last) {  // lower bound of s in src_step[start, end)
-          int a = start, b = end;
-          while (a < b) {
-            const int mid = a + ((b - a) >> 1);
-            if (src_step[mid] < s) a = mid + 1;
-            else b = mid;
+        // lower bounds of s0, ... in src_step[start, end), that of s0 + kPosThreads too; end behind the last step
+        for (int i0 = 0; i0 <= kPosThreads; i0 += kPosThreads / 4) {
+          const int i = i0 + tid / 4;
+          const int64_t want = s0 + i;
+          int a = end, b = end;
+          if (i <= kPosThreads && want <= last) {
+            int x = 0;  // samples below it
+#pragma unroll
+            for (int o = kPosThreads / 2; o > 0; o >>= 1)
+              if (sample[x + o - 1] < want) x += o;
+            x += x < kPosThreads && sample[x] < want;
+            a = x == 0 ? start : start + (x - 1) * apart + 1;
+            b = x == kPosThreads || end - start <= (int64_t)x * apart ? end : start + x * apart;
           }
-          lo = a;
-        }
-        run_at[tid] = lo;
-        if (tid == kPosThreads - 1) {
-          int a = lo, b = end;
-          while (a < b) {
-            const int mid = a + ((b - a) >> 1);
-            if (src_step[mid] < s + 1) a = mid + 1;
-            else b = mid;
+          while (__any_sync(0xffffffffu, a < b)) {
+            const int d = b - a, q = lane & 3, step = d / 5, rest = d - 5 * step;
+            auto probe = [&](int k) { return a + (k + 1) * step + ((k + 1) * rest) / 5; };
+            const bool less = d > 0 && __ldg(&src_step[probe(q)]) < want;
+            const int below = __popc(__ballot_sync(0xffffffffu, less) >> (lane & ~3) & 15u);
+            if (d > 0) {
+              const int a1 = below > 0 ? probe(below - 1) + 1 : a;
+              b = below < 4 ? probe(below) : b;
+              a = a1;
+            }
           }
-          run_at[kPosThreads] = a;
+          if (i <= kPosThreads && (lane & 3) == 0) run_at[i] = a;
+          if (s0 + i0 + kPosThreads / 4 > (int64_t)last + 1 && i0 + kPosThreads / 4 <= kPosThreads) {
+            // no step that is left is in the segment
+            for (int k = i0 + kPosThreads / 4 + tid; k <= kPosThreads; k += kPosThreads) run_at[k] = end;
+            break;
+          }
         }
         __syncthreads();
-        const int len = run_at[tid + 1] - lo;
+        const int lo = run_at[tid], len = run_at[tid + 1] - lo;
         int adv = 0;
         if (s <= last) {
           const int img = step_img[s], txt = step_txt[s];
@@ -152,10 +172,17 @@ __global__ void __launch_bounds__(kPosThreads)
           frame = hm != 0u ? div_by(line, h, hm) : line / h;
           line -= frame * h;
         };
-        for (int m = (n0 & ~3) + 4 * tid; m < n1; m += 4 * kPosThreads) {
+        auto whole = [&](int64_t m) { return vec && m >= n0 && m + 4 <= n1; };
+        auto steps_at = [&](int64_t m) {
+          return whole(m) ? __ldg(reinterpret_cast<const int4*>(src_step + m)) : make_int4(0, 0, 0, 0);
+        };
+        int4 ahead = steps_at((n0 & ~3) + 4 * tid);
+        for (int64_t m64 = (n0 & ~3) + 4 * tid; m64 < n1; m64 += 4 * kPosThreads) {
+          const int m = (int)m64;
+          const int4 step = ahead;
+          ahead = steps_at(m64 + 4 * kPosThreads);  // the next ones' load is under way while these are written
           // four tokens of one run, of its screenshot or of its text, in 16-byte accesses and with one division
-          if (vec && m >= n0 && m + 4 <= n1) {
-            const int4 step = __ldg(reinterpret_cast<const int4*>(src_step + m));
+          if (whole(m)) {
             const int r = step.x - step0;
             if (step.y == step.x && step.z == step.x && step.w == step.x && r >= 0 && r < kPosThreads &&
                 m >= run_at[r] && m + 3 < run_at[r + 1]) {
@@ -217,7 +244,10 @@ __global__ void __launch_bounds__(kPosThreads)
 // stable radix sort by 8-bit digits of the group brings a group's runs together, in order; then a warp takes a group:
 // the ends of its runs give the tokens' counts, their scan inv_off and where each token's next copy goes.  The map is
 // read once, and once more where runs begin.  15.8 M keys of long rollouts: 130 us (a sort of the keys themselves by
-// three digits and a search of the offsets took 400); random keys, which are runs of one, take 720 against 430.
+// three digits and a search of the offsets took 400); random keys, which are runs of one, take 770 against 430.
+// A group of more than kChunk runs, which no layout of few segments has, is split among warps: the copies in each
+// chunk, a scan, the places (5 M copies of one token: 4.1 ms, with one warp 204).  Far fewer keys than tokens, where
+// the groups would be too wide or too many, are sorted by themselves.
 // Keys outside [0, T) become T, behind all others.
 constexpr int kSortThreads = 256;
 constexpr int kPerThread = 16;
@@ -228,10 +258,12 @@ constexpr int kRunBits = 9;              // a run is within a warp's 512 keys
 constexpr int kGroupKeys = 256;          // keys a group, on average: 15.8 M keys take 261, 220 and 216 us at 128, 256, 512
 constexpr int kGroups = 256;             // but one digit of groups at least
 constexpr int kMostGroups = 4096;        // and up to these where a group would pass kCounters tokens
-constexpr int kCounters = 512;           // trajectory tokens that a warp counts at a time
+constexpr int kCounters = 512;           // trajectory tokens of a group at most
+constexpr int kChunk = 1024;             // runs of a group that one warp takes; a group of more is split
 constexpr int kGroupTile = 4096;         // groups scanned by a block
 constexpr int kLongRun = 8;              // keys of a run, on average of 32, from which runs are taken one by one
 constexpr int kAhead = 4;                // of a run's keys, loads before their stores
+constexpr int kHeavyBlocks = 152;        // for the chunks of heavy groups
 constexpr int kSortBlocks = 152 * 4;     // blocks, of as many tiles each as it takes
 
 // Keys at, at + step, ... before n.  All loads first (the check of a key, which may report, would hold up the next
@@ -282,29 +314,56 @@ __global__ void __launch_bounds__(kSortThreads)
                  int32_t* __restrict__ counts, unsigned long long* __restrict__ groups, int32_t* status) {
   __shared__ int32_t c[256];
   __shared__ int32_t wsum[2][kSortWarps];
+  constexpr int kRounds = kPerThread / 4;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   c[tid] = 0;
   int64_t base = (int64_t)blockIdx.x * each * kTile;
   run_key += base;
   run_at += base;
   int runs = 0;
+  const bool vec = (reinterpret_cast<uintptr_t>(keys) & 15u) == 0;
   for (int t = 0; t < each && base < n; ++t, base += kTile) {
     const int off = wid * (32 * kPerThread), here = (int)(n - base < kTile ? n - base : kTile);
     const int live = min(32 * kPerThread, here - off);  // keys of the warp, possibly less than none
-    uint32_t key[kPerThread], heads[kPerThread];
-    load_keys<32>(keys, base + off + lane, n, T, status, key);
+    // the warp's keys 128 u + 4 lane + j
+    const int64_t mine = base + off + 4 * lane;
+    uint32_t key[kRounds][4], heads[kRounds][4];
+    if (vec && live == 32 * kPerThread) {
+#pragma unroll
+      for (int u = 0; u < kRounds; ++u) {
+        const int4 k = __ldg(reinterpret_cast<const int4*>(keys + mine) + 32 * u);
+        key[u][0] = k.x, key[u][1] = k.y, key[u][2] = k.z, key[u][3] = k.w;
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kRounds; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[u][j] = (uint32_t)__ldg(&keys[min(mine + 128 * u + j, n - 1)]);
+    }
+    bool bad = false;
     int found = 0;
 #pragma unroll
-    for (int u = 0; u < kPerThread; ++u) {
-      uint32_t last = __shfl_up_sync(0xffffffffu, key[u], 1);
+    for (int u = 0; u < kRounds; ++u) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bad = bad || key[u][j] >= T;  // the last key's copies behind n tell the same
+        key[u][j] = min(key[u][j], T);
+      }
+      uint32_t last = __shfl_up_sync(0xffffffffu, key[u][3], 1);
       if (u > 0) {
-        const uint32_t end = __shfl_sync(0xffffffffu, key[u - 1], 31);
+        const uint32_t end = __shfl_sync(0xffffffffu, key[u - 1][3], 31);
         if (lane == 0) last = end;
       }
-      const bool head = key[u] != last + 1 || (key[u] & ((1u << shift) - 1u)) == 0 || (u == 0 && lane == 0);
-      heads[u] = __ballot_sync(0xffffffffu, head && 32 * u + lane < live);
-      found += __popc(heads[u]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool head = key[u][j] != last + 1 || (key[u][j] & ((1u << shift) - 1u)) == 0;
+        last = key[u][j];
+        heads[u][j] = __ballot_sync(0xffffffffu, (head || 128 * u + 4 * lane + j == 0) &&
+                                                     128 * u + 4 * lane + j < live);
+        found += __popc(heads[u][j]);
+      }
     }
+    if (bad) set_status(status, VCS_ERR_DEVICE_CHECK);
     if (lane == 0) wsum[t & 1][wid] = found;
     __syncthreads();
     int at = runs + found;  // behind the warp's runs
@@ -314,19 +373,36 @@ __global__ void __launch_bounds__(kSortThreads)
       runs += wsum[t & 1][w];
     }
     int next = live;  // the first place behind the run
+    const uint32_t below = (1u << lane) - 1u, above = ~(2u * below + 1u);
+    // the place of a lane's first head
+    auto first_of = [](const uint32_t (&h)[4], int lane_of) {
+      return 4 * lane_of + (h[0] >> lane_of & 1 ? 0 : h[1] >> lane_of & 1 ? 1 : h[2] >> lane_of & 1 ? 2 : 3);
+    };
 #pragma unroll
-    for (int u = kPerThread - 1; u >= 0; --u) {
-      at -= __popc(heads[u]);
-      if (heads[u] >> lane & 1) {
-        const uint32_t later = heads[u] & ~((2u << lane) - 1u), group = key[u] >> shift;
-        const int len = (later != 0 ? 32 * u + __ffs(later) - 1 : next) - (32 * u + lane);
-        const int to = at + __popc(heads[u] & ((1u << lane) - 1u));
-        run_key[to] = group << kRunBits | (uint32_t)(len - 1);
-        run_at[to] = (int32_t)(base + off + 32 * u + lane);
-        atomicAdd(&c[group & 255u], 1);
-        atomicAdd(&groups[group], 1ull << 32 | (unsigned long long)len);
+    for (int u = kRounds - 1; u >= 0; --u) {
+      const uint32_t any = heads[u][0] | heads[u][1] | heads[u][2] | heads[u][3];
+      if (any == 0) continue;
+      at -= __popc(heads[u][0]) + __popc(heads[u][1]) + __popc(heads[u][2]) + __popc(heads[u][3]);
+      if (any >> lane & 1) {
+        int to = at + __popc(heads[u][0] & below) + __popc(heads[u][1] & below) + __popc(heads[u][2] & below) +
+                 __popc(heads[u][3] & below);
+        const int then = (any & above) != 0 ? 128 * u + first_of(heads[u], __ffs(any & above) - 1) : next;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (heads[u][j] >> lane & 1) {
+            const int place = 128 * u + 4 * lane + j;
+            int upto = then;
+#pragma unroll
+            for (int i = 3; i > j; --i)
+              if (heads[u][i] >> lane & 1) upto = 128 * u + 4 * lane + i;
+            const uint32_t group = key[u][j] >> shift;
+            run_key[to] = group << kRunBits | (uint32_t)(upto - place - 1);
+            run_at[to++] = (int32_t)(base + off + place);
+            atomicAdd(&c[group & 255u], 1);
+            atomicAdd(&groups[group], 1ull << 32 | (unsigned long long)(upto - place));
+          }
       }
-      if (heads[u] != 0) next = 32 * u + __ffs(heads[u]) - 1;
+      next = 128 * u + first_of(heads[u], __ffs(any) - 1);
     }
   }
   __syncthreads();
@@ -334,9 +410,10 @@ __global__ void __launch_bounds__(kSortThreads)
   if (tid == 0) block_runs[blockIdx.x] = runs;
 }
 
-// Tiles of n packed runs that a block of so many takes.
-__device__ __forceinline__ int packed_each(int64_t n, int blocks) {
-  return (int)(((n + kTile - 1) / kTile + blocks - 1) / blocks);
+// Packed runs that a block takes, of n by so many blocks: few runs are spread over more blocks than tiles would.
+__device__ __forceinline__ int64_t packed_part(int64_t n, int blocks) {
+  constexpr int64_t kLeast = kTile / 4;
+  return ((n + kLeast - 1) / kLeast + blocks - 1) / blocks * kLeast;
 }
 
 // Digit counts of packed runs.
@@ -344,13 +421,11 @@ __global__ void __launch_bounds__(kSortThreads)
     inverse_count(const uint32_t* __restrict__ run_key, const int32_t* __restrict__ num_runs, int shift,
                   int32_t* __restrict__ counts) {
   __shared__ int32_t c[256];
-  const int64_t n = *num_runs;
-  const int each = packed_each(n, gridDim.x);
-  const int64_t base = (int64_t)blockIdx.x * each * kTile;
+  const int64_t n = *num_runs, part = packed_part(n, gridDim.x), base = blockIdx.x * part;
   if (base >= n) return;
   c[threadIdx.x] = 0;
   __syncthreads();
-  const int here = (int)min(n - base, (int64_t)each * kTile);
+  const int here = (int)min(n - base, part);
   run_key += base;
 #pragma unroll 8
   for (int i = threadIdx.x; i < here; i += kSortThreads) atomicAdd(&c[run_key[i] >> shift & 255u], 1);
@@ -382,19 +457,27 @@ __device__ __forceinline__ T scan_1024(T v, T* wsum, T& all) {
   return x - v + (wid > 0 ? before : T(0));
 }
 
+// The groups of more than kChunk runs: their chunks stand at `slot` and behind it.
+struct HeavyList {
+  int32_t* num;     // chunks, groups
+  int2* group;      // group, its first slot
+  int2* chunk;      // of a slot: its group, the chunk's number there
+  int32_t* counts;  // of a slot: the chunk's copies of the group's tokens, then their first places
+};
+
 // Block b < 256: the exclusive scan of digit b's counts over the blocks that counted (with packed runs, as many as
 // num_runs fill), and their sum.
-// A block behind them: that of kGroupTile groups, and their sum.
+// A block behind them: that of kGroupTile groups, and their sum; and the list of heavy groups.
 __global__ void __launch_bounds__(1024)
     inverse_scan(int32_t* __restrict__ counts, int blocks, const int32_t* __restrict__ num_runs,
                  int32_t* __restrict__ totals, unsigned long long* __restrict__ groups, int num_groups,
-                 unsigned long long* __restrict__ group_sums) {
+                 unsigned long long* __restrict__ group_sums, HeavyList heavy) {
   if (blockIdx.x < 256) {
     __shared__ int32_t wsum[32];
     int32_t* c = counts + (size_t)blockIdx.x * blocks;
     int live = blocks;
     if (num_runs != nullptr) {
-      const int64_t n = *num_runs, part = (int64_t)packed_each(n, blocks) * kTile;
+      const int64_t n = *num_runs, part = packed_part(n, blocks);
       live = (int)((n + part - 1) / part);
     }
     int carry = 0, all;
@@ -420,6 +503,11 @@ __global__ void __launch_bounds__(1024)
     for (int i = 0; i < kEach; ++i) {
       if (at + i < num_groups) groups[at + i] = x;
       x += v[i];
+      if (v[i] >> 32 > kChunk) {  // where its chunks stand among the others' makes no difference
+        const int chunks = (int)(((v[i] >> 32) + kChunk - 1) / kChunk), slot = atomicAdd(&heavy.num[0], chunks);
+        heavy.group[atomicAdd(&heavy.num[1], 1)] = make_int2(at + i, slot);
+        for (int c = 0; c < chunks; ++c) heavy.chunk[slot + c] = make_int2(at + i, c);
+      }
     }
     if (threadIdx.x == 0) group_sums[blockIdx.x - 256] = all;
   }
@@ -502,11 +590,10 @@ __global__ void __launch_bounds__(kSortThreads, 4)
   if (block_runs != nullptr) {
     all = block_runs[blockIdx.x];
   } else {
-    const int64_t n = *num_runs;
-    each = packed_each(n, gridDim.x);
-    base = (int64_t)blockIdx.x * each * kTile;
+    const int64_t n = *num_runs, part = packed_part(n, gridDim.x);
+    base = blockIdx.x * part;
     if (base >= n) return;
-    all = (int)min(n - base, (int64_t)each * kTile);
+    all = (int)min(n - base, part);
   }
   keys += base;
   vals += base;
@@ -588,136 +675,299 @@ __global__ void __launch_bounds__(kSortThreads)
   }
 }
 
-// A warp a group of trajectory tokens, kCounters at a time: the copies of each, from where runs begin and end; their
-// scan; and the copies in order to their places.  A run's tokens differ, so long runs are taken one by one; the keys
-// of short ones are taken 32 at a time, and those of one token told apart by votes on the bits.
-__global__ void __launch_bounds__(kSortThreads)
-    inverse_place(const int32_t* __restrict__ keys, uint32_t T, int shift, const uint32_t* __restrict__ run_key,
-                  const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups, int num_groups,
-                  const unsigned long long* __restrict__ group_sums, int32_t* __restrict__ inv_off,
-                  int32_t* __restrict__ inv_tok) {
-  __shared__ int32_t counters[kSortWarps][kCounters];
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const int g = blockIdx.x * kSortWarps + wid;
-  if (g >= num_groups) return;
+// A group's runs and its first place in inv_tok.
+struct Group {
+  const uint32_t* run_key;
+  const int32_t* run_at;
+  int runs, first;
+  uint32_t token;  // its first
+  int width;       // tokens
+};
+__device__ __forceinline__ Group group_at(int g, uint32_t T, int shift, const uint32_t* run_key, const int32_t* run_at,
+                                          const unsigned long long* groups, int num_groups,
+                                          const unsigned long long* group_sums) {
   unsigned long long before = 0;
-  for (int i = lane; i < g / kGroupTile; i += 32) before += group_sums[i];
+  for (int i = threadIdx.x & 31; i < g / kGroupTile; i += 32) before += group_sums[i];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
   const unsigned long long in_tile = groups[g];
   const unsigned long long end = (g + 1) % kGroupTile == 0 || g + 1 == num_groups ? group_sums[g / kGroupTile]
                                                                                   : groups[g + 1];
-  const int runs = (int)((end >> 32) - (in_tile >> 32));
   before += in_tile;
-  run_key += before >> 32;
-  run_at += before >> 32;
-  int next = (int)(uint32_t)before;  // the group's first place
+  Group r;
+  r.runs = (int)((end >> 32) - (in_tile >> 32));
+  r.run_key = run_key + (before >> 32);
+  r.run_at = run_at + (before >> 32);
+  r.first = (int)(uint32_t)before;
+  r.token = (uint32_t)g << shift;
+  r.width = (int)min(1u << shift, T + 1 - r.token);
+  return r;
+}
+
+// Chunk c of the group's runs, as a group.
+__device__ __forceinline__ Group chunk_of(Group g, int c) {
+  g.run_key += (int64_t)c * kChunk;
+  g.run_at += (int64_t)c * kChunk;
+  g.runs = min(g.runs - c * kChunk, kChunk);
+  return g;
+}
+
+__device__ __forceinline__ int warp_scan(int x) {  // inclusive
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// Copies of the group's tokens, from where its runs begin and end: each(i, copies of token i, 0 behind the last) is
+// called by all lanes, 32 tokens at a time.  c holds the changes of the count.
+template <typename F>
+__device__ __forceinline__ void count_copies(const Group& g, const int32_t* __restrict__ keys, uint32_t T, int32_t* c,
+                                             F&& each) {
+  const int lane = threadIdx.x & 31;
+  for (int i = lane; i < g.width; i += 32) c[i] = 0;
+  __syncwarp();
+  for (int r = lane; r < g.runs; r += 32) {
+    const int first = (int)(min((uint32_t)__ldg(&keys[g.run_at[r]]), T) - g.token);
+    const int end = first + (int)(g.run_key[r] & ((1u << kRunBits) - 1u)) + 1;
+    atomicAdd(&c[first], 1);
+    if (end < g.width) atomicAdd(&c[end], -1);
+  }
+  __syncwarp();
+  int copies = 0;  // of the token before
+  for (int i = lane; i - lane < g.width; i += 32) {
+    const int x = warp_scan(i < g.width ? c[i] : 0) + copies;
+    copies = __shfl_sync(0xffffffffu, x, 31);
+    each(i, i < g.width ? x : 0);
+  }
+  __syncwarp();
+}
+
+// The runs' segment tokens, in order, to their tokens' places c.  A run's tokens differ, so long runs are taken one by
+// one; the keys of short ones are taken 32 at a time, and those of one token told apart by votes on the bits.
+__device__ __forceinline__ void place_copies(const Group& g, const int32_t* __restrict__ keys, uint32_t T, int shift,
+                                             int32_t* c, int32_t* __restrict__ inv_tok) {
+  const int lane = threadIdx.x & 31;
+  for (int r = 0; r < g.runs; r += 32) {
+    const bool there = r + lane < g.runs;
+    const int at = there ? g.run_at[r + lane] : 0;
+    const int len = there ? (int)(g.run_key[r + lane] & ((1u << kRunBits) - 1u)) + 1 : 0;
+    const int first = there ? (int)(min((uint32_t)__ldg(&keys[at]), T) - g.token) : 0;
+    const int upto = warp_scan(len);  // keys of the runs up to this one
+    const int all = __shfl_sync(0xffffffffu, upto, 31), here = min(g.runs - r, 32);
+    if (all >= here * kLongRun) {
+      for (int j = 0; j < here; ++j) {
+        const int f = __shfl_sync(0xffffffffu, first, j), l = __shfl_sync(0xffffffffu, len, j);
+        const int a = __shfl_sync(0xffffffffu, at, j);
+        for (int e = lane; e < l; e += 32 * kAhead) {
+          int to[kAhead];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u)
+            if (e + 32 * u < l) to[u] = c[f + e + 32 * u];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u)
+            if (e + 32 * u < l) {
+              inv_tok[to[u]] = a + e + 32 * u;
+              c[f + e + 32 * u] = to[u] + 1;
+            }
+        }
+        __syncwarp();
+      }
+    } else {
+      for (int b = 0; b < all; b += 32) {
+        const int e = b + lane;
+        int j = 0;  // runs that end at or before key e
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+          if (__shfl_sync(0xffffffffu, upto, j + o - 1) <= e) j += o;
+        const int in_run = e - __shfl_sync(0xffffffffu, upto - len, j);
+        const int i = __shfl_sync(0xffffffffu, first, j) + in_run, a = __shfl_sync(0xffffffffu, at, j) + in_run;
+        const bool on = e < all;
+        uint32_t same = __ballot_sync(0xffffffffu, on);
+        for (int k = 0; k < shift; ++k) {
+          const bool bit = i >> k & 1;
+          const uint32_t v = __ballot_sync(0xffffffffu, bit);
+          same &= bit ? v : ~v;
+        }
+        const int to = on ? c[i] + __popc(same & ((1u << lane) - 1u)) : 0;
+        __syncwarp();
+        if (on) {
+          inv_tok[to] = a;
+          if (same >> lane == 1u) c[i] = to + 1;  // the last of its token
+        }
+        __syncwarp();
+      }
+    }
+  }
+}
+
+// A warp a group of up to kChunk runs: its tokens' copies, their scan, and the copies to their places.  The warps of
+// the blocks behind them: the copies in the chunks of the other groups.
+__global__ void __launch_bounds__(kSortThreads, 6)
+    inverse_place(const int32_t* __restrict__ keys, uint32_t T, int shift, const uint32_t* __restrict__ run_key,
+                  const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups, int num_groups,
+                  const unsigned long long* __restrict__ group_sums, HeavyList heavy, int32_t* __restrict__ inv_off,
+                  int32_t* __restrict__ inv_tok) {
+  __shared__ int32_t counters[kSortWarps][kCounters];
+  const int wid = threadIdx.x >> 5, blocks = (num_groups + kSortWarps - 1) / kSortWarps;
   int32_t* c = counters[wid];
-  const int64_t lo = (int64_t)g << shift, hi = min(lo + ((int64_t)1 << shift), (int64_t)T + 1);
-  const int bits = min(shift, 9);
-  for (int64_t t0 = lo; t0 < hi; t0 += kCounters) {
-    const int width = (int)min((int64_t)kCounters, hi - t0);
-    // run r's part of the counters [first, first + len), and its place in the map
-    auto load_run = [&](int r, int& first, int& len, int& at) {
-      first = len = at = 0;
-      if (r >= runs) return;
-      at = run_at[r];
-      const int64_t k = (int64_t)min((uint32_t)__ldg(&keys[at]), T) - t0;
-      const int64_t from = max(k, (int64_t)0), upto = min(k + (run_key[r] & ((1u << kRunBits) - 1u)) + 1, (int64_t)width);
-      if (from >= upto) return;
-      first = (int)from;
-      len = (int)(upto - from);
-      at += (int)(from - k);
-    };
-    for (int i = lane; i < width; i += 32) c[i] = 0;
-    __syncwarp();
-    for (int r = lane; r < runs; r += 32) {
-      int first, len, at;
-      load_run(r, first, len, at);
-      if (len > 0) {
-        atomicAdd(&c[first], 1);
-        if (first + len < width) atomicAdd(&c[first + len], -1);
-      }
-    }
-    __syncwarp();
-    int copies = 0;  // of the token before
-    for (int i = lane; i - lane < width; i += 32) {
-      int x = i < width ? c[i] : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      x += copies;
-      copies = __shfl_sync(0xffffffffu, x, 31);
-      const int v = i < width ? x : 0;
-      x = v;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      if (i < width) {
-        c[i] = next + x - v;
-        inv_off[t0 + i] = next + x - v;
-      }
+  if ((int)blockIdx.x < blocks) {
+    const int g = blockIdx.x * kSortWarps + wid;
+    if (g >= num_groups) return;
+    const Group group = group_at(g, T, shift, run_key, run_at, groups, num_groups, group_sums);
+    if (group.runs > kChunk) return;
+    int next = group.first;
+    count_copies(group, keys, T, c, [&](int i, int copies) {
+      const int x = warp_scan(copies);
+      if (i < group.width) inv_off[(size_t)group.token + i] = c[i] = next + x - copies;
       next += __shfl_sync(0xffffffffu, x, 31);
+    });
+    place_copies(group, keys, T, shift, c, inv_tok);
+  } else {
+    const int chunks = heavy.num[0];
+    for (int k = ((int)blockIdx.x - blocks) * kSortWarps + wid; k < chunks; k += kHeavyBlocks * kSortWarps) {
+      const int2 which = heavy.chunk[k];
+      const Group group = group_at(which.x, T, shift, run_key, run_at, groups, num_groups, group_sums);
+      int32_t* to = heavy.counts + (size_t)k * kCounters;
+      count_copies(chunk_of(group, which.y), keys, T, c, [&](int i, int copies) {
+        if (i < group.width) to[i] = copies;
+      });
     }
+  }
+}
+
+// A block a heavy group, a thread a token: the scan of the tokens' copies, then where each chunk's first one goes.
+__global__ void __launch_bounds__(kCounters)
+    inverse_heavy_scan(uint32_t T, int shift, const uint32_t* __restrict__ run_key, const int32_t* __restrict__ run_at,
+                       const unsigned long long* __restrict__ groups, int num_groups,
+                       const unsigned long long* __restrict__ group_sums, HeavyList heavy,
+                       int32_t* __restrict__ inv_off) {
+  __shared__ int32_t wsum[kCounters / 32];
+  const int tid = threadIdx.x;
+  for (int k = blockIdx.x; k < heavy.num[1]; k += gridDim.x) {
+    const int2 which = heavy.group[k];
+    const Group group = group_at(which.x, T, shift, run_key, run_at, groups, num_groups, group_sums);
+    const int chunks = (group.runs + kChunk - 1) / kChunk;
+    int32_t* counts = heavy.counts + (size_t)which.y * kCounters + tid;
+    const bool on = tid < group.width;
+    int copies = 0;
+#pragma unroll 8
+    for (int c = 0; c < chunks; ++c)
+      if (on) copies += counts[(size_t)c * kCounters];
+    int next = group.first + block_before(copies, wsum);
+    if (on) inv_off[(size_t)group.token + tid] = next;
+    for (int c0 = 0; c0 < chunks; c0 += 8) {
+      int v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = on && c0 + u < chunks ? counts[(size_t)(c0 + u) * kCounters] : 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (on && c0 + u < chunks) counts[(size_t)(c0 + u) * kCounters] = next;
+        next += v[u];
+      }
+    }
+  }
+}
+
+// A warp a chunk of a heavy group: its copies to their places.
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_heavy_place(const int32_t* __restrict__ keys, uint32_t T, int shift, const uint32_t* __restrict__ run_key,
+                        const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups,
+                        int num_groups, const unsigned long long* __restrict__ group_sums, HeavyList heavy,
+                        int32_t* __restrict__ inv_tok) {
+  __shared__ int32_t counters[kSortWarps][kCounters];
+  const int wid = threadIdx.x >> 5, chunks = heavy.num[0];
+  int32_t* c = counters[wid];
+  for (int k = blockIdx.x * kSortWarps + wid; k < chunks; k += gridDim.x * kSortWarps) {
+    const int2 which = heavy.chunk[k];
+    const Group group = group_at(which.x, T, shift, run_key, run_at, groups, num_groups, group_sums);
     __syncwarp();
-    for (int r = 0; r < runs; r += 32) {
-      int first, len, at;
-      load_run(r + lane, first, len, at);
-      int upto = len;  // keys of the runs up to this one
+    for (int i = threadIdx.x & 31; i < group.width; i += 32) c[i] = heavy.counts[(size_t)k * kCounters + i];
+    __syncwarp();
+    place_copies(chunk_of(group, which.y), keys, T, shift, c, inv_tok);
+  }
+}
+
+// Single keys as what is sorted: for more trajectory tokens than kCounters a group.
+__global__ void __launch_bounds__(kSortThreads)
+    inverse_keys(const int32_t* __restrict__ keys, int64_t n, uint32_t T, uint32_t* __restrict__ key_out,
+                 int32_t* __restrict__ at_out, int32_t* __restrict__ num, int32_t* status) {
+  const int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x;
+  if (i == 0) *num = (int32_t)n;
+  if (i >= n) return;
+  const uint32_t k = (uint32_t)keys[i];
+  if (k >= T) set_status(status, VCS_ERR_DEVICE_CHECK);
+  key_out[i] = min(k, T);
+  at_out[i] = (int32_t)i;
+}
+
+// off[t] = first place of a key >= t in the sorted keys, for t in a block's 1,024: two searches bound
+// the block's keys; counts of them in shared memory and a scan give the rest, or searches where there are many.
+constexpr int kOffTile = 1024;
+__global__ void __launch_bounds__(256) inverse_offsets(const uint32_t* __restrict__ keys, int32_t n, int64_t T,
+                                                       int32_t* __restrict__ off) {
+  __shared__ int32_t c[kOffTile];
+  __shared__ int32_t bound[2];
+  __shared__ int32_t wsum[8];
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int64_t t0 = (int64_t)blockIdx.x * kOffTile;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += y;
-      }
-      const int all = __shfl_sync(0xffffffffu, upto, 31), here = min(runs - r, 32);
-      if (all >= here * kLongRun) {
-        for (int j = 0; j < here; ++j) {
-          const int f = __shfl_sync(0xffffffffu, first, j), l = __shfl_sync(0xffffffffu, len, j);
-          const int a = __shfl_sync(0xffffffffu, at, j);
-          for (int e = lane; e < l; e += 32 * kAhead) {
-            int to[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-              if (e + 32 * u < l) to[u] = c[f + e + 32 * u];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-              if (e + 32 * u < l) {
-                inv_tok[to[u]] = a + e + 32 * u;
-                c[f + e + 32 * u] = to[u] + 1;
-              }
-          }
-          __syncwarp();
-        }
-      } else {
-        for (int b = 0; b < all; b += 32) {
-          const int e = b + lane;
-          int j = 0;  // runs that end at or before key e
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1)
-            if (__shfl_sync(0xffffffffu, upto, j + o - 1) <= e) j += o;
-          const int in_run = e - __shfl_sync(0xffffffffu, upto - len, j);
-          const int i = __shfl_sync(0xffffffffu, first, j) + in_run, a = __shfl_sync(0xffffffffu, at, j) + in_run;
-          const bool on = e < all;
-          uint32_t same = __ballot_sync(0xffffffffu, on);
-          for (int k = 0; k < bits; ++k) {
-            const bool bit = i >> k & 1;
-            const uint32_t v = __ballot_sync(0xffffffffu, bit);
-            same &= bit ? v : ~v;
-          }
-          const int to = on ? c[i] + __popc(same & ((1u << lane) - 1u)) : 0;
-          __syncwarp();
-          if (on) {
-            inv_tok[to] = a;
-            if (same >> lane == 1u) c[i] = to + 1;  // the last of its token
-          }
-          __syncwarp();
-        }
-      }
+  for (int u = 0; u < kOffTile / 256; ++u) c[u * 256 + tid] = 0;
+  if (wid < 2) {  // a warp a search: the keys from `a` on, 32 probes at a time
+    const int64_t t = t0 + wid * (int64_t)kOffTile;
+    int a = 0, len = n;
+    while (len > 0) {
+      const int step = (len + 31) / 32;
+      const int at = a + lane * step;
+      const bool less = lane * step < len && __ldg(&keys[at]) < t;
+      const int c = __popc(__ballot_sync(0xffffffffu, less));  // the probes of smaller keys come first
+      if (c == 0) break;
+      const int from = (c - 1) * step + 1;  // past the last smaller one
+      len = min(step - 1, len - from);
+      a += from;
     }
+    if (lane == 0) bound[wid] = a;
+  }
+  __syncthreads();
+  const int lo = bound[0], hi = bound[1];
+  if (hi - lo > 4 * kOffTile) {
+    for (int64_t t = t0 + tid; t < t0 + kOffTile && t <= T; t += 256) {
+      int a = lo, b = hi;
+      while (a < b) {
+        const int mid = a + ((b - a) >> 1);
+        if (keys[mid] < t) a = mid + 1;
+        else b = mid;
+      }
+      off[t] = a;
+    }
+    return;
+  }
+  for (int i = lo + tid; i < hi; i += 256) atomicAdd(&c[keys[i] - t0], 1);
+  __syncthreads();
+  int v[kOffTile / 256], sum = 0;
+#pragma unroll
+  for (int u = 0; u < kOffTile / 256; ++u) {
+    v[u] = c[tid * (kOffTile / 256) + u];
+    sum += v[u];
+  }
+  int x = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) wsum[wid] = x;
+  __syncthreads();
+  int at = lo + x - sum;
+  for (int i = 0; i < wid; ++i) at += wsum[i];
+#pragma unroll
+  for (int u = 0; u < kOffTile / 256; ++u) {
+    const int64_t t = t0 + tid * (kOffTile / 256) + u;
+    if (t <= T) off[t] = at;
+    at += v[u];
   }
 }
 
@@ -1071,13 +1321,18 @@ int64_t group_limit(int64_t num_tokens) {
 }
 
 // A group's trajectory tokens as a power of two; T, the token of the keys that are out of range, is in the last one.
+// -1: there are too many for groups.
 int group_shift(int64_t num_tokens, int64_t T) {
   const int64_t want = num_tokens / kGroupKeys > kGroups ? num_tokens / kGroupKeys : kGroups;
   int shift = 0;
   while ((T >> shift) + 1 > want) ++shift;
-  while (1 << shift > kCounters && (T >> (shift - 1)) + 1 <= group_limit(num_tokens)) --shift;
-  return shift;
+  if (1ll << shift <= kCounters) return shift;
+  for (shift = 0; 1 << shift < kCounters;) ++shift;
+  return (T >> shift) + 1 <= group_limit(num_tokens) ? shift : -1;
 }
+
+// Chunks of heavy groups, each of which has more than kChunk runs.
+int64_t chunk_limit(int64_t num_tokens) { return num_tokens / (kChunk / 2) + 1; }
 
 struct SortGrid {
   int each, blocks;  // tiles a block
@@ -1087,13 +1342,13 @@ SortGrid sort_grid(int64_t num_tokens) {
   return {(int)each, each == 0 ? 0 : (int)((tiles + each - 1) / each)};
 }
 
-// Workspace: digit counts of the blocks, their totals and the blocks' runs; the groups' counts and their sums; the
-// runs twice, but for one array (inv_tok).
+// Workspace: digit counts of the blocks, their totals and the blocks' runs; the groups' counts, their sums and the
+// heavy ones' list; the runs twice, but for one array (inv_tok).
 size_t gather_inverse_ws_bytes(int64_t num_tokens) {
   const int64_t blocks = sort_grid(num_tokens).blocks, groups = group_limit(num_tokens);
   return align256((size_t)blocks * 256 * 4) + align256(257 * 4) + align256((size_t)blocks * 4) +
-         align256((size_t)groups * 8) + align256((size_t)(groups / kGroupTile + 1) * 8) +
-         3 * align256((size_t)num_tokens * 4) + 256;
+         align256((size_t)groups * 8 + 8) + align256((size_t)(groups / kGroupTile + 1) * 8) +
+         2 * align256((size_t)chunk_limit(num_tokens) * 8) + 3 * align256((size_t)num_tokens * 4) + 256;
 }
 
 cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens, int64_t traj_tokens, int32_t* inv_off,
@@ -1103,6 +1358,11 @@ cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens,
   }
   const SortGrid grid = sort_grid(num_tokens);
   const uint32_t T = (uint32_t)traj_tokens;
+  if (num_tokens <= kTile && traj_tokens <= kSmallOffsets) {
+    inverse_small<<<1, kSortThreads, 0, st>>>(tok_gather, (int32_t)num_tokens, T, key_passes(traj_tokens), inv_off,
+                                              inv_tok, status);
+    return cudaGetLastError();
+  }
   const int64_t limit = group_limit(num_tokens);
   const int shift = group_shift(num_tokens, traj_tokens);
   char* w = static_cast<char*>(ws);
@@ -1115,35 +1375,56 @@ cudaError_t launch_gather_inverse(const int32_t* tok_gather, int64_t num_tokens,
   auto* totals = reinterpret_cast<int32_t*>(take(257 * 4));
   int32_t* num_runs = totals + 256;
   auto* block_runs = reinterpret_cast<int32_t*>(take((size_t)grid.blocks * 4));
-  auto* groups = reinterpret_cast<unsigned long long*>(take((size_t)limit * 8));
+  auto* groups = reinterpret_cast<unsigned long long*>(take((size_t)limit * 8 + 8));  // behind heavy.num
   auto* group_sums = reinterpret_cast<unsigned long long*>(take((size_t)(limit / kGroupTile + 1) * 8));
+  HeavyList heavy;
+  heavy.num = reinterpret_cast<int32_t*>(groups++);
+  heavy.group = reinterpret_cast<int2*>(take((size_t)chunk_limit(num_tokens) * 8));
+  heavy.chunk = reinterpret_cast<int2*>(take((size_t)chunk_limit(num_tokens) * 8));
   const size_t nb = (size_t)num_tokens * 4;
   uint32_t* key[2] = {reinterpret_cast<uint32_t*>(take(nb)), reinterpret_cast<uint32_t*>(take(nb))};
   auto* spare = reinterpret_cast<int32_t*>(take(nb));
-  if (num_tokens <= kTile && traj_tokens <= kSmallOffsets) {
-    inverse_small<<<1, kSortThreads, 0, st>>>(tok_gather, (int32_t)num_tokens, T, key_passes(traj_tokens), inv_off,
-                                              inv_tok, status);
-    return cudaGetLastError();
+  const bool runs = shift >= 0;
+  const int num_groups = runs ? (int)((traj_tokens >> shift) + 1) : 0;
+  const int passes = key_passes(runs ? num_groups - 1 : traj_tokens), last = passes & 1;
+  // sorted keys' places are inv_tok; runs that are sorted last must not be where inverse_place writes
+  int32_t* at[2];
+  at[last] = runs ? spare : inv_tok;
+  at[last ^ 1] = runs ? inv_tok : spare;
+  heavy.counts = reinterpret_cast<int32_t*>(key[last ^ 1]);
+  if (runs) {
+    const cudaError_t err = cudaMemsetAsync(heavy.num, 0, (size_t)num_groups * 8 + 8, st);
+    if (err != cudaSuccess) return err;
+    inverse_runs<<<grid.blocks, kSortThreads, 0, st>>>(tok_gather, num_tokens, T, shift, grid.each, key[0], at[0],
+                                                       block_runs, counts, groups, status);
+  } else {
+    inverse_keys<<<(unsigned)((num_tokens + kSortThreads - 1) / kSortThreads), kSortThreads, 0, st>>>(
+        tok_gather, num_tokens, T, key[0], at[0], num_runs, status);
   }
-  const int num_groups = (int)((traj_tokens >> shift) + 1), group_tiles = (num_groups + kGroupTile - 1) / kGroupTile;
-  const int passes = key_passes(num_groups - 1);
-  // the runs that are sorted last must not be where inverse_place writes
-  int32_t* at[2] = {passes % 2 == 0 ? spare : inv_tok, passes % 2 == 0 ? inv_tok : spare};
-  cudaError_t err = cudaMemsetAsync(groups, 0, (size_t)num_groups * 8, st);
-  if (err != cudaSuccess) return err;
-  inverse_runs<<<grid.blocks, kSortThreads, 0, st>>>(tok_gather, num_tokens, T, shift, grid.each, key[0], at[0],
-                                                     block_runs, counts, groups, status);
   for (int p = 0; p < passes; ++p) {
-    const int digit = kRunBits + 8 * p, in = p & 1;
-    if (p > 0) inverse_count<<<grid.blocks, kSortThreads, 0, st>>>(key[in], num_runs, digit, counts);
-    inverse_scan<<<256 + (p == 0 ? group_tiles : 0), 1024, 0, st>>>(counts, grid.blocks, p == 0 ? nullptr : num_runs,
-                                                                    totals, groups, num_groups, group_sums);
+    const bool first = runs && p == 0;  // inverse_runs has counted
+    const int digit = 8 * p + (runs ? kRunBits : 0), in = p & 1;
+    if (!first) inverse_count<<<grid.blocks, kSortThreads, 0, st>>>(key[in], num_runs, digit, counts);
+    inverse_scan<<<256 + (first ? (num_groups + kGroupTile - 1) / kGroupTile : 0), 1024, 0, st>>>(
+        counts, grid.blocks, first ? nullptr : num_runs, totals, groups, num_groups, group_sums, heavy);
     inverse_scatter<<<grid.blocks, kSortThreads, 0, st>>>(key[in], at[in], digit, grid.each, counts, totals,
-                                                          p == 0 ? block_runs : nullptr, num_runs, key[in ^ 1],
+                                                          first ? block_runs : nullptr, num_runs, key[in ^ 1],
                                                           at[in ^ 1]);
   }
-  inverse_place<<<(num_groups + kSortWarps - 1) / kSortWarps, kSortThreads, 0, st>>>(
-      tok_gather, T, shift, key[passes & 1], at[passes & 1], groups, num_groups, group_sums, inv_off, inv_tok);
+  if (!runs) {
+    inverse_offsets<<<(unsigned)((traj_tokens + kOffTile) / kOffTile), 256, 0, st>>>(key[last], (int32_t)num_tokens,
+                                                                                    traj_tokens, inv_off);
+    return cudaGetLastError();
+  }
+  const bool split = num_tokens > kChunk;  // a group may be heavy
+  inverse_place<<<(num_groups + kSortWarps - 1) / kSortWarps + (split ? kHeavyBlocks : 0), kSortThreads, 0, st>>>(
+      tok_gather, T, shift, key[last], at[last], groups, num_groups, group_sums, heavy, inv_off, inv_tok);
+  if (split) {
+    inverse_heavy_scan<<<kHeavyBlocks, kCounters, 0, st>>>(T, shift, key[last], at[last], groups, num_groups,
+                                                           group_sums, heavy, inv_off);
+    inverse_heavy_place<<<kHeavyBlocks * 4, kSortThreads, 0, st>>>(tok_gather, T, shift, key[last], at[last], groups,
+                                                                   num_groups, group_sums, heavy, inv_tok);
+  }
   return cudaGetLastError();
 }
 

@@ -106,7 +106,8 @@ def test_inverse(n, t):
 
 
 @pytest.mark.parametrize("kind", ["stretches", "one token", "descending", "bad", "pairs"])
-@pytest.mark.parametrize("n,t", [(4097, 9000), (100_003, 8191), (100_003, 3_000_001), (5_000_011, 1_200_000)])
+@pytest.mark.parametrize("n,t", [(4097, 9000), (100_003, 8191), (100_003, 1_900_000), (100_003, 3_000_001), (5_000_011, 1_200_000),
+                                 (5_000_011, 40)])
 def test_inverse_of_runs(n, t, kind):
     """Stretches of consecutive tokens (a layout's map), and maps whose runs are longest, shortest, or out of range."""
     vcs = _vcs()
@@ -130,6 +131,16 @@ def test_inverse_of_runs(n, t, kind):
     order = np.argsort(key, kind="stable")
     assert np.array_equal(tok.cpu().numpy(), order)
     assert np.array_equal(off.cpu().numpy(), np.searchsorted(key[order], np.arange(t + 1)))
+
+
+def test_inverse_of_a_part_of_a_map():
+    vcs = _vcs()
+    gat = np.arange(20_001) * 2 // 3
+    for cut in (1, 2, 3):
+        part = dev(gat)[0][cut:]  # at an address that 16 bytes do not divide
+        off, tok = vcs.gather_inverse(part, int(gat[-1]) + 1)
+        assert np.array_equal(tok.cpu().numpy(), np.arange(len(gat) - cut))
+        assert np.array_equal(off.cpu().numpy(), np.searchsorted(gat[cut:], np.arange(gat[-1] + 2)))
 
 
 def test_inverse_of_a_layout_and_bad_entries():
