@@ -243,8 +243,8 @@ __global__ void __launch_bounds__(kPosThreads, 6)
 // length - 1) and the place of the first.  inverse_runs finds them and counts every group's runs and keys; a
 // stable radix sort by 8-bit digits of the group brings a group's runs together, in order; then a warp takes a group:
 // the ends of its runs give the tokens' counts, their scan inv_off and where each token's next copy goes.  The map is
-// read once, and once more where runs begin.  15.8 M keys of long rollouts: 130 us (a sort of the keys themselves by
-// three digits and a search of the offsets took 400); random keys, which are runs of one, take 770 against 430.
+// read once, and once more where runs begin.  15.8 M keys of long rollouts: 125 us (a sort of the keys themselves by
+// three digits and a search of the offsets took 400); random keys, which are runs of one, take 790 against 430.
 // A group of more than kChunk runs, which no layout of few segments has, is split among warps: the copies in each
 // chunk, a scan, the places (5 M copies of one token: 4.1 ms, with one warp 204).  Far fewer keys than tokens, where
 // the groups would be too wide or too many, are sorted by themselves.
@@ -722,13 +722,38 @@ __device__ __forceinline__ int warp_scan(int x) {  // inclusive
   return x;
 }
 
-// Copies of the group's tokens, from where its runs begin and end: each(i, copies of token i, 0 behind the last) is
-// called by all lanes, 32 tokens at a time.  c holds the changes of the count.
-template <typename F>
-__device__ __forceinline__ void count_copies(const Group& g, const int32_t* __restrict__ keys, uint32_t T, int32_t* c,
-                                             F&& each) {
+// Sums of c[0], ... in its place, from `carry` on: of those before (places of counts), or with the own (counts of
+// changes).  256 at a time, eight a lane: a scan over the warp for every 32 was half of inverse_place's instructions.
+constexpr int kSpan = 256;
+template <bool BEFORE>
+__device__ __forceinline__ void sums(int32_t* c, int width, int carry) {
   const int lane = threadIdx.x & 31;
-  for (int i = lane; i < g.width; i += 32) c[i] = 0;
+  for (int i0 = 0; i0 < width; i0 += kSpan) {
+    int4* at = reinterpret_cast<int4*>(c + i0) + 2 * lane;
+    const int4 lo = at[0], hi = at[1];
+    int v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w}, sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += v[i];
+    const int upto = warp_scan(sum) + carry;
+    int x = upto - sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int own = v[i];
+      v[i] = BEFORE ? x : x + own;
+      x += own;
+    }
+    at[0] = make_int4(v[0], v[1], v[2], v[3]);
+    at[1] = make_int4(v[4], v[5], v[6], v[7]);
+    carry = __shfl_sync(0xffffffffu, upto, 31);
+  }
+  __syncwarp();
+}
+
+// The copies of the group's tokens into c, from where its runs begin and end.
+__device__ __forceinline__ void count_copies(const Group& g, const int32_t* __restrict__ keys, uint32_t T, int32_t* c) {
+  const int lane = threadIdx.x & 31;
+  for (int i = 4 * lane; i < g.width; i += 128) *reinterpret_cast<int4*>(c + i) = make_int4(0, 0, 0, 0);
+  for (int i = g.width + lane; i < (g.width + kSpan - 1) / kSpan * kSpan; i += 32) c[i] = 0;
   __syncwarp();
   for (int r = lane; r < g.runs; r += 32) {
     const int first = (int)(min((uint32_t)__ldg(&keys[g.run_at[r]]), T) - g.token);
@@ -737,13 +762,7 @@ __device__ __forceinline__ void count_copies(const Group& g, const int32_t* __re
     if (end < g.width) atomicAdd(&c[end], -1);
   }
   __syncwarp();
-  int copies = 0;  // of the token before
-  for (int i = lane; i - lane < g.width; i += 32) {
-    const int x = warp_scan(i < g.width ? c[i] : 0) + copies;
-    copies = __shfl_sync(0xffffffffu, x, 31);
-    each(i, i < g.width ? x : 0);
-  }
-  __syncwarp();
+  sums<false>(c, g.width, 0);
 }
 
 // The runs' segment tokens, in order, to their tokens' places c.  A run's tokens differ, so long runs are taken one by
@@ -811,20 +830,18 @@ __global__ void __launch_bounds__(kSortThreads, 6)
                   const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups, int num_groups,
                   const unsigned long long* __restrict__ group_sums, HeavyList heavy, int32_t* __restrict__ inv_off,
                   int32_t* __restrict__ inv_tok) {
-  __shared__ int32_t counters[kSortWarps][kCounters];
-  const int wid = threadIdx.x >> 5, blocks = (num_groups + kSortWarps - 1) / kSortWarps;
+  __shared__ __align__(16) int32_t counters[kSortWarps][kCounters];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, blocks = (num_groups + kSortWarps - 1) / kSortWarps;
   int32_t* c = counters[wid];
   if ((int)blockIdx.x < blocks) {
     const int g = blockIdx.x * kSortWarps + wid;
     if (g >= num_groups) return;
     const Group group = group_at(g, T, shift, run_key, run_at, groups, num_groups, group_sums);
     if (group.runs > kChunk) return;
-    int next = group.first;
-    count_copies(group, keys, T, c, [&](int i, int copies) {
-      const int x = warp_scan(copies);
-      if (i < group.width) inv_off[(size_t)group.token + i] = c[i] = next + x - copies;
-      next += __shfl_sync(0xffffffffu, x, 31);
-    });
+    count_copies(group, keys, T, c);
+    sums<true>(c, group.width, group.first);
+    for (int i = lane; i < group.width; i += 32) inv_off[(size_t)group.token + i] = c[i];
+    __syncwarp();
     place_copies(group, keys, T, shift, c, inv_tok);
   } else {
     const int chunks = heavy.num[0];
@@ -832,9 +849,9 @@ __global__ void __launch_bounds__(kSortThreads, 6)
       const int2 which = heavy.chunk[k];
       const Group group = group_at(which.x, T, shift, run_key, run_at, groups, num_groups, group_sums);
       int32_t* to = heavy.counts + (size_t)k * kCounters;
-      count_copies(chunk_of(group, which.y), keys, T, c, [&](int i, int copies) {
-        if (i < group.width) to[i] = copies;
-      });
+      count_copies(chunk_of(group, which.y), keys, T, c);
+      for (int i = lane; i < group.width; i += 32) to[i] = c[i];
+      __syncwarp();
     }
   }
 }
