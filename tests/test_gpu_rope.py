@@ -143,6 +143,42 @@ def test_inverse_of_a_part_of_a_map():
         assert np.array_equal(off.cpu().numpy(), np.searchsorted(gat[cut:], np.arange(gat[-1] + 2)))
 
 
+def test_inverse_captured_replayed_and_beside_another():
+    vcs = _vcs()
+    t = 20_000
+    maps = [dev((np.arange(60_000) * 7 // 8 + c) % t)[0] for c in (0, 5)] + dev(np.full(60_000, 3))
+    want = []
+    for m in maps:
+        key = m.cpu().numpy()
+        order = np.argsort(key, kind="stable")
+        want.append((np.searchsorted(key[order], np.arange(t + 1)), order))
+
+    def check(got, i):
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(got, want[i])), i
+    gat = maps[0].clone()
+    vcs.gather_inverse(gat, t)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = vcs.gather_inverse(gat, t, check=False)
+    for i in (2, 0, 1, 2):  # one token's 60,000 copies before and behind others: nothing is left of a replay
+        gat.copy_(maps[i])
+        g.replay()
+        check(got, i)
+    sides = [torch.cuda.Stream() for _ in maps]
+    torch.cuda.synchronize()
+    outs = [vcs.gather_inverse(m, t, stream=x, check=False) for x, m in list(zip(sides, maps)) * 3]
+    torch.cuda.synchronize()
+    for k, o in enumerate(outs):
+        check(o, k % 3)
+
+
+@pytest.mark.parametrize("n", [5, 5000])
+def test_inverse_of_no_tokens(n):
+    vcs = _vcs()
+    off, tok = vcs.gather_inverse(torch.zeros(n, dtype=torch.int32, device="cuda"), 0, check=False)
+    assert off.tolist() == [0] and tok.tolist() == list(range(n))
+
+
 def test_inverse_of_a_layout_and_bad_entries():
     vcs = _vcs()
     cu, img, txt = random_steps(3)
