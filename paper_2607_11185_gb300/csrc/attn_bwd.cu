@@ -284,21 +284,24 @@ __device__ __forceinline__ void drain_d64(const uint32_t (&v)[2][32], int lane, 
 
 // Sliding window and sinks: key j is visible to query i >= j if i - j < window or j < sinks.  A key tile past
 // the sinks meets the row tiles up to its last key's window; a tile that holds sinks meets all of them, and
-// would run long after the others of a long segment.  So its row tiles are dealt to up to `parts` CTAs, in
-// runs of `chunk`; each leaves its dK and dV in fp32 in a slot of `acc`, and bwd_sink_sum adds a tile's slots
-// in order (the sum does not depend on which CTA comes first).  chunk is at least 16 row tiles, twice a
-// window's and a quarter of what an SM has to do, so that a launch of many segments, or of short ones, splits
-// none and pays nothing.  28/4/128, 4 sinks, ms without and with: one segment of 32,768 at window 128 4.37 and 0.84,
-// at window 1,024 4.85 and 1.41; 32 segments of 4,096 3.10 and 2.93, 4.99 and 4.99.
+// would run long after the others of a long segment.  So its row tiles are dealt to up to `parts` CTAs, `chunk`
+// each and up to 5/3 of that for the first; each leaves its dK and dV in fp32 in a slot of `acc`, and bwd_sink_sum
+// adds a tile's slots in order (the sum does not depend on which CTA comes first).  chunk is a window's row tiles:
+// the parts walk the heads at the pace of the key tiles, next to which the grid lists them, and meet the same lines
+// of Q, dO and dQ in L2.  With 16 row tiles or more, listed first, the sinks took all of them through HBM again:
+// forward and backward of one long rollout, 40/8/128, window 1,024, 4 sinks 21.0 ms and 19.1; the backward of 16
+// segments of 4,096, 28/4/128, window 128, 1.56 and 1.36.  chunk is at least 28 tiles over the heads of a group (a
+// part leaves 128 KB; 40/40/128, 50 segments of 1,300: 2.45 ms unsplit, 3.0 in parts of four tiles) and twice the sink
+// tiles.
 struct WinArgs {
   int32_t window, sinks;   // at most max_seqlen (and the window at least 1)
   int32_t tiles;           // key tiles that hold sinks
   int32_t parts, chunk;    // CTAs a sink tile may take (1: it is not split), row tiles of each
   float* acc;              // slots of [kv head][sink tile], each dK then dV, [128][D]
 };
-// A segment has split sink tiles only if it is longer than chunk row tiles.  Part p of it begins chunk * p row
-// tiles into it; at most one part that is no segment's first and one that is begin in any run of chunk * 128
-// tokens of the packed buffer, which gives each of them a slot.
+// A segment has split sink tiles only if it is longer than chunk row tiles.  The places chunk * p row tiles into it
+// give its parts p their slots: at most one of a part that is no segment's first and one of a first part are in any
+// run of chunk * 128 tokens of the packed buffer.
 __host__ __device__ __forceinline__ int64_t sink_slots(int64_t num_tokens, int chunk) {
   return 2 * (num_tokens / ((int64_t)chunk * 128) + 1);
 }
@@ -306,7 +309,7 @@ __device__ __forceinline__ int64_t sink_slot(int start, int p, int chunk) {
   return 2 * ((start + (int64_t)p * chunk * 128) / ((int64_t)chunk * 128)) + (p == 0 ? 1 : 0);
 }
 __device__ __forceinline__ int sink_parts(const WinArgs& w, int rows) {  // of a sink tile with `rows` row tiles
-  return w.parts > 1 ? (rows + w.chunk - 1) / w.chunk : 1;
+  return w.parts > 1 ? max(1, (rows + w.chunk / 3) / w.chunk) : 1;
 }
 
 // GATHER: Q, K and V are trajectory-layout tensors read through tok_gather, one warp per
@@ -346,13 +349,17 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     sg = ngroups - tail_groups + (int)(t % tail_groups);
   }
   int part = 0;
-  if constexpr (WIN) {  // the sink tiles' further parts come first
-    const int more = win.tiles * (win.parts - 1);
-    if (n < more) {
-      part = 1 + n / win.tiles;
-      n %= win.tiles;
-    } else {
-      n -= more;
+  if constexpr (WIN) {  // the sink tiles' parts p come before the key tiles [(p - 1) * chunk, p * chunk)
+    if (win.parts > 1) {
+      const int period = win.tiles + win.chunk, p = 1 + n / period, r = n % period;
+      if (p >= win.parts) {
+        n -= (win.parts - 1) * win.tiles;
+      } else if (r < win.tiles) {
+        part = p;
+        n = r;
+      } else {
+        n = (p - 1) * win.chunk + r - win.tiles;
+      }
     }
   }
   const int seg = sg / hkv;
@@ -385,8 +392,8 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
       parts = sink_parts(win, nsub);
       if (part >= parts) return;
       if (parts > 1) {
-        sub0 = part * win.chunk;
-        nsub = min(nsub, sub0 + win.chunk);
+        if (part > 0) sub0 = nsub - (parts - part) * win.chunk;
+        nsub -= (parts - 1 - part) * win.chunk;
       }
     }
   }
@@ -1112,6 +1119,7 @@ __global__ void __launch_bounds__(256) bwd_sink_sum(const int32_t* __restrict__ 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // How a windowed launch splits its sink tiles (WinArgs).
+constexpr int64_t kPartTiles = 28;  // tiles of a part, over the group's heads, at least
 WinArgs plan_window(const AttnArgs& a) {
   WinArgs w{};
   const int32_t longest = a.max_seqlen > 1 ? a.max_seqlen : 1;
@@ -1121,13 +1129,14 @@ WinArgs plan_window(const AttnArgs& a) {
   w.parts = 1;
   w.chunk = 1;
   const int64_t rows = ((int64_t)longest + 127) / 128, wrows = ((int64_t)w.window + 126) / 128 + 1;
-  int64_t chunk = a.hkv * (a.num_tokens / 128) * wrows / 152 / 4;  // a quarter of an SM's row tiles
-  if (chunk < 2 * wrows) chunk = 2 * wrows;
-  if (chunk < 16) chunk = 16;
+  const int64_t G = a.hkv > 0 && a.hq > a.hkv ? a.hq / a.hkv : 1;  // sizes are asked for before arguments are checked
+  int64_t chunk = wrows;
+  if (chunk < 2 * w.tiles) chunk = 2 * w.tiles;
+  if (chunk * G < kPartTiles) chunk = (kPartTiles + G - 1) / G;
   // many sinks are many tiles, which balance each other as the causal kernel's do
-  if (w.tiles > 0 && w.tiles <= 8 && chunk < rows) {
+  if (w.tiles > 0 && w.tiles <= 8 && chunk + chunk - chunk / 3 <= rows) {
     w.chunk = (int32_t)chunk;
-    w.parts = (int32_t)((rows + chunk - 1) / chunk);
+    w.parts = (int32_t)((rows + chunk / 3) / chunk);
   }
   return w;
 }

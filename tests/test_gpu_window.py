@@ -131,6 +131,16 @@ def test_split_sink_tiles(hq, hkv, d, lens, window, sinks):
     check(q, k, v, do, lens, window, sinks)
 
 
+@pytest.mark.parametrize("hq,hkv,d,lens,window,sinks", [
+    (7, 1, 64, [900, 800, 768, 640, 1200], 100, 4),   # parts of four row tiles and a first of up to six
+    (7, 1, 128, [1700, 130], 100, 200),               # two sink tiles, of which the second has a row tile less
+    (14, 2, 64, [3000, 900, 1], 200, 300),            # three, in parts of six row tiles
+    (28, 1, 64, [1100], 64, 5), (4, 4, 64, [6100], 64, 1)])  # parts of two, and of 28
+def test_sink_tiles_in_many_parts(hq, hkv, d, lens, window, sinks):
+    q, k, v, do = workloads.draw_dense(len(lens), sum(lens), hq, hkv, d, device="cuda")
+    check(q, k, v, do, lens, window, sinks)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_wide_window_equals_causal(d):
     vcs = _vcs()

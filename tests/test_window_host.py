@@ -43,12 +43,11 @@ def test_refusals(vcs):
     assert bwd(nt=50_000, mx=50_000, w=128, s=4, n=need - 1) == 8
 
 
-def chunk_of(hkv, nt, mx, w, s):
+def chunk_of(G, mx, w, s):
     """The documented rule: row tiles of a part, None where sink tiles are not split."""
     w, s, rows = min(w, mx), min(s, mx), -(-mx // 128)
-    wrows = (w + 126) // 128 + 1
-    chunk = max(hkv * (nt // 128) * wrows // 152 // 4, 2 * wrows, 16)
-    return chunk if 0 < s <= 8 * 128 and chunk < rows else None
+    chunk = max((w + 126) // 128 + 1, 2 * -(-s // 128), -(-28 // G))
+    return chunk if 0 < s <= 8 * 128 and 2 * chunk - chunk // 3 <= rows else None
 
 
 def test_backward_workspace(vcs):
@@ -56,7 +55,7 @@ def test_backward_workspace(vcs):
     for ns, nt, mx, hq, hkv, d, w, s in ((1, 50_000, 50_000, 2, 1, 64, 128, 4), (3, 9000, 4000, 8, 2, 128, 256, 300),
                                          (7, 246_616, 46_176, 40, 8, 128, 1024, 4), (1, 70_000, 70_000, 4, 4, 64, 64, 0),
                                          (2, 100, 64, 4, 1, 64, 1, 1), (1, 50_000, 50_000, 2, 1, 64, 128, 2000)):
-        chunk = chunk_of(hkv, nt, mx, w, s)
+        chunk = chunk_of(hq // hkv, mx, w, s)
         more = up(hkv * -(-min(s, mx) // 128) * 2 * (nt // (chunk * 128) + 1) * 2 * 128 * d * 4) if chunk else 0
         assert vcs.vcs_attn_bwd_window_workspace_size(ns, nt, mx, hq, hkv, d, w, s) == \
             vcs.vcs_attn_bwd_workspace_size(ns, nt, mx, hq, hkv, d) + more
@@ -78,6 +77,47 @@ def test_slots_of_split_tiles_are_distinct():
                 slot = 2 * ((int(start) + p * chunk * 128) // (chunk * 128)) + (p == 0)
                 assert slot not in seen and slot < 2 * (int(ends[-1]) // (chunk * 128) + 1)
                 seen.add(slot)
+
+
+def test_parts_of_sink_tiles_cover_every_row_tile_once():
+    # the kernel's rules: which key tile and part a CTA takes, and which row tiles a part has
+    rng = np.random.default_rng(1)
+    for _ in range(400):
+        longest, G = int(rng.integers(1, 40_000)), int(rng.choice([1, 2, 5, 7, 8, 40]))
+        window, sinks = int(rng.choice([1, 64, 128, 200, 1024, 5000])), int(rng.integers(1, 1100))
+        chunk, tiles, rows = chunk_of(G, longest, window, sinks), -(-min(sinks, longest) // 128), -(-longest // 128)
+        if chunk is None:
+            continue
+        parts = (rows + chunk // 3) // chunk
+        assert parts >= 2
+        seen = set()
+        for x in range(rows + tiles * (parts - 1)):
+            p, r = divmod(x, tiles + chunk)
+            p += 1
+            seen.add((x - (parts - 1) * tiles, 0) if p >= parts else (r, p) if r < tiles else
+                     ((p - 1) * chunk + r - tiles, 0))
+        assert seen == {(n, 0) for n in range(rows)} | {(n, p) for n in range(tiles) for p in range(1, parts)}
+        start, slots, nt = 0, set(), longest + 3 * 777
+        for length in (longest, 777, 777, 777):  # and shorter segments, of fewer parts or one
+            for n in range(min(tiles, -(-length // 128))):
+                mine = -(-(length - n * 128) // 128)
+                count = max(1, (mine + chunk // 3) // chunk)
+                assert count <= parts
+                rows_of = []
+                for p in range(count):
+                    first = mine - (count - p) * chunk if p > 0 else 0
+                    rows_of += range(first, mine - (count - 1 - p) * chunk)
+                    if count > 1:
+                        slot = (n, 2 * ((start + p * chunk * 128) // (chunk * 128)) + (p == 0))
+                        assert slot not in slots and slot[1] < 2 * (nt // (chunk * 128) + 1)
+                        slots.add(slot)
+                assert rows_of == list(range(mine))
+            start += length
+
+
+def test_sizes_for_any_arguments(vcs):
+    for hq, hkv in ((0, 1), (1, 0), (-4, 2), (4, -2), (1, 8), (0, 0)):
+        vcs.vcs_attn_bwd_window_workspace_size(1, 9000, 9000, hq, hkv, 64, 128, 4)  # returns
 
 
 def test_no_lane_decides_alone():
