@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kPosThreads, 6)
 // stable radix sort by 8-bit digits of the group brings a group's runs together, in order; then a warp takes a group:
 // the ends of its runs give the tokens' counts, their scan inv_off and where each token's next copy goes.  The map is
 // read once, and once more where runs begin.  15.8 M keys of long rollouts: 125 us (a sort of the keys themselves by
-// three digits and a search of the offsets took 400); random keys, which are runs of one, take 790 against 430.
+// three digits and a search of the offsets took 400); random keys, which are runs of one, take 770 against 430.
 // A group of more than kChunk runs, which no layout of few segments has, is split among warps: the copies in each
 // chunk, a scan, the places (5 M copies of one token: 4.1 ms, with one warp 204).  Far fewer keys than tokens, where
 // the groups would be too wide or too many, are sorted by themselves.
@@ -578,7 +578,7 @@ __device__ __forceinline__ int place_tile(SortTile& s, const uint32_t (&key)[kPe
 
 // A pass of the runs' sort.  The first one's blocks have block_runs runs each, and it says how many there are; later
 // ones' are packed.  A tile is sorted in shared memory first, so that a digit's runs leave together.
-__global__ void __launch_bounds__(kSortThreads, 4)
+__global__ void __launch_bounds__(kSortThreads, 3)
     inverse_scatter(const uint32_t* __restrict__ keys, const int32_t* __restrict__ vals, int shift, int each,
                     const int32_t* __restrict__ counts, const int32_t* __restrict__ totals,
                     const int32_t* __restrict__ block_runs, int32_t* __restrict__ num_runs,
@@ -825,7 +825,7 @@ __device__ __forceinline__ void place_copies(const Group& g, const int32_t* __re
 
 // A warp a group of up to kChunk runs: its tokens' copies, their scan, and the copies to their places.  The warps of
 // the blocks behind them: the copies in the chunks of the other groups.
-__global__ void __launch_bounds__(kSortThreads, 6)
+__global__ void __launch_bounds__(kSortThreads, 5)
     inverse_place(const int32_t* __restrict__ keys, uint32_t T, int shift, const uint32_t* __restrict__ run_key,
                   const int32_t* __restrict__ run_at, const unsigned long long* __restrict__ groups, int num_groups,
                   const unsigned long long* __restrict__ group_sums, HeavyList heavy, int32_t* __restrict__ inv_off,
