@@ -20,6 +20,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "rope_table.h"
 #include "sm100.cuh"
 
 namespace vcs {
@@ -989,9 +990,8 @@ __global__ void __launch_bounds__(256) inverse_offsets(const uint32_t* __restric
 }
 
 // ------------------------------------------------------------------ rotation
-constexpr int kRopeThreads = 128;
-constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kBatch = 8;  // copies of rows whose angles a warp holds
+constexpr int kRopeThreads = 32 * kRopeWarps;
+constexpr int kBatch = kRopeCopies;
 constexpr int kMaxPairs = VCS_ROPE_MAX_PAIRS;
 
 struct RopeArgs {
@@ -1047,9 +1047,9 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_rows(const __grid_consta
   constexpr int H = INTER ? 2 : 4;         // two pairs each: an item's table entries
   constexpr int IC = INTER ? 1 : 2;        // chunks of an item
   constexpr int U = INTER ? 2 : 1;         // items a lane has in flight
-  extern __shared__ float4 table[];        // [warp][copy][NP * 16]
+  extern __shared__ float4 table[];        // rope_table.h
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  float4* tab = table + (size_t)wid * (BWD ? B : a.per) * NP * 16;
+  float4* tab = table + rope_copy_at<NP>(wid, BWD ? B : a.per, 0);
   uint64_t turn[NP];
   int axis[NP], slot[NP];                  // slot: of the pair's cosine in the table, as floats; -1: none
 #pragma unroll
@@ -1057,7 +1057,7 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_rows(const __grid_consta
     const int pair = lane + 32 * p, item = pair / (2 * H), k = pair % (2 * H);
     turn[p] = a.turn[pair];
     axis[p] = a.axis[pair];
-    slot[p] = pair < a.turned * 2 * H ? 4 * ((k >> 1) * a.turned + item) + (k & 1) : -1;
+    slot[p] = pair < a.turned * 2 * H ? 4 * rope_entry(k >> 1, a.turned, item) + (k & 1) : -1;
   }
   const int heads = a.hq + a.hkv;
   const int turned = heads * a.turned, plain = heads * a.plain;
@@ -1073,7 +1073,7 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_rows(const __grid_consta
       for (int j = 0; j < count; ++j) {
         const int64_t n = BWD ? __shfl_sync(0xffffffffu, held, j) : first + j;
         if (n < 0) continue;
-        float* t = reinterpret_cast<float*>(tab + j * NP * 16);
+        float* t = reinterpret_cast<float*>(tab + rope_copy_at<NP>(0, 0, j));
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           const uint64_t ph = (uint64_t)(int64_t)__ldg(&a.pos[axis[p] * a.pos_stride + n]) * turn[p];
@@ -1156,13 +1156,13 @@ __global__ void __launch_bounds__(kRopeThreads, 8) rope_rows(const __grid_consta
 #pragma unroll
                 for (int e = 0; e < IC; ++e) x[u][e] = ld_stream(src + e * a.turned);
               }
-            const float4* t0 = tab + (at0 + j) * NP * 16;
+            const float4* t0 = tab + rope_copy_at<NP>(0, 0, at0 + j);
 #pragma unroll
             for (int u = 0; u < U; ++u)
               if (live[u]) {
 #pragma unroll
                 for (int k = 0; k < H; ++k) {
-                  const float4 cs = t0[k * a.turned + entry[u]];
+                  const float4 cs = t0[rope_entry(k, a.turned, entry[u])];
                   const uint64_t c = dev::f2pack(cs.x, cs.y), s = dev::f2pack(cs.z, cs.w);
                   const uint64_t ns = s ^ 0x8000000080000000ull;
                   uint64_t f, g;  // first and second dims of two pairs
@@ -1285,9 +1285,8 @@ int key_passes(int64_t traj_tokens) {  // 8-bit digits of the keys 0 .. traj_tok
   return p;
 }
 
-template <bool INTER, bool BWD>
-cudaError_t launch_rope(RopeArgs a, int pairs, cudaStream_t st) {
-  const int np = (pairs + 31) / 32;
+template <int NP, bool INTER, bool BWD>
+cudaError_t launch_rope_rows(RopeArgs a, cudaStream_t st) {
   // Rows of some 8 KB are a warp's each; of smaller ones it takes up to eight together, so that the latencies of
   // the map, the positions and the sines are met once for all, while enough warps for every SM remain.
   const int64_t chunks = (int64_t)(a.hq + 2 * a.hkv) * a.chunks;
@@ -1298,18 +1297,17 @@ cudaError_t launch_rope(RopeArgs a, int pairs, cudaStream_t st) {
   // that walk rows in a fixed stride, eight an SM, 1,324 and 925.
   int64_t blocks = (a.rows_out + kRopeWarps * a.per - 1) / (kRopeWarps * a.per);
   if (!BWD && blocks > 152 * 32) blocks = 152 * 32;
-  const size_t smem = (size_t)kRopeWarps * (BWD ? kBatch : a.per) * np * 16 * sizeof(float4);
-  auto go = [&](auto kernel) {
-    if (smem > 48 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) return e;
-    }
-    kernel<<<(unsigned)blocks, kRopeThreads, smem, st>>>(a);
-    return cudaGetLastError();
-  };
-  if (np == 1) return go(rope_rows<1, INTER, BWD>);
-  if (np == 2) return go(rope_rows<2, INTER, BWD>);
-  return go(rope_rows<4, INTER, BWD>);
+  static_assert(rope_table_bytes<NP>(kBatch) <= 48 * 1024, "a launch of more asks for it first");
+  rope_rows<NP, INTER, BWD><<<(unsigned)blocks, kRopeThreads, rope_table_bytes<NP>(BWD ? kBatch : a.per), st>>>(a);
+  return cudaGetLastError();
+}
+
+template <bool INTER, bool BWD>
+cudaError_t launch_rope(const RopeArgs& a, int pairs, cudaStream_t st) {
+  const int np = rope_lane_pairs(pairs);
+  if (np == 1) return launch_rope_rows<1, INTER, BWD>(a, st);
+  if (np == 2) return launch_rope_rows<2, INTER, BWD>(a, st);
+  return launch_rope_rows<4, INTER, BWD>(a, st);
 }
 
 }  // namespace

@@ -253,6 +253,16 @@ def test_gather_rope_and_backward(hq, hkv, d, rot, sections, inter, n, t):
 
 
 @pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("d,rot", [(160, 144), (160, 160), (176, 176), (192, 176), (192, 192), (256, 144), (256, 160),
+                                   (256, 192), (256, 208)])
+@pytest.mark.parametrize("hq,hkv,n,t", [(1, 1, 1, 1), (3, 1, 700, 90), (1, 1, 40_000, 39_000), (28, 4, 300, 90)])
+def test_heads_of_128_to_256_rotated_dims(hq, hkv, n, t, d, rot, inter):
+    # 65 to 104 pairs, with a row and (40,000 short rows) several a warp
+    a = rot // 8
+    test_gather_rope_and_backward(hq, hkv, d, rot, (a, 2 * a - 8, rot // 2 - 3 * a + 8), inter, n, t)
+
+
+@pytest.mark.parametrize("inter", [False, True])
 def test_identity_map_any_position(inter):
     # no map: row n is token n; positions of any int32, exact angles far out and negative ones
     vcs = _vcs()
