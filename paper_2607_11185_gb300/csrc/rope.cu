@@ -119,6 +119,9 @@ __global__ void __launch_bounds__(kPosThreads, 6)
         }
         __syncthreads();
         const int lo = run_at[tid], len = run_at[tid + 1] - lo;
+        // Of steps that are not in order the first one's lower bound may be behind tokens that no run then holds.  From
+        // it on every token is compared with the run that it is in.
+        if (tid == 0 && s0 == first && lo != start) set_status(status, VCS_ERR_DEVICE_CHECK);
         int adv = 0;
         if (s <= last) {
           const int img = step_img[s], txt = step_txt[s];

@@ -85,6 +85,24 @@ def test_positions_device_checks():
         assert e.value.status == 6, bad
 
 
+@pytest.mark.parametrize("src", [
+    [5] * 4 + [3] * 8 + [5] * 20, [5] + [0] * 11 + [5] * 20, [9] + [2] * 299 + [9] * 300, [9] * 100 + [3] * 60 + [9] * 300,
+    [9] * 40 + [0] * 260 + [9] * 20, [7] * 2 + [6] * 998 + [7] * 700, [8] * 10 + [2] * 9000 + [8] * 20_000])
+def test_positions_that_start_out_of_order(src):
+    # the tokens that stand in for a run of the first step are its whole number, but it begins behind them
+    vcs = _vcs()
+    steps = np.arange(10)
+    img = np.where(steps == 5, 12, 280).astype(np.int32)
+    txt = np.where(steps == 5, 8, 20).astype(np.int32)
+    txt[7], txt[8], txt[0] = 420, 20_000, 4
+    grid = np.stack([np.ones(10, int), np.where(steps == 5, 3, 14), np.where(steps == 5, 4, 20)], 1)
+    for head in (0, 4):  # alone, and behind a segment that is in order
+        cu = [0, head, head + len(src)] if head else [0, len(src)]
+        with pytest.raises(vcs.VcsError) as e:
+            vcs.stream_positions(*dev(cu, [0] * head + src, img, txt, grid))
+        assert e.value.status == 6
+
+
 def test_positions_empty():
     vcs = _vcs()
     i = torch.zeros(0, dtype=torch.int32, device="cuda")
