@@ -199,7 +199,8 @@ static AttnArgs make_args(const void* q, const void* k, const void* v, const int
   a.cu_seqlens = cu_seqlens;
   a.num_segments = num_segments;
   a.num_tokens = num_tokens;
-  a.max_seqlen = max_seqlen;
+  // a bound: no segment is longer than all tokens.  The kernels' grids and the workspaces follow from it.
+  a.max_seqlen = max_seqlen < num_tokens ? max_seqlen : (int32_t)num_tokens;
   a.hq = hq;
   a.hkv = hkv;
   a.d = d;

@@ -61,6 +61,17 @@ def test_backward_workspace(vcs):
             vcs.vcs_attn_bwd_workspace_size(ns, nt, mx, hq, hkv, d) + more
 
 
+def test_workspaces_follow_the_tokens_where_the_bound_is_loose(vcs):
+    # max_seqlen is a bound; no segment is longer than all tokens
+    for nt in (0, 1, 300, 9000, 50_000):
+        for mx in (nt + 1, 10 * nt + 129, 2 ** 31 - 128, 2 ** 31 - 1):
+            for w, s in ((64, 4), (1024, 300), (2 ** 31 - 1, 5), (1, 2 ** 31 - 1)):
+                assert vcs.vcs_attn_bwd_window_workspace_size(1, nt, mx, 4, 1, 64, w, s) == \
+                    vcs.vcs_attn_bwd_window_workspace_size(1, nt, nt, 4, 1, 64, w, s), (nt, mx, w, s)
+            assert vcs.vcs_attn_bwd_workspace_size(1, nt, mx, 4, 1, 64) == vcs.vcs_attn_bwd_workspace_size(1, nt, nt, 4, 1, 64)
+            assert vcs.vcs_attn_fwd_workspace_size(1, nt, mx, 4, 1, 64) == vcs.vcs_attn_fwd_workspace_size(1, nt, nt, 4, 1, 64)
+
+
 def test_slots_of_split_tiles_are_distinct():
     # the kernel's rule: part p of a segment of more than `chunk` row tiles takes slot
     # 2 ((start + 128 chunk p) / (128 chunk)) + (p == 0), below 2 (tokens / (128 chunk) + 1)
