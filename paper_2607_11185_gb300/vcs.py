@@ -524,6 +524,11 @@ def _checked(status: int, word, where: str):
     _check(word.tolist()[0], where + " (device)")
 
 
+def _i32_of(n: int) -> int:
+    """n, or the int32 next to it: ctypes would drop the upper bits."""
+    return n if -2 ** 31 <= n < 2 ** 31 else -2 ** 31 if n < 0 else 2 ** 31 - 1
+
+
 def _expect_attn(where: str, q, k, v, cu_seqlens):
     bf16 = torch.bfloat16
     _expect(where, ("q", q, bf16, 3), ("k", k, bf16, 3))
@@ -539,6 +544,7 @@ def attn_fwd_window(q, k, v, cu_seqlens, max_seqlen: int, window: int, sinks: in
         return _on_stream(stream, attn_fwd_window, q, k, v, cu_seqlens, max_seqlen, window, sinks, softmax_scale,
                           check=check)
     _expect_attn("attn_fwd_window", q, k, v, cu_seqlens)
+    max_seqlen, window, sinks = _i32_of(max_seqlen), _i32_of(window), _i32_of(sinks)
     nt, hq, d = q.shape
     hkv = k.shape[1]
     ns = cu_seqlens.numel() - 1
@@ -560,6 +566,7 @@ def attn_bwd_window(q, k, v, o, lse, dout, cu_seqlens, max_seqlen: int, window: 
         return _on_stream(stream, attn_bwd_window, q, k, v, o, lse, dout, cu_seqlens, max_seqlen, window, sinks,
                           softmax_scale, check=check)
     _expect_attn("attn_bwd_window", q, k, v, cu_seqlens)
+    max_seqlen, window, sinks = _i32_of(max_seqlen), _i32_of(window), _i32_of(sinks)
     nt, hq, d = q.shape
     _expect("attn_bwd_window", ("o", o, q.dtype, q.shape), ("lse", lse, torch.float32, (hq, nt)),
             ("dout", dout, q.dtype, q.shape))
@@ -600,7 +607,8 @@ def rope_plan(d: int, sections=None, theta: float = 10000.0, rot_dim: Optional[i
     rot = d if rot_dim is None else rot_dim
     rope = VcsRope()
     sections = (rot // 2,) if sections is None else tuple(sections)
-    _check(vcs_rope_init(rope, rot, len(sections), sections, theta, int(interleaved)), "vcs_rope_init")
+    _check(vcs_rope_init(rope, _i32_of(rot), len(sections), [_i32_of(x) for x in sections], theta, int(interleaved)),
+           "vcs_rope_init")
     return rope
 
 

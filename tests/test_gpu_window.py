@@ -153,6 +153,29 @@ def test_wide_window_equals_causal(d):
         assert (ow.float() - o.float()).abs().max() <= 2e-2 and (lw - lse).abs().max() <= 1e-4
 
 
+def test_numbers_past_32_bits():
+    # a window, sinks or a bound that an int32 cannot hold is as wide as any that reaches past the longest segment
+    vcs = _vcs()
+    lens = [300, 40, 700]
+    q, k, v, do = workloads.draw_dense(6, sum(lens), 4, 2, 64, device="cuda")
+    cu = torch.from_numpy(cu_from_lengths(lens)).cuda()
+    wide = [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, 10 ** 30]
+    for want_args, calls in (((700, 700, 0), [(700, w, 0) for w in wide]), ((700, 3, 700), [(700, 3, w) for w in wide]),
+                             ((700, 90, 4), [(w, 90, 4) for w in wide])):
+        o, lse = vcs.attn_fwd_window(q, k, v, cu, *want_args)
+        dk, dv = vcs.attn_bwd_window(q, k, v, o, lse, do, cu, *want_args)[1:]
+        for args in calls:
+            o2, lse2 = vcs.attn_fwd_window(q, k, v, cu, *args)
+            dk2, dv2 = vcs.attn_bwd_window(q, k, v, o, lse, do, cu, *args)[1:]
+            assert torch.equal(o2, o) and torch.equal(lse2, lse), args
+            assert all((a.double() - b.double()).norm() <= 1e-3 * b.double().norm() for a, b in ((dk2, dk), (dv2, dv))), args
+    for args in ((700, 5 - 2 ** 32, 0), (700, 5, 5 - 2 ** 32), (700 - 2 ** 32, 5, 0)):
+        for f in (lambda: vcs.attn_fwd_window(q, k, v, cu, *args), lambda: vcs.attn_bwd_window(q, k, v, o, lse, do, cu, *args)):
+            with pytest.raises(vcs.VcsError) as e:
+                f()
+            assert e.value.status == 1, args
+
+
 def test_keys_out_of_sight_do_not_matter():
     # scores that no mask value could stand beside: the largest finite keys, out of the window
     vcs = _vcs()

@@ -34,6 +34,14 @@ def test_plan_refusals(vcs):
     assert vcs.vcs_rope_init(None, 64, 1, (32,), 1e4, 0) == 1
 
 
+def test_plan_refuses_numbers_past_32_bits(vcs):
+    wide = 1 << 32
+    for kw in (dict(d=64, rot_dim=wide + 64, sections=(32,)), dict(d=64, sections=(wide + 32,)),
+               dict(d=64, sections=(wide + 8, 12, 12)), dict(d=64, sections=(8 - wide, 12, 12)), dict(d=wide + 64)):
+        with pytest.raises(vcs.VcsError):
+            vcs.rope_plan(**kw)
+
+
 def test_positions_refusals(vcs):
     def f(cu=A, ns=1, nt=10, src=A, img=A, txt=A, grid=A, steps=4, pos=A):
         return vcs.vcs_stream_positions(cu, ns, nt, src, img, txt, grid, steps, pos, None, 0)
