@@ -387,7 +387,9 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
  *   rope        host pointer, read during the call
  *   q, k, v     must not overlap the inputs (VCS_ERR_INVALID_ARG); likewise
  *               the backward's outputs
- * The angle is exact to 2^-32 of a turn for every position; products and sums
+ * The angle is off by at most 2^-25 of a turn, which the sines' fp32 argument
+ * takes, and 2^-52 of the turns |pos inv_freq| / 2 pi that it has passed; that
+ * of -inv_freq at pos is that of inv_freq at -pos to the bit.  Products and sums
  * are fp32, rounded once to bf16.  The v rows are copied bit for bit.
  *
  * vcs_gather_inverse: the gather map the other way, for vcs_gather_rope_bwd:

@@ -9,10 +9,11 @@
 // R turns pair i, dims (a, b), by the angle x = inv_freq[i] * pos[axis[i]]:
 //   (a, b) -> (a cos x - b sin x, b cos x + a sin x).
 //
-// The angle is reduced exactly: inv_freq / 2 pi is a 64-bit fraction of a turn, its product with the
+// The angle is reduced in integers: inv_freq / 2 pi is a 64-bit fraction of a turn, its product with the
 // position modulo 2^64 is the fraction of a turn the angle ends at, and the upper 32 bits of that go to
-// sincospi.  A position of 2^31 is as exact as a position of 1 (a product in fp32 would be off by
-// 4e-3 radians at 67,000).
+// sincospi as a float, off by up to 2^-26 of a turn.  What grows with the position is the rounding of
+// inv_freq / 2 pi, a double: up to 2^-52 of the turns passed, 8e-8 of a turn at a position of 2^31 and a radian a
+// position (a product in fp32 would be off by 4e-3 radians at 67,000).
 //
 // All three are bound by HBM.  The rotation reads and writes each row once; a pass of its own over
 // the gathered rows would double that.
@@ -1478,10 +1479,10 @@ cudaError_t launch_gather_rope(const void* q_in, const void* k_in, const void* v
     a.turn[i] = 0;
     a.axis[i] = 0;
     if (i >= pairs) continue;
-    const double turns = rope.inv_freq[i] * 0.15915494309189533577;
-    double f = turns - std::floor(turns);
-    if (!(f < 1.0)) f = 0.0;  // a tiny negative's fraction rounds to 1
-    a.turn[i] = (uint64_t)(f * 18446744073709551616.0);
+    // of the size, whose fraction is exact: that of a small negative number would be rounded next to 1
+    const double turns = std::fabs(rope.inv_freq[i]) * 0.15915494309189533577;
+    const uint64_t turn = (uint64_t)((turns - std::floor(turns)) * 18446744073709551616.0);
+    a.turn[i] = rope.inv_freq[i] < 0.0 ? 0 - turn : turn;
     a.axis[i] = (uint8_t)rope.pair_axis[i];
   }
   if (backward)

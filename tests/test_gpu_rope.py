@@ -317,6 +317,21 @@ def test_changed_frequencies_and_axes():
     assert (np.abs(got[0].double().cpu().numpy() - ref) <= bound(ref, pair_size(src, 32, False), 40 * pos)).all()
 
 
+@pytest.mark.parametrize("inter", [False, True])
+def test_negative_frequencies_turn_the_other_way(inter):
+    # -f at n is f at -n, bit for bit, however far n is and however small f
+    vcs = _vcs()
+    rng = np.random.default_rng(9)
+    n = 4000
+    pos = rng.integers(-2 ** 31 + 1, 2 ** 31, size=(1, n))
+    one, other = (vcs.rope_plan(128, (64,), 1e9, interleaved=inter) for _ in range(2))
+    for i in range(64):
+        other.inv_freq[i] = -one.inv_freq[i]
+    x = rows(1, n, 8, 128)
+    got, want = (vcs.gather_rope(x, x, x, None, *dev(p), r) for p, r in ((pos, other), (-pos, one)))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_many_copies_and_none():
     # a token of 1,000 copies, some of 7 to 9 (around a warp's batch of angles), some of none
     vcs = _vcs()
