@@ -364,6 +364,8 @@ vcs_status vcs_attn_bwd_window(const void* q, const void* k, const void* v, cons
  *               out of order (skipped), a run of tokens that is neither all of
  *               its step nor its response, or a grid that does not hold the
  *               screenshot (its tokens are counted like text)
+ * A segment's steps are gone through once for every 8,192 of its tokens: in a
+ * segment of many thousand steps the time grows with tokens times steps.
  * Returns VCS_ERR_INVALID_ARG for negative counts or null pointers,
  * VCS_ERR_OVERFLOW for counts above INT32_MAX - 4096 (as the other calls of
  * this section).

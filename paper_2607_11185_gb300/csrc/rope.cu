@@ -43,9 +43,11 @@ constexpr int kPosChunk = 8192;  // tokens of a segment a block writes
 // tok_src_step (non-decreasing within a segment), how far it moves the position follows from the run's
 // length (text only, or screenshot and text), and a block scan gives each run's first position.  Every
 // chunk of a segment repeats the scan of the steps before it: the searches' latency against a launch and a
-// workspace.  A search is one of 256 samples of the segment in shared memory, then four lanes' probes at a time: 5
-// loads that wait on one another for a segment of 46,176 tokens, where halving takes 16.  15.8 M tokens: 54 us, 71
-// with searches by halving and without the loads ahead.
+// workspace.  That suits segments of one or a few tiles of steps: steps of 15 tokens on average, 299,355 and
+// 11,996,577 tokens of them, take 0.03 and 0.16 ms in segments of 50 steps and 0.7 and 67 ms in a single one.  A search
+// is one of 256 samples of the segment in shared memory, then four lanes' probes at a time: 5 loads that wait on one
+// another for a segment of 46,176 tokens, where halving takes 16.  15.8 M tokens: 54 us, 71 with searches by halving
+// and without the loads ahead.
 __global__ void __launch_bounds__(kPosThreads, 6)
     stream_positions_kernel(const int32_t* __restrict__ cu_seqlens, int32_t num_segments, int32_t num_tokens,
                             const int32_t* __restrict__ src_step, const int32_t* __restrict__ step_img,

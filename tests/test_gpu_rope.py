@@ -70,6 +70,14 @@ def test_positions_many_steps_and_chunks():
     check_positions(oseg.build(cu, img, txt, 1000, 0), img, txt, grids(img, rng))
 
 
+def test_positions_of_a_segment_of_thousands_of_steps():
+    # 20,000 short steps in one segment (79 tiles of steps, 37 chunks of tokens), one of a single step behind it
+    rng = np.random.default_rng(6)
+    img, txt = (rng.integers(0, most, size=20_001).astype(np.int32) for most in (21, 11))
+    img[-1], txt[-1] = 12, 3
+    check_positions(oseg.build(np.array([0, 20_000, 20_001], np.int32), img, txt, 30_000, 0), img, txt, grids(img, rng))
+
+
 def test_positions_device_checks():
     vcs = _vcs()
     img, txt, grid = [6, 4], [2, 1], [[1, 2, 3], [1, 1, 4]]
