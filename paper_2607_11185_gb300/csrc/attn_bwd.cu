@@ -289,12 +289,12 @@ __device__ __forceinline__ void drain_d64(const uint32_t (&v)[2][32], int lane, 
 // adds a tile's slots in order (the sum does not depend on which CTA comes first).  chunk is a window's row tiles:
 // the parts walk the heads at the pace of the key tiles, next to which the grid lists them, and meet the same lines
 // of Q, dO and dQ in L2.  With 16 row tiles or more, listed first, the sinks took all of them through HBM again:
-// forward and backward of one long rollout, 40/8/128, window 1,024, 4 sinks 21.0 ms and 19.1; the backward of 16
+// forward and backward of one long rollout, 40/8/128, window 1,024, 4 sinks 21.0 ms and 19.5; the backward of 16
 // segments of 4,096, 28/4/128, window 128, 1.56 and 1.36.  chunk is at least 28 tiles over the heads of a group (a
 // part leaves 128 KB; 40/40/128, 50 segments of 1,300: 2.45 ms unsplit, 3.0 in parts of four tiles) and twice the sink
 // tiles.
 struct WinArgs {
-  int32_t window, sinks;   // at most max_seqlen (and the window at least 1)
+  int32_t window, sinks;   // at most the longest segment's bound (and the window at least 1)
   int32_t tiles;           // key tiles that hold sinks
   int32_t parts, chunk;    // CTAs a sink tile may take (1: it is not split), row tiles of each
   float* acc;              // slots of [kv head][sink tile], each dK then dV, [128][D]
@@ -318,7 +318,7 @@ __device__ __forceinline__ int sink_parts(const WinArgs& w, int rows) {  // of a
 // run of consecutive trajectory rows), and dQ, dK, dV are added in fp32 to trajectory-layout
 // accumulators (dq_acc, dk_acc, dv_acc) at row tok_gather[token]; otherwise segment-layout tiled
 // loads, dq_acc in segment layout, bf16 dK, dV, and the other maps unused.
-// WIN: a sliding window and sinks (WinArgs below).
+// WIN: a sliding window and sinks (WinArgs above).
 template <int D, bool GATHER, bool WIN>
 __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     bwd_main(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,

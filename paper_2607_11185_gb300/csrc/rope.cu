@@ -262,7 +262,10 @@ constexpr int kTile = kSortThreads * kPerThread;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int64_t kSmallOffsets = 8192;  // trajectory tokens whose searches take the one block about a launch's time
 constexpr int kRunBits = 9;              // a run is within a warp's 512 keys
-constexpr int kGroupKeys = 256;          // keys a group, on average: 15.8 M keys take 261, 220 and 216 us at 128, 256, 512
+// Keys a group, on average.  A layout of 15.8 M keys takes 180, 135 and 130 us at 128, 256 and 512 (a call from
+// Python), a map with as many trajectory tokens as keys 125 and 588 at 256 and 512: with 512 it would need groups of
+// more than kCounters tokens, and its keys are sorted by themselves.
+constexpr int kGroupKeys = 256;
 constexpr int kGroups = 256;             // but one digit of groups at least
 constexpr int kMostGroups = 4096;        // and up to these where a group would pass kCounters tokens
 constexpr int kCounters = 512;           // trajectory tokens of a group at most
