@@ -395,6 +395,28 @@ def test_device_checks_leave_rows_out():
     assert torch.equal(got[2][2], (y[3].float() + y[4].float()).bfloat16())
 
 
+@pytest.mark.parametrize("inter", [False, True])
+def test_rows_past_32_bit_offsets(inter):
+    # 2.2 billion elements of q, in and out: rows at both ends and around element 2^31 are those of a call on them alone
+    vcs = _vcs()
+    n = 2 ** 23 + 300_000
+    rope = vcs.rope_plan(64, (8, 12, 12), 1e6, interleaved=inter)
+    q, k, v = rows(1, n, 4, 64), rows(2, n, 1, 64), rows(3, n, 1, 64)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    pos = torch.randint(0, 100_000, (3, n), generator=g, device="cuda", dtype=torch.int32)
+    back_to_front = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    off, tok = vcs.gather_inverse(back_to_front, n)
+    there = vcs.gather_rope(q, k, v, back_to_front, pos, rope)
+    back = vcs.gather_rope_bwd(q, k, v, pos, off, tok, rope)
+    for a, b in ((0, 1000), (2 ** 23 - 500, 2 ** 23 + 500), (n - 1000, n)):
+        at = slice(n - b, n - a)  # the rows' other ends, in reverse
+        flip = [x[at].flip(0).contiguous() for x in (q, k, v)]
+        want = vcs.gather_rope(*flip, None, pos[:, a:b].contiguous(), rope)
+        assert all(torch.equal(x[a:b], y) for x, y in zip(there, want))
+        want = vcs.gather_rope_bwd(*flip, pos[:, at].flip(1).contiguous(), None, None, rope)
+        assert all(torch.equal(x[a:b], y) for x, y in zip(back, want))
+
+
 def test_wrappers_refuse_other_layouts():
     vcs = _vcs()
     rope = vcs.rope_plan(64)
