@@ -1190,7 +1190,8 @@ cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, con
     return cudaErrorInvalidValue;
   }
   if (!encode_tma_3d_bf16(&tdo, dout, D, a.hq, a.num_tokens, 64, 128)) return cudaErrorInvalidValue;
-  const int ntiles = (a.max_seqlen + C::BM - 1) / C::BM;
+  // one at least, whose CTAs report segments of more tokens than a bound of 0
+  const int ntiles = a.max_seqlen > 0 ? (a.max_seqlen + C::BM - 1) / C::BM : 1;
   WinArgs win{};
   if (WIN) {
     win = plan_window(a);
@@ -1212,31 +1213,29 @@ cudaError_t launch_bwd_d(const AttnArgs& a, const void* o, const float* lse, con
     tail_groups = 0.0;
     grid.x = (unsigned)(ntiles + win.tiles * (win.parts - 1));
   }
-  if (ntiles > 0) {
-    static std::atomic<int> regs_cache{-1};
-    bool regs_ok = false;
-    if (cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(bwd_main<D, GATHER, WIN>), C::REG_LAUNCH,
-                                          &regs_cache, &regs_ok);
-        e != cudaSuccess)
-      return e;
-    if (!regs_ok) return cudaErrorInvalidConfiguration;
-    cudaError_t e = cudaFuncSetAttribute(bwd_main<D, GATHER, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  static std::atomic<int> regs_cache{-1};
+  bool regs_ok = false;
+  if (cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(bwd_main<D, GATHER, WIN>), C::REG_LAUNCH,
+                                        &regs_cache, &regs_ok);
+      e != cudaSuccess)
+    return e;
+  if (!regs_ok) return cudaErrorInvalidConfiguration;
+  cudaError_t e = cudaFuncSetAttribute(bwd_main<D, GATHER, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  bwd_main<D, GATHER, WIN><<<grid, C::THREADS, C::SMEM, st>>>(
+      tq, tk, tv, tdo, a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens, a.max_seqlen, a.hq, a.hkv,
+      (int32_t)tail_groups, a.scale, a.scale * 1.4426950408889634f, lse, dvec, GATHER ? dq_t : dq_acc, static_cast<__nv_bfloat16*>(dk),
+      static_cast<__nv_bfloat16*>(dv), a.status, a.tok_gather, (int32_t)a.traj_tokens, dk_t, dv_t,
+      GATHER ? tqr : tq, GATHER ? tkr : tk, GATHER ? tvr : tv, GATHER ? tqs : tq, GATHER ? tks : tk,
+      GATHER ? tvs : tv, win);
+  if (WIN && win.parts > 1) {
+    e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    bwd_main<D, GATHER, WIN><<<grid, C::THREADS, C::SMEM, st>>>(
-        tq, tk, tv, tdo, a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens, a.max_seqlen, a.hq, a.hkv,
-        (int32_t)tail_groups, a.scale, a.scale * 1.4426950408889634f, lse, dvec, GATHER ? dq_t : dq_acc, static_cast<__nv_bfloat16*>(dk),
-        static_cast<__nv_bfloat16*>(dv), a.status, a.tok_gather, (int32_t)a.traj_tokens, dk_t, dv_t,
-        GATHER ? tqr : tq, GATHER ? tkr : tk, GATHER ? tvr : tv, GATHER ? tqs : tq, GATHER ? tks : tk,
-        GATHER ? tvs : tv, win);
-    if (WIN && win.parts > 1) {
-      e = cudaGetLastError();
-      if (e != cudaSuccess) return e;
-      int64_t blocks = gx * win.tiles * (2 * 128 * D / 4 / 256);
-      if (blocks > 152 * 32) blocks = 152 * 32;
-      bwd_sink_sum<D><<<(unsigned)blocks, 256, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens,
-                                                        a.max_seqlen, a.hkv, win, static_cast<__nv_bfloat16*>(dk),
-                                                        static_cast<__nv_bfloat16*>(dv));
-    }
+    int64_t blocks = gx * win.tiles * (2 * 128 * D / 4 / 256);
+    if (blocks > 152 * 32) blocks = 152 * 32;
+    bwd_sink_sum<D><<<(unsigned)blocks, 256, 0, st>>>(a.cu_seqlens, a.num_segments, (int32_t)a.num_tokens,
+                                                      a.max_seqlen, a.hkv, win, static_cast<__nv_bfloat16*>(dk),
+                                                      static_cast<__nv_bfloat16*>(dv));
   }
   auto convert = [&](const float* acc, void* out, int64_t elems) {
     const int64_t n8 = elems / 8;
