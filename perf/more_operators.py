@@ -309,7 +309,7 @@ def _own(s):
     from paper_2607_11185_gb300 import vcs
     kind = s["case"]["kind"]
     if kind == "step":
-        o = vcs.linear_attn_step(s["q"], s["k"], s["v"], s["decay"], s["state"])
+        o = vcs.linear_attn_step(s["q"], s["k"], s["v"], s["decay"], s["state"], check=False)
         return dict(o=o, state=s["state"])
     if kind == "prompt":
         o, state = vcs.linear_attn_fwd(s["q"], s["k"], s["v"], s["decay"], s["cu"], state=s["state"], with_state=True,
