@@ -546,6 +546,126 @@ vcs_status vcs_grpo_loss(const float* logp, const float* old_logp, const float* 
 vcs_status vcs_group_advantage(const float* rewards, int64_t num_groups, int32_t group_size, float eps, float* adv,
                                void* stream);
 
+/* ------------------------------------------------------------------------
+ * Linear attention with a decay for each key/value head (not in the paper:
+ * for policies whose history runs through states instead of keys).  Over the
+ * tokens t of a segment, with lam = exp(log_decay[head]), a state S [d, d]
+ * for each key/value head and g = h / (hq / hkv) as for vcs_attn_fwd:
+ *   S_t = lam S_{t-1} + k_t v_t^T,   o_t[h] = scale q_t[h]^T S_t[g]
+ * that is o_t = scale sum_{s <= t} lam^(t-s) (q_t . k_s) v_s.  The decays are
+ * constants of the layer: no call returns a gradient of them.
+ *
+ *   q, o, dout, dq   bf16 [num_tokens, hq, d] device
+ *   k, v, dk, dv     bf16 [num_tokens, hkv, d] device
+ *   log_decay        fp32 [hkv] device: finite and at most 0 (0: no decay)
+ *   cu_seqlens       int32 [num_segments + 1] device, 0 <= cu_seqlens[s] <=
+ *                    cu_seqlens[s+1] <= num_tokens; rows of tokens that no
+ *                    segment holds are left as they were
+ *   scale            of the outputs; 0 or less, or not finite: 1 / sqrt(d)
+ *   ws               device workspace of the call's ..._workspace_size()
+ *                    bytes, 256-byte aligned; its first int32 is the device
+ *                    status word: VCS_ERR_DEVICE_CHECK for segment bounds
+ *                    outside those above (that segment is left out) or a
+ *                    log_decay that is positive or not finite (that head is
+ *                    left out), VCS_ERR_DEVICE_TIMEOUT
+ *
+ * vcs_linear_attn_fwd: prompts and training segments.
+ *   state_in         fp32 [num_segments, hkv, d, d] device or NULL (zeros):
+ *                    S before each segment's first token, rows of k's dims
+ *   state_out        fp32, likewise, or NULL: S behind its last token
+ *                    (written; of an empty segment, state_in)
+ * Outputs must not overlap the inputs (VCS_ERR_INVALID_ARG).
+ *
+ * vcs_linear_attn_bwd: dq, dk, dv of a forward without state_in, from dout =
+ * d loss / d o.  Neither o nor a forward's workspace is needed.
+ *
+ * vcs_linear_attn_step: one token of each of num_seqs sequences (q, k, v, o
+ * with num_seqs rows), states fp32 [num_seqs, hkv, d, d] updated in place.
+ *   dev_status       int32 device-visible word or NULL, zeroed by the caller:
+ *                    VCS_ERR_DEVICE_CHECK as above (that head is left out)
+ *
+ * States, decays and sums are fp32.  The forward's products between tokens of
+ * a chunk, and a chunk's starting state where queries read it, are rounded to
+ * bf16; the states handed from chunk to chunk and state_out are not.  The same
+ * inputs give the same bits.
+ * Return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
+ * bytes) pointers or overlapping outputs; VCS_ERR_UNSUPPORTED for d other
+ * than 64 and 128, hq not a multiple of hkv or more than 65,535 heads;
+ * VCS_ERR_OVERFLOW for more than INT32_MAX - 256 tokens; VCS_ERR_WORKSPACE.
+ * ------------------------------------------------------------------------ */
+size_t vcs_linear_attn_fwd_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv,
+                                          int32_t d);
+
+vcs_status vcs_linear_attn_fwd(const void* q, const void* k, const void* v, const float* log_decay,
+                               const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, float scale, const float* state_in, float* state_out, void* o,
+                               void* ws, size_t ws_bytes, void* stream);
+
+size_t vcs_linear_attn_bwd_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv,
+                                          int32_t d);
+
+vcs_status vcs_linear_attn_bwd(const void* q, const void* k, const void* v, const void* dout, const float* log_decay,
+                               const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, float scale, void* dq, void* dk, void* dv, void* ws,
+                               size_t ws_bytes, void* stream);
+
+vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, const float* log_decay, int64_t num_seqs,
+                                int32_t hq, int32_t hkv, int32_t d, float scale, float* states, void* o,
+                                int32_t* dev_status, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Distillation from a teacher's top logits (not in the paper: a policy that
+ * learns from another one's rollouts, which keep for every token the top
+ * entries of the distribution it was drawn from).  Row r has the logits z of
+ * one trained token and the list l = teacher_rows[r] (or r):
+ *   p_j   = softmax over the list's entries of teacher_logits[l, j] / T
+ *   log q = z / T - ln sum_v exp(z_v / T), over the whole vocabulary
+ *   row_kl[r] = sum_j p_j (ln p_j - log q[teacher_ids[l, j]])
+ *   loss      = sum_r weights[r] row_kl[r]
+ *   dlogits[r, v] = weights[r] / T (q_v - sum_{j: teacher_ids[l, j] = v} p_j)
+ *
+ * vcs_distill_topk: forward and, with dlogits, backward in one pass.
+ *   logits      [rows, vocab] device, VCS_BF16 or VCS_F32 (logits_type),
+ *               logits_stride elements from row to row (>= vocab)
+ *   teacher_ids int32 [lists, top] device: entries in [0, vocab), in any
+ *               order; -1: no entry.  One that comes twice counts twice.
+ *   teacher_logits  fp32 [lists, top] device; -inf: an entry of p 0
+ *   teacher_rows    int32 [rows] device or NULL (row r has list r; lists >=
+ *               rows): the list of each row, such as the trajectory token of
+ *               a trainable segment token
+ *   weights     fp32 [rows] device.  A row of weight 0 is not read: its
+ *               row_kl and dlogits are 0
+ *   temperature T, positive and finite
+ *   loss        fp32 device, 1 value (written): a double sum, in row order
+ *   row_kl      fp32 [rows] device (written); 0 of a row without entries, or
+ *               none of whose entries has a finite logit
+ *   dlogits     as logits, with dlogits_stride, or NULL; may be logits itself
+ *               (with the same stride), otherwise they must not overlap.
+ *               Columns from vocab on are left as they were
+ *   ws          device workspace of vcs_distill_topk_workspace_size(rows)
+ *               bytes, 256-byte aligned; its first int32 is the device status
+ *               word: VCS_ERR_DEVICE_CHECK for an id outside [-1, vocab) (read
+ *               as -1) or a list outside [0, lists) (read as empty)
+ * Sums and statistics are fp32 and wider; the same inputs give the same bits.
+ * Returns VCS_ERR_INVALID_ARG for negative counts, vocab or top of 0, a null
+ * pointer, one that is not aligned to its elements, a stride below vocab, a
+ * bad temperature, lists < rows without teacher_rows, or overlap;
+ * VCS_ERR_UNSUPPORTED for another logits_type or more than VCS_DISTILL_MAX_TOP
+ * entries; VCS_ERR_OVERFLOW for rows, lists or vocab above INT32_MAX;
+ * VCS_ERR_WORKSPACE.
+ * ------------------------------------------------------------------------ */
+#define VCS_BF16 0
+#define VCS_F32 1
+#define VCS_DISTILL_MAX_TOP 1024
+
+size_t vcs_distill_topk_workspace_size(int64_t rows);
+
+vcs_status vcs_distill_topk(const void* logits, int32_t logits_type, int64_t rows, int64_t vocab,
+                            int64_t logits_stride, const int32_t* teacher_ids, const float* teacher_logits,
+                            int32_t top, int64_t lists, const int32_t* teacher_rows, const float* weights,
+                            float temperature, float* loss, float* row_kl, void* dlogits, int64_t dlogits_stride,
+                            void* ws, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------------------ *
  * Self-test of the bounded device waits.
  *

@@ -49,6 +49,56 @@ vcs_status check_attn(const AttnArgs& a) {
   return VCS_OK;
 }
 
+struct Span {
+  const void* p;
+  uint64_t bytes;
+};
+
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p != nullptr && b.p != nullptr && x < y + b.bytes && y < x + a.bytes;
+}
+
+// Null and alignment of every span that holds anything, and that no output overlaps another or an input.
+template <int I, int O>
+bool spans_ok(const Span (&in)[I], const Span (&out)[O]) {
+  for (const Span& s : in)
+    if (s.bytes > 0 && (s.p == nullptr || !aligned16(s.p))) return false;
+  for (int i = 0; i < O; ++i) {
+    if (out[i].bytes > 0 && (out[i].p == nullptr || !aligned16(out[i].p))) return false;
+    for (const Span& s : in)
+      if (overlap(out[i], s)) return false;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return false;
+  }
+  return true;
+}
+
+LinearArgs linear_args(const void* q, const void* k, const void* v, const float* log_decay, const int32_t* cu_seqlens,
+                       int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv, int32_t d, float scale) {
+  LinearArgs a;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.log_decay = log_decay;
+  a.cu_seqlens = cu_seqlens;
+  a.num_segments = num_segments;
+  a.num_tokens = num_tokens;
+  a.hq = hq;
+  a.hkv = hkv;
+  a.d = d;
+  a.scale = (scale > 0.f && std::isfinite(scale)) ? scale : 1.0f / std::sqrt((float)(d > 0 ? d : 1));
+  return a;
+}
+
+vcs_status check_linear(const LinearArgs& a) {
+  if (a.num_segments < 0 || a.num_tokens < 0 || a.hq <= 0 || a.hkv <= 0 || a.log_decay == nullptr)
+    return VCS_ERR_INVALID_ARG;
+  if (a.num_tokens > INT32_MAX - 256) return VCS_ERR_OVERFLOW;
+  if ((a.d != 64 && a.d != 128) || a.hq % a.hkv != 0 || a.hq > 65535) return VCS_ERR_UNSUPPORTED;
+  return VCS_OK;
+}
+
 }  // namespace
 
 bool encode_tma_3d_bf16(void* map, const void* base, uint64_t d, uint64_t heads, uint64_t tokens, uint32_t box_d,
@@ -414,6 +464,138 @@ vcs_status vcs_gather_rope_bwd(const void* dq, const void* dk, const void* dv, i
   if (launch_gather_rope(dq, dk, dv, num_tokens, traj_tokens, pos, num_tokens, inv_tok, inv_off, true, hq, hkv, d,
                          *rope, dq_traj, dk_traj, dv_traj, dev_status, as_stream(stream)) != cudaSuccess)
     return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+// ---------------------------------------------------------------- linear attention
+size_t vcs_linear_attn_fwd_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv,
+                                          int32_t d) {
+  if (num_segments < 0 || num_tokens < 0 || hq <= 0 || hkv <= 0 || d <= 0) return 0;
+  return linear_fwd_ws_bytes(num_segments, num_tokens, hq, hkv, d);
+}
+
+vcs_status vcs_linear_attn_fwd(const void* q, const void* k, const void* v, const float* log_decay,
+                               const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, float scale, const float* state_in, float* state_out, void* o,
+                               void* ws, size_t ws_bytes, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_linear_attn_fwd");
+  const LinearArgs a = linear_args(q, k, v, log_decay, cu_seqlens, num_segments, num_tokens, hq, hkv, d, scale);
+  if (const vcs_status s = check_linear(a); s != VCS_OK) return s;
+  if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
+  const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
+  const uint64_t ns = (uint64_t)num_segments * hkv * d * d * 4;
+  const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {state_in, state_in == nullptr ? 0 : ns}};
+  const Span out[] = {{o, nq}, {state_out, state_out == nullptr ? 0 : ns}};
+  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < linear_fwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
+      (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  if (num_segments == 0 || (num_tokens == 0 && state_out == nullptr)) return clear_header(ws, as_stream(stream));
+  if (launch_linear_fwd(a, state_in, state_out, o, ws, as_stream(stream)) != cudaSuccess) return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+size_t vcs_linear_attn_bwd_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv,
+                                          int32_t d) {
+  if (num_segments < 0 || num_tokens < 0 || hq <= 0 || hkv <= 0 || d <= 0) return 0;
+  return linear_bwd_ws_bytes(num_segments, num_tokens, hq, hkv, d);
+}
+
+vcs_status vcs_linear_attn_bwd(const void* q, const void* k, const void* v, const void* dout, const float* log_decay,
+                               const int32_t* cu_seqlens, int32_t num_segments, int64_t num_tokens, int32_t hq,
+                               int32_t hkv, int32_t d, float scale, void* dq, void* dk, void* dv, void* ws,
+                               size_t ws_bytes, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_linear_attn_bwd");
+  const LinearArgs a = linear_args(q, k, v, log_decay, cu_seqlens, num_segments, num_tokens, hq, hkv, d, scale);
+  if (const vcs_status s = check_linear(a); s != VCS_OK) return s;
+  if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
+  const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
+  const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {dout, nq}};
+  const Span out[] = {{dq, nq}, {dk, nk}, {dv, nk}};
+  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < linear_bwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
+      (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  if (num_segments == 0 || num_tokens == 0) return clear_header(ws, as_stream(stream));
+  if (launch_linear_bwd(a, dout, dq, dk, dv, ws, as_stream(stream)) != cudaSuccess) return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, const float* log_decay, int64_t num_seqs,
+                                int32_t hq, int32_t hkv, int32_t d, float scale, float* states, void* o,
+                                int32_t* dev_status, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_linear_attn_step");
+  const LinearArgs a = linear_args(q, k, v, log_decay, nullptr, 0, num_seqs, hq, hkv, d, scale);
+  if (const vcs_status s = check_linear(a); s != VCS_OK) return s;
+  const uint64_t nq = (uint64_t)num_seqs * hq * d * 2, nk = (uint64_t)num_seqs * hkv * d * 2;
+  const Span in[] = {{q, nq}, {k, nk}, {v, nk}};
+  const Span out[] = {{states, (uint64_t)num_seqs * hkv * d * d * 4}, {o, nq}};
+  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (num_seqs == 0) return VCS_OK;
+  if (launch_linear_step(a, states, o, dev_status, as_stream(stream)) != cudaSuccess) return VCS_ERR_CUDA;
+  return VCS_OK;
+}
+
+// ---------------------------------------------------------------- distillation
+size_t vcs_distill_topk_workspace_size(int64_t rows) { return distill_ws_bytes(rows < 0 ? 0 : rows); }
+
+vcs_status vcs_distill_topk(const void* logits, int32_t logits_type, int64_t rows, int64_t vocab,
+                            int64_t logits_stride, const int32_t* teacher_ids, const float* teacher_logits,
+                            int32_t top, int64_t lists, const int32_t* teacher_rows, const float* weights,
+                            float temperature, float* loss, float* row_kl, void* dlogits, int64_t dlogits_stride,
+                            void* ws, size_t ws_bytes, void* stream) {
+  vcs::ApiRange nvtx_range("vcs_distill_topk");
+  if (rows < 0 || lists < 0 || vocab <= 0 || top <= 0 || loss == nullptr) return VCS_ERR_INVALID_ARG;
+  if (logits_type != VCS_BF16 && logits_type != VCS_F32) return VCS_ERR_UNSUPPORTED;
+  if (top > VCS_DISTILL_MAX_TOP) return VCS_ERR_UNSUPPORTED;
+  if (rows > INT32_MAX || lists > INT32_MAX || vocab > INT32_MAX) return VCS_ERR_OVERFLOW;
+  if (logits_stride < vocab || (dlogits != nullptr && dlogits_stride < vocab)) return VCS_ERR_INVALID_ARG;
+  const int64_t size = logits_type == VCS_F32 ? 4 : 2;
+  if (logits_stride > INT64_MAX / (size * (rows + 1)) || dlogits_stride > INT64_MAX / (size * (rows + 1)))
+    return VCS_ERR_OVERFLOW;
+  if (!(temperature > 0.f) || !std::isfinite(temperature)) return VCS_ERR_INVALID_ARG;
+  if (teacher_rows == nullptr && lists < rows) return VCS_ERR_INVALID_ARG;
+  auto off = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
+  if (rows > 0 && (logits == nullptr || weights == nullptr || row_kl == nullptr ||
+                   (lists > 0 && (teacher_ids == nullptr || teacher_logits == nullptr))))
+    return VCS_ERR_INVALID_ARG;
+  if (off(logits, size) || off(dlogits, size) || off(teacher_ids, 4) || off(teacher_logits, 4) ||
+      off(teacher_rows, 4) || off(weights, 4) || off(loss, 4) || off(row_kl, 4))
+    return VCS_ERR_INVALID_ARG;
+  if (rows > 0) {
+    auto bytes = [&](int64_t stride) { return (uint64_t)((rows - 1) * stride + vocab) * size; };
+    const Span z{logits, bytes(logits_stride)}, g{dlogits, dlogits == nullptr ? 0 : bytes(dlogits_stride)};
+    const uint64_t n = (uint64_t)lists * top * 4, r = (uint64_t)rows * 4;
+    const Span in[] = {z, {teacher_ids, n}, {teacher_logits, n}, {teacher_rows, r}, {weights, r}};
+    const Span out[] = {g, {loss, 4}, {row_kl, r}};
+    const bool in_place = dlogits == logits && dlogits_stride == logits_stride;
+    for (int i = 0; i < 3; ++i) {
+      for (int j = 0; j < 5; ++j)
+        if (!(i == 0 && j == 0 && in_place) && overlap(out[i], in[j])) return VCS_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (overlap(out[i], out[j])) return VCS_ERR_INVALID_ARG;
+    }
+  }
+  if (ws == nullptr || ws_bytes < distill_ws_bytes(rows) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
+    return VCS_ERR_WORKSPACE;
+  DistillArgs a;
+  a.logits = logits;
+  a.f32 = logits_type == VCS_F32;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.stride = logits_stride;
+  a.ids = teacher_ids;
+  a.teacher = teacher_logits;
+  a.top = top;
+  a.lists = lists;
+  a.map = teacher_rows;
+  a.weights = weights;
+  a.temperature = temperature;
+  a.loss = loss;
+  a.row_kl = row_kl;
+  a.dlogits = dlogits;
+  a.grad_stride = dlogits_stride;
+  if (launch_distill(a, ws, as_stream(stream)) != cudaSuccess) return VCS_ERR_CUDA;
   return VCS_OK;
 }
 

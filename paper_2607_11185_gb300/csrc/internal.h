@@ -123,6 +123,46 @@ cudaError_t launch_gather_rope(const void* q_in, const void* k_in, const void* v
                                bool backward, int32_t hq, int32_t hkv, int32_t d, const vcs_rope& rope, void* q_out,
                                void* k_out, void* v_out, int32_t* status, cudaStream_t st);
 
+// ---- linear attention over segments (linear.cu) ----
+struct LinearArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* log_decay;
+  const int32_t* cu_seqlens;
+  int32_t num_segments;
+  int64_t num_tokens;  // of a step, its sequences
+  int32_t hq, hkv, d;
+  float scale;
+};
+size_t linear_fwd_ws_bytes(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv, int32_t d);
+cudaError_t launch_linear_fwd(const LinearArgs& a, const float* state_in, float* state_out, void* o, void* ws,
+                              cudaStream_t st);
+size_t linear_bwd_ws_bytes(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv, int32_t d);
+cudaError_t launch_linear_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk, void* dv, void* ws,
+                              cudaStream_t st);
+cudaError_t launch_linear_step(const LinearArgs& a, float* states, void* o, int32_t* status, cudaStream_t st);
+
+// ---- distillation from a teacher's top logits (distill.cu) ----
+struct DistillArgs {
+  const void* logits;
+  bool f32;
+  int64_t rows, vocab, stride;
+  const int32_t* ids;
+  const float* teacher;
+  int32_t top;
+  int64_t lists;
+  const int32_t* map;
+  const float* weights;
+  float temperature;
+  float* loss;
+  float* row_kl;
+  void* dlogits;
+  int64_t grad_stride;
+};
+size_t distill_ws_bytes(int64_t rows);
+cudaError_t launch_distill(const DistillArgs& a, void* ws, cudaStream_t st);
+
 // TMA descriptor encoding through the driver entry point (no libcuda link).
 bool encode_tma_3d_bf16(void* map /*CUtensorMap*/, const void* base, uint64_t d, uint64_t heads, uint64_t tokens,
                         uint32_t box_d, uint32_t box_rows);

@@ -99,6 +99,16 @@ _lib_bwd_w_ws = _sig("vcs_attn_bwd_window_workspace_size", _sz, [_i32, _i64, _i3
 _lib_bwd_w = _sig("vcs_attn_bwd_window", _i32,
                   [_p, _p, _p, _p, _p, _p, _p, _i32, _i64, _i32, _i32, _i32, _i32, _f32, _i32, _i32, _p, _p, _p, _p,
                    _sz, _p])
+_lib_lin_fwd_ws = _sig("vcs_linear_attn_fwd_workspace_size", _sz, [_i32, _i64, _i32, _i32, _i32])
+_lib_lin_fwd = _sig("vcs_linear_attn_fwd", _i32,
+                    [_p, _p, _p, _p, _p, _i32, _i64, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _sz, _p])
+_lib_lin_bwd_ws = _sig("vcs_linear_attn_bwd_workspace_size", _sz, [_i32, _i64, _i32, _i32, _i32])
+_lib_lin_bwd = _sig("vcs_linear_attn_bwd", _i32,
+                    [_p, _p, _p, _p, _p, _p, _i32, _i64, _i32, _i32, _i32, _f32, _p, _p, _p, _p, _sz, _p])
+_lib_lin_step = _sig("vcs_linear_attn_step", _i32, [_p, _p, _p, _p, _i64, _i32, _i32, _i32, _f32, _p, _p, _p, _p])
+_lib_distill_ws = _sig("vcs_distill_topk_workspace_size", _sz, [_i64])
+_lib_distill = _sig("vcs_distill_topk", _i32,
+                    [_p, _i32, _i64, _i64, _i64, _p, _p, _i32, _i64, _p, _p, _f32, _p, _p, _p, _i64, _p, _sz, _p])
 _lib_selftest_wait = _sig("vcs_selftest_bounded_wait", _i32, [_p, _i64, _p])
 
 EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "vcs_plan_segments",
@@ -109,6 +119,8 @@ EXPORTED = ["vcs_status_string", "vcs_version", "vcs_segments_workspace_size", "
             "vcs_attn_bwd_gathered", "vcs_shared_prefix", "vcs_attn_fwd_reuse", "vcs_stream_positions", "vcs_rope_init",
             "vcs_gather_rope", "vcs_gather_inverse_workspace_size", "vcs_gather_inverse", "vcs_gather_rope_bwd",
             "vcs_attn_fwd_window", "vcs_attn_bwd_window_workspace_size", "vcs_attn_bwd_window",
+            "vcs_linear_attn_fwd_workspace_size", "vcs_linear_attn_fwd", "vcs_linear_attn_bwd_workspace_size",
+            "vcs_linear_attn_bwd", "vcs_linear_attn_step", "vcs_distill_topk_workspace_size", "vcs_distill_topk",
             "vcs_selftest_bounded_wait"]
 
 LIB_PATH = _LIB_PATH
@@ -325,6 +337,44 @@ def vcs_gather_rope_bwd(dq, dk, dv, num_tokens, pos, inv_off, inv_tok, traj_toke
     return _lib_gather_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), num_tokens, _ptr(pos), _ptr(inv_off), _ptr(inv_tok),
                                 traj_tokens, hq, hkv, d, _ptr(rope), _ptr(dq_traj), _ptr(dk_traj), _ptr(dv_traj),
                                 _ptr(dev_status), _stream(stream))
+
+
+def vcs_linear_attn_fwd_workspace_size(num_segments, num_tokens, hq, hkv, d) -> int:
+    return int(_lib_lin_fwd_ws(num_segments, num_tokens, hq, hkv, d))
+
+
+def vcs_linear_attn_fwd(q, k, v, log_decay, cu_seqlens, num_segments, num_tokens, hq, hkv, d, scale, state_in,
+                        state_out, o, ws, ws_bytes, stream=None) -> int:
+    return _lib_lin_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(cu_seqlens), num_segments, num_tokens, hq,
+                        hkv, d, scale, _ptr(state_in), _ptr(state_out), _ptr(o), _ptr(ws), ws_bytes, _stream(stream))
+
+
+def vcs_linear_attn_bwd_workspace_size(num_segments, num_tokens, hq, hkv, d) -> int:
+    return int(_lib_lin_bwd_ws(num_segments, num_tokens, hq, hkv, d))
+
+
+def vcs_linear_attn_bwd(q, k, v, dout, log_decay, cu_seqlens, num_segments, num_tokens, hq, hkv, d, scale, dq, dk, dv,
+                        ws, ws_bytes, stream=None) -> int:
+    return _lib_lin_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(log_decay), _ptr(cu_seqlens), num_segments,
+                        num_tokens, hq, hkv, d, scale, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), ws_bytes,
+                        _stream(stream))
+
+
+def vcs_linear_attn_step(q, k, v, log_decay, num_seqs, hq, hkv, d, scale, states, o, dev_status, stream=None) -> int:
+    return _lib_lin_step(_ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), num_seqs, hq, hkv, d, scale, _ptr(states),
+                         _ptr(o), _ptr(dev_status), _stream(stream))
+
+
+def vcs_distill_topk_workspace_size(rows: int) -> int:
+    return int(_lib_distill_ws(rows))
+
+
+def vcs_distill_topk(logits, logits_type, rows, vocab, logits_stride, teacher_ids, teacher_logits, top, lists,
+                     teacher_rows, weights, temperature, loss, row_kl, dlogits, dlogits_stride, ws, ws_bytes,
+                     stream=None) -> int:
+    return _lib_distill(_ptr(logits), logits_type, rows, vocab, logits_stride, _ptr(teacher_ids),
+                        _ptr(teacher_logits), top, lists, _ptr(teacher_rows), _ptr(weights), temperature, _ptr(loss),
+                        _ptr(row_kl), _ptr(dlogits), dlogits_stride, _ptr(ws), ws_bytes, _stream(stream))
 
 
 def vcs_selftest_bounded_wait(dev_status, limit_cycles, stream=None) -> int:
@@ -808,6 +858,127 @@ def group_advantage(rewards, group_size: int, eps: float = 1e-6, stream=None):
     _check(vcs_group_advantage(rewards, rewards.numel() // group_size, group_size, eps, adv),
            "vcs_group_advantage")
     return adv
+
+
+def _expect_linear(where: str, q, k, v, log_decay):
+    bf16 = torch.bfloat16
+    _expect(where, ("q", q, bf16, 3), ("k", k, bf16, 3))
+    kv = (q.shape[0], k.shape[1], q.shape[2])
+    _expect(where, ("k", k, bf16, kv), ("v", v, bf16, kv), ("log_decay", log_decay, torch.float32, (kv[1],)))
+
+
+def linear_attn_fwd(q, k, v, log_decay, cu_seqlens, scale: float = 0.0, state=None, with_state: bool = False,
+                    stream=None, check=True):
+    """Linear attention over the segments, log_decay [hkv] at most 0: (o [num_tokens, hq, d], the states behind the
+    segments [num_segments, hkv, d, d] fp32, or None without with_state).  `state`: the states before them."""
+    if stream is not None:
+        return _on_stream(stream, linear_attn_fwd, q, k, v, log_decay, cu_seqlens, scale, state, with_state,
+                          check=check)
+    _expect_linear("linear_attn_fwd", q, k, v, log_decay)
+    nt, hq, d = q.shape
+    hkv = k.shape[1]
+    _expect("linear_attn_fwd", ("cu_seqlens", cu_seqlens, torch.int32, 1))
+    ns = cu_seqlens.numel() - 1
+    if state is not None:
+        _expect("linear_attn_fwd", ("state", state, torch.float32, (ns, hkv, d, d)))
+    o = torch.empty_like(q)
+    out = torch.empty((max(ns, 0), hkv, d, d), dtype=torch.float32, device=q.device) if with_state else None
+    nb = vcs_linear_attn_fwd_workspace_size(ns, nt, hq, hkv, d)
+    ws = _ws(nb, q.device)
+    _check(vcs_linear_attn_fwd(q, k, v, log_decay, cu_seqlens, ns, nt, hq, hkv, d, scale, state, out, o, ws, nb),
+           "vcs_linear_attn_fwd")
+    if check:
+        _check(int(ws[0].item()), "vcs_linear_attn_fwd (device)")
+    return o, out
+
+
+def linear_attn_bwd(q, k, v, dout, log_decay, cu_seqlens, scale: float = 0.0, stream=None, check=True):
+    """dq, dk, dv of linear_attn_fwd without a state."""
+    if stream is not None:
+        return _on_stream(stream, linear_attn_bwd, q, k, v, dout, log_decay, cu_seqlens, scale, check=check)
+    _expect_linear("linear_attn_bwd", q, k, v, log_decay)
+    nt, hq, d = q.shape
+    hkv = k.shape[1]
+    _expect("linear_attn_bwd", ("dout", dout, q.dtype, q.shape), ("cu_seqlens", cu_seqlens, torch.int32, 1))
+    ns = cu_seqlens.numel() - 1
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    nb = vcs_linear_attn_bwd_workspace_size(ns, nt, hq, hkv, d)
+    ws = _ws(nb, q.device)
+    _check(vcs_linear_attn_bwd(q, k, v, dout, log_decay, cu_seqlens, ns, nt, hq, hkv, d, scale, dq, dk, dv, ws, nb),
+           "vcs_linear_attn_bwd")
+    if check:
+        _check(int(ws[0].item()), "vcs_linear_attn_bwd (device)")
+    return dq, dk, dv
+
+
+def linear_attn_step(q, k, v, log_decay, states, scale: float = 0.0, stream=None, check=True):
+    """linear_attn_fwd of one token of each sequence: o [num_seqs, hq, d]; states [num_seqs, hkv, d, d] fp32 are
+    updated in place."""
+    if stream is not None:
+        return _on_stream(stream, linear_attn_step, q, k, v, log_decay, states, scale, check=check)
+    _expect_linear("linear_attn_step", q, k, v, log_decay)
+    n, hq, d = q.shape
+    hkv = k.shape[1]
+    _expect("linear_attn_step", ("states", states, torch.float32, (n, hkv, d, d)))
+    o = torch.empty_like(q)
+    word = _word(check)
+    _checked(vcs_linear_attn_step(q, k, v, log_decay, n, hq, hkv, d, scale, states, o, word), word,
+             "vcs_linear_attn_step")
+    return o
+
+
+_LOGITS = {torch.bfloat16: 0, torch.float32: 1}  # VCS_BF16, VCS_F32
+
+
+def _expect_rows(where: str, name: str, t, dtype, shape):
+    """As _expect, but rows may be apart: a [rows, vocab] tensor whose columns are consecutive."""
+    ok = t.dim() == 2 and t.is_cuda and t.get_device() == torch.cuda.current_device() and t.dtype is dtype
+    if not (ok and (shape is None or t.shape == shape)):
+        _refuse(where, name, t, dtype, 2 if shape is None else shape) if t.is_contiguous() else \
+            _refuse(where, name, t.contiguous(), dtype, 2 if shape is None else shape)
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{where}: the rows of {name} overlap or their columns are not consecutive")
+
+
+def distill_topk(logits, teacher_ids, teacher_logits, weights, teacher_rows=None, temperature: float = 1.0,
+                 with_grad: bool = True, out=None, stream=None, check=True):
+    """Weighted divergence of rows of logits [rows, vocab] (bf16 or fp32; rows may be apart) from a teacher's top entries
+    [lists, top], and its gradient: (loss [1] fp32, row_kl [rows] fp32, dlogits or None).  teacher_rows [rows] int32: the
+    list of each row (default: its own).  out: where dlogits goes, which may be logits itself."""
+    if stream is not None:
+        return _on_stream(stream, distill_topk, logits, teacher_ids, teacher_logits, weights, teacher_rows, temperature,
+                          with_grad, out, check=check)
+    where = "distill_topk"
+    if logits.dtype not in _LOGITS:
+        raise ValueError(f"{where}: logits is {logits.dtype}, not torch.bfloat16 or torch.float32")
+    _expect_rows(where, "logits", logits, logits.dtype, None)
+    rows, vocab = logits.shape
+    _expect(where, ("teacher_ids", teacher_ids, torch.int32, 2))
+    lists, top = teacher_ids.shape
+    _expect(where, ("teacher_logits", teacher_logits, torch.float32, (lists, top)),
+            ("weights", weights, torch.float32, (rows,)))
+    if teacher_rows is not None:
+        _expect(where, ("teacher_rows", teacher_rows, torch.int32, (rows,)))
+    if out is not None:
+        if not with_grad:
+            raise ValueError(f"{where}: out is where the gradient goes, which with_grad=False leaves out")
+        _expect_rows(where, "out", out, logits.dtype, logits.shape)
+    dev = logits.device
+    dlogits = out if out is not None else torch.empty((rows, vocab), dtype=logits.dtype, device=dev) if with_grad else None
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    row_kl = torch.empty(rows, dtype=torch.float32, device=dev)
+    nb = vcs_distill_topk_workspace_size(rows)
+    ws = _ws(nb, dev)
+
+    def step(t):  # of a single row torch leaves any stride
+        return t.stride(0) if t is not None and rows > 1 else vocab
+
+    _check(vcs_distill_topk(logits, _LOGITS[logits.dtype], rows, vocab, step(logits), teacher_ids, teacher_logits, top,
+                            lists, teacher_rows, weights, temperature, loss, row_kl, dlogits, step(dlogits), ws, nb),
+           "vcs_distill_topk")
+    if check:
+        _check(int(ws[0].item()), "vcs_distill_topk (device)")
+    return loss, row_kl, dlogits
 
 
 def selftest_bounded_wait(limit_cycles: int = 200_000_000, device="cuda", stream=None) -> int:
