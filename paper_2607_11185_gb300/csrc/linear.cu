@@ -7,6 +7,16 @@
 //   dk_t = scale R_t v_t    (queries v, keys do, values q, from the last token to the first)
 //   dv_t = scale R_t^T k_t  (queries k, keys q, values do, likewise)
 // where the first has a group of query heads to a state, the others a group of key heads.
+//
+// Chunks of 128 tokens.  From the state S before a chunk's first token, for its n tokens i, j = 0 .. n - 1:
+//   o_i = scale [ lam^(i+1) q_i S + sum_{j <= i} lam^(i-j) (q_i . k_j) v_j ],
+//   S'  = lam^n S + sum_j lam^(n-1-j) k_j v_j^T
+// four 128-wide products a chunk on the tensor pipe (the other way in time: lam^(n-i), j >= i, lam^j).
+//
+// A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among the
+// CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.  linear_states
+// adds up the keys and values of every such piece first; each CTA then puts its starting state together from the
+// pieces before it.  So a cut costs its piece's keys and values read twice.
 #include <cfloat>
 #include <cstdint>
 
@@ -19,84 +29,1011 @@ namespace {
 using namespace dev;
 using bf16 = __nv_bfloat16;
 
+constexpr int kGrid = 152;   // a CTA an SM
+constexpr int kChunk = 128;
+// Sequences up to this many chunks are not cut where all are: a CTA takes those that start in its range.
+constexpr int kWhole = 16;
+
 __device__ __forceinline__ bool decay_ok(float g) { return g <= 0.f && g >= -FLT_MAX; }
 
-struct WalkArgs {
-  const bf16 *q, *k, *v;  // [tokens, state heads * gq], [tokens, state heads * gk] twice
+// ------------------------------------------------------------------ division of the work
+struct Plan {        // in the workspace header, behind the status word
+  int64_t total;     // chunks of all sequences
+  int64_t range;     // of a CTA
+  int32_t cut;       // sequences are cut at the ranges' ends
+};
+constexpr size_t kWsPlan = 64;
+
+__device__ __forceinline__ int seg_chunks(const int32_t* __restrict__ cu, int32_t num_tokens, int s, int32_t* status) {
+  const int start = cu[s], end = cu[s + 1];
+  if (start < 0 || end < start || end > num_tokens) {
+    set_status(status, VCS_ERR_DEVICE_CHECK);
+    return 0;
+  }
+  return (end - start + kChunk - 1) / kChunk;
+}
+
+// off[s] = chunks of segments 0 .. s - 1, and the plan.  The call's first kernel: it clears the status word.
+__global__ void __launch_bounds__(1024) linear_plan(const int32_t* __restrict__ cu, int32_t num_segments,
+                                                    int32_t num_tokens, int32_t heads, int32_t grid, int32_t* off,
+                                                    Plan* plan, int32_t* status) {
+  __shared__ long long wsum[32];
+  __shared__ long long carry;
+  __shared__ int longest;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    carry = 0;
+    longest = 0;
+    *reinterpret_cast<volatile int32_t*>(status) = VCS_OK;
+  }
+  __syncthreads();
+  const long long most = (long long)num_tokens / kChunk + num_segments;  // segments that overlap may pass it
+  for (int base = 0; base < num_segments; base += 1024) {
+    const int s = base + (int)threadIdx.x;
+    const int n = s < num_segments ? seg_chunks(cu, num_tokens, s, status) : 0;
+    if (n > 0) atomicMax(&longest, n);
+    long long x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) wsum[wid] = x;
+    __syncthreads();
+    if (wid == 0) {
+      long long w = wsum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+      }
+      wsum[lane] = w;
+    }
+    __syncthreads();
+    const long long incl = carry + (wid > 0 ? wsum[wid - 1] : 0) + x;
+    if (s < num_segments) off[s] = (int32_t)(incl - n < most ? incl - n : most);
+    __syncthreads();
+    if (threadIdx.x == 1023) carry = incl;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    if (carry > most) set_status(status, VCS_ERR_DEVICE_CHECK);
+    const long long all = carry > most ? 0 : carry * heads;
+    off[num_segments] = (int32_t)(carry > most ? 0 : carry);
+    plan->total = all;
+    plan->cut = longest > kWhole;
+    plan->range = (all + grid - 1) / grid;
+  }
+}
+
+struct Common {
   const float* log_decay;
-  const int32_t* cu_seqlens;
-  int32_t num_segments, num_tokens, heads, gq, gk;
-  float scale;
-  bool back;  // from each segment's last token to its first
-  const float* state_in;
-  float* state_out;
-  bf16* o;
+  const int32_t* cu;
+  const int32_t* off;
+  const Plan* plan;
+  int32_t num_segments, num_tokens, heads;
   int32_t* status;
 };
 
-constexpr int kCols = 32, kGroups = 8;
-
-// Token by token.  A block holds 32 columns of one head's state in registers, thread (g, c) rows g D/8 .. of column c.
-template <int D>
-__global__ void __launch_bounds__(256) linear_walk(const __grid_constant__ WalkArgs a) {
-  constexpr int R = D / kGroups;
-  __shared__ float sk[D], sq[D], sv[kCols], red[kGroups * kCols];
-  const int slices = D / kCols;
-  const int unit = blockIdx.x / slices, col0 = blockIdx.x % slices * kCols;
-  const int seg = unit / a.heads, head = unit % a.heads;
-  const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
-  const int start = a.cu_seqlens[seg], end = a.cu_seqlens[seg + 1];
-  const float ld = a.log_decay[head];
-  if (start < 0 || end < start || end > a.num_tokens || !decay_ok(ld)) {
-    if (threadIdx.x == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
-    return;
+// The pieces of CTA b's range, one after another: chunks c0 .. c1 of a sequence.
+struct Walk {
+  const Common& a;
+  int64_t g, hi, base, range;
+  int seg, head, nch, start, len, c0, c1;
+  float l2;     // log2 of the decay
+  bool cut, located;
+  __device__ __forceinline__ Walk(const Common& a, int b) : a(a) {
+    const int64_t total = a.plan->total;
+    range = a.plan->range;
+    cut = a.plan->cut != 0;
+    g = range * b < total ? range * b : total;
+    hi = range * (b + 1) < total ? range * (b + 1) : total;
+    located = false;
   }
-  const float lam = expf(ld);
-  float s[R];
-  const size_t at = ((size_t)unit * D + g * R) * D + col0 + c;
-#pragma unroll
-  for (int i = 0; i < R; ++i) s[i] = a.state_in != nullptr ? a.state_in[at + (size_t)i * D] : 0.f;
-  for (int n = 0; n < end - start; ++n) {
-    const size_t t = a.back ? end - 1 - n : start + n;
-#pragma unroll
-    for (int i = 0; i < R; ++i) s[i] *= lam;
-    for (int h = 0; h < a.gk; ++h) {
-      const size_t row = (t * a.heads + head) * a.gk + h;
-      __syncthreads();
-      if (threadIdx.x < D) sk[threadIdx.x] = __bfloat162float(a.k[row * D + threadIdx.x]);
-      if (threadIdx.x < kCols) sv[threadIdx.x] = __bfloat162float(a.v[row * D + col0 + threadIdx.x]);
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < R; ++i) s[i] += sk[g * R + i] * sv[c];
+  __device__ __forceinline__ void locate(int64_t at) {  // the sequence that holds chunk `at` < total
+    const int q = (int)(at / a.heads);
+    int lo = 0, up = a.num_segments;  // off[lo] <= q < off[up]
+    while (up - lo > 1) {
+      const int mid = (lo + up) >> 1;
+      if (__ldg(&a.off[mid]) <= q) lo = mid;
+      else up = mid;
     }
-    for (int h = 0; h < a.gq; ++h) {
-      const size_t row = (t * a.heads + head) * a.gq + h;
-      if (threadIdx.x < D) sq[threadIdx.x] = __bfloat162float(a.q[row * D + threadIdx.x]);
-      __syncthreads();
-      float x = 0.f;
-#pragma unroll
-      for (int i = 0; i < R; ++i) x += sq[g * R + i] * s[i];
-      red[g * kCols + c] = x;
-      __syncthreads();
-      if (g == 0) {
-#pragma unroll
-        for (int i = 1; i < kGroups; ++i) x += red[i * kCols + c];
-        a.o[row * D + col0 + c] = __float2bfloat16(a.scale * x);
+    seg = lo;
+    const int first = __ldg(&a.off[seg]);
+    nch = __ldg(&a.off[seg + 1]) - first;
+    const int64_t rest = at - (int64_t)first * a.heads;
+    head = (int)(rest / nch);
+    base = (int64_t)first * a.heads + (int64_t)head * nch;
+    bounds();
+    located = true;
+  }
+  __device__ __forceinline__ void bounds() {
+    start = __ldg(&a.cu[seg]);
+    len = __ldg(&a.cu[seg + 1]) - start;
+  }
+  __device__ __forceinline__ bool next() {
+    while (true) {
+      if (g >= hi) return false;
+      if (!located) {
+        locate(g);
+        if (!cut && g != base) {  // it started in an earlier range
+          g = base + nch;
+          if (g >= hi) return false;
+          advance();
+        }
+      } else {
+        advance();
       }
-      __syncthreads();
+      c0 = (int)(g - base);
+      c1 = cut && hi - base < nch ? (int)(hi - base) : nch;
+      g = base + c1;
+      const float ld = __ldg(&a.log_decay[head]);
+      l2 = ld * 1.4426950408889634f;
+      if (decay_ok(ld)) return true;
+      set_status(a.status, VCS_ERR_DEVICE_CHECK);
     }
   }
-  if (a.state_out != nullptr)
-#pragma unroll
-    for (int i = 0; i < R; ++i) a.state_out[at + (size_t)i * D] = s[i];
+  __device__ __forceinline__ void advance() {  // to the sequence behind this one
+    base += nch;
+    if (++head < a.heads) return;
+    head = 0;
+    do ++seg;
+    while (__ldg(&a.off[seg + 1]) == __ldg(&a.off[seg]));
+    nch = __ldg(&a.off[seg + 1]) - __ldg(&a.off[seg]);
+    bounds();
+  }
+  __device__ __forceinline__ int rows(int c) const { return min(kChunk, len - c * kChunk); }
+};
+
+// ------------------------------------------------------------------ shared pieces
+__device__ __forceinline__ void tma_store_3d(const void* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+               "r"(src), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
+__device__ __forceinline__ void set_abort(int32_t* abort, int32_t* status) {
+  set_status(status, VCS_ERR_DEVICE_TIMEOUT);
+  *reinterpret_cast<volatile int32_t*>(abort) = 1;
 }
 
+__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Row r of a 128 x D tile (64-column blocks of 128-byte rows) set to zero.
 template <int D>
-cudaError_t launch_walk(const WalkArgs& a, cudaStream_t st) {
-  const int64_t blocks = (int64_t)a.num_segments * a.heads * (D / kCols);
-  if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  if (blocks > 0) linear_walk<D><<<(unsigned)blocks, 256, 0, st>>>(a);
-  return cudaGetLastError();
+__device__ __forceinline__ void zero_row(uint32_t tile, int r) {
+#pragma unroll
+  for (int kb = 0; kb < D / 64; ++kb)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) st_shared_v4(tile + kb * 16384 + r * 128 + (((u + r) & 7) << 4), 0u, 0u, 0u, 0u);
+}
+
+// ------------------------------------------------------------------ states of the pieces
+// TERMS: bf16 terms that a weighted key is split into.  Where the states are results (state_out) there are three,
+// which hold its 24 bits; where queries read them, rounded to bf16 themselves, one.
+struct StateArgs {
+  Common c;
+  float* slots;            // [grid][D][D]
+  const float* state_in;   // state_out != nullptr: every piece
+  float* state_out;
+  int32_t group;           // key heads of a state
+  bool back;
+};
+
+template <int D>
+struct Sta {
+  static constexpr int TILE = kChunk * D * 2;
+  static constexpr int NKV = 2;
+  static constexpr int OFF_KV = 0;
+  static constexpr int OFF_TERM = NKV * 2 * TILE;        // second and third term of a weighted key tile
+  // at D = 64 the upper lanes of an MMA (see Lin) read a tile further than the last term
+  static constexpr int OFF_BAR = OFF_TERM + (D == 64 ? 3 : 2) * TILE;
+  static constexpr int SMEM = OFF_BAR + 256;
+  static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
+  static_assert(SMEM <= 232448, "shared memory budget");
+};
+
+struct StaBars {
+  uint64_t kv_full[2], kv_empty[2];
+  uint64_t kt_full[2];   // the weighted keys of a slot are written
+  uint64_t term_free;    // and read
+  uint64_t u_full[2], u_free[2];
+  uint32_t tmem_base;
+  int32_t abort;
+};
+static_assert(sizeof(StaBars) <= 256, "barrier space");
+
+constexpr int kStaThreads = 384;
+
+template <int D, int TERMS>
+__global__ void __launch_bounds__(kStaThreads, 1)
+    linear_states(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                  const __grid_constant__ StateArgs p) {
+  using C = Sta<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  StaBars* bars = reinterpret_cast<StaBars*>(smem + C::OFF_BAR);
+  Walk w(p.c, blockIdx.x);
+  if (p.state_out == nullptr) {
+    // only the piece that goes on: the last one of the range, the other way in time the first one
+    if (!w.cut || w.g >= w.hi) return;
+    if (!p.back) {
+      if (w.hi >= p.c.plan->total) return;
+      w.locate(w.hi);
+      if (w.base >= w.hi) return;
+      if (w.base > w.g) w.g = w.base;
+    } else {
+      w.locate(w.g);
+      if (w.base >= w.g) return;
+      if (w.base + w.nch < w.hi) w.hi = w.base + w.nch;
+    }
+    w.located = false;
+  }
+  if (w.g >= w.hi || smem_u32(smem) & 1023u) {
+    if (w.g < w.hi && threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t sbase = smem_u32(smem);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->kv_full[i], 1);
+      mbar_init(&bars->kv_empty[i], 1);
+      mbar_init(&bars->u_full[i], 1);
+      mbar_init(&bars->u_free[i], 4);
+      mbar_init(&bars->kt_full[i], 128);
+    }
+    mbar_init(&bars->term_free, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, 256);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
+
+  if (warp == 0) {
+    // ---------------------------------------------------------- producer
+    if (lane == 0) {
+      bool go = true;
+      uint32_t it = 0;
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+          const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
+          for (int h = 0; h < p.group; ++h, ++it) {
+            const uint32_t slot = it & 1;
+            if ((it >= 2 && !mbar_wait(&bars->kv_empty[slot], (it / 2 - 1) & 1)) || gave_up()) {
+              set_abort(&bars->abort, p.c.status);
+              go = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&bars->kv_full[slot], 2 * C::TILE);
+#pragma unroll
+            for (int kb = 0; kb < D / 64; ++kb) {
+              uint8_t* dst = smem + C::OFF_KV + slot * 2 * C::TILE + kb * 16384;
+              tma_load_3d(dst, &tm_k, &bars->kv_full[slot], kb * 64, w.head * p.group + h, w.start + c * kChunk);
+              tma_load_3d(dst + C::TILE, &tm_v, &bars->kv_full[slot], kb * 64, w.head * p.group + h,
+                          w.start + c * kChunk);
+            }
+          }
+        }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------- MMA issuer
+    // Every lane runs every step and no lane's answer to a wait decides where the warp goes; a vote an item does.
+    const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16384, 1024), td = smem_desc(sbase + C::OFF_TERM, 16384, 1024);
+    bool ok = true, go = true;
+    uint32_t it = 0, un = 0;
+    while (go && w.next())
+      for (int n = 0; go && n < w.c1 - w.c0; ++n, ++un)
+        for (int h = 0; h < p.group; ++h, ++it) {
+          const uint32_t slot = it & 1, buf = un & 1;
+          ok = ok && mbar_wait(&bars->kt_full[slot], (it / 2) & 1);
+          if (h == 0 && un >= 2) ok = ok && mbar_wait(&bars->u_free[buf], (un / 2 - 1) & 1);
+          go = __all_sync(0xffffffffu, ok);
+          if (!go) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t a0 = desc_at(kd, slot * 2 * C::TILE), b = desc_at(a0, C::TILE);
+#pragma unroll
+            for (int t = TERMS - 1; t >= 0; --t)   // the smallest term first
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                tc_mma_ss(tmem + buf * 128, desc_at(t == 0 ? a0 : desc_at(td, (t - 1) * C::TILE), kk * 2048),
+                          desc_at(b, kk * 2048), C::IDESC_U, h > 0 || t < TERMS - 1 || kk > 0);
+            tc_commit(&bars->kv_empty[slot]);
+            if (TERMS > 1) tc_commit(&bars->term_free);
+            if (h == p.group - 1) tc_commit(&bars->u_full[buf]);
+          }
+          __syncwarp();
+        }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  } else if (warp >= 4 && warp < 8) {
+    // ---------------------------------------------------------- weighted keys, a thread a token
+    const int r = threadIdx.x - 128;
+    bool go = true;
+    uint32_t it = 0;
+    while (go && w.next())
+      for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+        const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
+        const int rows = w.rows(c);
+        const float wt = r < rows ? exp2f(w.l2 * (float)(p.back ? r : rows - 1 - r)) : 0.f;
+        for (int h = 0; h < p.group; ++h, ++it) {
+          const uint32_t tile = sbase + C::OFF_KV + (it & 1) * 2 * C::TILE, term = sbase + C::OFF_TERM;
+          if (!mbar_wait_warp(&bars->kv_full[it & 1], (it / 2) & 1) ||
+              (TERMS > 1 && it > 0 && !mbar_wait_warp(&bars->term_free, (it - 1) & 1)) ||
+              __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          if (r >= rows) {  // rows of the next segment, which may hold anything
+            zero_row<D>(tile, r);
+            zero_row<D>(tile + C::TILE, r);
+            if (TERMS > 1) {
+              zero_row<D>(term, r);
+              zero_row<D>(term + C::TILE, r);
+            }
+          } else {
+#pragma unroll
+            for (int kb = 0; kb < D / 64; ++kb)
+#pragma unroll
+              for (int u = 0; u < 8; ++u) {
+                const uint32_t at = kb * 16384 + r * 128 + (((u + r) & 7) << 4);
+                const uint4 x = ld_shared_v4(tile + at);
+                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+                uint32_t y[3][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  float a = lo_f(in[i]) * wt, b = hi_f(in[i]) * wt;
+#pragma unroll
+                  for (int t = 0; t < TERMS; ++t) {
+                    y[t][i] = pack_bf16(a, b);
+                    a -= lo_f(y[t][i]);
+                    b -= hi_f(y[t][i]);
+                  }
+                }
+                st_shared_v4(tile + at, y[0][0], y[0][1], y[0][2], y[0][3]);
+#pragma unroll
+                for (int t = 1; t < TERMS; ++t)
+                  st_shared_v4(term + (t - 1) * C::TILE + at, y[t][0], y[t][1], y[t][2], y[t][3]);
+              }
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(&bars->kt_full[it & 1]);
+        }
+      }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  } else if (warp >= 8) {
+    // ---------------------------------------------------------- sums, a thread a row of the state
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    bool go = true;
+    uint32_t un = 0;
+    while (go && w.next()) {
+      float s[D];
+#pragma unroll
+      for (int i = 0; i < D; ++i) s[i] = 0.f;
+      const int last = min(w.len, w.c1 * kChunk);
+      for (int n = 0; n < w.c1 - w.c0; ++n, ++un) {
+        const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
+        // from the chunk's end to the piece's (or between their beginnings), at once: the factors do not add up errors
+        const int gap = p.back ? (c - w.c0) * kChunk : last - (c * kChunk + w.rows(c));
+        const float f = exp2f(w.l2 * (float)gap);
+        if (!mbar_wait_warp(&bars->u_full[un & 1], (un / 2) & 1) || __any_sync(0xffffffffu, gave_up())) {
+          go = false;
+          break;
+        }
+        tc_fence_after();
+        if (D == 128 || quad < 2) {
+#pragma unroll
+          for (int g = 0; g < D / 32; ++g) {
+            uint32_t u[32];
+            tmem_ld_32x32b_x32(trow + (un & 1) * 128 + g * 32, u);
+            tmem_ld_wait();
+            reg_fence<32>(u);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[g * 32 + i] = fmaf(f, __uint_as_float(u[i]), s[g * 32 + i]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->u_free[un & 1]);
+      }
+      if (!go) break;
+      if (D == 128 || quad < 2) {
+        float* dst;
+        const size_t state = ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
+        const bool on = p.back ? w.c0 > 0 : w.c1 < w.nch;   // it goes on in another CTA
+        if (on) {
+          dst = p.slots + ((size_t)blockIdx.x * D + r) * D;
+        } else {
+          dst = p.state_out + state;
+          if (p.state_in != nullptr && w.c0 == 0) {
+            const float f = exp2f(w.l2 * (float)w.len);
+#pragma unroll
+            for (int i = 0; i < D; i += 4) {
+              const float4 x = *reinterpret_cast<const float4*>(p.state_in + state + i);
+              s[i] = fmaf(f, x.x, s[i]);
+              s[i + 1] = fmaf(f, x.y, s[i + 1]);
+              s[i + 2] = fmaf(f, x.z, s[i + 2]);
+              s[i + 3] = fmaf(f, x.w, s[i + 3]);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < D; i += 4)
+          *reinterpret_cast<float4*>(dst + i) = make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
+      }
+    }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 256);
+  }
+}
+
+// ------------------------------------------------------------------ outputs
+struct OutArgs {
+  Common c;
+  const float* slots;
+  const float* state_in;
+  float* state_out;
+  int32_t gx, gy;          // query heads and key heads of a state; one of them is 1
+  float scale;
+  bf16* out;
+};
+
+template <int D>
+struct Lin {
+  static constexpr int TILE = kChunk * D * 2;
+  static constexpr int NQ = D == 64 ? 4 : 2;
+  static constexpr int NKV = D == 64 ? 3 : 2;
+  static constexpr int OFF_Q = 0;                        // Q tiles, then O on its way out
+  static constexpr int OFF_KV = NQ * TILE;               // K, V of a slot
+  static constexpr int OFF_S = OFF_KV + NKV * 2 * TILE;  // the state, D rows of k's dims, like a V tile
+  static constexpr int OFF_BAR = OFF_S + D * D * 2;
+  static constexpr int SMEM = OFF_BAR + 512;
+  static constexpr int TM_P = 0, TM_A = 128, TM_B = 128 + D, TM_U = 128 + 2 * D;
+  static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);  // Q (K-major) x K^T (K-major)
+  static constexpr uint32_t IDESC_A = idesc_bf16(128, D, 0, 1);    // Q (K-major) x S (MN-major)
+  static constexpr uint32_t IDESC_B = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
+  // K^T (MN-major) x V (MN-major).  M = 128 at D = 64 too, whose lanes 64 .. 127 take the V tile behind K's and are
+  // not read: an M of 64 lies in other lanes.
+  static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
+  static constexpr int REG_CTRL = 72, REG_P = 128, REG_OUT = 104, REG_STATE = 208;
+  static_assert(REG_CTRL + REG_P + REG_OUT + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
+  static_assert(SMEM <= 232448, "shared memory budget");
+};
+
+struct LinBars {
+  uint64_t q_full[4], q_empty[4], kv_full[3], kv_empty[3];
+  uint64_t s_full;     // Q K^T of an item
+  uint64_t p_full;     // its P is in TMEM
+  uint64_t o_full;     // the item's products of an output are complete
+  uint64_t ab_free;    // and in registers
+  uint64_t out_ready[4];         // of a Q tile: the output is in it, or its rows are written
+  // Two of each, as the issuer may be a K ahead of the warps that weight them and they of it.
+  uint64_t k_done[2];  // K is no longer read as it was loaded
+  uint64_t kt_full[2]; // and weighted
+  uint64_t u_full;     // the chunk's K^T V
+  uint64_t s_ready;    // the state that the next chunk's queries read
+  uint32_t tmem_base;
+  int32_t abort;
+};
+static_assert(sizeof(LinBars) <= 512, "barrier space");
+
+constexpr int kThreads = 512;
+constexpr int kRegLaunch = 128;
+
+// An item is a chunk with one query and one key head: of a group of query heads (gx) each item has an output and the
+// chunk one K and V, of a group of key heads (gy) each item has a K and V and the chunk one output.
+// Warp roles:
+//   warp 0       TMA producer;  warp 1  TMEM and every MMA;  warp 2  O out of shared memory
+//   warps 4-7    P = lam^(i-j) Q K^T below the diagonal, in bf16 for P V (a thread a query)
+//   warps 8-11   O = scale (lam^(i+1) Q S + P V) into its Q tile
+//   warps 12-15  the weighted keys, and the state in registers (a thread a row), its bf16 copy in shared memory
+template <int D, bool BACK>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_out(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
+               const __grid_constant__ OutArgs p) {
+  using C = Lin<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  LinBars* bars = reinterpret_cast<LinBars*>(smem + C::OFF_BAR);
+  Walk w(p.c, blockIdx.x);
+  // sequences without a token: their states go through
+  if (!BACK && p.state_out != nullptr)
+    for (int s = blockIdx.x; s < p.c.num_segments; s += gridDim.x)
+      if (p.c.cu[s] == p.c.cu[s + 1] && p.c.cu[s] >= 0 && p.c.cu[s] <= p.c.num_tokens) {
+        const size_t n = (size_t)p.c.heads * D * D / 4, at = n * s;
+        for (size_t i = threadIdx.x; i < n; i += kThreads) {
+          const int head = (int)(i / (D * D / 4));
+          if (!decay_ok(p.c.log_decay[head])) {
+            set_status(p.c.status, VCS_ERR_DEVICE_CHECK);
+            continue;
+          }
+          reinterpret_cast<float4*>(p.state_out)[at + i] =
+              p.state_in != nullptr ? reinterpret_cast<const float4*>(p.state_in)[at + i]
+                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+  if (w.g >= w.hi) return;
+  // once any CTA of this call has given up on a wait, those not started stand down
+  if (*reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT) return;
+  if (smem_u32(smem) & 1023u) {  // the tiles' swizzle wants 1,024-byte aligned blocks
+    if (threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t sbase = smem_u32(smem);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::NQ; ++i) {
+      mbar_init(&bars->q_full[i], 1);
+      mbar_init(&bars->q_empty[i], 1);
+      mbar_init(&bars->out_ready[i], 128);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->k_done[i], 1);
+      mbar_init(&bars->kt_full[i], 128);
+    }
+    for (int i = 0; i < C::NKV; ++i) {
+      mbar_init(&bars->kv_full[i], 1);
+      mbar_init(&bars->kv_empty[i], 1);
+    }
+    mbar_init(&bars->s_full, 1);
+    mbar_init(&bars->p_full, 128);
+    mbar_init(&bars->o_full, 1);
+    mbar_init(&bars->ab_free, 4);
+    mbar_init(&bars->u_full, 1);
+    mbar_init(&bars->s_ready, 128);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
+  const int group = BACK ? p.gy : p.gx;
+  // Every role walks the same items and counts what it has passed: items (it), chunks (ch), Q tiles (qi), K/V tiles (ki).
+
+  if (warp < 4) {
+    setmaxnreg_dec<C::REG_CTRL>();
+    if (warp == 0 && lane == 0) {
+      // -------------------------------------------------------- producer
+      bool go = true;
+      uint32_t qi = 0, ki = 0;
+      auto fail = [&] {
+        set_abort(&bars->abort, p.c.status);
+        go = false;
+      };
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+          const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+          const int tok = w.start + c * kChunk;
+          for (int h = 0; go && h < group; ++h) {
+            if (gave_up()) {
+              go = false;
+              break;
+            }
+            if (BACK || h == 0) {
+              const uint32_t slot = ki % C::NKV;
+              if (ki >= C::NKV && !mbar_wait(&bars->kv_empty[slot], (ki / C::NKV - 1) & 1)) {
+                fail();
+                break;
+              }
+              mbar_arrive_expect_tx(&bars->kv_full[slot], 2 * C::TILE);
+#pragma unroll
+              for (int kb = 0; kb < D / 64; ++kb) {
+                uint8_t* dst = smem + C::OFF_KV + slot * 2 * C::TILE + kb * 16384;
+                tma_load_3d(dst, &tm_k, &bars->kv_full[slot], kb * 64, w.head * p.gy + (BACK ? h : 0), tok);
+                tma_load_3d(dst + C::TILE, &tm_v, &bars->kv_full[slot], kb * 64, w.head * p.gy + (BACK ? h : 0), tok);
+              }
+              ++ki;
+            }
+            if (!BACK || h == 0) {
+              const uint32_t slot = qi % C::NQ;
+              if (qi >= C::NQ && !mbar_wait(&bars->q_empty[slot], (qi / C::NQ - 1) & 1)) {
+                fail();
+                break;
+              }
+              mbar_arrive_expect_tx(&bars->q_full[slot], C::TILE);
+#pragma unroll
+              for (int kb = 0; kb < D / 64; ++kb)
+                tma_load_3d(smem + C::OFF_Q + slot * C::TILE + kb * 16384, &tm_q, &bars->q_full[slot], kb * 64,
+                            w.head * p.gx + (BACK ? 0 : h), tok);
+              ++qi;
+            }
+          }
+        }
+    } else if (warp == 1) {
+      // -------------------------------------------------------- MMA issuer
+      // Every lane runs every step, no lane's answer to a wait decides where the warp goes, and the elected lane issues
+      // as long as its own waits were met; a vote an item ends the walk.  The MMAs of one issuer execute in order, so
+      // Q K^T of an item, issued behind P V of the one before, may overwrite its P.
+      const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
+      const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16, 1024), kt = smem_desc(sbase + C::OFF_KV, 16384, 1024);
+      const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
+      bool ok = true;
+      uint32_t qi = 0, ki = 0, it = 0, ch = 0, oi = 0;   // oi: outputs
+      // Q K^T of an item whose tiles are qi and ki
+      auto issue_s = [&](bool new_q, bool new_k, bool last_k) {
+        if (new_q) ok = ok && mbar_wait(&bars->q_full[qi % C::NQ], (qi / C::NQ) & 1);
+        if (new_k) ok = ok && mbar_wait(&bars->kv_full[ki % C::NKV], (ki / C::NKV) & 1);
+        tc_fence_after();
+        if (elect_one() && ok) {
+          const uint64_t a = desc_at(qd, qi % C::NQ * C::TILE), b = desc_at(kd, ki % C::NKV * 2 * C::TILE);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
+            tc_mma_ss(tmem + C::TM_P, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
+          }
+          tc_commit(&bars->s_full);
+          if (last_k) tc_commit(&bars->k_done[ki & 1]);
+        }
+        __syncwarp();
+      };
+      bool more = w.next(), go = true;
+      if (more) issue_s(true, true, BACK || group == 1);
+      while (go && more) {
+        const int chunks = w.c1 - w.c0;
+        for (int n = 0; go && n < chunks; ++n, ++ch) {
+          for (int h = 0; h < group; ++h, ++it) {
+            const bool first = !BACK || h == 0, out = !BACK || h == group - 1, lastk = BACK || h == group - 1;
+            const uint32_t q = qi % C::NQ, k = ki % C::NKV;
+            if (first) {  // A = Q S
+              if (h == 0) ok = ok && mbar_wait(&bars->s_ready, ch & 1);
+              if (oi > 0) ok = ok && mbar_wait(&bars->ab_free, (oi - 1) & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                const uint64_t a = desc_at(qd, q * C::TILE);
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                  tc_mma_ss(tmem + C::TM_A, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048),
+                            C::IDESC_A, kk > 0);
+              }
+              __syncwarp();
+            }
+            ok = ok && mbar_wait(&bars->p_full, it & 1);
+            go = __all_sync(0xffffffffu, ok);
+            if (!go) break;
+            tc_fence_after();
+            if (elect_one()) {  // B (+)= P V
+              const uint64_t b = desc_at(kt, k * 2 * C::TILE + C::TILE);
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                tc_mma_ts(tmem + C::TM_B, tmem + C::TM_P + kk * 8, desc_at(b, kk * 2048), C::IDESC_B,
+                          kk > 0 || !first);
+              if (out) tc_commit(&bars->o_full);
+            }
+            __syncwarp();
+            // the next item's Q K^T ahead of the wait for this one's weighted keys
+            const bool end = h == group - 1;
+            bool follows = true;
+            if (end && n == chunks - 1) follows = more = w.next();
+            if (out) ++qi, ++oi;
+            if (lastk) ++ki;
+            if (follows) issue_s(out, lastk, BACK || (end ? group == 1 : h + 1 == group - 1));
+            if (lastk) {  // U (+)= K^T V
+              ok = ok && mbar_wait(&bars->kt_full[(ki - 1) & 1], ((ki - 1) >> 1) & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                const uint64_t a = desc_at(kt, k * 2 * C::TILE), b = desc_at(a, C::TILE);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U,
+                            kk > 0 || (BACK && h > 0));
+                tc_commit(&bars->kv_empty[k]);
+                if (end) tc_commit(&bars->u_full);
+              }
+              __syncwarp();
+            }
+          }
+        }
+      }
+      go = __all_sync(0xffffffffu, ok);
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else if (warp == 2 && lane == 0) {
+      // -------------------------------------------------------- O out of shared memory
+      bool go = true;
+      uint32_t oi = 0;
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+          const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+          for (int h = 0; h < p.gx; ++h, ++oi) {
+            const uint32_t slot = oi % C::NQ;
+            if (!mbar_wait(&bars->out_ready[slot], (oi / C::NQ) & 1) || gave_up()) {
+              set_abort(&bars->abort, p.c.status);
+              go = false;
+              break;
+            }
+            if (w.rows(c) == kChunk) {
+#pragma unroll
+              for (int kb = 0; kb < D / 64; ++kb)
+                tma_store_3d(&tm_o, sbase + C::OFF_Q + slot * C::TILE + kb * 16384, kb * 64, w.head * p.gx + h,
+                             w.start + c * kChunk);
+              bulk_commit();
+              bulk_wait_read();
+            }
+            mbar_arrive(&bars->q_empty[slot]);
+          }
+        }
+    }
+  } else if (warp < 8) {
+    // ---------------------------------------------------------- P
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    bool go = true;
+    uint32_t it = 0, ki = 0;
+    while (go && w.next()) {
+      // lam^(r - c) (c - r) of columns c, c + 1 from the exact distances: a token sees itself with weight 1 however fast
+      // the head forgets
+      const float sl = BACK ? -w.l2 : w.l2;
+      const uint64_t slope = f2pack(sl, sl), at = f2pack((float)r, (float)r);
+      for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+        const int rows = w.rows(c);
+        for (int h = 0; h < group; ++h, ++it) {
+          if (!mbar_wait_warp(&bars->s_full, it & 1) || __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          tc_fence_after();
+          uint32_t pk[64];
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const bool none = BACK ? g < quad || g * 32 >= rows : g > quad;
+            if (none) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) pk[g * 16 + i] = 0u;
+              continue;
+            }
+            uint32_t s[32];
+            tmem_ld_32x32b_x32(trow + C::TM_P + g * 32, s);
+            tmem_ld_wait();
+            reg_fence<32>(s);
+            // columns of the group that the row takes, a bit each
+            uint32_t seen = 0xffffffffu;
+            if (g == quad) seen = BACK ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+            if (BACK && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float c0 = (float)(g * 32 + 2 * i);
+              float e0, e1, x0, x1;
+              f2unpack(fmul2(slope, fadd2(at, f2pack(-c0, -c0 - 1.f))), e0, e1);
+              f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), f2pack(ex2(e0), ex2(e1))),
+                       x0, x1);
+              x0 = seen >> (2 * i) & 1 ? x0 : 0.f;
+              x1 = seen >> (2 * i + 1) & 1 ? x1 : 0.f;
+              pk[g * 16 + i] = pack_bf16(x0, x1);
+            }
+          }
+          if ((BACK || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
+            const uint32_t slot = ki % C::NKV;
+            if (!mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1)) {
+              go = false;
+              break;
+            }
+            if (r >= rows) zero_row<D>(sbase + C::OFF_KV + slot * 2 * C::TILE + C::TILE, r);
+            fence_proxy_async_smem();
+          }
+          if (BACK || h == group - 1) ++ki;
+          tmem_st_32x32b_x32(trow + C::TM_P, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
+          tmem_st_32x32b_x32(trow + C::TM_P + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&bars->p_full);
+        }
+      }
+    }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  } else if (warp < 12) {
+    // ---------------------------------------------------------- O
+    setmaxnreg_dec<C::REG_OUT>();
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    bool go = true;
+    uint32_t oi = 0;
+    while (go && w.next())
+      for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+        const int rows = w.rows(c);
+        const float fa = p.scale * exp2f(w.l2 * (float)(BACK ? max(rows - r, 0) : r + 1));
+        const uint64_t fa2 = f2pack(fa, fa), fb2 = f2pack(p.scale, p.scale);
+        for (int h = 0; h < p.gx; ++h, ++oi) {
+          if (!mbar_wait_warp(&bars->o_full, oi & 1) || __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t tile = sbase + C::OFF_Q + oi % C::NQ * C::TILE + r * 128;
+          bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + w.head * p.gx + h) * D;
+#pragma unroll
+          for (int g = 0; g < D / 32; ++g) {
+            uint32_t a[32], b[32], o[16];
+            tmem_ld_32x32b_x32(trow + C::TM_A + g * 32, a);
+            tmem_ld_32x32b_x32(trow + C::TM_B + g * 32, b);
+            tmem_ld_wait();
+            reg_fence<32>(a);
+            reg_fence<32>(b);
+            if (g == D / 32 - 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars->ab_free);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x0, x1;
+              f2unpack(ffma2(fa2, f2pack(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
+                             fmul2(fb2, f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])))),
+                       x0, x1);
+              o[i] = pack_bf16(x0, x1);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              if (rows == kChunk)
+                st_shared_v4(tile + (g >> 1) * 16384 + ((((g & 1) * 4 + u) ^ (r & 7)) << 4), o[4 * u], o[4 * u + 1],
+                             o[4 * u + 2], o[4 * u + 3]);
+              else if (r < rows)
+                *reinterpret_cast<uint4*>(row + g * 32 + u * 8) =
+                    make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+            }
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(&bars->out_ready[oi % C::NQ]);
+        }
+      }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  } else {
+    // ---------------------------------------------------------- state
+    setmaxnreg_inc<C::REG_STATE>();
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    const bool mine = D == 128 || quad < 2;   // a row of the state
+    bool go = true;
+    uint32_t ki = 0, ch = 0;
+    while (go && w.next()) {
+      float s[D];
+      if (mine) {
+#pragma unroll
+        for (int i = 0; i < D; ++i) s[i] = 0.f;
+        auto add = [&](const float* src, float f) {
+#pragma unroll
+          for (int i = 0; i < D; i += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(src + i);
+            s[i] = fmaf(f, x.x, s[i]);
+            s[i + 1] = fmaf(f, x.y, s[i + 1]);
+            s[i + 2] = fmaf(f, x.z, s[i + 2]);
+            s[i + 3] = fmaf(f, x.w, s[i + 3]);
+          }
+        };
+        // what other CTAs' pieces bring, the nearest first, until it has faded below fp32
+        bool faded = false;
+        if (!BACK) {
+          for (int x = blockIdx.x - 1; w.c0 > 0 && x >= 0 && !faded; --x) {
+            const int64_t e = (x + 1) * w.range - w.base;    // chunk behind that CTA's piece
+            const float f = exp2f(w.l2 * (float)((w.c0 - e) * kChunk));
+            faded = f == 0.f;
+            if (!faded) add(p.slots + ((size_t)x * D + r) * D, f);
+            if (x * w.range <= w.base) break;
+          }
+          if (p.state_in != nullptr && !faded)
+            add(p.state_in + ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D,
+                exp2f(w.l2 * (float)((int64_t)w.c0 * kChunk)));
+          if (p.state_out != nullptr && w.c0 > 0 && w.c1 == w.nch) {  // its last piece's own sum is there
+            float* dst = p.state_out + ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
+            const float f = exp2f(w.l2 * (float)(w.len - w.c0 * kChunk));
+#pragma unroll
+            for (int i = 0; i < D; i += 4) {
+              float4 x = *reinterpret_cast<const float4*>(dst + i);
+              x.x = fmaf(f, s[i], x.x);
+              x.y = fmaf(f, s[i + 1], x.y);
+              x.z = fmaf(f, s[i + 2], x.z);
+              x.w = fmaf(f, s[i + 3], x.w);
+              *reinterpret_cast<float4*>(dst + i) = x;
+            }
+          }
+        } else {
+          for (int x = blockIdx.x + 1; w.c1 < w.nch && x < (int)gridDim.x && !faded; ++x) {
+            const int64_t b = x * w.range - w.base;          // that CTA's first chunk
+            if (b >= w.nch) break;
+            const float f = exp2f(w.l2 * (float)((b - w.c1) * kChunk));
+            faded = f == 0.f;
+            if (!faded) add(p.slots + ((size_t)x * D + r) * D, f);
+          }
+        }
+      }
+      for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ch) {
+        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+        const int rows = w.rows(c);
+        // the copy that the chunk's queries read: the products with the one before are complete (u_full)
+        if (mine) {
+          const uint32_t dst = sbase + C::OFF_S + r * 128;
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i)
+            st_shared_v4(dst + (i >> 3) * (D * 128) + (((i & 7) ^ (r & 7)) << 4), pack_bf16(s[8 * i], s[8 * i + 1]),
+                         pack_bf16(s[8 * i + 2], s[8 * i + 3]), pack_bf16(s[8 * i + 4], s[8 * i + 5]),
+                         pack_bf16(s[8 * i + 6], s[8 * i + 7]));
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(&bars->s_ready);
+        const float wt = r < rows ? exp2f(w.l2 * (float)(BACK ? r : rows - 1 - r)) : 0.f;
+        for (int j = 0; j < p.gy; ++j, ++ki) {
+          const uint32_t slot = ki % C::NKV, tile = sbase + C::OFF_KV + slot * 2 * C::TILE;
+          if (!mbar_wait_warp(&bars->k_done[ki & 1], (ki >> 1) & 1) || !mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1) ||
+              __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          if (r >= rows) {
+            zero_row<D>(tile, r);
+          } else {
+            const uint64_t wt2 = f2pack(wt, wt);
+#pragma unroll
+            for (int kb = 0; kb < D / 64; ++kb)
+#pragma unroll
+              for (int u = 0; u < 8; ++u) {
+                const uint32_t at = tile + kb * 16384 + r * 128 + (((u + r) & 7) << 4);
+                const uint4 x = ld_shared_v4(at);
+                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+                uint32_t y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  float a, b;
+                  f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
+                  y[i] = pack_bf16(a, b);
+                }
+                st_shared_v4(at, y[0], y[1], y[2], y[3]);
+              }
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(&bars->kt_full[ki & 1]);
+        }
+        if (!go) break;
+        if (!mbar_wait_warp(&bars->u_full, ch & 1)) {
+          go = false;
+          break;
+        }
+        tc_fence_after();
+        if (mine) {
+          const float f = exp2f(w.l2 * (float)rows);
+#pragma unroll
+          for (int g = 0; g < D / 32; ++g) {
+            uint32_t u[32];
+            tmem_ld_32x32b_x32(trow + C::TM_U + g * 32, u);
+            tmem_ld_wait();
+            reg_fence<32>(u);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[g * 32 + i] = fmaf(f, s[g * 32 + i], __uint_as_float(u[i]));
+          }
+        }
+        tc_fence_before();
+      }
+    }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
 }
 
 // One token of a sequence.  A block takes 4 SLICE_LANES columns of one head's state: lane l of a row's lanes holds four
@@ -175,59 +1112,157 @@ __global__ void __launch_bounds__(kStepThreads) linear_step(const __grid_constan
 
 }  // namespace
 
-size_t linear_fwd_ws_bytes(int32_t, int64_t, int32_t, int32_t, int32_t) { return kWsHeader; }
-size_t linear_bwd_ws_bytes(int32_t, int64_t, int32_t, int32_t, int32_t) { return kWsHeader; }
+namespace {
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// Workspace: header (status word, plan), the segments' chunk offsets, a state a CTA (the backward: two).
+size_t ws_off(int32_t num_segments) { return align256(((size_t)num_segments + 1) * 4); }
+size_t ws_slots(int32_t d) { return (size_t)kGrid * d * d * 4; }
+
+struct Work {
+  Common c;
+  float* slots[2];
+  int64_t chunks;   // upper bound of the sequences'
+  int32_t grid;
+};
+
+Work make_work(const LinearArgs& a, void* ws) {
+  Work w;
+  char* p = static_cast<char*>(ws);
+  w.c.log_decay = a.log_decay;
+  w.c.cu = a.cu_seqlens;
+  w.c.off = reinterpret_cast<int32_t*>(p + kWsHeader);
+  w.c.plan = reinterpret_cast<Plan*>(p + kWsPlan);
+  w.c.num_segments = a.num_segments;
+  w.c.num_tokens = (int32_t)a.num_tokens;
+  w.c.heads = a.hkv;
+  w.c.status = static_cast<int32_t*>(ws);
+  w.slots[0] = reinterpret_cast<float*>(p + kWsHeader + ws_off(a.num_segments));
+  w.slots[1] = w.slots[0] + (size_t)kGrid * a.d * a.d;
+  w.chunks = a.hkv * (a.num_tokens / kChunk + (int64_t)a.num_segments);
+  w.grid = (int32_t)(w.chunks < kGrid ? w.chunks : kGrid);
+  return w;
+}
+
+// A tensor map of [tokens, heads, D].  Without tokens nothing is read and the pointer may be null: any address serves.
+bool encode(CUtensorMap* map, const void* base, int d, int64_t heads, const LinearArgs& a) {
+  return encode_tma_3d_bf16(map, a.num_tokens > 0 ? base : a.log_decay, d, heads, a.num_tokens, 64, 128);
+}
+
+cudaError_t launch_plan(const Work& w, cudaStream_t st) {
+  linear_plan<<<1, 1024, 0, st>>>(w.c.cu, w.c.num_segments, w.c.num_tokens, w.c.heads, w.grid,
+                                  const_cast<int32_t*>(w.c.off), const_cast<Plan*>(w.c.plan), w.c.status);
+  return cudaGetLastError();
+}
+
+template <int D, int TERMS>
+cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, const void* v, int group, bool back,
+                          float* slots, const float* state_in, float* state_out, cudaStream_t st) {
+  using C = Sta<D>;
+  alignas(64) CUtensorMap tk, tv;
+  const int64_t heads = (int64_t)a.hkv * group;
+  if (!encode(&tk, k, D, heads, a) ||
+      !encode(&tv, v, D, heads, a))
+    return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  StateArgs p;
+  p.c = w.c;
+  p.slots = slots;
+  p.state_in = state_in;
+  p.state_out = state_out;
+  p.group = group;
+  p.back = back;
+  linear_states<D, TERMS><<<w.grid, kStaThreads, C::SMEM, st>>>(tk, tv, p);
+  return cudaGetLastError();
+}
+
+template <int D, bool BACK>
+cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int gx, int gy,
+                       const float* slots, const float* state_in, float* state_out, void* out, cudaStream_t st) {
+  using C = Lin<D>;
+  alignas(64) CUtensorMap tq, tk, tv, to;
+  const int64_t hx = (int64_t)a.hkv * gx, hy = (int64_t)a.hkv * gy;
+  if (!encode(&tq, q, D, hx, a) ||
+      !encode(&tk, k, D, hy, a) ||
+      !encode(&tv, v, D, hy, a) ||
+      !encode(&to, out, D, hx, a))
+    return cudaErrorInvalidValue;
+  const void* fn = reinterpret_cast<const void*>(linear_out<D, BACK>);
+  static std::atomic<int> regs_cache{-1};
+  bool regs_ok = false;
+  if (cudaError_t e = launch_regs_match(fn, kRegLaunch, &regs_cache, &regs_ok); e != cudaSuccess) return e;
+  if (!regs_ok) return cudaErrorInvalidConfiguration;
+  cudaError_t e = cudaFuncSetAttribute(linear_out<D, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  OutArgs p;
+  p.c = w.c;
+  p.slots = slots;
+  p.state_in = state_in;
+  p.state_out = state_out;
+  p.gx = gx;
+  p.gy = gy;
+  p.scale = a.scale;
+  p.out = static_cast<bf16*>(out);
+  linear_out<D, BACK><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, to, p);
+  return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_fwd(const LinearArgs& a, const float* state_in, float* state_out, void* o, void* ws,
+                       cudaStream_t st) {
+  const Work w = make_work(a, ws);
+  const int group = a.hq / a.hkv;
+  cudaError_t e = launch_plan(w, st);
+  if (e != cudaSuccess) return e;
+  if (state_out != nullptr)
+    e = launch_states<D, 3>(w, a, a.k, a.v, 1, false, w.slots[0], state_in, state_out, st);
+  else if (a.num_tokens > kWhole * kChunk)   // else no sequence is cut
+    e = launch_states<D, 1>(w, a, a.k, a.v, 1, false, w.slots[0], nullptr, nullptr, st);
+  if (e != cudaSuccess) return e;
+  return launch_out<D, false>(w, a, a.q, a.k, a.v, group, 1, w.slots[0], state_in, state_out, o, st);
+}
+
+template <int D>
+cudaError_t launch_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk, void* dv, void* ws,
+                       cudaStream_t st) {
+  const Work w = make_work(a, ws);
+  const int group = a.hq / a.hkv;
+  cudaError_t e = launch_plan(w, st);
+  if (e == cudaSuccess && a.num_tokens > kWhole * kChunk) {
+    e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, w.slots[0], nullptr, nullptr, st);
+  }
+  if (e == cudaSuccess)
+    e = launch_out<D, false>(w, a, dout, a.v, a.k, group, 1, w.slots[0], nullptr, nullptr, dq, st);
+  if (e == cudaSuccess && a.num_tokens > kWhole * kChunk) {
+    e = launch_states<D, 1>(w, a, dout, a.q, group, true, w.slots[0], nullptr, nullptr, st);
+    if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.q, dout, group, true, w.slots[1], nullptr, nullptr, st);
+  }
+  if (e == cudaSuccess)
+    e = launch_out<D, true>(w, a, a.v, dout, a.q, 1, group, w.slots[0], nullptr, nullptr, dk, st);
+  if (e == cudaSuccess)
+    e = launch_out<D, true>(w, a, a.k, a.q, dout, 1, group, w.slots[1], nullptr, nullptr, dv, st);
+  return e;
+}
+
+}  // namespace
+
+size_t linear_fwd_ws_bytes(int32_t num_segments, int64_t, int32_t, int32_t, int32_t d) {
+  return kWsHeader + ws_off(num_segments) + ws_slots(d);
+}
+size_t linear_bwd_ws_bytes(int32_t num_segments, int64_t, int32_t, int32_t, int32_t d) {
+  return kWsHeader + ws_off(num_segments) + 2 * ws_slots(d);
+}
 
 cudaError_t launch_linear_fwd(const LinearArgs& a, const float* state_in, float* state_out, void* o, void* ws,
                               cudaStream_t st) {
-  if (cudaError_t e = cudaMemsetAsync(ws, 0, kWsHeader, st); e != cudaSuccess) return e;
-  WalkArgs w{};
-  w.q = static_cast<const bf16*>(a.q);
-  w.k = static_cast<const bf16*>(a.k);
-  w.v = static_cast<const bf16*>(a.v);
-  w.log_decay = a.log_decay;
-  w.cu_seqlens = a.cu_seqlens;
-  w.num_segments = a.num_segments;
-  w.num_tokens = (int32_t)a.num_tokens;
-  w.heads = a.hkv;
-  w.gq = a.hq / a.hkv;
-  w.gk = 1;
-  w.scale = a.scale;
-  w.state_in = state_in;
-  w.state_out = state_out;
-  w.o = static_cast<bf16*>(o);
-  w.status = static_cast<int32_t*>(ws);
-  return a.d == 64 ? launch_walk<64>(w, st) : launch_walk<128>(w, st);
+  return a.d == 64 ? launch_fwd<64>(a, state_in, state_out, o, ws, st) : launch_fwd<128>(a, state_in, state_out, o, ws, st);
 }
 
 cudaError_t launch_linear_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk, void* dv, void* ws,
                               cudaStream_t st) {
-  if (cudaError_t e = cudaMemsetAsync(ws, 0, kWsHeader, st); e != cudaSuccess) return e;
-  const bf16 *q = static_cast<const bf16*>(a.q), *k = static_cast<const bf16*>(a.k),
-             *v = static_cast<const bf16*>(a.v), *g = static_cast<const bf16*>(dout);
-  WalkArgs w{};
-  w.log_decay = a.log_decay;
-  w.cu_seqlens = a.cu_seqlens;
-  w.num_segments = a.num_segments;
-  w.num_tokens = (int32_t)a.num_tokens;
-  w.heads = a.hkv;
-  w.scale = a.scale;
-  w.status = static_cast<int32_t*>(ws);
-  auto run = [&](const bf16* x, const bf16* y, const bf16* z, int gq, int gk, bool back, void* out) {
-    w.q = x;
-    w.k = y;
-    w.v = z;
-    w.gq = gq;
-    w.gk = gk;
-    w.back = back;
-    w.o = static_cast<bf16*>(out);
-    return a.d == 64 ? launch_walk<64>(w, st) : launch_walk<128>(w, st);
-  };
-  const int group = a.hq / a.hkv;
-  cudaError_t e = run(g, v, k, group, 1, false, dq);
-  if (e == cudaSuccess) e = run(v, g, q, 1, group, true, dk);
-  if (e == cudaSuccess) e = run(k, q, g, 1, group, true, dv);
-  return e;
+  return a.d == 64 ? launch_bwd<64>(a, dout, dq, dk, dv, ws, st) : launch_bwd<128>(a, dout, dq, dk, dv, ws, st);
 }
 
 template <int D>

@@ -1,4 +1,5 @@
 """Linear attention and distillation on the host (CPU only): refusals and workspaces."""
+import numpy as np
 import pytest
 import torch
 
@@ -109,3 +110,56 @@ def test_tensors_on_the_host_are_refused(vcs):
               lambda: vcs.distill_topk(torch.zeros(4, 9).half(), cu.view(1, 2), torch.zeros(1, 2), torch.zeros(4))):
         with pytest.raises(ValueError):
             f()
+
+
+# ------------------------------------------------------------------ how the forward's and backward's work is divided
+CHUNK, GRID, WHOLE = 128, 152, 16
+
+
+def pieces(lens, heads, bound):
+    """The documented rule, CTA by CTA: lists of (segment, head, c0, c1) and whether sequences are cut."""
+    nch = [-(-n // CHUNK) for n in lens]
+    off = np.concatenate([[0], np.cumsum(nch)])
+    total, cut = int(off[-1]) * heads, max(nch, default=0) > WHOLE
+    grid = min(GRID, bound)
+    size = -(-total // grid) if grid else 0
+    out = []
+    for b in range(grid):
+        g, hi, mine = min(size * b, total), min(size * (b + 1), total), []
+        while g < hi:
+            seg = int(np.searchsorted(off, g // heads, side="right")) - 1
+            head = (g - int(off[seg]) * heads) // nch[seg]
+            base = int(off[seg]) * heads + head * nch[seg]
+            if not cut and g != base:
+                g = base + nch[seg]
+                continue
+            c0, c1 = g - base, min(nch[seg], hi - base) if cut else nch[seg]
+            mine.append((seg, head, c0, c1))
+            g = base + c1
+        out.append(mine)
+    return out, cut
+
+
+def test_every_chunk_is_taken_once_and_cuts_lead_to_the_next_cta():
+    rng = np.random.default_rng(0)
+    for _ in range(120):
+        heads = int(rng.integers(1, 9))
+        most = int(rng.choice([5, 300, 3000, 60_000]))
+        lens = [int(x) for x in rng.integers(0, most, size=int(rng.integers(1, 40)))]
+        if rng.random() < 0.2:
+            lens[0] = int(rng.integers(1, 400_000))
+        work, cut = pieces(lens, heads, heads * (sum(lens) // CHUNK + len(lens)))
+        seen = {}
+        for b, mine in enumerate(work):
+            for i, (seg, head, c0, c1) in enumerate(mine):
+                assert c1 > c0
+                assert c0 == 0 or (cut and i == 0)                      # only the first goes on from another CTA
+                assert c1 == -(-lens[seg] // CHUNK) or (cut and i == len(mine) - 1)
+                at, last = seen.get((seg, head), (0, None))
+                assert c0 == at and (last is None or last == b - 1)     # cuts lead to the very next CTA
+                seen[seg, head] = c1, b
+        assert {k: v[0] for k, v in seen.items()} == {(s, h): -(-n // CHUNK) for s, n in enumerate(lens) if n
+                                                      for h in range(heads)}
+        if not cut:  # no CTA takes more than its share and one sequence
+            share = -(-sum(c1 - c0 for m in work for *_, c0, c1 in m) // max(len(work), 1))
+            assert max((sum(c1 - c0 for *_, c0, c1 in m) for m in work), default=0) <= share + WHOLE
