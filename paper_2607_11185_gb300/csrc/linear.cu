@@ -186,14 +186,6 @@ struct Walk {
 };
 
 // ------------------------------------------------------------------ shared pieces
-__device__ __forceinline__ void tma_store_3d(const void* map, uint32_t src, int x, int y, int z) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
-               "r"(src), "r"(x), "r"(y), "r"(z)
-               : "memory");
-}
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-
 __device__ __forceinline__ void set_abort(int32_t* abort, int32_t* status) {
   set_status(status, VCS_ERR_DEVICE_TIMEOUT);
   *reinterpret_cast<volatile int32_t*>(abort) = 1;
@@ -491,6 +483,7 @@ struct OutArgs {
   float* state_out;
   int32_t gx, gy;          // query heads and key heads of a state; one of them is 1
   float scale;
+  bool wide;               // out is 32-byte aligned
   bf16* out;
 };
 
@@ -499,12 +492,14 @@ struct Lin {
   static constexpr int TILE = kChunk * D * 2;
   static constexpr int NQ = D == 64 ? 4 : 2;
   static constexpr int NKV = D == 64 ? 3 : 2;
-  static constexpr int OFF_Q = 0;                        // Q tiles, then O on its way out
+  static constexpr int NP = D == 64 ? 2 : 1;             // buffers of Q K^T and P
+  static constexpr int OFF_Q = 0;
   static constexpr int OFF_KV = NQ * TILE;               // K, V of a slot
   static constexpr int OFF_S = OFF_KV + NKV * 2 * TILE;  // the state, D rows of k's dims, like a V tile
-  static constexpr int OFF_BAR = OFF_S + D * D * 2;
+  static constexpr int OFF_TAB = OFF_S + D * D * 2;      // 32 powers of the decay for each warp that makes P
+  static constexpr int OFF_BAR = OFF_TAB + 512;
   static constexpr int SMEM = OFF_BAR + 512;
-  static constexpr int TM_P = 0, TM_A = 128, TM_B = 128 + D, TM_U = 128 + 2 * D;
+  static constexpr int TM_P = 0, TM_A = NP * 128, TM_B = TM_A + D, TM_U = TM_B + D;
   static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);  // Q (K-major) x K^T (K-major)
   static constexpr uint32_t IDESC_A = idesc_bf16(128, D, 0, 1);    // Q (K-major) x S (MN-major)
   static constexpr uint32_t IDESC_B = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
@@ -513,20 +508,19 @@ struct Lin {
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
   static constexpr int REG_CTRL = 72, REG_P = 128, REG_OUT = 104, REG_STATE = 208;
   static_assert(REG_CTRL + REG_P + REG_OUT + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
-  static_assert(SMEM <= 232448, "shared memory budget");
+  static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
 };
 
 struct LinBars {
   uint64_t q_full[4], q_empty[4], kv_full[3], kv_empty[3];
-  uint64_t s_full;     // Q K^T of an item
-  uint64_t p_full;     // its P is in TMEM
-  uint64_t o_full;     // the item's products of an output are complete
+  uint64_t s_full[2];  // Q K^T of an item
+  uint64_t p_full[2];  // its P is in TMEM
+  uint64_t o_full;     // the products of an output are complete
   uint64_t ab_free;    // and in registers
-  uint64_t out_ready[4];         // of a Q tile: the output is in it, or its rows are written
   // Two of each, as the issuer may be a K ahead of the warps that weight them and they of it.
-  uint64_t k_done[2];  // K is no longer read as it was loaded
+  uint64_t k_done[2];  // a K that is to be weighted is no longer read as it was loaded
   uint64_t kt_full[2]; // and weighted
-  uint64_t u_full;     // the chunk's K^T V
+  uint64_t u_full;     // the chunk's K^T V, or, of a piece's last chunk, what reads the state
   uint64_t s_ready;    // the state that the next chunk's queries read
   uint32_t tmem_base;
   int32_t abort;
@@ -536,18 +530,29 @@ static_assert(sizeof(LinBars) <= 512, "barrier space");
 constexpr int kThreads = 512;
 constexpr int kRegLaunch = 128;
 
+// 32 bytes at p, which is 32-byte aligned (wide) or 16.
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8], bool wide) {
+  if (!wide) {
+    static_cast<uint4*>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+    return;
+  }
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]),
+               "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+               : "memory");
+}
+
 // An item is a chunk with one query and one key head: of a group of query heads (gx) each item has an output and the
 // chunk one K and V, of a group of key heads (gy) each item has a K and V and the chunk one output.
 // Warp roles:
-//   warp 0       TMA producer;  warp 1  TMEM and every MMA;  warp 2  O out of shared memory
+//   warp 0       TMA producer;  warp 1  TMEM and every MMA
 //   warps 4-7    P = lam^(i-j) Q K^T below the diagonal, in bf16 for P V (a thread a query)
-//   warps 8-11   O = scale (lam^(i+1) Q S + P V) into its Q tile
+//   warps 8-11   O = scale (lam^(i+1) Q S + P V)
 //   warps 12-15  the weighted keys, and the state in registers (a thread a row), its bf16 copy in shared memory
 template <int D, bool BACK>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_out(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
-               const __grid_constant__ OutArgs p) {
+               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ OutArgs p) {
   using C = Lin<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
   LinBars* bars = reinterpret_cast<LinBars*>(smem + C::OFF_BAR);
@@ -581,18 +586,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < C::NQ; ++i) {
       mbar_init(&bars->q_full[i], 1);
       mbar_init(&bars->q_empty[i], 1);
-      mbar_init(&bars->out_ready[i], 128);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->k_done[i], 1);
-      mbar_init(&bars->kt_full[i], 128);
     }
     for (int i = 0; i < C::NKV; ++i) {
       mbar_init(&bars->kv_full[i], 1);
       mbar_init(&bars->kv_empty[i], 1);
     }
-    mbar_init(&bars->s_full, 1);
-    mbar_init(&bars->p_full, 128);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->k_done[i], 1);
+      mbar_init(&bars->kt_full[i], 128);
+    }
     mbar_init(&bars->o_full, 1);
     mbar_init(&bars->ab_free, 4);
     mbar_init(&bars->u_full, 1);
@@ -610,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
   const int group = BACK ? p.gy : p.gx;
-  // Every role walks the same items and counts what it has passed: items (it), chunks (ch), Q tiles (qi), K/V tiles (ki).
+  // Every role walks the same items and counts what it has passed.
 
   if (warp < 4) {
     setmaxnreg_dec<C::REG_CTRL>();
@@ -665,36 +669,49 @@ __global__ void __launch_bounds__(kThreads, 1)
       // -------------------------------------------------------- MMA issuer
       // Every lane runs every step, no lane's answer to a wait decides where the warp goes, and the elected lane issues
       // as long as its own waits were met; a vote an item ends the walk.  The MMAs of one issuer execute in order, so
-      // Q K^T of an item, issued behind P V of the one before, may overwrite its P.
+      // Q K^T of an item may overwrite a P whose P V was issued before.
       const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
       const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16, 1024), kt = smem_desc(sbase + C::OFF_KV, 16384, 1024);
       const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
       bool ok = true;
-      uint32_t qi = 0, ki = 0, it = 0, ch = 0, oi = 0;   // oi: outputs
-      // Q K^T of an item whose tiles are qi and ki
-      auto issue_s = [&](bool new_q, bool new_k, bool last_k) {
-        if (new_q) ok = ok && mbar_wait(&bars->q_full[qi % C::NQ], (qi / C::NQ) & 1);
-        if (new_k) ok = ok && mbar_wait(&bars->kv_full[ki % C::NKV], (ki / C::NKV) & 1);
+      // The next Q K^T: its Q and K tile, item, and the number of keys handed over for weighting.
+      uint32_t sq = 0xffffffffu, sk = 0xffffffffu, si = 0, handed = 0;
+      auto issue_s = [&](int h, bool weigh) {
+        const bool lastk = BACK || h == group - 1;
+        if (!BACK || h == 0) {
+          ++sq;
+          ok = ok && mbar_wait(&bars->q_full[sq % C::NQ], (sq / C::NQ) & 1);
+        }
+        if (BACK || h == 0) {
+          ++sk;
+          ok = ok && mbar_wait(&bars->kv_full[sk % C::NKV], (sk / C::NKV) & 1);
+        }
         tc_fence_after();
         if (elect_one() && ok) {
-          const uint64_t a = desc_at(qd, qi % C::NQ * C::TILE), b = desc_at(kd, ki % C::NKV * 2 * C::TILE);
+          const uint64_t a = desc_at(qd, sq % C::NQ * C::TILE), b = desc_at(kd, sk % C::NKV * 2 * C::TILE);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
-            tc_mma_ss(tmem + C::TM_P, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
+            tc_mma_ss(tmem + C::TM_P + si % C::NP * 128, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
           }
-          tc_commit(&bars->s_full);
-          if (last_k) tc_commit(&bars->k_done[ki & 1]);
+          tc_commit(&bars->s_full[si % C::NP]);
+          if (lastk && weigh) tc_commit(&bars->k_done[handed & 1]);
+          if (BACK && group > 1 && h == group - 1) tc_commit(&bars->q_empty[sq % C::NQ]);
         }
         __syncwarp();
+        ++si;
+        if (lastk && weigh) ++handed;
       };
+      uint32_t qi = 0, ki = 0, it = 0, ch = 0, oi = 0, weighed = 0;   // tiles, items, chunks, outputs
       bool more = w.next(), go = true;
-      if (more) issue_s(true, true, BACK || group == 1);
+      if (more) issue_s(0, w.c1 - w.c0 > 1);
       while (go && more) {
         const int chunks = w.c1 - w.c0;
         for (int n = 0; go && n < chunks; ++n, ++ch) {
+          const bool weigh = n < chunks - 1;
           for (int h = 0; h < group; ++h, ++it) {
             const bool first = !BACK || h == 0, out = !BACK || h == group - 1, lastk = BACK || h == group - 1;
+            const bool end = h == group - 1;
             const uint32_t q = qi % C::NQ, k = ki % C::NKV;
             if (first) {  // A = Q S
               if (h == 0) ok = ok && mbar_wait(&bars->s_ready, ch & 1);
@@ -706,10 +723,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int kk = 0; kk < D / 16; ++kk)
                   tc_mma_ss(tmem + C::TM_A, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048),
                             C::IDESC_A, kk > 0);
+                if (!BACK || group == 1) tc_commit(&bars->q_empty[q]);
               }
               __syncwarp();
             }
-            ok = ok && mbar_wait(&bars->p_full, it & 1);
+            // the next item's Q K^T: ahead of this one's P where P has two buffers, else behind its P V
+            auto ahead = [&] {
+              if (!end) {
+                issue_s(h + 1, weigh);
+              } else if (weigh) {
+                issue_s(0, n + 1 < chunks - 1);
+              } else {
+                more = w.next();
+                if (more) issue_s(0, w.c1 - w.c0 > 1);
+              }
+            };
+            if (C::NP == 2) ahead();
+            ok = ok && mbar_wait(&bars->p_full[it % C::NP], (it / C::NP) & 1);
             go = __all_sync(0xffffffffu, ok);
             if (!go) break;
             tc_fence_after();
@@ -717,20 +747,18 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t b = desc_at(kt, k * 2 * C::TILE + C::TILE);
 #pragma unroll
               for (int kk = 0; kk < 8; ++kk)
-                tc_mma_ts(tmem + C::TM_B, tmem + C::TM_P + kk * 8, desc_at(b, kk * 2048), C::IDESC_B,
+                tc_mma_ts(tmem + C::TM_B, tmem + C::TM_P + it % C::NP * 128 + kk * 8, desc_at(b, kk * 2048), C::IDESC_B,
                           kk > 0 || !first);
               if (out) tc_commit(&bars->o_full);
+              if (lastk && !weigh) {   // the piece's last state is not needed
+                tc_commit(&bars->kv_empty[k]);
+                if (end) tc_commit(&bars->u_full);
+              }
             }
             __syncwarp();
-            // the next item's Q K^T ahead of the wait for this one's weighted keys
-            const bool end = h == group - 1;
-            bool follows = true;
-            if (end && n == chunks - 1) follows = more = w.next();
-            if (out) ++qi, ++oi;
-            if (lastk) ++ki;
-            if (follows) issue_s(out, lastk, BACK || (end ? group == 1 : h + 1 == group - 1));
-            if (lastk) {  // U (+)= K^T V
-              ok = ok && mbar_wait(&bars->kt_full[(ki - 1) & 1], ((ki - 1) >> 1) & 1);
+            if (C::NP == 1) ahead();
+            if (lastk && weigh) {  // U (+)= K^T V
+              ok = ok && mbar_wait(&bars->kt_full[weighed & 1], (weighed >> 1) & 1);
               tc_fence_after();
               if (elect_one() && ok) {
                 const uint64_t a = desc_at(kt, k * 2 * C::TILE), b = desc_at(a, C::TILE);
@@ -742,86 +770,94 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (end) tc_commit(&bars->u_full);
               }
               __syncwarp();
+              ++weighed;
             }
+            if (out) ++qi, ++oi;
+            if (lastk) ++ki;
           }
         }
       }
       go = __all_sync(0xffffffffu, ok);
       if (!go) set_abort(&bars->abort, p.c.status);
-    } else if (warp == 2 && lane == 0) {
-      // -------------------------------------------------------- O out of shared memory
-      bool go = true;
-      uint32_t oi = 0;
-      while (go && w.next())
-        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
-          for (int h = 0; h < p.gx; ++h, ++oi) {
-            const uint32_t slot = oi % C::NQ;
-            if (!mbar_wait(&bars->out_ready[slot], (oi / C::NQ) & 1) || gave_up()) {
-              set_abort(&bars->abort, p.c.status);
-              go = false;
-              break;
-            }
-            if (w.rows(c) == kChunk) {
-#pragma unroll
-              for (int kb = 0; kb < D / 64; ++kb)
-                tma_store_3d(&tm_o, sbase + C::OFF_Q + slot * C::TILE + kb * 16384, kb * 64, w.head * p.gx + h,
-                             w.start + c * kChunk);
-              bulk_commit();
-              bulk_wait_read();
-            }
-            mbar_arrive(&bars->q_empty[slot]);
-          }
-        }
     }
   } else if (warp < 8) {
     // ---------------------------------------------------------- P
     const int quad = warp & 3, r = quad * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    float* tab = reinterpret_cast<float*>(smem + C::OFF_TAB) + quad * 32;
+    const uint32_t tab_at = smem_u32(tab);
     bool go = true;
     uint32_t it = 0, ki = 0;
     while (go && w.next()) {
-      // lam^(r - c) (c - r) of columns c, c + 1 from the exact distances: a token sees itself with weight 1 however fast
-      // the head forgets
+      // Weights lam^|r - c|.  In a group of 32 columns that the diagonal does not cross they are a power for the row, from
+      // the group's near end, times one of 32 powers for the column, at most 1 both; in the diagonal's, powers of the
+      // exact distances, so that a token sees itself with weight 1 however fast the head forgets.
+      __syncwarp();
+      tab[lane] = exp2f(w.l2 * (float)(BACK ? lane : 31 - lane));
+      __syncwarp();
       const float sl = BACK ? -w.l2 : w.l2;
-      const uint64_t slope = f2pack(sl, sl), at = f2pack((float)r, (float)r);
+      const uint64_t slope = f2pack(sl, sl);
       for (int n = 0; go && n < w.c1 - w.c0; ++n) {
         const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
         const int rows = w.rows(c);
         for (int h = 0; h < group; ++h, ++it) {
-          if (!mbar_wait_warp(&bars->s_full, it & 1) || __any_sync(0xffffffffu, gave_up())) {
+          const uint32_t tp = trow + C::TM_P + it % C::NP * 128;
+          if (!mbar_wait_warp(&bars->s_full[it % C::NP], (it / C::NP) & 1) || __any_sync(0xffffffffu, gave_up())) {
             go = false;
             break;
           }
           tc_fence_after();
-          uint32_t pk[64];
-#pragma unroll
+          // Group by group of 32 columns in a loop that is not unrolled: the roles' code together outgrows the
+          // instruction cache.  P of a group goes over columns of Q K^T that have been read.
+#pragma unroll 1
           for (int g = 0; g < 4; ++g) {
-            const bool none = BACK ? g < quad || g * 32 >= rows : g > quad;
-            if (none) {
+            uint32_t pk[16];
+            if (BACK ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
 #pragma unroll
-              for (int i = 0; i < 16; ++i) pk[g * 16 + i] = 0u;
-              continue;
-            }
-            uint32_t s[32];
-            tmem_ld_32x32b_x32(trow + C::TM_P + g * 32, s);
-            tmem_ld_wait();
-            reg_fence<32>(s);
-            // columns of the group that the row takes, a bit each
-            uint32_t seen = 0xffffffffu;
-            if (g == quad) seen = BACK ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-            if (BACK && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
+              for (int i = 0; i < 16; ++i) pk[i] = 0u;
+            } else {
+              uint32_t s[32];
+              tmem_ld_32x32b_x32(tp + g * 32, s);
+              if (g == quad || (BACK && rows - g * 32 < 32)) {
+                uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
+                if (g == quad) seen = BACK ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                if (BACK && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
+                const float gap = (float)(r - g * 32);
+                const uint64_t at = f2pack(gap, gap);
+                tmem_ld_wait();
+                reg_fence<32>(s);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float c0 = (float)(g * 32 + 2 * i);
-              float e0, e1, x0, x1;
-              f2unpack(fmul2(slope, fadd2(at, f2pack(-c0, -c0 - 1.f))), e0, e1);
-              f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), f2pack(ex2(e0), ex2(e1))),
-                       x0, x1);
-              x0 = seen >> (2 * i) & 1 ? x0 : 0.f;
-              x1 = seen >> (2 * i + 1) & 1 ? x1 : 0.f;
-              pk[g * 16 + i] = pack_bf16(x0, x1);
+                for (int i = 0; i < 16; ++i) {
+                  float e0, e1, x0, x1;
+                  f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                 f2pack(ex2(e0), ex2(e1))),
+                           x0, x1);
+                  x0 = seen >> (2 * i) & 1 ? x0 : 0.f;
+                  x1 = seen >> (2 * i + 1) & 1 ? x1 : 0.f;
+                  pk[i] = pack_bf16(x0, x1);
+                }
+              } else {
+                const float rf = ex2(w.l2 * (float)(BACK ? g * 32 - r : r - g * 32 - 31));
+                const uint64_t rf2 = f2pack(rf, rf);
+                tmem_ld_wait();
+                reg_fence<32>(s);
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                  const uint4 f = ld_shared_v4(tab_at + i * 8);
+                  float x0, x1;
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                 fmul2(rf2, f2pack(__uint_as_float(f.x), __uint_as_float(f.y)))),
+                           x0, x1);
+                  pk[i] = pack_bf16(x0, x1);
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i + 2]), __uint_as_float(s[2 * i + 3])),
+                                 fmul2(rf2, f2pack(__uint_as_float(f.z), __uint_as_float(f.w)))),
+                           x0, x1);
+                  pk[i + 1] = pack_bf16(x0, x1);
+                }
+              }
             }
+            tmem_st_32x32b_x16(tp + g * 16, pk);
           }
           if ((BACK || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
             const uint32_t slot = ki % C::NKV;
@@ -833,17 +869,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             fence_proxy_async_smem();
           }
           if (BACK || h == group - 1) ++ki;
-          tmem_st_32x32b_x32(trow + C::TM_P, *reinterpret_cast<uint32_t(*)[32]>(&pk[0]));
-          tmem_st_32x32b_x32(trow + C::TM_P + 32, *reinterpret_cast<uint32_t(*)[32]>(&pk[32]));
           tmem_st_wait();
           tc_fence_before();
-          mbar_arrive(&bars->p_full);
+          mbar_arrive(&bars->p_full[it % C::NP]);
         }
       }
     }
     if (!go) set_abort(&bars->abort, p.c.status);
   } else if (warp < 12) {
     // ---------------------------------------------------------- O
+    // A thread stores its row from registers, whole 32-byte sectors.  Through the Q tile by a bulk copy the tile was
+    // held until the copy had read it, 2,000 cycles, and loads came late: 40/8/128, one long rollout, 1.41 ms.
     setmaxnreg_dec<C::REG_OUT>();
     const int quad = warp & 3, r = quad * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
@@ -861,11 +897,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           tc_fence_after();
-          const uint32_t tile = sbase + C::OFF_Q + oi % C::NQ * C::TILE + r * 128;
           bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + w.head * p.gx + h) * D;
-#pragma unroll
+#pragma unroll 1
           for (int g = 0; g < D / 32; ++g) {
-            uint32_t a[32], b[32], o[16];
+            uint32_t a[32], b[32], o[2][8];
             tmem_ld_32x32b_x32(trow + C::TM_A + g * 32, a);
             tmem_ld_32x32b_x32(trow + C::TM_B + g * 32, b);
             tmem_ld_wait();
@@ -882,20 +917,13 @@ __global__ void __launch_bounds__(kThreads, 1)
               f2unpack(ffma2(fa2, f2pack(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
                              fmul2(fb2, f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])))),
                        x0, x1);
-              o[i] = pack_bf16(x0, x1);
+              o[i >> 3][i & 7] = pack_bf16(x0, x1);
             }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              if (rows == kChunk)
-                st_shared_v4(tile + (g >> 1) * 16384 + ((((g & 1) * 4 + u) ^ (r & 7)) << 4), o[4 * u], o[4 * u + 1],
-                             o[4 * u + 2], o[4 * u + 3]);
-              else if (r < rows)
-                *reinterpret_cast<uint4*>(row + g * 32 + u * 8) =
-                    make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+            if (r < rows) {
+              st_global_32(row + g * 32, o[0], p.wide);
+              st_global_32(row + g * 32 + 16, o[1], p.wide);
             }
           }
-          fence_proxy_async_smem();
-          mbar_arrive(&bars->out_ready[oi % C::NQ]);
         }
       }
     if (!go) set_abort(&bars->abort, p.c.status);
@@ -906,8 +934,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     const bool mine = D == 128 || quad < 2;   // a row of the state
     bool go = true;
-    uint32_t ki = 0, ch = 0;
+    uint32_t ki = 0, ch = 0, weighed = 0;     // ki: the K tile of the next one to weight
     while (go && w.next()) {
+      const int chunks = w.c1 - w.c0;
       float s[D];
       if (mine) {
 #pragma unroll
@@ -958,9 +987,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ch) {
-        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
-        const int rows = w.rows(c);
+      // Key tiles weighted before the state of chunk n + 1 is made: those of chunks up to n, and the first of chunk n + 1
+      // where one product alone reads it as it was loaded, without waiting for that chunk's state.
+      const bool early = BACK || group == 1;
+      const int64_t keys = (int64_t)(chunks - 1) * p.gy;   // the last chunk's are not: no state comes behind it
+      int64_t done = 0;
+      for (int n = 0; go && n < chunks; ++n, ++ch) {
+        const bool weigh = n < chunks - 1;
         // the copy that the chunk's queries read: the products with the one before are complete (u_full)
         if (mine) {
           const uint32_t dst = sbase + C::OFF_S + r * 128;
@@ -972,46 +1005,44 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         fence_proxy_async_smem();
         mbar_arrive(&bars->s_ready);
-        const float wt = r < rows ? exp2f(w.l2 * (float)(BACK ? r : rows - 1 - r)) : 0.f;
-        for (int j = 0; j < p.gy; ++j, ++ki) {
-          const uint32_t slot = ki % C::NKV, tile = sbase + C::OFF_KV + slot * 2 * C::TILE;
-          if (!mbar_wait_warp(&bars->k_done[ki & 1], (ki >> 1) & 1) || !mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1) ||
-              __any_sync(0xffffffffu, gave_up())) {
+        int64_t target = (int64_t)(n + 1) * p.gy + (early ? 1 : 0);
+        if (target > keys) target = keys;
+        for (; done < target; ++done, ++weighed, ++ki) {
+          const uint32_t slot = ki % C::NKV, tile = sbase + C::OFF_KV + slot * 2 * C::TILE + r * 128;
+          const int m = (int)(done / p.gy), rows = w.rows(BACK ? w.c1 - 1 - m : w.c0 + m);
+          const float wt = exp2f(w.l2 * (float)(BACK ? r : max(rows - 1 - r, 0)));
+          const uint64_t wt2 = f2pack(wt, wt);
+          if (!mbar_wait_warp(&bars->k_done[weighed & 1], (weighed >> 1) & 1) ||
+              !mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1) || __any_sync(0xffffffffu, gave_up())) {
             go = false;
             break;
           }
-          if (r >= rows) {
-            zero_row<D>(tile, r);
-          } else {
-            const uint64_t wt2 = f2pack(wt, wt);
+#pragma unroll 4
+          for (int u = 0; u < D / 8; ++u) {
+            const uint32_t at = tile + (u >> 3) * 16384 + (((u + r) & 7) << 4);
+            const uint4 x = ld_shared_v4(at);
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            uint32_t y[4];
 #pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb)
-#pragma unroll
-              for (int u = 0; u < 8; ++u) {
-                const uint32_t at = tile + kb * 16384 + r * 128 + (((u + r) & 7) << 4);
-                const uint4 x = ld_shared_v4(at);
-                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-                uint32_t y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  float a, b;
-                  f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
-                  y[i] = pack_bf16(a, b);
-                }
-                st_shared_v4(at, y[0], y[1], y[2], y[3]);
-              }
+            for (int i = 0; i < 4; ++i) {
+              float a, b;
+              f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
+              y[i] = r < rows ? pack_bf16(a, b) : 0u;   // rows of the next segment may hold anything
+            }
+            st_shared_v4(at, y[0], y[1], y[2], y[3]);
           }
           fence_proxy_async_smem();
-          mbar_arrive(&bars->kt_full[ki & 1]);
+          mbar_arrive(&bars->kt_full[weighed & 1]);
         }
-        if (!go) break;
-        if (!mbar_wait_warp(&bars->u_full, ch & 1)) {
+        if (!weigh) ki += p.gy;
+        if (!go || !mbar_wait_warp(&bars->u_full, ch & 1)) {
           go = false;
           break;
         }
         tc_fence_after();
-        if (mine) {
-          const float f = exp2f(w.l2 * (float)rows);
+        if (weigh && mine) {
+          const float f = exp2f(w.l2 * (float)w.rows(BACK ? w.c1 - 1 - n : w.c0 + n));
+          const uint64_t f2 = f2pack(f, f);
 #pragma unroll
           for (int g = 0; g < D / 32; ++g) {
             uint32_t u[32];
@@ -1019,7 +1050,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld_wait();
             reg_fence<32>(u);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[g * 32 + i] = fmaf(f, s[g * 32 + i], __uint_as_float(u[i]));
+            for (int i = 0; i < 32; i += 2)
+              f2unpack(ffma2(f2, f2pack(s[g * 32 + i], s[g * 32 + i + 1]),
+                             f2pack(__uint_as_float(u[i]), __uint_as_float(u[i + 1]))),
+                       s[g * 32 + i], s[g * 32 + i + 1]);
           }
         }
         tc_fence_before();
@@ -1162,8 +1196,7 @@ cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, con
   using C = Sta<D>;
   alignas(64) CUtensorMap tk, tv;
   const int64_t heads = (int64_t)a.hkv * group;
-  if (!encode(&tk, k, D, heads, a) ||
-      !encode(&tv, v, D, heads, a))
+  if (!encode(&tk, k, D, heads, a) || !encode(&tv, v, D, heads, a))
     return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
@@ -1182,12 +1215,9 @@ template <int D, bool BACK>
 cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int gx, int gy,
                        const float* slots, const float* state_in, float* state_out, void* out, cudaStream_t st) {
   using C = Lin<D>;
-  alignas(64) CUtensorMap tq, tk, tv, to;
+  alignas(64) CUtensorMap tq, tk, tv;
   const int64_t hx = (int64_t)a.hkv * gx, hy = (int64_t)a.hkv * gy;
-  if (!encode(&tq, q, D, hx, a) ||
-      !encode(&tk, k, D, hy, a) ||
-      !encode(&tv, v, D, hy, a) ||
-      !encode(&to, out, D, hx, a))
+  if (!encode(&tq, q, D, hx, a) || !encode(&tk, k, D, hy, a) || !encode(&tv, v, D, hy, a))
     return cudaErrorInvalidValue;
   const void* fn = reinterpret_cast<const void*>(linear_out<D, BACK>);
   static std::atomic<int> regs_cache{-1};
@@ -1205,7 +1235,8 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
   p.gy = gy;
   p.scale = a.scale;
   p.out = static_cast<bf16*>(out);
-  linear_out<D, BACK><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, to, p);
+  p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
+  linear_out<D, BACK><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, p);
   return cudaGetLastError();
 }
 
