@@ -290,13 +290,25 @@ __global__ void __launch_bounds__(kStaThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
+  // The next piece, for states between pieces without the chunks so far from its end that their weight is 0 in fp32
+  // (2^-150 and less, which rounds to 0): a head that forgets in a thousand tokens reads a tenth of a long piece.
+  auto next = [&] {
+    if (!w.next()) return false;
+    if (p.state_out == nullptr && w.l2 < 0.f) {
+      const float far = 150.f / (-w.l2 * kChunk);
+      const int keep = far < 1e6f ? (int)far + 2 : 1 << 24;
+      if (p.back) w.c1 = min(w.c1, w.c0 + keep);
+      else w.c0 = max(w.c0, w.c1 - keep);
+    }
+    return true;
+  };
 
   if (warp == 0) {
     // ---------------------------------------------------------- producer
     if (lane == 0) {
       bool go = true;
       uint32_t it = 0;
-      while (go && w.next())
+      while (go && next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n) {
           const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
           for (int h = 0; h < p.group; ++h, ++it) {
@@ -323,7 +335,7 @@ __global__ void __launch_bounds__(kStaThreads, 1)
     const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16384, 1024), td = smem_desc(sbase + C::OFF_TERM, 16384, 1024);
     bool ok = true, go = true;
     uint32_t it = 0, un = 0;
-    while (go && w.next())
+    while (go && next())
       for (int n = 0; go && n < w.c1 - w.c0; ++n, ++un)
         for (int h = 0; h < p.group; ++h, ++it) {
           const uint32_t slot = it & 1, buf = un & 1;
@@ -352,7 +364,7 @@ __global__ void __launch_bounds__(kStaThreads, 1)
     const int r = threadIdx.x - 128;
     bool go = true;
     uint32_t it = 0;
-    while (go && w.next())
+    while (go && next())
       for (int n = 0; go && n < w.c1 - w.c0; ++n) {
         const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
         const int rows = w.rows(c);
@@ -408,7 +420,7 @@ __global__ void __launch_bounds__(kStaThreads, 1)
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     bool go = true;
     uint32_t un = 0;
-    while (go && w.next()) {
+    while (go && next()) {
       float s[D];
 #pragma unroll
       for (int i = 0; i < D; ++i) s[i] = 0.f;
@@ -484,39 +496,48 @@ struct OutArgs {
   int32_t gx, gy;          // query heads and key heads of a state; one of them is 1
   float scale;
   bool wide;               // out is 32-byte aligned
+  bool transposed;         // of the slots' states (the way back in time)
   bf16* out;
 };
 
-template <int D>
+// What a launch of linear_out works on: a group of query heads to a key head (FWD, also one), in order; or, from the last
+// token to the first, one key head (BACK1) or a group of them (BACK) to a query head.
+enum { FWD, BACK1, BACK };
+
+template <int D, int KIND>
 struct Lin {
   static constexpr int TILE = kChunk * D * 2;
-  static constexpr int NQ = D == 64 ? 4 : 2;
-  static constexpr int NKV = D == 64 ? 3 : 2;
-  static constexpr int NP = D == 64 ? 2 : 1;             // buffers of Q K^T and P
+  // Tiles of Q, and of K and V, which take turns.  A group of key heads has a K and a V to each item and keeps its Q.
+  static constexpr int NQ = D == 64 ? 4 : KIND == BACK ? 1 : 2;
+  static constexpr int NT = D == 64 ? 8 : KIND == BACK ? 5 : 4;
+  static constexpr int NP = 2;                           // buffers of Q K^T and P
+  static constexpr int NR = D == 64 ? 4 : 2;             // of outputs and K^T V, which take turns
   static constexpr int OFF_Q = 0;
-  static constexpr int OFF_KV = NQ * TILE;               // K, V of a slot
-  static constexpr int OFF_S = OFF_KV + NKV * 2 * TILE;  // the state, D rows of k's dims, like a V tile
+  static constexpr int OFF_T = NQ * TILE;
+  static constexpr int OFF_S = OFF_T + NT * TILE;        // the state, D rows of k's dims, like a V tile
   static constexpr int OFF_TAB = OFF_S + D * D * 2;      // 32 powers of the decay for each warp that makes P
-  static constexpr int OFF_BAR = OFF_TAB + 512;
+  static constexpr int OFF_BAR = OFF_TAB + 8 * 128;
   static constexpr int SMEM = OFF_BAR + 512;
-  static constexpr int TM_P = 0, TM_A = NP * 128, TM_B = TM_A + D, TM_U = TM_B + D;
+  static constexpr int TM_P = 0, TM_R = NP * 128;
   static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);  // Q (K-major) x K^T (K-major)
   static constexpr uint32_t IDESC_A = idesc_bf16(128, D, 0, 1);    // Q (K-major) x S (MN-major)
   static constexpr uint32_t IDESC_B = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
-  // K^T (MN-major) x V (MN-major).  M = 128 at D = 64 too, whose lanes 64 .. 127 take the V tile behind K's and are
-  // not read: an M of 64 lies in other lanes.
+  // K^T (MN-major) x V (MN-major).  M = 128 at D = 64 too, whose lanes 64 .. 127 take the tile behind K's (or the
+  // state) and are not read: an M of 64 lies in other lanes.
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
-  static constexpr int REG_CTRL = 72, REG_P = 128, REG_OUT = 104, REG_STATE = 208;
-  static_assert(REG_CTRL + REG_P + REG_OUT + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
-  static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
+  static constexpr int REG_CTRL = 96, REG_ROWS = 96, REG_STATE = 224;
+  static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
+  static_assert(SMEM <= 232448 && TM_R + NR * D <= 512, "shared memory and TMEM budgets");
+  static_assert(D == 128 || NT % 2 == 0, "behind a K tile lies another tile");
 };
 
 struct LinBars {
-  uint64_t q_full[4], q_empty[4], kv_full[3], kv_empty[3];
+  uint64_t q_full[4], q_empty[4], t_full[8], t_empty[8];
   uint64_t s_full[2];  // Q K^T of an item
   uint64_t p_full[2];  // its P is in TMEM
-  uint64_t o_full;     // the products of an output are complete
-  uint64_t ab_free;    // and in registers
+  uint64_t a_full[2];  // Q S, for the warpgroup that scales its rows
+  uint64_t o_full[4];  // of an output buffer: its products are complete
+  uint64_t r_free[4];  // and what it held, an output or K^T V, is in registers
   // Two of each, as the issuer may be a K ahead of the warps that weight them and they of it.
   uint64_t k_done[2];  // a K that is to be weighted is no longer read as it was loaded
   uint64_t kt_full[2]; // and weighted
@@ -542,23 +563,32 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8], bo
                : "memory");
 }
 
+// O is one accumulator for both terms: Q S first, then P V on top.  With m = 64, the middle of a chunk,
+//   o_i = scale lam^(i+1-m) [ q_i (lam^m S) + sum_{j <= i} lam^(m-j-1) (q_i . k_j) v_j ]
+// so that P has a factor for each column alone and the row's comes last, as long as lam^-m stays small: 2^32 at most
+// (kSlow; the other way in time: rows lam^(m-i), columns lam^(j-m), the state lam^(n-m)).  For a head that forgets faster P has its
+// exact powers and the rows of Q S are scaled in TMEM.
+constexpr int kMiddle = 64;
+constexpr float kSlow = -0.5f;   // log2 of the decay
+
 // An item is a chunk with one query and one key head: of a group of query heads (gx) each item has an output and the
 // chunk one K and V, of a group of key heads (gy) each item has a K and V and the chunk one output.
 // Warp roles:
 //   warp 0       TMA producer;  warp 1  TMEM and every MMA
-//   warps 4-7    P = lam^(i-j) Q K^T below the diagonal, in bf16 for P V (a thread a query)
-//   warps 8-11   O = scale (lam^(i+1) Q S + P V)
+//   warps 4-11   two warpgroups, for every other item: P below the diagonal, in bf16 for P V (a thread a query), then
+//                O out of TMEM, scaled
 //   warps 12-15  the weighted keys, and the state in registers (a thread a row), its bf16 copy in shared memory
-template <int D, bool BACK>
+template <int D, int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_out(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ OutArgs p) {
-  using C = Lin<D>;
+  using C = Lin<D, KIND>;
+  constexpr bool back = KIND != FWD;
   extern __shared__ __align__(1024) uint8_t smem[];
   LinBars* bars = reinterpret_cast<LinBars*>(smem + C::OFF_BAR);
   Walk w(p.c, blockIdx.x);
   // sequences without a token: their states go through
-  if (!BACK && p.state_out != nullptr)
+  if (!back && p.state_out != nullptr)
     for (int s = blockIdx.x; s < p.c.num_segments; s += gridDim.x)
       if (p.c.cu[s] == p.c.cu[s + 1] && p.c.cu[s] >= 0 && p.c.cu[s] <= p.c.num_tokens) {
         const size_t n = (size_t)p.c.heads * D * D / 4, at = n * s;
@@ -587,18 +617,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars->q_full[i], 1);
       mbar_init(&bars->q_empty[i], 1);
     }
-    for (int i = 0; i < C::NKV; ++i) {
-      mbar_init(&bars->kv_full[i], 1);
-      mbar_init(&bars->kv_empty[i], 1);
+    for (int i = 0; i < C::NT; ++i) {
+      mbar_init(&bars->t_full[i], 1);
+      mbar_init(&bars->t_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->s_full[i], 1);
       mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->a_full[i], 1);
       mbar_init(&bars->k_done[i], 1);
       mbar_init(&bars->kt_full[i], 128);
     }
-    mbar_init(&bars->o_full, 1);
-    mbar_init(&bars->ab_free, 4);
+    for (int i = 0; i < C::NR; ++i) {
+      mbar_init(&bars->o_full[i], 1);
+      mbar_init(&bars->r_free[i], 4);
+    }
     mbar_init(&bars->u_full, 1);
     mbar_init(&bars->s_ready, 128);
     bars->abort = 0;
@@ -613,7 +646,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
-  const int group = BACK ? p.gy : p.gx;
+  const int group = KIND == FWD ? p.gx : KIND == BACK ? p.gy : 1;
+  constexpr bool per_k = KIND != FWD;   // an item has a K and V of its own; else an output of its own
   // Every role walks the same items and counts what it has passed.
 
   if (warp < 4) {
@@ -621,74 +655,58 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0 && lane == 0) {
       // -------------------------------------------------------- producer
       bool go = true;
-      uint32_t qi = 0, ki = 0;
-      auto fail = [&] {
-        set_abort(&bars->abort, p.c.status);
-        go = false;
+      uint32_t qi = 0, ti = 0;
+      auto load = [&](int off, uint64_t* full, uint64_t* empty, uint32_t i, uint32_t n, const CUtensorMap* tm, int head,
+                      int tok) {
+        const uint32_t slot = i % n;
+        if (!go || (i >= n && !mbar_wait(&empty[slot], (i / n - 1) & 1)) || gave_up()) {
+          go = false;
+          return;
+        }
+        mbar_arrive_expect_tx(&full[slot], C::TILE);
+#pragma unroll
+        for (int kb = 0; kb < D / 64; ++kb)
+          tma_load_3d(smem + off + slot * C::TILE + kb * 16384, tm, &full[slot], kb * 64, head, tok);
       };
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
-          const int tok = w.start + c * kChunk;
+          const int tok = w.start + (back ? w.c1 - 1 - n : w.c0 + n) * kChunk;
           for (int h = 0; go && h < group; ++h) {
-            if (gave_up()) {
-              go = false;
-              break;
-            }
-            if (BACK || h == 0) {
-              const uint32_t slot = ki % C::NKV;
-              if (ki >= C::NKV && !mbar_wait(&bars->kv_empty[slot], (ki / C::NKV - 1) & 1)) {
-                fail();
-                break;
-              }
-              mbar_arrive_expect_tx(&bars->kv_full[slot], 2 * C::TILE);
-#pragma unroll
-              for (int kb = 0; kb < D / 64; ++kb) {
-                uint8_t* dst = smem + C::OFF_KV + slot * 2 * C::TILE + kb * 16384;
-                tma_load_3d(dst, &tm_k, &bars->kv_full[slot], kb * 64, w.head * p.gy + (BACK ? h : 0), tok);
-                tma_load_3d(dst + C::TILE, &tm_v, &bars->kv_full[slot], kb * 64, w.head * p.gy + (BACK ? h : 0), tok);
-              }
-              ++ki;
-            }
-            if (!BACK || h == 0) {
-              const uint32_t slot = qi % C::NQ;
-              if (qi >= C::NQ && !mbar_wait(&bars->q_empty[slot], (qi / C::NQ - 1) & 1)) {
-                fail();
-                break;
-              }
-              mbar_arrive_expect_tx(&bars->q_full[slot], C::TILE);
-#pragma unroll
-              for (int kb = 0; kb < D / 64; ++kb)
-                tma_load_3d(smem + C::OFF_Q + slot * C::TILE + kb * 16384, &tm_q, &bars->q_full[slot], kb * 64,
-                            w.head * p.gx + (BACK ? 0 : h), tok);
-              ++qi;
-            }
+            const bool new_k = per_k || h == 0, new_q = !per_k || h == 0;
+            if (new_k) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_k, w.head * p.gy + (per_k ? h : 0), tok);
+            if (new_q) load(C::OFF_Q, bars->q_full, bars->q_empty, qi++, C::NQ, &tm_q, w.head * p.gx + (per_k ? 0 : h), tok);
+            if (new_k) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_v, w.head * p.gy + (per_k ? h : 0), tok);
           }
         }
+      if (!go) set_abort(&bars->abort, p.c.status);
     } else if (warp == 1) {
       // -------------------------------------------------------- MMA issuer
       // Every lane runs every step, no lane's answer to a wait decides where the warp goes, and the elected lane issues
       // as long as its own waits were met; a vote an item ends the walk.  The MMAs of one issuer execute in order, so
       // Q K^T of an item may overwrite a P whose P V was issued before.
+      //   FWD:          Q K^T of the next item;  K^T V after the chunk's last Q K^T;  P V;  Q S of the next item
+      //   BACK1, BACK:  Q K^T of the next item;  P V;  K^T V;  Q S of the next item if it is a chunk's first
+      // so that two items' P are made at a time, K^T V, which the next chunk's state waits for, comes early (the way back it
+      // waits for P's warps, which clear the rows of V behind a segment's end), and a Q tile is given back soon.
       const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
-      const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16, 1024), kt = smem_desc(sbase + C::OFF_KV, 16384, 1024);
+      const uint64_t kd = smem_desc(sbase + C::OFF_T, 16, 1024), kt = smem_desc(sbase + C::OFF_T, 16384, 1024);
       const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
       bool ok = true;
-      // The next Q K^T: its Q and K tile, item, and the number of keys handed over for weighting.
+      // Of the next Q K^T: its Q tile and K (and V) pair, item, and the number of keys handed over for weighting.
       uint32_t sq = 0xffffffffu, sk = 0xffffffffu, si = 0, handed = 0;
       auto issue_s = [&](int h, bool weigh) {
-        const bool lastk = BACK || h == group - 1;
-        if (!BACK || h == 0) {
+        const bool lastk = per_k || h == group - 1;
+        if (!per_k || h == 0) {
           ++sq;
           ok = ok && mbar_wait(&bars->q_full[sq % C::NQ], (sq / C::NQ) & 1);
         }
-        if (BACK || h == 0) {
+        if (per_k || h == 0) {
           ++sk;
-          ok = ok && mbar_wait(&bars->kv_full[sk % C::NKV], (sk / C::NKV) & 1);
+          ok = ok && mbar_wait(&bars->t_full[2 * sk % C::NT], (2 * sk / C::NT) & 1);
         }
         tc_fence_after();
         if (elect_one() && ok) {
-          const uint64_t a = desc_at(qd, sq % C::NQ * C::TILE), b = desc_at(kd, sk % C::NKV * 2 * C::TILE);
+          const uint64_t a = desc_at(qd, sq % C::NQ * C::TILE), b = desc_at(kd, 2 * sk % C::NT * C::TILE);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
@@ -696,38 +714,46 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tc_commit(&bars->s_full[si % C::NP]);
           if (lastk && weigh) tc_commit(&bars->k_done[handed & 1]);
-          if (BACK && group > 1 && h == group - 1) tc_commit(&bars->q_empty[sq % C::NQ]);
+          if (KIND == BACK && h == group - 1) tc_commit(&bars->q_empty[sq % C::NQ]);
         }
         __syncwarp();
         ++si;
         if (lastk && weigh) ++handed;
       };
-      uint32_t qi = 0, ki = 0, it = 0, ch = 0, oi = 0, weighed = 0;   // tiles, items, chunks, outputs
+      uint32_t ru = 0, aq = 0, chunk = 0;   // output buffers taken, and of the next Q S its Q tile and chunk
+      // an output buffer, when what it held last has been read
+      auto take = [&] {
+        if (ru >= C::NR) ok = ok && mbar_wait(&bars->r_free[ru % C::NR], (ru / C::NR - 1) & 1);
+        return tmem + C::TM_R + ru++ % C::NR * D;
+      };
+      auto issue_a = [&](bool new_chunk, bool fast, uint32_t item) {   // B = Q S of an item
+        if (new_chunk) ok = ok && mbar_wait(&bars->s_ready, chunk++ & 1);
+        const uint32_t dst = take(), q = aq++ % C::NQ;
+        tc_fence_after();
+        if (elect_one() && ok) {
+          const uint64_t a = desc_at(qd, q * C::TILE);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_ss(dst, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048), C::IDESC_A, kk > 0);
+          if (KIND != BACK) tc_commit(&bars->q_empty[q]);
+          if (fast) tc_commit(&bars->a_full[item & 1]);
+        }
+        __syncwarp();
+        return dst;
+      };
+      uint32_t ki = 0, it = 0, weighed = 0, tm_u = 0;
       bool more = w.next(), go = true;
       if (more) issue_s(0, w.c1 - w.c0 > 1);
+      uint32_t tm_b = 0, tm_next = more ? issue_a(true, w.l2 < kSlow, 0) : 0, outs = 0;
       while (go && more) {
         const int chunks = w.c1 - w.c0;
-        for (int n = 0; go && n < chunks; ++n, ++ch) {
+        bool fast = w.l2 < kSlow;
+        for (int n = 0; go && n < chunks; ++n) {
           const bool weigh = n < chunks - 1;
           for (int h = 0; h < group; ++h, ++it) {
-            const bool first = !BACK || h == 0, out = !BACK || h == group - 1, lastk = BACK || h == group - 1;
-            const bool end = h == group - 1;
-            const uint32_t q = qi % C::NQ, k = ki % C::NKV;
-            if (first) {  // A = Q S
-              if (h == 0) ok = ok && mbar_wait(&bars->s_ready, ch & 1);
-              if (oi > 0) ok = ok && mbar_wait(&bars->ab_free, (oi - 1) & 1);
-              tc_fence_after();
-              if (elect_one() && ok) {
-                const uint64_t a = desc_at(qd, q * C::TILE);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
-                  tc_mma_ss(tmem + C::TM_A, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048),
-                            C::IDESC_A, kk > 0);
-                if (!BACK || group == 1) tc_commit(&bars->q_empty[q]);
-              }
-              __syncwarp();
-            }
-            // the next item's Q K^T: ahead of this one's P where P has two buffers, else behind its P V
+            const bool out = !per_k || h == group - 1, lastk = per_k || h == group - 1, end = h == group - 1;
+            const uint32_t kslot = 2 * ki % C::NT, vslot = (2 * ki + 1) % C::NT;
+            if (!per_k || h == 0) tm_b = tm_next;
             auto ahead = [&] {
               if (!end) {
                 issue_s(h + 1, weigh);
@@ -735,44 +761,53 @@ __global__ void __launch_bounds__(kThreads, 1)
                 issue_s(0, n + 1 < chunks - 1);
               } else {
                 more = w.next();
+                fast = w.l2 < kSlow;
                 if (more) issue_s(0, w.c1 - w.c0 > 1);
               }
             };
-            if (C::NP == 2) ahead();
-            ok = ok && mbar_wait(&bars->p_full[it % C::NP], (it / C::NP) & 1);
-            go = __all_sync(0xffffffffu, ok);
-            if (!go) break;
-            tc_fence_after();
-            if (elect_one()) {  // B (+)= P V
-              const uint64_t b = desc_at(kt, k * 2 * C::TILE + C::TILE);
-#pragma unroll
-              for (int kk = 0; kk < 8; ++kk)
-                tc_mma_ts(tmem + C::TM_B, tmem + C::TM_P + it % C::NP * 128 + kk * 8, desc_at(b, kk * 2048), C::IDESC_B,
-                          kk > 0 || !first);
-              if (out) tc_commit(&bars->o_full);
-              if (lastk && !weigh) {   // the piece's last state is not needed
-                tc_commit(&bars->kv_empty[k]);
-                if (end) tc_commit(&bars->u_full);
-              }
-            }
-            __syncwarp();
-            if (C::NP == 1) ahead();
-            if (lastk && weigh) {  // U (+)= K^T V
+            auto issue_u = [&] {   // U (+)= K^T V
+              if (!per_k || h == 0) tm_u = take();
               ok = ok && mbar_wait(&bars->kt_full[weighed & 1], (weighed >> 1) & 1);
+              ok = ok && mbar_wait(&bars->t_full[vslot], ((2 * ki + 1) / C::NT) & 1);
               tc_fence_after();
               if (elect_one() && ok) {
-                const uint64_t a = desc_at(kt, k * 2 * C::TILE), b = desc_at(a, C::TILE);
+                const uint64_t a = desc_at(kt, kslot * C::TILE), b = desc_at(kt, vslot * C::TILE);
 #pragma unroll
                 for (int kk = 0; kk < 8; ++kk)
-                  tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U,
-                            kk > 0 || (BACK && h > 0));
-                tc_commit(&bars->kv_empty[k]);
+                  tc_mma_ss(tm_u, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U,
+                            kk > 0 || (per_k && h > 0));
+                tc_commit(&bars->t_empty[kslot]);
+                if (per_k) tc_commit(&bars->t_empty[vslot]);
                 if (end) tc_commit(&bars->u_full);
               }
               __syncwarp();
               ++weighed;
+            };
+            ahead();
+            if (!per_k && lastk && weigh) issue_u();
+            ok = ok && mbar_wait(&bars->p_full[it % C::NP], (it / C::NP) & 1);
+            ok = ok && mbar_wait(&bars->t_full[vslot], ((2 * ki + 1) / C::NT) & 1);
+            go = __all_sync(0xffffffffu, ok);
+            if (!go) break;
+            tc_fence_after();
+            if (elect_one()) {  // B += P V
+              const uint64_t b = desc_at(kt, vslot * C::TILE);
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                tc_mma_ts(tm_b, tmem + C::TM_P + it % C::NP * 128 + kk * 8, desc_at(b, kk * 2048), C::IDESC_B, 1);
+              if (out) tc_commit(&bars->o_full[outs % C::NR]);
+              if (lastk && !weigh) {   // the piece's last state is not needed
+                tc_commit(&bars->t_empty[kslot]);
+                tc_commit(&bars->t_empty[vslot]);
+                if (end) tc_commit(&bars->u_full);
+              } else if (!per_k && lastk) {
+                tc_commit(&bars->t_empty[vslot]);
+              }
             }
-            if (out) ++qi, ++oi;
+            __syncwarp();
+            if (out) ++outs;
+            if (per_k && weigh) issue_u();
+            if (end ? more : !per_k) tm_next = issue_a(end, fast, it + 1);
             if (lastk) ++ki;
           }
         }
@@ -780,152 +815,178 @@ __global__ void __launch_bounds__(kThreads, 1)
       go = __all_sync(0xffffffffu, ok);
       if (!go) set_abort(&bars->abort, p.c.status);
     }
-  } else if (warp < 8) {
-    // ---------------------------------------------------------- P
+  } else if (warp < 12) {
+    // ---------------------------------------------------------- P and O
+    setmaxnreg_dec<C::REG_ROWS>();
+    const uint32_t mine = warp < 8 ? 0 : 1;
     const int quad = warp & 3, r = quad * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
-    float* tab = reinterpret_cast<float*>(smem + C::OFF_TAB) + quad * 32;
+    float* tab = reinterpret_cast<float*>(smem + C::OFF_TAB) + (warp - 4) * 32;
     const uint32_t tab_at = smem_u32(tab);
     bool go = true;
-    uint32_t it = 0, ki = 0;
+    uint32_t it = 0, ki = 0, ru = 0, oi = 0, fasts = 0;   // ru: output buffers taken;  oi: outputs
     while (go && w.next()) {
-      // Weights lam^|r - c|.  In a group of 32 columns that the diagonal does not cross they are a power for the row, from
-      // the group's near end, times one of 32 powers for the column, at most 1 both; in the diagonal's, powers of the
-      // exact distances, so that a token sees itself with weight 1 however fast the head forgets.
+      // A column's factor is one of 32 powers, by its place in a group of 32, times one for the group; for a head that
+      // forgets fast the latter goes from the group's near end to the row, so that both are at most 1, and the group that
+      // the diagonal crosses takes powers of the exact distances: a token sees itself with weight 1.
+      const bool fast = w.l2 < kSlow;
       __syncwarp();
-      tab[lane] = exp2f(w.l2 * (float)(BACK ? lane : 31 - lane));
+      tab[lane] = exp2f(w.l2 * (float)(back ? lane : 31 - lane));
       __syncwarp();
-      const float sl = BACK ? -w.l2 : w.l2;
+      const float sl = back ? -w.l2 : w.l2;
       const uint64_t slope = f2pack(sl, sl);
       for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
+        const int c = back ? w.c1 - 1 - n : w.c0 + n;
         const int rows = w.rows(c);
+        const float f_out = fast ? p.scale : p.scale * exp2f(w.l2 * (float)(back ? kMiddle - r : r + 1 - kMiddle));
         for (int h = 0; h < group; ++h, ++it) {
-          const uint32_t tp = trow + C::TM_P + it % C::NP * 128;
-          if (!mbar_wait_warp(&bars->s_full[it % C::NP], (it / C::NP) & 1) || __any_sync(0xffffffffu, gave_up())) {
-            go = false;
-            break;
-          }
-          tc_fence_after();
-          // Group by group of 32 columns in a loop that is not unrolled: the roles' code together outgrows the
-          // instruction cache.  P of a group goes over columns of Q K^T that have been read.
-#pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
-            uint32_t pk[16];
-            if (BACK ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
-#pragma unroll
-              for (int i = 0; i < 16; ++i) pk[i] = 0u;
-            } else {
-              uint32_t s[32];
-              tmem_ld_32x32b_x32(tp + g * 32, s);
-              if (g == quad || (BACK && rows - g * 32 < 32)) {
-                uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
-                if (g == quad) seen = BACK ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-                if (BACK && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
-                const float gap = (float)(r - g * 32);
-                const uint64_t at = f2pack(gap, gap);
-                tmem_ld_wait();
-                reg_fence<32>(s);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  float e0, e1, x0, x1;
-                  f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
-                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
-                                 f2pack(ex2(e0), ex2(e1))),
-                           x0, x1);
-                  x0 = seen >> (2 * i) & 1 ? x0 : 0.f;
-                  x1 = seen >> (2 * i + 1) & 1 ? x1 : 0.f;
-                  pk[i] = pack_bf16(x0, x1);
-                }
-              } else {
-                const float rf = ex2(w.l2 * (float)(BACK ? g * 32 - r : r - g * 32 - 31));
-                const uint64_t rf2 = f2pack(rf, rf);
-                tmem_ld_wait();
-                reg_fence<32>(s);
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                  const uint4 f = ld_shared_v4(tab_at + i * 8);
-                  float x0, x1;
-                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
-                                 fmul2(rf2, f2pack(__uint_as_float(f.x), __uint_as_float(f.y)))),
-                           x0, x1);
-                  pk[i] = pack_bf16(x0, x1);
-                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i + 2]), __uint_as_float(s[2 * i + 3])),
-                                 fmul2(rf2, f2pack(__uint_as_float(f.z), __uint_as_float(f.w)))),
-                           x0, x1);
-                  pk[i + 1] = pack_bf16(x0, x1);
-                }
-              }
-            }
-            tmem_st_32x32b_x16(tp + g * 16, pk);
-          }
-          if ((BACK || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
-            const uint32_t slot = ki % C::NKV;
-            if (!mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1)) {
+          if ((it & 1) == mine) {
+            const uint32_t tp = trow + C::TM_P + it % C::NP * 128;
+            if (!mbar_wait_warp(&bars->s_full[it % C::NP], (it / C::NP) & 1) || __any_sync(0xffffffffu, gave_up())) {
               go = false;
               break;
             }
-            if (r >= rows) zero_row<D>(sbase + C::OFF_KV + slot * 2 * C::TILE + C::TILE, r);
-            fence_proxy_async_smem();
+            tc_fence_after();
+            // Group by group of 32 columns in a loop that is not unrolled: the roles' code together outgrows the
+            // instruction cache.  P of a group goes over columns of Q K^T that have been read.
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+              uint32_t pk[16];
+              if (back ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pk[i] = 0u;
+              } else {
+                uint32_t s[32];
+                tmem_ld_32x32b_x32(tp + g * 32, s);
+                uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
+                if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                if (back && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
+                const bool masked = g == quad || (back && rows - g * 32 < 32);
+                if (fast && masked) {
+                  const float gap = (float)(r - g * 32);
+                  const uint64_t at = f2pack(gap, gap);
+                  tmem_ld_wait();
+                  reg_fence<32>(s);
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) {
+                    float e0, e1, x0, x1;
+                    f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
+                    f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                   f2pack(ex2(e0), ex2(e1))),
+                             x0, x1);
+                    s[2 * i] = __float_as_uint(x0);
+                    s[2 * i + 1] = __float_as_uint(x1);
+                  }
+                } else {
+                  const float rf = exp2f(w.l2 * (float)(fast ? (back ? g * 32 - r : r - g * 32 - 31)
+                                                             : (back ? g * 32 - kMiddle : kMiddle - 32 - g * 32)));
+                  const uint64_t rf2 = f2pack(rf, rf);
+                  tmem_ld_wait();
+                  reg_fence<32>(s);
+#pragma unroll
+                  for (int i = 0; i < 32; i += 4) {
+                    const uint4 f = ld_shared_v4(tab_at + i * 4);
+                    const uint64_t f0 = fmul2(f2pack(__uint_as_float(f.x), __uint_as_float(f.y)), rf2);
+                    const uint64_t f1 = fmul2(f2pack(__uint_as_float(f.z), __uint_as_float(f.w)), rf2);
+                    float x0, x1, x2, x3;
+                    f2unpack(fmul2(f2pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), f0), x0, x1);
+                    f2unpack(fmul2(f2pack(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), f1), x2, x3);
+                    s[i] = __float_as_uint(x0);
+                    s[i + 1] = __float_as_uint(x1);
+                    s[i + 2] = __float_as_uint(x2);
+                    s[i + 3] = __float_as_uint(x3);
+                  }
+                }
+                if (masked) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (!(seen >> i & 1)) s[i] = 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+              }
+              tmem_st_32x32b_x16(tp + g * 16, pk);
+            }
+            if (fast && (!per_k || h == 0)) {   // the rows of Q S
+              if (!mbar_wait_warp(&bars->a_full[mine], fasts & 1)) {
+                go = false;
+                break;
+              }
+              tc_fence_after();
+              const float f = exp2f(w.l2 * (float)(back ? max(rows - r, 0) : r + 1));
+              const uint64_t f2 = f2pack(f, f);
+              const uint32_t tb = trow + C::TM_R + ru % C::NR * D;
+#pragma unroll 1
+              for (int g = 0; g < D / 32; ++g) {
+                uint32_t s[32];
+                tmem_ld_32x32b_x32(tb + g * 32, s);
+                tmem_ld_wait();
+                reg_fence<32>(s);
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                  float x0, x1;
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), f2), x0, x1);
+                  s[i] = __float_as_uint(x0);
+                  s[i + 1] = __float_as_uint(x1);
+                }
+                tmem_st_32x32b_x32(tb + g * 32, s);
+              }
+              ++fasts;
+            }
+            if ((per_k || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
+              const uint32_t v = 2 * ki + 1;
+              if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
+                go = false;
+                break;
+              }
+              if (r >= rows) zero_row<D>(sbase + C::OFF_T + v % C::NT * C::TILE, r);
+              fence_proxy_async_smem();
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(&bars->p_full[it % C::NP]);
           }
-          if (BACK || h == group - 1) ++ki;
-          tmem_st_wait();
-          tc_fence_before();
-          mbar_arrive(&bars->p_full[it % C::NP]);
+          if (per_k || h == group - 1) ++ki;
+          if (per_k && h < group - 1) continue;
+          // A thread stores its row from registers, whole 32-byte sectors.  Through shared memory by a bulk copy the row's
+          // tile was held for 2,000 cycles until the copy had read it.
+          if ((oi & 1) == mine) {
+            if (!mbar_wait_warp(&bars->o_full[oi % C::NR], (oi / C::NR) & 1)) {
+              go = false;
+              break;
+            }
+            tc_fence_after();
+            const int head = w.head * p.gx + (per_k ? 0 : h);
+            bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + head) * D;
+#pragma unroll 1
+            for (int g = 0; g < D / 32; ++g) {
+              uint32_t b[32], o[2][8];
+              tmem_ld_32x32b_x32(trow + C::TM_R + ru % C::NR * D + g * 32, b);
+              tmem_ld_wait();
+              reg_fence<32>(b);
+              if (g == D / 32 - 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->r_free[ru % C::NR]);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float x0, x1;
+                f2unpack(fmul2(f2pack(f_out, f_out), f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1]))), x0, x1);
+                o[i >> 3][i & 7] = pack_bf16(x0, x1);
+              }
+              if (r < rows) {
+                st_global_32(row + g * 32, o[0], p.wide);
+                st_global_32(row + g * 32 + 16, o[1], p.wide);
+              }
+            }
+          }
+          ++oi;
+          ++ru;
         }
+        if (n < w.c1 - w.c0 - 1) ++ru;   // K^T V takes one too
       }
     }
-    if (!go) set_abort(&bars->abort, p.c.status);
-  } else if (warp < 12) {
-    // ---------------------------------------------------------- O
-    // A thread stores its row from registers, whole 32-byte sectors.  Through the Q tile by a bulk copy the tile was
-    // held until the copy had read it, 2,000 cycles, and loads came late: 40/8/128, one long rollout, 1.41 ms.
-    setmaxnreg_dec<C::REG_OUT>();
-    const int quad = warp & 3, r = quad * 32 + lane;
-    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
-    bool go = true;
-    uint32_t oi = 0;
-    while (go && w.next())
-      for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-        const int c = BACK ? w.c1 - 1 - n : w.c0 + n;
-        const int rows = w.rows(c);
-        const float fa = p.scale * exp2f(w.l2 * (float)(BACK ? max(rows - r, 0) : r + 1));
-        const uint64_t fa2 = f2pack(fa, fa), fb2 = f2pack(p.scale, p.scale);
-        for (int h = 0; h < p.gx; ++h, ++oi) {
-          if (!mbar_wait_warp(&bars->o_full, oi & 1) || __any_sync(0xffffffffu, gave_up())) {
-            go = false;
-            break;
-          }
-          tc_fence_after();
-          bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + w.head * p.gx + h) * D;
-#pragma unroll 1
-          for (int g = 0; g < D / 32; ++g) {
-            uint32_t a[32], b[32], o[2][8];
-            tmem_ld_32x32b_x32(trow + C::TM_A + g * 32, a);
-            tmem_ld_32x32b_x32(trow + C::TM_B + g * 32, b);
-            tmem_ld_wait();
-            reg_fence<32>(a);
-            reg_fence<32>(b);
-            if (g == D / 32 - 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&bars->ab_free);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float x0, x1;
-              f2unpack(ffma2(fa2, f2pack(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1])),
-                             fmul2(fb2, f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1])))),
-                       x0, x1);
-              o[i >> 3][i & 7] = pack_bf16(x0, x1);
-            }
-            if (r < rows) {
-              st_global_32(row + g * 32, o[0], p.wide);
-              st_global_32(row + g * 32 + 16, o[1], p.wide);
-            }
-          }
-        }
-      }
     if (!go) set_abort(&bars->abort, p.c.status);
   } else {
     // ---------------------------------------------------------- state
@@ -934,7 +995,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     const bool mine = D == 128 || quad < 2;   // a row of the state
     bool go = true;
-    uint32_t ki = 0, ch = 0, weighed = 0;     // ki: the K tile of the next one to weight
+    uint32_t ki = 0, ch = 0, weighed = 0, ru = 0;   // ki: the K of the next one to weight;  ru: output buffers taken
     while (go && w.next()) {
       const int chunks = w.c1 - w.c0;
       float s[D];
@@ -953,7 +1014,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         // what other CTAs' pieces bring, the nearest first, until it has faded below fp32
         bool faded = false;
-        if (!BACK) {
+        if (!back) {
           for (int x = blockIdx.x - 1; w.c0 > 0 && x >= 0 && !faded; --x) {
             const int64_t e = (x + 1) * w.range - w.base;    // chunk behind that CTA's piece
             const float f = exp2f(w.l2 * (float)((w.c0 - e) * kChunk));
@@ -983,53 +1044,72 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (b >= w.nch) break;
             const float f = exp2f(w.l2 * (float)((b - w.c1) * kChunk));
             faded = f == 0.f;
-            if (!faded) add(p.slots + ((size_t)x * D + r) * D, f);
+            if (faded) break;
+            if (!p.transposed) {
+              add(p.slots + ((size_t)x * D + r) * D, f);
+            } else {
+#pragma unroll
+              for (int i = 0; i < D; ++i) s[i] = fmaf(f, p.slots[((size_t)x * D + i) * D + r], s[i]);
+            }
           }
         }
       }
       // Key tiles weighted before the state of chunk n + 1 is made: those of chunks up to n, and the first of chunk n + 1
       // where one product alone reads it as it was loaded, without waiting for that chunk's state.
-      const bool early = BACK || group == 1;
+      const bool early = per_k || group == 1;
       const int64_t keys = (int64_t)(chunks - 1) * p.gy;   // the last chunk's are not: no state comes behind it
       int64_t done = 0;
       for (int n = 0; go && n < chunks; ++n, ++ch) {
         const bool weigh = n < chunks - 1;
         // the copy that the chunk's queries read: the products with the one before are complete (u_full)
         if (mine) {
+          const int rows = w.rows(back ? w.c1 - 1 - n : w.c0 + n);
+          const float f = w.l2 < kSlow ? 1.f : exp2f(w.l2 * (float)(back ? rows - kMiddle : kMiddle));
+          const uint64_t f2 = f2pack(f, f);
           const uint32_t dst = sbase + C::OFF_S + r * 128;
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i)
-            st_shared_v4(dst + (i >> 3) * (D * 128) + (((i & 7) ^ (r & 7)) << 4), pack_bf16(s[8 * i], s[8 * i + 1]),
-                         pack_bf16(s[8 * i + 2], s[8 * i + 3]), pack_bf16(s[8 * i + 4], s[8 * i + 5]),
-                         pack_bf16(s[8 * i + 6], s[8 * i + 7]));
+          for (int i = 0; i < D / 8; ++i) {
+            uint32_t y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float a, b;
+              f2unpack(fmul2(f2, f2pack(s[8 * i + 2 * j], s[8 * i + 2 * j + 1])), a, b);
+              y[j] = pack_bf16(a, b);
+            }
+            st_shared_v4(dst + (i >> 3) * (D * 128) + (((i & 7) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+          }
         }
         fence_proxy_async_smem();
         mbar_arrive(&bars->s_ready);
         int64_t target = (int64_t)(n + 1) * p.gy + (early ? 1 : 0);
         if (target > keys) target = keys;
         for (; done < target; ++done, ++weighed, ++ki) {
-          const uint32_t slot = ki % C::NKV, tile = sbase + C::OFF_KV + slot * 2 * C::TILE + r * 128;
-          const int m = (int)(done / p.gy), rows = w.rows(BACK ? w.c1 - 1 - m : w.c0 + m);
-          const float wt = exp2f(w.l2 * (float)(BACK ? r : max(rows - 1 - r, 0)));
+          const uint32_t slot = 2 * ki % C::NT, tile = sbase + C::OFF_T + slot * C::TILE + r * 128;
+          const int m = (int)(done / p.gy), rows = w.rows(back ? w.c1 - 1 - m : w.c0 + m);
+          const float wt = exp2f(w.l2 * (float)(back ? r : max(rows - 1 - r, 0)));
           const uint64_t wt2 = f2pack(wt, wt);
           if (!mbar_wait_warp(&bars->k_done[weighed & 1], (weighed >> 1) & 1) ||
-              !mbar_wait_warp(&bars->kv_full[slot], (ki / C::NKV) & 1) || __any_sync(0xffffffffu, gave_up())) {
+              !mbar_wait_warp(&bars->t_full[slot], (2 * ki / C::NT) & 1) || __any_sync(0xffffffffu, gave_up())) {
             go = false;
             break;
           }
-#pragma unroll 4
-          for (int u = 0; u < D / 8; ++u) {
-            const uint32_t at = tile + (u >> 3) * 16384 + (((u + r) & 7) << 4);
-            const uint4 x = ld_shared_v4(at);
-            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-            uint32_t y[4];
+#pragma unroll 1
+          for (int kb = 0; kb < D / 64; ++kb) {   // eight loads under way
+            uint4 x[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float a, b;
-              f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
-              y[i] = r < rows ? pack_bf16(a, b) : 0u;   // rows of the next segment may hold anything
+            for (int u = 0; u < 8; ++u) x[u] = ld_shared_v4(tile + kb * 16384 + (((u + r) & 7) << 4));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+              uint32_t y[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float a, b;
+                f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
+                y[i] = r < rows ? pack_bf16(a, b) : 0u;   // rows of the next segment may hold anything
+              }
+              st_shared_v4(tile + kb * 16384 + (((u + r) & 7) << 4), y[0], y[1], y[2], y[3]);
             }
-            st_shared_v4(at, y[0], y[1], y[2], y[3]);
           }
           fence_proxy_async_smem();
           mbar_arrive(&bars->kt_full[weighed & 1]);
@@ -1040,13 +1120,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         tc_fence_after();
+        ru += p.gx;
         if (weigh && mine) {
-          const float f = exp2f(w.l2 * (float)w.rows(BACK ? w.c1 - 1 - n : w.c0 + n));
+          const float f = exp2f(w.l2 * (float)w.rows(back ? w.c1 - 1 - n : w.c0 + n));
           const uint64_t f2 = f2pack(f, f);
 #pragma unroll
           for (int g = 0; g < D / 32; ++g) {
             uint32_t u[32];
-            tmem_ld_32x32b_x32(trow + C::TM_U + g * 32, u);
+            tmem_ld_32x32b_x32(trow + C::TM_R + ru % C::NR * D + g * 32, u);
             tmem_ld_wait();
             reg_fence<32>(u);
 #pragma unroll
@@ -1056,7 +1137,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                        s[g * 32 + i], s[g * 32 + i + 1]);
           }
         }
-        tc_fence_before();
+        if (weigh) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->r_free[ru++ % C::NR]);
+        }
       }
     }
     if (!go) set_abort(&bars->abort, p.c.status);
@@ -1211,20 +1296,21 @@ cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, con
   return cudaGetLastError();
 }
 
-template <int D, bool BACK>
+template <int D, int KIND>
 cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int gx, int gy,
-                       const float* slots, const float* state_in, float* state_out, void* out, cudaStream_t st) {
-  using C = Lin<D>;
+                       const float* slots, bool transposed, const float* state_in, float* state_out, void* out,
+                       cudaStream_t st) {
+  using C = Lin<D, KIND>;
   alignas(64) CUtensorMap tq, tk, tv;
   const int64_t hx = (int64_t)a.hkv * gx, hy = (int64_t)a.hkv * gy;
   if (!encode(&tq, q, D, hx, a) || !encode(&tk, k, D, hy, a) || !encode(&tv, v, D, hy, a))
     return cudaErrorInvalidValue;
-  const void* fn = reinterpret_cast<const void*>(linear_out<D, BACK>);
+  const void* fn = reinterpret_cast<const void*>(linear_out<D, KIND>);
   static std::atomic<int> regs_cache{-1};
   bool regs_ok = false;
   if (cudaError_t e = launch_regs_match(fn, kRegLaunch, &regs_cache, &regs_ok); e != cudaSuccess) return e;
   if (!regs_ok) return cudaErrorInvalidConfiguration;
-  cudaError_t e = cudaFuncSetAttribute(linear_out<D, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  cudaError_t e = cudaFuncSetAttribute(linear_out<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   OutArgs p;
   p.c = w.c;
@@ -1234,10 +1320,18 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
   p.gx = gx;
   p.gy = gy;
   p.scale = a.scale;
+  p.transposed = transposed;
   p.out = static_cast<bf16*>(out);
   p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
-  linear_out<D, BACK><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, p);
+  linear_out<D, KIND><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, p);
   return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_back(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
+                        const float* slots, bool transposed, void* out, cudaStream_t st) {
+  return group == 1 ? launch_out<D, BACK1>(w, a, q, k, v, 1, 1, slots, transposed, nullptr, nullptr, out, st)
+                    : launch_out<D, BACK>(w, a, q, k, v, 1, group, slots, transposed, nullptr, nullptr, out, st);
 }
 
 template <int D>
@@ -1252,7 +1346,7 @@ cudaError_t launch_fwd(const LinearArgs& a, const float* state_in, float* state_
   else if (a.num_tokens > kWhole * kChunk)   // else no sequence is cut
     e = launch_states<D, 1>(w, a, a.k, a.v, 1, false, w.slots[0], nullptr, nullptr, st);
   if (e != cudaSuccess) return e;
-  return launch_out<D, false>(w, a, a.q, a.k, a.v, group, 1, w.slots[0], state_in, state_out, o, st);
+  return launch_out<D, FWD>(w, a, a.q, a.k, a.v, group, 1, w.slots[0], false, state_in, state_out, o, st);
 }
 
 template <int D>
@@ -1261,19 +1355,14 @@ cudaError_t launch_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk
   const Work w = make_work(a, ws);
   const int group = a.hq / a.hkv;
   cudaError_t e = launch_plan(w, st);
-  if (e == cudaSuccess && a.num_tokens > kWhole * kChunk) {
-    e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, w.slots[0], nullptr, nullptr, st);
-  }
+  const bool cut = a.num_tokens > kWhole * kChunk;   // else no sequence is
+  if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, w.slots[0], nullptr, nullptr, st);
   if (e == cudaSuccess)
-    e = launch_out<D, false>(w, a, dout, a.v, a.k, group, 1, w.slots[0], nullptr, nullptr, dq, st);
-  if (e == cudaSuccess && a.num_tokens > kWhole * kChunk) {
-    e = launch_states<D, 1>(w, a, dout, a.q, group, true, w.slots[0], nullptr, nullptr, st);
-    if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.q, dout, group, true, w.slots[1], nullptr, nullptr, st);
-  }
+    e = launch_out<D, FWD>(w, a, dout, a.v, a.k, group, 1, w.slots[0], false, nullptr, nullptr, dq, st);
+  if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.q, dout, group, true, w.slots[1], nullptr, nullptr, st);
   if (e == cudaSuccess)
-    e = launch_out<D, true>(w, a, a.v, dout, a.q, 1, group, w.slots[0], nullptr, nullptr, dk, st);
-  if (e == cudaSuccess)
-    e = launch_out<D, true>(w, a, a.k, a.q, dout, 1, group, w.slots[1], nullptr, nullptr, dv, st);
+    e = launch_back<D>(w, a, a.v, dout, a.q, group, w.slots[1], true, dk, st);
+  if (e == cudaSuccess) e = launch_back<D>(w, a, a.k, a.q, dout, group, w.slots[1], false, dv, st);
   return e;
 }
 
