@@ -186,6 +186,14 @@ struct Walk {
 };
 
 // ------------------------------------------------------------------ shared pieces
+__device__ __forceinline__ void tma_store_3d(const void* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+               "r"(src), "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
 __device__ __forceinline__ void set_abort(int32_t* abort, int32_t* status) {
   set_status(status, VCS_ERR_DEVICE_TIMEOUT);
   *reinterpret_cast<volatile int32_t*>(abort) = 1;
@@ -500,49 +508,58 @@ struct OutArgs {
   bf16* out;
 };
 
-// What a launch of linear_out works on: a group of query heads to a key head (FWD, also one), in order; or, from the last
-// token to the first, one key head (BACK1) or a group of them (BACK) to a query head.
-enum { FWD, BACK1, BACK };
+// What a launch of linear_out works on: one query head to a key head (FWD1) or a group of them (FWD), in order; or, from the
+// last token to the first, one key head (BACK1) or a group of them (BACK) to a query head.
+enum { FWD1, FWD, BACK1, BACK };
 
 template <int D, int KIND>
 struct Lin {
   static constexpr int TILE = kChunk * D * 2;
-  // Tiles of Q, and of K and V, which take turns.  A group of key heads has a K and a V to each item and keeps its Q.
-  static constexpr int NQ = D == 64 ? 4 : KIND == BACK ? 1 : 2;
-  static constexpr int NT = D == 64 ? 8 : KIND == BACK ? 5 : 4;
-  static constexpr int NP = 2;                           // buffers of Q K^T and P
-  static constexpr int NR = D == 64 ? 4 : 2;             // of outputs and K^T V, which take turns
+  // Tiles of Q, and of K and V, which take turns.  A load takes 2 to 4 thousand cycles under way and an item the memory 3 to
+  // 6, so that what streams has to have two to three tiles on its way: a group of query heads streams Q, a group of key
+  // heads K and V, one head of each both.
+  static constexpr int NQ = D == 64 ? 4 : KIND == FWD ? 2 : 1;
+  static constexpr int NT = D == 64 ? 8 : KIND == FWD ? 3 : KIND == BACK ? 5 : 4;
+  static constexpr bool STAGE = D == 64 || KIND != BACK; // outputs go through a tile of their own
+  // Buffers of Q K^T and P, and of outputs: two of the one or of the other at D = 128, whose K^T V takes the rest.
+  static constexpr int NP = D == 64 || KIND == BACK ? 2 : 1;
+  static constexpr int NB = D == 64 || KIND != BACK ? 2 : 1;
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_T = NQ * TILE;
-  static constexpr int OFF_S = OFF_T + NT * TILE;        // the state, D rows of k's dims, like a V tile
+  static constexpr int OFF_O = OFF_T + NT * TILE;
+  static constexpr int OFF_S = OFF_O + (STAGE ? TILE : 0);  // the state, D rows of k's dims, like a V tile
   static constexpr int OFF_TAB = OFF_S + D * D * 2;      // 32 powers of the decay for each warp that makes P
   static constexpr int OFF_BAR = OFF_TAB + 8 * 128;
   static constexpr int SMEM = OFF_BAR + 512;
-  static constexpr int TM_P = 0, TM_R = NP * 128;
+  static constexpr int TM_P = 0, TM_B = NP * 128, TM_U = TM_B + NB * D;
   static constexpr uint32_t IDESC_S = idesc_bf16(128, 128, 0, 0);  // Q (K-major) x K^T (K-major)
   static constexpr uint32_t IDESC_A = idesc_bf16(128, D, 0, 1);    // Q (K-major) x S (MN-major)
   static constexpr uint32_t IDESC_B = idesc_bf16(128, D, 0, 1);    // P (TMEM) x V (MN-major)
   // K^T (MN-major) x V (MN-major).  M = 128 at D = 64 too, whose lanes 64 .. 127 take the tile behind K's (or the
   // state) and are not read: an M of 64 lies in other lanes.
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
-  static constexpr int REG_CTRL = 96, REG_ROWS = 96, REG_STATE = 224;
+  static constexpr int REG_CTRL = 80, REG_ROWS = 104, REG_STATE = 224;
   static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
-  static_assert(SMEM <= 232448 && TM_R + NR * D <= 512, "shared memory and TMEM budgets");
+  static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
   static_assert(D == 128 || NT % 2 == 0, "behind a K tile lies another tile");
 };
 
 struct LinBars {
   uint64_t q_full[4], q_empty[4], t_full[8], t_empty[8];
-  uint64_t s_full[2];  // Q K^T of an item
+  // Of an item or an output of one warpgroup and of the other:
+  uint64_t s_full[2];  // Q K^T
   uint64_t p_full[2];  // its P is in TMEM
   uint64_t a_full[2];  // Q S, for the warpgroup that scales its rows
-  uint64_t o_full[4];  // of an output buffer: its products are complete
-  uint64_t r_free[4];  // and what it held, an output or K^T V, is in registers
-  // Two of each, as the issuer may be a K ahead of the warps that weight them and they of it.
+  uint64_t o_full[2];  // the products of an output are complete
+  uint64_t o_free[2];  // and in registers
+  uint64_t out_full;   // an output is in its tile, or its rows are written
+  uint64_t out_free;   // and on its way
   uint64_t k_done[2];  // a K that is to be weighted is no longer read as it was loaded
-  uint64_t kt_full[2]; // and weighted
-  uint64_t u_full;     // the chunk's K^T V, or, of a piece's last chunk, what reads the state
-  uint64_t s_ready;    // the state that the next chunk's queries read
+  uint64_t wt_full[4]; // a pair's V, or K, is weighted; four, as the warps that do it may be some pairs ahead of the issuer
+  uint64_t u_full;     // the chunk's K^T V
+  uint64_t u_free;     // and in registers
+  uint64_t s_ready;    // the state that the chunk's queries read is in shared memory
+  uint64_t s_read;     // and has been read
   uint32_t tmem_base;
   int32_t abort;
 };
@@ -564,26 +581,29 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8], bo
 }
 
 // O is one accumulator for both terms: Q S first, then P V on top.  With m = 64, the middle of a chunk,
-//   o_i = scale lam^(i+1-m) [ q_i (lam^m S) + sum_{j <= i} lam^(m-j-1) (q_i . k_j) v_j ]
-// so that P has a factor for each column alone and the row's comes last, as long as lam^-m stays small: 2^32 at most
-// (kSlow; the other way in time: rows lam^(m-i), columns lam^(j-m), the state lam^(n-m)).  For a head that forgets faster P has its
-// exact powers and the rows of Q S are scaled in TMEM.
+//   o_i = scale lam^(i+1-m) [ q_i (lam^m S) + sum_{j <= i} (q_i . k_j) w_j ],  w_j = lam^(m-1-j) v_j,
+//   S'  = lam^n S + lam^(n-m) sum_j k_j w_j^T
+// so that P = Q K^T below the diagonal has no factors at all, V is weighted once for both products, as soon as it is
+// loaded, and the row's factor comes last, as long as lam^-m stays in range: 2^64 at most (kSlow; the other way in time: rows
+// lam^(m-i), w_j = lam^(j-m) v_j, the state lam^(n-m), the sum lam^m).  For a head that forgets faster P has the exact powers, the
+// rows of Q S are scaled in TMEM, and K is weighted for the state when Q K^T has read it.
 constexpr int kMiddle = 64;
-constexpr float kSlow = -0.5f;   // log2 of the decay
+constexpr float kSlow = -1.0f;   // log2 of the decay
 
 // An item is a chunk with one query and one key head: of a group of query heads (gx) each item has an output and the
 // chunk one K and V, of a group of key heads (gy) each item has a K and V and the chunk one output.
 // Warp roles:
-//   warp 0       TMA producer;  warp 1  TMEM and every MMA
+//   warp 0       TMA producer;  warp 1  TMEM and every MMA;  warp 2  O out of shared memory
 //   warps 4-11   two warpgroups, for every other item: P below the diagonal, in bf16 for P V (a thread a query), then
 //                O out of TMEM, scaled
-//   warps 12-15  the weighted keys, and the state in registers (a thread a row), its bf16 copy in shared memory
+//   warps 12-15  the weighted tiles, and the state in registers (a thread a row), its bf16 copy in shared memory
 template <int D, int KIND>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_out(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ OutArgs p) {
+               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
+               const __grid_constant__ OutArgs p) {
   using C = Lin<D, KIND>;
-  constexpr bool back = KIND != FWD;
+  constexpr bool back = KIND == BACK1 || KIND == BACK;
   extern __shared__ __align__(1024) uint8_t smem[];
   LinBars* bars = reinterpret_cast<LinBars*>(smem + C::OFF_BAR);
   Walk w(p.c, blockIdx.x);
@@ -626,12 +646,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars->p_full[i], 128);
       mbar_init(&bars->a_full[i], 1);
       mbar_init(&bars->k_done[i], 1);
-      mbar_init(&bars->kt_full[i], 128);
-    }
-    for (int i = 0; i < C::NR; ++i) {
       mbar_init(&bars->o_full[i], 1);
-      mbar_init(&bars->r_free[i], 4);
+      mbar_init(&bars->o_free[i], 4);
     }
+    for (int i = 0; i < 4; ++i) mbar_init(&bars->wt_full[i], 128);
+    mbar_init(&bars->s_read, 1);
+    mbar_init(&bars->out_full, 128);
+    mbar_init(&bars->out_free, 1);
+    mbar_init(&bars->u_free, 4);
     mbar_init(&bars->u_full, 1);
     mbar_init(&bars->s_ready, 128);
     bars->abort = 0;
@@ -647,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
   const int group = KIND == FWD ? p.gx : KIND == BACK ? p.gy : 1;
-  constexpr bool per_k = KIND != FWD;   // an item has a K and V of its own; else an output of its own
+  constexpr bool per_k = KIND == BACK;   // items share a Q and an output; else a K and V, if there is more than one
   // Every role walks the same items and counts what it has passed.
 
   if (warp < 4) {
@@ -683,19 +705,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       // -------------------------------------------------------- MMA issuer
       // Every lane runs every step, no lane's answer to a wait decides where the warp goes, and the elected lane issues
       // as long as its own waits were met; a vote an item ends the walk.  The MMAs of one issuer execute in order, so
-      // Q K^T of an item may overwrite a P whose P V was issued before.
-      //   FWD:          Q K^T of the next item;  K^T V after the chunk's last Q K^T;  P V;  Q S of the next item
-      //   BACK1, BACK:  Q K^T of the next item;  P V;  K^T V;  Q S of the next item if it is a chunk's first
-      // so that two items' P are made at a time, K^T V, which the next chunk's state waits for, comes early (the way back it
-      // waits for P's warps, which clear the rows of V behind a segment's end), and a Q tile is given back soon.
+      // Q K^T of an item may overwrite a P whose P V was issued before.  For an item, in this order:
+      //   BACK   Q K^T of the next item;  K^T V;  of a chunk's second item (its first of one or two) Q S: the state has had an
+      //          item's time;  P V
+      //   else   of a chunk's first item K^T V, so that the next chunk's state is made while this one's queries are worked
+      //          on;  P V;  Q K^T and Q S of the next item, whose Q tile is then free
+      // (with two buffers of P Q K^T of the next item is first there too).  For a head that forgets fast K^T V waits for Q K^T, the
+      // chunk's last, and Q S comes first of an output's products.  A wait takes its thread 200 to 300 cycles while the
+      // pipe streams from shared memory: none twice.
       const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
       const uint64_t kd = smem_desc(sbase + C::OFF_T, 16, 1024), kt = smem_desc(sbase + C::OFF_T, 16384, 1024);
       const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
       bool ok = true;
-      // Of the next Q K^T: its Q tile and K (and V) pair, item, and the number of keys handed over for weighting.
-      uint32_t sq = 0xffffffffu, sk = 0xffffffffu, si = 0, handed = 0;
-      auto issue_s = [&](int h, bool weigh) {
-        const bool lastk = per_k || h == group - 1;
+      // What has been issued: Q tiles, pairs of K and V, items and handed-over keys of Q K^T; Q S and its chunks; K^T V.
+      uint32_t sq = 0xffffffffu, sk = 0xffffffffu, si = 0, handed = 0, aq = 0, ac = 0, us = 0;
+      auto issue_s = [&](int h, int n) {   // item h of the walk's chunk n
+        const bool fast = w.l2 < kSlow, lastk = per_k || h == group - 1, weigh = n < w.c1 - w.c0 - 1;
+        // keys that are weighted, or, the way back, whose rows behind the segment's end have to be cleared
+        const bool hand = weigh && lastk && (fast || (back && n == 0 && w.rows(w.c1 - 1) < kChunk));
+        const bool free_k = !per_k && lastk && (!weigh || (!fast && group > (C::NP == 1 ? 1 : 2)));
+        const bool free_q = KIND == BACK && h == group - 1 && h - 1 > (fast || group == 2 ? 0 : 1);
         if (!per_k || h == 0) {
           ++sq;
           ok = ok && mbar_wait(&bars->q_full[sq % C::NQ], (sq / C::NQ) & 1);
@@ -712,107 +741,138 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
             tc_mma_ss(tmem + C::TM_P + si % C::NP * 128, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
           }
-          tc_commit(&bars->s_full[si % C::NP]);
-          if (lastk && weigh) tc_commit(&bars->k_done[handed & 1]);
-          if (KIND == BACK && h == group - 1) tc_commit(&bars->q_empty[sq % C::NQ]);
+          tc_commit(&bars->s_full[si & 1]);
+          if (hand) tc_commit(&bars->k_done[handed & 1]);
+          if (free_k) tc_commit(&bars->t_empty[2 * sk % C::NT]);
+          if (free_q) tc_commit(&bars->q_empty[sq % C::NQ]);
         }
         __syncwarp();
         ++si;
-        if (lastk && weigh) ++handed;
+        if (hand) ++handed;
       };
-      uint32_t ru = 0, aq = 0, chunk = 0;   // output buffers taken, and of the next Q S its Q tile and chunk
-      // an output buffer, when what it held last has been read
-      auto take = [&] {
-        if (ru >= C::NR) ok = ok && mbar_wait(&bars->r_free[ru % C::NR], (ru / C::NR - 1) & 1);
-        return tmem + C::TM_R + ru++ % C::NR * D;
+      // an output's buffer, when the output that had it before is in registers
+      auto take = [&](uint32_t o) {
+        if (o >= C::NB) ok = ok && mbar_wait(&bars->o_free[(o - C::NB) & 1], ((o - C::NB) >> 1) & 1);
       };
-      auto issue_a = [&](bool new_chunk, bool fast, uint32_t item) {   // B = Q S of an item
-        if (new_chunk) ok = ok && mbar_wait(&bars->s_ready, chunk++ & 1);
-        const uint32_t dst = take(), q = aq++ % C::NQ;
+      // B = or += Q S of output o
+      auto issue_a = [&](uint32_t o, bool new_chunk, bool fresh, bool fast, bool last, bool free_q, uint32_t item) {
+        if (new_chunk) ok = ok && mbar_wait(&bars->s_ready, ac++ & 1);
+        if (fresh) take(o);
+        const uint32_t q = aq++ % C::NQ;
         tc_fence_after();
         if (elect_one() && ok) {
           const uint64_t a = desc_at(qd, q * C::TILE);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            tc_mma_ss(dst, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048), C::IDESC_A, kk > 0);
-          if (KIND != BACK) tc_commit(&bars->q_empty[q]);
+            tc_mma_ss(tmem + C::TM_B + o % C::NB * D, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32),
+                      desc_at(sd, kk * 2048), C::IDESC_A, kk > 0 || !fresh);
+          if (free_q) tc_commit(&bars->q_empty[q]);
           if (fast) tc_commit(&bars->a_full[item & 1]);
+          if (last) tc_commit(&bars->s_read);
         }
         __syncwarp();
-        return dst;
       };
-      uint32_t ki = 0, it = 0, weighed = 0, tm_u = 0;
+      // U (+)= K^T V of pair k
+      auto issue_u = [&](uint32_t k, bool first, bool last, bool free_k) {   // (V is there if it, or K, is weighted)
+        const uint32_t ks = 2 * k % C::NT, vs = (2 * k + 1) % C::NT;
+        if (first && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
+        ok = ok && mbar_wait(&bars->wt_full[k & 3], (k >> 2) & 1);
+        tc_fence_after();
+        if (elect_one() && ok) {
+          const uint64_t a = desc_at(kt, ks * C::TILE), b = desc_at(kt, vs * C::TILE);
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U, kk > 0 || !first);
+          if (free_k) tc_commit(&bars->t_empty[ks]);
+          if (last) tc_commit(&bars->u_full);
+        }
+        __syncwarp();
+      };
+      uint32_t ki = 0, it = 0, outs = 0;
       bool more = w.next(), go = true;
-      if (more) issue_s(0, w.c1 - w.c0 > 1);
-      uint32_t tm_b = 0, tm_next = more ? issue_a(true, w.l2 < kSlow, 0) : 0, outs = 0;
+      if (more) {
+        issue_s(0, 0);
+        if (!per_k) issue_a(0, true, true, w.l2 < kSlow, group == 1, true, 0);
+      }
       while (go && more) {
         const int chunks = w.c1 - w.c0;
-        bool fast = w.l2 < kSlow;
+        const bool fast = w.l2 < kSlow;
         for (int n = 0; go && n < chunks; ++n) {
           const bool weigh = n < chunks - 1;
           for (int h = 0; h < group; ++h, ++it) {
-            const bool out = !per_k || h == group - 1, lastk = per_k || h == group - 1, end = h == group - 1;
-            const uint32_t kslot = 2 * ki % C::NT, vslot = (2 * ki + 1) % C::NT;
-            if (!per_k || h == 0) tm_b = tm_next;
-            auto ahead = [&] {
-              if (!end) {
-                issue_s(h + 1, weigh);
-              } else if (weigh) {
-                issue_s(0, n + 1 < chunks - 1);
-              } else {
-                more = w.next();
-                fast = w.l2 < kSlow;
-                if (more) issue_s(0, w.c1 - w.c0 > 1);
-              }
+            const bool out = !per_k || h == group - 1, end = h == group - 1;
+            const uint32_t ks = 2 * ki % C::NT, vs = (2 * ki + 1) % C::NT;
+            auto ahead = [&] {   // Q K^T of the next item
+              if (!end) issue_s(h + 1, n);
+              else if (weigh) issue_s(0, n + 1);
+              else if ((more = w.next())) issue_s(0, 0);
             };
-            auto issue_u = [&] {   // U (+)= K^T V
-              if (!per_k || h == 0) tm_u = take();
-              ok = ok && mbar_wait(&bars->kt_full[weighed & 1], (weighed >> 1) & 1);
-              ok = ok && mbar_wait(&bars->t_full[vslot], ((2 * ki + 1) / C::NT) & 1);
-              tc_fence_after();
-              if (elect_one() && ok) {
-                const uint64_t a = desc_at(kt, kslot * C::TILE), b = desc_at(kt, vslot * C::TILE);
-#pragma unroll
-                for (int kk = 0; kk < 8; ++kk)
-                  tc_mma_ss(tm_u, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U,
-                            kk > 0 || (per_k && h > 0));
-                tc_commit(&bars->t_empty[kslot]);
-                if (per_k) tc_commit(&bars->t_empty[vslot]);
-                if (end) tc_commit(&bars->u_full);
-              }
-              __syncwarp();
-              ++weighed;
-            };
-            ahead();
-            if (!per_k && lastk && weigh) issue_u();
-            ok = ok && mbar_wait(&bars->p_full[it % C::NP], (it / C::NP) & 1);
-            ok = ok && mbar_wait(&bars->t_full[vslot], ((2 * ki + 1) / C::NT) & 1);
+            // (a group of key heads at D = 128 has one Q tile, whose next load a chunk's last item would wait for)
+            const bool late = C::NP == 1 || (C::NQ == 1 && end);
+            if (!late) ahead();
+            bool fresh = false;                    // P V is the first of its output's products
+            bool weighted = !per_k && h > 0;       // what P V waits for is known to be weighted
+            if (weigh && (per_k || (fast ? end : h == 0))) {
+              issue_u(ki, !per_k || h == 0, end || !per_k, per_k || fast || group <= (C::NP == 1 ? 1 : 2));
+              weighted = true;
+            }
+            if (per_k) {
+              const int hq = fast || group <= 2 ? 0 : 1;
+              if (h == hq) issue_a(outs, true, hq == 0, fast, true, group - 2 <= hq, it);
+              fresh = h < hq;
+              if (fresh) take(outs);
+            }
+            if (fast && (per_k || h == 0)) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
+            if (!fast && !weighted) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
+            ok = ok && mbar_wait(&bars->p_full[it & 1], (it >> 1) & 1);
             go = __all_sync(0xffffffffu, ok);
             if (!go) break;
             tc_fence_after();
-            if (elect_one()) {  // B += P V
-              const uint64_t b = desc_at(kt, vslot * C::TILE);
+            if (elect_one()) {  // B = or += P V
+              const uint64_t b = desc_at(kt, vs * C::TILE);
 #pragma unroll
               for (int kk = 0; kk < 8; ++kk)
-                tc_mma_ts(tm_b, tmem + C::TM_P + it % C::NP * 128 + kk * 8, desc_at(b, kk * 2048), C::IDESC_B, 1);
-              if (out) tc_commit(&bars->o_full[outs % C::NR]);
-              if (lastk && !weigh) {   // the piece's last state is not needed
-                tc_commit(&bars->t_empty[kslot]);
-                tc_commit(&bars->t_empty[vslot]);
-                if (end) tc_commit(&bars->u_full);
-              } else if (!per_k && lastk) {
-                tc_commit(&bars->t_empty[vslot]);
-              }
+                tc_mma_ts(tmem + C::TM_B + outs % C::NB * D, tmem + C::TM_P + it % C::NP * 128 + kk * 8,
+                          desc_at(b, kk * 2048), C::IDESC_B, kk > 0 || !fresh);
+              if (out) tc_commit(&bars->o_full[outs & 1]);
+              if (per_k || end) tc_commit(&bars->t_empty[vs]);
+              if (per_k && !weigh) tc_commit(&bars->t_empty[ks]);
             }
             __syncwarp();
+            if (late) ahead();
+            if (!per_k && (!end || more)) {        // Q S of the next item
+              const int h1 = end ? 0 : h + 1;
+              issue_a(outs + 1, end, true, w.l2 < kSlow, h1 == group - 1, true, it + 1);
+            }
             if (out) ++outs;
-            if (per_k && weigh) issue_u();
-            if (end ? more : !per_k) tm_next = issue_a(end, fast, it + 1);
-            if (lastk) ++ki;
+            if (per_k || end) ++ki;
           }
         }
       }
       go = __all_sync(0xffffffffu, ok);
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else if (C::STAGE && warp == 2 && lane == 0) {
+      // -------------------------------------------------------- O out of shared memory
+      bool go = true;
+      uint32_t oi = 0;
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+          const int c = back ? w.c1 - 1 - n : w.c0 + n;
+          for (int h = 0; h < p.gx; ++h, ++oi) {
+            if (!mbar_wait(&bars->out_full, oi & 1) || gave_up()) {
+              go = false;
+              break;
+            }
+            if (w.rows(c) == kChunk) {
+#pragma unroll
+              for (int kb = 0; kb < D / 64; ++kb)
+                tma_store_3d(&tm_o, sbase + C::OFF_O + kb * 16384, kb * 64, w.head * p.gx + h, w.start + c * kChunk);
+              bulk_commit();
+              bulk_wait_read();
+            }
+            mbar_arrive(&bars->out_free);
+          }
+        }
       if (!go) set_abort(&bars->abort, p.c.status);
     }
   } else if (warp < 12) {
@@ -824,11 +884,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     float* tab = reinterpret_cast<float*>(smem + C::OFF_TAB) + (warp - 4) * 32;
     const uint32_t tab_at = smem_u32(tab);
     bool go = true;
-    uint32_t it = 0, ki = 0, ru = 0, oi = 0, fasts = 0;   // ru: output buffers taken;  oi: outputs
+    uint32_t it = 0, ki = 0, oi = 0, fasts = 0;   // oi: outputs
     while (go && w.next()) {
-      // A column's factor is one of 32 powers, by its place in a group of 32, times one for the group; for a head that
-      // forgets fast the latter goes from the group's near end to the row, so that both are at most 1, and the group that
-      // the diagonal crosses takes powers of the exact distances: a token sees itself with weight 1.
       const bool fast = w.l2 < kSlow;
       __syncwarp();
       tab[lane] = exp2f(w.l2 * (float)(back ? lane : 31 - lane));
@@ -842,70 +899,91 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; h < group; ++h, ++it) {
           if ((it & 1) == mine) {
             const uint32_t tp = trow + C::TM_P + it % C::NP * 128;
-            if (!mbar_wait_warp(&bars->s_full[it % C::NP], (it / C::NP) & 1) || __any_sync(0xffffffffu, gave_up())) {
+            if (!mbar_wait_warp(&bars->s_full[mine], (it >> 1) & 1) || __any_sync(0xffffffffu, gave_up())) {
               go = false;
               break;
             }
             tc_fence_after();
-            // Group by group of 32 columns in a loop that is not unrolled: the roles' code together outgrows the
-            // instruction cache.  P of a group goes over columns of Q K^T that have been read.
+            // Loops over columns are not unrolled: the roles' code together outgrows the instruction cache.  P goes over
+            // columns of Q K^T that have been read.
+            if (!fast) {
 #pragma unroll 1
-            for (int g = 0; g < 4; ++g) {
-              uint32_t pk[16];
-              if (back ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
-#pragma unroll
-                for (int i = 0; i < 16; ++i) pk[i] = 0u;
-              } else {
+              for (int g = 0; g < 4; ++g) {
+                const int c0 = g * 32;
                 uint32_t s[32];
-                tmem_ld_32x32b_x32(tp + g * 32, s);
-                uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
-                if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-                if (back && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
-                const bool masked = g == quad || (back && rows - g * 32 < 32);
-                if (fast && masked) {
-                  const float gap = (float)(r - g * 32);
-                  const uint64_t at = f2pack(gap, gap);
-                  tmem_ld_wait();
-                  reg_fence<32>(s);
+                if (back ? g < quad || c0 >= rows : g > quad) {   // nothing seen
 #pragma unroll
-                  for (int i = 0; i < 16; ++i) {
-                    float e0, e1, x0, x1;
-                    f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
-                    f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
-                                   f2pack(ex2(e0), ex2(e1))),
-                             x0, x1);
-                    s[2 * i] = __float_as_uint(x0);
-                    s[2 * i + 1] = __float_as_uint(x1);
-                  }
+                  for (int i = 0; i < 16; ++i) s[i] = 0u;
                 } else {
-                  const float rf = exp2f(w.l2 * (float)(fast ? (back ? g * 32 - r : r - g * 32 - 31)
-                                                             : (back ? g * 32 - kMiddle : kMiddle - 32 - g * 32)));
-                  const uint64_t rf2 = f2pack(rf, rf);
+                  tmem_ld_32x32b_x32(tp + c0, s);
                   tmem_ld_wait();
                   reg_fence<32>(s);
+                  if (g == quad || (back && rows - c0 < 32)) {
+                    uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
+                    if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                    if (back && rows - c0 < 32) seen &= (1u << (rows - c0)) - 1u;
 #pragma unroll
-                  for (int i = 0; i < 32; i += 4) {
-                    const uint4 f = ld_shared_v4(tab_at + i * 4);
-                    const uint64_t f0 = fmul2(f2pack(__uint_as_float(f.x), __uint_as_float(f.y)), rf2);
-                    const uint64_t f1 = fmul2(f2pack(__uint_as_float(f.z), __uint_as_float(f.w)), rf2);
-                    float x0, x1, x2, x3;
-                    f2unpack(fmul2(f2pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), f0), x0, x1);
-                    f2unpack(fmul2(f2pack(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), f1), x2, x3);
-                    s[i] = __float_as_uint(x0);
-                    s[i + 1] = __float_as_uint(x1);
-                    s[i + 2] = __float_as_uint(x2);
-                    s[i + 3] = __float_as_uint(x3);
+                    for (int i = 0; i < 32; ++i)
+                      if (!(seen >> i & 1)) s[i] = 0u;
+                  }
+#pragma unroll
+                  for (int i = 0; i < 16; ++i)
+                    s[i] = pack_bf16(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                }
+                tmem_st_32x32b_x16(tp + g * 16, *reinterpret_cast<uint32_t(*)[16]>(&s[0]));
+              }
+            } else {
+              // lam^|r - c|: in a group of 32 columns that the diagonal does not cross a power for the row, from the group's
+              // near end, times one of 32 for the column, at most 1 both; in the diagonal's, powers of the exact distances,
+              // so that a token sees itself with weight 1.
+#pragma unroll 1
+              for (int g = 0; g < 4; ++g) {
+                uint32_t pk[16];
+                if (back ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) pk[i] = 0u;
+                } else {
+                  uint32_t s[32];
+                  tmem_ld_32x32b_x32(tp + g * 32, s);
+                  uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
+                  if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
+                  if (back && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
+                  if (g == quad || (back && rows - g * 32 < 32)) {
+                    const float gap = (float)(r - g * 32);
+                    const uint64_t at = f2pack(gap, gap);
+                    tmem_ld_wait();
+                    reg_fence<32>(s);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                      float e0, e1, x0, x1;
+                      f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
+                      f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                     f2pack(ex2(e0), ex2(e1))),
+                               x0, x1);
+                      pk[i] = pack_bf16(seen >> (2 * i) & 1 ? x0 : 0.f, seen >> (2 * i + 1) & 1 ? x1 : 0.f);
+                    }
+                  } else {
+                    const float rf = ex2(w.l2 * (float)(back ? g * 32 - r : r - g * 32 - 31));
+                    const uint64_t rf2 = f2pack(rf, rf);
+                    tmem_ld_wait();
+                    reg_fence<32>(s);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                      const uint4 f = ld_shared_v4(tab_at + i * 8);
+                      float x0, x1;
+                      f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                     fmul2(rf2, f2pack(__uint_as_float(f.x), __uint_as_float(f.y)))),
+                               x0, x1);
+                      pk[i] = pack_bf16(x0, x1);
+                      f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i + 2]), __uint_as_float(s[2 * i + 3])),
+                                     fmul2(rf2, f2pack(__uint_as_float(f.z), __uint_as_float(f.w)))),
+                               x0, x1);
+                      pk[i + 1] = pack_bf16(x0, x1);
+                    }
                   }
                 }
-                if (masked) {
-#pragma unroll
-                  for (int i = 0; i < 32; ++i)
-                    if (!(seen >> i & 1)) s[i] = 0u;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) pk[i] = pack_bf16(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                tmem_st_32x32b_x16(tp + g * 16, pk);
               }
-              tmem_st_32x32b_x16(tp + g * 16, pk);
             }
             if (fast && (!per_k || h == 0)) {   // the rows of Q S
               if (!mbar_wait_warp(&bars->a_full[mine], fasts & 1)) {
@@ -915,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               tc_fence_after();
               const float f = exp2f(w.l2 * (float)(back ? max(rows - r, 0) : r + 1));
               const uint64_t f2 = f2pack(f, f);
-              const uint32_t tb = trow + C::TM_R + ru % C::NR * D;
+              const uint32_t tb = trow + C::TM_B + oi % C::NB * D;
 #pragma unroll 1
               for (int g = 0; g < D / 32; ++g) {
                 uint32_t s[32];
@@ -933,7 +1011,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               ++fasts;
             }
-            if ((per_k || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
+            if (fast && (per_k || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
               const uint32_t v = 2 * ki + 1;
               if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
                 go = false;
@@ -944,47 +1022,64 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(&bars->p_full[it % C::NP]);
+            mbar_arrive(&bars->p_full[mine]);
           }
           if (per_k || h == group - 1) ++ki;
           if (per_k && h < group - 1) continue;
-          // A thread stores its row from registers, whole 32-byte sectors.  Through shared memory by a bulk copy the row's
-          // tile was held for 2,000 cycles until the copy had read it.
+          // Through a tile and a bulk copy: rows stored from registers, a line to a lane, kept the load/store unit so busy that
+          // every wait of the other warps took a thousand cycles (40/8/128, one long rollout: 1,260 us).  They are where a
+          // chunk ends inside the tile, and the way back at D = 128, an output to a group's items, where there is no room.
           if ((oi & 1) == mine) {
-            if (!mbar_wait_warp(&bars->o_full[oi % C::NR], (oi / C::NR) & 1)) {
+            if (!mbar_wait_warp(&bars->o_full[mine], (oi >> 1) & 1)) {
               go = false;
               break;
             }
             tc_fence_after();
             const int head = w.head * p.gx + (per_k ? 0 : h);
             bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + head) * D;
+            const uint64_t f2 = f2pack(f_out, f_out);
+            const uint32_t tb = trow + C::TM_B + oi % C::NB * D;
+            const bool staged = C::STAGE && rows == kChunk;
+            const uint32_t tile = sbase + C::OFF_O + r * 128;
+            // the output before has left the tile (and this one's place in the order of out_full)
+            if (C::STAGE && oi > 0 && !mbar_wait_warp(&bars->out_free, (oi - 1) & 1)) {
+              go = false;
+              break;
+            }
 #pragma unroll 1
             for (int g = 0; g < D / 32; ++g) {
-              uint32_t b[32], o[2][8];
-              tmem_ld_32x32b_x32(trow + C::TM_R + ru % C::NR * D + g * 32, b);
+              uint32_t b[32];
+              tmem_ld_32x32b_x32(tb + g * 32, b);
               tmem_ld_wait();
               reg_fence<32>(b);
               if (g == D / 32 - 1) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars->r_free[ru % C::NR]);
+                if (lane == 0) mbar_arrive(&bars->o_free[mine]);
               }
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
                 float x0, x1;
-                f2unpack(fmul2(f2pack(f_out, f_out), f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1]))), x0, x1);
-                o[i >> 3][i & 7] = pack_bf16(x0, x1);
+                f2unpack(fmul2(f2, f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1]))), x0, x1);
+                b[i] = pack_bf16(x0, x1);
               }
-              if (r < rows) {
-                st_global_32(row + g * 32, o[0], p.wide);
-                st_global_32(row + g * 32 + 16, o[1], p.wide);
+              if (staged) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  st_shared_v4(tile + (g >> 1) * 16384 + ((((g & 1) * 4 + u) ^ (r & 7)) << 4), b[4 * u], b[4 * u + 1],
+                               b[4 * u + 2], b[4 * u + 3]);
+              } else if (r < rows) {
+                st_global_32(row + g * 32, *reinterpret_cast<const uint32_t(*)[8]>(&b[0]), p.wide);
+                st_global_32(row + g * 32 + 16, *reinterpret_cast<const uint32_t(*)[8]>(&b[8]), p.wide);
               }
+            }
+            if (C::STAGE) {
+              fence_proxy_async_smem();
+              mbar_arrive(&bars->out_full);
             }
           }
           ++oi;
-          ++ru;
         }
-        if (n < w.c1 - w.c0 - 1) ++ru;   // K^T V takes one too
       }
     }
     if (!go) set_abort(&bars->abort, p.c.status);
@@ -995,7 +1090,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     const bool mine = D == 128 || quad < 2;   // a row of the state
     bool go = true;
-    uint32_t ki = 0, ch = 0, weighed = 0, ru = 0;   // ki: the K of the next one to weight;  ru: output buffers taken
+    uint32_t ki = 0, ch = 0, handed = 0, sums = 0;   // ki: the next pair to weight;  sums: K^T V read
     while (go && w.next()) {
       const int chunks = w.c1 - w.c0;
       float s[D];
@@ -1010,6 +1105,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             s[i + 1] = fmaf(f, x.y, s[i + 1]);
             s[i + 2] = fmaf(f, x.z, s[i + 2]);
             s[i + 3] = fmaf(f, x.w, s[i + 3]);
+            if (i % 32 == 28) asm volatile("" ::: "memory");   // not all loads ahead: the registers are the state's
           }
         };
         // what other CTAs' pieces bring, the nearest first, until it has faded below fp32
@@ -1036,6 +1132,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               x.z = fmaf(f, s[i + 2], x.z);
               x.w = fmaf(f, s[i + 3], x.w);
               *reinterpret_cast<float4*>(dst + i) = x;
+              if (i % 32 == 28) asm volatile("" ::: "memory");
             }
           }
         } else {
@@ -1049,22 +1146,29 @@ __global__ void __launch_bounds__(kThreads, 1)
               add(p.slots + ((size_t)x * D + r) * D, f);
             } else {
 #pragma unroll
-              for (int i = 0; i < D; ++i) s[i] = fmaf(f, p.slots[((size_t)x * D + i) * D + r], s[i]);
+              for (int i = 0; i < D; ++i) {
+                s[i] = fmaf(f, p.slots[((size_t)x * D + i) * D + r], s[i]);
+                if (i % 32 == 31) asm volatile("" ::: "memory");
+              }
             }
           }
         }
       }
-      // Key tiles weighted before the state of chunk n + 1 is made: those of chunks up to n, and the first of chunk n + 1
-      // where one product alone reads it as it was loaded, without waiting for that chunk's state.
-      const bool early = per_k || group == 1;
-      const int64_t keys = (int64_t)(chunks - 1) * p.gy;   // the last chunk's are not: no state comes behind it
+      // Pairs weighted before the state of chunk n + 1 is made: those of chunks up to n and, in a group of key heads, whose
+      // next chunk's first is wanted before that chunk's state, that one.
+      const bool fast = w.l2 < kSlow, early = !fast && KIND == BACK;
+      const int64_t pairs = (int64_t)chunks * p.gy;
       int64_t done = 0;
       for (int n = 0; go && n < chunks; ++n, ++ch) {
         const bool weigh = n < chunks - 1;
-        // the copy that the chunk's queries read: the products with the one before are complete (u_full)
+        // the copy that the chunk's queries read, when the one before has been read
+        if (ch > 0 && !mbar_wait_warp(&bars->s_read, (ch - 1) & 1)) {
+          go = false;
+          break;
+        }
         if (mine) {
           const int rows = w.rows(back ? w.c1 - 1 - n : w.c0 + n);
-          const float f = w.l2 < kSlow ? 1.f : exp2f(w.l2 * (float)(back ? rows - kMiddle : kMiddle));
+          const float f = fast ? 1.f : exp2f(w.l2 * (float)(back ? rows - kMiddle : kMiddle));
           const uint64_t f2 = f2pack(f, f);
           const uint32_t dst = sbase + C::OFF_S + r * 128;
 #pragma unroll
@@ -1082,24 +1186,49 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_proxy_async_smem();
         mbar_arrive(&bars->s_ready);
         int64_t target = (int64_t)(n + 1) * p.gy + (early ? 1 : 0);
-        if (target > keys) target = keys;
-        for (; done < target; ++done, ++weighed, ++ki) {
-          const uint32_t slot = 2 * ki % C::NT, tile = sbase + C::OFF_T + slot * C::TILE + r * 128;
+        if (target > pairs) target = pairs;
+        for (; done < target; ++done, ++ki) {
           const int m = (int)(done / p.gy), rows = w.rows(back ? w.c1 - 1 - m : w.c0 + m);
-          const float wt = exp2f(w.l2 * (float)(back ? r : max(rows - 1 - r, 0)));
+          if (fast && m == chunks - 1) {   // no state comes behind the last chunk; in turn with its V all the same
+            const uint32_t v = 2 * ki + 1;
+            if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
+              go = false;
+              break;
+            }
+            mbar_arrive(&bars->wt_full[ki & 3]);
+            continue;
+          }
+          const uint32_t at = 2 * ki + (fast ? 0 : 1), tile = sbase + C::OFF_T + at % C::NT * C::TILE + r * 128;
+          const float wt = exp2f(w.l2 * (float)(fast ? (back ? r : max(rows - 1 - r, 0))
+                                                     : (back ? r - kMiddle : kMiddle - 1 - r)));
           const uint64_t wt2 = f2pack(wt, wt);
-          if (!mbar_wait_warp(&bars->k_done[weighed & 1], (weighed >> 1) & 1) ||
-              !mbar_wait_warp(&bars->t_full[slot], (2 * ki / C::NT) & 1) || __any_sync(0xffffffffu, gave_up())) {
+          const uint32_t k_at = 2 * ki, k_tile = sbase + C::OFF_T + k_at % C::NT * C::TILE;
+          const bool hand = fast || (back && m < chunks - 1 && rows < kChunk);
+          if ((hand && (!mbar_wait_warp(&bars->k_done[handed & 1], (handed >> 1) & 1) ||
+                        !mbar_wait_warp(&bars->t_full[k_at % C::NT], (k_at / C::NT) & 1))) ||
+              !mbar_wait_warp(&bars->t_full[at % C::NT], (at / C::NT) & 1) || __any_sync(0xffffffffu, gave_up())) {
             go = false;
             break;
           }
+          if (hand) ++handed;
+          if (hand && !fast && r >= rows) zero_row<D>(k_tile, r);
+          if (fast && rows < kChunk) {   // K^T V comes before P V, whose warps clear them for a piece's last chunk
+            const uint32_t v = 2 * ki + 1;
+            if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
+              go = false;
+              break;
+            }
+            if (r >= rows) zero_row<D>(sbase + C::OFF_T + v % C::NT * C::TILE, r);
+          }
 #pragma unroll 1
-          for (int kb = 0; kb < D / 64; ++kb) {   // eight loads under way
-            uint4 x[8];
+          for (int kb = 0; kb < D / 32; ++kb) {   // four loads under way
+            uint4 x[4];
+            const uint32_t row = tile + (kb >> 1) * 16384;
+            const int u0 = (kb & 1) * 4 + r;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = ld_shared_v4(tile + kb * 16384 + (((u + r) & 7) << 4));
+            for (int u = 0; u < 4; ++u) x[u] = ld_shared_v4(row + (((u0 + u) & 7) << 4));
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 4; ++u) {
               const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
               uint32_t y[4];
 #pragma unroll
@@ -1108,40 +1237,39 @@ __global__ void __launch_bounds__(kThreads, 1)
                 f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
                 y[i] = r < rows ? pack_bf16(a, b) : 0u;   // rows of the next segment may hold anything
               }
-              st_shared_v4(tile + kb * 16384 + (((u + r) & 7) << 4), y[0], y[1], y[2], y[3]);
+              st_shared_v4(row + (((u0 + u) & 7) << 4), y[0], y[1], y[2], y[3]);
             }
           }
           fence_proxy_async_smem();
-          mbar_arrive(&bars->kt_full[weighed & 1]);
+          mbar_arrive(&bars->wt_full[ki & 3]);
         }
-        if (!weigh) ki += p.gy;
-        if (!go || !mbar_wait_warp(&bars->u_full, ch & 1)) {
+        if (!go || !weigh) continue;
+        if (!mbar_wait_warp(&bars->u_full, sums++ & 1)) {
           go = false;
           break;
         }
         tc_fence_after();
-        ru += p.gx;
-        if (weigh && mine) {
-          const float f = exp2f(w.l2 * (float)w.rows(back ? w.c1 - 1 - n : w.c0 + n));
-          const uint64_t f2 = f2pack(f, f);
+        if (mine) {
+          const int rows = w.rows(back ? w.c1 - 1 - n : w.c0 + n);
+          const float f = exp2f(w.l2 * (float)rows);
+          const float fu = fast ? 1.f : exp2f(w.l2 * (float)(back ? kMiddle : rows - kMiddle));
+          const uint64_t f2 = f2pack(f, f), fu2 = f2pack(fu, fu);
 #pragma unroll
-          for (int g = 0; g < D / 32; ++g) {
-            uint32_t u[32];
-            tmem_ld_32x32b_x32(trow + C::TM_R + ru % C::NR * D + g * 32, u);
+          for (int g = 0; g < D / 16; ++g) {
+            uint32_t u[16];
+            tmem_ld_32x32b_x16(trow + C::TM_U + g * 16, u);
             tmem_ld_wait();
-            reg_fence<32>(u);
+            reg_fence<16>(u);
 #pragma unroll
-            for (int i = 0; i < 32; i += 2)
-              f2unpack(ffma2(f2, f2pack(s[g * 32 + i], s[g * 32 + i + 1]),
-                             f2pack(__uint_as_float(u[i]), __uint_as_float(u[i + 1]))),
-                       s[g * 32 + i], s[g * 32 + i + 1]);
+            for (int i = 0; i < 16; i += 2)
+              f2unpack(ffma2(f2, f2pack(s[g * 16 + i], s[g * 16 + i + 1]),
+                             fmul2(fu2, f2pack(__uint_as_float(u[i]), __uint_as_float(u[i + 1])))),
+                       s[g * 16 + i], s[g * 16 + i + 1]);
           }
         }
-        if (weigh) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars->r_free[ru++ % C::NR]);
-        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->u_free);
       }
     }
     if (!go) set_abort(&bars->abort, p.c.status);
@@ -1301,9 +1429,9 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
                        const float* slots, bool transposed, const float* state_in, float* state_out, void* out,
                        cudaStream_t st) {
   using C = Lin<D, KIND>;
-  alignas(64) CUtensorMap tq, tk, tv;
+  alignas(64) CUtensorMap tq, tk, tv, to;
   const int64_t hx = (int64_t)a.hkv * gx, hy = (int64_t)a.hkv * gy;
-  if (!encode(&tq, q, D, hx, a) || !encode(&tk, k, D, hy, a) || !encode(&tv, v, D, hy, a))
+  if (!encode(&tq, q, D, hx, a) || !encode(&tk, k, D, hy, a) || !encode(&tv, v, D, hy, a) || !encode(&to, out, D, hx, a))
     return cudaErrorInvalidValue;
   const void* fn = reinterpret_cast<const void*>(linear_out<D, KIND>);
   static std::atomic<int> regs_cache{-1};
@@ -1323,8 +1451,15 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
   p.transposed = transposed;
   p.out = static_cast<bf16*>(out);
   p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
-  linear_out<D, KIND><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, p);
+  linear_out<D, KIND><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, to, p);
   return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_forth(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
+                         const float* slots, const float* state_in, float* state_out, void* out, cudaStream_t st) {
+  return group == 1 ? launch_out<D, FWD1>(w, a, q, k, v, 1, 1, slots, false, state_in, state_out, out, st)
+                    : launch_out<D, FWD>(w, a, q, k, v, group, 1, slots, false, state_in, state_out, out, st);
 }
 
 template <int D>
@@ -1346,7 +1481,7 @@ cudaError_t launch_fwd(const LinearArgs& a, const float* state_in, float* state_
   else if (a.num_tokens > kWhole * kChunk)   // else no sequence is cut
     e = launch_states<D, 1>(w, a, a.k, a.v, 1, false, w.slots[0], nullptr, nullptr, st);
   if (e != cudaSuccess) return e;
-  return launch_out<D, FWD>(w, a, a.q, a.k, a.v, group, 1, w.slots[0], false, state_in, state_out, o, st);
+  return launch_forth<D>(w, a, a.q, a.k, a.v, group, w.slots[0], state_in, state_out, o, st);
 }
 
 template <int D>
@@ -1358,7 +1493,7 @@ cudaError_t launch_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk
   const bool cut = a.num_tokens > kWhole * kChunk;   // else no sequence is
   if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, w.slots[0], nullptr, nullptr, st);
   if (e == cudaSuccess)
-    e = launch_out<D, FWD>(w, a, dout, a.v, a.k, group, 1, w.slots[0], false, nullptr, nullptr, dq, st);
+    e = launch_forth<D>(w, a, dout, a.v, a.k, group, w.slots[0], nullptr, nullptr, dq, st);
   if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.q, dout, group, true, w.slots[1], nullptr, nullptr, st);
   if (e == cudaSuccess)
     e = launch_back<D>(w, a, a.v, dout, a.q, group, w.slots[1], true, dk, st);

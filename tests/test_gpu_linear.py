@@ -176,12 +176,14 @@ def test_rows_of_no_segment_stay():
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_segments_do_not_meet(d):
+@pytest.mark.parametrize("decay", [(-0.3, 0.0), (-4.0, -1.2)])
+@pytest.mark.parametrize("hq", [2, 4, 6])
+def test_segments_do_not_meet(d, decay, hq):
     # NaN and infinities in one segment are not seen by its neighbours, whose last tiles reach into it
     vcs = _vcs()
     lens = [100, 3, 150, 1, 70]
-    q, k, v, do = draw(6, lens, 4, 2, d)
-    cu, g = cu_from_lengths(lens), decays(-0.3, 0.0)
+    q, k, v, do = draw(6, lens, hq, 2, d)
+    cu, g = cu_from_lengths(lens), decays(*decay)
     cud = torch.from_numpy(cu).cuda()
     want = [*vcs.linear_attn_fwd(q, k, v, g, cud, with_state=True), *vcs.linear_attn_bwd(q, k, v, do, g, cud)]
     for bad, s in ((float("nan"), 1), (float("inf"), 3), (3e38, 1), (float("nan"), 2)):
