@@ -4,7 +4,11 @@ Bounds.  ln sum exp is off by at most 2^-17: the exponentials by 2^-21 of themse
 size (whose terms e^-x x stay below 0.4), the fp32 sum by 2^-24 an addition in chains of a few hundred.  A list's log
 p_j and z_j / T are off by 2^-22 of their size.  So
   kl       2^-17 + 2^-21 max (|t_j| + |z_j|) / T
-  dlogits  |w| / T 2^-16 (q + p) + half a step of its type of itself
+  dlogits  |w| / T ((2^-16 + 2^-22 x) q + (2^-16 + 2^-22 88) p) + half a step of its type of itself
+where x = (max z - z) / T is the exponential's argument: the difference, its factor and their product are rounded once
+each (2^-24) and T itself to fp32 (2^-25 of what the oracle is given), 3.5 2^-24 x < 2^-22 x in all, which is no small
+part of 2^-16 where q is; p's arguments likewise, below 88 where p is not flushed.  An exponential below 2^-126 is
+flushed to 0, which |w| / T multiplies, and so is a gradient.
   loss     sum |w| (error of kl) + 2^-24 of itself
 """
 import math
@@ -39,9 +43,9 @@ def draw(seed, rows, vocab, top, dtype=torch.float32, lists=None, pad=0, twice=F
 def check(z, ids, t, w, rows=None, temp=1.0, **kw):
     vcs = _vcs()
     n, vocab = z.shape
-    z0, zn = z.clone(), z.double().cpu().numpy()
+    zn = z.double().cpu().numpy()
+    only = vcs.distill_topk(z, ids, t, w, rows, temp, with_grad=False)
     loss, kl, g = vcs.distill_topk(z, ids, t, w, rows, temp, **kw)
-    only = vcs.distill_topk(z0, ids, t, w, rows, temp, with_grad=False)
     assert only[2] is None and torch.equal(only[0], loss) and torch.equal(only[1], kl)
     assert loss.dtype == kl.dtype == torch.float32 and g.dtype == z.dtype and g.shape == z.shape
     idn, tn, wn = ids.cpu().numpy(), t.double().cpu().numpy(), w.double().cpu().numpy()
@@ -59,7 +63,9 @@ def check(z, ids, t, w, rows=None, temp=1.0, **kw):
     lz = zn / temp - (zn / temp).max(1, keepdims=True)
     q = np.exp(lz) / np.exp(lz).sum(1, keepdims=True) * live[:, None]
     p = np.abs(q - np.divide(gw, (wn / temp)[:, None], out=np.zeros_like(gw), where=live[:, None]))
-    bound = c * 2.0 ** -16 * (q + p) + HALF[z.dtype] * np.abs(gw) + 2.0 ** -126   # below it fp32 flushes
+    far = np.minimum(-lz, 1e3)
+    bound = c * ((2.0 ** -16 + 2.0 ** -22 * far) * q + (2.0 ** -16 + 2.0 ** -22 * 88) * p) \
+        + HALF[z.dtype] * np.abs(gw) + 2.0 ** -126 * (1 + c)
     dg = np.abs(g.double().cpu().numpy() - gw)
     assert (dg <= bound).all(), (dg.max(), np.unravel_index((dg - bound).argmax(), dg.shape))
 
