@@ -46,7 +46,7 @@ def check(z, ids, t, w, rows=None, temp=1.0, **kw):
     zn = z.double().cpu().numpy()
     only = vcs.distill_topk(z, ids, t, w, rows, temp, with_grad=False)
     loss, kl, g = vcs.distill_topk(z, ids, t, w, rows, temp, **kw)
-    assert only[2] is None and torch.equal(only[0], loss) and torch.equal(only[1], kl)
+    assert only[2] is None
     assert loss.dtype == kl.dtype == torch.float32 and g.dtype == z.dtype and g.shape == z.shape
     idn, tn, wn = ids.cpu().numpy(), t.double().cpu().numpy(), w.double().cpu().numpy()
     rn = None if rows is None else rows.cpu().numpy()
@@ -55,9 +55,10 @@ def check(z, ids, t, w, rows=None, temp=1.0, **kw):
     here = (idn[at] >= 0) & np.isfinite(tn[at])
     size = np.where(here, np.abs(np.where(here, tn[at], 0)) + np.abs(np.take_along_axis(zn, np.maximum(idn[at], 0), 1)), 0)
     ek = 2.0 ** -17 + 2.0 ** -21 * size.max(1, initial=0) / temp
-    dk = np.abs(kl.double().cpu().numpy() - kw_)
-    assert (dk <= ek + 2.0 ** -24 * np.abs(kw_)).all(), (dk.max(), ek.max())
-    assert abs(float(loss) - lw) <= (np.abs(wn) * ek).sum() + 2.0 ** -24 * abs(lw)
+    for ls, x in ((loss, kl), only[:2]):   # with the gradient, and without, where the sums may be in another order
+        dk = np.abs(x.double().cpu().numpy() - kw_)
+        assert (dk <= ek + 2.0 ** -24 * np.abs(kw_)).all(), (dk.max(), ek.max())
+        assert abs(float(ls) - lw) <= (np.abs(wn) * ek).sum() + 2.0 ** -24 * abs(lw)
     c = np.abs(wn)[:, None] / temp
     live = (wn != 0) & here.any(1)
     lz = zn / temp - (zn / temp).max(1, keepdims=True)
@@ -266,4 +267,6 @@ def test_rows_past_2_31_elements():
     tail = [x[-3:].clone() for x in (z, ids, t, w)]
     want = vcs.distill_topk(*tail)
     _, kl, g = vcs.distill_topk(z, ids, t, w, out=z)
-    assert torch.equal(kl[-3:], want[1]) and torch.equal(g[-3:], want[2])
+    # (few rows are split over more of the chip, in another order of their sums: 2^-16 of both, a step of the rounding)
+    assert ((kl[-3:] - want[1]).abs() <= 2.0 ** -16).all()
+    assert ((g[-3:].double() - want[2].double()).abs() <= (2.0 ** -15 + 2.0 ** -7) * want[2].double().abs()).all()
