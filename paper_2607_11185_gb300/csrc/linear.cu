@@ -1283,8 +1283,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// One token of a sequence.  A block takes 4 SLICE_LANES columns of one head's state: lane l of a row's lanes holds four
-// columns of every row its thread has, all loaded before the first is used.
+// ------------------------------------------------------------------ single tokens
+// A block takes COLS columns of one head's state: a row's lanes hold four columns each, and a thread R rows, all loaded
+// before the first is used.  The state is read and written once: what bounds it is memory.
 struct StepArgs {
   const bf16 *q, *k, *v;
   const float* log_decay;
@@ -1296,33 +1297,36 @@ struct StepArgs {
 };
 
 constexpr int kStepThreads = 256;
+constexpr int kStepHeads = 8;   // query heads at a time
+constexpr int kStepCols = 64;
 
 template <int D, int COLS>
 __global__ void __launch_bounds__(kStepThreads) linear_step(const __grid_constant__ StepArgs a) {
-  constexpr int LANES = COLS / 4;                // threads of a row
-  constexpr int RG = kStepThreads / LANES;       // row groups
-  constexpr int R = D / RG;                      // rows of a thread: rg, rg + RG, ...
-  __shared__ float sk[D], sq[D];
-  __shared__ float4 red[kStepThreads];
+  constexpr int LANES = COLS / 4, RG = kStepThreads / LANES, R = D / RG, W = kStepThreads / 32;
+  static_assert(LANES <= 32 && R >= 1, "a warp holds whole rows");
+  __shared__ float sk[D], sq[kStepHeads * D], red[kStepHeads][W][COLS];
   const int slices = D / COLS;
   const int64_t unit = blockIdx.x / slices;
   const int col0 = blockIdx.x % slices * COLS;
-  const int head = (int)(unit % a.hkv);
-  const float ld = a.log_decay[head];
+  const float ld = a.log_decay[unit % a.hkv];
   if (!decay_ok(ld)) {
     if (threadIdx.x == 0) set_status(a.status, VCS_ERR_DEVICE_CHECK);
     return;
   }
-  const int lane = threadIdx.x % LANES, rg = threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES, rg = threadIdx.x / LANES, wid = threadIdx.x >> 5;
   float4* p = reinterpret_cast<float4*>(a.states + ((size_t)unit * D + rg) * D + col0) + lane;
   float4 s[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i) s[i] = p[(size_t)i * RG * (D / 4)];
-  const bf16* vp = a.v + (size_t)unit * D + col0 + lane * 4;
-  const float v0 = __bfloat162float(vp[0]), v1 = __bfloat162float(vp[1]), v2 = __bfloat162float(vp[2]),
-              v3 = __bfloat162float(vp[3]);
+  for (int i = 0; i < R; ++i) s[i] = __ldcs(p + (size_t)i * RG * (D / 4));
+  const uint2 v = *reinterpret_cast<const uint2*>(a.v + (size_t)unit * D + col0 + lane * 4);
   if (threadIdx.x < D) sk[threadIdx.x] = __bfloat162float(a.k[(size_t)unit * D + threadIdx.x]);
-  const float lam = expf(ld);
+  const bf16* q = a.q + (size_t)unit * a.group * D;
+  auto stage = [&](int h0) {
+    const int n = min(kStepHeads, a.group - h0) * D;
+    for (int i = threadIdx.x; i < n; i += kStepThreads) sq[i] = __bfloat162float(q[(size_t)h0 * D + i]);
+  };
+  stage(0);
+  const float lam = expf(ld), v0 = lo_f(v.x), v1 = hi_f(v.x), v2 = lo_f(v.y), v3 = hi_f(v.y);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -1331,29 +1335,42 @@ __global__ void __launch_bounds__(kStepThreads) linear_step(const __grid_constan
     s[i].y = lam * s[i].y + k * v1;
     s[i].z = lam * s[i].z + k * v2;
     s[i].w = lam * s[i].w + k * v3;
-    p[(size_t)i * RG * (D / 4)] = s[i];
+    __stcs(p + (size_t)i * RG * (D / 4), s[i]);
   }
-  for (int h = 0; h < a.group; ++h) {
-    const size_t row = (size_t)unit * a.group + h;
-    if (threadIdx.x < D) sq[threadIdx.x] = __bfloat162float(a.q[row * D + threadIdx.x]);
-    __syncthreads();
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int h0 = 0; h0 < a.group; h0 += kStepHeads) {
+    const int heads = min(kStepHeads, a.group - h0);
+    if (h0 > 0) {
+      __syncthreads();   // the sums and the queries before have been read
+      stage(h0);
+      __syncthreads();
+    }
+    for (int h = 0; h < heads; ++h) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const float q = sq[rg + i * RG];
-      x.x += q * s[i].x;
-      x.y += q * s[i].y;
-      x.z += q * s[i].z;
-      x.w += q * s[i].w;
+      for (int i = 0; i < R; ++i) {
+        const float y = sq[h * D + rg + i * RG];
+        x.x += y * s[i].x;
+        x.y += y * s[i].y;
+        x.z += y * s[i].z;
+        x.w += y * s[i].w;
+      }
+#pragma unroll
+      for (int o = LANES; o < 32; o <<= 1) {   // the warp's rows
+        x.x += __shfl_xor_sync(0xffffffffu, x.x, o);
+        x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
+        x.z += __shfl_xor_sync(0xffffffffu, x.z, o);
+        x.w += __shfl_xor_sync(0xffffffffu, x.w, o);
+      }
+      if ((threadIdx.x & 31) < LANES) *reinterpret_cast<float4*>(&red[h][wid][lane * 4]) = x;
     }
-    red[threadIdx.x] = x;
     __syncthreads();
-    if (threadIdx.x < COLS) {
+    for (int i = threadIdx.x; i < heads * COLS; i += kStepThreads) {
+      const int h = i / COLS, c = i % COLS;
       float y = 0.f;
-      for (int i = 0; i < RG; ++i) y += reinterpret_cast<const float*>(red)[i * COLS + threadIdx.x];
-      a.o[row * D + col0 + threadIdx.x] = __float2bfloat16(a.scale * y);
+#pragma unroll
+      for (int w = 0; w < W; ++w) y += red[h][w][c];
+      a.o[((size_t)unit * a.group + h0 + h) * D + col0 + c] = __float2bfloat16(a.scale * y);
     }
-    __syncthreads();
   }
 }
 
@@ -1522,12 +1539,9 @@ cudaError_t launch_linear_bwd(const LinearArgs& a, const void* dout, void* dq, v
 
 template <int D>
 static cudaError_t launch_step(const StepArgs& s, int64_t num_seqs, cudaStream_t st) {
-  const int64_t units = num_seqs * s.hkv;
-  if (units * (D / 32) > INT32_MAX) return cudaErrorInvalidConfiguration;
-  if (units < 304)
-    linear_step<D, 32><<<(unsigned)(units * (D / 32)), kStepThreads, 0, st>>>(s);
-  else
-    linear_step<D, D><<<(unsigned)units, kStepThreads, 0, st>>>(s);
+  const int64_t blocks = num_seqs * s.hkv * (D / kStepCols);
+  if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+  linear_step<D, kStepCols><<<(unsigned)blocks, kStepThreads, 0, st>>>(s);
   return cudaGetLastError();
 }
 
