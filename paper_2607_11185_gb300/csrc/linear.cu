@@ -15,8 +15,11 @@
 //
 // A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among the
 // CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.  linear_states
-// adds up the keys and values of every such piece first; each CTA then puts its starting state together from the
-// pieces before it.  So a cut costs its piece's keys and values read twice.
+// adds up the keys and values before every cut, as far back as the decay leaves anything in fp32, in parts of equal size
+// spread over the chip, and linear_join makes the cuts' states of them.  So a cut costs its piece's keys and values
+// read twice.  (A CTA that adds up the piece before its own cut takes as long as the head that forgets slowest: the three
+// passes of a backward pass at 40 / 8 heads of 128 and 135,512 tokens 955 us, the parts 480 with what joins them.)
+
 #include <cfloat>
 #include <cstdint>
 
@@ -34,15 +37,30 @@ constexpr int kChunk = 128;
 // Sequences up to this many chunks are not cut where all are: a CTA takes those that start in its range.
 constexpr int kWhole = 16;
 
+// (the lowest decays would be -inf as a log2, and not a number times 0 tokens)
+__device__ __forceinline__ float log2_decay(float g) { return fmaxf(g * 1.4426950408889634f, -1e30f); }
 __device__ __forceinline__ bool decay_ok(float g) { return g <= 0.f && g >= -FLT_MAX; }
 
 // ------------------------------------------------------------------ division of the work
-struct Plan {        // in the workspace header, behind the status word
+constexpr int kFade = 150;   // a weight of 2^-150 and less is 0 in fp32
+constexpr int kWaves = 3;    // parts to a CTA, at most
+constexpr int kPartCost = 3; // of a part, in chunks: its first loads and its sum's way out
+
+// Chunks of a head with the log2 decay l2 behind which a key's weight is 0.
+__device__ __forceinline__ int fade_chunks(float l2) {
+  const float far = kFade / fabsf(l2 * kChunk);   // l2 = 0: infinite
+  return far < 1e8f ? (int)far + 2 : 1 << 30;
+}
+
+struct Plan {        // in the workspace, behind the header
   int64_t total;     // chunks of all sequences
   int64_t range;     // of a CTA
   int32_t cut;       // sequences are cut at the ranges' ends
+  int32_t part[2];   // chunks of a part, in order and the other way in time
+  int32_t pad;
+  // Of the cut behind range t: chunks whose keys and values its state needs, and the parts before it (the last: all).
+  int32_t need[2][kGrid], first[2][kGrid + 1];
 };
-constexpr size_t kWsPlan = 64;
 
 __device__ __forceinline__ int seg_chunks(const int32_t* __restrict__ cu, int32_t num_tokens, int s, int32_t* status) {
   const int start = cu[s], end = cu[s + 1];
@@ -55,9 +73,11 @@ __device__ __forceinline__ int seg_chunks(const int32_t* __restrict__ cu, int32_
 
 // off[s] = chunks of segments 0 .. s - 1, and the plan.  The call's first kernel: it clears the status word.
 __global__ void __launch_bounds__(1024) linear_plan(const int32_t* __restrict__ cu, int32_t num_segments,
-                                                    int32_t num_tokens, int32_t heads, int32_t grid, int32_t* off,
-                                                    Plan* plan, int32_t* status) {
-  __shared__ long long wsum[32];
+                                                    int32_t num_tokens, int32_t heads, int32_t grid,
+                                                    const float* __restrict__ log_decay, int32_t* off, Plan* plan,
+                                                    int32_t* status) {
+  __shared__ long long wsum[32], s_total, s_range;
+  __shared__ int need[2][kGrid], s_part[2][kWaves];
   __shared__ long long carry;
   __shared__ int longest;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -100,9 +120,82 @@ __global__ void __launch_bounds__(1024) linear_plan(const int32_t* __restrict__ 
     if (carry > most) set_status(status, VCS_ERR_DEVICE_CHECK);
     const long long all = carry > most ? 0 : carry * heads;
     off[num_segments] = (int32_t)(carry > most ? 0 : carry);
-    plan->total = all;
+    s_total = plan->total = all;
+    s_range = plan->range = (all + grid - 1) / grid;
     plan->cut = longest > kWhole;
-    plan->range = (all + grid - 1) / grid;
+  }
+  if (num_tokens <= kWhole * kChunk) return;   // no sequence is so long
+  __syncthreads();
+  const long long total = s_total, range = s_range;
+  const bool cut = longest > kWhole;
+  if (threadIdx.x < kGrid) {
+    const int t = threadIdx.x;
+    const long long g = range * (t + 1);
+    int fwd = 0, bwd = 0;
+    if (cut && g < total) {   // the sequence that chunk g is in
+      const int q = (int)(g / heads);
+      int lo = 0, up = num_segments;
+      while (up - lo > 1) {
+        const int mid = (lo + up) >> 1;
+        if (off[mid] <= q) lo = mid;
+        else up = mid;
+      }
+      const int first = off[lo], nch = off[lo + 1] - first;
+      const long long rest = g - (long long)first * heads, base = (long long)first * heads + rest / nch * nch;
+      const float ld = log_decay[rest / nch], l2 = log2_decay(ld);
+      if (g > base && decay_ok(ld)) {
+        const int keep = fade_chunks(l2);
+        const long long back = g - (g - range > base ? g - range : base);
+        const long long end = base + nch < total ? base + nch : total, ahead = (g + range < end ? g + range : end) - g;
+        fwd = (int)(back < keep ? back : keep);
+        bwd = (int)(ahead < keep ? ahead : keep);
+      }
+    }
+    need[0][t] = plan->need[0][t] = fwd;
+    need[1][t] = plan->need[1][t] = bwd;
+  }
+  __syncthreads();
+  // The smallest parts that make one, two or three to a CTA: a warp each, for both directions.
+  const int d = wid & 1;
+  if (wid < 2 * kWaves) {
+    const int most_parts = (wid / 2 + 1) * grid;
+    int lo = 4, up = 4;   // up is enough: no more than one part a cut
+    for (int t = lane; t < kGrid; t += 32) up = max(up, need[d][t]);
+    up = __reduce_max_sync(0xffffffffu, up);
+    while (lo < up) {
+      const int mid = (lo + up) >> 1;
+      int n = 0;
+      for (int t = lane; t < kGrid; t += 32) n += (need[d][t] + mid - 1) / mid;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (n <= most_parts) up = mid;
+      else lo = mid + 1;
+    }
+    if (lane == 0) s_part[d][wid / 2] = up;
+  }
+  __syncthreads();
+  if (wid < 2) {
+    int part = s_part[d][0];
+    for (int i = 1, best = part + kPartCost; i < kWaves; ++i)
+      if ((i + 1) * (s_part[d][i] + kPartCost) < best) {
+        part = s_part[d][i];
+        best = (i + 1) * (part + kPartCost);
+      }
+    int carry = 0;
+    for (int t0 = 0; t0 < kGrid; t0 += 32) {
+      const int t = t0 + lane, n = t < kGrid ? (need[d][t] + part - 1) / part : 0;
+      int x = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (t < kGrid) plan->first[d][t] = carry + x - n;
+      carry += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) {
+      plan->first[d][kGrid] = carry;
+      plan->part[d] = part;
+    }
   }
 }
 
@@ -168,7 +261,7 @@ struct Walk {
       c1 = cut && hi - base < nch ? (int)(hi - base) : nch;
       g = base + c1;
       const float ld = __ldg(&a.log_decay[head]);
-      l2 = ld * 1.4426950408889634f;
+      l2 = log2_decay(ld);
       if (decay_ok(ld)) return true;
       set_status(a.status, VCS_ERR_DEVICE_CHECK);
     }
@@ -216,76 +309,70 @@ __device__ __forceinline__ void zero_row(uint32_t tile, int r) {
 // which hold its 24 bits; where queries read them, rounded to bf16 themselves, one.
 struct StateArgs {
   Common c;
-  float* slots;            // [grid][D][D]
-  const float* state_in;   // state_out != nullptr: every piece
+  float* slots;            // [parts][D][D]; state_out != nullptr: every piece of the ranges, a slot a CTA
+  const float* state_in;
   float* state_out;
   int32_t group;           // key heads of a state
   bool back;
 };
 
-template <int D>
+template <int D, int TERMS>
 struct Sta {
   static constexpr int TILE = kChunk * D * 2;
-  static constexpr int NKV = 2;
+  static constexpr int NKV = (TERMS == 1 ? 3 : 2) * (D == 64 ? 2 : 1);
   static constexpr int OFF_KV = 0;
   static constexpr int OFF_TERM = NKV * 2 * TILE;        // second and third term of a weighted key tile
   // at D = 64 the upper lanes of an MMA (see Lin) read a tile further than the last term
-  static constexpr int OFF_BAR = OFF_TERM + (D == 64 ? 3 : 2) * TILE;
+  static constexpr int OFF_BAR = OFF_TERM + (TERMS == 1 ? 0 : D == 64 ? 3 : 2) * TILE;
   static constexpr int SMEM = OFF_BAR + 256;
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
+  static constexpr int REG_CTRL = 80, REG_ROWS = 96, REG_STATE = 224;
+  static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
   static_assert(SMEM <= 232448, "shared memory budget");
 };
 
 struct StaBars {
-  uint64_t kv_full[2], kv_empty[2];
-  uint64_t kt_full[2];   // the weighted keys of a slot are written
-  uint64_t term_free;    // and read
+  uint64_t kv_full[6], kv_empty[6];
+  uint64_t kt_full[6][2];  // the weighted keys of a slot's first and second 64 tokens are written
+  uint64_t term_free[2];   // and read
   uint64_t u_full[2], u_free[2];
   uint32_t tmem_base;
   int32_t abort;
 };
 static_assert(sizeof(StaBars) <= 256, "barrier space");
 
-constexpr int kStaThreads = 384;
+constexpr int kStaThreads = 512;
 
 template <int D, int TERMS>
 __global__ void __launch_bounds__(kStaThreads, 1)
     linear_states(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ StateArgs p) {
-  using C = Sta<D>;
+  using C = Sta<D, TERMS>;
   extern __shared__ __align__(1024) uint8_t smem[];
   StaBars* bars = reinterpret_cast<StaBars*>(smem + C::OFF_BAR);
   Walk w(p.c, blockIdx.x);
-  if (p.state_out == nullptr) {
-    // only the piece that goes on: the last one of the range, the other way in time the first one
-    if (!w.cut || w.g >= w.hi) return;
-    if (!p.back) {
-      if (w.hi >= p.c.plan->total) return;
-      w.locate(w.hi);
-      if (w.base >= w.hi) return;
-      if (w.base > w.g) w.g = w.base;
-    } else {
-      w.locate(w.g);
-      if (w.base >= w.g) return;
-      if (w.base + w.nch < w.hi) w.hi = w.base + w.nch;
-    }
-    w.located = false;
-  }
-  if (w.g >= w.hi || smem_u32(smem) & 1023u) {
-    if (w.g < w.hi && threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
+  const bool all = p.state_out != nullptr;
+  const Plan& plan = *p.c.plan;
+  const int parts = all || !w.cut ? 0 : plan.first[p.back][kGrid];
+  if (all ? w.g >= w.hi : (int)blockIdx.x >= parts) return;
+  if (smem_u32(smem) & 1023u) {
+    if (threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t sbase = smem_u32(smem);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < C::NKV; ++i) {
       mbar_init(&bars->kv_full[i], 1);
       mbar_init(&bars->kv_empty[i], 1);
+      mbar_init(&bars->kt_full[i][0], 128);
+      mbar_init(&bars->kt_full[i][1], 128);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->term_free[i], 1);
       mbar_init(&bars->u_full[i], 1);
       mbar_init(&bars->u_free[i], 4);
-      mbar_init(&bars->kt_full[i], 128);
     }
-    mbar_init(&bars->term_free, 1);
     bars->abort = 0;
     fence_mbar_init();
   }
@@ -298,78 +385,99 @@ __global__ void __launch_bounds__(kStaThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
-  // The next piece, for states between pieces without the chunks so far from its end that their weight is 0 in fp32
-  // (2^-150 and less, which rounds to 0): a head that forgets in a thousand tokens reads a tenth of a long piece.
+  // The next piece: of the CTA's range, or every grid-th part of what the cuts need, from the cut outwards.
+  int slot = (int)blockIdx.x - (int)gridDim.x;
   auto next = [&] {
-    if (!w.next()) return false;
-    if (p.state_out == nullptr && w.l2 < 0.f) {
-      const float far = 150.f / (-w.l2 * kChunk);
-      const int keep = far < 1e6f ? (int)far + 2 : 1 << 24;
-      if (p.back) w.c1 = min(w.c1, w.c0 + keep);
-      else w.c0 = max(w.c0, w.c1 - keep);
+    if (all) {
+      slot = blockIdx.x;
+      if (!w.next()) return false;
+      w.c0 = max(w.c0, w.c1 - fade_chunks(w.l2));   // (what lies before a fade adds 0, a state that goes in too)
+      return true;
     }
+    slot += gridDim.x;
+    if (slot >= parts) return false;
+    int lo = 0, up = kGrid;   // first[lo] <= slot < first[up]
+    while (up - lo > 1) {
+      const int mid = (lo + up) >> 1;
+      if (__ldg(&plan.first[p.back][mid]) <= slot) lo = mid;
+      else up = mid;
+    }
+    const int64_t g = plan.range * (lo + 1);
+    w.locate(g);
+    w.l2 = log2_decay(__ldg(&p.c.log_decay[w.head]));
+    const int size = plan.part[p.back], j = slot - __ldg(&plan.first[p.back][lo]), e = (int)(g - w.base);
+    const int near = j * size, far = min(near + size, __ldg(&plan.need[p.back][lo]));
+    w.c0 = p.back ? e + near : e - far;
+    w.c1 = p.back ? e + far : e - near;
     return true;
   };
 
-  if (warp == 0) {
-    // ---------------------------------------------------------- producer
-    if (lane == 0) {
-      bool go = true;
-      uint32_t it = 0;
+  if (warp < 4) {
+    setmaxnreg_dec<C::REG_CTRL>();
+    if (warp == 0) {
+      // ---------------------------------------------------------- producer
+      if (lane == 0) {
+        bool go = true;
+        uint32_t it = 0;
+        while (go && next())
+          for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+            const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
+            for (int h = 0; h < p.group; ++h, ++it) {
+              const uint32_t slot = it % C::NKV;
+              if ((it >= C::NKV && !mbar_wait(&bars->kv_empty[slot], (it / C::NKV - 1) & 1)) || gave_up()) {
+                set_abort(&bars->abort, p.c.status);
+                go = false;
+                break;
+              }
+              mbar_arrive_expect_tx(&bars->kv_full[slot], 2 * C::TILE);
+#pragma unroll
+              for (int kb = 0; kb < D / 64; ++kb) {
+                uint8_t* dst = smem + C::OFF_KV + slot * 2 * C::TILE + kb * 16384;
+                tma_load_3d(dst, &tm_k, &bars->kv_full[slot], kb * 64, w.head * p.group + h, w.start + c * kChunk);
+                tma_load_3d(dst + C::TILE, &tm_v, &bars->kv_full[slot], kb * 64, w.head * p.group + h,
+                            w.start + c * kChunk);
+              }
+            }
+          }
+      }
+    } else if (warp == 1) {
+      // ---------------------------------------------------------- MMA issuer
+      // Every lane runs every step and no lane's answer to a wait decides where the warp goes; a vote an item does.
+      const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16384, 1024), td = smem_desc(sbase + C::OFF_TERM, 16384, 1024);
+      bool ok = true, go = true;
+      uint32_t it = 0, un = 0;
       while (go && next())
-        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int c = p.back ? w.c1 - 1 - n : w.c0 + n;
+        for (int n = 0; go && n < w.c1 - w.c0; ++n, ++un)
           for (int h = 0; h < p.group; ++h, ++it) {
-            const uint32_t slot = it & 1;
-            if ((it >= 2 && !mbar_wait(&bars->kv_empty[slot], (it / 2 - 1) & 1)) || gave_up()) {
-              set_abort(&bars->abort, p.c.status);
-              go = false;
-              break;
-            }
-            mbar_arrive_expect_tx(&bars->kv_full[slot], 2 * C::TILE);
+            const uint32_t slot = it % C::NKV, buf = un & 1;
+            if (h == 0 && un >= 2) ok = ok && mbar_wait(&bars->u_free[buf], (un / 2 - 1) & 1);
+            for (int half = 0; half < 2; ++half) {
+              ok = ok && mbar_wait(&bars->kt_full[slot][half], (it / C::NKV) & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                const uint64_t a0 = desc_at(kd, slot * 2 * C::TILE + half * 8192), b = desc_at(a0, C::TILE);
 #pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb) {
-              uint8_t* dst = smem + C::OFF_KV + slot * 2 * C::TILE + kb * 16384;
-              tma_load_3d(dst, &tm_k, &bars->kv_full[slot], kb * 64, w.head * p.group + h, w.start + c * kChunk);
-              tma_load_3d(dst + C::TILE, &tm_v, &bars->kv_full[slot], kb * 64, w.head * p.group + h,
-                          w.start + c * kChunk);
+                for (int t = TERMS - 1; t >= 0; --t)   // the smallest term first
+#pragma unroll
+                  for (int kk = 0; kk < 4; ++kk)
+                    tc_mma_ss(tmem + buf * 128,
+                              desc_at(t == 0 ? a0 : desc_at(td, (t - 1) * C::TILE + half * 8192), kk * 2048),
+                              desc_at(b, kk * 2048), C::IDESC_U, h > 0 || half > 0 || t < TERMS - 1 || kk > 0);
+                if (TERMS > 1) tc_commit(&bars->term_free[half]);
+                if (half == 1) tc_commit(&bars->kv_empty[slot]);
+                if (half == 1 && h == p.group - 1) tc_commit(&bars->u_full[buf]);
+              }
+              __syncwarp();
             }
+            go = __all_sync(0xffffffffu, ok);
+            if (!go) break;
           }
-        }
+      if (!go) set_abort(&bars->abort, p.c.status);
     }
-  } else if (warp == 1) {
-    // ---------------------------------------------------------- MMA issuer
-    // Every lane runs every step and no lane's answer to a wait decides where the warp goes; a vote an item does.
-    const uint64_t kd = smem_desc(sbase + C::OFF_KV, 16384, 1024), td = smem_desc(sbase + C::OFF_TERM, 16384, 1024);
-    bool ok = true, go = true;
-    uint32_t it = 0, un = 0;
-    while (go && next())
-      for (int n = 0; go && n < w.c1 - w.c0; ++n, ++un)
-        for (int h = 0; h < p.group; ++h, ++it) {
-          const uint32_t slot = it & 1, buf = un & 1;
-          ok = ok && mbar_wait(&bars->kt_full[slot], (it / 2) & 1);
-          if (h == 0 && un >= 2) ok = ok && mbar_wait(&bars->u_free[buf], (un / 2 - 1) & 1);
-          go = __all_sync(0xffffffffu, ok);
-          if (!go) break;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint64_t a0 = desc_at(kd, slot * 2 * C::TILE), b = desc_at(a0, C::TILE);
-#pragma unroll
-            for (int t = TERMS - 1; t >= 0; --t)   // the smallest term first
-#pragma unroll
-              for (int kk = 0; kk < 8; ++kk)
-                tc_mma_ss(tmem + buf * 128, desc_at(t == 0 ? a0 : desc_at(td, (t - 1) * C::TILE), kk * 2048),
-                          desc_at(b, kk * 2048), C::IDESC_U, h > 0 || t < TERMS - 1 || kk > 0);
-            tc_commit(&bars->kv_empty[slot]);
-            if (TERMS > 1) tc_commit(&bars->term_free);
-            if (h == p.group - 1) tc_commit(&bars->u_full[buf]);
-          }
-          __syncwarp();
-        }
-    if (!go) set_abort(&bars->abort, p.c.status);
-  } else if (warp >= 4 && warp < 8) {
-    // ---------------------------------------------------------- weighted keys, a thread a token
-    const int r = threadIdx.x - 128;
+  } else if (warp < 12) {
+    // ---------------------------------------------------------- weighted keys: a warpgroup's 64 tokens, two threads each
+    setmaxnreg_dec<C::REG_ROWS>();
+    const int half = warp < 8 ? 0 : 1, r = half * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6 & 1;
     bool go = true;
     uint32_t it = 0;
     while (go && next())
@@ -378,52 +486,52 @@ __global__ void __launch_bounds__(kStaThreads, 1)
         const int rows = w.rows(c);
         const float wt = r < rows ? exp2f(w.l2 * (float)(p.back ? r : rows - 1 - r)) : 0.f;
         for (int h = 0; h < p.group; ++h, ++it) {
-          const uint32_t tile = sbase + C::OFF_KV + (it & 1) * 2 * C::TILE, term = sbase + C::OFF_TERM;
-          if (!mbar_wait_warp(&bars->kv_full[it & 1], (it / 2) & 1) ||
-              (TERMS > 1 && it > 0 && !mbar_wait_warp(&bars->term_free, (it - 1) & 1)) ||
+          const uint32_t slot = it % C::NKV, tile = sbase + C::OFF_KV + slot * 2 * C::TILE, term = sbase + C::OFF_TERM;
+          if (!mbar_wait_warp(&bars->kv_full[slot], (it / C::NKV) & 1) ||
+              (TERMS > 1 && it > 0 && !mbar_wait_warp(&bars->term_free[half], (it - 1) & 1)) ||
               __any_sync(0xffffffffu, gave_up())) {
             go = false;
             break;
           }
-          if (r >= rows) {  // rows of the next segment, which may hold anything
-            zero_row<D>(tile, r);
-            zero_row<D>(tile + C::TILE, r);
-            if (TERMS > 1) {
-              zero_row<D>(term, r);
-              zero_row<D>(term + C::TILE, r);
+          // its part of a row: 8 vectors of the one 64-column block or the other, or 4 of the only one
+          const uint32_t row = (D == 128 ? part * 16384 : 0) + r * 128;
+          const int u0 = D == 128 ? 0 : part * 4;
+#pragma unroll
+          for (int i8 = 0; i8 < D / 16; ++i8) {
+            const uint32_t at = row + (((u0 + i8 + r) & 7) << 4);
+            if (r >= rows) {  // rows of the next segment, which may hold anything
+              st_shared_v4(tile + at, 0u, 0u, 0u, 0u);
+              st_shared_v4(tile + C::TILE + at, 0u, 0u, 0u, 0u);
+#pragma unroll
+              for (int t = 1; t < TERMS; ++t) st_shared_v4(term + (t - 1) * C::TILE + at, 0u, 0u, 0u, 0u);
+              continue;
             }
-          } else {
+            const uint4 x = ld_shared_v4(tile + at);
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            uint32_t y[3][4];
 #pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb)
+            for (int i = 0; i < 4; ++i) {
+              float a = lo_f(in[i]) * wt, b = hi_f(in[i]) * wt;
 #pragma unroll
-              for (int u = 0; u < 8; ++u) {
-                const uint32_t at = kb * 16384 + r * 128 + (((u + r) & 7) << 4);
-                const uint4 x = ld_shared_v4(tile + at);
-                const uint32_t in[4] = {x.x, x.y, x.z, x.w};
-                uint32_t y[3][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  float a = lo_f(in[i]) * wt, b = hi_f(in[i]) * wt;
-#pragma unroll
-                  for (int t = 0; t < TERMS; ++t) {
-                    y[t][i] = pack_bf16(a, b);
-                    a -= lo_f(y[t][i]);
-                    b -= hi_f(y[t][i]);
-                  }
-                }
-                st_shared_v4(tile + at, y[0][0], y[0][1], y[0][2], y[0][3]);
-#pragma unroll
-                for (int t = 1; t < TERMS; ++t)
-                  st_shared_v4(term + (t - 1) * C::TILE + at, y[t][0], y[t][1], y[t][2], y[t][3]);
+              for (int t = 0; t < TERMS; ++t) {
+                y[t][i] = pack_bf16(a, b);
+                a -= lo_f(y[t][i]);
+                b -= hi_f(y[t][i]);
               }
+            }
+            st_shared_v4(tile + at, y[0][0], y[0][1], y[0][2], y[0][3]);
+#pragma unroll
+            for (int t = 1; t < TERMS; ++t)
+              st_shared_v4(term + (t - 1) * C::TILE + at, y[t][0], y[t][1], y[t][2], y[t][3]);
           }
           fence_proxy_async_smem();
-          mbar_arrive(&bars->kt_full[it & 1]);
+          mbar_arrive(&bars->kt_full[slot][half]);
         }
       }
     if (!go) set_abort(&bars->abort, p.c.status);
-  } else if (warp >= 8) {
+  } else {
     // ---------------------------------------------------------- sums, a thread a row of the state
+    setmaxnreg_inc<C::REG_STATE>();
     const int quad = warp & 3, r = quad * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
     bool go = true;
@@ -462,9 +570,8 @@ __global__ void __launch_bounds__(kStaThreads, 1)
       if (D == 128 || quad < 2) {
         float* dst;
         const size_t state = ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
-        const bool on = p.back ? w.c0 > 0 : w.c1 < w.nch;   // it goes on in another CTA
-        if (on) {
-          dst = p.slots + ((size_t)blockIdx.x * D + r) * D;
+        if (!all || w.c1 < w.nch) {   // for the cut
+          dst = p.slots + ((size_t)slot * D + r) * D;
         } else {
           dst = p.state_out + state;
           if (p.state_in != nullptr && w.c0 == 0) {
@@ -495,16 +602,62 @@ __global__ void __launch_bounds__(kStaThreads, 1)
   }
 }
 
+// ------------------------------------------------------------------ states at the cuts
+struct JoinArgs {
+  Common c;
+  const float* slots;
+  const float* state_in;
+  float* starts;   // [grid][D][D]: of the cut behind range t
+  bool back, all;  // all: a slot a CTA, the sum of its last piece
+};
+
+// A block a cut and 1,024 elements: the parts before it, the nearest first, until they have faded.
+template <int D>
+__global__ void __launch_bounds__(256) linear_join(const __grid_constant__ JoinArgs p) {
+  const Plan& plan = *p.c.plan;
+  const int t = blockIdx.x;
+  if (!plan.cut || plan.need[p.back][t] == 0) return;
+  Walk w(p.c, t);
+  const int64_t g = plan.range * (t + 1);
+  w.locate(g);
+  const float l2 = log2_decay(__ldg(&p.c.log_decay[w.head]));
+  const int size = plan.part[p.back], e = (int)(g - w.base);
+  const size_t at = (size_t)blockIdx.y * 1024 + threadIdx.x * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float* src, float f) {
+    const float4 x = *reinterpret_cast<const float4*>(src + at);
+    s.x = fmaf(f, x.x, s.x);
+    s.y = fmaf(f, x.y, s.y);
+    s.z = fmaf(f, x.z, s.z);
+    s.w = fmaf(f, x.w, s.w);
+  };
+  bool faded = false;
+  for (int x = t; !faded && x >= 0 && x < kGrid; p.back ? ++x : --x) {
+    const int64_t gap = p.back ? plan.range * (x + 1) - g : g - plan.range * (x + 1);   // chunks between the cuts
+    if (p.back ? plan.range * (x + 1) >= w.base + w.nch : plan.range * (x + 1) <= w.base) break;   // in another sequence
+    const int first = p.all ? x : plan.first[p.back][x], end = p.all ? x + 1 : plan.first[p.back][x + 1];
+    for (int i = first; i < end; ++i) {
+      const float f = exp2f(l2 * (float)((gap + (int64_t)(i - first) * size) * kChunk));
+      faded = f == 0.f;
+      if (faded) break;
+      add(p.slots + (size_t)i * D * D, f);
+    }
+  }
+  if (p.state_in != nullptr && !faded)
+    add(p.state_in + ((size_t)w.seg * p.c.heads + w.head) * D * D, exp2f(l2 * (float)((int64_t)e * kChunk)));
+  *reinterpret_cast<float4*>(p.starts + (size_t)t * D * D + at) = s;
+}
+
 // ------------------------------------------------------------------ outputs
 struct OutArgs {
   Common c;
-  const float* slots;
+  const float* starts;     // the states at the cuts
   const float* state_in;
   float* state_out;
   int32_t gx, gy;          // query heads and key heads of a state; one of them is 1
   float scale;
   bool wide;               // out is 32-byte aligned
-  bool transposed;         // of the slots' states (the way back in time)
+  bool transposed;         // of the states at the cuts (the way back in time)
   bf16* out;
 };
 
@@ -1108,21 +1261,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (i % 32 == 28) asm volatile("" ::: "memory");   // not all loads ahead: the registers are the state's
           }
         };
-        // what other CTAs' pieces bring, the nearest first, until it has faded below fp32
-        bool faded = false;
+        const size_t state = ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
         if (!back) {
-          for (int x = blockIdx.x - 1; w.c0 > 0 && x >= 0 && !faded; --x) {
-            const int64_t e = (x + 1) * w.range - w.base;    // chunk behind that CTA's piece
-            const float f = exp2f(w.l2 * (float)((w.c0 - e) * kChunk));
-            faded = f == 0.f;
-            if (!faded) add(p.slots + ((size_t)x * D + r) * D, f);
-            if (x * w.range <= w.base) break;
-          }
-          if (p.state_in != nullptr && !faded)
-            add(p.state_in + ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D,
-                exp2f(w.l2 * (float)((int64_t)w.c0 * kChunk)));
+          if (w.c0 > 0) add(p.starts + ((size_t)(blockIdx.x - 1) * D + r) * D, 1.f);
+          else if (p.state_in != nullptr) add(p.state_in + state, 1.f);
           if (p.state_out != nullptr && w.c0 > 0 && w.c1 == w.nch) {  // its last piece's own sum is there
-            float* dst = p.state_out + ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
+            float* dst = p.state_out + state;
             const float f = exp2f(w.l2 * (float)(w.len - w.c0 * kChunk));
 #pragma unroll
             for (int i = 0; i < D; i += 4) {
@@ -1135,21 +1279,14 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (i % 32 == 28) asm volatile("" ::: "memory");
             }
           }
-        } else {
-          for (int x = blockIdx.x + 1; w.c1 < w.nch && x < (int)gridDim.x && !faded; ++x) {
-            const int64_t b = x * w.range - w.base;          // that CTA's first chunk
-            if (b >= w.nch) break;
-            const float f = exp2f(w.l2 * (float)((b - w.c1) * kChunk));
-            faded = f == 0.f;
-            if (faded) break;
-            if (!p.transposed) {
-              add(p.slots + ((size_t)x * D + r) * D, f);
-            } else {
+        } else if (w.c1 < w.nch) {
+          if (!p.transposed) {
+            add(p.starts + ((size_t)blockIdx.x * D + r) * D, 1.f);
+          } else {
 #pragma unroll
-              for (int i = 0; i < D; ++i) {
-                s[i] = fmaf(f, p.slots[((size_t)x * D + i) * D + r], s[i]);
-                if (i % 32 == 31) asm volatile("" ::: "memory");
-              }
+            for (int i = 0; i < D; ++i) {
+              s[i] = p.starts[((size_t)blockIdx.x * D + i) * D + r];
+              if (i % 32 == 31) asm volatile("" ::: "memory");
             }
           }
         }
@@ -1380,32 +1517,42 @@ namespace {
 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-// Workspace: header (status word, plan), the segments' chunk offsets, a state a CTA (the backward: two).
+// Workspace: header (status word), the plan, the segments' chunk offsets, and, where a sequence may be cut, the parts' sums
+// (three to a CTA at most) and the states at the cuts.
+int32_t grid_of(int32_t num_segments, int64_t num_tokens, int32_t hkv) {
+  const int64_t chunks = hkv * (num_tokens / kChunk + (int64_t)num_segments);   // no fewer than the sequences'
+  return (int32_t)(chunks < kGrid ? chunks : kGrid);
+}
+bool may_cut(int64_t num_tokens) { return num_tokens > kWhole * kChunk; }
+size_t ws_plan() { return align256(sizeof(Plan)); }
 size_t ws_off(int32_t num_segments) { return align256(((size_t)num_segments + 1) * 4); }
-size_t ws_slots(int32_t d) { return (size_t)kGrid * d * d * 4; }
+size_t ws_bytes(int32_t num_segments, int64_t num_tokens, int32_t hkv, int32_t d) {
+  const size_t states = may_cut(num_tokens) ? 4 * (size_t)grid_of(num_segments, num_tokens, hkv) : 0;
+  return kWsHeader + ws_plan() + ws_off(num_segments) + states * d * d * 4;
+}
 
 struct Work {
   Common c;
-  float* slots[2];
-  int64_t chunks;   // upper bound of the sequences'
+  float *slots, *starts;
   int32_t grid;
+  bool cut;
 };
 
 Work make_work(const LinearArgs& a, void* ws) {
   Work w;
   char* p = static_cast<char*>(ws);
+  w.grid = grid_of(a.num_segments, a.num_tokens, a.hkv);
+  w.cut = may_cut(a.num_tokens);
   w.c.log_decay = a.log_decay;
   w.c.cu = a.cu_seqlens;
-  w.c.off = reinterpret_cast<int32_t*>(p + kWsHeader);
-  w.c.plan = reinterpret_cast<Plan*>(p + kWsPlan);
+  w.c.plan = reinterpret_cast<Plan*>(p + kWsHeader);
+  w.c.off = reinterpret_cast<int32_t*>(p + kWsHeader + ws_plan());
   w.c.num_segments = a.num_segments;
   w.c.num_tokens = (int32_t)a.num_tokens;
   w.c.heads = a.hkv;
   w.c.status = static_cast<int32_t*>(ws);
-  w.slots[0] = reinterpret_cast<float*>(p + kWsHeader + ws_off(a.num_segments));
-  w.slots[1] = w.slots[0] + (size_t)kGrid * a.d * a.d;
-  w.chunks = a.hkv * (a.num_tokens / kChunk + (int64_t)a.num_segments);
-  w.grid = (int32_t)(w.chunks < kGrid ? w.chunks : kGrid);
+  w.slots = reinterpret_cast<float*>(p + kWsHeader + ws_plan() + ws_off(a.num_segments));
+  w.starts = w.slots + 3 * (size_t)w.grid * a.d * a.d;
   return w;
 }
 
@@ -1415,35 +1562,45 @@ bool encode(CUtensorMap* map, const void* base, int d, int64_t heads, const Line
 }
 
 cudaError_t launch_plan(const Work& w, cudaStream_t st) {
-  linear_plan<<<1, 1024, 0, st>>>(w.c.cu, w.c.num_segments, w.c.num_tokens, w.c.heads, w.grid,
+  linear_plan<<<1, 1024, 0, st>>>(w.c.cu, w.c.num_segments, w.c.num_tokens, w.c.heads, w.grid, w.c.log_decay,
                                   const_cast<int32_t*>(w.c.off), const_cast<Plan*>(w.c.plan), w.c.status);
   return cudaGetLastError();
 }
 
+// The states at the cuts (and, with state_out, behind the segments, but for what pieces before the last add to them).
 template <int D, int TERMS>
 cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, const void* v, int group, bool back,
-                          float* slots, const float* state_in, float* state_out, cudaStream_t st) {
-  using C = Sta<D>;
+                          const float* state_in, float* state_out, cudaStream_t st) {
+  using C = Sta<D, TERMS>;
+  if (!w.cut && state_out == nullptr) return cudaSuccess;
   alignas(64) CUtensorMap tk, tv;
   const int64_t heads = (int64_t)a.hkv * group;
-  if (!encode(&tk, k, D, heads, a) || !encode(&tv, v, D, heads, a))
-    return cudaErrorInvalidValue;
+  if (!encode(&tk, k, D, heads, a) || !encode(&tv, v, D, heads, a)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   StateArgs p;
   p.c = w.c;
-  p.slots = slots;
+  p.slots = w.slots;
   p.state_in = state_in;
   p.state_out = state_out;
   p.group = group;
   p.back = back;
   linear_states<D, TERMS><<<w.grid, kStaThreads, C::SMEM, st>>>(tk, tv, p);
+  if (e = cudaGetLastError(); e != cudaSuccess || !w.cut) return e;
+  JoinArgs j;
+  j.c = w.c;
+  j.slots = w.slots;
+  j.state_in = state_in;
+  j.starts = w.starts;
+  j.back = back;
+  j.all = state_out != nullptr;
+  linear_join<D><<<dim3(w.grid, D * D / 1024), 256, 0, st>>>(j);
   return cudaGetLastError();
 }
 
 template <int D, int KIND>
 cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int gx, int gy,
-                       const float* slots, bool transposed, const float* state_in, float* state_out, void* out,
+                       bool transposed, const float* state_in, float* state_out, void* out,
                        cudaStream_t st) {
   using C = Lin<D, KIND>;
   alignas(64) CUtensorMap tq, tk, tv, to;
@@ -1459,7 +1616,7 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
   if (e != cudaSuccess) return e;
   OutArgs p;
   p.c = w.c;
-  p.slots = slots;
+  p.starts = w.starts;
   p.state_in = state_in;
   p.state_out = state_out;
   p.gx = gx;
@@ -1474,31 +1631,28 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
 
 template <int D>
 cudaError_t launch_forth(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
-                         const float* slots, const float* state_in, float* state_out, void* out, cudaStream_t st) {
-  return group == 1 ? launch_out<D, FWD1>(w, a, q, k, v, 1, 1, slots, false, state_in, state_out, out, st)
-                    : launch_out<D, FWD>(w, a, q, k, v, group, 1, slots, false, state_in, state_out, out, st);
+                         const float* state_in, float* state_out, void* out, cudaStream_t st) {
+  return group == 1 ? launch_out<D, FWD1>(w, a, q, k, v, 1, 1, false, state_in, state_out, out, st)
+                    : launch_out<D, FWD>(w, a, q, k, v, group, 1, false, state_in, state_out, out, st);
 }
 
 template <int D>
 cudaError_t launch_back(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
-                        const float* slots, bool transposed, void* out, cudaStream_t st) {
-  return group == 1 ? launch_out<D, BACK1>(w, a, q, k, v, 1, 1, slots, transposed, nullptr, nullptr, out, st)
-                    : launch_out<D, BACK>(w, a, q, k, v, 1, group, slots, transposed, nullptr, nullptr, out, st);
+                        bool transposed, void* out, cudaStream_t st) {
+  return group == 1 ? launch_out<D, BACK1>(w, a, q, k, v, 1, 1, transposed, nullptr, nullptr, out, st)
+                    : launch_out<D, BACK>(w, a, q, k, v, 1, group, transposed, nullptr, nullptr, out, st);
 }
 
 template <int D>
 cudaError_t launch_fwd(const LinearArgs& a, const float* state_in, float* state_out, void* o, void* ws,
                        cudaStream_t st) {
   const Work w = make_work(a, ws);
-  const int group = a.hq / a.hkv;
   cudaError_t e = launch_plan(w, st);
   if (e != cudaSuccess) return e;
-  if (state_out != nullptr)
-    e = launch_states<D, 3>(w, a, a.k, a.v, 1, false, w.slots[0], state_in, state_out, st);
-  else if (a.num_tokens > kWhole * kChunk)   // else no sequence is cut
-    e = launch_states<D, 1>(w, a, a.k, a.v, 1, false, w.slots[0], nullptr, nullptr, st);
+  e = state_out != nullptr ? launch_states<D, 3>(w, a, a.k, a.v, 1, false, state_in, state_out, st)
+                           : launch_states<D, 1>(w, a, a.k, a.v, 1, false, state_in, nullptr, st);
   if (e != cudaSuccess) return e;
-  return launch_forth<D>(w, a, a.q, a.k, a.v, group, w.slots[0], state_in, state_out, o, st);
+  return launch_forth<D>(w, a, a.q, a.k, a.v, a.hq / a.hkv, state_in, state_out, o, st);
 }
 
 template <int D>
@@ -1507,24 +1661,21 @@ cudaError_t launch_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk
   const Work w = make_work(a, ws);
   const int group = a.hq / a.hkv;
   cudaError_t e = launch_plan(w, st);
-  const bool cut = a.num_tokens > kWhole * kChunk;   // else no sequence is
-  if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, w.slots[0], nullptr, nullptr, st);
-  if (e == cudaSuccess)
-    e = launch_forth<D>(w, a, dout, a.v, a.k, group, w.slots[0], nullptr, nullptr, dq, st);
-  if (e == cudaSuccess && cut) e = launch_states<D, 1>(w, a, a.q, dout, group, true, w.slots[1], nullptr, nullptr, st);
-  if (e == cudaSuccess)
-    e = launch_back<D>(w, a, a.v, dout, a.q, group, w.slots[1], true, dk, st);
-  if (e == cudaSuccess) e = launch_back<D>(w, a, a.k, a.q, dout, group, w.slots[1], false, dv, st);
+  if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, nullptr, nullptr, st);
+  if (e == cudaSuccess) e = launch_forth<D>(w, a, dout, a.v, a.k, group, nullptr, nullptr, dq, st);
+  if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.q, dout, group, true, nullptr, nullptr, st);
+  if (e == cudaSuccess) e = launch_back<D>(w, a, a.v, dout, a.q, group, true, dk, st);
+  if (e == cudaSuccess) e = launch_back<D>(w, a, a.k, a.q, dout, group, false, dv, st);
   return e;
 }
 
 }  // namespace
 
-size_t linear_fwd_ws_bytes(int32_t num_segments, int64_t, int32_t, int32_t, int32_t d) {
-  return kWsHeader + ws_off(num_segments) + ws_slots(d);
+size_t linear_fwd_ws_bytes(int32_t num_segments, int64_t num_tokens, int32_t, int32_t hkv, int32_t d) {
+  return ws_bytes(num_segments, num_tokens, hkv, d);
 }
-size_t linear_bwd_ws_bytes(int32_t num_segments, int64_t, int32_t, int32_t, int32_t d) {
-  return kWsHeader + ws_off(num_segments) + 2 * ws_slots(d);
+size_t linear_bwd_ws_bytes(int32_t num_segments, int64_t num_tokens, int32_t, int32_t hkv, int32_t d) {
+  return ws_bytes(num_segments, num_tokens, hkv, d);
 }
 
 cudaError_t launch_linear_fwd(const LinearArgs& a, const float* state_in, float* state_out, void* o, void* ws,
