@@ -706,7 +706,7 @@ struct LinBars {
   uint64_t o_full[2];  // the products of an output are complete
   uint64_t o_free[2];  // and in registers
   uint64_t out_full;   // an output is in its tile, or its rows are written
-  uint64_t out_free;   // and on its way
+  uint64_t out_free[2];  // and on its way, of one warpgroup's or the other's (each waits for the other's, in turn)
   uint64_t k_done[2];  // a K that is to be weighted is no longer read as it was loaded
   uint64_t wt_full[4]; // a pair's V, or K, is weighted; four, as the warps that do it may be some pairs ahead of the issuer
   uint64_t u_full;     // the chunk's K^T V
@@ -801,11 +801,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars->k_done[i], 1);
       mbar_init(&bars->o_full[i], 1);
       mbar_init(&bars->o_free[i], 4);
+      mbar_init(&bars->out_free[i], 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&bars->wt_full[i], 128);
     mbar_init(&bars->s_read, 1);
     mbar_init(&bars->out_full, 128);
-    mbar_init(&bars->out_free, 1);
     mbar_init(&bars->u_free, 4);
     mbar_init(&bars->u_full, 1);
     mbar_init(&bars->s_ready, 128);
@@ -976,7 +976,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (fresh) take(outs);
             }
             if (fast && (per_k || h == 0)) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
-            if (!fast && !weighted) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
+            // (a fast head's last V is not weighted, but its slot is not given back before the warps that do it have passed it)
+            if (fast ? !weigh && (per_k || h == 0) : !weighted) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
             ok = ok && mbar_wait(&bars->p_full[it & 1], (it >> 1) & 1);
             go = __all_sync(0xffffffffu, ok);
             if (!go) break;
@@ -1023,7 +1024,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               bulk_commit();
               bulk_wait_read();
             }
-            mbar_arrive(&bars->out_free);
+            mbar_arrive(&bars->out_free[oi & 1]);
           }
         }
       if (!go) set_abort(&bars->abort, p.c.status);
@@ -1195,7 +1196,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool staged = C::STAGE && rows == kChunk;
             const uint32_t tile = sbase + C::OFF_O + r * 128;
             // the output before has left the tile (and this one's place in the order of out_full)
-            if (C::STAGE && oi > 0 && !mbar_wait_warp(&bars->out_free, (oi - 1) & 1)) {
+            if (C::STAGE && oi > 0 && !mbar_wait_warp(&bars->out_free[(oi - 1) & 1], ((oi - 1) >> 1) & 1)) {
               go = false;
               break;
             }

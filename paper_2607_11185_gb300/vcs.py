@@ -862,9 +862,9 @@ def group_advantage(rewards, group_size: int, eps: float = 1e-6, stream=None):
 
 def _expect_linear(where: str, q, k, v, log_decay):
     bf16 = torch.bfloat16
-    _expect(where, ("q", q, bf16, 3), ("k", k, bf16, 3))
-    kv = (q.shape[0], k.shape[1], q.shape[2])
-    _expect(where, ("k", k, bf16, kv), ("v", v, bf16, kv), ("log_decay", log_decay, torch.float32, (kv[1],)))
+    heads = k.shape[1:2]
+    _expect(where, ("q", q, bf16, 3), ("k", k, bf16, q.shape[:1] + heads + q.shape[2:]), ("v", v, bf16, k.shape),
+            ("log_decay", log_decay, torch.float32, heads))
 
 
 def linear_attn_fwd(q, k, v, log_decay, cu_seqlens, scale: float = 0.0, state=None, with_state: bool = False,
@@ -932,11 +932,11 @@ _LOGITS = {torch.bfloat16: 0, torch.float32: 1}  # VCS_BF16, VCS_F32
 
 def _expect_rows(where: str, name: str, t, dtype, shape):
     """As _expect, but rows may be apart: a [rows, vocab] tensor whose columns are consecutive."""
-    ok = t.dim() == 2 and t.is_cuda and t.get_device() == torch.cuda.current_device() and t.dtype is dtype
-    if not (ok and (shape is None or t.shape == shape)):
-        _refuse(where, name, t, dtype, 2 if shape is None else shape) if t.is_contiguous() else \
-            _refuse(where, name, t.contiguous(), dtype, 2 if shape is None else shape)
-    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    if not (t.is_cuda and t.get_device() == torch.cuda.current_device() and t.dtype is dtype and
+            (t.shape == shape or t.dim() == shape)):
+        _refuse(where, name, t if t.is_contiguous() else t.contiguous(), dtype, shape)
+    if not t.is_contiguous() and ((t.shape[1] > 1 and t.stride(1) != 1) or
+                                  (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
         raise ValueError(f"{where}: the rows of {name} overlap or their columns are not consecutive")
 
 
@@ -951,12 +951,12 @@ def distill_topk(logits, teacher_ids, teacher_logits, weights, teacher_rows=None
     where = "distill_topk"
     if logits.dtype not in _LOGITS:
         raise ValueError(f"{where}: logits is {logits.dtype}, not torch.bfloat16 or torch.float32")
-    _expect_rows(where, "logits", logits, logits.dtype, None)
+    _expect_rows(where, "logits", logits, logits.dtype, 2)
     rows, vocab = logits.shape
-    _expect(where, ("teacher_ids", teacher_ids, torch.int32, 2))
-    lists, top = teacher_ids.shape
-    _expect(where, ("teacher_logits", teacher_logits, torch.float32, (lists, top)),
+    _expect(where, ("teacher_ids", teacher_ids, torch.int32, 2),
+            ("teacher_logits", teacher_logits, torch.float32, teacher_ids.shape),
             ("weights", weights, torch.float32, (rows,)))
+    lists, top = teacher_ids.shape
     if teacher_rows is not None:
         _expect(where, ("teacher_rows", teacher_rows, torch.int32, (rows,)))
     if out is not None:

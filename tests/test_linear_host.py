@@ -163,3 +163,60 @@ def test_every_chunk_is_taken_once_and_cuts_lead_to_the_next_cta():
         if not cut:  # no CTA takes more than its share and one sequence
             share = -(-sum(c1 - c0 for m in work for *_, c0, c1 in m) // max(len(work), 1))
             assert max((sum(c1 - c0 for *_, c0, c1 in m) for m in work), default=0) <= share + WHOLE
+
+
+def parts_of(lens, heads, decays, back):
+    """The documented rule for the states at the cuts: (cuts, parts, size); a cut (t, sequence, chunk e in it, chunks of
+    its own that it needs), its parts' (cut, first chunk, end), the nearest first."""
+    nch = [-(-n // CHUNK) for n in lens]
+    work, cut = pieces(lens, heads, heads * (sum(lens) // CHUNK + len(lens)))
+    keep = [int(min(150 / max(-g * 1.4426950408889634 * CHUNK, 1e-30), 2.0 ** 30)) + 2 for g in decays]
+    cuts = []
+    for t, mine in enumerate(work):
+        if cut and mine and mine[-1][3] < nch[mine[-1][0]]:
+            seg, head, c0, e = mine[-1]
+            nxt = work[t + 1][0]
+            cuts.append((t, (seg, head), e, min(keep[head], nxt[3] - nxt[2] if back else e - c0)))
+    need = np.array([c[3] for c in cuts] or [0])
+    sizes = []
+    for waves in (1, 2, 3):
+        s = 4
+        while (-(-need // s)).sum() > waves * len(work):
+            s += 1
+        sizes.append(s)
+    size = min(sizes, key=lambda s: (sizes.index(s) + 1) * (s + 3))
+    parts = []
+    for t, _, e, n in cuts:
+        for j in range(-(-n // size)):
+            near, away = j * size, min((j + 1) * size, n)
+            parts.append((t, e + near, e + away) if back else (t, e - away, e - near))
+    assert len(parts) <= 3 * len(work)
+    return cuts, parts, size
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_the_parts_hold_what_every_cut_needs_once(back):
+    rng = np.random.default_rng(1)
+    for _ in range(60):
+        heads = int(rng.integers(1, 9))
+        lens = [int(x) for x in rng.integers(0, int(rng.choice([300, 3000, 40_000])), size=int(rng.integers(1, 20)))]
+        lens[0] = int(rng.integers(2100, 200_000))
+        decays = [-float(10 ** rng.uniform(-6, 1)) if rng.random() < 0.8 else 0.0 for _ in range(heads)]
+        cuts, parts, size = parts_of(lens, heads, decays, back)
+        assert cuts
+        by = {t: [(a, b) for u, a, b in parts if u == t] for t, *_ in cuts}
+        for t, (seg, head), e, _ in cuts:
+            nch = -(-lens[seg] // CHUNK)
+            want, at, faded = (nch if back else 0), e, False
+            for u, seq, eu, n in (cuts if back else cuts[::-1]):
+                if seq != (seg, head) or (u < t if back else u > t) or faded:
+                    continue
+                for a, b in by[u]:
+                    near = a - e if back else e - b
+                    assert near == abs(at - e)                          # the next chunks, nothing twice
+                    if -decays[head] * 1.4426950408889634 * CHUNK * near > 150:
+                        faded = True
+                        break
+                    at = b if back else a
+                faded = faded or -decays[head] * 1.4426950408889634 * CHUNK * abs(at - e) > 150
+            assert at == want or faded                                  # all there is, or all that is not 0
