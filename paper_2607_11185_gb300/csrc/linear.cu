@@ -1421,6 +1421,593 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+// ------------------------------------------------------------------ gradients of keys and values
+struct BackArgs {
+  Common c;
+  const float* starts;     // the states at the cuts
+  int32_t group;
+  float scale;
+  bool wide;               // dk and dv are 32-byte aligned
+  bf16 *dk, *dv;
+};
+
+template <int D>
+struct Bck {
+  static constexpr int TILE = kChunk * D * 2;
+  static constexpr int NKV = D == 64 ? 2 : 1;    // tiles of a chunk's K and V
+  static constexpr int NQ = D == 64 ? 4 : 2;     // of an item's Q and dO
+  // Queries of a step: at D = 128 TMEM has room for two products of 64 queries beside dK, dV and Q^T dO.
+  static constexpr int QN = D == 64 ? 128 : 64, NS = kChunk / QN;
+  static constexpr int OFF_K = 0, OFF_V = NKV * TILE, OFF_Q = 2 * NKV * TILE, OFF_D = OFF_Q + NQ * TILE;
+  static constexpr int OFF_S = OFF_D + NQ * TILE;        // the state, a row a dim of q
+  static constexpr int OFF_TAB = OFF_S + D * D * 2;      // 32 powers of the decay for each warp that makes P
+  static constexpr int OFF_BAR = OFF_TAB + 8 * 128;
+  static constexpr int SMEM = OFF_BAR + 512;
+  static constexpr int TM_O = 2 * QN, TM_U = TM_O + 2 * D;   // dV, dK; before them K Q^T, V dO^T
+  static constexpr uint32_t IDESC_S = idesc_bf16(128, QN, 0, 0);   // K (K-major) x Q^T (K-major), V x dO^T
+  static constexpr uint32_t IDESC_V = idesc_bf16(128, D, 0, 1);    // K (K-major) x S (MN-major), P (TMEM) x dO or Q
+  static constexpr uint32_t IDESC_K = idesc_bf16(128, D, 0, 0);    // V (K-major) x S^T (K-major)
+  static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);    // Q^T (MN-major) x dO (MN-major); see Lin for M
+  static constexpr int REG_CTRL = 80, REG_ROWS = 104, REG_STATE = 224;
+  static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
+  static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
+};
+
+struct BckBars {
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t q_full[4], q_empty[4];   // an item's Q and dO
+  uint64_t wt_full[4];              // and Q is weighted, rows behind the segment's end are cleared in both
+  uint64_t k_done, wt2;             // of a head that forgets fast: Q has been read as it was loaded; it is weighted
+  uint64_t s_full[2], p_full[2];    // of a step: K Q^T and V dO^T, their P in TMEM
+  uint64_t a_full;                  // the products with the state, for the warps that scale their rows
+  uint64_t o_full, o_free;          // a chunk's dV and dK are complete, and in registers
+  uint64_t u_full, u_free;          // the chunk's Q^T dO, and in registers
+  uint64_t s_ready, s_read;         // the state that the chunk's keys read is in shared memory, and has been read
+  uint32_t tmem_base;
+  int32_t abort;
+};
+static_assert(sizeof(BckBars) <= 512, "barrier space");
+
+// dK and dV of a chunk together, from the last chunk to the first: with m = 64 and w_i = lam^(i-m) q_i, weighted in place
+// as soon as it is loaded,
+//   dv_j = scale lam^(m-j) [ k_j (lam^(n-m) R) + sum_{i >= j} (k_j . w_i) do_i ]
+//   dk_j = scale lam^(m-j) [ v_j (lam^(n-m) R)^T + sum_{i >= j} (v_j . do_i) w_i ]
+//   R'   = lam^n R + lam^m sum_i w_i do_i^T
+// with one load of q and do and one state for both.  (A pass each loads them twice and has six products an item, not five:
+// 40 / 8 heads of 128, 135,512 tokens, ... .)  Both factors are at most 2^64 (kSlow); for a head that forgets faster both P have
+// the exact powers, the rows of the products with R are scaled in TMEM, and Q is weighted when they have read it.
+//
+// An item is a chunk with one query head; a step an item's QN queries.  In a step: P dO;  K Q^T of the next step, so that its P
+// is made meanwhile;  P Q;  V dO^T of the next step;  Q^T dO.  The products with R come in a chunk's second item (of one,
+// the first): R has had an item's time.
+//   warp 0  loads Q and dO;  warp 2  K and V;  warp 1  TMEM and every MMA
+//   warps 4-7    P of K Q^T, dV;  warps 8-11  P of V dO^T, dK  (a thread a key)
+//   warps 12-15  weighted Q, and the state in registers (a thread a row), its bf16 copy in shared memory
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    linear_back(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do,
+                const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                const __grid_constant__ BackArgs p) {
+  using C = Bck<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  BckBars* bars = reinterpret_cast<BckBars*>(smem + C::OFF_BAR);
+  Walk w(p.c, blockIdx.x);
+  if (w.g >= w.hi) return;
+  if (*reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT) return;
+  if (smem_u32(smem) & 1023u) {
+    if (threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = p.group;
+  const uint32_t sbase = smem_u32(smem);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::NKV; ++i) {
+      mbar_init(&bars->k_full[i], 1);
+      mbar_init(&bars->k_empty[i], 1);
+      mbar_init(&bars->v_full[i], 1);
+      mbar_init(&bars->v_empty[i], 1);
+    }
+    for (int i = 0; i < C::NQ; ++i) {
+      mbar_init(&bars->q_full[i], 1);
+      mbar_init(&bars->q_empty[i], 1);
+      mbar_init(&bars->wt_full[i], 128);
+    }
+    mbar_init(&bars->k_done, 1);
+    mbar_init(&bars->wt2, 128);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->s_full[i], 1);
+      mbar_init(&bars->p_full[i], 128);
+    }
+    mbar_init(&bars->a_full, 1);
+    mbar_init(&bars->o_full, 1);
+    mbar_init(&bars->o_free, 8);
+    mbar_init(&bars->u_full, 1);
+    mbar_init(&bars->u_free, 4);
+    mbar_init(&bars->s_ready, 128);
+    mbar_init(&bars->s_read, 1);
+    bars->abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
+
+  if (warp < 4) {
+    setmaxnreg_dec<C::REG_CTRL>();
+    if (warp == 0 && lane == 0) {
+      // -------------------------------------------------------- loads of Q and dO
+      bool go = true;
+      uint32_t it = 0;
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
+          const int tok = w.start + (w.c1 - 1 - n) * kChunk;
+          for (int h = 0; h < group; ++h, ++it) {
+            const uint32_t slot = it % C::NQ;
+            if ((it >= C::NQ && !mbar_wait(&bars->q_empty[slot], (it / C::NQ - 1) & 1)) || gave_up()) {
+              go = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&bars->q_full[slot], 2 * C::TILE);
+#pragma unroll
+            for (int kb = 0; kb < D / 64; ++kb) {
+              uint8_t* dst = smem + slot * C::TILE + kb * 16384;
+              tma_load_3d(dst + C::OFF_Q, &tm_q, &bars->q_full[slot], kb * 64, w.head * group + h, tok);
+              tma_load_3d(dst + C::OFF_D, &tm_do, &bars->q_full[slot], kb * 64, w.head * group + h, tok);
+            }
+          }
+        }
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else if (warp == 2 && lane == 0) {
+      // -------------------------------------------------------- loads of K and V
+      bool go = true;
+      uint32_t ck = 0;
+      while (go && w.next())
+        for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ck) {
+          const int tok = w.start + (w.c1 - 1 - n) * kChunk;
+          const uint32_t slot = ck % C::NKV;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            uint64_t *full = x ? bars->v_full : bars->k_full, *empty = x ? bars->v_empty : bars->k_empty;
+            if ((ck >= C::NKV && !mbar_wait(&empty[slot], (ck / C::NKV - 1) & 1)) || gave_up()) {
+              go = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&full[slot], C::TILE);
+#pragma unroll
+            for (int kb = 0; kb < D / 64; ++kb)
+              tma_load_3d(smem + (x ? C::OFF_V : C::OFF_K) + slot * C::TILE + kb * 16384, x ? &tm_v : &tm_k, &full[slot],
+                          kb * 64, w.head, tok);
+          }
+        }
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else if (warp == 1) {
+      // -------------------------------------------------------- MMA issuer (see linear_out)
+      const uint64_t kd = smem_desc(sbase + C::OFF_K, 16, 1024), qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
+      const uint64_t qt = smem_desc(sbase + C::OFF_Q, 16384, 1024);
+      const uint64_t sm = smem_desc(sbase + C::OFF_S, D * 128, 1024), sk = smem_desc(sbase + C::OFF_S, 16, 1024);
+      bool ok = true, go = true, more = w.next();
+      // The step whose K Q^T and V dO^T come next: its item and chunk, and whether it is its item's first or last.
+      uint32_t nit = 0, nck = 0;
+      int ns = 0, nh = 0;
+      bool nfast = w.l2 < kSlow;
+      auto issue_s = [&](int x) {   // K Q^T (0) or V dO^T (1)
+        if (x == 0 && ns == 0) {
+          ok = ok && mbar_wait(&bars->wt_full[nit % C::NQ], (nit / C::NQ) & 1);
+          if (nfast) ok = ok && mbar_wait(&bars->q_full[nit % C::NQ], (nit / C::NQ) & 1);
+        }
+        if (ns == 0 && nh == 0)
+          ok = ok && mbar_wait(&(x ? bars->v_full : bars->k_full)[nck % C::NKV], (nck / C::NKV) & 1);
+        tc_fence_after();
+        if (elect_one() && ok) {
+          const uint64_t a = desc_at(kd, (x ? C::OFF_V : 0) + nck % C::NKV * C::TILE);
+          const uint64_t b = desc_at(qd, (x ? C::NQ * C::TILE : 0) + nit % C::NQ * C::TILE + ns * C::QN * 128);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
+            tc_mma_ss(tmem + x * C::QN, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
+          }
+          tc_commit(&bars->s_full[x]);
+          if (C::NKV == 1 && ns == C::NS - 1 && nh == group - 1) tc_commit(&(x ? bars->v_empty : bars->k_empty)[0]);
+        }
+        __syncwarp();
+      };
+      if (more) {
+        issue_s(0);
+        issue_s(1);
+      }
+      uint32_t t = 0, it = 0, ck = 0, us = 0, fasts = 0;   // steps, items, chunks, Q^T dO (also of fast heads' items)
+      while (go && more) {
+        const int chunks = w.c1 - w.c0;
+        const bool fast = w.l2 < kSlow;
+        const int hr = fast || group == 1 ? 0 : 1;   // the item that the products with R come in
+        for (int n = 0; go && n < chunks; ++n) {
+          const bool weigh = n < chunks - 1;
+          for (int h = 0; go && h < group; ++h)
+            for (int s = 0; s < C::NS; ++s) {
+              const bool first = h == 0 && s == 0, item = s == C::NS - 1, end = item && h == group - 1;
+              const bool late = item && (fast || (end && C::NKV == 1));
+              const uint32_t q = it % C::NQ, kv = ck % C::NKV;
+              if (first && ck > 0) ok = ok && mbar_wait(&bars->o_free, (ck - 1) & 1);
+              if (h == hr && s == 0) {
+                ok = ok && mbar_wait(&bars->s_ready, ck & 1);
+                tc_fence_after();
+                if (elect_one() && ok) {
+                  const uint64_t a = desc_at(kd, kv * C::TILE), b = desc_at(a, C::OFF_V);
+#pragma unroll
+                  for (int kk = 0; kk < D / 16; ++kk)
+                    tc_mma_ss(tmem + C::TM_O, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sm, kk * 2048),
+                              C::IDESC_V, kk > 0 || !first);
+#pragma unroll
+                  for (int kk = 0; kk < D / 16; ++kk)
+                    tc_mma_ss(tmem + C::TM_O + D, desc_at(b, (kk >> 2) * 16384 + (kk & 3) * 32),
+                              desc_at(sk, (kk >> 2) * (D * 128) + (kk & 3) * 32), C::IDESC_K, kk > 0 || !first);
+                  if (fast) tc_commit(&bars->a_full);
+                  tc_commit(&bars->s_read);
+                }
+                __syncwarp();
+              }
+              // the step behind this one
+              bool next = true;
+              ns = s + 1;
+              if (item) {
+                ns = 0;
+                ++nit;
+                nh = h + 1;
+                if (end) {
+                  nh = 0;
+                  ++nck;
+                  if (!weigh) next = more = w.next();
+                  nfast = w.l2 < kSlow;
+                }
+              }
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {   // dV += P dO, dK += P Q
+                ok = ok && mbar_wait(&bars->p_full[x], t & 1);
+                go = __all_sync(0xffffffffu, ok);
+                if (!go) break;
+                tc_fence_after();
+                if (elect_one()) {
+                  const uint64_t b = desc_at(qt, (x ? 0 : C::NQ * C::TILE) + q * C::TILE + s * C::QN * 128);
+#pragma unroll
+                  for (int kk = 0; kk < C::QN / 16; ++kk)
+                    tc_mma_ts(tmem + C::TM_O + x * D, tmem + x * C::QN + kk * 8, desc_at(b, kk * 2048), C::IDESC_V,
+                              kk > 0 || !(first && hr > 0));
+                }
+                __syncwarp();
+                if (next && !late) issue_s(x);
+              }
+              if (!go) break;
+              auto issue_u = [&](int from, int to, bool fresh) {
+                const uint64_t a = desc_at(qt, q * C::TILE), b = desc_at(a, C::NQ * C::TILE);
+#pragma unroll
+                for (int kk = 0; kk < to - from; ++kk)
+                  tc_mma_ss(tmem + C::TM_U, desc_at(a, (from + kk) * 2048), desc_at(b, (from + kk) * 2048), C::IDESC_U,
+                            kk > 0 || !fresh);
+              };
+              if (weigh && !fast) {
+                if (first && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
+                tc_fence_after();
+                if (elect_one() && ok) issue_u(s * (C::QN / 16), (s + 1) * (C::QN / 16), first);
+              } else if (weigh && item) {
+                if (elect_one() && ok) tc_commit(&bars->k_done);
+                __syncwarp();
+                if (h == 0 && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
+                ok = ok && mbar_wait(&bars->wt2, fasts++ & 1);
+                tc_fence_after();
+                if (elect_one() && ok) issue_u(0, 8, h == 0);
+              }
+              __syncwarp();
+              if (elect_one() && ok) {
+                if (weigh && end) tc_commit(&bars->u_full);
+                if (item) tc_commit(&bars->q_empty[q]);
+                if (end) tc_commit(&bars->o_full);
+                if (end && C::NKV > 1) {
+                  tc_commit(&bars->k_empty[kv]);
+                  tc_commit(&bars->v_empty[kv]);
+                }
+              }
+              __syncwarp();
+              if (next && late) {
+                issue_s(0);
+                issue_s(1);
+              }
+              ++t;
+              if (item) ++it;
+              if (end) ++ck;
+            }
+        }
+      }
+      go = __all_sync(0xffffffffu, ok);
+      if (!go) set_abort(&bars->abort, p.c.status);
+    }
+  } else if (warp < 12) {
+    // ---------------------------------------------------------- P, dV and dK
+    setmaxnreg_dec<C::REG_ROWS>();
+    const int x = warp < 8 ? 0 : 1;
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16), tp = trow + x * C::QN, tb = trow + C::TM_O + x * D;
+    bf16* out = x ? p.dk : p.dv;
+    float* tab = reinterpret_cast<float*>(smem + C::OFF_TAB) + (warp - 4) * 32;
+    const uint32_t tab_at = smem_u32(tab);
+    bool go = true;
+    uint32_t t = 0, ck = 0, fasts = 0;
+    while (go && w.next()) {
+      const bool fast = w.l2 < kSlow;
+      __syncwarp();
+      tab[lane] = exp2f(w.l2 * (float)lane);
+      __syncwarp();
+      const uint64_t slope = f2pack(-w.l2, -w.l2);
+      for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ck) {
+        const int c = w.c1 - 1 - n, rows = w.rows(c);
+        const float f_out = fast ? p.scale : p.scale * exp2f(w.l2 * (float)(kMiddle - r));
+        if (fast) {   // the rows of the product with R
+          if (!mbar_wait_warp(&bars->a_full, fasts++ & 1)) {
+            go = false;
+            break;
+          }
+          tc_fence_after();
+          const float f = exp2f(w.l2 * (float)max(rows - r, 0));
+          const uint64_t f2 = f2pack(f, f);
+#pragma unroll 1
+          for (int g = 0; g < D / 32; ++g) {
+            uint32_t s[32];
+            tmem_ld_32x32b_x32(tb + g * 32, s);
+            tmem_ld_wait();
+            reg_fence<32>(s);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float x0, x1;
+              f2unpack(fmul2(f2pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), f2), x0, x1);
+              s[i] = __float_as_uint(x0);
+              s[i + 1] = __float_as_uint(x1);
+            }
+            tmem_st_32x32b_x32(tb + g * 32, s);
+          }
+        }
+        for (int st = 0; go && st < group * C::NS; ++st, ++t) {
+          if (!mbar_wait_warp(&bars->s_full[x], t & 1) || __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          tc_fence_after();
+          // P goes over columns that have been read.  Loops are not unrolled: see linear_out.
+#pragma unroll 1
+          for (int g = 0; g < C::QN / 32; ++g) {
+            const int q0 = (st % C::NS) * C::QN + g * 32;   // the group's first query
+            uint32_t s[32];
+            if (q0 + 31 < quad * 32 || q0 >= rows) {   // nothing seen
+#pragma unroll
+              for (int i = 0; i < 16; ++i) s[i] = 0u;
+            } else {
+              tmem_ld_32x32b_x32(tp + g * 32, s);
+              uint32_t seen = 0xffffffffu;   // queries of the group that the key is seen by, a bit each
+              if (q0 == quad * 32) seen = 0xffffffffu << lane;
+              if (rows - q0 < 32) seen &= (1u << (rows - q0)) - 1u;
+              const bool all = q0 > quad * 32 && rows - q0 >= 32;
+              tmem_ld_wait();
+              reg_fence<32>(s);
+              if (!fast) {
+                if (!all) {
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (!(seen >> i & 1)) s[i] = 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                  s[i] = pack_bf16(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+              } else if (!all) {   // lam^(query - key): powers of the exact distances (see linear_out)
+                const float gap = (float)(r - q0);
+                const uint64_t at = f2pack(gap, gap);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  float e0, e1, x0, x1;
+                  f2unpack(fmul2(slope, fadd2(at, f2pack(-2.f * i, -2.f * i - 1.f))), e0, e1);
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                 f2pack(ex2(e0), ex2(e1))),
+                           x0, x1);
+                  s[i] = pack_bf16(seen >> (2 * i) & 1 ? x0 : 0.f, seen >> (2 * i + 1) & 1 ? x1 : 0.f);
+                }
+              } else {
+                const float rf = ex2(w.l2 * (float)(q0 - r));
+                const uint64_t rf2 = f2pack(rf, rf);
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                  const uint4 f = ld_shared_v4(tab_at + i * 8);
+                  float x0, x1;
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])),
+                                 fmul2(rf2, f2pack(__uint_as_float(f.x), __uint_as_float(f.y)))),
+                           x0, x1);
+                  s[i] = pack_bf16(x0, x1);
+                  f2unpack(fmul2(f2pack(__uint_as_float(s[2 * i + 2]), __uint_as_float(s[2 * i + 3])),
+                                 fmul2(rf2, f2pack(__uint_as_float(f.z), __uint_as_float(f.w)))),
+                           x0, x1);
+                  s[i + 1] = pack_bf16(x0, x1);
+                }
+              }
+            }
+            tmem_st_32x32b_x16(tp + g * 16, *reinterpret_cast<uint32_t(*)[16]>(&s[0]));
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&bars->p_full[x]);
+        }
+        if (!go || !mbar_wait_warp(&bars->o_full, ck & 1)) {
+          go = false;
+          break;
+        }
+        tc_fence_after();
+        bf16* row = out + ((size_t)(w.start + c * kChunk + r) * p.c.heads + w.head) * D;
+        const uint64_t f2 = f2pack(f_out, f_out);
+#pragma unroll 1
+        for (int g = 0; g < D / 32; ++g) {
+          uint32_t b[32];
+          tmem_ld_32x32b_x32(tb + g * 32, b);
+          tmem_ld_wait();
+          reg_fence<32>(b);
+          if (g == D / 32 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->o_free);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float x0, x1;
+            f2unpack(fmul2(f2, f2pack(__uint_as_float(b[2 * i]), __uint_as_float(b[2 * i + 1]))), x0, x1);
+            b[i] = pack_bf16(x0, x1);
+          }
+          if (r < rows) {
+            st_global_32(row + g * 32, *reinterpret_cast<const uint32_t(*)[8]>(&b[0]), p.wide);
+            st_global_32(row + g * 32 + 16, *reinterpret_cast<const uint32_t(*)[8]>(&b[8]), p.wide);
+          }
+        }
+      }
+    }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  } else {
+    // ---------------------------------------------------------- weighted Q, state
+    setmaxnreg_inc<C::REG_STATE>();
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quad * 32) << 16);
+    const bool mine = D == 128 || quad < 2;   // a row of the state
+    bool go = true;
+    uint32_t it = 0, ck = 0, fasts = 0, sums = 0;
+    while (go && w.next()) {
+      const int chunks = w.c1 - w.c0;
+      const bool fast = w.l2 < kSlow;
+      float s[D];
+      if (mine) {
+        const float* src = p.starts + ((size_t)blockIdx.x * D + r) * D;
+#pragma unroll
+        for (int i = 0; i < D; i += 4) {
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (w.c1 < w.nch) x = *reinterpret_cast<const float4*>(src + i);
+          s[i] = x.x;
+          s[i + 1] = x.y;
+          s[i + 2] = x.z;
+          s[i + 3] = x.w;
+          if (i % 32 == 28) asm volatile("" ::: "memory");   // not all loads ahead: the registers are the state's
+        }
+      }
+      const int64_t items = (int64_t)chunks * group;
+      int64_t done = 0;
+      for (int n = 0; go && n < chunks; ++n, ++ck) {
+        if (ck > 0 && !mbar_wait_warp(&bars->s_read, (ck - 1) & 1)) {
+          go = false;
+          break;
+        }
+        if (mine) {
+          const float f = fast ? 1.f : exp2f(w.l2 * (float)(w.rows(w.c1 - 1 - n) - kMiddle));
+          const uint64_t f2 = f2pack(f, f);
+          const uint32_t dst = sbase + C::OFF_S + r * 128;
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i) {
+            uint32_t y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float a, b;
+              f2unpack(fmul2(f2, f2pack(s[8 * i + 2 * j], s[8 * i + 2 * j + 1])), a, b);
+              y[j] = pack_bf16(a, b);
+            }
+            st_shared_v4(dst + (i >> 3) * (D * 128) + (((i & 7) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(&bars->s_ready);
+        // Items up to this chunk's and, as K Q^T runs a step ahead, the next one's first (which for a fast head waits).
+        int64_t target = (int64_t)(n + 1) * group + (fast ? 0 : 1);
+        if (target > items) target = items;
+        for (; done < target; ++done, ++it) {
+          const int m = (int)(done / group), rows = w.rows(w.c1 - 1 - m);
+          const uint32_t slot = it % C::NQ, tile = sbase + C::OFF_Q + slot * C::TILE;
+          if (!mbar_wait_warp(&bars->q_full[slot], (it / C::NQ) & 1) || __any_sync(0xffffffffu, gave_up())) {
+            go = false;
+            break;
+          }
+          if (r >= rows) {   // rows of the next segment, which may hold anything
+            zero_row<D>(tile, r);
+            zero_row<D>(tile + C::NQ * C::TILE, r);
+          }
+          if (fast) {
+            fence_proxy_async_smem();
+            mbar_arrive(&bars->wt_full[slot]);
+            if (m == chunks - 1) continue;   // no state comes behind the last chunk
+            if (!mbar_wait_warp(&bars->k_done, fasts++ & 1)) {
+              go = false;
+              break;
+            }
+          }
+          const float wt = exp2f(w.l2 * (float)(fast ? r : r - kMiddle));
+          const uint64_t wt2 = f2pack(wt, wt);
+          if (r < rows) {
+#pragma unroll 1
+            for (int kb = 0; kb < D / 32; ++kb) {   // four loads under way
+              uint4 x[4];
+              const uint32_t row = tile + (kb >> 1) * 16384 + r * 128;
+              const int u0 = (kb & 1) * 4 + r;
+#pragma unroll
+              for (int u = 0; u < 4; ++u) x[u] = ld_shared_v4(row + (((u0 + u) & 7) << 4));
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint32_t in[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+                uint32_t y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  float a, b;
+                  f2unpack(fmul2(f2pack(lo_f(in[i]), hi_f(in[i])), wt2), a, b);
+                  y[i] = pack_bf16(a, b);
+                }
+                st_shared_v4(row + (((u0 + u) & 7) << 4), y[0], y[1], y[2], y[3]);
+              }
+            }
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(fast ? &bars->wt2 : &bars->wt_full[slot]);
+        }
+        if (!go || n == chunks - 1) continue;
+        if (!mbar_wait_warp(&bars->u_full, sums++ & 1)) {
+          go = false;
+          break;
+        }
+        tc_fence_after();
+        if (mine) {
+          const float f = exp2f(w.l2 * (float)w.rows(w.c1 - 1 - n));
+          const float fu = fast ? 1.f : exp2f(w.l2 * (float)kMiddle);
+          const uint64_t f2 = f2pack(f, f), fu2 = f2pack(fu, fu);
+#pragma unroll
+          for (int g = 0; g < D / 16; ++g) {
+            uint32_t u[16];
+            tmem_ld_32x32b_x16(trow + C::TM_U + g * 16, u);
+            tmem_ld_wait();
+            reg_fence<16>(u);
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+              f2unpack(ffma2(f2, f2pack(s[g * 16 + i], s[g * 16 + i + 1]),
+                             fmul2(fu2, f2pack(__uint_as_float(u[i]), __uint_as_float(u[i + 1])))),
+                       s[g * 16 + i], s[g * 16 + i + 1]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->u_free);
+      }
+    }
+    if (!go) set_abort(&bars->abort, p.c.status);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
 // ------------------------------------------------------------------ single tokens
 // A block takes COLS columns of one head's state: a row's lanes hold four columns each, and a thread R rows, all loaded
 // before the first is used.  The state is read and written once: what bounds it is memory.
@@ -1638,10 +2225,30 @@ cudaError_t launch_forth(const Work& w, const LinearArgs& a, const void* q, cons
 }
 
 template <int D>
-cudaError_t launch_back(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
-                        bool transposed, void* out, cudaStream_t st) {
-  return group == 1 ? launch_out<D, BACK1>(w, a, q, k, v, 1, 1, transposed, nullptr, nullptr, out, st)
-                    : launch_out<D, BACK>(w, a, q, k, v, 1, group, transposed, nullptr, nullptr, out, st);
+cudaError_t launch_back(const Work& w, const LinearArgs& a, const void* dout, void* dk, void* dv, int group,
+                        cudaStream_t st) {
+  using C = Bck<D>;
+  alignas(64) CUtensorMap tq, td, tk, tv;
+  if (!encode(&tq, a.q, D, a.hq, a) || !encode(&td, dout, D, a.hq, a) || !encode(&tk, a.k, D, a.hkv, a) ||
+      !encode(&tv, a.v, D, a.hkv, a))
+    return cudaErrorInvalidValue;
+  const void* fn = reinterpret_cast<const void*>(linear_back<D>);
+  static std::atomic<int> regs_cache{-1};
+  bool regs_ok = false;
+  if (cudaError_t e = launch_regs_match(fn, kRegLaunch, &regs_cache, &regs_ok); e != cudaSuccess) return e;
+  if (!regs_ok) return cudaErrorInvalidConfiguration;
+  cudaError_t e = cudaFuncSetAttribute(linear_back<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e != cudaSuccess) return e;
+  BackArgs p;
+  p.c = w.c;
+  p.starts = w.starts;
+  p.group = group;
+  p.scale = a.scale;
+  p.wide = ((reinterpret_cast<uintptr_t>(dk) | reinterpret_cast<uintptr_t>(dv)) & 31u) == 0;
+  p.dk = static_cast<bf16*>(dk);
+  p.dv = static_cast<bf16*>(dv);
+  linear_back<D><<<w.grid, kThreads, C::SMEM, st>>>(tq, td, tk, tv, p);
+  return cudaGetLastError();
 }
 
 template <int D>
@@ -1665,8 +2272,7 @@ cudaError_t launch_bwd(const LinearArgs& a, const void* dout, void* dq, void* dk
   if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.v, a.k, 1, false, nullptr, nullptr, st);
   if (e == cudaSuccess) e = launch_forth<D>(w, a, dout, a.v, a.k, group, nullptr, nullptr, dq, st);
   if (e == cudaSuccess) e = launch_states<D, 1>(w, a, a.q, dout, group, true, nullptr, nullptr, st);
-  if (e == cudaSuccess) e = launch_back<D>(w, a, a.v, dout, a.q, group, true, dk, st);
-  if (e == cudaSuccess) e = launch_back<D>(w, a, a.k, a.q, dout, group, false, dv, st);
+  if (e == cudaSuccess) e = launch_back<D>(w, a, dout, dk, dv, group, st);
   return e;
 }
 
