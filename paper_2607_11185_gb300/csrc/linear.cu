@@ -956,9 +956,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool out = !per_k || h == group - 1, end = h == group - 1;
             const uint32_t ks = 2 * ki % C::NT, vs = (2 * ki + 1) % C::NT;
             auto ahead = [&] {   // Q K^T of the next item
-              if (!end) issue_s(h + 1, n);
-              else if (weigh) issue_s(0, n + 1);
-              else if ((more = w.next())) issue_s(0, 0);
+              if (end && !weigh) more = w.next();
+              if (more) issue_s(end ? 0 : h + 1, !end ? n : weigh ? n + 1 : 0);
             };
             // (a group of key heads at D = 128 has one Q tile, whose next load a chunk's last item would wait for)
             const bool late = C::NP == 1 || (C::NQ == 1 && end);
@@ -1454,13 +1453,14 @@ struct Bck {
 };
 
 struct BckBars {
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t k_full[2][2], k_empty[2][2];   // K and V
   uint64_t q_full[4], q_empty[4];   // an item's Q and dO
   uint64_t wt_full[4];              // and Q is weighted, rows behind the segment's end are cleared in both
-  uint64_t k_done, wt2;             // of a head that forgets fast: Q has been read as it was loaded; it is weighted
-  uint64_t s_full[2], p_full[2];    // of a step: K Q^T and V dO^T, their P in TMEM
-  uint64_t a_full;                  // the products with the state, for the warps that scale their rows
-  uint64_t o_full, o_free;          // a chunk's dV and dK are complete, and in registers
+  uint64_t k_done, wt2[4];          // of a head that forgets fast: Q has been read as it was loaded; it is weighted
+  // Of dV's products and of dK's:
+  uint64_t s_full[2], p_full[2];    // of a step: K Q^T, V dO^T, and its P in TMEM
+  uint64_t a_full[2];               // the product with the state, for the warps that scale its rows
+  uint64_t o_full[2], o_free[2];    // a chunk's sum is complete, and in registers
   uint64_t u_full, u_free;          // the chunk's Q^T dO, and in registers
   uint64_t s_ready, s_read;         // the state that the chunk's keys read is in shared memory, and has been read
   uint32_t tmem_base;
@@ -1477,10 +1477,11 @@ static_assert(sizeof(BckBars) <= 512, "barrier space");
 // 40 / 8 heads of 128, 135,512 tokens, ... .)  Both factors are at most 2^64 (kSlow); for a head that forgets faster both P have
 // the exact powers, the rows of the products with R are scaled in TMEM, and Q is weighted when they have read it.
 //
-// An item is a chunk with one query head; a step an item's QN queries.  In a step: P dO;  K Q^T of the next step, so that its P
-// is made meanwhile;  P Q;  V dO^T of the next step;  Q^T dO.  The products with R come in a chunk's second item (of one,
-// the first): R has had an item's time.
-//   warp 0  loads Q and dO;  warp 2  K and V;  warp 1  TMEM and every MMA
+// An item is a chunk with one query head; a step an item's QN queries.  Three warps issue MMAs, each its own chain and in
+// order: dV's  P dO, K Q^T of the next step;  dK's  P Q, V dO^T of the next step;  the state's  Q^T dO of an item.  A chunk's
+// products with R come in its second item (of one, the first): R has had an item's time.  (One warp for all is held up by
+// its waits and commits: 1,940 us of dK and dV at 40 / 8 heads of 128 and 135,512 tokens, ....)
+//   warp 0  loads;  warps 1, 3  MMAs of dV and of dK;  warp 2  TMEM, MMAs of the state
 //   warps 4-7    P of K Q^T, dV;  warps 8-11  P of V dO^T, dK  (a thread a key)
 //   warps 12-15  weighted Q, and the state in registers (a thread a row), its bf16 copy in shared memory
 template <int D>
@@ -1501,34 +1502,32 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = p.group;
   const uint32_t sbase = smem_u32(smem);
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C::NKV; ++i) {
-      mbar_init(&bars->k_full[i], 1);
-      mbar_init(&bars->k_empty[i], 1);
-      mbar_init(&bars->v_full[i], 1);
-      mbar_init(&bars->v_empty[i], 1);
-    }
-    for (int i = 0; i < C::NQ; ++i) {
-      mbar_init(&bars->q_full[i], 1);
-      mbar_init(&bars->q_empty[i], 1);
-      mbar_init(&bars->wt_full[i], 128);
-    }
-    mbar_init(&bars->k_done, 1);
-    mbar_init(&bars->wt2, 128);
     for (int i = 0; i < 2; ++i) {
+      for (int j = 0; j < 2; ++j) {
+        mbar_init(&bars->k_full[i][j], 1);
+        mbar_init(&bars->k_empty[i][j], 1);
+      }
       mbar_init(&bars->s_full[i], 1);
       mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->a_full[i], 1);
+      mbar_init(&bars->o_full[i], 1);
+      mbar_init(&bars->o_free[i], 4);
     }
-    mbar_init(&bars->a_full, 1);
-    mbar_init(&bars->o_full, 1);
-    mbar_init(&bars->o_free, 8);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&bars->q_full[i], 1);
+      mbar_init(&bars->q_empty[i], 3);
+      mbar_init(&bars->wt_full[i], 128);
+      mbar_init(&bars->wt2[i], 128);
+    }
+    mbar_init(&bars->k_done, 2);
     mbar_init(&bars->u_full, 1);
     mbar_init(&bars->u_free, 4);
     mbar_init(&bars->s_ready, 128);
-    mbar_init(&bars->s_read, 1);
+    mbar_init(&bars->s_read, 2);
     bars->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 1) {
+  if (warp == 2) {
     tmem_alloc(&bars->tmem_base, 512);
     tmem_relinquish();
   }
@@ -1540,186 +1539,164 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp < 4) {
     setmaxnreg_dec<C::REG_CTRL>();
-    if (warp == 0 && lane == 0) {
-      // -------------------------------------------------------- loads of Q and dO
-      bool go = true;
-      uint32_t it = 0;
-      while (go && w.next())
-        for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int tok = w.start + (w.c1 - 1 - n) * kChunk;
-          for (int h = 0; h < group; ++h, ++it) {
-            const uint32_t slot = it % C::NQ;
-            if ((it >= C::NQ && !mbar_wait(&bars->q_empty[slot], (it / C::NQ - 1) & 1)) || gave_up()) {
-              go = false;
-              break;
-            }
-            mbar_arrive_expect_tx(&bars->q_full[slot], 2 * C::TILE);
-#pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb) {
-              uint8_t* dst = smem + slot * C::TILE + kb * 16384;
-              tma_load_3d(dst + C::OFF_Q, &tm_q, &bars->q_full[slot], kb * 64, w.head * group + h, tok);
-              tma_load_3d(dst + C::OFF_D, &tm_do, &bars->q_full[slot], kb * 64, w.head * group + h, tok);
-            }
-          }
-        }
-      if (!go) set_abort(&bars->abort, p.c.status);
-    } else if (warp == 2 && lane == 0) {
-      // -------------------------------------------------------- loads of K and V
-      bool go = true;
-      uint32_t ck = 0;
+    if (warp == 0) {
+      // -------------------------------------------------------- loads
+      bool go = lane == 0;
+      uint32_t it = 0, ck = 0;
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ck) {
           const int tok = w.start + (w.c1 - 1 - n) * kChunk;
-          const uint32_t slot = ck % C::NKV;
+          auto load = [&](int off, const CUtensorMap* tm, uint64_t* full, int head) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint64_t *full = x ? bars->v_full : bars->k_full, *empty = x ? bars->v_empty : bars->k_empty;
-            if ((ck >= C::NKV && !mbar_wait(&empty[slot], (ck / C::NKV - 1) & 1)) || gave_up()) {
-              go = false;
-              break;
+            for (int kb = 0; kb < D / 64; ++kb) tma_load_3d(smem + off + kb * 16384, tm, full, kb * 64, head, tok);
+          };
+          for (int h = 0; go && h < group; ++h, ++it) {
+            const uint32_t slot = it % C::NQ, kv = ck % C::NKV;
+            go = (it < C::NQ || mbar_wait(&bars->q_empty[slot], (it / C::NQ - 1) & 1)) && !gave_up();
+            if (!go) break;
+            mbar_arrive_expect_tx(&bars->q_full[slot], 2 * C::TILE);
+            load(C::OFF_Q + slot * C::TILE, &tm_q, &bars->q_full[slot], w.head * group + h);
+            load(C::OFF_D + slot * C::TILE, &tm_do, &bars->q_full[slot], w.head * group + h);
+            if (h > 0) continue;
+            for (int x = 0; x < 2; ++x) {
+              go = go && (ck < C::NKV || mbar_wait(&bars->k_empty[x][kv], (ck / C::NKV - 1) & 1));
+              if (!go) break;
+              mbar_arrive_expect_tx(&bars->k_full[x][kv], C::TILE);
+              load((x ? C::OFF_V : C::OFF_K) + kv * C::TILE, x ? &tm_v : &tm_k, &bars->k_full[x][kv], w.head);
             }
-            mbar_arrive_expect_tx(&full[slot], C::TILE);
-#pragma unroll
-            for (int kb = 0; kb < D / 64; ++kb)
-              tma_load_3d(smem + (x ? C::OFF_V : C::OFF_K) + slot * C::TILE + kb * 16384, x ? &tm_v : &tm_k, &full[slot],
-                          kb * 64, w.head, tok);
           }
         }
-      if (!go) set_abort(&bars->abort, p.c.status);
-    } else if (warp == 1) {
-      // -------------------------------------------------------- MMA issuer (see linear_out)
-      const uint64_t kd = smem_desc(sbase + C::OFF_K, 16, 1024), qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
+      if (lane == 0 && !go) set_abort(&bars->abort, p.c.status);
+    } else if (warp == 2) {
+      // -------------------------------------------------------- MMAs of the state (see linear_out for the issuers' form)
       const uint64_t qt = smem_desc(sbase + C::OFF_Q, 16384, 1024);
-      const uint64_t sm = smem_desc(sbase + C::OFF_S, D * 128, 1024), sk = smem_desc(sbase + C::OFF_S, 16, 1024);
+      bool ok = true, go = true;
+      uint32_t it = 0, us = 0, fasts = 0;
+      while (go && w.next()) {
+        const bool fast = w.l2 < kSlow;
+        const int chunks = w.c1 - w.c0;
+        for (int n = 0; go && n < chunks; ++n)
+          for (int h = 0; h < group; ++h, ++it) {
+            const uint32_t q = it % C::NQ;
+            const bool weigh = n < chunks - 1;
+            if (weigh && fast) {
+              ok = ok && mbar_wait(&bars->wt2[fasts & 3], (fasts >> 2) & 1);
+              ++fasts;
+            } else {
+              ok = ok && mbar_wait(&bars->wt_full[q], (it / C::NQ) & 1);
+            }
+            if (weigh && h == 0 && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
+            go = __all_sync(0xffffffffu, ok) && !__any_sync(0xffffffffu, gave_up());
+            if (!go) break;
+            tc_fence_after();
+            if (elect_one()) {
+              if (weigh) {
+                const uint64_t a = desc_at(qt, q * C::TILE), d = desc_at(a, C::NQ * C::TILE);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(d, kk * 2048), C::IDESC_U, kk > 0 || h > 0);
+                if (h == group - 1) tc_commit(&bars->u_full);
+              }
+              tc_commit(&bars->q_empty[q]);
+            }
+            __syncwarp();
+          }
+      }
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else {
+      // -------------------------------------------------------- MMAs of dV (x = 0) and of dK (1)
+      const int x = warp >> 1;
+      const uint32_t ts = tmem + x * C::QN, to = tmem + C::TM_O + x * D;
+      uint64_t *k_full = bars->k_full[x], *k_empty = bars->k_empty[x];
+      const uint64_t kd = smem_desc(sbase + (x ? C::OFF_V : C::OFF_K), 16, 1024);      // K or V
+      const uint64_t qd = smem_desc(sbase + (x ? C::OFF_D : C::OFF_Q), 16, 1024);      // x Q^T or dO^T
+      const uint64_t pd = smem_desc(sbase + (x ? C::OFF_Q : C::OFF_D), 16384, 1024);   // P x dO or Q
+      const uint64_t rd = x ? smem_desc(sbase + C::OFF_S, 16, 1024) : smem_desc(sbase + C::OFF_S, D * 128, 1024);
+      const uint32_t r_step = x ? 32 : 2048, r_block = x ? D * 128 : 4 * 2048, r_idesc = x ? C::IDESC_K : C::IDESC_V;
       bool ok = true, go = true, more = w.next();
-      // The step whose K Q^T and V dO^T come next: its item and chunk, and whether it is its item's first or last.
+      uint32_t t = 0, it = 0, ck = 0;   // steps, items, chunks
+      // The step whose product comes next: its item and chunk, and place in them.
       uint32_t nit = 0, nck = 0;
       int ns = 0, nh = 0;
-      bool nfast = w.l2 < kSlow;
-      auto issue_s = [&](int x) {   // K Q^T (0) or V dO^T (1)
-        if (x == 0 && ns == 0) {
+      auto issue_s = [&] {
+        if (ns == 0) {
           ok = ok && mbar_wait(&bars->wt_full[nit % C::NQ], (nit / C::NQ) & 1);
-          if (nfast) ok = ok && mbar_wait(&bars->q_full[nit % C::NQ], (nit / C::NQ) & 1);
+          if (w.l2 < kSlow) ok = ok && mbar_wait(&bars->q_full[nit % C::NQ], (nit / C::NQ) & 1);
+          if (nh == 0) ok = ok && mbar_wait(&k_full[nck % C::NKV], (nck / C::NKV) & 1);
         }
-        if (ns == 0 && nh == 0)
-          ok = ok && mbar_wait(&(x ? bars->v_full : bars->k_full)[nck % C::NKV], (nck / C::NKV) & 1);
         tc_fence_after();
         if (elect_one() && ok) {
-          const uint64_t a = desc_at(kd, (x ? C::OFF_V : 0) + nck % C::NKV * C::TILE);
-          const uint64_t b = desc_at(qd, (x ? C::NQ * C::TILE : 0) + nit % C::NQ * C::TILE + ns * C::QN * 128);
+          const uint64_t a = desc_at(kd, nck % C::NKV * C::TILE);
+          const uint64_t d = desc_at(qd, nit % C::NQ * C::TILE + ns * C::QN * 128);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
-            tc_mma_ss(tmem + x * C::QN, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
+            tc_mma_ss(ts, desc_at(a, off), desc_at(d, off), C::IDESC_S, kk > 0);
           }
           tc_commit(&bars->s_full[x]);
-          if (C::NKV == 1 && ns == C::NS - 1 && nh == group - 1) tc_commit(&(x ? bars->v_empty : bars->k_empty)[0]);
+          if (C::NKV == 1 && ns == C::NS - 1 && nh == group - 1) tc_commit(&k_empty[0]);
         }
         __syncwarp();
       };
-      if (more) {
-        issue_s(0);
-        issue_s(1);
-      }
-      uint32_t t = 0, it = 0, ck = 0, us = 0, fasts = 0;   // steps, items, chunks, Q^T dO (also of fast heads' items)
+      if (more) issue_s();
       while (go && more) {
         const int chunks = w.c1 - w.c0;
         const bool fast = w.l2 < kSlow;
-        const int hr = fast || group == 1 ? 0 : 1;   // the item that the products with R come in
+        const int hr = fast || group == 1 ? 0 : 1;   // the item that the product with R comes in
         for (int n = 0; go && n < chunks; ++n) {
           const bool weigh = n < chunks - 1;
           for (int h = 0; go && h < group; ++h)
             for (int s = 0; s < C::NS; ++s) {
               const bool first = h == 0 && s == 0, item = s == C::NS - 1, end = item && h == group - 1;
-              const bool late = item && (fast || (end && C::NKV == 1));
               const uint32_t q = it % C::NQ, kv = ck % C::NKV;
-              if (first && ck > 0) ok = ok && mbar_wait(&bars->o_free, (ck - 1) & 1);
-              if (h == hr && s == 0) {
+              if (first && ck > 0) ok = ok && mbar_wait(&bars->o_free[x], (ck - 1) & 1);
+              if (h == hr && s == 0) {   // dV += K R, dK += V R^T
                 ok = ok && mbar_wait(&bars->s_ready, ck & 1);
                 tc_fence_after();
                 if (elect_one() && ok) {
-                  const uint64_t a = desc_at(kd, kv * C::TILE), b = desc_at(a, C::OFF_V);
+                  const uint64_t a = desc_at(kd, kv * C::TILE);
 #pragma unroll
                   for (int kk = 0; kk < D / 16; ++kk)
-                    tc_mma_ss(tmem + C::TM_O, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sm, kk * 2048),
-                              C::IDESC_V, kk > 0 || !first);
-#pragma unroll
-                  for (int kk = 0; kk < D / 16; ++kk)
-                    tc_mma_ss(tmem + C::TM_O + D, desc_at(b, (kk >> 2) * 16384 + (kk & 3) * 32),
-                              desc_at(sk, (kk >> 2) * (D * 128) + (kk & 3) * 32), C::IDESC_K, kk > 0 || !first);
-                  if (fast) tc_commit(&bars->a_full);
+                    tc_mma_ss(to, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32),
+                              desc_at(rd, (kk >> 2) * r_block + (kk & 3) * r_step), r_idesc, kk > 0 || !first);
+                  if (fast) tc_commit(&bars->a_full[x]);
                   tc_commit(&bars->s_read);
                 }
                 __syncwarp();
               }
-              // the step behind this one
+              ok = ok && mbar_wait(&bars->p_full[x], t & 1);
+              go = __all_sync(0xffffffffu, ok);
+              if (!go) break;
+              tc_fence_after();
+              if (elect_one()) {   // dV += P dO, dK += P Q
+                const uint64_t d = desc_at(pd, q * C::TILE + s * C::QN * 128);
+#pragma unroll
+                for (int kk = 0; kk < C::QN / 16; ++kk)
+                  tc_mma_ts(to, ts + kk * 8, desc_at(d, kk * 2048), C::IDESC_V, kk > 0 || !(first && hr > 0));
+                if (item) {
+                  tc_commit(&bars->q_empty[q]);
+                  if (fast && weigh) tc_commit(&bars->k_done);
+                }
+                if (end) {
+                  tc_commit(&bars->o_full[x]);
+                  if (C::NKV > 1) tc_commit(&k_empty[kv]);
+                }
+              }
+              __syncwarp();
               bool next = true;
               ns = s + 1;
+              ++t;
               if (item) {
                 ns = 0;
-                ++nit;
+                ++nit, ++it;
                 nh = h + 1;
                 if (end) {
                   nh = 0;
-                  ++nck;
+                  ++nck, ++ck;
                   if (!weigh) next = more = w.next();
-                  nfast = w.l2 < kSlow;
                 }
               }
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {   // dV += P dO, dK += P Q
-                ok = ok && mbar_wait(&bars->p_full[x], t & 1);
-                go = __all_sync(0xffffffffu, ok);
-                if (!go) break;
-                tc_fence_after();
-                if (elect_one()) {
-                  const uint64_t b = desc_at(qt, (x ? 0 : C::NQ * C::TILE) + q * C::TILE + s * C::QN * 128);
-#pragma unroll
-                  for (int kk = 0; kk < C::QN / 16; ++kk)
-                    tc_mma_ts(tmem + C::TM_O + x * D, tmem + x * C::QN + kk * 8, desc_at(b, kk * 2048), C::IDESC_V,
-                              kk > 0 || !(first && hr > 0));
-                }
-                __syncwarp();
-                if (next && !late) issue_s(x);
-              }
-              if (!go) break;
-              auto issue_u = [&](int from, int to, bool fresh) {
-                const uint64_t a = desc_at(qt, q * C::TILE), b = desc_at(a, C::NQ * C::TILE);
-#pragma unroll
-                for (int kk = 0; kk < to - from; ++kk)
-                  tc_mma_ss(tmem + C::TM_U, desc_at(a, (from + kk) * 2048), desc_at(b, (from + kk) * 2048), C::IDESC_U,
-                            kk > 0 || !fresh);
-              };
-              if (weigh && !fast) {
-                if (first && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
-                tc_fence_after();
-                if (elect_one() && ok) issue_u(s * (C::QN / 16), (s + 1) * (C::QN / 16), first);
-              } else if (weigh && item) {
-                if (elect_one() && ok) tc_commit(&bars->k_done);
-                __syncwarp();
-                if (h == 0 && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
-                ok = ok && mbar_wait(&bars->wt2, fasts++ & 1);
-                tc_fence_after();
-                if (elect_one() && ok) issue_u(0, 8, h == 0);
-              }
-              __syncwarp();
-              if (elect_one() && ok) {
-                if (weigh && end) tc_commit(&bars->u_full);
-                if (item) tc_commit(&bars->q_empty[q]);
-                if (end) tc_commit(&bars->o_full);
-                if (end && C::NKV > 1) {
-                  tc_commit(&bars->k_empty[kv]);
-                  tc_commit(&bars->v_empty[kv]);
-                }
-              }
-              __syncwarp();
-              if (next && late) {
-                issue_s(0);
-                issue_s(1);
-              }
-              ++t;
-              if (item) ++it;
-              if (end) ++ck;
+              if (next) issue_s();
             }
         }
       }
@@ -1747,7 +1724,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int c = w.c1 - 1 - n, rows = w.rows(c);
         const float f_out = fast ? p.scale : p.scale * exp2f(w.l2 * (float)(kMiddle - r));
         if (fast) {   // the rows of the product with R
-          if (!mbar_wait_warp(&bars->a_full, fasts++ & 1)) {
+          if (!mbar_wait_warp(&bars->a_full[x], fasts++ & 1)) {
             go = false;
             break;
           }
@@ -1837,7 +1814,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           mbar_arrive(&bars->p_full[x]);
         }
-        if (!go || !mbar_wait_warp(&bars->o_full, ck & 1)) {
+        if (!go || !mbar_wait_warp(&bars->o_full[x], ck & 1)) {
           go = false;
           break;
         }
@@ -1853,7 +1830,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (g == D / 32 - 1) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->o_free);
+            if (lane == 0) mbar_arrive(&bars->o_free[x]);
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -1937,7 +1914,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             fence_proxy_async_smem();
             mbar_arrive(&bars->wt_full[slot]);
             if (m == chunks - 1) continue;   // no state comes behind the last chunk
-            if (!mbar_wait_warp(&bars->k_done, fasts++ & 1)) {
+            if (!mbar_wait_warp(&bars->k_done, fasts & 1)) {
               go = false;
               break;
             }
@@ -1967,7 +1944,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           fence_proxy_async_smem();
-          mbar_arrive(fast ? &bars->wt2 : &bars->wt_full[slot]);
+          mbar_arrive(fast ? &bars->wt2[fasts++ & 3] : &bars->wt_full[slot]);
         }
         if (!go || n == chunks - 1) continue;
         if (!mbar_wait_warp(&bars->u_full, sums++ & 1)) {
@@ -2001,7 +1978,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == 2) {
     __syncwarp();
     tc_fence_after();
     tmem_dealloc(tmem, 512);
