@@ -654,33 +654,28 @@ struct OutArgs {
   const float* starts;     // the states at the cuts
   const float* state_in;
   float* state_out;
-  int32_t gx, gy;          // query heads and key heads of a state; one of them is 1
+  int32_t group;           // query heads of a state
   float scale;
   bool wide;               // out is 32-byte aligned
-  bool transposed;         // of the states at the cuts (the way back in time)
   bf16* out;
 };
 
-// What a launch of linear_out works on: one query head to a key head (FWD1) or a group of them (FWD), in order; or, from the
-// last token to the first, one key head (BACK1) or a group of them (BACK) to a query head.
-enum { FWD1, FWD, BACK1, BACK };
-
-template <int D, int KIND>
+// ONE: one query head to a key head, else a group of them.
+template <int D, bool ONE>
 struct Lin {
   static constexpr int TILE = kChunk * D * 2;
   // Tiles of Q, and of K and V, which take turns.  A load takes 2 to 4 thousand cycles under way and an item the memory 3 to
-  // 6, so that what streams has to have two to three tiles on its way: a group of query heads streams Q, a group of key
-  // heads K and V, one head of each both.
-  static constexpr int NQ = D == 64 ? 4 : KIND == FWD ? 2 : 1;
-  static constexpr int NT = D == 64 ? 8 : KIND == FWD ? 3 : KIND == BACK ? 5 : 4;
-  static constexpr bool STAGE = D == 64 || KIND != BACK; // outputs go through a tile of their own
-  // Buffers of Q K^T and P, and of outputs: two of the one or of the other at D = 128, whose K^T V takes the rest.
-  static constexpr int NP = D == 64 || KIND == BACK ? 2 : 1;
-  static constexpr int NB = D == 64 || KIND != BACK ? 2 : 1;
+  // 6, so that what streams has to have two to three tiles on its way: a group of query heads streams Q, one head of each
+  // K and V too.
+  static constexpr int NQ = D == 64 ? 4 : ONE ? 1 : 2;
+  static constexpr int NT = D == 64 ? 8 : ONE ? 4 : 3;
+  // Buffers of Q K^T and P: two if K^T V and two outputs leave room.  Outputs: two.
+  static constexpr int NP = D == 64 ? 2 : 1;
+  static constexpr int NB = 2;
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_T = NQ * TILE;
   static constexpr int OFF_O = OFF_T + NT * TILE;
-  static constexpr int OFF_S = OFF_O + (STAGE ? TILE : 0);  // the state, D rows of k's dims, like a V tile
+  static constexpr int OFF_S = OFF_O + TILE;  // the state, D rows of k's dims, like a V tile
   static constexpr int OFF_TAB = OFF_S + D * D * 2;      // 32 powers of the decay for each warp that makes P
   static constexpr int OFF_BAR = OFF_TAB + 8 * 128;
   static constexpr int SMEM = OFF_BAR + 512;
@@ -707,7 +702,7 @@ struct LinBars {
   uint64_t o_free[2];  // and in registers
   uint64_t out_full;   // an output is in its tile, or its rows are written
   uint64_t out_free[2];  // and on its way, of one warpgroup's or the other's (each waits for the other's, in turn)
-  uint64_t k_done[2];  // a K that is to be weighted is no longer read as it was loaded
+  uint64_t k_done;     // a K that is to be weighted is no longer read as it was loaded
   uint64_t wt_full[4]; // a pair's V, or K, is weighted; four, as the warps that do it may be some pairs ahead of the issuer
   uint64_t u_full;     // the chunk's K^T V
   uint64_t u_free;     // and in registers
@@ -737,31 +732,29 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8], bo
 //   o_i = scale lam^(i+1-m) [ q_i (lam^m S) + sum_{j <= i} (q_i . k_j) w_j ],  w_j = lam^(m-1-j) v_j,
 //   S'  = lam^n S + lam^(n-m) sum_j k_j w_j^T
 // so that P = Q K^T below the diagonal has no factors at all, V is weighted once for both products, as soon as it is
-// loaded, and the row's factor comes last, as long as lam^-m stays in range: 2^64 at most (kSlow; the other way in time: rows
-// lam^(m-i), w_j = lam^(j-m) v_j, the state lam^(n-m), the sum lam^m).  For a head that forgets faster P has the exact powers, the
-// rows of Q S are scaled in TMEM, and K is weighted for the state when Q K^T has read it.
+// loaded, and the row's factor comes last, as long as lam^-m stays in range: 2^64 at most (kSlow).  For a head that forgets
+// faster P has the exact powers, the rows of Q S are scaled in TMEM, and K is weighted for the state when Q K^T has read it.
 constexpr int kMiddle = 64;
 constexpr float kSlow = -1.0f;   // log2 of the decay
 
-// An item is a chunk with one query and one key head: of a group of query heads (gx) each item has an output and the
-// chunk one K and V, of a group of key heads (gy) each item has a K and V and the chunk one output.
+// An item is a chunk with one query head.
 // Warp roles:
-//   warp 0       TMA producer;  warp 1  TMEM and every MMA;  warp 2  O out of shared memory
+//   warp 0       loads;  warp 2  O out of shared memory
+//   warps 1, 3   MMAs: Q K^T and K^T V (and TMEM);  Q S and P V.  (One warp for all is held up by its waits and commits: ....)
 //   warps 4-11   two warpgroups, for every other item: P below the diagonal, in bf16 for P V (a thread a query), then
 //                O out of TMEM, scaled
 //   warps 12-15  the weighted tiles, and the state in registers (a thread a row), its bf16 copy in shared memory
-template <int D, int KIND>
+template <int D, bool ONE>
 __global__ void __launch_bounds__(kThreads, 1)
     linear_out(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o,
                const __grid_constant__ OutArgs p) {
-  using C = Lin<D, KIND>;
-  constexpr bool back = KIND == BACK1 || KIND == BACK;
+  using C = Lin<D, ONE>;
   extern __shared__ __align__(1024) uint8_t smem[];
   LinBars* bars = reinterpret_cast<LinBars*>(smem + C::OFF_BAR);
   Walk w(p.c, blockIdx.x);
   // sequences without a token: their states go through
-  if (!back && p.state_out != nullptr)
+  if (p.state_out != nullptr)
     for (int s = blockIdx.x; s < p.c.num_segments; s += gridDim.x)
       if (p.c.cu[s] == p.c.cu[s + 1] && p.c.cu[s] >= 0 && p.c.cu[s] <= p.c.num_tokens) {
         const size_t n = (size_t)p.c.heads * D * D / 4, at = n * s;
@@ -788,22 +781,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::NQ; ++i) {
       mbar_init(&bars->q_full[i], 1);
-      mbar_init(&bars->q_empty[i], 1);
+      mbar_init(&bars->q_empty[i], 2);
     }
     for (int i = 0; i < C::NT; ++i) {
       mbar_init(&bars->t_full[i], 1);
-      mbar_init(&bars->t_empty[i], 1);
+      mbar_init(&bars->t_empty[i], 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->s_full[i], 1);
       mbar_init(&bars->p_full[i], 128);
       mbar_init(&bars->a_full[i], 1);
-      mbar_init(&bars->k_done[i], 1);
       mbar_init(&bars->o_full[i], 1);
       mbar_init(&bars->o_free[i], 4);
       mbar_init(&bars->out_free[i], 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&bars->wt_full[i], 128);
+    mbar_init(&bars->k_done, 1);
     mbar_init(&bars->s_read, 1);
     mbar_init(&bars->out_full, 128);
     mbar_init(&bars->u_free, 4);
@@ -821,8 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
   auto gave_up = [&] { return *reinterpret_cast<volatile int32_t*>(&bars->abort) != 0; };
-  const int group = KIND == FWD ? p.gx : KIND == BACK ? p.gy : 1;
-  constexpr bool per_k = KIND == BACK;   // items share a Q and an output; else a K and V, if there is more than one
+  const int group = ONE ? 1 : p.group;
   // Every role walks the same items and counts what it has passed.
 
   if (warp < 4) {
@@ -845,173 +837,143 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int tok = w.start + (back ? w.c1 - 1 - n : w.c0 + n) * kChunk;
+          const int tok = w.start + (w.c0 + n) * kChunk;
           for (int h = 0; go && h < group; ++h) {
-            const bool new_k = per_k || h == 0, new_q = !per_k || h == 0;
-            if (new_k) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_k, w.head * p.gy + (per_k ? h : 0), tok);
-            if (new_q) load(C::OFF_Q, bars->q_full, bars->q_empty, qi++, C::NQ, &tm_q, w.head * p.gx + (per_k ? 0 : h), tok);
-            if (new_k) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_v, w.head * p.gy + (per_k ? h : 0), tok);
+            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_k, w.head, tok);
+            load(C::OFF_Q, bars->q_full, bars->q_empty, qi++, C::NQ, &tm_q, w.head * group + h, tok);
+            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_v, w.head, tok);
           }
         }
       if (!go) set_abort(&bars->abort, p.c.status);
     } else if (warp == 1) {
-      // -------------------------------------------------------- MMA issuer
-      // Every lane runs every step, no lane's answer to a wait decides where the warp goes, and the elected lane issues
-      // as long as its own waits were met; a vote an item ends the walk.  The MMAs of one issuer execute in order, so
-      // Q K^T of an item may overwrite a P whose P V was issued before.  For an item, in this order:
-      //   BACK   Q K^T of the next item;  K^T V;  of a chunk's second item (its first of one or two) Q S: the state has had an
-      //          item's time;  P V
-      //   else   of a chunk's first item K^T V, so that the next chunk's state is made while this one's queries are worked
-      //          on;  P V;  Q K^T and Q S of the next item, whose Q tile is then free
-      // (with two buffers of P Q K^T of the next item is first there too).  For a head that forgets fast K^T V waits for Q K^T, the
-      // chunk's last, and Q S comes first of an output's products.  A wait takes its thread 200 to 300 cycles while the
-      // pipe streams from shared memory: none twice.
+      // -------------------------------------------------------- MMAs of Q K^T and of the state
+      // Every lane of an issuer runs every step, no lane's answer to a wait decides where the warp goes, and a vote an item
+      // ends the walk.  A chunk's K^T V comes behind its second item's Q K^T (its only one's): V is weighted by then, and the
+      // next chunk's state is made while this one's queries are worked on; for a head that forgets fast behind the last
+      // item's, when K is weighted.
       const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
       const uint64_t kd = smem_desc(sbase + C::OFF_T, 16, 1024), kt = smem_desc(sbase + C::OFF_T, 16384, 1024);
-      const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
-      bool ok = true;
-      // What has been issued: Q tiles, pairs of K and V, items and handed-over keys of Q K^T; Q S and its chunks; K^T V.
-      uint32_t sq = 0xffffffffu, sk = 0xffffffffu, si = 0, handed = 0, aq = 0, ac = 0, us = 0;
-      auto issue_s = [&](int h, int n) {   // item h of the walk's chunk n
-        const bool fast = w.l2 < kSlow, lastk = per_k || h == group - 1, weigh = n < w.c1 - w.c0 - 1;
-        // keys that are weighted, or, the way back, whose rows behind the segment's end have to be cleared
-        const bool hand = weigh && lastk && (fast || (back && n == 0 && w.rows(w.c1 - 1) < kChunk));
-        const bool free_k = !per_k && lastk && (!weigh || (!fast && group > (C::NP == 1 ? 1 : 2)));
-        const bool free_q = KIND == BACK && h == group - 1 && h - 1 > (fast || group == 2 ? 0 : 1);
-        if (!per_k || h == 0) {
-          ++sq;
-          ok = ok && mbar_wait(&bars->q_full[sq % C::NQ], (sq / C::NQ) & 1);
-        }
-        if (per_k || h == 0) {
-          ++sk;
-          ok = ok && mbar_wait(&bars->t_full[2 * sk % C::NT], (2 * sk / C::NT) & 1);
-        }
-        tc_fence_after();
-        if (elect_one() && ok) {
-          const uint64_t a = desc_at(qd, sq % C::NQ * C::TILE), b = desc_at(kd, 2 * sk % C::NT * C::TILE);
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
-            tc_mma_ss(tmem + C::TM_P + si % C::NP * 128, desc_at(a, off), desc_at(b, off), C::IDESC_S, kk > 0);
-          }
-          tc_commit(&bars->s_full[si & 1]);
-          if (hand) tc_commit(&bars->k_done[handed & 1]);
-          if (free_k) tc_commit(&bars->t_empty[2 * sk % C::NT]);
-          if (free_q) tc_commit(&bars->q_empty[sq % C::NQ]);
-        }
-        __syncwarp();
-        ++si;
-        if (hand) ++handed;
-      };
-      // an output's buffer, when the output that had it before is in registers
-      auto take = [&](uint32_t o) {
-        if (o >= C::NB) ok = ok && mbar_wait(&bars->o_free[(o - C::NB) & 1], ((o - C::NB) >> 1) & 1);
-      };
-      // B = or += Q S of output o
-      auto issue_a = [&](uint32_t o, bool new_chunk, bool fresh, bool fast, bool last, bool free_q, uint32_t item) {
-        if (new_chunk) ok = ok && mbar_wait(&bars->s_ready, ac++ & 1);
-        if (fresh) take(o);
-        const uint32_t q = aq++ % C::NQ;
-        tc_fence_after();
-        if (elect_one() && ok) {
-          const uint64_t a = desc_at(qd, q * C::TILE);
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            tc_mma_ss(tmem + C::TM_B + o % C::NB * D, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32),
-                      desc_at(sd, kk * 2048), C::IDESC_A, kk > 0 || !fresh);
-          if (free_q) tc_commit(&bars->q_empty[q]);
-          if (fast) tc_commit(&bars->a_full[item & 1]);
-          if (last) tc_commit(&bars->s_read);
-        }
-        __syncwarp();
-      };
-      // U (+)= K^T V of pair k
-      auto issue_u = [&](uint32_t k, bool first, bool last, bool free_k) {   // (V is there if it, or K, is weighted)
-        const uint32_t ks = 2 * k % C::NT, vs = (2 * k + 1) % C::NT;
-        if (first && us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
-        ok = ok && mbar_wait(&bars->wt_full[k & 3], (k >> 2) & 1);
-        tc_fence_after();
-        if (elect_one() && ok) {
-          const uint64_t a = desc_at(kt, ks * C::TILE), b = desc_at(kt, vs * C::TILE);
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(b, kk * 2048), C::IDESC_U, kk > 0 || !first);
-          if (free_k) tc_commit(&bars->t_empty[ks]);
-          if (last) tc_commit(&bars->u_full);
-        }
-        __syncwarp();
-      };
-      uint32_t ki = 0, it = 0, outs = 0;
-      bool more = w.next(), go = true;
-      if (more) {
-        issue_s(0, 0);
-        if (!per_k) issue_a(0, true, true, w.l2 < kSlow, group == 1, true, 0);
-      }
-      while (go && more) {
+      bool ok = true, go = true;
+      uint32_t it = 0, ki = 0, us = 0;
+      while (go && w.next()) {
         const int chunks = w.c1 - w.c0;
         const bool fast = w.l2 < kSlow;
-        for (int n = 0; go && n < chunks; ++n) {
+        for (int n = 0; go && n < chunks; ++n, ++ki) {
           const bool weigh = n < chunks - 1;
+          const uint32_t ks = 2 * ki % C::NT, vs = (2 * ki + 1) % C::NT;
           for (int h = 0; h < group; ++h, ++it) {
-            const bool out = !per_k || h == group - 1, end = h == group - 1;
-            const uint32_t ks = 2 * ki % C::NT, vs = (2 * ki + 1) % C::NT;
-            auto ahead = [&] {   // Q K^T of the next item
-              if (end && !weigh) more = w.next();
-              if (more) issue_s(end ? 0 : h + 1, !end ? n : weigh ? n + 1 : 0);
-            };
-            // (a group of key heads at D = 128 has one Q tile, whose next load a chunk's last item would wait for)
-            const bool late = C::NP == 1 || (C::NQ == 1 && end);
-            if (!late) ahead();
-            bool fresh = false;                    // P V is the first of its output's products
-            bool weighted = !per_k && h > 0;       // what P V waits for is known to be weighted
-            if (weigh && (per_k || (fast ? end : h == 0))) {
-              issue_u(ki, !per_k || h == 0, end || !per_k, per_k || fast || group <= (C::NP == 1 ? 1 : 2));
-              weighted = true;
-            }
-            if (per_k) {
-              const int hq = fast || group <= 2 ? 0 : 1;
-              if (h == hq) issue_a(outs, true, hq == 0, fast, true, group - 2 <= hq, it);
-              fresh = h < hq;
-              if (fresh) take(outs);
-            }
-            if (fast && (per_k || h == 0)) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
-            // (a fast head's last V is not weighted, but its slot is not given back before the warps that do it have passed it)
-            if (fast ? !weigh && (per_k || h == 0) : !weighted) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
-            ok = ok && mbar_wait(&bars->p_full[it & 1], (it >> 1) & 1);
+            const bool last = h == group - 1, state = weigh && h == (fast || group == 1 ? group - 1 : 1);
+            const uint32_t q = it % C::NQ;
+            if (h == 0) ok = ok && mbar_wait(&bars->t_full[ks], (2 * ki / C::NT) & 1);
+            ok = ok && mbar_wait(&bars->q_full[q], (it / C::NQ) & 1);
+            if (it >= C::NP) ok = ok && mbar_wait(&bars->o_full[(it - C::NP) & 1], ((it - C::NP) >> 1) & 1);   // its P was read
             go = __all_sync(0xffffffffu, ok);
             if (!go) break;
             tc_fence_after();
-            if (elect_one()) {  // B = or += P V
-              const uint64_t b = desc_at(kt, vs * C::TILE);
+            if (elect_one()) {
+              const uint64_t a = desc_at(qd, q * C::TILE), d = desc_at(kd, ks * C::TILE);
 #pragma unroll
-              for (int kk = 0; kk < 8; ++kk)
-                tc_mma_ts(tmem + C::TM_B + outs % C::NB * D, tmem + C::TM_P + it % C::NP * 128 + kk * 8,
-                          desc_at(b, kk * 2048), C::IDESC_B, kk > 0 || !fresh);
-              if (out) tc_commit(&bars->o_full[outs & 1]);
-              if (per_k || end) tc_commit(&bars->t_empty[vs]);
-              if (per_k && !weigh) tc_commit(&bars->t_empty[ks]);
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
+                tc_mma_ss(tmem + C::TM_P + it % C::NP * 128, desc_at(a, off), desc_at(d, off), C::IDESC_S, kk > 0);
+              }
+              tc_commit(&bars->s_full[it & 1]);
+              tc_commit(&bars->q_empty[q]);
+              if (fast && weigh && last) tc_commit(&bars->k_done);
             }
             __syncwarp();
-            if (late) ahead();
-            if (!per_k && (!end || more)) {        // Q S of the next item
-              const int h1 = end ? 0 : h + 1;
-              issue_a(outs + 1, end, true, w.l2 < kSlow, h1 == group - 1, true, it + 1);
+            if (state) {
+              ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
+              if (us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
+              tc_fence_after();
+              if (elect_one() && ok) {
+                const uint64_t a = desc_at(kt, ks * C::TILE), d = desc_at(kt, vs * C::TILE);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk)
+                  tc_mma_ss(tmem + C::TM_U, desc_at(a, kk * 2048), desc_at(d, kk * 2048), C::IDESC_U, kk > 0);
+                tc_commit(&bars->u_full);
+                tc_commit(&bars->t_empty[vs]);
+              }
+              __syncwarp();
             }
-            if (out) ++outs;
-            if (per_k || end) ++ki;
+            if (last && elect_one() && ok) {   // a tile's slot takes two arrivals
+              tc_commit(&bars->t_empty[ks]);
+              tc_commit(&bars->t_empty[ks]);
+              if (!weigh) tc_commit(&bars->t_empty[vs]);
+            }
+            __syncwarp();
           }
         }
       }
       go = __all_sync(0xffffffffu, ok);
       if (!go) set_abort(&bars->abort, p.c.status);
-    } else if (C::STAGE && warp == 2 && lane == 0) {
+    } else if (warp == 3) {
+      // -------------------------------------------------------- MMAs of the outputs: P V, Q S of the next item
+      const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024), vd = smem_desc(sbase + C::OFF_T, 16384, 1024);
+      const uint64_t sd = smem_desc(sbase + C::OFF_S, D * 128, 1024);
+      bool ok = true, go = true, more = w.next();
+      uint32_t it = 0, ki = 0, qi = 0, ck = 0;   // items and chunks of P V, of Q S
+      auto issue_a = [&](int h) {   // B = Q S
+        const bool fast = w.l2 < kSlow;
+        const uint32_t q = qi % C::NQ;
+        if (h == 0) ok = ok && mbar_wait(&bars->s_ready, ck++ & 1);
+        if (qi >= 2) ok = ok && mbar_wait(&bars->o_free[qi & 1], ((qi - 2) >> 1) & 1);   // the output before is in registers
+        ok = ok && mbar_wait(&bars->q_full[q], (qi / C::NQ) & 1);
+        tc_fence_after();
+        if (elect_one() && ok) {
+          const uint64_t a = desc_at(qd, q * C::TILE);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_ss(tmem + C::TM_B + (qi & 1) * D, desc_at(a, (kk >> 2) * 16384 + (kk & 3) * 32), desc_at(sd, kk * 2048),
+                      C::IDESC_A, kk > 0);
+          tc_commit(&bars->q_empty[q]);
+          if (fast) tc_commit(&bars->a_full[qi & 1]);
+          if (h == group - 1) tc_commit(&bars->s_read);
+        }
+        __syncwarp();
+        ++qi;
+      };
+      if (more) issue_a(0);
+      while (go && more) {
+        const int chunks = w.c1 - w.c0;
+        const bool fast = w.l2 < kSlow;
+        for (int n = 0; go && n < chunks; ++n, ++ki) {
+          const bool weigh = n < chunks - 1;
+          const uint32_t vs = (2 * ki + 1) % C::NT;
+          for (int h = 0; h < group; ++h, ++it) {
+            const bool last = h == group - 1;
+            if (h == 0 && fast) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
+            // (a fast head's last V is not weighted, but its slot is not given back before the warps that do it have passed it)
+            if (h == 0 && !(fast && weigh)) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
+            ok = ok && mbar_wait(&bars->p_full[it & 1], (it >> 1) & 1);
+            go = __all_sync(0xffffffffu, ok);
+            if (!go) break;
+            tc_fence_after();
+            if (elect_one()) {   // B += P V
+              const uint64_t d = desc_at(vd, vs * C::TILE);
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                tc_mma_ts(tmem + C::TM_B + (it & 1) * D, tmem + C::TM_P + it % C::NP * 128 + kk * 8, desc_at(d, kk * 2048),
+                          C::IDESC_B, 1);
+              tc_commit(&bars->o_full[it & 1]);
+              if (last) tc_commit(&bars->t_empty[vs]);
+            }
+            __syncwarp();
+            if (last && !weigh) more = w.next();
+            if (!last || more) issue_a(last ? 0 : h + 1);
+          }
+        }
+      }
+      go = __all_sync(0xffffffffu, ok);
+      if (!go) set_abort(&bars->abort, p.c.status);
+    } else if (warp == 2 && lane == 0) {
       // -------------------------------------------------------- O out of shared memory
       bool go = true;
       uint32_t oi = 0;
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-          const int c = back ? w.c1 - 1 - n : w.c0 + n;
-          for (int h = 0; h < p.gx; ++h, ++oi) {
+          const int c = w.c0 + n;
+          for (int h = 0; h < group; ++h, ++oi) {
             if (!mbar_wait(&bars->out_full, oi & 1) || gave_up()) {
               go = false;
               break;
@@ -1019,7 +981,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (w.rows(c) == kChunk) {
 #pragma unroll
               for (int kb = 0; kb < D / 64; ++kb)
-                tma_store_3d(&tm_o, sbase + C::OFF_O + kb * 16384, kb * 64, w.head * p.gx + h, w.start + c * kChunk);
+                tma_store_3d(&tm_o, sbase + C::OFF_O + kb * 16384, kb * 64, w.head * group + h, w.start + c * kChunk);
               bulk_commit();
               bulk_wait_read();
             }
@@ -1041,14 +1003,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     while (go && w.next()) {
       const bool fast = w.l2 < kSlow;
       __syncwarp();
-      tab[lane] = exp2f(w.l2 * (float)(back ? lane : 31 - lane));
+      tab[lane] = exp2f(w.l2 * (float)(31 - lane));
       __syncwarp();
-      const float sl = back ? -w.l2 : w.l2;
-      const uint64_t slope = f2pack(sl, sl);
+      const uint64_t slope = f2pack(w.l2, w.l2);
       for (int n = 0; go && n < w.c1 - w.c0; ++n) {
-        const int c = back ? w.c1 - 1 - n : w.c0 + n;
+        const int c = w.c0 + n;
         const int rows = w.rows(c);
-        const float f_out = fast ? p.scale : p.scale * exp2f(w.l2 * (float)(back ? kMiddle - r : r + 1 - kMiddle));
+        const float f_out = fast ? p.scale : p.scale * exp2f(w.l2 * (float)(r + 1 - kMiddle));
         for (int h = 0; h < group; ++h, ++it) {
           if ((it & 1) == mine) {
             const uint32_t tp = trow + C::TM_P + it % C::NP * 128;
@@ -1064,17 +1025,15 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int g = 0; g < 4; ++g) {
                 const int c0 = g * 32;
                 uint32_t s[32];
-                if (back ? g < quad || c0 >= rows : g > quad) {   // nothing seen
+                if (g > quad) {   // nothing seen
 #pragma unroll
                   for (int i = 0; i < 16; ++i) s[i] = 0u;
                 } else {
                   tmem_ld_32x32b_x32(tp + c0, s);
                   tmem_ld_wait();
                   reg_fence<32>(s);
-                  if (g == quad || (back && rows - c0 < 32)) {
-                    uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
-                    if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-                    if (back && rows - c0 < 32) seen &= (1u << (rows - c0)) - 1u;
+                  if (g == quad) {
+                    const uint32_t seen = 0xffffffffu >> (31 - lane);   // columns of the group that the row takes, a bit each
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                       if (!(seen >> i & 1)) s[i] = 0u;
@@ -1092,16 +1051,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
               for (int g = 0; g < 4; ++g) {
                 uint32_t pk[16];
-                if (back ? g < quad || g * 32 >= rows : g > quad) {   // nothing seen
+                if (g > quad) {   // nothing seen
 #pragma unroll
                   for (int i = 0; i < 16; ++i) pk[i] = 0u;
                 } else {
                   uint32_t s[32];
                   tmem_ld_32x32b_x32(tp + g * 32, s);
-                  uint32_t seen = 0xffffffffu;   // columns of the group that the row takes, a bit each
-                  if (g == quad) seen = back ? 0xffffffffu << lane : 0xffffffffu >> (31 - lane);
-                  if (back && rows - g * 32 < 32) seen &= (1u << (rows - g * 32)) - 1u;
-                  if (g == quad || (back && rows - g * 32 < 32)) {
+                  if (g == quad) {
+                    const uint32_t seen = 0xffffffffu >> (31 - lane);
                     const float gap = (float)(r - g * 32);
                     const uint64_t at = f2pack(gap, gap);
                     tmem_ld_wait();
@@ -1116,7 +1073,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                       pk[i] = pack_bf16(seen >> (2 * i) & 1 ? x0 : 0.f, seen >> (2 * i + 1) & 1 ? x1 : 0.f);
                     }
                   } else {
-                    const float rf = ex2(w.l2 * (float)(back ? g * 32 - r : r - g * 32 - 31));
+                    const float rf = ex2(w.l2 * (float)(r - g * 32 - 31));
                     const uint64_t rf2 = f2pack(rf, rf);
                     tmem_ld_wait();
                     reg_fence<32>(s);
@@ -1138,13 +1095,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_st_32x32b_x16(tp + g * 16, pk);
               }
             }
-            if (fast && (!per_k || h == 0)) {   // the rows of Q S
+            if (fast) {   // the rows of Q S
               if (!mbar_wait_warp(&bars->a_full[mine], fasts & 1)) {
                 go = false;
                 break;
               }
               tc_fence_after();
-              const float f = exp2f(w.l2 * (float)(back ? max(rows - r, 0) : r + 1));
+              const float f = exp2f(w.l2 * (float)(r + 1));
               const uint64_t f2 = f2pack(f, f);
               const uint32_t tb = trow + C::TM_B + oi % C::NB * D;
 #pragma unroll 1
@@ -1164,7 +1121,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               ++fasts;
             }
-            if (fast && (per_k || h == 0) && rows < kChunk) {  // V's rows of the next segment, which may hold anything
+            if (fast && h == 0 && rows < kChunk) {  // V's rows of the next segment, which may hold anything
               const uint32_t v = 2 * ki + 1;
               if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
                 go = false;
@@ -1177,25 +1134,24 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_before();
             mbar_arrive(&bars->p_full[mine]);
           }
-          if (per_k || h == group - 1) ++ki;
-          if (per_k && h < group - 1) continue;
+          if (h == group - 1) ++ki;
           // Through a tile and a bulk copy: rows stored from registers, a line to a lane, kept the load/store unit so busy that
           // every wait of the other warps took a thousand cycles (40/8/128, one long rollout: 1,260 us).  They are where a
-          // chunk ends inside the tile, and the way back at D = 128, an output to a group's items, where there is no room.
+          // chunk ends inside the tile.
           if ((oi & 1) == mine) {
             if (!mbar_wait_warp(&bars->o_full[mine], (oi >> 1) & 1)) {
               go = false;
               break;
             }
             tc_fence_after();
-            const int head = w.head * p.gx + (per_k ? 0 : h);
-            bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * p.gx) + head) * D;
+            const int head = w.head * group + h;
+            bf16* row = p.out + ((size_t)(w.start + c * kChunk + r) * ((size_t)p.c.heads * group) + head) * D;
             const uint64_t f2 = f2pack(f_out, f_out);
             const uint32_t tb = trow + C::TM_B + oi % C::NB * D;
-            const bool staged = C::STAGE && rows == kChunk;
+            const bool staged = rows == kChunk;
             const uint32_t tile = sbase + C::OFF_O + r * 128;
             // the output before has left the tile (and this one's place in the order of out_full)
-            if (C::STAGE && oi > 0 && !mbar_wait_warp(&bars->out_free[(oi - 1) & 1], ((oi - 1) >> 1) & 1)) {
+            if (oi > 0 && !mbar_wait_warp(&bars->out_free[(oi - 1) & 1], ((oi - 1) >> 1) & 1)) {
               go = false;
               break;
             }
@@ -1226,10 +1182,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 st_global_32(row + g * 32 + 16, *reinterpret_cast<const uint32_t(*)[8]>(&b[8]), p.wide);
               }
             }
-            if (C::STAGE) {
-              fence_proxy_async_smem();
-              mbar_arrive(&bars->out_full);
-            }
+            fence_proxy_async_smem();
+            mbar_arrive(&bars->out_full);
           }
           ++oi;
         }
@@ -1262,40 +1216,24 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         };
         const size_t state = ((size_t)w.seg * p.c.heads + w.head) * D * D + (size_t)r * D;
-        if (!back) {
-          if (w.c0 > 0) add(p.starts + ((size_t)(blockIdx.x - 1) * D + r) * D, 1.f);
-          else if (p.state_in != nullptr) add(p.state_in + state, 1.f);
-          if (p.state_out != nullptr && w.c0 > 0 && w.c1 == w.nch) {  // its last piece's own sum is there
-            float* dst = p.state_out + state;
-            const float f = exp2f(w.l2 * (float)(w.len - w.c0 * kChunk));
+        if (w.c0 > 0) add(p.starts + ((size_t)(blockIdx.x - 1) * D + r) * D, 1.f);
+        else if (p.state_in != nullptr) add(p.state_in + state, 1.f);
+        if (p.state_out != nullptr && w.c0 > 0 && w.c1 == w.nch) {  // its last piece's own sum is there
+          float* dst = p.state_out + state;
+          const float f = exp2f(w.l2 * (float)(w.len - w.c0 * kChunk));
 #pragma unroll
-            for (int i = 0; i < D; i += 4) {
-              float4 x = *reinterpret_cast<const float4*>(dst + i);
-              x.x = fmaf(f, s[i], x.x);
-              x.y = fmaf(f, s[i + 1], x.y);
-              x.z = fmaf(f, s[i + 2], x.z);
-              x.w = fmaf(f, s[i + 3], x.w);
-              *reinterpret_cast<float4*>(dst + i) = x;
-              if (i % 32 == 28) asm volatile("" ::: "memory");
-            }
-          }
-        } else if (w.c1 < w.nch) {
-          if (!p.transposed) {
-            add(p.starts + ((size_t)blockIdx.x * D + r) * D, 1.f);
-          } else {
-#pragma unroll
-            for (int i = 0; i < D; ++i) {
-              s[i] = p.starts[((size_t)blockIdx.x * D + i) * D + r];
-              if (i % 32 == 31) asm volatile("" ::: "memory");
-            }
+          for (int i = 0; i < D; i += 4) {
+            float4 x = *reinterpret_cast<const float4*>(dst + i);
+            x.x = fmaf(f, s[i], x.x);
+            x.y = fmaf(f, s[i + 1], x.y);
+            x.z = fmaf(f, s[i + 2], x.z);
+            x.w = fmaf(f, s[i + 3], x.w);
+            *reinterpret_cast<float4*>(dst + i) = x;
+            if (i % 32 == 28) asm volatile("" ::: "memory");
           }
         }
       }
-      // Pairs weighted before the state of chunk n + 1 is made: those of chunks up to n and, in a group of key heads, whose
-      // next chunk's first is wanted before that chunk's state, that one.
-      const bool fast = w.l2 < kSlow, early = !fast && KIND == BACK;
-      const int64_t pairs = (int64_t)chunks * p.gy;
-      int64_t done = 0;
+      const bool fast = w.l2 < kSlow;
       for (int n = 0; go && n < chunks; ++n, ++ch) {
         const bool weigh = n < chunks - 1;
         // the copy that the chunk's queries read, when the one before has been read
@@ -1304,8 +1242,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           break;
         }
         if (mine) {
-          const int rows = w.rows(back ? w.c1 - 1 - n : w.c0 + n);
-          const float f = fast ? 1.f : exp2f(w.l2 * (float)(back ? rows - kMiddle : kMiddle));
+          const float f = fast ? 1.f : exp2f(w.l2 * (float)kMiddle);
           const uint64_t f2 = f2pack(f, f);
           const uint32_t dst = sbase + C::OFF_S + r * 128;
 #pragma unroll
@@ -1322,41 +1259,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         fence_proxy_async_smem();
         mbar_arrive(&bars->s_ready);
-        int64_t target = (int64_t)(n + 1) * p.gy + (early ? 1 : 0);
-        if (target > pairs) target = pairs;
-        for (; done < target; ++done, ++ki) {
-          const int m = (int)(done / p.gy), rows = w.rows(back ? w.c1 - 1 - m : w.c0 + m);
-          if (fast && m == chunks - 1) {   // no state comes behind the last chunk; in turn with its V all the same
-            const uint32_t v = 2 * ki + 1;
-            if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
-              go = false;
-              break;
-            }
-            mbar_arrive(&bars->wt_full[ki & 3]);
-            continue;
-          }
-          const uint32_t at = 2 * ki + (fast ? 0 : 1), tile = sbase + C::OFF_T + at % C::NT * C::TILE + r * 128;
-          const float wt = exp2f(w.l2 * (float)(fast ? (back ? r : max(rows - 1 - r, 0))
-                                                     : (back ? r - kMiddle : kMiddle - 1 - r)));
+        // the chunk's V weighted, or its K when Q K^T has read it
+        const int rows = w.rows(w.c0 + n);
+        const uint32_t at = 2 * ki + (fast ? 0 : 1), tile = sbase + C::OFF_T + at % C::NT * C::TILE + r * 128;
+        if ((fast && weigh && !mbar_wait_warp(&bars->k_done, handed++ & 1)) ||
+            (fast && !weigh ? !mbar_wait_warp(&bars->t_full[(2 * ki + 1) % C::NT], ((2 * ki + 1) / C::NT) & 1)
+                            : !mbar_wait_warp(&bars->t_full[at % C::NT], (at / C::NT) & 1)) ||
+            __any_sync(0xffffffffu, gave_up())) {
+          go = false;
+          break;
+        }
+        if (!fast || weigh) {   // (no state comes behind a piece's last chunk)
+          const float wt = exp2f(w.l2 * (float)(fast ? kChunk - 1 - r : kMiddle - 1 - r));
           const uint64_t wt2 = f2pack(wt, wt);
-          const uint32_t k_at = 2 * ki, k_tile = sbase + C::OFF_T + k_at % C::NT * C::TILE;
-          const bool hand = fast || (back && m < chunks - 1 && rows < kChunk);
-          if ((hand && (!mbar_wait_warp(&bars->k_done[handed & 1], (handed >> 1) & 1) ||
-                        !mbar_wait_warp(&bars->t_full[k_at % C::NT], (k_at / C::NT) & 1))) ||
-              !mbar_wait_warp(&bars->t_full[at % C::NT], (at / C::NT) & 1) || __any_sync(0xffffffffu, gave_up())) {
-            go = false;
-            break;
-          }
-          if (hand) ++handed;
-          if (hand && !fast && r >= rows) zero_row<D>(k_tile, r);
-          if (fast && rows < kChunk) {   // K^T V comes before P V, whose warps clear them for a piece's last chunk
-            const uint32_t v = 2 * ki + 1;
-            if (!mbar_wait_warp(&bars->t_full[v % C::NT], (v / C::NT) & 1)) {
-              go = false;
-              break;
-            }
-            if (r >= rows) zero_row<D>(sbase + C::OFF_T + v % C::NT * C::TILE, r);
-          }
 #pragma unroll 1
           for (int kb = 0; kb < D / 32; ++kb) {   // four loads under way
             uint4 x[4];
@@ -1378,8 +1293,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           fence_proxy_async_smem();
-          mbar_arrive(&bars->wt_full[ki & 3]);
         }
+        mbar_arrive(&bars->wt_full[ki++ & 3]);
         if (!go || !weigh) continue;
         if (!mbar_wait_warp(&bars->u_full, sums++ & 1)) {
           go = false;
@@ -1387,9 +1302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         tc_fence_after();
         if (mine) {
-          const int rows = w.rows(back ? w.c1 - 1 - n : w.c0 + n);
-          const float f = exp2f(w.l2 * (float)rows);
-          const float fu = fast ? 1.f : exp2f(w.l2 * (float)(back ? kMiddle : rows - kMiddle));
+          const float f = exp2f(w.l2 * (float)kChunk), fu = fast ? 1.f : exp2f(w.l2 * (float)(kChunk - kMiddle));
           const uint64_t f2 = f2pack(f, f), fu2 = f2pack(fu, fu);
 #pragma unroll
           for (int g = 0; g < D / 16; ++g) {
@@ -2163,42 +2076,39 @@ cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, con
   return cudaGetLastError();
 }
 
-template <int D, int KIND>
-cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int gx, int gy,
-                       bool transposed, const float* state_in, float* state_out, void* out,
-                       cudaStream_t st) {
-  using C = Lin<D, KIND>;
+template <int D, bool ONE>
+cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
+                       const float* state_in, float* state_out, void* out, cudaStream_t st) {
+  using C = Lin<D, ONE>;
   alignas(64) CUtensorMap tq, tk, tv, to;
-  const int64_t hx = (int64_t)a.hkv * gx, hy = (int64_t)a.hkv * gy;
-  if (!encode(&tq, q, D, hx, a) || !encode(&tk, k, D, hy, a) || !encode(&tv, v, D, hy, a) || !encode(&to, out, D, hx, a))
+  if (!encode(&tq, q, D, a.hq, a) || !encode(&tk, k, D, a.hkv, a) || !encode(&tv, v, D, a.hkv, a) ||
+      !encode(&to, out, D, a.hq, a))
     return cudaErrorInvalidValue;
-  const void* fn = reinterpret_cast<const void*>(linear_out<D, KIND>);
+  const void* fn = reinterpret_cast<const void*>(linear_out<D, ONE>);
   static std::atomic<int> regs_cache{-1};
   bool regs_ok = false;
   if (cudaError_t e = launch_regs_match(fn, kRegLaunch, &regs_cache, &regs_ok); e != cudaSuccess) return e;
   if (!regs_ok) return cudaErrorInvalidConfiguration;
-  cudaError_t e = cudaFuncSetAttribute(linear_out<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  cudaError_t e = cudaFuncSetAttribute(linear_out<D, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   OutArgs p;
   p.c = w.c;
   p.starts = w.starts;
   p.state_in = state_in;
   p.state_out = state_out;
-  p.gx = gx;
-  p.gy = gy;
+  p.group = group;
   p.scale = a.scale;
-  p.transposed = transposed;
   p.out = static_cast<bf16*>(out);
   p.wide = (reinterpret_cast<uintptr_t>(out) & 31u) == 0;
-  linear_out<D, KIND><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, to, p);
+  linear_out<D, ONE><<<w.grid, kThreads, C::SMEM, st>>>(tq, tk, tv, to, p);
   return cudaGetLastError();
 }
 
 template <int D>
 cudaError_t launch_forth(const Work& w, const LinearArgs& a, const void* q, const void* k, const void* v, int group,
                          const float* state_in, float* state_out, void* out, cudaStream_t st) {
-  return group == 1 ? launch_out<D, FWD1>(w, a, q, k, v, 1, 1, false, state_in, state_out, out, st)
-                    : launch_out<D, FWD>(w, a, q, k, v, group, 1, false, state_in, state_out, out, st);
+  return group == 1 ? launch_out<D, true>(w, a, q, k, v, 1, state_in, state_out, out, st)
+                    : launch_out<D, false>(w, a, q, k, v, group, state_in, state_out, out, st);
 }
 
 template <int D>
