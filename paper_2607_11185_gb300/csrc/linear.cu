@@ -686,7 +686,7 @@ struct Lin {
   // K^T (MN-major) x V (MN-major).  M = 128 at D = 64 too, whose lanes 64 .. 127 take the tile behind K's (or the
   // state) and are not read: an M of 64 lies in other lanes.
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
-  static constexpr int REG_CTRL = 80, REG_ROWS = 104, REG_STATE = 224;
+  static constexpr int REG_CTRL = 96, REG_ROWS = 104, REG_STATE = 208;
   static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
   static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
   static_assert(D == 128 || NT % 2 == 0, "behind a K tile lies another tile");
@@ -789,7 +789,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars->s_full[i], 1);
-      mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->p_full[i], 4);
       mbar_init(&bars->a_full[i], 1);
       mbar_init(&bars->o_full[i], 1);
       mbar_init(&bars->o_free[i], 4);
@@ -1132,7 +1132,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(&bars->p_full[mine]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars->p_full[mine]);
           }
           if (h == group - 1) ++ki;
           // Through a tile and a bulk copy: rows stored from registers, a line to a lane, kept the load/store unit so busy that
@@ -1360,7 +1361,7 @@ struct Bck {
   static constexpr uint32_t IDESC_V = idesc_bf16(128, D, 0, 1);    // K (K-major) x S (MN-major), P (TMEM) x dO or Q
   static constexpr uint32_t IDESC_K = idesc_bf16(128, D, 0, 0);    // V (K-major) x S^T (K-major)
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);    // Q^T (MN-major) x dO (MN-major); see Lin for M
-  static constexpr int REG_CTRL = 80, REG_ROWS = 104, REG_STATE = 224;
+  static constexpr int REG_CTRL = 96, REG_ROWS = 104, REG_STATE = 208;
   static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
   static_assert(SMEM <= 232448 && TM_U + D <= 512, "shared memory and TMEM budgets");
 };
@@ -1421,7 +1422,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(&bars->k_empty[i][j], 1);
       }
       mbar_init(&bars->s_full[i], 1);
-      mbar_init(&bars->p_full[i], 128);
+      mbar_init(&bars->p_full[i], 4);
       mbar_init(&bars->a_full[i], 1);
       mbar_init(&bars->o_full[i], 1);
       mbar_init(&bars->o_free[i], 4);
@@ -1725,7 +1726,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_wait();
           tc_fence_before();
-          mbar_arrive(&bars->p_full[x]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->p_full[x]);
         }
         if (!go || !mbar_wait_warp(&bars->o_full[x], ck & 1)) {
           go = false;
