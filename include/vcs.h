@@ -584,10 +584,17 @@ vcs_status vcs_group_advantage(const float* rewards, int64_t num_groups, int32_t
  *   dev_status       int32 device-visible word or NULL, zeroed by the caller:
  *                    VCS_ERR_DEVICE_CHECK as above (that head is left out)
  *
- * States, decays and sums are fp32.  The forward's products between tokens of
- * a chunk, and a chunk's starting state where queries read it, are rounded to
- * bf16; the states handed from chunk to chunk and state_out are not.  The same
- * inputs give the same bits.
+ * States, decays and sums are fp32.  Rounded to bf16 are, in both directions,
+ * the products between tokens of a chunk of 128, one factor of theirs weighted
+ * by the decay (v; of a head with a log2 decay below -1 k; backward q), and
+ * the copy of a state that the chunk's queries read; state_out is not rounded.
+ * A weight of 2^-150 and less is 0.  Of heads whose log2 decay lies between -1
+ * and 0 weights of up to 2^64 are taken and given back, so that sums beyond
+ * 2^63 overflow.  An input that is not finite may reach the results of its
+ * whole chunk, earlier tokens' too, and of all that read the chunk's state,
+ * but no other segment.  The same inputs give the same bits; o may differ in
+ * its roundings between calls with and without state_out where a segment has
+ * more than 2,048 tokens.
  * Return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
  * bytes) pointers or overlapping outputs; VCS_ERR_UNSUPPORTED for d other
  * than 64 and 128, hq not a multiple of hkv or more than 65,535 heads;
@@ -645,8 +652,11 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
  *   ws          device workspace of vcs_distill_topk_workspace_size(rows)
  *               bytes, 256-byte aligned; its first int32 is the device status
  *               word: VCS_ERR_DEVICE_CHECK for an id outside [-1, vocab) (read
- *               as -1) or a list outside [0, lists) (read as empty)
- * Sums and statistics are fp32 and wider; the same inputs give the same bits.
+ *               as -1) or a list outside [0, lists) (read as empty),
+ *               VCS_ERR_DEVICE_TIMEOUT
+ * Sums and statistics are fp32 and wider; the same inputs give the same bits
+ * (with and without dlogits, or in another number of rows, the order of a
+ * row's sums may be another one).
  * Returns VCS_ERR_INVALID_ARG for negative counts, vocab or top of 0, a null
  * pointer, one that is not aligned to its elements, a stride below vocab, a
  * bad temperature, lists < rows without teacher_rows, or overlap;

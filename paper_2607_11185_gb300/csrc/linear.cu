@@ -2,23 +2,25 @@
 //
 // With lam = exp(log_decay) of the head, over the tokens t of a segment:
 //   S_t = lam S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t
-// Its gradients are calls of the same kind: with R_t = lam R_{t+1} + sum_group q_t do_t^T,
-//   dq_t = scale S_t do_t   (queries do, keys v, values k)
-//   dk_t = scale R_t v_t    (queries v, keys do, values q, from the last token to the first)
-//   dv_t = scale R_t^T k_t  (queries k, keys q, values do, likewise)
-// where the first has a group of query heads to a state, the others a group of key heads.
+// Its gradients are sums of the same kind: with R_t = lam R_{t+1} + sum_group q_t do_t^T,
+//   dq_t = scale S_t do_t   (the same call: queries do, keys v, values k)
+//   dk_t = scale R_t v_t,  dv_t = scale R_t^T k_t   (linear_back, from the last token to the first)
 //
 // Chunks of 128 tokens.  From the state S before a chunk's first token, for its n tokens i, j = 0 .. n - 1:
 //   o_i = scale [ lam^(i+1) q_i S + sum_{j <= i} lam^(i-j) (q_i . k_j) v_j ],
 //   S'  = lam^n S + sum_j lam^(n-1-j) k_j v_j^T
-// four 128-wide products a chunk on the tensor pipe (the other way in time: lam^(n-i), j >= i, lam^j).
+// four 128-wide products a chunk on the tensor pipe.
 //
-// A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among the
-// CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.  linear_states
-// adds up the keys and values before every cut, as far back as the decay leaves anything in fp32, in parts of equal size
-// spread over the chip, and linear_join makes the cuts' states of them.  So a cut costs its piece's keys and values
-// read twice.  (A CTA that adds up the piece before its own cut takes as long as the head that forgets slowest: the three
-// passes of a backward pass at 40 / 8 heads of 128 and 135,512 tokens 955 us, the parts 480 with what joins them.)
+// A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among
+// the CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.
+// linear_states adds up the keys and values before every cut, as far back as the decay leaves anything in fp32, in
+// parts of equal size spread over the chip, and linear_join makes the cuts' states of them.  So a cut costs its
+// piece's keys and values read twice.  (A CTA that adds up the piece before its own cut takes as long as the head that
+// forgets slowest: the three passes of a training step over one rollout of 246,616 tokens at 40 / 8 heads of 128 955
+// us, the parts 480 with what joins them.)
+//
+// One rollout as above, us: the outputs 940 (6.06 GB, 6.45 TB/s), the states at the cuts 74 for K and V, 283 for a
+// group's Q and dO (about 6 TB/s of what the decays leave of them) and 16 to join them, dK and dV 1,545.
 
 #include <cfloat>
 #include <cstdint>
@@ -634,7 +636,8 @@ __global__ void __launch_bounds__(256) linear_join(const __grid_constant__ JoinA
   bool faded = false;
   for (int x = t; !faded && x >= 0 && x < kGrid; p.back ? ++x : --x) {
     const int64_t gap = p.back ? plan.range * (x + 1) - g : g - plan.range * (x + 1);   // chunks between the cuts
-    if (p.back ? plan.range * (x + 1) >= w.base + w.nch : plan.range * (x + 1) <= w.base) break;   // in another sequence
+    // in another sequence
+    if (p.back ? plan.range * (x + 1) >= w.base + w.nch : plan.range * (x + 1) <= w.base) break;
     const int first = p.all ? x : plan.first[p.back][x], end = p.all ? x + 1 : plan.first[p.back][x + 1];
     for (int i = first; i < end; ++i) {
       const float f = exp2f(l2 * (float)((gap + (int64_t)(i - first) * size) * kChunk));
@@ -664,9 +667,9 @@ struct OutArgs {
 template <int D, bool ONE>
 struct Lin {
   static constexpr int TILE = kChunk * D * 2;
-  // Tiles of Q, and of K and V, which take turns.  A load takes 2 to 4 thousand cycles under way and an item the memory 3 to
-  // 6, so that what streams has to have two to three tiles on its way: a group of query heads streams Q, one head of each
-  // K and V too.
+  // Tiles of Q, and of K and V, which take turns.  A load takes 2 to 4 thousand cycles under way and an item the
+  // memory 3 to 6, so that what streams has to have two to three tiles on its way: a group of query heads streams Q,
+  // one head of each K and V too.
   static constexpr int NQ = D == 64 ? 4 : ONE ? 1 : 2;
   static constexpr int NT = D == 64 ? 8 : ONE ? 4 : 3;
   // Buffers of Q K^T and P: two if K^T V and two outputs leave room.  Outputs: two.
@@ -703,7 +706,7 @@ struct LinBars {
   uint64_t out_full;   // an output is in its tile, or its rows are written
   uint64_t out_free[2];  // and on its way, of one warpgroup's or the other's (each waits for the other's, in turn)
   uint64_t k_done;     // a K that is to be weighted is no longer read as it was loaded
-  uint64_t wt_full[4]; // a pair's V, or K, is weighted; four, as the warps that do it may be some pairs ahead of the issuer
+  uint64_t wt_full[4]; // a pair's V, or K, is weighted; four, as the warps that do it may be some pairs ahead
   uint64_t u_full;     // the chunk's K^T V
   uint64_t u_free;     // and in registers
   uint64_t s_ready;    // the state that the chunk's queries read is in shared memory
@@ -732,15 +735,19 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8], bo
 //   o_i = scale lam^(i+1-m) [ q_i (lam^m S) + sum_{j <= i} (q_i . k_j) w_j ],  w_j = lam^(m-1-j) v_j,
 //   S'  = lam^n S + lam^(n-m) sum_j k_j w_j^T
 // so that P = Q K^T below the diagonal has no factors at all, V is weighted once for both products, as soon as it is
-// loaded, and the row's factor comes last, as long as lam^-m stays in range: 2^64 at most (kSlow).  For a head that forgets
-// faster P has the exact powers, the rows of Q S are scaled in TMEM, and K is weighted for the state when Q K^T has read it.
+// loaded, and the row's factor comes last, as long as lam^-m stays in range: 2^64 at most (kSlow).  For a head that
+// forgets faster P has the exact powers, the rows of Q S are scaled in TMEM, and K is weighted for the state when Q
+// K^T has read it.
 constexpr int kMiddle = 64;
 constexpr float kSlow = -1.0f;   // log2 of the decay
 
-// An item is a chunk with one query head.
+// An item is a chunk with one query head.  What bounds it is memory: Q in and O out, 64 KB an item at D = 128, 3,400
+// cycles at the copy rate, of which the MMAs take 1,700.  Two warps issue them, as one is held up by its waits and
+// commits (90 cycles a wait that is met): 975 -> 940 us a pass over one rollout at 40 / 8 heads of 128, 97 -> 86 over
+// eight short ones at 14 / 2 of 64, where an item is 1,500 cycles of memory and takes 2,000.
 // Warp roles:
 //   warp 0       loads;  warp 2  O out of shared memory
-//   warps 1, 3   MMAs: Q K^T and K^T V (and TMEM);  Q S and P V.  (One warp for all is held up by its waits and commits: ....)
+//   warps 1, 3   MMAs: Q K^T and K^T V (and TMEM);  Q S and P V
 //   warps 4-11   two warpgroups, for every other item: P below the diagonal, in bf16 for P V (a thread a query), then
 //                O out of TMEM, scaled
 //   warps 12-15  the weighted tiles, and the state in registers (a thread a row), its bf16 copy in shared memory
@@ -847,10 +854,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!go) set_abort(&bars->abort, p.c.status);
     } else if (warp == 1) {
       // -------------------------------------------------------- MMAs of Q K^T and of the state
-      // Every lane of an issuer runs every step, no lane's answer to a wait decides where the warp goes, and a vote an item
-      // ends the walk.  A chunk's K^T V comes behind its second item's Q K^T (its only one's): V is weighted by then, and the
-      // next chunk's state is made while this one's queries are worked on; for a head that forgets fast behind the last
-      // item's, when K is weighted.
+      // Every lane of an issuer runs every step, no lane's answer to a wait decides where the warp goes, and a vote an
+      // item ends the walk.  A chunk's K^T V comes behind its second item's Q K^T (its only one's): V is weighted by
+      // then, and the next chunk's state is made while this one's queries are worked on; for a head that forgets fast
+      // behind the last item's, when K is weighted.
       const uint64_t qd = smem_desc(sbase + C::OFF_Q, 16, 1024);
       const uint64_t kd = smem_desc(sbase + C::OFF_T, 16, 1024), kt = smem_desc(sbase + C::OFF_T, 16384, 1024);
       bool ok = true, go = true;
@@ -866,7 +873,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t q = it % C::NQ;
             if (h == 0) ok = ok && mbar_wait(&bars->t_full[ks], (2 * ki / C::NT) & 1);
             ok = ok && mbar_wait(&bars->q_full[q], (it / C::NQ) & 1);
-            if (it >= C::NP) ok = ok && mbar_wait(&bars->o_full[(it - C::NP) & 1], ((it - C::NP) >> 1) & 1);   // its P was read
+            // its P was read
+            if (it >= C::NP) ok = ok && mbar_wait(&bars->o_full[(it - C::NP) & 1], ((it - C::NP) >> 1) & 1);
             go = __all_sync(0xffffffffu, ok);
             if (!go) break;
             tc_fence_after();
@@ -917,7 +925,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool fast = w.l2 < kSlow;
         const uint32_t q = qi % C::NQ;
         if (h == 0) ok = ok && mbar_wait(&bars->s_ready, ck++ & 1);
-        if (qi >= 2) ok = ok && mbar_wait(&bars->o_free[qi & 1], ((qi - 2) >> 1) & 1);   // the output before is in registers
+        // the output before is in registers
+        if (qi >= 2) ok = ok && mbar_wait(&bars->o_free[qi & 1], ((qi - 2) >> 1) & 1);
         ok = ok && mbar_wait(&bars->q_full[q], (qi / C::NQ) & 1);
         tc_fence_after();
         if (elect_one() && ok) {
@@ -943,7 +952,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int h = 0; h < group; ++h, ++it) {
             const bool last = h == group - 1;
             if (h == 0 && fast) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
-            // (a fast head's last V is not weighted, but its slot is not given back before the warps that do it have passed it)
+            // (a fast head's last V is not weighted, but its slot is not given back before the warps that do it have
+            // passed it)
             if (h == 0 && !(fast && weigh)) ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
             ok = ok && mbar_wait(&bars->p_full[it & 1], (it >> 1) & 1);
             go = __all_sync(0xffffffffu, ok);
@@ -1018,8 +1028,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               break;
             }
             tc_fence_after();
-            // Loops over columns are not unrolled: the roles' code together outgrows the instruction cache.  P goes over
-            // columns of Q K^T that have been read.
+            // Loops over columns are not unrolled: the roles' code together outgrows the instruction cache.  P goes
+            // over columns of Q K^T that have been read.
             if (!fast) {
 #pragma unroll 1
               for (int g = 0; g < 4; ++g) {
@@ -1033,7 +1043,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                   tmem_ld_wait();
                   reg_fence<32>(s);
                   if (g == quad) {
-                    const uint32_t seen = 0xffffffffu >> (31 - lane);   // columns of the group that the row takes, a bit each
+                    // columns of the group that the row takes, a bit each
+                    const uint32_t seen = 0xffffffffu >> (31 - lane);
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                       if (!(seen >> i & 1)) s[i] = 0u;
@@ -1045,9 +1056,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_st_32x32b_x16(tp + g * 16, *reinterpret_cast<uint32_t(*)[16]>(&s[0]));
               }
             } else {
-              // lam^|r - c|: in a group of 32 columns that the diagonal does not cross a power for the row, from the group's
-              // near end, times one of 32 for the column, at most 1 both; in the diagonal's, powers of the exact distances,
-              // so that a token sees itself with weight 1.
+              // lam^|r - c|: in a group of 32 columns that the diagonal does not cross a power for the row, from the
+              // group's near end, times one of 32 for the column, at most 1 both; in the diagonal's, powers of the
+              // exact distances, so that a token sees itself with weight 1.
 #pragma unroll 1
               for (int g = 0; g < 4; ++g) {
                 uint32_t pk[16];
@@ -1136,9 +1147,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) mbar_arrive(&bars->p_full[mine]);
           }
           if (h == group - 1) ++ki;
-          // Through a tile and a bulk copy: rows stored from registers, a line to a lane, kept the load/store unit so busy that
-          // every wait of the other warps took a thousand cycles (40/8/128, one long rollout: 1,260 us).  They are where a
-          // chunk ends inside the tile.
+          // Through a tile and a bulk copy: rows stored from registers, a line to a lane, kept the load/store unit so
+          // busy that every wait of the other warps took a thousand cycles (40/8/128, one long rollout: 1,260 us).
+          // They are where a chunk ends inside the tile.
           if ((oi & 1) == mine) {
             if (!mbar_wait_warp(&bars->o_full[mine], (oi >> 1) & 1)) {
               go = false;
@@ -1382,19 +1393,22 @@ struct BckBars {
 };
 static_assert(sizeof(BckBars) <= 512, "barrier space");
 
-// dK and dV of a chunk together, from the last chunk to the first: with m = 64 and w_i = lam^(i-m) q_i, weighted in place
-// as soon as it is loaded,
+// dK and dV of a chunk together, from the last chunk to the first: with m = 64 and w_i = lam^(i-m) q_i, weighted in
+// place as soon as it is loaded,
 //   dv_j = scale lam^(m-j) [ k_j (lam^(n-m) R) + sum_{i >= j} (k_j . w_i) do_i ]
 //   dk_j = scale lam^(m-j) [ v_j (lam^(n-m) R)^T + sum_{i >= j} (v_j . do_i) w_i ]
 //   R'   = lam^n R + lam^m sum_i w_i do_i^T
-// with one load of q and do and one state for both.  (A pass each loads them twice and has six products an item, not five:
-// 40 / 8 heads of 128, 135,512 tokens, ... .)  Both factors are at most 2^64 (kSlow); for a head that forgets faster both P have
-// the exact powers, the rows of the products with R are scaled in TMEM, and Q is weighted when they have read it.
+// with one load of q and do and one state for both.  (A pass each loads them twice and has six products an item, not
+// five: 2,166 us over one rollout of 246,616 tokens at 40 / 8 heads of 128, this 1,545.)  Both factors are at most
+// 2^64 (kSlow); for a head that forgets faster both P have the exact powers, the rows of the products with R are
+// scaled in TMEM, and Q is weighted when they have read it.
 //
-// An item is a chunk with one query head; a step an item's QN queries.  Three warps issue MMAs, each its own chain and in
-// order: dV's  P dO, K Q^T of the next step;  dK's  P Q, V dO^T of the next step;  the state's  Q^T dO of an item.  A chunk's
-// products with R come in its second item (of one, the first): R has had an item's time.  (One warp for all is held up by
-// its waits and commits: 1,940 us of dK and dV at 40 / 8 heads of 128 and 135,512 tokens, ....)
+// An item is a chunk with one query head; a step an item's QN queries.  Three warps issue MMAs, each its own chain and
+// in order: dV's  P dO, K Q^T of the next step;  dK's  P Q, V dO^T of the next step;  the state's  Q^T dO of an item.
+// A chunk's products with R come in its second item (of one, the first): R has had an item's time.  One warp for all
+// is held up by its waits and commits: 1,940 us of the rollout above.  What bounds it now is the chain of a step, a
+// product's P into TMEM and back: 2,500 cycles, of which the MMAs of both chains and the state take 1,536 and memory
+// 1,690.  (At D = 64 a second buffer of steps does not shorten it: 2,600 cycles an item of 1,408 with one or two.)
 //   warp 0  loads;  warps 1, 3  MMAs of dV and of dK;  warp 2  TMEM, MMAs of the state
 //   warps 4-7    P of K Q^T, dV;  warps 8-11  P of V dO^T, dK  (a thread a key)
 //   warps 12-15  weighted Q, and the state in registers (a thread a row), its bf16 copy in shared memory
@@ -1901,8 +1915,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ------------------------------------------------------------------ single tokens
-// A block takes COLS columns of one head's state: a row's lanes hold four columns each, and a thread R rows, all loaded
-// before the first is used.  The state is read and written once: what bounds it is memory.
+// A block takes COLS columns of one head's state: a row's lanes hold four columns each, and a thread R rows, all
+// loaded before the first is used.  The state is read and written once: what bounds it is memory (512 sequences at 40
+// / 8 heads of 128, 537 MB: 84 us, 6.4 TB/s).
 struct StepArgs {
   const bf16 *q, *k, *v;
   const float* log_decay;
@@ -1997,8 +2012,8 @@ namespace {
 
 inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-// Workspace: header (status word), the plan, the segments' chunk offsets, and, where a sequence may be cut, the parts' sums
-// (three to a CTA at most) and the states at the cuts.
+// Workspace: header (status word), the plan, the segments' chunk offsets, and, where a sequence may be cut, the parts'
+// sums (three to a CTA at most) and the states at the cuts.
 int32_t grid_of(int32_t num_segments, int64_t num_tokens, int32_t hkv) {
   const int64_t chunks = hkv * (num_tokens / kChunk + (int64_t)num_segments);   // no fewer than the sequences'
   return (int32_t)(chunks < kGrid ? chunks : kGrid);

@@ -1,12 +1,13 @@
 """GPU parity of linear attention against the fp64 oracle.
 
 Elementwise bounds, from the roundings (u = 2^-8, half a step of bf16).  An output is a sum of terms
-lam^(i-j) q_ia k_ja v_je; the products between the tokens of a chunk are rounded once to bf16 (u), a term that comes
-through the state twice at most (the weighted key, and the state that the query reads: 2 u), and the output once:
+lam^(i-j) q_ia k_ja v_je, each with two roundings to bf16 at most: between the tokens of a chunk the weighted value (the
+gradients of keys and values: the weighted query) and the product that multiplies it; through the state the weighted
+value or key, and the state that the query reads.  The output itself is rounded once:
   |error| <= (2 u + u^2 + 2^-15) sum |terms| + u |o|
 where 2^-15 holds the fp32 additions (2^-24 each; up to a chunk's 128 and a chunk's states one after another), the
 decays' own rounding (a weight e^-x is off by x 2^-23, at most 0.4 2^-23 of 1) and their products from chunk to chunk.
-States carry no bf16 rounding but a key split into two (2^-16 of it):
+States carry no bf16 rounding but a weighted key in three terms, which hold its 24 bits:
   |error| <= 2^-14 sum |terms|
 The gradients are sums of the same kind, over their own terms.
 """
