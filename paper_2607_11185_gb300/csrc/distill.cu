@@ -450,12 +450,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
-  uint32_t at;
-  float x;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
-  return x;
+// {x, y} at `dst` of a CTA of the cluster, whose barrier counts the 8 bytes (addresses as in this CTA).
+__device__ __forceinline__ void send(float* dst, uint64_t* bar, uint32_t rank, float x, float y) {
+  uint32_t at, on;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(dst)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(on) : "r"(smem_u32(bar)), "r"(rank));
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(x),
+               "f"(y), "r"(on)
+               : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
@@ -470,8 +472,9 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
   __shared__ __align__(16) int32_t ids[kMaxTop];
   __shared__ __align__(16) float ps[kMaxTop];
   __shared__ double red64[W];
-  __shared__ float red_m[W], red_s[W], red_t[W], red_p[W], red_k[W], peer[2][2];   // peer: the CTA's maximum and sum, by turns
-  __shared__ uint64_t full[kParts];
+  __shared__ float red_m[W], red_s[W], red_t[W], red_p[W], red_k[W];
+  __shared__ __align__(16) float peer[2][8][2];   // the CTAs' maxima and sums, by turns
+  __shared__ uint64_t full[kParts], met[2];
   __shared__ bool last;
   const float k = a.k;
   const uint64_t kk = f2pack(k, k);
@@ -480,9 +483,14 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
   const uint32_t base_s = smem_u32(held);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kParts; ++i) mbar_init(&full[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&met[i], 1);
     fence_mbar_init();
   }
   __syncthreads();
+  if (size > 1) {   // the others' barriers are there
+    cluster_arrive();
+    cluster_wait();
+  }
   // A row's vectors, from its first 16-byte boundary on, and this CTA's share of them.
   struct Row {
     const T* z;
@@ -593,12 +601,11 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
 #pragma unroll
     for (int i = 1; i < W; ++i) tmax = fmaxf(tmax, red_t[i]);
     join_warps<W>(red_m, red_s, k, sum.m, sum.s);
-    if (size > 1) {   // by turns: whoever writes a turn's words again has met all that read them
-      if (threadIdx.x == 0) {
-        peer[turn & 1][0] = sum.m;
-        peer[turn & 1][1] = sum.s;
-      }
-      cluster_arrive();
+    // Each CTA's maximum and sum to all of them: no store of a gradient is waited for, as a barrier of the cluster does.  By
+    // turns: whoever writes a turn's words again has met all that read them.
+    if (size > 1) {
+      if (threadIdx.x == 0) mbar_arrive_expect_tx(&met[turn & 1], 8 * size);
+      if ((int)threadIdx.x < size) send(peer[turn & 1][rank], &met[turn & 1], threadIdx.x, sum.m, sum.s);
     }
     float mine = en.weigh(a, tmax);
     if (wid < warps) {
@@ -610,12 +617,12 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
 #pragma unroll
     for (int i = 0; i < E; ++i) place[i] = en.place(a, ids, i);
     if (size > 1) {
-      cluster_wait();
+      ok = ok && mbar_wait(&met[turn & 1], turn >> 1 & 1);
       float m[8], s[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        m[i] = i < size ? ld_cluster(&peer[turn & 1][0], i) : -INFINITY;
-        s[i] = i < size ? ld_cluster(&peer[turn & 1][1], i) : 0.f;
+        m[i] = i < size ? peer[turn & 1][i][0] : -INFINITY;
+        s[i] = i < size ? peer[turn & 1][i][1] : 0.f;
       }
       join_warps<8>(m, s, k, sum.m, sum.s);
     }
@@ -689,7 +696,7 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
     __syncthreads();   // the lists are read
   }
   if (!ok) set_status(a.status, VCS_ERR_DEVICE_TIMEOUT);
-  if (size > 1) {   // the others may read this CTA's words
+  if (size > 1) {   // what this CTA sent has arrived before the others end, and they have its words
     cluster_arrive();
     cluster_wait();
   }
