@@ -768,6 +768,11 @@ cudaError_t launch_rows(const Args& a, cudaStream_t st) {
       return a.top <= kHeldThreads ? launch_held<T, 1>(a, l, (size_t)share, st)
                                    : launch_held<T, (kMaxTop + kHeldThreads - 1) / kHeldThreads>(a, l, (size_t)share, st);
   }
+  // Between a row's last load and the next one's first lie its sums and its list.  With more rows than large blocks smaller
+  // ones take turns at that (us, blocks of 128, 256 and 512 threads: 20,000 rows of 10,000 fp32 167, 194, 302; 4,096 of
+  // 131,072 bf16 193, 188, 202; 512 of 99,991 fp32 65, 54, 57), with fewer a large one has more loads under way (304 of
+  // these 58, 44, 38).
+  if (a.dz == nullptr && a.rows > 2 * 152) return bytes <= kShare ? launch_block<T, 128>(a, st) : launch_block<T, 256>(a, st);
   return launch_block<T, 512>(a, st);
 }
 
