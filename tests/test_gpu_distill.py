@@ -270,3 +270,23 @@ def test_rows_past_2_31_elements():
     # (few rows are split over more of the chip, in another order of their sums: 2^-16 of both, a step of the rounding)
     assert ((kl[-3:] - want[1]).abs() <= 2.0 ** -16).all()
     assert ((g[-3:].double() - want[2].double()).abs() <= (2.0 ** -15 + 2.0 ** -7) * want[2].double().abs()).all()
+
+
+@pytest.mark.parametrize("dtype,vocab,rows", [(torch.bfloat16, 131_072, 5), (torch.float32, 160_000, 3), (torch.bfloat16, 32_000, 200),
+                                              (torch.bfloat16, 3001, 700), (torch.float32, 2_000_003, 1)])
+def test_in_place_and_entries_twice_on_every_route(dtype, vocab, rows):
+    # one CTA a row, clusters of them, blocks in turn, rows beyond a cluster; a list's ids from few, at both ends of the row
+    vcs = _vcs()
+    z, ids, t, w = draw(vocab, rows, vocab, 64, dtype)
+    ids = torch.where(ids % 2 == 0, ids % 20, vocab - 1 - ids % 20).contiguous()
+    check(z, ids, t, w, temp=0.7)
+    loss, kl, want = vcs.distill_topk(z, ids, t, w, temperature=0.7)
+    over = z.clone()
+    again = vcs.distill_topk(over, ids, t, w, temperature=0.7, out=over)
+    assert again[2] is over and torch.equal(over, want) and torch.equal(again[0], loss) and torch.equal(again[1], kl)
+
+
+@pytest.mark.parametrize("rows", [304, 305, 1300])
+def test_the_loss_alone_by_blocks_of_every_size(rows):
+    z, ids, t, w = draw(rows, rows, 9001 if rows < 1000 else 40_007, 20, torch.bfloat16)
+    check(z, ids, t, w)

@@ -376,3 +376,66 @@ def test_rows_past_2_31_elements():
     r = olin.grads(*end, g, [0, 333])
     for x, name in zip(grads, ("dq", "dk", "dv")):
         near(f64(x[-333:]), r[name], r[name + "_abs"], name)
+
+
+def test_no_tokens_and_no_segments():
+    vcs = _vcs()
+    q, k, v, do = draw(6, [7], 4, 2, 64)
+    none = [x[:0] for x in (q, k, v, do)]
+    g, st = decays(-0.1, 0.0), torch.randn(3, 2, 64, 64, device="cuda")
+    cu = torch.zeros(4, dtype=torch.int32, device="cuda")
+    o, end = vcs.linear_attn_fwd(*none[:3], g, cu, state=st, with_state=True)
+    assert o.shape == (0, 4, 64) and torch.equal(end, st)
+    o, end = vcs.linear_attn_fwd(*none[:3], g, cu, with_state=True)
+    assert (end == 0).all()
+    assert all(x.shape[0] == 0 for x in vcs.linear_attn_bwd(*none, g, cu))
+    o, end = vcs.linear_attn_fwd(q, k, v, g, cu[:1], with_state=True)
+    assert o.shape == q.shape and end.shape[0] == 0
+    o, end = vcs.linear_attn_fwd(q, k, v, g, cu, state=st, with_state=True)   # segments without tokens among some
+    assert torch.equal(end, st)
+    assert vcs.linear_attn_step(*none[:3], g, st[:0]).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("d,hq,hkv,n", [(64, 1024, 1, 140), (128, 320, 320, 30), (64, 600, 300, 300), (128, 200, 1, 2100)])
+def test_many_heads(d, hq, hkv, n):
+    lens = [n // 2, n - n // 2] if n < 2000 else [n]
+    q, k, v, do = draw(hq, lens, hq, hkv, d)
+    g = decays(*np.linspace(-3, 0, hkv).tolist())
+    vcs = _vcs()
+    cu = cu_from_lengths(lens)
+    cud = torch.from_numpy(cu).cuda()
+    o, end = vcs.linear_attn_fwd(q, k, v, g, cud, with_state=True)
+    grads = vcs.linear_attn_bwd(q, k, v, do, g, cud)
+    for h in sorted({0, hkv // 2, hkv - 1}):    # a state's heads by themselves
+        x = slice(h * hq // hkv, (h + 1) * hq // hkv)
+        part = [q[:, x], k[:, h:h + 1], v[:, h:h + 1], do[:, x]]
+        r = olin.attn(*part[:3], g[h:h + 1], cu)
+        near(f64(o[:, x]), r["o"], r["o_abs"], "o")
+        within(f64(end[:, h:h + 1]), r["state"], ST * r["state_abs"], "state")
+        r = olin.grads(*part, g[h:h + 1], cu)
+        for got, name, y in zip(grads, ("dq", "dk", "dv"), (x, slice(h, h + 1), slice(h, h + 1))):
+            # (dk and dv of a group of hundreds: as many more additions, 2^-24 of the sum each)
+            near(f64(got[:, y]), r[name], r[name + "_abs"], name)
+
+
+def test_thousands_of_segments():
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 6, size=2600)]
+    check(*draw(7, lens, 2, 1, 64), decays(-0.2), lens)
+
+
+def test_states_past_2_31_elements():
+    n, hkv, d = 16_600, 8, 128
+    assert (n - 3) * hkv * d * d > 2 ** 31
+    vcs = _vcs()
+    q, k, v, _ = draw(8, [n], 8, hkv, d)
+    st = torch.zeros(n, hkv, d, d, device="cuda")
+    st[-2:] = torch.randn(2, hkv, d, d, device="cuda")
+    before = st[-3:].clone()
+    g = decays(*([-0.1, 0.0] * 4))
+    o = vcs.linear_attn_step(q, k, v, g, st)
+    want, end = olin.walk(q[-3:], k[-3:], v[-3:], g, [0, 1, 2, 3], state=before)
+    # states: three roundings of 2^-24 of at most 30; outputs: half a step of bf16, and 128 additions of 2^-24 of a sum of
+    # sizes below 14
+    assert np.abs(f64(st[-3:]) - end).max() <= 1e-5
+    assert np.abs(f64(o[-3:]) - want).max() <= U * np.abs(want).max() + 1e-4
