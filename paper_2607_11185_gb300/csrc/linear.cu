@@ -891,6 +891,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             __syncwarp();
             if (state) {
+              // (of a head that forgets fast K is weighted, and V may still be on its way)
+              if (fast) ok = ok && mbar_wait(&bars->t_full[vs], ((2 * ki + 1) / C::NT) & 1);
               ok = ok && mbar_wait(&bars->wt_full[ki & 3], (ki >> 2) & 1);
               if (us++ > 0) ok = ok && mbar_wait(&bars->u_free, us & 1);
               tc_fence_after();

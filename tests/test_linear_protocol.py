@@ -21,6 +21,10 @@ class Cta:
         if self.parts[bar] % of == 0:
             self.done[bar] = self.done.get(bar, 0) + 1
 
+    def there(self, bar, phases):
+        """What an MMA reads has arrived, whichever wait it relied on."""
+        assert self.done.get(bar, 0) >= phases, (bar, phases, self.pieces)
+
     def run(self, rng, starved):
         """None, or what each role waits for when none can go on.  A wait that the parity misleads raises."""
         roles, want = self.roles(), {}
@@ -64,6 +68,7 @@ class Out(Cta):
         q = t = 0
         for _, _, h in self.items:
             for tile in ("k", "q", "v") if h == 0 else ("q",):
+                yield "nothing", 0      # loads arrive one by one
                 if tile == "q":
                     if q >= self.nq:
                         yield ("q_empty", q % self.nq), q // self.nq
@@ -89,15 +94,21 @@ class Out(Cta):
             yield ("q_full", it % self.nq), it // self.nq + 1
             if it >= self.np:
                 yield ("o_full", (it - self.np) & 1), (it - self.np) // 2 + 1
+            self.there(*self.tile(2 * ki))
+            self.there(("q_full", it % self.nq), it // self.nq + 1)
             self.arrive(("s_full", it & 1))
             self.arrive(("q_empty", it % self.nq), 2)
             if fast and weigh and last:
                 self.arrive("k_done")
             if weigh and h == (self.group - 1 if fast or self.group == 1 else 1):
+                if fast:
+                    yield self.tile(2 * ki + 1)
                 yield ("wt_full", ki & 3), ki // 4 + 1
                 if us > 0:
                     yield "u_free", us
                 us += 1
+                self.there(*self.tile(2 * ki))
+                self.there(*self.tile(2 * ki + 1))
                 self.arrive("u_full")
                 self.arrive(("t_empty", vs), 2)
             if last:
@@ -114,6 +125,7 @@ class Out(Cta):
             if it >= 2:
                 yield ("o_free", it & 1), (it - 2) // 2 + 1
             yield ("q_full", it % self.nq), it // self.nq + 1
+            self.there("s_ready", it // self.group + 1)
             self.arrive(("q_empty", it % self.nq), 2)
             if self.pieces[p][1]:
                 self.arrive(("a_full", it & 1))
@@ -129,6 +141,9 @@ class Out(Cta):
             if h == 0 and not (fast and n < chunks - 1):
                 yield ("wt_full", ki & 3), ki // 4 + 1
             yield ("p_full", it & 1), it // 2 + 1
+            self.there(*self.tile(2 * ki + 1))
+            if not fast:
+                self.there(("wt_full", ki & 3), ki // 4 + 1)
             self.arrive(("o_full", it & 1))
             if h == self.group - 1:
                 self.arrive(("t_empty", (2 * ki + 1) % self.nt), 2)
@@ -191,11 +206,13 @@ class Back(Cta):
 
     def load(self):
         for it, (_, _, h) in enumerate(self.items):
+            yield "nothing", 0
             if it >= self.nq:
                 yield ("q_empty", it % self.nq), it // self.nq
             self.arrive(("q_full", it % self.nq))
             c = it // self.group
             for x in range(2) if h == 0 else ():
+                yield "nothing", 0
                 if c >= self.nkv:
                     yield ("k_empty", x, c % self.nkv), c // self.nkv
                 self.arrive(("k_full", x, c % self.nkv))
@@ -210,6 +227,8 @@ class Back(Cta):
                     yield ("q_full", it % self.nq), it // self.nq + 1
                 if h == 0:
                     yield ("k_full", x, c % self.nkv), c // self.nkv + 1
+            self.there(("q_full", it % self.nq), it // self.nq + 1)
+            self.there(("k_full", x, c % self.nkv), c // self.nkv + 1)
             self.arrive(("s_full", x))
             if self.nkv == 1 and s == self.ns - 1 and h == self.group - 1:
                 self.arrive(("k_empty", x, 0))
@@ -227,6 +246,7 @@ class Back(Cta):
                     self.arrive(("a_full", x))
                 self.arrive("s_read", 2)
             yield ("p_full", x), t + 1
+            self.there(("q_full", it % self.nq), it // self.nq + 1)
             if item:
                 self.arrive(("q_empty", it % self.nq), 3)
                 if fast and n < chunks - 1:
@@ -252,6 +272,7 @@ class Back(Cta):
                 if us > 0:
                     yield "u_free", us
                 us += 1
+            self.there(("q_full", it % self.nq), it // self.nq + 1)
             if weigh and h == self.group - 1:
                 self.arrive("u_full")
             self.arrive(("q_empty", it % self.nq), 3)
@@ -302,6 +323,18 @@ def test_no_schedule_deadlocks_or_misleads_a_wait(kind, group, d):
         for starved in (*kind(d, group, pieces).roles(), None):
             stuck = kind(d, group, pieces).run(rng, starved)
             assert stuck is None, (starved, pieces, stuck)
+
+
+def test_the_simulation_sees_a_tile_that_is_not_there():
+    class Early(Out):
+        def scores(self):   # K^T V of a head that forgets fast without waiting for V
+            for bar, phases in super().scores():
+                if not (bar[0] == "t_full" and bar[1] % 2 == 1):
+                    yield bar, phases
+
+    with pytest.raises(AssertionError):
+        for seed in range(40):
+            Early(64, 1, [(3, True, False), (2, True, True)]).run(random.Random(seed), "load")
 
 
 def test_the_simulation_sees_a_wait_two_phases_behind():
