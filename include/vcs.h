@@ -590,11 +590,11 @@ vcs_status vcs_group_advantage(const float* rewards, int64_t num_groups, int32_t
  * the copy of a state that the chunk's queries read; state_out is not rounded.
  * A weight of 2^-150 and less is 0.  Of heads whose log2 decay lies between -1
  * and 0 weights of up to 2^64 are taken and given back, so that sums beyond
- * 2^63 overflow.  An input that is not finite may reach the results of its
- * whole chunk, earlier tokens' too, and of all that read the chunk's state,
- * but no other segment.  The same inputs give the same bits; o may differ in
- * its roundings between calls with and without state_out where a segment has
- * more than 2,048 tokens.
+ * 2^63 overflow and weighted values below 2^-126 are lost.  An input that is
+ * not finite may reach the results of its whole chunk, earlier tokens' too,
+ * and of all that read the chunk's state, but no other segment.  The same
+ * inputs give the same bits; o may differ in its roundings between calls with
+ * and without state_out where a segment has more than 2,048 tokens.
  * Return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
  * bytes) pointers or overlapping outputs; VCS_ERR_UNSUPPORTED for d other
  * than 64 and 128, hq not a multiple of hkv or more than 65,535 heads;

@@ -11,6 +11,11 @@
 //   S'  = lam^n S + sum_j lam^(n-1-j) k_j v_j^T
 // four 128-wide products a chunk on the tensor pipe.
 //
+// Operands of the tensor pipe are bf16: the inputs as they are, the products between a chunk's tokens, the factor that the
+// decay weighs, and the copy of the state that a chunk's queries read.  Two such roundings and the result's own leave 0.0029
+// of a result's norm where its own alone leaves 0.0017; a second bf16 term of each would take as many products and tiles
+// again, for which D = 128 has no shared memory.  The state itself, all sums and the states that are results are fp32.
+//
 // A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among
 // the CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.
 // linear_states adds up the keys and values before every cut, as far back as the decay leaves anything in fp32, in
