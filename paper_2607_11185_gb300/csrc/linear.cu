@@ -25,7 +25,7 @@
 // us, the parts 480 with what joins them.)
 //
 // One rollout as above, us: the outputs 940 (6.06 GB, 6.45 TB/s), the states at the cuts 74 for K and V, 283 for a
-// group's Q and dO (about 6 TB/s of what the decays leave of them) and 16 to join them, dK and dV 1,545.
+// group's Q and dO (about 6 TB/s of what the decays leave of them) and 16 to join them, dK and dV 1,472.
 
 #include <cfloat>
 #include <cstdint>
@@ -1397,6 +1397,7 @@ struct BckBars {
   uint64_t s_ready, s_read;         // the state that the chunk's keys read is in shared memory, and has been read
   uint32_t tmem_base;
   int32_t abort;
+  int32_t steps;           // of dV whose K Q^T is there
 };
 static_assert(sizeof(BckBars) <= 512, "barrier space");
 
@@ -1406,7 +1407,7 @@ static_assert(sizeof(BckBars) <= 512, "barrier space");
 //   dk_j = scale lam^(m-j) [ v_j (lam^(n-m) R)^T + sum_{i >= j} (v_j . do_i) w_i ]
 //   R'   = lam^n R + lam^m sum_i w_i do_i^T
 // with one load of q and do and one state for both.  (A pass each loads them twice and has six products an item, not
-// five: 2,166 us over one rollout of 246,616 tokens at 40 / 8 heads of 128, this 1,545.)  Both factors are at most
+// five: 2,166 us over one rollout of 246,616 tokens at 40 / 8 heads of 128, this 1,472.)  Both factors are at most
 // 2^64 (kSlow); for a head that forgets faster both P have the exact powers, the rows of the products with R are
 // scaled in TMEM, and Q is weighted when they have read it.
 //
@@ -1414,7 +1415,7 @@ static_assert(sizeof(BckBars) <= 512, "barrier space");
 // in order: dV's  P dO, K Q^T of the next step;  dK's  P Q, V dO^T of the next step;  the state's  Q^T dO of an item.
 // A chunk's products with R come in its second item (of one, the first): R has had an item's time.  One warp for all
 // is held up by its waits and commits: 1,940 us of the rollout above.  What bounds it now is the chain of a step, a
-// product's P into TMEM and back: 2,500 cycles, of which the MMAs of both chains and the state take 1,536 and memory
+// product's P into TMEM and back: 2,400 cycles, of which the MMAs of both chains and the state take 1,536 and memory
 // 1,690.  (At D = 64 a second buffer of steps does not shorten it: 2,600 cycles an item of 1,408 with one or two.)
 //   warp 0  loads;  warps 1, 3  MMAs of dV and of dK;  warp 2  TMEM, MMAs of the state
 //   warps 4-7    P of K Q^T, dV;  warps 8-11  P of V dO^T, dK  (a thread a key)
@@ -1460,6 +1461,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars->s_ready, 128);
     mbar_init(&bars->s_read, 2);
     bars->abort = 0;
+    bars->steps = 0;
     fence_mbar_init();
   }
   if (warp == 2) {
@@ -1558,6 +1560,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = ok && mbar_wait(&bars->wt_full[nit % C::NQ], (nit / C::NQ) & 1);
           if (w.l2 < kSlow) ok = ok && mbar_wait(&bars->q_full[nit % C::NQ], (nit / C::NQ) & 1);
           if (nh == 0) ok = ok && mbar_wait(&k_full[nck % C::NKV], (nck / C::NKV) & 1);
+          // Both chains wait for the same Q and dO.  In step they want the pipe at once and leave it idle at once, so dK's
+          // begins an item when dV's first product is there, or 500 cycles after (300 to 800 are as good, 1,500 half as
+          // good): 1,570 -> 1,472 us of one rollout at 40 / 8 heads of 128.
+          if (x == 1) {
+            const long long t0 = clock64();
+            while (*reinterpret_cast<volatile int32_t*>(&bars->steps) <= (int)t && clock64() - t0 < 500) {
+            }
+          }
         }
         tc_fence_after();
         if (elect_one() && ok) {
@@ -1687,6 +1697,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             go = false;
             break;
           }
+          if (threadIdx.x == 128) *reinterpret_cast<volatile int32_t*>(&bars->steps) = (int)t + 1;
           tc_fence_after();
           // P goes over columns that have been read.  Loops are not unrolled: see linear_out.
 #pragma unroll 1
