@@ -654,7 +654,8 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
  *               word: VCS_ERR_DEVICE_CHECK for an id outside [-1, vocab) (read
  *               as -1) or a list outside [0, lists) (read as empty),
  *               VCS_ERR_DEVICE_TIMEOUT
- * Sums and statistics are fp32 and wider; the same inputs give the same bits
+ * Sums and statistics are fp32 and wider (a row's ln sum exp is off by at most
+ * 2^-17); the same inputs give the same bits
  * (with and without dlogits, or in another number of rows, the order of a
  * row's sums may be another one).
  * Returns VCS_ERR_INVALID_ARG for negative counts, vocab or top of 0, a null

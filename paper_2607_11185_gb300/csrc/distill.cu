@@ -87,9 +87,12 @@ __device__ __forceinline__ double ln(float x) {
 }
 
 // Largest logit and sum of exponentials, taken together in one pass.  Before the first finite logit the exponentials are
-// taken from 0: nothing but -inf sums to 0.
+// taken from 0: nothing but -inf sums to 0.  A vector's exponentials are added up by themselves and then to the sum; LONG:
+// with what that addition rounds off kept beside it (Knuth's two-sum), as a row of a million equal logits would be rounded
+// the same way a thousand times.  (A share in shared memory is 52 vectors a thread at most: there it would cost 3%.)
+template <bool LONG>
 struct Sum {
-  float m = -INFINITY, s = 0.f;
+  float m = -INFINITY, s = 0.f, rest = 0.f;
   uint64_t neg = 0ull;   // -m, twice
   __device__ __forceinline__ void join(float m2, float s2, float k) {
     const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
@@ -102,20 +105,27 @@ struct Sum {
 #pragma unroll
     for (int i = 2; i < N; i += 2) top = fmax3(top, x[i], x[i + 1]);
     if (top > m) {   // rarely, after the first elements
-      s *= ex2((m - top) * k);
+      const float f = ex2((m - top) * k);
+      s *= f;
+      if (LONG) rest *= f;
       m = top;
       neg = f2pack(-m, -m);
     }
-    uint64_t acc = f2pack(s, 0.f);
+    float a, b;
+    exp_pair(x[0], x[1], neg, kk, a, b);
+    uint64_t acc = f2pack(a, b);
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      float a, b;
+    for (int i = 2; i < N; i += 2) {
       exp_pair(x[i], x[i + 1], neg, kk, a, b);
       acc = fadd2(acc, f2pack(a, b));
     }
-    float a, b;
     f2unpack(acc, a, b);
-    s = a + b;
+    const float v = a + b, sum = s + v, back = sum - s;
+    if (LONG) rest += (s - (sum - back)) + (v - back);
+    s = sum;
+  }
+  __device__ __forceinline__ void close() {
+    if (LONG) s += rest;
   }
 };
 
@@ -305,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
     Entries<THREADS, E> en;
     en.load(a, list);
     // ---- statistics of the row
-    Sum sum;
+    Sum<true> sum;
     {
       const int64_t head = min(a.vocab, (int64_t)((kBytes - (reinterpret_cast<uintptr_t>(z) & (kBytes - 1))) / sizeof(T)) % N);
       const int64_t vecs = (a.vocab - head) / N;
@@ -334,6 +344,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
         sum.add<2>(f, k, kk);
       }
     }
+    sum.close();
     float tmax = en.check(a, z, ids);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -555,7 +566,7 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
     const int64_t my_loose = (int)threadIdx.x < row.head ? (int64_t)threadIdx.x : (int64_t)row.vecs * N + threadIdx.x;
     const float x_loose = (int)threadIdx.x < loose ? to_float(row.z[my_loose]) : -INFINITY;
     // ---- statistics
-    Sum sum;
+    Sum<false> sum;
 #pragma unroll 1
     for (int i = 0; i < kParts; ++i) {
       const int e = row.part(i + 1);

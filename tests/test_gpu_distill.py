@@ -1,7 +1,8 @@
 """GPU parity of distillation from a teacher's top logits against the fp64 oracle.
 
 Bounds.  ln sum exp is off by at most 2^-17: the exponentials by 2^-21 of themselves and 2^-23 of their argument's
-size (whose terms e^-x x stay below 0.4), the fp32 sum by 2^-24 an addition in chains of a few hundred.  A list's log
+size (whose terms e^-x x stay below 0.4), the fp32 sums by 2^-24 an addition in trees (what a thread's chain rounds off
+is kept beside it).  A list's log
 p_j and z_j / T are off by 2^-22 of their size.  So
   kl       2^-17 + 2^-21 max (|t_j| + |z_j|) / T
   dlogits  |w| / T ((2^-16 + 2^-22 x) q + (2^-16 + 2^-22 88) p) + half a step of its type of itself
@@ -289,4 +290,15 @@ def test_in_place_and_entries_twice_on_every_route(dtype, vocab, rows):
 @pytest.mark.parametrize("rows", [304, 305, 1300])
 def test_the_loss_alone_by_blocks_of_every_size(rows):
     z, ids, t, w = draw(rows, rows, 9001 if rows < 1000 else 40_007, 20, torch.bfloat16)
+    check(z, ids, t, w)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab", [(1, 1_000_003), (2, 100_000), (1, 3_000_001), (320, 9000)])
+@pytest.mark.parametrize("below", [0.0, 1.0, 3.3])
+def test_rows_of_equal_logits(dtype, rows, vocab, below):
+    # every addition of a chain rounds the same way
+    z, ids, t, w = draw(1, rows, vocab, 16, dtype)
+    z.fill_(-below)
+    z[:, vocab // 3] = 0.0
     check(z, ids, t, w)
