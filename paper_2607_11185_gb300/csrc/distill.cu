@@ -196,10 +196,10 @@ struct Entries {
       }
     }
   }
-  // Checks the ids, reads the entries' logits (before any is overwritten: dz may be z); the largest t, where a NaN counts as
+  // Checks the ids, takes the entries' logits (before any is overwritten: dz may be z); the largest t, where a NaN counts as
   // infinite, so that it goes through (fmaxf drops it, the sums do not).
-  template <class T>
-  __device__ __forceinline__ float check(const Args& a, const T* z, int32_t* ids) {
+  template <class Logit>
+  __device__ __forceinline__ float check(const Args& a, int32_t* ids, Logit logit) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -209,7 +209,7 @@ struct Entries {
         id[i] = -1;
       }
       keep[i] = 0.f;
-      if (id[i] >= 0) keep[i] = to_float(z[id[i]]);
+      if (id[i] >= 0) keep[i] = logit(id[i]);
       else t[i] = -INFINITY;
       top = fmaxf(top, t[i] != t[i] ? INFINITY : t[i]);
       if (j < ((a.top + 3) & ~3)) ids[j] = id[i];
@@ -255,13 +255,14 @@ struct Entries {
       if (ids[m] == id[i]) sum += ps[m];
     return sum;
   }
-  // The thread's terms of the divergence: ln p - log q is the difference of the two differences from the maxima and of
-  // the two logarithms.
-  __device__ __forceinline__ float divergence(const Args& a, float zmax, float logs) const {
+  // The thread's terms of the divergence, of entries that are `mine`: ln p - log q is the difference of the two differences
+  // from the maxima and of the two logarithms.
+  template <class Mine>
+  __device__ __forceinline__ float divergence(const Args& a, float zmax, float logs, Mine mine) const {
     float kl = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if (p[i] != 0.f) kl = fmaf(p[i], fmaf(t[i] - (keep[i] - zmax), a.inv_t, logs), kl);
+      if (p[i] != 0.f && mine(id[i])) kl = fmaf(p[i], fmaf(t[i] - (keep[i] - zmax), a.inv_t, logs), kl);
     return kl;
   }
 };
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
       }
     }
     sum.close();
-    float tmax = en.check(a, z, ids);
+    float tmax = en.check(a, ids, [&](int v) { return to_float(z[v]); });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       sum.join(__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), k);
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
     for (int i = 0; i < warps; ++i) psum += red_p[i];
     en.normalise(a, psum, ps);
     if (wid < warps) {
-      float kl = en.divergence(a, zmax, (float)(ln(sum.s) - ln(psum)));
+      float kl = en.divergence(a, zmax, (float)(ln(sum.s) - ln(psum)), [](int) { return true; });
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
       if (lane == 0) red_k[wid] = kl;
@@ -470,6 +471,21 @@ __device__ __forceinline__ void send(float* dst, uint64_t* bar, uint32_t rank, f
                "f"(y), "r"(on)
                : "memory");
 }
+// mbar_wait for what other CTAs of the cluster have sent.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (true) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok != 0) return true;
+    if (clock64() - t0 > kWaitLimitCycles) return false;
+  }
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(smem_u32(bar))
@@ -485,7 +501,8 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
   __shared__ double red64[W];
   __shared__ float red_m[W], red_s[W], red_t[W], red_p[W], red_k[W];
   __shared__ __align__(16) float peer[2][8][2];   // the CTAs' maxima and sums, by turns
-  __shared__ uint64_t full[kParts], met[2];
+  __shared__ __align__(16) float terms[2][8][W][2];  // the first CTA's: the others' terms of the divergence, a warp's each
+  __shared__ uint64_t full[kParts], met[2], added[2];
   __shared__ bool last;
   const float k = a.k;
   const uint64_t kk = f2pack(k, k);
@@ -494,7 +511,7 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
   const uint32_t base_s = smem_u32(held);
   if (threadIdx.x == 0) {
     for (int i = 0; i < kParts; ++i) mbar_init(&full[i], 1);
-    for (int i = 0; i < 2; ++i) mbar_init(&met[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&met[i], 1), mbar_init(&added[i], 1);
     fence_mbar_init();
   }
   __syncthreads();
@@ -538,7 +555,21 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
   int list_next = r < a.rows && a.map != nullptr ? a.map[r] : (int)r;
   fetch(r, w_next);
   uint32_t turn = 0;
-  bool ok = true;
+  bool ok = true, go = true;
+  // A row whose divergence waits for the other CTAs' terms: they have sent them before their sums of the next row, so that
+  // the first CTA takes them when it has met those.  (Waiting in the row itself: 4,096 rows of 131,072 bf16 388 us, so 381;
+  // 1,024 of fp32 188 and 185.)
+  int64_t open_row = -1;
+  float open_kl = 0.f, open_w = 0.f;
+  auto finish = [&](uint32_t t) {
+    if (open_row < 0) return;
+    ok = ok && mbar_wait_cluster(&added[t & 1], t >> 1 & 1);
+    for (int c = 1; c < size; ++c)
+      for (int i = 0; i < warps; ++i) open_kl += terms[t & 1][c][i][0];
+    a.row_kl[open_row] = open_kl;
+    a.terms[open_row] = (double)open_w * open_kl;
+    open_row = -1;
+  };
   for (; r < a.rows; r += clusters) {
     const Row row(a, r, rank, log_size);
     T* dz = static_cast<T*>(a.dz) + r * a.ldg;
@@ -593,7 +624,14 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
       const float f[2] = {x_loose, -INFINITY};
       sum.add<2>(f, k, kk);
     }
-    float tmax = en.check(a, row.z, ids);   // (all CTAs meet before the first store)
+    // An entry's logit is taken, and its gradient written, by the CTA whose element it is: in place another CTA's loads would
+    // have to be waited for.
+    const int s0 = row.head + row.v0 * N, s1 = s0 + row.n * N, tail = row.head + row.vecs * N;   // (a row held is short)
+    auto outside = [&](int v) { return rank == 0 && (v < s0 || v >= tail); };
+    auto owned = [&](int v) { return (v >= s0 && v < s1) || outside(v); };
+    float tmax = en.check(a, ids, [&](int v) {
+      return outside(v) ? to_float(row.z[v]) : v >= s0 && v < s1 ? to_float(reinterpret_cast<const T*>(held)[v - s0]) : 0.f;
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       sum.join(__shfl_xor_sync(0xffffffffu, sum.m, o), __shfl_xor_sync(0xffffffffu, sum.s, o), k);
@@ -604,9 +642,6 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
       red_s[wid] = sum.s;
       red_t[wid] = tmax;
     }
-    // the entries' logits have arrived before this CTA says that it has read the row
-#pragma unroll
-    for (int i = 0; i < E; ++i) asm volatile("" ::"f"(en.keep[i]) : "memory");
     __syncthreads();
     tmax = red_t[0];
 #pragma unroll
@@ -628,7 +663,7 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
 #pragma unroll
     for (int i = 0; i < E; ++i) place[i] = en.place(a, ids, i);
     if (size > 1) {
-      ok = ok && mbar_wait(&met[turn & 1], turn >> 1 & 1);
+      ok = ok && mbar_wait_cluster(&met[turn & 1], turn >> 1 & 1);
       float m[8], s[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -637,7 +672,10 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
       }
       join_warps<8>(m, s, k, sum.m, sum.s);
     }
-    __syncthreads();
+    // (The predicate takes the words, which so have been read when this CTA sends its next ones.)
+    go = __syncthreads_and(ok && !(sum.s < 0.f));
+    if (!go) break;
+    if (rank == 0 && threadIdx.x == 0) finish(turn - 1);
     ++turn;
     const bool empty = tmax == -INFINITY;                    // nothing to learn from
     const float zmax = sum.m == -INFINITY ? NAN : sum.m;     // nothing but -inf: no distribution
@@ -680,33 +718,44 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
     fetch(r + clusters, w_next);   // everybody is done with the share
     // the entries again, less their p, by the CTA whose elements they are: one that comes twice by its first place, with the
     // sum of both
-    const int64_t s0 = row.head + (int64_t)row.v0 * N, s1 = s0 + (int64_t)row.n * N;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      if (place[i] == 0 || empty) continue;
-      const bool outside = rank == 0 && (en.id[i] < row.head || en.id[i] >= row.head + (int64_t)row.vecs * N);
-      if (!outside && (en.id[i] < s0 || en.id[i] >= s1)) continue;
+      if (place[i] == 0 || empty || !owned(en.id[i])) continue;
       put(dz + en.id[i], c * (ex2((en.keep[i] - zmax) * k) * inv - en.mass(a, ids, ps, i, place[i])));
     }
-    // ---- the divergence, by the first CTA
-    if (rank == 0) {
-      if (wid < warps) {
-        float kl = en.divergence(a, zmax, (float)(ln(sum.s) - ln(psum)));
+    // ---- the divergence: each CTA's terms to the first, which adds them up in order (turn is the next row's by now)
+    if (wid < warps) {
+      float kl = en.divergence(a, zmax, (float)(ln(sum.s) - ln(psum)), owned);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
-        if (lane == 0) red_k[wid] = kl;
-      }
+      for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
+      if (lane == 0 && rank == 0) red_k[wid] = kl;
+      if (lane == 0 && rank > 0) send(terms[~turn & 1][rank][wid], &added[~turn & 1], 0, kl, 0.f);
+    }
+    if (rank == 0) {
       __syncthreads();
       if (threadIdx.x == 0) {
         float kl = 0.f;
         for (int i = 0; i < warps; ++i) kl += red_k[i];
-        a.row_kl[r] = empty ? 0.f : kl;
-        a.terms[r] = empty ? 0.0 : (double)w * kl;
+        const float weight = empty ? 0.f : w;   // (without entries kl is 0)
+        if (size == 1) {
+          a.row_kl[r] = kl;
+          a.terms[r] = (double)weight * kl;
+        } else {
+          mbar_arrive_expect_tx(&added[~turn & 1], 8 * (size - 1) * warps);
+          open_row = r;
+          open_kl = kl;
+          open_w = weight;
+        }
       }
     }
     __syncthreads();   // the lists are read
   }
+  if (rank == 0 && threadIdx.x == 0 && go) finish(turn - 1);
+  __syncwarp();
   if (!ok) set_status(a.status, VCS_ERR_DEVICE_TIMEOUT);
+  if (!go && threadIdx.x == 0)   // a wait has run out: the row's loads, once more with a limit
+    for (int i = 0; i < kParts; ++i) mbar_wait(&full[i], turn & 1);
+  __syncwarp();
   if (size > 1) {   // what this CTA sent has arrived before the others end, and they have its words
     cluster_arrive();
     cluster_wait();
