@@ -379,9 +379,10 @@ __global__ void __launch_bounds__(Bwd<D>::THREADS, 1)
     if (threadIdx.x == 0) set_status(status, VCS_ERR_CUDA);
     return;
   }
-  // once any CTA of this launch has given up on a wait, the rest stand down (read only by the
-  // CTAs that have a key tile)
-  if (*reinterpret_cast<volatile int32_t*>(status) == VCS_ERR_DEVICE_TIMEOUT) return;
+  // Once any CTA of this launch has given up on a wait, the rest stand down (read only by the CTAs that
+  // have a key tile).  The word may be set between two threads' reads: one of them decides for all.
+  if (__syncthreads_or(threadIdx.x == 0 && *reinterpret_cast<volatile int32_t*>(status) == VCS_ERR_DEVICE_TIMEOUT))
+    return;
   const int G = hq / hkv;
   int nsub = (L - n * C::BM + C::BQ - 1) / C::BQ;  // 128-row query tiles at or after this key tile
   int sub0 = 0, parts = 1;                         // WIN: the first of this CTA's, the CTAs of the tile

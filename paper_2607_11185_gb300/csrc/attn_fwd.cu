@@ -300,8 +300,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = *item_total;
   const int st = *reinterpret_cast<volatile int32_t*>(status);
   if ((int)blockIdx.x >= total) return;  // the grid is an upper bound of the listed units
-  // once any CTA of this launch has given up on a wait, the rest stand down
-  if (st == VCS_ERR_DEVICE_TIMEOUT) return;
+  // Once any CTA of this launch has given up on a wait, the rest stand down.  The word may be set between two threads'
+  // reads: one of them decides for all.
+  if (__syncthreads_or(threadIdx.x == 0 && st == VCS_ERR_DEVICE_TIMEOUT)) return;
   const int start = e.x, end = e.y, p = e.z, h = e.w, g = h / G;
   const int L = end - start;
   const int m0 = 2 * p, m1 = 2 * p + 1;

@@ -289,8 +289,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int total = *item_total;
   const int st = *reinterpret_cast<volatile int32_t*>(status);
   if ((int)blockIdx.x >= total) return;  // the grid is bounded by an upper bound of the listed units
-  // once any CTA of this launch has given up on a wait, those not started stand down
-  if (st == VCS_ERR_DEVICE_TIMEOUT) return;
+  // Once any CTA of this launch has given up on a wait, those not started stand down.  The word may be set between two
+  // threads' reads: one of them decides for all.
+  if (__syncthreads_or(threadIdx.x == 0 && st == VCS_ERR_DEVICE_TIMEOUT)) return;
   // The tiles' 128-byte swizzle wants 1,024-byte aligned blocks.  A kernel without static shared memory gets
   // its dynamic shared memory so aligned; there is no room to align it here.
   if (smem_u32(smem) & 1023u) {

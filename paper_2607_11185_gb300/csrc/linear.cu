@@ -782,8 +782,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
   if (w.g >= w.hi) return;
-  // once any CTA of this call has given up on a wait, those not started stand down
-  if (*reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT) return;
+  // Once any CTA of this call has given up on a wait, those not started stand down.  The word may be set between two
+  // threads' reads: one of them decides for all.
+  if (__syncthreads_or(threadIdx.x == 0 && *reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT))
+    return;
   if (smem_u32(smem) & 1023u) {  // the tiles' swizzle wants 1,024-byte aligned blocks
     if (threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
     return;
@@ -1430,7 +1432,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   BckBars* bars = reinterpret_cast<BckBars*>(smem + C::OFF_BAR);
   Walk w(p.c, blockIdx.x);
   if (w.g >= w.hi) return;
-  if (*reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT) return;
+  if (__syncthreads_or(threadIdx.x == 0 && *reinterpret_cast<volatile int32_t*>(p.c.status) == VCS_ERR_DEVICE_TIMEOUT))
+    return;
   if (smem_u32(smem) & 1023u) {
     if (threadIdx.x == 0) set_status(p.c.status, VCS_ERR_CUDA);
     return;
