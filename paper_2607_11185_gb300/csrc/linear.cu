@@ -2072,9 +2072,10 @@ Work make_work(const LinearArgs& a, void* ws) {
   return w;
 }
 
-// A tensor map of [tokens, heads, D].  Without tokens nothing is read and the pointer may be null: any address serves.
-bool encode(CUtensorMap* map, const void* base, int d, int64_t heads, const LinearArgs& a) {
-  return encode_tma_3d_bf16(map, a.num_tokens > 0 ? base : a.log_decay, d, heads, a.num_tokens, 64, 128);
+// A tensor map of [tokens, heads, D].  Without tokens nothing is read and the pointer may be null: any address that is
+// aligned as a map's has to be serves, such as the workspace's.
+bool encode(CUtensorMap* map, const void* base, int d, int64_t heads, const LinearArgs& a, const Work& w) {
+  return encode_tma_3d_bf16(map, a.num_tokens > 0 ? base : w.c.status, d, heads, a.num_tokens, 64, 128);
 }
 
 cudaError_t launch_plan(const Work& w, cudaStream_t st) {
@@ -2091,7 +2092,7 @@ cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, con
   if (!w.cut && state_out == nullptr) return cudaSuccess;
   alignas(64) CUtensorMap tk, tv;
   const int64_t heads = (int64_t)a.hkv * group;
-  if (!encode(&tk, k, D, heads, a) || !encode(&tv, v, D, heads, a)) return cudaErrorInvalidValue;
+  if (!encode(&tk, k, D, heads, a, w) || !encode(&tv, v, D, heads, a, w)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   StateArgs p;
@@ -2119,8 +2120,8 @@ cudaError_t launch_out(const Work& w, const LinearArgs& a, const void* q, const 
                        const float* state_in, float* state_out, void* out, cudaStream_t st) {
   using C = Lin<D, ONE>;
   alignas(64) CUtensorMap tq, tk, tv, to;
-  if (!encode(&tq, q, D, a.hq, a) || !encode(&tk, k, D, a.hkv, a) || !encode(&tv, v, D, a.hkv, a) ||
-      !encode(&to, out, D, a.hq, a))
+  if (!encode(&tq, q, D, a.hq, a, w) || !encode(&tk, k, D, a.hkv, a, w) || !encode(&tv, v, D, a.hkv, a, w) ||
+      !encode(&to, out, D, a.hq, a, w))
     return cudaErrorInvalidValue;
   const void* fn = reinterpret_cast<const void*>(linear_out<D, ONE>);
   static std::atomic<int> regs_cache{-1};
@@ -2154,8 +2155,8 @@ cudaError_t launch_back(const Work& w, const LinearArgs& a, const void* dout, vo
                         cudaStream_t st) {
   using C = Bck<D>;
   alignas(64) CUtensorMap tq, td, tk, tv;
-  if (!encode(&tq, a.q, D, a.hq, a) || !encode(&td, dout, D, a.hq, a) || !encode(&tk, a.k, D, a.hkv, a) ||
-      !encode(&tv, a.v, D, a.hkv, a))
+  if (!encode(&tq, a.q, D, a.hq, a, w) || !encode(&td, dout, D, a.hq, a, w) || !encode(&tk, a.k, D, a.hkv, a, w) ||
+      !encode(&tv, a.v, D, a.hkv, a, w))
     return cudaErrorInvalidValue;
   const void* fn = reinterpret_cast<const void*>(linear_back<D>);
   static std::atomic<int> regs_cache{-1};
