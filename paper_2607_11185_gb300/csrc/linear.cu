@@ -2093,7 +2093,12 @@ cudaError_t launch_states(const Work& w, const LinearArgs& a, const void* k, con
   alignas(64) CUtensorMap tk, tv;
   const int64_t heads = (int64_t)a.hkv * group;
   if (!encode(&tk, k, D, heads, a, w) || !encode(&tv, v, D, heads, a, w)) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  static std::atomic<int> regs_cache{-1};
+  bool regs_ok = false;
+  cudaError_t e = launch_regs_match(reinterpret_cast<const void*>(linear_states<D, TERMS>), kRegLaunch, &regs_cache, &regs_ok);
+  if (e != cudaSuccess) return e;
+  if (!regs_ok) return cudaErrorInvalidConfiguration;
+  e = cudaFuncSetAttribute(linear_states<D, TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   StateArgs p;
   p.c = w.c;

@@ -40,3 +40,59 @@ def test_the_reader_sees_a_thread_by_itself():
       if (__syncthreads_or(threadIdx.x == 0 && *status == VCS_ERR_DEVICE_TIMEOUT)) return; }"""
     found, one = stand_downs(src)
     assert len(found) == 2 and one == [" if (st == VCS_ERR_DEVICE_TIMEOUT) return;"]
+
+
+def functions(src):
+    """Bodies of the functions and kernels that stand at the file's outer levels, by their names."""
+    out = {}
+    for m in re.finditer(r"\n(?:template [^\n]*\n)?[a-z_][^;{}()]*?\b(\w+)\(", src):
+        at = src.find("{", m.end())
+        semi = src.find(";", m.end())
+        if at < 0 or 0 <= semi < at:
+            continue
+        depth = 0
+        for end in range(at, len(src)):
+            depth += (src[end] == "{") - (src[end] == "}")
+            if depth == 0:
+                break
+        out.setdefault(m.group(1), src[at:end])
+    return out
+
+
+def kernels_that_move_registers(src):
+    out = []
+    for m in re.finditer(r"__launch_bounds__\(.*?\)\s*\n?\s*(\w+)\(", src):
+        at = src.index("{", src.index(")", m.end()))
+        nxt = src.find("__global__", at)
+        if "setmaxnreg_inc<" in src[at:nxt if nxt > 0 else len(src)]:
+            out.append(m.group(1))
+    return out
+
+
+def launches(src):
+    """Kernels that move registers, the functions that launch them, and whether these check the build's registers."""
+    return [(k, f, "launch_regs_match(" in b) for k in kernels_that_move_registers(src) for f, b in functions(src).items()
+            if re.search(r"\b%s<[^;{}()]*>\s*<<<" % k, b)]
+
+
+@pytest.mark.parametrize("path", FILES, ids=os.path.basename)
+def test_a_kernel_that_moves_registers_is_launched_with_what_it_counts_on(path):
+    # a warpgroup that asks for more than the block was launched with would wait without a limit
+    found = launches(source(path))
+    assert {k for k, *_ in found} == set(kernels_that_move_registers(source(path)))
+    assert [x for x in found if not x[2]] == []
+
+
+def test_the_readers_of_launches_find_them():
+    moving = {k for p in FILES for k in kernels_that_move_registers(source(p))}
+    assert {"attn_fwd_kernel", "attn_window_kernel", "bwd_main", "linear_states", "linear_out", "linear_back"} <= moving
+    src = """
+__global__ void __launch_bounds__(512, 1)
+    kernel(int a) { setmaxnreg_inc<C::R>(); }
+
+template <int D>
+cudaError_t go(int x) { kernel<D><<<1, 512>>>(x); return 0; }
+template <int D>
+cudaError_t checked(int x) { launch_regs_match(fn, 128, &c, &ok); kernel<D><<<1, 512>>>(x); return 0; }
+"""
+    assert launches(src) == [("kernel", "go", False), ("kernel", "checked", True)]
