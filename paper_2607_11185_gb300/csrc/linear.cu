@@ -299,6 +299,17 @@ __device__ __forceinline__ void set_abort(int32_t* abort, int32_t* status) {
   *reinterpret_cast<volatile int32_t*>(abort) = 1;
 }
 
+// What a block has under way when it has given up on a wait ends before it.  (Otherwise somebody has waited for all of it.)
+// Of `n` loads into `slots` slots, the last ones:
+__device__ __forceinline__ void finish_loads(uint64_t* full, uint32_t n, uint32_t slots) {
+  for (uint32_t i = n > slots ? n - slots : 0; i < n; ++i) mbar_wait(&full[i % slots], (i / slots) & 1);
+}
+__device__ __forceinline__ void finish_mmas(uint64_t* idle) {   // the issuer's whole warp
+  if (elect_one()) tc_commit(idle);
+  __syncwarp();
+  mbar_wait(idle, 0);
+}
+
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
@@ -331,7 +342,7 @@ struct Sta {
   static constexpr int OFF_TERM = NKV * 2 * TILE;        // second and third term of a weighted key tile
   // at D = 64 the upper lanes of an MMA (see Lin) read a tile further than the last term
   static constexpr int OFF_BAR = OFF_TERM + (TERMS == 1 ? 0 : D == 64 ? 3 : 2) * TILE;
-  static constexpr int SMEM = OFF_BAR + 256;
+  static constexpr int SMEM = OFF_BAR + 512;
   static constexpr uint32_t IDESC_U = idesc_bf16(128, D, 1, 1);
   static constexpr int REG_CTRL = 80, REG_ROWS = 96, REG_STATE = 224;
   static_assert(REG_CTRL + 2 * REG_ROWS + REG_STATE <= 512, "setmaxnreg targets exceed the launch registers");
@@ -343,10 +354,12 @@ struct StaBars {
   uint64_t kt_full[6][2];  // the weighted keys of a slot's first and second 64 tokens are written
   uint64_t term_free[2];   // and read
   uint64_t u_full[2], u_free[2];
+  uint64_t idle;           // given up: all MMAs are complete
+  uint32_t loads;
   uint32_t tmem_base;
   int32_t abort;
 };
-static_assert(sizeof(StaBars) <= 256, "barrier space");
+static_assert(sizeof(StaBars) <= 512, "barrier space");
 
 constexpr int kStaThreads = 512;
 
@@ -380,6 +393,7 @@ __global__ void __launch_bounds__(kStaThreads, 1)
       mbar_init(&bars->u_full[i], 1);
       mbar_init(&bars->u_free[i], 4);
     }
+    mbar_init(&bars->idle, 1);
     bars->abort = 0;
     fence_mbar_init();
   }
@@ -446,6 +460,7 @@ __global__ void __launch_bounds__(kStaThreads, 1)
               }
             }
           }
+        bars->loads = it;
       }
     } else if (warp == 1) {
       // ---------------------------------------------------------- MMA issuer
@@ -602,6 +617,11 @@ __global__ void __launch_bounds__(kStaThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if (gave_up()) {
+    if (threadIdx.x == 0) finish_loads(bars->kv_full, bars->loads, C::NKV);
+    if (warp == 1) finish_mmas(&bars->idle);
+    __syncthreads();
+  }
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -716,6 +736,8 @@ struct LinBars {
   uint64_t u_free;     // and in registers
   uint64_t s_ready;    // the state that the chunk's queries read is in shared memory
   uint64_t s_read;     // and has been read
+  uint64_t idle[2];    // given up: all MMAs of an issuer are complete
+  uint32_t loads[2];   // of Q, and of K and V
   uint32_t tmem_base;
   int32_t abort;
 };
@@ -808,6 +830,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&bars->o_full[i], 1);
       mbar_init(&bars->o_free[i], 4);
       mbar_init(&bars->out_free[i], 1);
+      mbar_init(&bars->idle[i], 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(&bars->wt_full[i], 128);
     mbar_init(&bars->k_done, 1);
@@ -837,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // -------------------------------------------------------- producer
       bool go = true;
       uint32_t qi = 0, ti = 0;
-      auto load = [&](int off, uint64_t* full, uint64_t* empty, uint32_t i, uint32_t n, const CUtensorMap* tm, int head,
+      auto load = [&](int off, uint64_t* full, uint64_t* empty, uint32_t& i, uint32_t n, const CUtensorMap* tm, int head,
                       int tok) {
         const uint32_t slot = i % n;
         if (!go || (i >= n && !mbar_wait(&empty[slot], (i / n - 1) & 1)) || gave_up()) {
@@ -848,17 +871,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int kb = 0; kb < D / 64; ++kb)
           tma_load_3d(smem + off + slot * C::TILE + kb * 16384, tm, &full[slot], kb * 64, head, tok);
+        ++i;
       };
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n) {
           const int tok = w.start + (w.c0 + n) * kChunk;
           for (int h = 0; go && h < group; ++h) {
-            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_k, w.head, tok);
-            load(C::OFF_Q, bars->q_full, bars->q_empty, qi++, C::NQ, &tm_q, w.head * group + h, tok);
-            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti++, C::NT, &tm_v, w.head, tok);
+            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti, C::NT, &tm_k, w.head, tok);
+            load(C::OFF_Q, bars->q_full, bars->q_empty, qi, C::NQ, &tm_q, w.head * group + h, tok);
+            if (h == 0) load(C::OFF_T, bars->t_full, bars->t_empty, ti, C::NT, &tm_v, w.head, tok);
           }
         }
       if (!go) set_abort(&bars->abort, p.c.status);
+      bars->loads[0] = qi;
+      bars->loads[1] = ti;
     } else if (warp == 1) {
       // -------------------------------------------------------- MMAs of Q K^T and of the state
       // Every lane of an issuer runs every step, no lane's answer to a wait decides where the warp goes, and a vote an
@@ -1347,6 +1373,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if (gave_up()) {
+    if (threadIdx.x == 0) {
+      finish_loads(bars->q_full, bars->loads[0], C::NQ);
+      finish_loads(bars->t_full, bars->loads[1], C::NT);
+    }
+    if (warp == 1 || warp == 3) finish_mmas(&bars->idle[warp >> 1]);
+    __syncthreads();
+  }
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
@@ -1397,6 +1431,8 @@ struct BckBars {
   uint64_t o_full[2], o_free[2];    // a chunk's sum is complete, and in registers
   uint64_t u_full, u_free;          // the chunk's Q^T dO, and in registers
   uint64_t s_ready, s_read;         // the state that the chunk's keys read is in shared memory, and has been read
+  uint64_t idle[3];                 // given up: all MMAs of an issuer are complete
+  uint32_t loads[3];                // of Q and dO, of K and of V
   uint32_t tmem_base;
   int32_t abort;
   int32_t steps;           // of dV whose K Q^T is there
@@ -1463,6 +1499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars->u_free, 4);
     mbar_init(&bars->s_ready, 128);
     mbar_init(&bars->s_read, 2);
+    for (int i = 0; i < 3; ++i) mbar_init(&bars->idle[i], 1);
     bars->abort = 0;
     bars->steps = 0;
     fence_mbar_init();
@@ -1482,7 +1519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0) {
       // -------------------------------------------------------- loads
       bool go = lane == 0;
-      uint32_t it = 0, ck = 0;
+      uint32_t it = 0, ck = 0, loads[2] = {0, 0};   // of K and of V
       while (go && w.next())
         for (int n = 0; go && n < w.c1 - w.c0; ++n, ++ck) {
           const int tok = w.start + (w.c1 - 1 - n) * kChunk;
@@ -1503,10 +1540,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!go) break;
               mbar_arrive_expect_tx(&bars->k_full[x][kv], C::TILE);
               load((x ? C::OFF_V : C::OFF_K) + kv * C::TILE, x ? &tm_v : &tm_k, &bars->k_full[x][kv], w.head);
+              ++loads[x];
             }
           }
         }
-      if (lane == 0 && !go) set_abort(&bars->abort, p.c.status);
+      if (lane == 0) {
+        if (!go) set_abort(&bars->abort, p.c.status);
+        bars->loads[0] = it;
+        bars->loads[1] = loads[0];
+        bars->loads[2] = loads[1];
+      }
     } else if (warp == 2) {
       // -------------------------------------------------------- MMAs of the state (see linear_out for the issuers' form)
       const uint64_t qt = smem_desc(sbase + C::OFF_Q, 16384, 1024);
@@ -1928,6 +1971,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if (gave_up()) {
+    if (threadIdx.x == 0) {
+      finish_loads(bars->q_full, bars->loads[0], C::NQ);
+      for (int x = 0; x < 2; ++x) finish_loads(bars->k_full[x], bars->loads[1 + x], C::NKV);
+    }
+    if (warp > 0 && warp < 4) finish_mmas(&bars->idle[warp - 1]);
+    __syncthreads();
+  }
   if (warp == 2) {
     __syncwarp();
     tc_fence_after();

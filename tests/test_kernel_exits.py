@@ -96,3 +96,25 @@ template <int D>
 cudaError_t checked(int x) { launch_regs_match(fn, 128, &c, &ok); kernel<D><<<1, 512>>>(x); return 0; }
 """
     assert launches(src) == [("kernel", "go", False), ("kernel", "checked", True)]
+
+
+def left_open(src):
+    """Kernels that may end with loads or MMAs under way where a wait has run out: (kernel, barriers of loads, MMAs end)."""
+    out = []
+    for k in kernels_that_move_registers(src):
+        at = re.search(r"__launch_bounds__\(.*?\)\s*\n?\s*%s\(" % k, src).start()
+        nxt = src.find("__global__", at)
+        b = src[at:nxt if nxt > 0 else len(src)]
+        end = re.search(r"__syncthreads\(\);\s*if \(gave_up\(\)\) \{(.*)\n  \}\n  if \(warp == \d\) \{", b, re.S)
+        end = end.group(1) if end else ""
+        filled = set(re.findall(r"mbar_arrive_expect_tx\(&bars->(\w+)", b))
+        filled |= set(re.findall(r"load\(\w+::\w+, bars->(\w+),", b))           # through a function of the kernel
+        waited = set(re.findall(r"finish_loads\(bars->(\w+)", end))
+        out.append((k, filled - waited, "finish_mmas(" in end))
+    return [x for x in out if x[1] or not x[2]]
+
+
+def test_what_a_block_has_under_way_ends_before_it():
+    # where a wait has run out nobody else waits for it, and it would write into the next block's shared memory
+    with open(os.path.join(CSRC, "linear.cu")) as f:
+        assert left_open(f.read()) == []
