@@ -26,3 +26,48 @@ def test_no_tokens_with_the_decays_of_one_layer(d, at):
     assert not vcs.linear_attn_fwd(q, k, k, g, cu, with_state=True)[1].any()
     for x in vcs.linear_attn_bwd(q, k, k, q, g, cu):
         assert x.numel() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("decay", [-0.3, -1.1, -0.01])
+def test_states_hold_the_bits_of_a_weighted_key(d, decay):
+    # A segment whose first token alone has a key: its state is one product, e^(decay (n - 1)) k v.  Errors of it, relative:
+    #   the weight's argument  |decay| (n - 1) (2^-25 + 2^-24 of log2's factor and product, 2^-24 of their product)
+    #   exp2f                  2^-22 (2 ulp)
+    #   times the key          2^-24, of which three bf16 terms leave 2^-27
+    #   three accumulations    2 2^-23 (the tensor pipe may cut off)
+    # in all below 2^-20 + |decay| (n - 1) 2^-22.  Two terms would leave 2^-18, and 2^-19 on average.
+    vcs = _vcs()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(d)
+    lens = list(range(2, 17)) + [100, 129, 300]
+    cu = torch.tensor([0] + lens, device="cuda").cumsum(0).to(torch.int32)
+    g = decays(decay, decay * 0.77)
+    k = torch.zeros(sum(lens), 2, d, device="cuda")
+    k[cu[:-1].long()] = torch.randn(len(lens), 2, d, generator=gen, device="cuda")
+    k = k.to(torch.bfloat16)
+    v = torch.randn(sum(lens), 2, d, generator=gen, device="cuda").to(torch.bfloat16)
+    q = torch.zeros(sum(lens), 2, d, dtype=torch.bfloat16, device="cuda")
+    state = vcs.linear_attn_fwd(q, k, v, g, cu, with_state=True)[1].double()
+    first = cu[:-1].long()
+    gap = torch.tensor(lens, device="cuda").double() - 1
+    want = torch.exp(g.double()[None] * gap[:, None])[..., None, None] * k[first].double()[..., None] * v[first].double()[:, :, None]
+    bound = (2.0 ** -20 + g.double().abs()[None] * gap[:, None] * 2.0 ** -22)[..., None, None] * want.abs() + 2.0 ** -126
+    over = (state - want).abs() - bound
+    assert over.max() <= 0, ((state - want).abs() / want.abs().clamp(min=1e-30)).max()
+
+
+def test_states_of_short_segments_in_norm():
+    # the terms as above, added up: their errors are of either sign, their sizes above the sum's by no more than 10 here
+    vcs = _vcs()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(0)
+    lens = [3, 16, 40, 128, 7]
+    cu = torch.tensor([0] + lens, device="cuda").cumsum(0).to(torch.int32)
+    g = decays(-0.3, -0.02)
+    q, k, v = (torch.randn(sum(lens), 2, 128, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(3))
+    state = vcs.linear_attn_fwd(q, k, v, g, cu, with_state=True)[1].double()
+    for s, (b, n) in enumerate(zip(cu.tolist(), lens)):
+        w = torch.exp(g.double()[None] * torch.arange(n - 1, -1, -1, device="cuda").double()[:, None])
+        want = torch.einsum("jha,jhb->hab", k[b:b + n].double() * w[..., None], v[b:b + n].double())
+        assert (state[s] - want).norm() <= 2.0 ** -20 * want.norm(), s
