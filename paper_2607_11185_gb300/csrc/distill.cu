@@ -7,6 +7,7 @@
 #include <cfloat>
 #include <cstdint>
 
+#include "cluster_counts.h"
 #include "internal.h"
 #include "sm100.cuh"
 
@@ -791,17 +792,17 @@ cudaError_t launch_held(const Args& a, int log_size, size_t share, cudaStream_t 
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   // As many clusters as run at a time: the SMs of a part of the chip are no multiple of a cluster, and two clusters that
-  // started when the others were done took as long again.  The answer for a share is kept: asking takes microseconds.
-  static std::atomic<uint64_t> known[4];   // share, then clusters
-  uint64_t last = known[log_size].load(std::memory_order_relaxed);
-  if (last >> 32 != (uint64_t)share) {
-    int n = 0;
+  // started when the others were done took as long again.  The answer is kept: asking takes microseconds.
+  static ClusterCounts known[4];
+  int device = 0;
+  if (e = cudaGetDevice(&device); e != cudaSuccess) return e;
+  int n = known[log_size].find(device, (uint32_t)share);
+  if (n == 0) {
     if (e = cudaOccupancyMaxActiveClusters(&n, distill_held<T, E>, &cfg); e != cudaSuccess) return e;
     if (n < 1) return cudaErrorInvalidConfiguration;
-    last = (uint64_t)share << 32 | (uint32_t)n;
-    known[log_size].store(last, std::memory_order_relaxed);
+    known[log_size].keep(device, (uint32_t)share, n);
   }
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>((int64_t)(last & 0xffffffffu), a.rows) << log_size);
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(n, a.rows) << log_size);
   return cudaLaunchKernelEx(&cfg, distill_held<T, E>, a, log_size);
 }
 
