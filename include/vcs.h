@@ -596,9 +596,10 @@ vcs_status vcs_group_advantage(const float* rewards, int64_t num_groups, int32_t
  * inputs give the same bits; o may differ in its roundings between calls with
  * and without state_out where a segment has more than 2,048 tokens.
  * Return VCS_ERR_INVALID_ARG for negative counts, null or misaligned (16
- * bytes) pointers or overlapping outputs; VCS_ERR_UNSUPPORTED for d other
- * than 64 and 128, hq not a multiple of hkv or more than 65,535 heads;
- * VCS_ERR_OVERFLOW for more than INT32_MAX - 256 tokens; VCS_ERR_WORKSPACE.
+ * bytes; log_decay, cu_seqlens and dev_status 4) pointers, or outputs that
+ * overlap each other or an input; VCS_ERR_UNSUPPORTED for d other than 64 and
+ * 128, hq not a multiple of hkv or more than 65,535 heads; VCS_ERR_OVERFLOW
+ * for more than INT32_MAX - 256 tokens; VCS_ERR_WORKSPACE.
  * ------------------------------------------------------------------------ */
 size_t vcs_linear_attn_fwd_workspace_size(int32_t num_segments, int64_t num_tokens, int32_t hq, int32_t hkv,
                                           int32_t d);

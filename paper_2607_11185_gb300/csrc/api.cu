@@ -19,6 +19,7 @@ namespace vcs {
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
 
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
@@ -59,11 +60,17 @@ bool overlap(const Span& a, const Span& b) {
   return a.p != nullptr && b.p != nullptr && x < y + b.bytes && y < x + a.bytes;
 }
 
-// Null and alignment of every span that holds anything, and that no output overlaps another or an input.
-template <int I, int O>
-bool spans_ok(const Span (&in)[I], const Span (&out)[O]) {
+// Null and alignment of every span that holds anything (`words` 32-bit values, read one by one), and that no output
+// overlaps another or what is read.
+template <int I, int W, int O>
+bool spans_ok(const Span (&in)[I], const Span (&words)[W], const Span (&out)[O]) {
   for (const Span& s : in)
     if (s.bytes > 0 && (s.p == nullptr || !aligned16(s.p))) return false;
+  for (const Span& s : words) {
+    if (s.bytes > 0 && (s.p == nullptr || !aligned4(s.p))) return false;
+    for (const Span& o : out)
+      if (overlap(o, s)) return false;
+  }
   for (int i = 0; i < O; ++i) {
     if (out[i].bytes > 0 && (out[i].p == nullptr || !aligned16(out[i].p))) return false;
     for (const Span& s : in)
@@ -485,8 +492,9 @@ vcs_status vcs_linear_attn_fwd(const void* q, const void* k, const void* v, cons
   const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
   const uint64_t ns = (uint64_t)num_segments * hkv * d * d * 4;
   const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {state_in, state_in == nullptr ? 0 : ns}};
+  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0}};
   const Span out[] = {{o, nq}, {state_out, state_out == nullptr ? 0 : ns}};
-  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (!spans_ok(in, words, out)) return VCS_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < linear_fwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
       (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
     return VCS_ERR_WORKSPACE;
@@ -511,8 +519,9 @@ vcs_status vcs_linear_attn_bwd(const void* q, const void* k, const void* v, cons
   if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
   const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
   const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {dout, nq}};
+  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0}};
   const Span out[] = {{dq, nq}, {dk, nk}, {dv, nk}};
-  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (!spans_ok(in, words, out)) return VCS_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < linear_bwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
       (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)
     return VCS_ERR_WORKSPACE;
@@ -529,8 +538,9 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
   if (const vcs_status s = check_linear(a); s != VCS_OK) return s;
   const uint64_t nq = (uint64_t)num_seqs * hq * d * 2, nk = (uint64_t)num_seqs * hkv * d * 2;
   const Span in[] = {{q, nq}, {k, nk}, {v, nk}};
+  const Span words[] = {{log_decay, (uint64_t)hkv * 4}};
   const Span out[] = {{states, (uint64_t)num_seqs * hkv * d * d * 4}, {o, nq}};
-  if (!spans_ok(in, out)) return VCS_ERR_INVALID_ARG;
+  if (!spans_ok(in, words, out) || !aligned4(dev_status)) return VCS_ERR_INVALID_ARG;
   if (num_seqs == 0) return VCS_OK;
   if (launch_linear_step(a, states, o, dev_status, as_stream(stream)) != cudaSuccess) return VCS_ERR_CUDA;
   return VCS_OK;

@@ -1,0 +1,34 @@
+"""Linear attention and distillation on the host (CPU only): calls that would read or write what they must not."""
+import pytest
+
+from tests.test_linear_host import bwd, distill, far, fwd, step
+
+
+@pytest.fixture(scope="module")
+def vcs():
+    from paper_2607_11185_gb300 import vcs as v
+    return v
+
+
+def test_outputs_over_decays_and_bounds(vcs):
+    row = 10 * 64 * 2                       # a key/value row tensor of 10 tokens; the queries' twice that
+    for kw in (dict(o=far(3)), dict(o=far(3) - 2 * row + 16), dict(g=far(5) + 2 * row - 4), dict(so=far(3)),
+               dict(o=far(4)), dict(o=far(4) - 2 * row + 16), dict(cu=far(5) + 2 * row - 8), dict(so=far(4)),
+               dict(so=far(9), g=far(9) + 64 * 64 * 4 - 4)):
+        assert fwd(vcs, **kw) == 1, kw
+    for x, size in (("dq", 2 * row), ("dk", row), ("dv", row)):
+        at = dict(dq=far(5), dk=far(7), dv=far(8))[x]
+        for kw in (dict(g=at), dict(g=at + size - 4), dict(cu=at), dict(cu=at + size - 8), dict(cu=at - 4)):
+            assert bwd(vcs, **kw) == 1, (x, kw)
+    for kw in (dict(so=far(3)), dict(o=far(3)), dict(g=far(5) + 2 * row - 4), dict(g=far(4) + 10 * 64 * 64 * 4 - 4)):
+        assert step(vcs, **kw) == 1, kw
+
+
+def test_scalars_that_are_not_aligned_to_themselves(vcs):
+    for f in (fwd, bwd, step):
+        for off in (1, 2, 3):
+            assert f(vcs, g=far(3) + off) == 1
+    for f in (fwd, bwd):
+        for off in (1, 2, 3):
+            assert f(vcs, cu=far(4) + off) == 1
+    assert step(vcs, w=far(7) + 2) == 1
