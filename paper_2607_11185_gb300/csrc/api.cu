@@ -57,7 +57,7 @@ struct Span {
 
 bool overlap(const Span& a, const Span& b) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p != nullptr && b.p != nullptr && x < y + b.bytes && y < x + a.bytes;
+  return a.bytes > 0 && b.bytes > 0 && a.p != nullptr && b.p != nullptr && x < y + b.bytes && y < x + a.bytes;
 }
 
 // Null and alignment of every span that holds anything (`words` 32-bit values, read one by one), and that no output

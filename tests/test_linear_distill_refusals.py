@@ -32,3 +32,9 @@ def test_scalars_that_are_not_aligned_to_themselves(vcs):
         for off in (1, 2, 3):
             assert f(vcs, cu=far(4) + off) == 1
     assert step(vcs, w=far(7) + 2) == 1
+
+
+def test_a_view_of_no_tokens_overlaps_nothing(vcs):
+    # its address lies in another buffer's span: the refusal that comes next shows that the spans passed
+    assert fwd(vcs, nt=0, q=None, k=None, v=None, si=far(9), so=far(10), o=far(9) + 64, ws=None) == 8
+    assert fwd(vcs, nt=0, q=None, k=None, v=None, si=far(9), so=far(10), o=far(10) + 64, ws=None) == 8
