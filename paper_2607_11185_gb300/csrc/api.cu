@@ -492,7 +492,8 @@ vcs_status vcs_linear_attn_fwd(const void* q, const void* k, const void* v, cons
   const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
   const uint64_t ns = (uint64_t)num_segments * hkv * d * d * 4;
   const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {state_in, state_in == nullptr ? 0 : ns}};
-  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0}};
+  const uint64_t nb = num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0;
+  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, nb}};
   const Span out[] = {{o, nq}, {state_out, state_out == nullptr ? 0 : ns}};
   if (!spans_ok(in, words, out)) return VCS_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < linear_fwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
@@ -519,7 +520,8 @@ vcs_status vcs_linear_attn_bwd(const void* q, const void* k, const void* v, cons
   if (num_segments > 0 && cu_seqlens == nullptr) return VCS_ERR_INVALID_ARG;
   const uint64_t nq = (uint64_t)num_tokens * hq * d * 2, nk = (uint64_t)num_tokens * hkv * d * 2;
   const Span in[] = {{q, nq}, {k, nk}, {v, nk}, {dout, nq}};
-  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0}};
+  const uint64_t nb = num_segments > 0 ? ((uint64_t)num_segments + 1) * 4 : 0;
+  const Span words[] = {{log_decay, (uint64_t)hkv * 4}, {cu_seqlens, nb}};
   const Span out[] = {{dq, nq}, {dk, nk}, {dv, nk}};
   if (!spans_ok(in, words, out)) return VCS_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < linear_bwd_ws_bytes(num_segments, num_tokens, hq, hkv, d) ||
@@ -561,8 +563,8 @@ vcs_status vcs_distill_topk(const void* logits, int32_t logits_type, int64_t row
   if (rows > INT32_MAX || lists > INT32_MAX || vocab > INT32_MAX) return VCS_ERR_OVERFLOW;
   if (logits_stride < vocab || (dlogits != nullptr && dlogits_stride < vocab)) return VCS_ERR_INVALID_ARG;
   const int64_t size = logits_type == VCS_F32 ? 4 : 2;
-  if (logits_stride > INT64_MAX / (size * (rows + 1)) || dlogits_stride > INT64_MAX / (size * (rows + 1)))
-    return VCS_ERR_OVERFLOW;
+  const int64_t most = INT64_MAX / (size * (rows + 1));
+  if (logits_stride > most || (dlogits != nullptr && dlogits_stride > most)) return VCS_ERR_OVERFLOW;
   if (!(temperature > 0.f) || !std::isfinite(temperature)) return VCS_ERR_INVALID_ARG;
   if (teacher_rows == nullptr && lists < rows) return VCS_ERR_INVALID_ARG;
   auto off = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };

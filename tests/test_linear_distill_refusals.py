@@ -38,3 +38,9 @@ def test_a_view_of_no_tokens_overlaps_nothing(vcs):
     # its address lies in another buffer's span: the refusal that comes next shows that the spans passed
     assert fwd(vcs, nt=0, q=None, k=None, v=None, si=far(9), so=far(10), o=far(9) + 64, ws=None) == 8
     assert fwd(vcs, nt=0, q=None, k=None, v=None, si=far(9), so=far(10), o=far(10) + 64, ws=None) == 8
+
+
+def test_the_gradient_s_stride_without_a_gradient(vcs):
+    # not looked at: the refusal that comes last is the workspace's
+    for ldg in (-1, 0, 99, 1 << 62, (1 << 63) - 1):
+        assert distill(vcs, g=None, ldg=ldg, ws=None) == 8
