@@ -643,7 +643,7 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
  *               a trainable segment token
  *   weights     fp32 [rows] device.  A row of weight 0 is not read: its
  *               row_kl and dlogits are 0
- *   temperature T, positive and finite
+ *   temperature T, finite and at least 1e-38
  *   loss        fp32 device, 1 value (written): a double sum, in row order
  *   row_kl      fp32 [rows] device (written); 0 of a row without entries, or
  *               none of whose entries has a finite logit

@@ -566,6 +566,8 @@ vcs_status vcs_distill_topk(const void* logits, int32_t logits_type, int64_t row
   const int64_t most = INT64_MAX / (size * (rows + 1));
   if (logits_stride > most || (dlogits != nullptr && dlogits_stride > most)) return VCS_ERR_OVERFLOW;
   if (!(temperature > 0.f) || !std::isfinite(temperature)) return VCS_ERR_INVALID_ARG;
+  // (its inverse times log2(e), which multiplies every difference of logits: 0 times infinity would not be a number)
+  if (!std::isfinite((float)(1.4426950408889634 / (double)temperature))) return VCS_ERR_INVALID_ARG;
   if (teacher_rows == nullptr && lists < rows) return VCS_ERR_INVALID_ARG;
   auto off = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
   if (rows > 0 && (logits == nullptr || weights == nullptr || row_kl == nullptr ||

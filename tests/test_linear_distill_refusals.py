@@ -44,3 +44,10 @@ def test_the_gradient_s_stride_without_a_gradient(vcs):
     # not looked at: the refusal that comes last is the workspace's
     for ldg in (-1, 0, 99, 1 << 62, (1 << 63) - 1):
         assert distill(vcs, g=None, ldg=ldg, ws=None) == 8
+
+
+def test_temperatures_without_a_finite_inverse(vcs):
+    for temp in (1e-45, 1e-40, 4e-39):
+        assert distill(vcs, temp=temp) == 1
+    for temp in (1e-38, 1e-30, 3e38):
+        assert distill(vcs, temp=temp, ws=None) == 8
