@@ -321,12 +321,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
     {
       const int64_t head = min(a.vocab, (int64_t)((kBytes - (reinterpret_cast<uintptr_t>(z) & (kBytes - 1))) / sizeof(T)) % N);
       const int64_t vecs = (a.vocab - head) / N;
-      const uint4* zv = reinterpret_cast<const uint4*>(z + head);
+      const uint4* zv = reinterpret_cast<const uint4*>(z + head);   // (plain loads: the gradient may go over them)
       int64_t v = threadIdx.x;
       for (; v + (U - 1) * THREADS < vecs; v += U * THREADS) {
         uint4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = __ldg(zv + v + u * THREADS);
+        for (int u = 0; u < U; ++u) x[u] = zv[v + u * THREADS];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float f[N];
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
       }
       for (; v < vecs; v += THREADS) {
         float f[N];
-        Vec<T>::open(__ldg(zv + v), f);
+        Vec<T>::open(zv[v], f);
         sum.add<N>(f, k, kk);
       }
       const int64_t rest = a.vocab - head - vecs * N;   // with the head, fewer than two vectors

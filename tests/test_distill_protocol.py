@@ -125,3 +125,11 @@ def test_the_simulation_sees_a_word_too_few():
         for seed in range(40):
             for starved in range(4):
                 Cluster(4, 6, buffers=1).run(random.Random(seed), starved)
+
+
+def test_logits_are_not_read_as_data_that_nobody_writes():
+    # __ldg and .nc want data that no thread writes while the kernel runs; in place the gradient goes over the logits
+    with open(os.path.join(CSRC, "distill.cu")) as f:
+        src = re.sub(r"//[^\n]*", "", f.read())
+    reads = re.findall(r"(?:__ldg|ld\.global\.nc)\(([^;]*?)\)", src)
+    assert reads and all(re.match(r"&a\.(ids|t|weights|map)\b", x) for x in reads), reads
