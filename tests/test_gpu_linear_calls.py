@@ -71,3 +71,42 @@ def test_states_of_short_segments_in_norm():
         w = torch.exp(g.double()[None] * torch.arange(n - 1, -1, -1, device="cuda").double()[:, None])
         want = torch.einsum("jha,jhb->hab", k[b:b + n].double() * w[..., None], v[b:b + n].double())
         assert (state[s] - want).norm() <= 2.0 ** -20 * want.norm(), s
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (6, 2)])
+def test_tensors_aligned_to_16_bytes_only(d, hq, hkv):
+    # rows behind a segment's last whole chunk are stored 32 bytes at a time, or 16 and 16
+    vcs = _vcs()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(d)
+    lens = [1, 127, 130, 300, 2300]
+    n, cu = sum(lens), torch.tensor([0] + lens, device="cuda").cumsum(0).to(torch.int32)
+    g = decays(-0.02, -1.3)
+    q, do = (torch.randn(n, hq, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    k, v = (torch.randn(n, hkv, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+
+    def off(x, elements):      # a copy 16 bytes behind a boundary of 32
+        room = torch.full((x.numel() + 2 * elements,), 3.0, dtype=x.dtype, device="cuda")
+        y = room[elements:elements + x.numel()].view(x.shape)
+        assert y.data_ptr() % 32 == 16
+        y.copy_(x)
+        return room, y
+
+    state = torch.randn(len(lens), hkv, d, d, generator=gen, device="cuda")
+    want = (*vcs.linear_attn_fwd(q, k, v, g, cu, state=state, with_state=True), *vcs.linear_attn_bwd(q, k, v, do, g, cu))
+    (_, q2), (_, k2), (_, v2), (_, d2), (_, s2) = off(q, 8), off(k, 8), off(v, 8), off(do, 8), off(state, 4)
+    ro, o = off(q, 8)
+    rs, out = off(state, 4)
+    grads = [off(x, 8) for x in (q, k, v)]
+    nb = max(f(len(lens), n, hq, hkv, d) for f in (vcs.vcs_linear_attn_fwd_workspace_size, vcs.vcs_linear_attn_bwd_workspace_size))
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    args = (cu, len(lens), n, hq, hkv, d, 0.0)
+    assert vcs.vcs_linear_attn_fwd(q2, k2, v2, g, *args, s2, out, o, ws, nb) == 0
+    assert int(ws[:4].view(torch.int32)) == 0
+    assert vcs.vcs_linear_attn_bwd(q2, k2, v2, d2, g, *args, *(y for _, y in grads), ws, nb) == 0
+    assert int(ws[:4].view(torch.int32)) == 0
+    for x, y in zip((o, out, *(y for _, y in grads)), want):
+        assert torch.equal(x, y)
+    for room, pad in ((ro, 8), (rs, 4), *((r, 8) for r, _ in grads)):
+        assert (room[:pad] == 3).all() and (room[-pad:] == 3).all()
