@@ -1608,8 +1608,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (nh == 0) ok = ok && mbar_wait(&k_full[nck % C::NKV], (nck / C::NKV) & 1);
           // Both chains wait for the same Q and dO.  In step they want the pipe at once and leave it idle at once, so dK's
           // begins an item when dV's first product is there, or 500 cycles after (300 to 800 are as good, 1,500 half as
-          // good): 1,570 -> 1,472 us of one rollout at 40 / 8 heads of 128.
-          if (x == 1) {
+          // good): 1,570 -> 1,472 us of one rollout at 40 / 8 heads of 128; with the forward 1,256 -> 1,198 us of two of
+          // 40,000 tokens at 16 / 16.  At D = 64, where the pipe is no bound, without: with the forward 894 -> 878 us of four
+          // of 60,000 tokens at 14 / 2, 510 -> 505 of 64 short ones at 16 / 2, 765 either way at 6 / 6.
+          if (D == 128 && x == 1) {
             const long long t0 = clock64();
             while (*reinterpret_cast<volatile int32_t*>(&bars->steps) <= (int)t && clock64() - t0 < 500) {
             }
@@ -1743,7 +1745,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             go = false;
             break;
           }
-          if (threadIdx.x == 128) *reinterpret_cast<volatile int32_t*>(&bars->steps) = (int)t + 1;
+          if (D == 128 && threadIdx.x == 128) *reinterpret_cast<volatile int32_t*>(&bars->steps) = (int)t + 1;
           tc_fence_after();
           // P goes over columns that have been read.  Loops are not unrolled: see linear_out.
 #pragma unroll 1
