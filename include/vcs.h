@@ -644,7 +644,8 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
  *   weights     fp32 [rows] device.  A row of weight 0 is not read: its
  *               row_kl and dlogits are 0
  *   temperature T, finite and at least 1e-38
- *   loss        fp32 device, 1 value (written): a double sum, in row order
+ *   loss        fp32 device, 1 value (written): a double sum, whose order
+ *               depends on the sizes alone
  *   row_kl      fp32 [rows] device (written); 0 of a row without entries, or
  *               none of whose entries has a finite logit
  *   dlogits     as logits, with dlogits_stride, or NULL; may be logits itself

@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_rows(const __
     }
     __syncthreads();   // the lists are read
   }
-  // the block that finishes last adds the rows' terms, in row order, so that the loss does not depend on scheduling
+  // the block that finishes last adds the rows' terms in an order of its threads, so that the loss does not depend on scheduling
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
@@ -761,7 +761,7 @@ __global__ void __launch_bounds__(kHeldThreads, 3) distill_held(const __grid_con
     cluster_arrive();
     cluster_wait();
   }
-  // the block that finishes last adds the rows' terms, in row order, so that the loss does not depend on scheduling
+  // the block that finishes last adds the rows' terms in an order of its threads, so that the loss does not depend on scheduling
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();

@@ -12,20 +12,23 @@
 // four 128-wide products a chunk on the tensor pipe.
 //
 // Operands of the tensor pipe are bf16: the inputs as they are, the products between a chunk's tokens, the factor that the
-// decay weighs, and the copy of the state that a chunk's queries read.  Two such roundings and the result's own leave 0.0029
-// of a result's norm where its own alone leaves 0.0017; a second bf16 term of each would take as many products and tiles
-// again, for which D = 128 has no shared memory.  The state itself, all sums and the states that are results are fp32.
+// decay weighs, and the copy of the state that a chunk's queries read.  Between a chunk's tokens two such roundings meet an
+// output, through the state two others; with its own they leave 0.0029 of a result's norm where its own alone leaves 0.0017.
+// One of each less leaves 0.0024 and was measured in two forms, over one rollout of 246,616 tokens at 40 / 8 heads of 128,
+// forward, where this takes 1,055 us, and a training step over 102,936 at 14 / 2 of 64, 441: a second bf16 term of the
+// weighted V in a tile of its own (at D = 128 in the place of the next chunk's K), 1,338 and 474; the decay's factors in P, V
+// as it is, and K weighted late with its second term over the state's copy, 1,203 and 482.  Neither helps dK and dV at
+// D = 128, where shared memory has no room.  The state itself, all sums and the states that are results are fp32.
 //
 // A "sequence" is one segment of one head.  The chunks of all sequences, one after another, are divided evenly among
 // the CTAs; a sequence that a CTA's range ends in goes on in the next one, which needs the state at the cut.
 // linear_states adds up the keys and values before every cut, as far back as the decay leaves anything in fp32, in
 // parts of equal size spread over the chip, and linear_join makes the cuts' states of them.  So a cut costs its
 // piece's keys and values read twice.  (A CTA that adds up the piece before its own cut takes as long as the head that
-// forgets slowest: the three passes of a training step over one rollout of 246,616 tokens at 40 / 8 heads of 128 955
-// us, the parts 480 with what joins them.)
+// forgets slowest: the three passes of a training step over the rollout above 955 us, the parts 480 with what joins them.)
 //
-// One rollout as above, us: the outputs 940 (6.06 GB, 6.45 TB/s), the states at the cuts 74 for K and V, 283 for a
-// group's Q and dO (about 6 TB/s of what the decays leave of them) and 16 to join them, dK and dV 1,472.
+// That rollout, us: the outputs 940 (6.06 GB, 6.45 TB/s), the states at the cuts 74 for K and V, 283 for a
+// group's Q and dO (about 6 TB/s of what the decays leave of them) and 16 to join them, dK and dV 1,465.
 
 #include <cfloat>
 #include <cstdint>
