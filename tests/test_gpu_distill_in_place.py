@@ -44,3 +44,40 @@ def test_a_cluster_whose_shares_hold_no_finite_logit(dtype):
     ids[2:] = torch.arange(24, dtype=torch.int32)
     check(z, ids, t, w)
     check(z, ids, t, w, out=z)
+
+
+@pytest.mark.parametrize("dtype,vocab,rows", [(torch.bfloat16, 20_011, 700), (torch.bfloat16, 131_072, 500), (torch.float32, 99_991, 160),
+                                              (torch.bfloat16, 50_000, 3), (torch.float32, 1_000_003, 5)])
+def test_two_calls_at_once_and_graphs_of_rows_in_clusters(dtype, vocab, rows):
+    vcs = _vcs()
+    a, b = (draw(seed, rows, vocab, 40, dtype) for seed in (1, 2))
+    want = [vcs.distill_topk(*x, temperature=0.9) for x in (a, b)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [vcs.distill_topk(*a, temperature=0.9, check=False), vcs.distill_topk(*b, temperature=0.9, stream=side, check=False),
+               vcs.distill_topk(*a, temperature=0.9, check=False)]
+        torch.cuda.synchronize()
+        for x, y in zip(got, (want[0], want[1], want[0])):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
+    graphs = []
+    for x in (a, b):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = vcs.distill_topk(*x, temperature=0.9, check=False)
+        graphs.append((graph, out))
+    for p, q in zip(a, b):       # each replay with the other's inputs
+        p_old = p.clone()
+        p.copy_(q)
+        q.copy_(p_old)
+    for _, out in graphs:
+        for y in out:
+            y.fill_(9.0)
+    for i in (0, 1, 1, 0):
+        graphs[i][0].replay()
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.current_stream())
+        graphs[1][0].replay()
+    torch.cuda.synchronize()
+    for (_, out), y in zip(graphs, want[::-1]):
+        assert all(torch.equal(p, q) for p, q in zip(out, y))
