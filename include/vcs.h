@@ -656,10 +656,12 @@ vcs_status vcs_linear_attn_step(const void* q, const void* k, const void* v, con
  *               word: VCS_ERR_DEVICE_CHECK for an id outside [-1, vocab) (read
  *               as -1) or a list outside [0, lists) (read as empty),
  *               VCS_ERR_DEVICE_TIMEOUT
- * Sums and statistics are fp32 and wider (a row's ln sum exp is off by at most
- * 2^-17); the same inputs give the same bits
- * (with and without dlogits, or in another number of rows, the order of a
- * row's sums may be another one).
+ * Sums and statistics are fp32 and wider: a row's ln sum exp is off by at most
+ * 2^-17, and its p and q by fp32's rounding beside 1, so that where student and
+ * teacher are certain of the same entry but for 2^-17, row_kl and that entry's
+ * dlogits, as small themselves, may be off by as much as they are.  The same
+ * inputs give the same bits (with and without dlogits, or in another number of
+ * rows, the order of a row's sums may be another one).
  * Returns VCS_ERR_INVALID_ARG for negative counts, vocab or top of 0, a null
  * pointer, one that is not aligned to its elements, a stride below vocab, a
  * bad temperature, lists < rows without teacher_rows, or overlap;
